@@ -256,6 +256,96 @@ GL_API int gl_compute_reduce_max(const gl_ap* in, const gl_windows* w_or_null, g
  * shape kept.  GL_F32.  in->data == out->data is allowed. */
 GL_API int gl_compute_relu(const gl_ap* in, gl_ap* out, void* stream);
 
+/* ----------------------------------------------------------------------- */
+/* Operands held in 4 bits (MX4; not in the paper)                           */
+/* ----------------------------------------------------------------------- */
+
+/* A pattern of shape S_A ++ S_C whose items (the prod(S_C) = K values of one access index) are cut into blocks of 32
+ * consecutive values.  A block is 32 E2M1 codes (sign and 0, 0.5, 1, 1.5, 2, 3, 4 or 6) and one E8M0 scale: value =
+ * code * 2^(scale - 127), scale 255 = NaN for the whole block.
+ *   data:  gl_mx4_data_bytes() bytes; one row per item of ceil(K/32)*16 bytes, two codes a byte, the even index in the
+ *          low half; codes past K are zero.
+ *   scale: gl_mx4_scale_bytes() bytes; tiles of 128 rows x 4 blocks, 512 bytes each, row tiles outermost; row r and
+ *          block b of a tile at byte (r % 32) * 16 + (r / 32) * 4 + b.
+ * Both device pointers are 16-byte aligned.  Size limits of all calls: rows * ceil(K/128)*16 < 2^31 (else
+ * GL_ERR_UNSUPPORTED); nothing else is assumed of K or of the rows. */
+typedef struct {
+  void* data;
+  void* scale;
+  int32_t ndim;
+  int32_t access_ndim;
+  int64_t shape[GL_MAX_DIMS];
+} gl_mx4;
+
+/* Bytes of the two arrays (0 on an invalid shape). */
+GL_API size_t gl_mx4_data_bytes(const gl_mx4* a);
+GL_API size_t gl_mx4_scale_bytes(const gl_mx4* a);
+
+/* Rounds `in` (GL_F32 or GL_BF16) to `out`, which carries the same shape: scale 2^(floor(log2 max|v|) - 2) of the
+ * block, not below 2^-127; values divided by it are rounded to the nearest code, ties to the even mantissa, larger
+ * values than 6 to 6.  A block that holds an Inf or a NaN becomes NaN as a whole. */
+GL_API int gl_mx4_quantize(const gl_ap* in, gl_mx4* out, void* stream);
+
+/* The values of `in` as `out` (GL_F32 or GL_BF16; both hold every one of them exactly). */
+GL_API int gl_mx4_dequantize(const gl_mx4* in, gl_ap* out, void* stream);
+
+/* compute dotProd (cartProd a0 a1) of two MX4 patterns of the same compute shape: ((m..),(k..)), ((o..),(k..)) ->
+ * ((m.., o..),()), sums in fp32, on the tensor cores' block-scaled 4-bit products.  flags: GL_EPILOGUE_RELU (NaN stays
+ * NaN), GL_OUT_BF16; `out` is GL_F32 or, with GL_OUT_BF16, GL_BF16. */
+GL_API int gl_cartesian_dot_mx4(const gl_mx4* a0, const gl_mx4* a1, gl_ap* out, uint32_t flags, void* stream);
+
+/* The same with the left operand given as GL_F32 or GL_BF16 and rounded to MX4 by the call (a dense layer: activations
+ * a0, weights a1 laid out once by gl_mx4_quantize).  The result does not depend on how many rows a0 has beyond the
+ * order of the sums.  `workspace`: gl_dense_mx4_workspace() bytes, 1024-byte aligned, scratch. */
+GL_API int gl_dense_mx4(const gl_ap* a0, const gl_mx4* a1, gl_ap* out, uint32_t flags, void* workspace,
+                        size_t workspace_bytes, void* stream);
+GL_API size_t gl_dense_mx4_workspace(const gl_ap* a0, const gl_mx4* a1);
+
+/* Pages of keys and values held in MX4, blocks along the head dimension.  A page holds `page_tokens` consecutive tokens
+ * of all kv heads: [kv_heads][page_tokens / 16] groups of 16 tokens, 17 * head_dim bytes each; the order inside a group
+ * is the library's own (gl_cache4_read gives values back).  head_dim 64, 128 or 256; page_tokens a multiple of 16. */
+typedef struct {
+  void* data;           /* gl_cache4_bytes() bytes, 16-byte aligned                                     */
+  int64_t pages;
+  int32_t kv_heads;
+  int32_t head_dim;
+  int32_t page_tokens;
+  int32_t reserved_;
+} gl_cache4;
+
+/* Where the tokens of a batch lie.  Token t of sequence b is token t % page_tokens of page
+ * page_table[b * table_width + t / page_tokens].  lengths[b] counts the tokens of sequence b, those of this call
+ * included.  Both arrays are in DEVICE memory and cannot be checked by the host: lengths are taken as
+ * 0..table_width * page_tokens, a token on a page that does not exist is not stored, reads as zeros and is not seen. */
+typedef struct {
+  const int32_t* page_table;
+  const int32_t* lengths;
+  int32_t batch;
+  int32_t table_width;
+} gl_pages;
+
+GL_API size_t gl_cache4_bytes(const gl_cache4* cache);
+
+/* Rounds k and v, ((B, T, kv_heads),(head_dim)) GL_BF16, into the cache: token i of sequence b becomes its token
+ * lengths[b] - T + i; those before token 0 (left padding of a ragged batch) are skipped.  token_pitch: elements between
+ * successive tokens of k and of v, a multiple of 8 (0: dense), so that both may be parts of one projection.  Pages that
+ * two sequences share may be read but not appended to. */
+GL_API int gl_cache4_append(const gl_cache4* cache, const gl_ap* k, const gl_ap* v, int64_t token_pitch, const gl_pages* at,
+                            void* stream);
+
+/* The values of the last T tokens of every sequence, k and v ((B, T, kv_heads),(head_dim)) dense GL_BF16; zeros where
+ * there is no such token. */
+GL_API int gl_cache4_read(const gl_cache4* cache, const gl_pages* at, gl_ap* k, gl_ap* v, void* stream);
+
+/* Attention of q, ((B, T, heads),(head_dim)) GL_BF16, over the cache: row (b, i, h) is token lengths[b] - T + i of its
+ * sequence, sees the tokens up to and including itself and reads kv head h / (heads / kv_heads):
+ *   out[b,i,h] = sum_t p_t V_t,  p = softmax_t(scale * q . K_t);  zeros for a row that sees nothing.
+ * scale > 0 and finite; token_pitch as above; out is dense, GL_F32 or, with GL_OUT_BF16 in flags, GL_BF16.
+ * Scores and softmax statistics are fp32.  `workspace`: gl_attend_cache4_workspace() bytes, 1024-byte aligned. */
+GL_API int gl_attend_cache4(const gl_ap* q, int64_t token_pitch, const gl_cache4* cache, const gl_pages* at, float scale,
+                            gl_ap* out, uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
+GL_API size_t gl_attend_cache4_workspace(const gl_ap* q, const gl_cache4* cache);
+
 /* Synchronises `stream`, then reports and clears the device status word:
  * GL_ERR_TIMEOUT if a bounded wait inside a kernel gave up since the last poll
  * (that kernel's output is then undefined), GL_ERR_CUDA on a runtime error. */

@@ -48,6 +48,36 @@ class GlWindows(ctypes.Structure):
     ]
 
 
+class GlMx4(ctypes.Structure):
+    _fields_ = [
+        ("data", ctypes.c_void_p),
+        ("scale", ctypes.c_void_p),
+        ("ndim", ctypes.c_int32),
+        ("access_ndim", ctypes.c_int32),
+        ("shape", ctypes.c_int64 * GL_MAX_DIMS),
+    ]
+
+
+class GlCache4(ctypes.Structure):
+    _fields_ = [
+        ("data", ctypes.c_void_p),
+        ("pages", ctypes.c_int64),
+        ("kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("page_tokens", ctypes.c_int32),
+        ("reserved_", ctypes.c_int32),
+    ]
+
+
+class GlPages(ctypes.Structure):
+    _fields_ = [
+        ("page_table", ctypes.c_void_p),
+        ("lengths", ctypes.c_void_p),
+        ("batch", ctypes.c_int32),
+        ("table_width", ctypes.c_int32),
+    ]
+
+
 EXPORTS = [
     "gl_shape_access", "gl_shape_windows", "gl_shape_flatten", "gl_shape_transpose", "gl_shape_pad",
     "gl_shape_cartesian_dot", "gl_shape_reduce_max", "gl_access_windows", "gl_access_flatten",
@@ -57,6 +87,9 @@ EXPORTS = [
     "gl_shape_slice", "gl_shape_concat", "gl_shape_pair", "gl_shape_squeeze", "gl_shape_reshape",
     "gl_shape_reduce_sum", "gl_access_slice", "gl_access_concat", "gl_access_pair", "gl_compute_reduce_sum",
     "gl_selftest_bounded_wait",
+    "gl_mx4_data_bytes", "gl_mx4_scale_bytes", "gl_mx4_quantize", "gl_mx4_dequantize", "gl_cartesian_dot_mx4",
+    "gl_dense_mx4", "gl_dense_mx4_workspace", "gl_cache4_bytes", "gl_cache4_append", "gl_cache4_read",
+    "gl_attend_cache4", "gl_attend_cache4_workspace",
 ]
 
 
@@ -68,6 +101,7 @@ def _load() -> ctypes.CDLL:
     lib = ctypes.CDLL(LIB_PATH)
     ap, win, vp = ctypes.POINTER(GlAp), ctypes.POINTER(GlWindows), ctypes.c_void_p
     i32p = ctypes.POINTER(ctypes.c_int32)
+    mx, ca, pg = ctypes.POINTER(GlMx4), ctypes.POINTER(GlCache4), ctypes.POINTER(GlPages)
     sig = {
         "gl_shape_access": [ap, ctypes.c_int32, ap],
         "gl_shape_windows": [ap, win, ap],
@@ -97,6 +131,13 @@ def _load() -> ctypes.CDLL:
         "gl_compute_relu": [ap, ap, vp],
         "gl_poll_device_status": [vp],
         "gl_selftest_bounded_wait": [ctypes.c_uint32, vp],
+        "gl_mx4_quantize": [ap, mx, vp],
+        "gl_mx4_dequantize": [mx, ap, vp],
+        "gl_cartesian_dot_mx4": [mx, mx, ap, ctypes.c_uint32, vp],
+        "gl_dense_mx4": [ap, mx, ap, ctypes.c_uint32, vp, ctypes.c_size_t, vp],
+        "gl_cache4_append": [ca, ap, ap, ctypes.c_int64, pg, vp],
+        "gl_cache4_read": [ca, pg, ap, ap, vp],
+        "gl_attend_cache4": [ap, ctypes.c_int64, ca, pg, ctypes.c_float, ap, ctypes.c_uint32, vp, ctypes.c_size_t, vp],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -104,6 +145,11 @@ def _load() -> ctypes.CDLL:
         fn.restype = ctypes.c_int
     lib.gl_cartesian_dot_workspace.argtypes = [ap, win, ap, ctypes.c_uint32]
     lib.gl_cartesian_dot_workspace.restype = ctypes.c_size_t
+    for name, args in {"gl_mx4_data_bytes": [mx], "gl_mx4_scale_bytes": [mx], "gl_dense_mx4_workspace": [ap, mx],
+                       "gl_cache4_bytes": [ca], "gl_attend_cache4_workspace": [ap, ca]}.items():
+        fn = getattr(lib, name)
+        fn.argtypes = args
+        fn.restype = ctypes.c_size_t
     lib.gl_strerror.argtypes = [ctypes.c_int]
     lib.gl_strerror.restype = ctypes.c_char_p
     lib.gl_version.restype = ctypes.c_int
@@ -434,6 +480,210 @@ def gl_compute_relu(a: AccessPattern, out: Optional[AccessPattern] = None, strea
     return out
 
 
+# ---- operands held in 4 bits ----
+
+@dataclass
+class Mx4:
+    """A pattern held in 4 bits: E2M1 codes (two a byte) and one E8M0 scale per 32 values of an item."""
+
+    data: torch.Tensor    # uint8, gl_mx4_data_bytes
+    scale: torch.Tensor   # uint8, gl_mx4_scale_bytes
+    dims: tuple           # S_A ++ S_C
+    access_ndim: int
+
+    @property
+    def shape(self):
+        return (self.dims[: self.access_ndim], self.dims[self.access_ndim:])
+
+
+def _mx4_struct(m: Mx4) -> GlMx4:
+    s = _mx4_meta(m.dims, m.access_ndim)
+    for t, need in ((m.data, LIB.gl_mx4_data_bytes(ctypes.byref(s))), (m.scale, LIB.gl_mx4_scale_bytes(ctypes.byref(s)))):
+        if t.dtype != torch.uint8 or not t.is_contiguous() or t.numel() < need:
+            raise ValueError("an MX4 operand of this shape wants %d contiguous bytes" % need)
+    s.data, s.scale = m.data.data_ptr(), m.scale.data_ptr()
+    return s
+
+
+def _mx4_meta(shape, access_ndim) -> GlMx4:
+    if len(shape) > GL_MAX_DIMS:
+        raise GlError(3, "too many dimensions")
+    s = GlMx4()
+    s.ndim, s.access_ndim = len(shape), access_ndim
+    for i, n in enumerate(shape):
+        s.shape[i] = int(n)
+    return s
+
+
+def mx4_empty(shape, access_ndim: int, device) -> Mx4:
+    """Storage for a pattern of this shape, contents undefined."""
+    s = _mx4_meta(shape, access_ndim)
+    nd, ns = LIB.gl_mx4_data_bytes(ctypes.byref(s)), LIB.gl_mx4_scale_bytes(ctypes.byref(s))
+    if not nd:
+        raise GlError(4, "mx4_empty")
+    return Mx4(torch.empty(nd, dtype=torch.uint8, device=device), torch.empty(ns, dtype=torch.uint8, device=device),
+               tuple(int(n) for n in shape), access_ndim)
+
+
+def gl_mx4_quantize(a: AccessPattern, out: Optional[Mx4] = None, stream=None) -> Mx4:
+    sa = _struct(a)
+    if out is None:
+        out = mx4_empty(tuple(a.tensor.shape), a.access_ndim, a.tensor.device)
+    _check(LIB.gl_mx4_quantize(ctypes.byref(sa), ctypes.byref(_mx4_struct(out)), _stream(stream)), "gl_mx4_quantize")
+    return out
+
+
+def gl_mx4_dequantize(m: Mx4, out: Optional[AccessPattern] = None, stream=None) -> AccessPattern:
+    if out is None:
+        out = AccessPattern(torch.empty(m.dims, dtype=torch.float32, device=m.data.device), m.access_ndim)
+    so = _struct(out)
+    _check(LIB.gl_mx4_dequantize(ctypes.byref(_mx4_struct(m)), ctypes.byref(so), _stream(stream)), "gl_mx4_dequantize")
+    return out
+
+
+def _product_out(access0, access1, flags, device) -> AccessPattern:
+    shape = tuple(access0) + tuple(access1)
+    dtype = torch.bfloat16 if flags & GL_OUT_BF16 else torch.float32
+    return AccessPattern(torch.empty(shape, dtype=dtype, device=device), len(shape))
+
+
+def gl_cartesian_dot_mx4(a0: Mx4, a1: Mx4, out: Optional[AccessPattern] = None, flags: int = 0, stream=None) -> AccessPattern:
+    if out is None:
+        out = _product_out(a0.shape[0], a1.shape[0], flags, a0.data.device)
+    so = _struct(out)
+    _check(LIB.gl_cartesian_dot_mx4(ctypes.byref(_mx4_struct(a0)), ctypes.byref(_mx4_struct(a1)), ctypes.byref(so), flags,
+                                    _stream(stream)), "gl_cartesian_dot_mx4")
+    return out
+
+
+def gl_dense_mx4_workspace(a0: AccessPattern, a1: Mx4) -> int:
+    return int(LIB.gl_dense_mx4_workspace(ctypes.byref(_struct(a0)), ctypes.byref(_mx4_struct(a1))))
+
+
+def _scratch(need: int, device) -> Optional[torch.Tensor]:
+    return torch.empty(need + 1024, dtype=torch.uint8, device=device) if need else None
+
+
+def gl_dense_mx4(a0: AccessPattern, a1: Mx4, out: Optional[AccessPattern] = None, flags: int = 0,
+                 workspace: Optional[torch.Tensor] = None, stream=None) -> AccessPattern:
+    if out is None:
+        out = _product_out(a0.access_shape, a1.shape[0], flags, a0.tensor.device)
+    if workspace is None:
+        workspace = _scratch(gl_dense_mx4_workspace(a0, a1), a0.tensor.device)
+    s0, so = _struct(a0), _struct(out)
+    _check(LIB.gl_dense_mx4(ctypes.byref(s0), ctypes.byref(_mx4_struct(a1)), ctypes.byref(so), flags, *_ws(workspace),
+                            _stream(stream)), "gl_dense_mx4")
+    return out
+
+
+# ---- pages of 4-bit keys and values ----
+
+@dataclass
+class Cache4:
+    """Pages of keys and values held in 4 bits; the order of the bytes is the library's own."""
+
+    data: torch.Tensor    # uint8, gl_cache4_bytes
+    pages: int
+    kv_heads: int
+    page_tokens: int
+    head_dim: int
+
+
+def _cache4_struct(c: Cache4) -> GlCache4:
+    s = GlCache4()
+    s.data, s.pages, s.kv_heads, s.head_dim, s.page_tokens = 0, c.pages, c.kv_heads, c.head_dim, c.page_tokens
+    if c.data is not None:
+        if c.data.dtype != torch.uint8 or not c.data.is_contiguous() or c.data.numel() < LIB.gl_cache4_bytes(ctypes.byref(s)):
+            raise ValueError("the cache's storage is smaller than gl_cache4_bytes, or not contiguous bytes")
+        s.data = c.data.data_ptr()
+    return s
+
+
+def cache4_empty(pages: int, kv_heads: int, page_tokens: int, head_dim: int, device) -> Cache4:
+    """Storage for `pages` pages, contents undefined (a token is readable once it has been appended)."""
+    c = Cache4(None, pages, kv_heads, page_tokens, head_dim)
+    need = LIB.gl_cache4_bytes(ctypes.byref(_cache4_struct(c)))
+    if not need:
+        raise GlError(7, "cache4_empty")
+    c.data = torch.empty(need, dtype=torch.uint8, device=device)
+    return c
+
+
+def _pages_struct(page_table: torch.Tensor, lengths: torch.Tensor) -> GlPages:
+    if page_table.dtype != torch.int32 or lengths.dtype != torch.int32 or page_table.dim() != 2 or lengths.dim() != 1:
+        raise ValueError("page_table is int32 [batch, width] and lengths int32 [batch]")
+    if not page_table.is_contiguous() or not lengths.is_contiguous() or page_table.shape[0] != lengths.shape[0]:
+        raise ValueError("page_table and lengths are contiguous and agree in the batch")
+    s = GlPages()
+    s.page_table, s.lengths = page_table.data_ptr(), lengths.data_ptr()
+    s.batch, s.table_width = page_table.shape
+    return s
+
+
+def _tokens_struct(t: torch.Tensor):
+    """[B, T, heads, head_dim] whose tokens may lie further apart than they are long (a part of a fused projection):
+    the struct and the distance in elements."""
+    b, n, h, d = t.shape
+    pitch = t.stride(1) if n > 1 else (t.stride(0) if b > 1 else h * d)
+    dense_heads = (d == 1 or t.stride(3) == 1) and (h == 1 or t.stride(2) == d)
+    if not dense_heads or (b > 1 and n > 1 and t.stride(0) != n * pitch):
+        raise ValueError("tokens are [batch, tokens, heads, head_dim] with dense heads and one distance between tokens")
+    return _meta(tuple(t.shape), 3, _DTYPES[t.dtype], t.data_ptr()), pitch
+
+
+def _append_args(cache: Cache4, k: torch.Tensor, v: torch.Tensor, page_table, lengths):
+    sk, pk = _tokens_struct(k)
+    sv, pv = _tokens_struct(v)
+    if pk != pv:
+        raise ValueError("k and v have one distance between tokens")
+    return (ctypes.byref(_cache4_struct(cache)), ctypes.byref(sk), ctypes.byref(sv), pk,
+            ctypes.byref(_pages_struct(page_table, lengths)))
+
+
+def gl_cache4_append(cache: Cache4, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor,
+                     stream=None) -> None:
+    _check(LIB.gl_cache4_append(*_append_args(cache, k, v, page_table, lengths), _stream(stream)), "gl_cache4_append")
+
+
+def _read_args(cache: Cache4, k: torch.Tensor, v: torch.Tensor, page_table, lengths):
+    return (ctypes.byref(_cache4_struct(cache)), ctypes.byref(_pages_struct(page_table, lengths)),
+            ctypes.byref(_struct(AccessPattern(k, 3))), ctypes.byref(_struct(AccessPattern(v, 3))))
+
+
+def gl_cache4_read(cache: Cache4, tokens: int, page_table: torch.Tensor, lengths: torch.Tensor, stream=None):
+    """The values of the last `tokens` tokens of every sequence: (k, v), bf16 [B, tokens, kv_heads, head_dim]."""
+    shape = (page_table.shape[0], tokens, cache.kv_heads, cache.head_dim)
+    k, v = (torch.empty(shape, dtype=torch.bfloat16, device=cache.data.device) for _ in range(2))
+    _check(LIB.gl_cache4_read(*_read_args(cache, k, v, page_table, lengths), _stream(stream)), "gl_cache4_read")
+    return k, v
+
+
+def gl_attend_cache4_workspace(q: AccessPattern, cache: Cache4) -> int:
+    return int(LIB.gl_attend_cache4_workspace(ctypes.byref(_tokens_struct(q.tensor)[0]), ctypes.byref(_cache4_struct(cache))))
+
+
+def _attend_args(q, cache, page_table, lengths, out, scale, flags, workspace):
+    sq, pitch = _tokens_struct(q.tensor)
+    return (ctypes.byref(sq), pitch, ctypes.byref(_cache4_struct(cache)), ctypes.byref(_pages_struct(page_table, lengths)),
+            float(scale), ctypes.byref(_struct(out)), flags, *_ws(workspace))
+
+
+def gl_attend_cache4(q: AccessPattern, cache: Cache4, page_table: torch.Tensor, lengths: torch.Tensor,
+                     scale: Optional[float] = None, out: Optional[AccessPattern] = None, flags: int = 0,
+                     workspace: Optional[torch.Tensor] = None, stream=None) -> AccessPattern:
+    """q ((B, T, heads),(head_dim)); scale defaults to 1 / sqrt(head_dim)."""
+    if scale is None:
+        scale = cache.head_dim ** -0.5
+    if out is None:
+        dtype = torch.bfloat16 if flags & GL_OUT_BF16 else torch.float32
+        out = AccessPattern(torch.empty(tuple(q.tensor.shape), dtype=dtype, device=q.tensor.device), 3)
+    if workspace is None:
+        workspace = _scratch(gl_attend_cache4_workspace(q, cache), q.tensor.device)
+    _check(LIB.gl_attend_cache4(*_attend_args(q, cache, page_table, lengths, out, scale, flags, workspace), _stream(stream)),
+           "gl_attend_cache4")
+    return out
+
+
 def gl_poll_device_status(stream=None) -> int:
     return int(LIB.gl_poll_device_status(_stream(stream)))
 
@@ -504,6 +754,43 @@ def prepare_access_pad(a: AccessPattern, dim: int, lo: int, hi: int, pad_kind: i
 def prepare_compute_relu(a: AccessPattern, out: AccessPattern) -> Prepared:
     sa, so = _struct(a), _struct(out)
     return Prepared(LIB.gl_compute_relu, (ctypes.byref(sa), ctypes.byref(so)), (sa, so, a, out))
+
+
+def prepare_mx4_quantize(a: AccessPattern, out: Mx4) -> Prepared:
+    return Prepared(LIB.gl_mx4_quantize, (ctypes.byref(_struct(a)), ctypes.byref(_mx4_struct(out))), (a, out))
+
+
+def prepare_mx4_dequantize(m: Mx4, out: AccessPattern) -> Prepared:
+    return Prepared(LIB.gl_mx4_dequantize, (ctypes.byref(_mx4_struct(m)), ctypes.byref(_struct(out))), (m, out))
+
+
+def prepare_cartesian_dot_mx4(a0: Mx4, a1: Mx4, out: AccessPattern, flags: int = 0) -> Prepared:
+    return Prepared(LIB.gl_cartesian_dot_mx4, (ctypes.byref(_mx4_struct(a0)), ctypes.byref(_mx4_struct(a1)),
+                                               ctypes.byref(_struct(out)), flags), (a0, a1, out))
+
+
+def prepare_dense_mx4(a0: AccessPattern, a1: Mx4, out: AccessPattern, flags: int = 0,
+                      workspace: Optional[torch.Tensor] = None) -> Prepared:
+    if workspace is None:
+        workspace = _scratch(gl_dense_mx4_workspace(a0, a1), a0.tensor.device)
+    return Prepared(LIB.gl_dense_mx4, (ctypes.byref(_struct(a0)), ctypes.byref(_mx4_struct(a1)), ctypes.byref(_struct(out)), flags,
+                                       *_ws(workspace)), (a0, a1, out, workspace))
+
+
+def prepare_cache4_append(cache: Cache4, k, v, page_table, lengths) -> Prepared:
+    return Prepared(LIB.gl_cache4_append, _append_args(cache, k, v, page_table, lengths), (cache, k, v, page_table, lengths))
+
+
+def prepare_cache4_read(cache: Cache4, k, v, page_table, lengths) -> Prepared:
+    return Prepared(LIB.gl_cache4_read, _read_args(cache, k, v, page_table, lengths), (cache, k, v, page_table, lengths))
+
+
+def prepare_attend_cache4(q: AccessPattern, cache: Cache4, page_table, lengths, out: AccessPattern,
+                          scale: Optional[float] = None, flags: int = 0, workspace: Optional[torch.Tensor] = None) -> Prepared:
+    if workspace is None:
+        workspace = _scratch(gl_attend_cache4_workspace(q, cache), q.tensor.device)
+    args = _attend_args(q, cache, page_table, lengths, out, cache.head_dim ** -0.5 if scale is None else scale, flags, workspace)
+    return Prepared(LIB.gl_attend_cache4, args, (q, cache, page_table, lengths, out, workspace))
 
 
 def output_like(shape_fn_result, device) -> AccessPattern:

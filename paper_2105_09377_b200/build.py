@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libglenside.so")
-SOURCES = ["gl_host.cpp", "gl_memops.cu", "gl_dot.cu"]
+SOURCES = ["gl_host.cpp", "gl_memops.cu", "gl_dot.cu", "gl_mx4.cu", "gl_attend.cu"]
 
 
 def _stale() -> bool:

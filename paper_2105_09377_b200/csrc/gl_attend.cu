@@ -1,0 +1,937 @@
+// Pages of 4-bit keys and values (gl_cache4) and the attention that reads them.
+//
+// Group of 16 tokens of one kv head (17 * D bytes, one bulk copy): codes of K, scales of K, codes of V, scales of V.
+// Inside a token's row of codes the order is the one the tensor-core fragments want, so that a thread reads all it
+// needs of a token in one access and converts whole 32-bit words:
+//   K: word (j, b) = dims 32 b + 8 j .. + 7 of block b, at word j * NB + b           (NB = D / 32 blocks)
+//   V: half word (g, b) = dims 32 b + 4 g .. + 3, at half word (g ^ s) * NB + b, s = 4 for tokens with bit 1 set
+// (the exclusive or spreads the four tokens that a warp reads together over all banks).
+#include <cuda.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cstring>
+
+#include "gl_internal.h"
+#include "gl_launch.cuh"
+#include "gl_mx4.cuh"
+#include "gl_tc.cuh"
+#include "gl_tmap.h"
+
+using namespace gl;
+
+namespace {
+
+constexpr int kGroup = 16;   // tokens per group
+
+__host__ __device__ constexpr int group_bytes(int d) { return 17 * d; }
+__host__ __device__ constexpr int k_scales_at(int d) { return 8 * d; }
+__host__ __device__ constexpr int v_codes_at(int d) { return 8 * d + d / 2; }
+__host__ __device__ constexpr int v_scales_at(int d) { return 16 * d + d / 2; }
+
+struct CacheView {
+  uint8_t* data;
+  const int32_t* table;
+  const int32_t* lengths;
+  int64_t pages;
+  int64_t head_stride, page_stride;   // bytes
+  int kv_heads, page_tokens, batch, width;
+  int capacity;                       // tokens a sequence can have: width * page_tokens
+};
+
+__device__ __forceinline__ int clamped_length(const CacheView& c, int b) { return min(max(c.lengths[b], 0), c.capacity); }
+
+// Start of the group that holds token `pos` of sequence b, or null where its page does not exist.
+__device__ __forceinline__ uint8_t* group_of(const CacheView& c, int b, int h, int pos) {
+  const int slot = pos / c.page_tokens;
+  const int page = c.table[static_cast<int64_t>(b) * c.width + slot];
+  if (page < 0 || page >= c.pages) return nullptr;
+  return c.data + page * c.page_stride + h * c.head_stride;
+}
+
+// ------------------------------------------------------------------------
+// Storing and reading back
+// ------------------------------------------------------------------------
+
+// Eight dims of one token and head per thread, K and V in the two halves of the grid's y dimension.
+struct TokensParams {
+  CacheView c;
+  int T, D;
+  int64_t pitch;         // elements between tokens of the dense side
+  uint32_t items;        // batch * T * kv_heads * (D / 8)
+  FastDiv div_row, div_heads, div_T;
+};
+
+struct TokenAt { int b, i, h, w, pos; };
+
+__device__ __forceinline__ TokenAt token_at(const TokensParams& p, uint32_t item) {
+  uint32_t row, w, tok, h, b, i;
+  p.div_row.divmod(item, row, w);
+  p.div_heads.divmod(row, tok, h);
+  p.div_T.divmod(tok, b, i);
+  TokenAt t = {static_cast<int>(b), static_cast<int>(i), static_cast<int>(h), static_cast<int>(w), 0};
+  t.pos = clamped_length(p.c, t.b) - p.T + t.i;
+  return t;
+}
+
+__global__ void __launch_bounds__(256) cache4_append(const uint16_t* __restrict__ k, const uint16_t* __restrict__ v,
+                                                     const TokensParams p) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const uint32_t item = blockIdx.x * 256u + threadIdx.x;
+  if (item >= p.items) return;   // D / 8 is a multiple of eight: groups of four threads (one block of values) stay whole
+  const TokenAt t = token_at(p, item);
+  const bool is_v = blockIdx.y != 0;
+  uint4 raw = make_uint4(0, 0, 0, 0);
+  if (t.pos >= 0)
+    raw = *reinterpret_cast<const uint4*>((is_v ? v : k) + (static_cast<int64_t>(t.b) * p.T + t.i) * p.pitch +
+                                          static_cast<int64_t>(t.h) * p.D + t.w * 8);
+  const uint32_t in[4] = {raw.x, raw.y, raw.z, raw.w};
+  float x[8];
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(in[i] << 16);
+    x[2 * i + 1] = __uint_as_float(in[i] & 0xFFFF0000u);
+    top = max(top, max(__float_as_uint(x[2 * i]) & 0x7FFFFFFFu, __float_as_uint(x[2 * i + 1]) & 0x7FFFFFFFu));
+  }
+  const unsigned four = 0xFu << (threadIdx.x & 28u);
+  top = max(top, __shfl_xor_sync(four, top, 1));
+  top = max(top, __shfl_xor_sync(four, top, 2));
+  if (t.pos < 0) return;
+  uint8_t* at = group_of(p.c, t.b, t.h, t.pos);
+  if (!at) return;
+  const int in_page = t.pos % p.c.page_tokens, tok = in_page % kGroup;
+  at += static_cast<int64_t>(in_page / kGroup) * group_bytes(p.D);
+  const uint32_t e = mx4_exponent(top), word = mx4_codes8(x, e);
+  const int NB = p.D / 32, b = t.w >> 2, j = t.w & 3;
+  if (is_v) {
+    uint8_t* row = at + v_codes_at(p.D) + tok * (p.D / 2);
+    const int swz = (tok & 2) ? 4 : 0;
+    *reinterpret_cast<uint16_t*>(row + (((2 * j) ^ swz) * NB + b) * 2) = static_cast<uint16_t>(word);
+    *reinterpret_cast<uint16_t*>(row + (((2 * j + 1) ^ swz) * NB + b) * 2) = static_cast<uint16_t>(word >> 16);
+    if (j == 0) at[v_scales_at(p.D) + tok * NB + b] = static_cast<uint8_t>(e);
+  } else {
+    *reinterpret_cast<uint32_t*>(at + tok * (p.D / 2) + (j * NB + b) * 4) = word;
+    if (j == 0) at[k_scales_at(p.D) + tok * NB + b] = static_cast<uint8_t>(e);
+  }
+}
+
+__global__ void __launch_bounds__(256) cache4_read(uint16_t* __restrict__ k, uint16_t* __restrict__ v, const TokensParams p) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const uint32_t item = blockIdx.x * 256u + threadIdx.x;
+  if (item >= p.items) return;
+  const TokenAt t = token_at(p, item);
+  const bool is_v = blockIdx.y != 0;
+  const uint8_t* at = t.pos >= 0 ? group_of(p.c, t.b, t.h, t.pos) : nullptr;
+  float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  if (at) {
+    const int in_page = t.pos % p.c.page_tokens, tok = in_page % kGroup;
+    at += static_cast<int64_t>(in_page / kGroup) * group_bytes(p.D);
+    const int NB = p.D / 32, b = t.w >> 2, j = t.w & 3;
+    uint32_t word, e;
+    if (is_v) {
+      const uint8_t* row = at + v_codes_at(p.D) + tok * (p.D / 2);
+      const int swz = (tok & 2) ? 4 : 0;
+      word = *reinterpret_cast<const uint16_t*>(row + (((2 * j) ^ swz) * NB + b) * 2);
+      word |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(row + (((2 * j + 1) ^ swz) * NB + b) * 2)) << 16;
+      e = at[v_scales_at(p.D) + tok * NB + b];
+    } else {
+      word = *reinterpret_cast<const uint32_t*>(at + tok * (p.D / 2) + (j * NB + b) * 4);
+      e = at[k_scales_at(p.D) + tok * NB + b];
+    }
+    mx4_values8(word, e, x);
+  }
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(__float_as_uint(x[2 * i]), __float_as_uint(x[2 * i + 1]));
+  *reinterpret_cast<uint4*>((is_v ? v : k) + static_cast<int64_t>(item) * 8) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// ------------------------------------------------------------------------
+// Attention
+// ------------------------------------------------------------------------
+//
+// Rows are the T * group query rows that share a kv head, 8 * NT of them per work item; scores are computed transposed,
+// S^T = K Q^T with tokens as the 16-row side of mma.m16n8k16, so that eight rows (a usual group) fill an instruction.
+// Codes become fp16 by moving bits (exact, times 2^-14); the scale of a block of K multiplies the fp32 result of that
+// block's two instructions, so no scale ever meets fp16's range.  Q is scaled per row by a power of two for the same
+// reason.  Of V, a token's scale varies along the result, so it goes into the weights: w = p * 2^(e - ref + 15) with ref the
+// largest exponent of the tile and block; tokens more than 14 binades below it take another turn with a smaller ref.
+// fp16 weights keep 11 bits, which a bf16 result cannot show; for fp32 results (HILO) the rounded-off part of the
+// weights is multiplied in a second instruction.
+//
+// The work is cut along the tokens of all sequences: tiles of 32 tokens of all (sequence, kv head, row block) in one
+// list, the same number to every block.  A block's four warps take turns in the tiles of a segment, each with its own
+// ring of bulk copies, running maximum, sum and result; the block joins its warps, and a second kernel joins the
+// blocks where a segment was cut.
+
+constexpr int kTileTok = 32;
+constexpr int kWarps = 4;
+constexpr int kStagesAt = 3;
+
+struct AttendParams {
+  CacheView c;
+  const uint16_t* q;
+  void* out;
+  float* part;           // partial results: per block two slots of rows * (D + 2) floats
+  int64_t q_pitch;
+  int T, heads, group;   // group = heads / kv_heads
+  int rows, row_blocks;  // rows = T * group
+  int grid;
+  float scale_log2;      // softmax scale * log2(e)
+  int out_bf16;
+};
+
+// Tokens that the rows of row block rb can see at most.
+__device__ __forceinline__ int seen_by(int len, int T, int group, int rows, int rb, int R) {
+  const int last = min(rows, (rb + 1) * R) - 1;
+  return min(max(len - T + last / group + 1, 0), len);
+}
+
+// Tiles of one kv head of sequence b over all row blocks.
+__device__ __forceinline__ int64_t head_tiles(const AttendParams& p, int b, int R) {
+  const int len = clamped_length(p.c, b);
+  int64_t n = 0;
+  for (int rb = 0; rb < p.row_blocks; ++rb) n += (seen_by(len, p.T, p.group, p.rows, rb, R) + kTileTok - 1) / kTileTok;
+  return n;
+}
+
+// Sum of head_tiles over the sequences before `upto` and over all of them, by the whole block.
+template <int THREADS>
+__device__ __forceinline__ void sum_tiles(const AttendParams& p, int R, int upto, int64_t* before, int64_t* all, int64_t* scratch) {
+  int64_t a = 0, b = 0;
+  for (int i = threadIdx.x; i < p.c.batch; i += THREADS) {
+    const int64_t n = head_tiles(p, i, R);
+    a += n;
+    if (i < upto) b += n;
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
+    b += __shfl_xor_sync(0xFFFFFFFFu, b, o);
+  }
+  if ((threadIdx.x & 31) == 0) {
+    scratch[2 * (threadIdx.x >> 5)] = a;
+    scratch[2 * (threadIdx.x >> 5) + 1] = b;
+  }
+  __syncthreads();
+  a = b = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 32; ++w) { a += scratch[2 * w]; b += scratch[2 * w + 1]; }
+  *all = a * p.c.kv_heads;
+  *before = b * p.c.kv_heads;
+}
+
+// Tiles per block: an even share, but no less than one tile for every warp.
+__device__ __forceinline__ int64_t block_share(int64_t all, int grid) {
+  const int64_t n = (all + grid - 1) / grid;
+  return n < kWarps ? kWarps : n;
+}
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
+  return d;
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+// Token (0..15) of the group that row i of a 16-row fragment stands for: spreads the tokens that a warp reads in one
+// access over the banks.  Rows come in pairs (2i, 2i+1) -> (i, 4 + (i ^ 1)), the upper eight likewise.
+__device__ __forceinline__ int token_of_row(int i) {
+  const int j = i & 7;
+  return (i & 8) + ((j & 1) ? 4 + ((j >> 1) ^ 1) : (j >> 1));
+}
+
+template <int NB, int NT>
+struct AttCfg {
+  static constexpr int D = 32 * NB;
+  static constexpr int R = 8 * NT;
+  static constexpr int kStage = 2 * group_bytes(D);                  // one tile: two groups
+  static constexpr int kRing = kWarps * kStagesAt * kStage;
+  static constexpr int kQ = NB * 2 * NT * 32 * 8;                    // fragments of Q
+  static constexpr int kAccPitch = D + 4;
+  static constexpr int kJoin = kWarps * R * (kAccPitch + 2) * 4;     // results, maxima and sums of the warps
+  static constexpr int kSmem = kRing + kQ + R * 4 + kJoin + 256;
+};
+
+template <int NB, int NT, bool HILO>
+__global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams p) {
+  using Cfg = AttCfg<NB, NT>;
+  constexpr int D = Cfg::D, R = Cfg::R;
+  extern __shared__ __align__(128) unsigned char smem[];
+  unsigned char* ring = smem;
+  uint2* qfrag = reinterpret_cast<uint2*>(smem + Cfg::kRing);
+  float* qfac = reinterpret_cast<float*>(smem + Cfg::kRing + Cfg::kQ);
+  float* join = qfac + R;
+  unsigned char* tail = smem + Cfg::kRing + Cfg::kQ + R * 4 + Cfg::kJoin;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(tail);                          // [kWarps][kStagesAt]
+  int64_t* scratch = reinterpret_cast<int64_t*>(tail + 8 * kWarps * kStagesAt);   // [2 * kWarps]
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 8 * kWarps * kStagesAt + 16 * kWarps);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, tq = lane & 3;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kWarps * kStagesAt; ++i) mbar_init(smem_u32(bars + i), 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  pdl_wait();
+  pdl_launch_dependents();
+  int64_t all, before;
+  sum_tiles<kWarps * 32>(p, R, 0, &before, &all, scratch);   // (its barrier also publishes the ones set up above)
+  const int64_t share = block_share(all, p.grid);
+  const int64_t begin = blockIdx.x * share, end = min(all, begin + share);
+
+  const uint32_t my_ring = smem_u32(ring) + warp * kStagesAt * Cfg::kStage;
+  const unsigned char* my_gen = ring + warp * kStagesAt * Cfg::kStage;
+  const uint32_t my_bar = smem_u32(bars + warp * kStagesAt);
+  uint32_t slot_in = 0, slot_out = 0, phase_out = 0;
+  bool ok = true;
+
+  // position in the list: sequence b, kv head h, row block rb, first tile of the segment `seg0`
+  int b = 0;
+  int64_t seg0 = 0, per_head = 0;
+  if (begin < end) {
+    for (;; ++b) {   // (block-uniform; batch is small next to the tiles)
+      per_head = head_tiles(p, b, R);
+      if (seg0 + per_head * p.c.kv_heads > begin) break;
+      seg0 += per_head * p.c.kv_heads;
+    }
+  }
+  int64_t at = begin;
+  while (at < end) {
+    // segment that holds tile `at`
+    while (seg0 + per_head * p.c.kv_heads <= at) {
+      seg0 += per_head * p.c.kv_heads;
+      per_head = head_tiles(p, ++b, R);
+    }
+    const int len = clamped_length(p.c, b);
+    const int h = static_cast<int>((at - seg0) / per_head);
+    int64_t s0 = seg0 + h * per_head;
+    int rb = 0, n_seg;
+    for (;; ++rb) {
+      n_seg = (seen_by(len, p.T, p.group, p.rows, rb, R) + kTileTok - 1) / kTileTok;
+      if (s0 + n_seg > at) break;
+      s0 += n_seg;
+    }
+    const int t0 = static_cast<int>(at - s0);
+    const int t1 = static_cast<int>(min(end - s0, static_cast<int64_t>(n_seg)));
+    const int seen = seen_by(len, p.T, p.group, p.rows, rb, R);
+    at = s0 + t1;
+
+    // ---- ring of this warp: tiles t0 + warp, + kWarps, ...
+    uint32_t there = 0;   // two bits per tile in flight: its groups that have a page (oldest tile lowest)
+    int in_flight = 0;
+    int next = t0 + warp;
+    int32_t page_lo = -1, page_hi = -1;
+    auto fetch_pages = [&](int tile) {
+      const int pos = tile * kTileTok;
+      page_lo = page_hi = -1;
+      if (tile < t1) {
+        const int64_t row = static_cast<int64_t>(b) * p.c.width;
+        page_lo = p.c.table[row + pos / p.c.page_tokens];
+        if (pos + kGroup < seen) page_hi = p.c.table[row + (pos + kGroup) / p.c.page_tokens];
+      }
+    };
+    auto issue = [&]() {   // copies of tile `next`, whose pages are in page_lo and page_hi
+      if (next >= t1) return;
+      const int pos = next * kTileTok;
+      const bool lo = page_lo >= 0 && page_lo < p.c.pages, hi = page_hi >= 0 && page_hi < p.c.pages;
+      if (lane == 0) {
+        const uint32_t bar = my_bar + 8 * slot_in, dst = my_ring + slot_in * Cfg::kStage;
+        mbar_expect_tx(bar, (lo ? group_bytes(D) : 0) + (hi ? group_bytes(D) : 0));
+        if (lo)
+          bulk_copy_g2s(dst, p.c.data + page_lo * p.c.page_stride + h * p.c.head_stride +
+                                 static_cast<int64_t>(pos % p.c.page_tokens / kGroup) * group_bytes(D), group_bytes(D), bar);
+        if (hi)
+          bulk_copy_g2s(dst + group_bytes(D), p.c.data + page_hi * p.c.page_stride + h * p.c.head_stride +
+                                 static_cast<int64_t>((pos + kGroup) % p.c.page_tokens / kGroup) * group_bytes(D), group_bytes(D), bar);
+      }
+      there |= ((lo ? 1u : 0u) | (hi ? 2u : 0u)) << (2 * in_flight);
+      ++in_flight;
+      slot_in = slot_in + 1 == kStagesAt ? 0 : slot_in + 1;
+      next += kWarps;
+      fetch_pages(next);
+    };
+    fetch_pages(next);
+#pragma unroll
+    for (int i = 0; i < kStagesAt; ++i) issue();
+
+    // ---- Q as fragments in shared memory, row r scaled by a power of two into [2^14, 2^15)
+    __syncthreads();   // the previous segment's fragments and joined results are read
+    for (int r = warp; r < R; r += kWarps) {
+      const int row = rb * R + r;
+      const bool live = row < p.rows;
+      const uint16_t* src = nullptr;
+      if (live) src = p.q + (static_cast<int64_t>(b) * p.T + row / p.group) * p.q_pitch + (static_cast<int64_t>(h) * p.group + row % p.group) * D;
+      float x[NB];
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        x[i] = live ? bf16_to_f32(src[i * 32 + lane]) : 0.f;
+        top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+      }
+      top = __reduce_max_sync(0xFFFFFFFFu, top);
+      const int e = max(static_cast<int>(top >> 23), 27) - 127;                 // floor(log2) of the largest
+      const float f = __uint_as_float(static_cast<uint32_t>(14 - e + 127 > 0 ? 14 - e + 127 : 0) << 23);
+      // lane = dim % 32: word j = lane / 8, pair lane % 4, half (lane / 4) & 1; pair 2i + s is register s of instruction i
+      const int j = lane >> 3, pr = lane & 3, half = (lane >> 2) & 1;
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        __half* dst = reinterpret_cast<__half*>(qfrag + ((i * 2 + (pr >> 1)) * NT + (r >> 3)) * 32 + (r & 7) * 4 + j);
+        dst[(pr & 1) * 2 + half] = __float2half_rn(x[i] * f);
+      }
+      // scores carry 2^-14 (codes) * 2^(14 - e) (Q)
+      if (lane == 0) qfac[r] = __uint_as_float(static_cast<uint32_t>(e + 127) << 23) * p.scale_log2;
+    }
+    __syncthreads();
+
+    float m[NT][2], l[NT][2], cf[NT][2];
+    int limit[NT][2];
+    float acc[NT][NB][2][4];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const int row = rb * R + n * 8 + tq * 2 + c;
+        m[n][c] = __uint_as_float(0xFF800000u);
+        l[n][c] = 0.f;
+        cf[n][c] = qfac[n * 8 + tq * 2 + c];
+        limit[n][c] = row < p.rows ? min(len, len - p.T + row / p.group + 1) : 0;
+      }
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) acc[n][i][0][c] = acc[n][i][1][c] = 0.f;
+    }
+
+    for (int tile = t0 + warp; tile < t1; tile += kWarps) {
+      if (!mbar_wait(my_bar + 8 * slot_out, phase_out, abort_flag)) { ok = false; break; }
+      const unsigned char* st = my_gen + slot_out * Cfg::kStage;
+      const uint32_t have = there & 3u;
+      const int pos0 = tile * kTileTok;
+
+      // ---- scores: s[mt][n] = 16 tokens x 8 rows; thread: tokens of rows g and g + 8, query rows 2 tq and 2 tq + 1
+      float s[2][NT][4];
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) s[mt][n][c] = 0.f;
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt) {
+        const unsigned char* grp = st + mt * group_bytes(D);
+        const int ta = token_of_row(g), tb = ta + 8;
+        uint32_t wa[NB], wb[NB];
+        if (NB == 2) {
+          const uint2 x = *reinterpret_cast<const uint2*>(grp + ta * (D / 2) + tq * 8);
+          const uint2 y = *reinterpret_cast<const uint2*>(grp + tb * (D / 2) + tq * 8);
+          wa[0] = x.x; wa[1] = x.y; wb[0] = y.x; wb[1] = y.y;
+        } else {
+#pragma unroll
+          for (int i = 0; i < NB / 4; ++i) {
+            const uint4 x = *reinterpret_cast<const uint4*>(grp + ta * (D / 2) + tq * (NB * 4) + i * 16);
+            const uint4 y = *reinterpret_cast<const uint4*>(grp + tb * (D / 2) + tq * (NB * 4) + i * 16);
+            wa[4 * i] = x.x; wa[4 * i + 1] = x.y; wa[4 * i + 2] = x.z; wa[4 * i + 3] = x.w;
+            wb[4 * i] = y.x; wb[4 * i + 1] = y.y; wb[4 * i + 2] = y.z; wb[4 * i + 3] = y.w;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+          uint32_t ha[4], hb[4];
+          mx4_pairs_f16(wa[i], ha);
+          mx4_pairs_f16(wb[i], hb);
+          const uint32_t a0[4] = {ha[0], hb[0], ha[1], hb[1]}, a1[4] = {ha[2], hb[2], ha[3], hb[3]};
+          const float sa = mx4_scale(grp[k_scales_at(D) + ta * NB + i]), sb = mx4_scale(grp[k_scales_at(D) + tb * NB + i]);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            float c[4] = {0.f, 0.f, 0.f, 0.f};
+            const uint2 b0 = qfrag[((i * 2) * NT + n) * 32 + lane], b1 = qfrag[((i * 2 + 1) * NT + n) * 32 + lane];
+            mma_f16(c, a0, b0.x, b0.y);
+            mma_f16(c, a1, b1.x, b1.y);
+            s[mt][n][0] += c[0] * sa;
+            s[mt][n][1] += c[1] * sa;
+            s[mt][n][2] += c[2] * sb;
+            s[mt][n][3] += c[3] * sb;
+          }
+        }
+      }
+
+      // ---- mask, running maximum, weights
+      float corr[NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          float top = m[n][c];
+#pragma unroll
+          for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+              const int pos = pos0 + mt * kGroup + token_of_row(g) + 8 * hf;
+              float& x = s[mt][n][2 * hf + c];
+              // what lies behind the end or on a missing page is never looked at
+              x = (pos < limit[n][c] && (have >> mt & 1u)) ? x * cf[n][c] : __uint_as_float(0xFF800000u);
+              top = fmaxf(top, x);
+            }
+          top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
+          top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
+          top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
+          const float base = top == __uint_as_float(0xFF800000u) ? 0.f : top;   // nothing seen yet
+          corr[n][c] = ex2(m[n][c] - base);
+          m[n][c] = top;
+          float sum = 0.f;
+#pragma unroll
+          for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+              float& x = s[mt][n][2 * hf + c];
+              x = ex2(x - base);
+              sum += x;
+            }
+          l[n][c] = l[n][c] * corr[n][c] + sum;
+        }
+      }
+
+      // ---- result, block by block: acc = acc * corr + V^T w
+      int last_seen = 0;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) last_seen = max(last_seen, max(limit[n][0], limit[n][1]));
+      last_seen = __reduce_max_sync(0xFFFFFFFFu, last_seen);
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        // exponents of this thread's four tokens; 256: not seen
+        uint32_t ex[2][2];
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            const int tok = token_of_row(g) + 8 * hf;
+            const bool vis = (have >> mt & 1u) && pos0 + mt * kGroup + tok < last_seen;
+            ex[mt][hf] = vis ? st[mt * group_bytes(D) + v_scales_at(D) + tok * NB + i] : 256u;
+          }
+        // V as the 16-row operand: rows = dims 4 g .. + 3 of the block, columns = tokens
+        uint32_t va[2][2][4];   // [16 tokens][instruction][register]
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) {
+          const unsigned char* vc = st + mt * group_bytes(D) + v_codes_at(D);
+          uint32_t hw[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {   // columns 2 tq, 2 tq + 1, 2 tq + 8, 2 tq + 9
+            const int tok = token_of_row(2 * tq + (k & 1) + 8 * (k >> 1));
+            hw[k] = *reinterpret_cast<const uint16_t*>(vc + tok * (D / 2) + ((g ^ ((tok & 2) ? 4 : 0)) * NB + i) * 2);
+          }
+          uint32_t lo[4], hi[4];
+          mx4_pairs_f16(hw[0] | hw[1] << 16, lo);
+          mx4_pairs_f16(hw[2] | hw[3] << 16, hi);
+          va[mt][0][0] = lo[0]; va[mt][0][1] = lo[1]; va[mt][0][2] = hi[0]; va[mt][0][3] = hi[1];
+          va[mt][1][0] = lo[2]; va[mt][1][1] = lo[3]; va[mt][1][2] = hi[2]; va[mt][1][3] = hi[3];
+        }
+        bool first = true, more;
+        uint32_t nan_here = 0;   // this thread's tokens whose block is NaN
+        do {
+          uint32_t top = 0;
+#pragma unroll
+          for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) top = max(top, ex[mt][hf] < 255u ? ex[mt][hf] : 0u);
+          const uint32_t ref = __reduce_max_sync(0xFFFFFFFFu, top);
+          float fac[2][2];
+          bool left = false;
+#pragma unroll
+          for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+              const uint32_t e = ex[mt][hf];
+              const bool now = e <= ref && e + 14u >= ref;
+              fac[mt][hf] = now ? __uint_as_float((e + 142u - ref) << 23) : 0.f;      // 2^(e - ref + 15)
+              if (e == 255u) nan_here |= 1u << (2 * mt + hf);
+              if (now || e >= 255u) ex[mt][hf] = 256u;
+              else if (e > 0u) left = true;    // (blocks of zeros have e = 0 and add nothing)
+            }
+          more = __any_sync(0xFFFFFFFFu, left);
+          const float back = ref >= 2u ? __uint_as_float((ref - 1u) << 23) : __uint_as_float(0x00200000u << ref);   // 2^(ref - 128)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            float c0[4] = {0.f, 0.f, 0.f, 0.f}, c1[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt) {
+              uint32_t w[2], wl[2];
+#pragma unroll
+              for (int hf = 0; hf < 2; ++hf) {
+                const float x = s[mt][n][2 * hf] * fac[mt][hf], y = s[mt][n][2 * hf + 1] * fac[mt][hf];
+                const uint32_t packed = pack_f16x2(x, y);
+                w[hf] = transpose8x8(packed);
+                if (HILO) {
+                  const __half2 r = *reinterpret_cast<const __half2*>(&packed);
+                  wl[hf] = transpose8x8(pack_f16x2(x - __low2float(r), y - __high2float(r)));
+                }
+              }
+              mma_f16(c0, va[mt][0], w[0], w[1]);
+              mma_f16(c1, va[mt][1], w[0], w[1]);
+              if (HILO) {
+                mma_f16(c0, va[mt][0], wl[0], wl[1]);
+                mma_f16(c1, va[mt][1], wl[0], wl[1]);
+              }
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              const float keep = first ? corr[n][c & 1] : 1.f;
+              acc[n][i][0][c] = acc[n][i][0][c] * keep + c0[c] * back;
+              acc[n][i][1][c] = acc[n][i][1][c] * keep + c1[c] * back;
+            }
+          }
+          first = false;
+        } while (more);
+        if (__any_sync(0xFFFFFFFFu, nan_here != 0)) {   // NaN for the rows that see such a token, and for no others
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              uint32_t bad = 0;
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                if ((nan_here >> k & 1u) && pos0 + (k >> 1) * kGroup + token_of_row(g) + 8 * (k & 1) < limit[n][c]) bad = 1;
+              bad |= __shfl_xor_sync(0xFFFFFFFFu, bad, 4);
+              bad |= __shfl_xor_sync(0xFFFFFFFFu, bad, 8);
+              bad |= __shfl_xor_sync(0xFFFFFFFFu, bad, 16);
+              if (bad)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) acc[n][i][k][c] = acc[n][i][k][2 + c] = __uint_as_float(0x7FC00000u);
+            }
+        }
+      }
+      __syncwarp();   // every lane has read the stage
+      there >>= 2;
+      --in_flight;
+      if (++slot_out == kStagesAt) { slot_out = 0; phase_out ^= 1u; }
+      issue();
+    }
+
+    // ---- join the warps
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        l[n][c] += __shfl_xor_sync(0xFFFFFFFFu, l[n][c], 4);
+        l[n][c] += __shfl_xor_sync(0xFFFFFFFFu, l[n][c], 8);
+        l[n][c] += __shfl_xor_sync(0xFFFFFFFFu, l[n][c], 16);
+      }
+    float* jm = join + kWarps * R * Cfg::kAccPitch;
+    float* jl = jm + kWarps * R;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const int r = n * 8 + tq * 2 + c;
+        if (g == 0) {
+          jm[warp * R + r] = m[n][c];
+          jl[warp * R + r] = l[n][c];
+        }
+        float* row = join + (warp * R + r) * Cfg::kAccPitch;
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+            *reinterpret_cast<float2*>(row + i * 32 + 4 * g + 2 * k) = make_float2(acc[n][i][k][c], acc[n][i][k][2 + c]);
+      }
+    __syncthreads();
+    const bool whole = t0 == 0 && t1 == n_seg;
+    float* slot = p.part + (static_cast<int64_t>(blockIdx.x) * 2 + (t0 == 0 ? 1 : 0)) * R * (D + 2);
+    for (int e = threadIdx.x; e < R * (D / 4); e += kWarps * 32) {
+      const int r = e / (D / 4), d = e % (D / 4) * 4;
+      const int row = rb * R + r;
+      float top = jm[r];
+#pragma unroll
+      for (int w = 1; w < kWarps; ++w) top = fmaxf(top, jm[w * R + r]);
+      const float base = top == __uint_as_float(0xFF800000u) ? 0.f : top;
+      float sum = 0.f;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float f = ex2(jm[w * R + r] - base);
+        const float4 x = *reinterpret_cast<const float4*>(join + (w * R + r) * Cfg::kAccPitch + d);
+        sum += jl[w * R + r] * f;
+        o.x += x.x * f; o.y += x.y * f; o.z += x.z * f; o.w += x.w * f;
+      }
+      if (!whole) {
+        *reinterpret_cast<float2*>(slot + r * (D + 2) + d + 2) = make_float2(o.x, o.y);
+        *reinterpret_cast<float2*>(slot + r * (D + 2) + d + 4) = make_float2(o.z, o.w);
+        if (d == 0) *reinterpret_cast<float2*>(slot + r * (D + 2)) = make_float2(top, sum);
+      } else if (row < p.rows) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const int64_t to = ((static_cast<int64_t>(b) * p.T + row / p.group) * p.heads + static_cast<int64_t>(h) * p.group + row % p.group) * D + d;
+        if (p.out_bf16)
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + to) =
+              make_uint2(pack_bf16x2(__float_as_uint(o.x * inv), __float_as_uint(o.y * inv)),
+                         pack_bf16x2(__float_as_uint(o.z * inv), __float_as_uint(o.w * inv)));
+        else
+          *reinterpret_cast<float4*>(static_cast<float*>(p.out) + to) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+      }
+    }
+  }
+  if (!ok || *abort_flag) {   // copies in flight land before the block leaves
+    const uint64_t wait0 = global_timer();
+    while (global_timer() - wait0 < 20000000ull) { }
+  }
+}
+
+// Segments that several blocks share, in block order; zeros for segments without a tile.  One block per segment.
+__global__ void __launch_bounds__(128) attend_join(const AttendParams p, int D, int R) {
+  __shared__ int64_t scratch[8];
+  pdl_wait();
+  pdl_launch_dependents();
+  const int rb = static_cast<int>(blockIdx.x) % p.row_blocks, bh = static_cast<int>(blockIdx.x) / p.row_blocks;
+  const int b = bh / p.c.kv_heads, h = bh % p.c.kv_heads;
+  int64_t all, first;
+  sum_tiles<128>(p, R, b, &first, &all, scratch);
+  const int64_t share = block_share(all, p.grid);
+  const int len = clamped_length(p.c, b);
+  first += h * head_tiles(p, b, R);
+  for (int i = 0; i < rb; ++i) first += (seen_by(len, p.T, p.group, p.rows, i, R) + kTileTok - 1) / kTileTok;
+  const int n = (seen_by(len, p.T, p.group, p.rows, rb, R) + kTileTok - 1) / kTileTok;
+  const int64_t c0 = first / share, c1 = n ? (first + n - 1) / share : c0;
+  if (n && c0 == c1) return;   // written by the block that had all of it
+  for (int e = threadIdx.x; e < R * (D / 4); e += 128) {
+    const int r = e / (D / 4), d = e % (D / 4) * 4;
+    const int row = rb * R + r;
+    if (row >= p.rows) break;
+    float top = __uint_as_float(0xFF800000u), sum = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (n)
+      for (int64_t c = c0; c <= c1; ++c) {
+        const float* slot = p.part + (c * 2 + (c == c0 ? 1 : 0)) * R * (D + 2) + r * (D + 2);
+        const float2 ml = *reinterpret_cast<const float2*>(slot);
+        const float2 x = *reinterpret_cast<const float2*>(slot + d + 2), y = *reinterpret_cast<const float2*>(slot + d + 4);
+        const float t = fmaxf(top, ml.x), base = t == __uint_as_float(0xFF800000u) ? 0.f : t;
+        const float fo = ex2(top - base), fn = ex2(ml.x - base);
+        sum = sum * fo + ml.y * fn;
+        o.x = o.x * fo + x.x * fn; o.y = o.y * fo + x.y * fn; o.z = o.z * fo + y.x * fn; o.w = o.w * fo + y.y * fn;
+        top = t;
+      }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const int64_t to = ((static_cast<int64_t>(b) * p.T + row / p.group) * p.heads + static_cast<int64_t>(h) * p.group + row % p.group) * D + d;
+    if (p.out_bf16)
+      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + to) =
+          make_uint2(pack_bf16x2(__float_as_uint(o.x * inv), __float_as_uint(o.y * inv)),
+                     pack_bf16x2(__float_as_uint(o.z * inv), __float_as_uint(o.w * inv)));
+    else
+      *reinterpret_cast<float4*>(static_cast<float*>(p.out) + to) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+  }
+}
+
+// ---- host side ----
+
+int check_cache_meta(const gl_cache4* c) {
+  if (!c) return GL_ERR_NULL;
+  if (c->pages < 1 || c->kv_heads < 1 || c->page_tokens < 1) return GL_ERR_SHAPE;
+  if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return GL_ERR_UNSUPPORTED;
+  if (c->page_tokens % kGroup) return GL_ERR_UNSUPPORTED;
+  return GL_OK;
+}
+
+int check_cache(const gl_cache4* c, const gl_pages* at, CacheView* v) {
+  const int rc = check_cache_meta(c);
+  if (rc) return rc;
+  if (!c->data || !at || !at->page_table || !at->lengths) return GL_ERR_NULL;
+  if (reinterpret_cast<uintptr_t>(c->data) & 15u) return GL_ERR_ALIGN;
+  if ((reinterpret_cast<uintptr_t>(at->page_table) | reinterpret_cast<uintptr_t>(at->lengths)) & 3u) return GL_ERR_ALIGN;
+  if (at->batch < 1 || at->table_width < 1) return GL_ERR_SHAPE;
+  const int64_t cap = static_cast<int64_t>(at->table_width) * c->page_tokens;
+  if (cap > INT32_MAX - 4096) return GL_ERR_UNSUPPORTED;
+  v->data = static_cast<uint8_t*>(c->data);
+  v->table = at->page_table;
+  v->lengths = at->lengths;
+  v->pages = c->pages;
+  v->head_stride = static_cast<int64_t>(c->page_tokens / kGroup) * group_bytes(c->head_dim);
+  v->page_stride = v->head_stride * c->kv_heads;
+  v->kv_heads = c->kv_heads;
+  v->page_tokens = c->page_tokens;
+  v->batch = at->batch;
+  v->width = at->table_width;
+  v->capacity = static_cast<int>(cap);
+  return GL_OK;
+}
+
+// x is ((batch, T, heads),(head_dim)), bf16; pitch 0 stands for dense.
+int check_tokens(const gl_ap* x, const gl_cache4* c, const gl_pages* at, int64_t* pitch) {
+  const int rc = check_data(x);
+  if (rc) return rc;
+  if (x->dtype != GL_BF16) return GL_ERR_DTYPE;
+  if (x->ndim != 4 || x->access_ndim != 3) return GL_ERR_NDIM;
+  if (x->shape[0] != at->batch || x->shape[3] != c->head_dim) return GL_ERR_SHAPE;
+  if (x->shape[1] > INT32_MAX || x->shape[2] > INT32_MAX) return GL_ERR_UNSUPPORTED;
+  const int64_t dense = x->shape[2] * x->shape[3];
+  if (*pitch == 0) *pitch = dense;
+  if (*pitch < dense) return GL_ERR_SHAPE;
+  if (*pitch % 8) return GL_ERR_ALIGN;
+  return GL_OK;
+}
+
+int tokens_params(const gl_cache4* cache, const gl_ap* k, const gl_ap* v, int64_t pitch, const gl_pages* at, TokensParams* p) {
+  int rc = check_cache(cache, at, &p->c);
+  if (rc) return rc;
+  int64_t pk = pitch, pv = pitch;
+  rc = check_tokens(k, cache, at, &pk);
+  if (rc) return rc;
+  rc = check_tokens(v, cache, at, &pv);
+  if (rc) return rc;
+  if (k->shape[1] != v->shape[1] || k->shape[2] != cache->kv_heads || v->shape[2] != cache->kv_heads) return GL_ERR_SHAPE;
+  const int64_t items = k->shape[0] * k->shape[1] * k->shape[2] * (cache->head_dim / 8);
+  if (items > INT32_MAX - 256) return GL_ERR_UNSUPPORTED;
+  p->T = static_cast<int>(k->shape[1]);
+  p->D = cache->head_dim;
+  p->pitch = pk;
+  p->items = static_cast<uint32_t>(items);
+  p->div_row.set(cache->head_dim / 8);
+  p->div_heads.set(cache->kv_heads);
+  p->div_T.set(p->T);
+  return GL_OK;
+}
+
+// Rows per work item: 8, 16 or 32, as many as there are (fewer registers for 256-wide heads).
+int row_tiles(int64_t rows, int d) {
+  if (rows <= 8) return 1;
+  if (rows <= 16 || d == 256) return 2;
+  return 4;
+}
+
+struct AttKernel { void (*fn)(AttendParams); int smem; };
+
+template <int NB, int NT>
+AttKernel att_kernel(bool hilo) {
+  return {hilo ? attend_cache4<NB, NT, true> : attend_cache4<NB, NT, false>, AttCfg<NB, NT>::kSmem};
+}
+
+AttKernel pick_kernel(int d, int nt, bool hilo) {
+  if (d == 64) return nt == 1 ? att_kernel<2, 1>(hilo) : nt == 2 ? att_kernel<2, 2>(hilo) : att_kernel<2, 4>(hilo);
+  if (d == 128) return nt == 1 ? att_kernel<4, 1>(hilo) : nt == 2 ? att_kernel<4, 2>(hilo) : att_kernel<4, 4>(hilo);
+  return nt == 1 ? att_kernel<8, 1>(hilo) : att_kernel<8, 2>(hilo);
+}
+
+constexpr int kMaxBlocksPerSm = 4;
+
+// Blocks of the persistent grid: what is resident at once.
+int att_grid(const AttKernel& k, int d, int nt, bool hilo, int* grid) {
+  static int cached[64][3][3][2];   // per device; benign race: the calls are idempotent
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return GL_ERR_CUDA;
+  int& n = cached[dev][d == 64 ? 0 : d == 128 ? 1 : 2][nt == 4 ? 2 : nt - 1][hilo ? 1 : 0];
+  if (!n) {
+    if (cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem) != cudaSuccess) return GL_ERR_CUDA;
+    int per = 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, k.fn, kWarps * 32, k.smem) != cudaSuccess || per < 1) return GL_ERR_CUDA;
+    n = std::min(per, kMaxBlocksPerSm) * num_sms();
+  }
+  *grid = n;
+  return GL_OK;
+}
+
+}  // namespace
+
+namespace gl {
+int take_status_attend() {
+  unsigned int v = 0;
+  if (cudaMemcpyFromSymbol(&v, g_status, sizeof(v)) != cudaSuccess) return GL_ERR_CUDA;
+  if (!v) return GL_OK;
+  const unsigned int zero = 0;
+  if (cudaMemcpyToSymbol(g_status, &zero, sizeof(zero)) != cudaSuccess) return GL_ERR_CUDA;
+  return GL_ERR_TIMEOUT;
+}
+}  // namespace gl
+
+extern "C" {
+
+size_t gl_cache4_bytes(const gl_cache4* c) {
+  if (check_cache_meta(c)) return 0;
+  return static_cast<size_t>(c->pages) * c->kv_heads * (c->page_tokens / kGroup) * group_bytes(c->head_dim);
+}
+
+int gl_cache4_append(const gl_cache4* cache, const gl_ap* k, const gl_ap* v, int64_t token_pitch, const gl_pages* at, void* stream) {
+  TokensParams p;
+  const int rc = tokens_params(cache, k, v, token_pitch, at, &p);
+  if (rc) return rc;
+  const dim3 grid((p.items + 255) / 256, 2);
+  return launch_pdl(cache4_append, grid, dim3(256), 0, static_cast<cudaStream_t>(stream), 1, static_cast<const uint16_t*>(k->data),
+                    static_cast<const uint16_t*>(v->data), p) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
+}
+
+int gl_cache4_read(const gl_cache4* cache, const gl_pages* at, gl_ap* k, gl_ap* v, void* stream) {
+  TokensParams p;
+  const int rc = tokens_params(cache, k, v, 0, at, &p);
+  if (rc) return rc;
+  const dim3 grid((p.items + 255) / 256, 2);
+  return launch_pdl(cache4_read, grid, dim3(256), 0, static_cast<cudaStream_t>(stream), 1, static_cast<uint16_t*>(k->data),
+                    static_cast<uint16_t*>(v->data), p) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
+}
+
+size_t gl_attend_cache4_workspace(const gl_ap* q, const gl_cache4* cache) {
+  if (check_meta(q) || check_cache_meta(cache) || q->ndim != 4 || q->shape[2] % cache->kv_heads) return 0;
+  const int64_t rows = q->shape[1] * (q->shape[2] / cache->kv_heads);
+  const int R = 8 * row_tiles(rows, cache->head_dim);
+  return static_cast<size_t>(kMaxBlocksPerSm) * num_sms() * 2 * R * (cache->head_dim + 2) * sizeof(float);
+}
+
+int gl_attend_cache4(const gl_ap* q, int64_t token_pitch, const gl_cache4* cache, const gl_pages* at, float scale, gl_ap* out,
+                     uint32_t flags, void* workspace, size_t workspace_bytes, void* stream) {
+  AttendParams p;
+  int rc = check_cache(cache, at, &p.c);
+  if (rc) return rc;
+  if (flags & ~GL_OUT_BF16) return GL_ERR_UNSUPPORTED;
+  int64_t pitch = token_pitch;
+  rc = check_tokens(q, cache, at, &pitch);
+  if (rc) return rc;
+  if (q->shape[2] % cache->kv_heads) return GL_ERR_SHAPE;
+  if (!(scale > 0.f) || !(scale <= 3.0e38f)) return GL_ERR_SHAPE;
+  gl_ap want = *q;
+  want.dtype = (flags & GL_OUT_BF16) ? GL_BF16 : GL_F32;
+  rc = check_same_meta(want, out);
+  if (rc) return rc;
+  rc = check_data(out);
+  if (rc) return rc;
+  const size_t need = gl_attend_cache4_workspace(q, cache);
+  if (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 1023u)) return GL_ERR_WORKSPACE;
+  const int64_t group = q->shape[2] / cache->kv_heads, rows = q->shape[1] * group;
+  const int nt = row_tiles(rows, cache->head_dim), R = 8 * nt;
+  const int64_t row_blocks = (rows + R - 1) / R, segments = q->shape[0] * cache->kv_heads * row_blocks;
+  if (rows > INT32_MAX - 64 || segments > INT32_MAX) return GL_ERR_UNSUPPORTED;
+  const bool hilo = !(flags & GL_OUT_BF16);
+  const AttKernel k = pick_kernel(cache->head_dim, nt, hilo);
+  rc = att_grid(k, cache->head_dim, nt, hilo, &p.grid);
+  if (rc) return rc;
+  p.q = static_cast<const uint16_t*>(q->data);
+  p.out = out->data;
+  p.part = static_cast<float*>(workspace);
+  p.q_pitch = pitch;
+  p.T = static_cast<int>(q->shape[1]);
+  p.heads = static_cast<int>(q->shape[2]);
+  p.group = static_cast<int>(group);
+  p.rows = static_cast<int>(rows);
+  p.row_blocks = static_cast<int>(row_blocks);
+  p.scale_log2 = scale * 1.4426950408889634f;
+  p.out_bf16 = hilo ? 0 : 1;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (launch_pdl(k.fn, dim3(static_cast<unsigned>(p.grid)), dim3(kWarps * 32), static_cast<size_t>(k.smem), st, 1, p) != cudaSuccess)
+    return GL_ERR_CUDA;
+  return launch_pdl(attend_join, dim3(static_cast<unsigned>(segments)), dim3(128), 0, st, 1, p, cache->head_dim, R) == cudaSuccess
+             ? GL_OK : GL_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -33,6 +33,9 @@ struct DotProblem {
   int64_t ph_lo = 0, ph_hi = 0, pw_lo = 0, pw_hi = 0, Ho = 0, Wo = 0;
   bool general = false;        // neither of the above: arbitrary-rank windows
 };
+// Device status words of the other kernel files: reads and clears, GL_ERR_TIMEOUT when one was raised.
+int take_status_mx4();
+int take_status_attend();
 int classify_dot(const gl_ap* a0, const gl_windows* w, const gl_ap* a1, DotProblem* p);
 
 }  // namespace gl

@@ -1,0 +1,814 @@
+// Operands held in 4 bits (MX4): blocks of 32 consecutive values of an item, E2M1 codes and one E8M0 scale per block.
+//   * gl_mx4_quantize / gl_mx4_dequantize: between GL_BF16 / GL_F32 patterns and MX4 operands;
+//   * gl_cartesian_dot_mx4: compute dotProd (cartProd A B) of two MX4 operands on the block-scaled tensor-core
+//     instructions (tcgen05.mma kind::mxf4), the scales applied by the hardware;
+//   * gl_dense_mx4: the same with the left operand quantised by the call.
+//
+// Storage.  Codes: one row per item, two codes a byte (even index in the low half), rows of 16-byte multiples, the
+// last block filled with zeros.  Scales: tiles of 128 rows x 4 blocks (512 bytes), row r and block b of a tile at
+// byte (r % 32) * 16 + (r / 32) * 4 + b: exactly what one tcgen05.cp (32x128b, replicated to the four lane
+// quarters) has to find in shared memory, so that a tile goes global -> shared -> tensor memory untouched.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cstring>
+
+#include "gl_internal.h"
+#include "gl_launch.cuh"
+#include "gl_mx4.cuh"
+#include "gl_tc.cuh"
+#include "gl_tmap.h"
+
+using namespace gl;
+
+namespace {
+
+constexpr int kBlock = 32;
+
+struct Mx4View {
+  int64_t rows, K;
+  int64_t pitch;      // bytes per row of codes
+  int64_t kt, rt;     // scale tiles along K (128 values each) and along the rows (128 each)
+};
+
+int check_mx4_meta(const gl_mx4* a, Mx4View* v) {
+  if (!a) return GL_ERR_NULL;
+  if (a->ndim < 0 || a->ndim > GL_MAX_DIMS) return GL_ERR_NDIM;
+  if (a->access_ndim < 0 || a->access_ndim > a->ndim) return GL_ERR_NDIM;
+  for (int i = 0; i < a->ndim; ++i)
+    if (a->shape[i] < 1) return GL_ERR_SHAPE;
+  v->rows = prod(a->shape, 0, a->access_ndim);
+  v->K = prod(a->shape, a->access_ndim, a->ndim);
+  v->pitch = (v->K + kBlock - 1) / kBlock * (kBlock / 2);
+  v->kt = (v->K + 127) / 128;
+  v->rt = (v->rows + 127) / 128;
+  return GL_OK;
+}
+
+int check_mx4_data(const gl_mx4* a, Mx4View* v) {
+  const int rc = check_mx4_meta(a, v);
+  if (rc) return rc;
+  if (!a->data || !a->scale) return GL_ERR_NULL;
+  if ((reinterpret_cast<uintptr_t>(a->data) | reinterpret_cast<uintptr_t>(a->scale)) & 15u) return GL_ERR_ALIGN;
+  // item indices are 32-bit in the kernels
+  if (v->rows > INT32_MAX - 256 || v->K > (int64_t{1} << 30)) return GL_ERR_UNSUPPORTED;
+  return GL_OK;
+}
+
+bool same_shape(const gl_ap* a, const gl_mx4* b) {
+  if (a->ndim != b->ndim || a->access_ndim != b->access_ndim) return false;
+  for (int i = 0; i < a->ndim; ++i)
+    if (a->shape[i] != b->shape[i]) return false;
+  return true;
+}
+
+// ------------------------------------------------------------------------
+// Quantisation and its inverse
+// ------------------------------------------------------------------------
+
+// Eight values per thread, four neighbouring threads per block, sixteen per 4-byte group of scales (one row, 128
+// values: the unit in which the scale tiles are addressed).  Thread i of the grid handles item i; U items per
+// thread, 256 apart, are requested before the first is used.
+struct QuantParams {
+  int64_t K, pitch, kt;
+  uint32_t items;        // rows * kt * 16
+  FastDiv div_row;       // kt * 16 items per row
+};
+
+// Byte of the scale tiles that holds block group `quad` (4 blocks) of row r.
+__device__ __forceinline__ int64_t scale_quad_at(uint32_t r, uint32_t quad, int64_t kt) {
+  return (static_cast<int64_t>(r >> 7) * kt + quad) * 512 + (r & 31u) * 16 + ((r >> 5) & 3u) * 4;
+}
+
+template <bool F32, bool VEC>
+__device__ __forceinline__ void load8(const void* __restrict__ in, uint32_t r, uint32_t c, int64_t K, float (&v)[8]) {
+  const int64_t at = static_cast<int64_t>(r) * K + static_cast<int64_t>(c) * 8;
+  const int64_t left = K - static_cast<int64_t>(c) * 8;
+  if (VEC) {
+    // K is a multiple of 8: a group of eight lies wholly inside the row or wholly behind it
+    if (left > 0) {
+      if (F32) {
+        const float4 a = __ldcs(reinterpret_cast<const float4*>(static_cast<const float*>(in) + at));
+        const float4 b = __ldcs(reinterpret_cast<const float4*>(static_cast<const float*>(in) + at) + 1);
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+      } else {
+        const uint4 a = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(in) + at));
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v[2 * i] = __uint_as_float(w[i] << 16);
+          v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = 0.f;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (i < left)
+        v[i] = F32 ? static_cast<const float*>(in)[at + i] : bf16_to_f32(static_cast<const uint16_t*>(in)[at + i]);
+      else
+        v[i] = 0.f;
+    }
+  }
+}
+
+template <bool F32, bool VEC, int U>
+__global__ void __launch_bounds__(256) quantize_mx4(const void* __restrict__ in, uint8_t* __restrict__ codes,
+                                                    uint8_t* __restrict__ scale, const QuantParams p) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const uint32_t first = blockIdx.x * (256u * U) + threadIdx.x;
+  float v[U][8];
+  uint32_t row[U], col[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const uint32_t i = first + u * 256u;
+    if (i < p.items) {
+      p.div_row.divmod(i, row[u], col[u]);
+      load8<F32, VEC>(in, row[u], col[u], p.K, v[u]);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const uint32_t i = first + u * 256u;
+    // groups of sixteen threads share a row and `items` is a multiple of sixteen: the shuffles stay inside a group
+    if (i >= p.items) continue;
+    const unsigned group = 0xFFFFu << (threadIdx.x & 16u);
+    uint32_t top = 0;   // largest magnitude as bits: NaN > Inf > finite
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[u][j]) & 0x7FFFFFFFu);
+    top = max(top, __shfl_xor_sync(group, top, 1));
+    top = max(top, __shfl_xor_sync(group, top, 2));
+    const uint32_t e = mx4_exponent(top);
+    const uint32_t word = mx4_codes8(v[u], e);
+    uint32_t quad = __shfl_down_sync(group, e, 4, 16) << 8 | e;
+    quad |= __shfl_down_sync(group, quad, 8, 16) << 16;
+    if (static_cast<int64_t>(col[u]) * 4 < p.pitch)
+      *reinterpret_cast<uint32_t*>(codes + static_cast<int64_t>(row[u]) * p.pitch + col[u] * 4) = word;
+    if ((threadIdx.x & 15u) == 0)
+      *reinterpret_cast<uint32_t*>(scale + scale_quad_at(row[u], col[u] >> 4, p.kt)) = quad;
+  }
+}
+
+template <bool F32, bool VEC, int U>
+__global__ void __launch_bounds__(256) dequantize_mx4(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scale,
+                                                      void* __restrict__ out, const QuantParams p) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const uint32_t first = blockIdx.x * (256u * U) + threadIdx.x;
+  uint32_t word[U], e[U], row[U], col[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const uint32_t i = first + u * 256u;
+    word[u] = 0;
+    e[u] = 0;
+    row[u] = col[u] = 0;
+    if (i < p.items) {
+      p.div_row.divmod(i, row[u], col[u]);
+      if (static_cast<int64_t>(col[u]) * 8 < p.K) {
+        word[u] = *reinterpret_cast<const uint32_t*>(codes + static_cast<int64_t>(row[u]) * p.pitch + col[u] * 4);
+        e[u] = scale[scale_quad_at(row[u], col[u] >> 4, p.kt) + ((col[u] >> 2) & 3u)];
+      }
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const uint32_t i = first + u * 256u;
+    const int64_t left = p.K - static_cast<int64_t>(col[u]) * 8;
+    if (i >= p.items || left <= 0) continue;
+    float v[8];
+    mx4_values8(word[u], e[u], v);
+    const int64_t at = static_cast<int64_t>(row[u]) * p.K + static_cast<int64_t>(col[u]) * 8;
+    if (VEC) {
+      if (F32) {
+        float4* o = reinterpret_cast<float4*>(static_cast<float*>(out) + at);
+        __stcs(o, make_float4(v[0], v[1], v[2], v[3]));
+        __stcs(o + 1, make_float4(v[4], v[5], v[6], v[7]));
+      } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = pack_bf16x2(__float_as_uint(v[2 * j]), __float_as_uint(v[2 * j + 1]));
+        __stcs(reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + at), make_uint4(w[0], w[1], w[2], w[3]));
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j < left) {
+          if (F32) static_cast<float*>(out)[at + j] = v[j];
+          else static_cast<uint16_t*>(out)[at + j] = f32_to_bf16(v[j]);
+        }
+    }
+  }
+}
+
+int quant_params(const Mx4View& v, QuantParams* p) {
+  const int64_t items = v.rows * v.kt * 16;
+  if (items > INT32_MAX - 4096) return GL_ERR_UNSUPPORTED;
+  p->K = v.K;
+  p->pitch = v.pitch;
+  p->kt = v.kt;
+  p->items = static_cast<uint32_t>(items);
+  p->div_row.set(v.kt * 16);
+  return GL_OK;
+}
+
+int launch_quantize(const gl_ap& in, const Mx4View& v, void* codes, void* scale, cudaStream_t st) {
+  QuantParams p;
+  const int rc = quant_params(v, &p);
+  if (rc) return rc;
+  const bool f32 = in.dtype == GL_F32, vec = v.K % 8 == 0;
+  constexpr int kU = 4;
+  const bool wide = p.items >= 148u * 4u * 256u * kU;   // several items per thread only when every SM has blocks to hold
+  const dim3 grid((p.items + 256u * (wide ? kU : 1) - 1) / (256u * (wide ? kU : 1)));
+  void (*k)(const void*, uint8_t*, uint8_t*, QuantParams) =
+      wide ? (f32 ? (vec ? quantize_mx4<true, true, kU> : quantize_mx4<true, false, kU>)
+                  : (vec ? quantize_mx4<false, true, kU> : quantize_mx4<false, false, kU>))
+           : (f32 ? (vec ? quantize_mx4<true, true, 1> : quantize_mx4<true, false, 1>)
+                  : (vec ? quantize_mx4<false, true, 1> : quantize_mx4<false, false, 1>));
+  return launch_pdl(k, grid, dim3(256), 0, st, 1, static_cast<const void*>(in.data), static_cast<uint8_t*>(codes),
+                    static_cast<uint8_t*>(scale), p) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
+}
+
+// ------------------------------------------------------------------------
+// Block-scaled product
+// ------------------------------------------------------------------------
+
+// D[tmem] (+)= (A * sfa)[smem] * (B * sfb)[smem]^T, K = 64, scales of 32 values each (two per row and instruction).
+template <int CTAS>
+__device__ __forceinline__ void tc_mma_mx4(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa,
+                                           uint32_t sfb, uint32_t accumulate) {
+  if (CTAS == 2)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+}
+
+// One scale tile (32 rows x 16 bytes of shared memory) into four columns of tensor memory, repeated in the four lane
+// quarters.  Copies and MMAs of one thread run in the order of their issue.
+template <int CTAS>
+__device__ __forceinline__ void tc_copy_scales(uint32_t taddr, uint64_t desc) {
+  if (CTAS == 2) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+  else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+
+// Instruction descriptor, kind::mxf4: A and B E2M1 (bits 7-9 and 10-11 = 1), both K-major, N >> 3 at bit 17, scales
+// E8M0 (bit 23), M >> 7 at bit 27; which half of the four scale bytes the instruction reads: bits 4-5 (B), 29-30 (A).
+__host__ __device__ constexpr uint32_t make_idesc_mx4(int m, int n, int half) {
+  return (static_cast<uint32_t>(half * 2) << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(n >> 3) << 17) | (1u << 23) |
+         (static_cast<uint32_t>(m >> 7) << 27) | (static_cast<uint32_t>(half * 2) << 29);
+}
+
+// relu that lets a NaN through (fmaxf would turn it into 0)
+__device__ __forceinline__ float relu_keep_nan(float v) { return v < 0.f ? 0.f : v; }
+
+constexpr int kTile = 128;           // rows of A per block
+constexpr int kKBytes = 128;         // bytes of a row per K block: 256 values, one 128-byte swizzle row
+constexpr int kMxThreads = 224;      // warp 0 TMA (A), warp 1 MMA, warps 2-5 epilogue, warp 6 TMA (B)
+
+struct Mx4Params {
+  int64_t M, O;
+  int tiles_m, tiles_n;   // tiles_m counts 128 * CTAS rows
+  int kblocks;            // K blocks of 256 values
+  int last_steps;         // instructions (64 values) in the last K block
+  int relu, out_bf16, tma_store;
+  FastDiv div_tiles_n;
+};
+
+template <int BN, int CTAS>
+struct MxCfg {
+  static constexpr int kStageA = kTile * kKBytes;
+  static constexpr int kStageB = (BN / CTAS) * kKBytes;
+  static constexpr int kScaleA = 1024, kScaleB = (BN / 128) * 1024;   // two scale tiles along K per row tile
+  static constexpr int kStage = kStageA + kStageB + kScaleA + kScaleB;
+  static constexpr int kEpiBytes = 4 * 2 * 4096;
+  static constexpr int kStages = (232448 - kEpiBytes - 1024 - 256) / kStage;
+  static constexpr int kSmemBytes = kStages * kStage + kEpiBytes + 1024 + 256;
+  // Tensor memory (512 columns): scales in the last kSfCols, two accumulators of BN columns before them.  256-wide
+  // accumulators do not fit twice: they share kSfCols columns, which the epilogue empties first.
+  static constexpr int kSfCols = 8 + BN / 16;
+  static constexpr int kSfBase = 512 - kSfCols;
+  static constexpr int kAcc1 = 2 * BN <= kSfBase ? BN : kSfBase - BN;
+  static constexpr bool kOverlap = kAcc1 < BN;
+};
+
+template <int BN, int CTAS>
+__global__ void __launch_bounds__(kMxThreads, 1)
+dot_mx4(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+        const __grid_constant__ CUtensorMap map_sa, const __grid_constant__ CUtensorMap map_sb,
+        const __grid_constant__ CUtensorMap map_c, void* __restrict__ out, const Mx4Params p) {
+  using Cfg = MxCfg<BN, CTAS>;
+  static_assert(Cfg::kStages >= 2, "ring too shallow");
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t tiles = (raw + 1023u) & ~1023u;   // the 128-byte swizzle wants 1024-byte aligned tiles
+  unsigned char* gen_tiles = smem_raw + (tiles - raw);
+  const uint32_t epi_base = tiles + Cfg::kStages * Cfg::kStage;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(gen_tiles + Cfg::kStages * Cfg::kStage + Cfg::kEpiBytes);
+  const uint32_t bar_full = smem_u32(bars);
+  const uint32_t bar_empty = bar_full + 8 * Cfg::kStages;
+  const uint32_t bar_tfull = bar_empty + 8 * Cfg::kStages;
+  const uint32_t bar_tempty = bar_tfull + 16;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * Cfg::kStages + 4);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = CTAS == 2 ? cluster_ctarank() : 0u;
+
+  if (threadIdx.x == 32) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_a)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_b)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_sa)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_sb)) : "memory");
+    if (p.tma_store) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_c)) : "memory");
+  }
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < Cfg::kStages; ++s) { mbar_init(bar_full + 8 * s, 2); mbar_init(bar_empty + 8 * s, 1); }
+    for (int a = 0; a < 2; ++a) { mbar_init(bar_tfull + 8 * a, 1); mbar_init(bar_tempty + 8 * a, 4 * CTAS); }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    if (CTAS == 2) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot)) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot)) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+  }
+  tc_fence_before();
+  if (CTAS == 2) cluster_sync_all();
+  else __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const int num_tiles = p.tiles_m * p.tiles_n;
+  const int unit0 = static_cast<int>(blockIdx.x) / CTAS, unit_step = static_cast<int>(gridDim.x) / CTAS;
+  pdl_wait();
+  pdl_launch_dependents();
+
+  if (warp == 0 || warp == 6) {
+    // ---------------- TMA producers: warp 0 stages A and its scales, warp 6 stages B and its scales ----------------
+    const bool load_a = warp == 0;
+    const bool leader = elect_one();
+    uint32_t s = 0, ph = 0;
+    bool ok = true;
+    for (int u = unit0; u < num_tiles && ok; u += unit_step) {
+      uint32_t tm, tn;
+      p.div_tiles_n.divmod(static_cast<uint32_t>(u), tm, tn);
+      const int m0 = (static_cast<int>(tm) * CTAS + static_cast<int>(rank)) * kTile;
+      const int n0 = static_cast<int>(tn) * BN + static_cast<int>(rank) * (BN / CTAS);
+      for (int kb = 0; kb < p.kblocks; ++kb) {
+        if (!mbar_wait(bar_empty + 8 * s, ph ^ 1u, abort_flag)) { ok = false; break; }
+        const uint32_t full = CTAS == 2 ? map_to_cta(bar_full + 8 * s, 0) : bar_full + 8 * s;
+        const uint32_t stage = tiles + s * Cfg::kStage;
+        const uint32_t sc = stage + Cfg::kStageA + Cfg::kStageB;
+        if (rank == 0 && leader)
+          mbar_expect_tx(bar_full + 8 * s, CTAS * (load_a ? Cfg::kStageA + Cfg::kScaleA : Cfg::kStageB + Cfg::kScaleB));
+        if (leader) {
+          if (load_a) {
+            if (CTAS == 2) {
+              tma_load_2d_pair(stage, &map_a, kb * kKBytes, m0, full);
+              tma_load_3d_pair(sc, &map_sa, 0, kb * 2, m0 / 128, full);
+            } else {
+              tma_load_2d(stage, &map_a, kb * kKBytes, m0, full);
+              tma_load_3d(sc, &map_sa, 0, kb * 2, m0 / 128, full);
+            }
+          } else {
+            // every block of a pair holds the scales of all BN columns
+            if (CTAS == 2) tma_load_2d_pair(stage + Cfg::kStageA, &map_b, kb * kKBytes, n0, full);
+            else tma_load_2d(stage + Cfg::kStageA, &map_b, kb * kKBytes, n0, full);
+#pragma unroll
+            for (int h = 0; h < BN / 128; ++h) {
+              const uint32_t dst = sc + Cfg::kScaleA + h * 1024;
+              const int rt = static_cast<int>(tn) * (BN / 128) + h;
+              if (CTAS == 2) tma_load_3d_pair(dst, &map_sb, 0, kb * 2, rt, full);
+              else tma_load_3d(dst, &map_sb, 0, kb * 2, rt, full);
+            }
+          }
+        }
+        if (++s == Cfg::kStages) { s = 0; ph ^= 1u; }
+      }
+    }
+  } else if (warp == 1) {
+    // ---------------- MMA issuer ----------------
+    if (rank == 0) {
+      const bool leader = elect_one();
+      const uint64_t desc_a0 = make_desc(tiles, 16, 1024, 2);
+      const uint64_t desc_b0 = make_desc(tiles + Cfg::kStageA, 16, 1024, 2);
+      const uint64_t desc_s0 = make_desc(tiles + Cfg::kStageA + Cfg::kStageB, 16, 128, 0);
+      const uint32_t sfa = tmem_base + Cfg::kSfBase, sfb = sfa + 8;
+      uint32_t s = 0, ph = 0, tile_it = 0;
+      bool ok = true;
+      for (int u = unit0; u < num_tiles && ok; u += unit_step, ++tile_it) {
+        const uint32_t acc = tile_it & 1u;
+        // separate accumulators: the one two tiles back has been read; overlapping ones: the shared columns of the
+        // previous tile have been read (its epilogue had then finished with the tile before)
+        const uint32_t wait_on = Cfg::kOverlap ? acc ^ 1u : acc;
+        const uint32_t round = Cfg::kOverlap ? (tile_it + 1) >> 1 : tile_it >> 1;
+        if (!mbar_wait(bar_tempty + 8 * wait_on, (round & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t d_tmem = tmem_base + (acc ? Cfg::kAcc1 : 0);
+        for (int kb = 0; kb < p.kblocks; ++kb) {
+          if (!mbar_wait(bar_full + 8 * s, ph, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+          const uint64_t da0 = desc_a0 + ((s * Cfg::kStage) >> 4);
+          const uint64_t db0 = desc_b0 + ((s * Cfg::kStage) >> 4);
+          const uint64_t ds0 = desc_s0 + ((s * Cfg::kStage) >> 4);
+          const int steps = kb + 1 == p.kblocks ? p.last_steps : 4;
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {   // 128 values: one scale tile per 128 rows
+            if (2 * g < steps) {
+              if (leader) {
+                tc_copy_scales<CTAS>(sfa + 4 * g, ds0 + ((g * 512) >> 4));
+#pragma unroll
+                for (int h = 0; h < BN / 128; ++h)
+                  tc_copy_scales<CTAS>(sfb + g * (BN / 32) + 4 * h, ds0 + ((Cfg::kScaleA + h * 1024 + g * 512) >> 4));
+              }
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+                const int k = 2 * g + j;
+                if (k < steps && leader)
+                  tc_mma_mx4<CTAS>(d_tmem, da0 + 2 * k, db0 + 2 * k, make_idesc_mx4(kTile * CTAS, BN, j), sfa + 4 * g,
+                                   sfb + g * (BN / 32), (kb | k) != 0 ? 1u : 0u);
+              }
+            }
+          }
+          if (leader) {
+            if (CTAS == 2) tc_commit_pair(bar_empty + 8 * s);
+            else tc_commit(bar_empty + 8 * s);
+          }
+          if (++s == Cfg::kStages) { s = 0; ph ^= 1u; }
+        }
+        if (ok && leader) {
+          if (CTAS == 2) tc_commit_pair(bar_tfull + 8 * acc);
+          else tc_commit(bar_tfull + 8 * acc);
+        }
+      }
+    }
+  } else {
+    // ---------------- epilogue: TMEM -> registers -> (shared memory -> TMA store | global) ----------------
+    const int q = warp & 3;
+    const bool leader = elect_one();
+    uint32_t tile_it = 0, chunk_it = 0;
+    bool ok = true;
+    const uint32_t stage_buf = epi_base + q * 8192;
+    const int cstep = p.out_bf16 ? 64 : 32;
+    const int nchunks = BN / cstep;
+    for (int u = unit0; u < num_tiles && ok; u += unit_step, ++tile_it) {
+      const uint32_t acc = tile_it & 1u, aph = (tile_it >> 1) & 1u;
+      uint32_t tmu, tn;
+      p.div_tiles_n.divmod(static_cast<uint32_t>(u), tmu, tn);
+      const int tm = static_cast<int>(tmu) * CTAS + static_cast<int>(rank);
+      if (!mbar_wait(bar_tfull + 8 * acc, aph, abort_flag)) { ok = false; break; }
+      tc_fence_after();
+      const int64_t m = static_cast<int64_t>(tm) * kTile + q * 32 + lane;
+      const uint32_t taddr = tmem_base + (acc ? Cfg::kAcc1 : 0) + (static_cast<uint32_t>(q * 32) << 16);
+#pragma unroll 1
+      for (int i = 0; i < nchunks; ++i) {
+        // the columns that two overlapping accumulators share go first: the last ones of the first, the first ones
+        // of the second
+        const int c = (Cfg::kOverlap && acc == 0 ? nchunks - 1 - i : i) * cstep;
+        const int64_t n0 = static_cast<int64_t>(tn) * BN + c;
+        uint32_t r[32];
+        tc_load_32cols(taddr + c, r);
+        if (p.relu) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(relu_keep_nan(__uint_as_float(r[j])));
+        }
+        if (p.out_bf16) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) r[j] = pack_bf16x2(r[2 * j], r[2 * j + 1]);
+          uint32_t r2[32];
+          tc_load_32cols(taddr + c + 32, r2);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            float a = __uint_as_float(r2[2 * j]), b = __uint_as_float(r2[2 * j + 1]);
+            if (p.relu) { a = relu_keep_nan(a); b = relu_keep_nan(b); }
+            r[16 + j] = pack_bf16x2(__float_as_uint(a), __float_as_uint(b));
+          }
+        }
+        if (i == (Cfg::kOverlap ? 0 : nchunks - 1)) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) {
+            if (CTAS == 2) mbar_arrive_cluster(map_to_cta(bar_tempty + 8 * acc, 0));
+            else mbar_arrive(bar_tempty + 8 * acc);
+          }
+        }
+        if (n0 >= p.O) continue;   // uniform across the warp
+        if (p.tma_store) {
+          const uint32_t buf = stage_buf + (chunk_it & 1u) * 4096;
+          if (leader) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+          __syncwarp();
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buf + lane * 128 + ((j ^ (lane & 7)) << 4)),
+                         "r"(r[4 * j]), "r"(r[4 * j + 1]), "r"(r[4 * j + 2]), "r"(r[4 * j + 3])
+                         : "memory");
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (leader) {
+            if (tm * kTile + q * 32 < p.M)
+              asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
+                               reinterpret_cast<uint64_t>(&map_c)),
+                           "r"(static_cast<int>(n0)), "r"(tm * kTile + q * 32), "r"(buf)
+                           : "memory");
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+          }
+          ++chunk_it;
+        } else if (m < p.M) {
+          if (p.out_bf16) {
+            uint16_t* row = static_cast<uint16_t*>(out) + m * p.O + n0;
+#pragma unroll
+            for (int j = 0; j < 64; ++j)
+              if (n0 + j < p.O) row[j] = static_cast<uint16_t>(r[j >> 1] >> (16 * (j & 1)));
+          } else {
+            float* row = static_cast<float*>(out) + m * p.O + n0;
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (n0 + j < p.O) row[j] = __uint_as_float(r[j]);
+          }
+        }
+      }
+    }
+    if (p.tma_store && leader) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+  }
+
+  // teardown: a block that gave up lets its copies in flight land before it leaves
+  __syncwarp();
+  if (*abort_flag) {
+    const uint64_t t0 = global_timer();
+    while (global_timer() - t0 < 20000000ull) { }
+  }
+  tc_fence_before();
+  if (CTAS == 2) cluster_sync_all();
+  else __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    if (CTAS == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem_base) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem_base) : "memory");
+  }
+}
+
+// ---- host side ----
+
+struct Mx4Operand { const void* codes; const void* scale; Mx4View v; };
+
+bool encode_codes(CUtensorMap* m, const Mx4Operand& a, int box_rows) {
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(a.v.pitch), static_cast<cuuint64_t>(a.v.rows)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(a.v.pitch)};
+  const cuuint32_t box[2] = {kKBytes, static_cast<cuuint32_t>(box_rows)};
+  const cuuint32_t estr[2] = {1, 1};
+  return encode_tiled_cached(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, a.codes, dims, strides, box, estr, CU_TENSOR_MAP_SWIZZLE_128B,
+                             CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
+}
+
+// Scale tiles as (128 words, tiles along K, tiles along the rows); a box is the two tiles of one K block.  Tiles past
+// the end read as zeros.
+bool encode_scales(CUtensorMap* m, const Mx4Operand& a) {
+  const cuuint64_t dims[3] = {128, static_cast<cuuint64_t>(a.v.kt), static_cast<cuuint64_t>(a.v.rt)};
+  const cuuint64_t strides[2] = {512, static_cast<cuuint64_t>(a.v.kt) * 512};
+  const cuuint32_t box[3] = {128, 2, 1};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return encode_tiled_cached(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, a.scale, dims, strides, box, estr, CU_TENSOR_MAP_SWIZZLE_NONE,
+                             CU_TENSOR_MAP_L2_PROMOTION_L2_128B);
+}
+
+bool encode_out(CUtensorMap* m, void* base, int64_t M, int64_t O, bool bf16) {
+  const cuuint64_t es = bf16 ? 2 : 4;
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(O), static_cast<cuuint64_t>(M)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(O) * es};
+  const cuuint32_t box[2] = {bf16 ? 64u : 32u, 32};
+  const cuuint32_t estr[2] = {1, 1};
+  return encode_tiled_cached(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, base, dims, strides,
+                             box, estr, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE);
+}
+
+struct TilePlanMx4 {
+  CUtensorMap ma, mb, msa, msb, mc;
+  Mx4Params p;
+  void* out;
+  int grid;
+};
+
+template <int BN, int CTAS>
+int plan_tiles(const Mx4Operand& a, const Mx4Operand& b, void* out, uint32_t flags, TilePlanMx4* t) {
+  using Cfg = MxCfg<BN, CTAS>;
+  static bool attr_set[64] = {false};   // per device; benign race: the calls are idempotent
+  static int resident[64] = {0};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return GL_ERR_CUDA;
+  if (!attr_set[dev]) {
+    if (cudaFuncSetAttribute(dot_mx4<BN, CTAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes) != cudaSuccess)
+      return GL_ERR_CUDA;
+    int units = num_sms();
+    if (CTAS == 2) {   // SMs pair up within a GPC: a persistent grid must not exceed what is resident at once
+      cudaLaunchConfig_t cfg;
+      std::memset(&cfg, 0, sizeof(cfg));
+      cudaLaunchAttribute at;
+      std::memset(&at, 0, sizeof(at));
+      at.id = cudaLaunchAttributeClusterDimension;
+      at.val.clusterDim.x = CTAS;
+      at.val.clusterDim.y = at.val.clusterDim.z = 1;
+      cfg.gridDim = dim3(static_cast<unsigned>(num_sms() / 2 * 2));
+      cfg.blockDim = dim3(kMxThreads);
+      cfg.dynamicSmemBytes = Cfg::kSmemBytes;
+      cfg.attrs = &at;
+      cfg.numAttrs = 1;
+      if (cudaOccupancyMaxActiveClusters(&units, dot_mx4<BN, CTAS>, &cfg) != cudaSuccess || units < 1) return GL_ERR_CUDA;
+      units = std::min(units, num_sms() / 2);
+    }
+    resident[dev] = units;
+    attr_set[dev] = true;
+  }
+  Mx4Params& p = t->p;
+  p.M = a.v.rows;
+  p.O = b.v.rows;
+  p.tiles_m = static_cast<int>((p.M + kTile * CTAS - 1) / (kTile * CTAS));
+  p.tiles_n = static_cast<int>((p.O + BN - 1) / BN);
+  if (static_cast<int64_t>(p.tiles_m) * p.tiles_n > (1 << 30)) return GL_ERR_UNSUPPORTED;
+  const int64_t steps = (a.v.K + 63) / 64;
+  p.kblocks = static_cast<int>((steps + 3) / 4);
+  p.last_steps = static_cast<int>(steps - 4 * static_cast<int64_t>(p.kblocks - 1));
+  p.relu = (flags & GL_EPILOGUE_RELU) ? 1 : 0;
+  p.out_bf16 = (flags & GL_OUT_BF16) ? 1 : 0;
+  p.tma_store = p.O % (p.out_bf16 ? 8 : 4) == 0 ? 1 : 0;
+  p.div_tiles_n.set(p.tiles_n);
+  t->out = out;
+  t->grid = CTAS * std::min(resident[dev], p.tiles_m * p.tiles_n);
+  if (!encode_codes(&t->ma, a, kTile) || !encode_codes(&t->mb, b, BN / CTAS) || !encode_scales(&t->msa, a) ||
+      !encode_scales(&t->msb, b))
+    return GL_ERR_CUDA;
+  t->mc = t->ma;   // unused without TMA stores; any valid map
+  if (p.tma_store && !encode_out(&t->mc, out, p.M, p.O, p.out_bf16 != 0)) return GL_ERR_CUDA;
+  return GL_OK;
+}
+
+template <int BN, int CTAS>
+int run_tiles(const TilePlanMx4& t, cudaStream_t st) {
+  return launch_pdl(dot_mx4<BN, CTAS>, dim3(static_cast<unsigned>(t.grid)), dim3(kMxThreads), MxCfg<BN, CTAS>::kSmemBytes, st, CTAS,
+                    t.ma, t.mb, t.msa, t.msb, t.mc, t.out, t.p) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
+}
+
+// Checks shared by the two products: shapes, result, aliasing rules are the caller's.
+int check_product(const gl_ap* out, int a_access, const int64_t* a_shape, int a_compute, const gl_mx4* a1, uint32_t flags) {
+  if (flags & ~(GL_EPILOGUE_RELU | GL_OUT_BF16)) return GL_ERR_UNSUPPORTED;
+  if (a_compute != a1->ndim - a1->access_ndim) return GL_ERR_SHAPE;
+  for (int i = 0; i < a_compute; ++i)
+    if (a_shape[a_access + i] != a1->shape[a1->access_ndim + i]) return GL_ERR_SHAPE;
+  if (a_access + a1->access_ndim > GL_MAX_DIMS) return GL_ERR_NDIM;
+  gl_ap want;
+  std::memset(&want, 0, sizeof(want));
+  want.dtype = (flags & GL_OUT_BF16) ? GL_BF16 : GL_F32;
+  for (int i = 0; i < a_access; ++i) want.shape[want.ndim++] = a_shape[i];
+  for (int i = 0; i < a1->access_ndim; ++i) want.shape[want.ndim++] = a1->shape[i];
+  want.access_ndim = want.ndim;
+  const int rc = check_same_meta(want, out);
+  if (rc) return rc;
+  return check_data(out);
+}
+
+// Product of two operands that have been checked; everything that can fail does so before `pre` enqueues anything.
+template <typename Pre>
+int product(const Mx4Operand& a, const Mx4Operand& b, gl_ap* out, uint32_t flags, cudaStream_t st, Pre&& pre) {
+  if (!driver_api().ok) return GL_ERR_CUDA;
+  TilePlanMx4 t;
+  int rc = plan_tiles<128, 1>(a, b, out->data, flags, &t);
+  if (rc) return rc;
+  rc = pre();
+  if (rc) return rc;
+  return run_tiles<128, 1>(t, st);
+}
+
+size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+
+}  // namespace
+
+namespace gl {
+int take_status_mx4() {
+  unsigned int v = 0;
+  if (cudaMemcpyFromSymbol(&v, g_status, sizeof(v)) != cudaSuccess) return GL_ERR_CUDA;
+  if (!v) return GL_OK;
+  const unsigned int zero = 0;
+  if (cudaMemcpyToSymbol(g_status, &zero, sizeof(zero)) != cudaSuccess) return GL_ERR_CUDA;
+  return GL_ERR_TIMEOUT;
+}
+}  // namespace gl
+
+extern "C" {
+
+size_t gl_mx4_data_bytes(const gl_mx4* a) {
+  Mx4View v;
+  return check_mx4_meta(a, &v) ? 0 : static_cast<size_t>(v.rows) * v.pitch;
+}
+
+size_t gl_mx4_scale_bytes(const gl_mx4* a) {
+  Mx4View v;
+  return check_mx4_meta(a, &v) ? 0 : static_cast<size_t>(v.rt) * v.kt * 512;
+}
+
+int gl_mx4_quantize(const gl_ap* in, gl_mx4* out, void* stream) {
+  int rc = check_data(in);
+  if (rc) return rc;
+  Mx4View v;
+  rc = check_mx4_data(out, &v);
+  if (rc) return rc;
+  if (!same_shape(in, out)) return GL_ERR_SHAPE;
+  return launch_quantize(*in, v, out->data, out->scale, static_cast<cudaStream_t>(stream));
+}
+
+int gl_mx4_dequantize(const gl_mx4* in, gl_ap* out, void* stream) {
+  Mx4View v;
+  int rc = check_mx4_data(in, &v);
+  if (rc) return rc;
+  rc = check_data(out);
+  if (rc) return rc;
+  if (!same_shape(out, in)) return GL_ERR_SHAPE;
+  QuantParams p;
+  rc = quant_params(v, &p);
+  if (rc) return rc;
+  const bool f32 = out->dtype == GL_F32, vec = v.K % 8 == 0;
+  constexpr int kU = 4;
+  const bool wide = p.items >= 148u * 4u * 256u * kU;
+  const dim3 grid((p.items + 256u * (wide ? kU : 1) - 1) / (256u * (wide ? kU : 1)));
+  void (*k)(const uint8_t*, const uint8_t*, void*, QuantParams) =
+      wide ? (f32 ? (vec ? dequantize_mx4<true, true, kU> : dequantize_mx4<true, false, kU>)
+                  : (vec ? dequantize_mx4<false, true, kU> : dequantize_mx4<false, false, kU>))
+           : (f32 ? (vec ? dequantize_mx4<true, true, 1> : dequantize_mx4<true, false, 1>)
+                  : (vec ? dequantize_mx4<false, true, 1> : dequantize_mx4<false, false, 1>));
+  return launch_pdl(k, grid, dim3(256), 0, static_cast<cudaStream_t>(stream), 1, static_cast<const uint8_t*>(in->data),
+                    static_cast<const uint8_t*>(in->scale), out->data, p) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
+}
+
+int gl_cartesian_dot_mx4(const gl_mx4* a0, const gl_mx4* a1, gl_ap* out, uint32_t flags, void* stream) {
+  Mx4Operand a, b;
+  int rc = check_mx4_data(a0, &a.v);
+  if (rc) return rc;
+  rc = check_mx4_data(a1, &b.v);
+  if (rc) return rc;
+  rc = check_product(out, a0->access_ndim, a0->shape, a0->ndim - a0->access_ndim, a1, flags);
+  if (rc) return rc;
+  a.codes = a0->data;
+  a.scale = a0->scale;
+  b.codes = a1->data;
+  b.scale = a1->scale;
+  return product(a, b, out, flags, static_cast<cudaStream_t>(stream), [] { return GL_OK; });
+}
+
+size_t gl_dense_mx4_workspace(const gl_ap* a0, const gl_mx4* a1) {
+  Mx4View v;
+  if (check_meta(a0) || check_mx4_meta(a1, &v)) return 0;
+  gl_mx4 q;
+  std::memset(&q, 0, sizeof(q));
+  q.ndim = a0->ndim;
+  q.access_ndim = a0->access_ndim;
+  for (int i = 0; i < a0->ndim; ++i) q.shape[i] = a0->shape[i];
+  return round_up(gl_mx4_data_bytes(&q), 1024) + gl_mx4_scale_bytes(&q);
+}
+
+int gl_dense_mx4(const gl_ap* a0, const gl_mx4* a1, gl_ap* out, uint32_t flags, void* workspace, size_t workspace_bytes,
+                 void* stream) {
+  int rc = check_data(a0);
+  if (rc) return rc;
+  Mx4Operand a, b;
+  rc = check_mx4_data(a1, &b.v);
+  if (rc) return rc;
+  rc = check_product(out, a0->access_ndim, a0->shape, a0->ndim - a0->access_ndim, a1, flags);
+  if (rc) return rc;
+  gl_mx4 q;
+  std::memset(&q, 0, sizeof(q));
+  q.ndim = a0->ndim;
+  q.access_ndim = a0->access_ndim;
+  for (int i = 0; i < a0->ndim; ++i) q.shape[i] = a0->shape[i];
+  const size_t need = gl_dense_mx4_workspace(a0, a1);
+  if (need && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 1023u))) return GL_ERR_WORKSPACE;
+  q.data = workspace;
+  q.scale = static_cast<char*>(workspace) + round_up(gl_mx4_data_bytes(&q), 1024);
+  rc = check_mx4_data(&q, &a.v);
+  if (rc) return rc;
+  QuantParams qp;
+  rc = quant_params(a.v, &qp);
+  if (rc) return rc;
+  b.codes = a1->data;
+  b.scale = a1->scale;
+  a.codes = q.data;
+  a.scale = q.scale;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return product(a, b, out, flags, st, [&] { return launch_quantize(*a0, a.v, q.data, q.scale, st); });
+}
+
+}  // extern "C"
