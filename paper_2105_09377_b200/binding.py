@@ -221,7 +221,9 @@ def _alloc(meta: GlAp, device) -> AccessPattern:
 
 def _stream(stream) -> int:
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+        # torch.cuda.current_stream() builds a Stream object: 3.3 us, next to 2 us for a kernel launch
+        torch.cuda.is_initialized() or torch.cuda.init()
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 

@@ -475,7 +475,6 @@ dot_mx4(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUten
       const int tm = static_cast<int>(tmu) * CTAS + static_cast<int>(rank);
       if (!mbar_wait(bar_tfull + 8 * acc, aph, abort_flag)) { ok = false; break; }
       tc_fence_after();
-      const int64_t m = static_cast<int64_t>(tm) * kTile + q * 32 + lane;
       const uint32_t taddr = tmem_base + (acc ? Cfg::kAcc1 : 0) + (static_cast<uint32_t>(q * 32) << 16);
 #pragma unroll 1
       for (int i = 0; i < nchunks; ++i) {
@@ -510,15 +509,16 @@ dot_mx4(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUten
           }
         }
         if (n0 >= p.O) continue;   // uniform across the warp
-        if (p.tma_store) {
-          const uint32_t buf = stage_buf + (chunk_it & 1u) * 4096;
-          if (leader) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-          __syncwarp();
+        const uint32_t buf = stage_buf + (chunk_it & 1u) * 4096;
+        ++chunk_it;
+        if (p.tma_store && leader) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+        __syncwarp();
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buf + lane * 128 + ((j ^ (lane & 7)) << 4)),
-                         "r"(r[4 * j]), "r"(r[4 * j + 1]), "r"(r[4 * j + 2]), "r"(r[4 * j + 3])
-                         : "memory");
+        for (int j = 0; j < 8; ++j)
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buf + lane * 128 + ((j ^ (lane & 7)) << 4)),
+                       "r"(r[4 * j]), "r"(r[4 * j + 1]), "r"(r[4 * j + 2]), "r"(r[4 * j + 3])
+                       : "memory");
+        if (p.tma_store) {
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
           if (leader) {
@@ -529,18 +529,28 @@ dot_mx4(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUten
                            : "memory");
             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
           }
-          ++chunk_it;
-        } else if (m < p.M) {
-          if (p.out_bf16) {
-            uint16_t* row = static_cast<uint16_t*>(out) + m * p.O + n0;
-#pragma unroll
-            for (int j = 0; j < 64; ++j)
-              if (n0 + j < p.O) row[j] = static_cast<uint16_t>(r[j >> 1] >> (16 * (j & 1)));
-          } else {
-            float* row = static_cast<float*>(out) + m * p.O + n0;
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-              if (n0 + j < p.O) row[j] = __uint_as_float(r[j]);
+        } else {
+          // rows that are no multiples of 16 bytes: row by row, neighbouring lanes on neighbouring columns (a lane
+          // per row instead takes 32 memory segments per store: 25 us against 12 us for 301 x 1111 x 777)
+          __syncwarp();
+          const int rows = static_cast<int>(min(static_cast<int64_t>(32), p.M - (static_cast<int64_t>(tm) * kTile + q * 32)));
+          const int cols = static_cast<int>(min(static_cast<int64_t>(cstep), p.O - n0));
+          const int64_t base = (static_cast<int64_t>(tm) * kTile + q * 32) * p.O + n0;
+#pragma unroll 8
+          for (int i = 0; i < rows; ++i) {
+            uint32_t v;
+            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(buf + i * 128 + (((lane >> 2) ^ (i & 7)) << 4) + (lane & 3) * 4));
+            if (p.out_bf16) {
+              uint16_t* to = static_cast<uint16_t*>(out) + base + i * p.O + 2 * lane;
+              if ((p.O & 1) == 0) {
+                if (2 * lane < cols) *reinterpret_cast<uint32_t*>(to) = v;   // (O even: whole pairs)
+              } else {
+                if (2 * lane < cols) to[0] = static_cast<uint16_t>(v);
+                if (2 * lane + 1 < cols) to[1] = static_cast<uint16_t>(v >> 16);
+              }
+            } else if (lane < cols) {
+              static_cast<float*>(out)[base + i * p.O + lane] = __uint_as_float(v);
+            }
           }
         }
       }
@@ -564,7 +574,218 @@ dot_mx4(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUten
   }
 }
 
+// ------------------------------------------------------------------------
+// Few rows of A: the weights take the 128-row side
+// ------------------------------------------------------------------------
+//
+// With at most 128 rows of A the product is bound by reading B (the weights) once.  Tiles of 128 rows of B, all rows of
+// A as the N side (BN = 16 to 128 of them), and K cut over the S blocks of a cluster so that the loads of all SMs are in
+// flight: the blocks' partial sums meet in distributed shared memory, added in rank order.  One tile per block, two
+// blocks per SM.  While the kernel that rounds A is still running the weights are on their way into L2.
+
+struct FewParams {
+  int M;
+  int64_t O;
+  int kblocks, last_steps;
+  int split;              // blocks per cluster
+  int relu, out_bf16;
+};
+
+// Rank r adds up the columns r, r + S, ...: the S partial sums of a value in rank order, those of four columns requested
+// before the first is added.
+template <int S>
+__device__ __forceinline__ void join_ranks(uint32_t mine, int rank, int64_t o, void* __restrict__ out, const FewParams& p) {
+  for (int c0 = rank; c0 < p.M; c0 += 4 * S) {
+    float x[4][S];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int from = 0; from < S; ++from)   // (columns past M are inside the partial sums' space only up to BN)
+        if (c0 + j * S < p.M)
+          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x[j][from]) : "r"(map_to_cta(mine + (c0 + j * S) * 512, from)));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int c = c0 + j * S;
+      if (c >= p.M) break;
+      float v = x[j][0];
+#pragma unroll
+      for (int from = 1; from < S; ++from) v += x[j][from];
+      if (p.relu) v = relu_keep_nan(v);
+      if (p.out_bf16) static_cast<uint16_t*>(out)[c * p.O + o] = f32_to_bf16(v);
+      else static_cast<float*>(out)[c * p.O + o] = v;
+    }
+  }
+}
+
+template <int BN>
+struct FewCfg {
+  static constexpr int kStageA = kTile * kKBytes;                  // weights
+  static constexpr int kStageB = BN * kKBytes;
+  static constexpr int kStage = kStageA + kStageB + 2048;          // and two scale tiles of each side
+  static constexpr int kStages = (112 * 1024 - 1024 - 256) / kStage;
+  static constexpr int kSmemBytes = kStages * kStage + 1024 + 256;
+  static constexpr int kTmemCols = BN + 16 <= 32 ? 32 : BN + 16 <= 64 ? 64 : BN + 16 <= 128 ? 128 : 256;
+  static constexpr int kSfBase = kTmemCols - 16;
+  static_assert(kStages * kStage >= BN * 128 * 4, "partial sums fit in the ring");
+};
+
+template <int BN>
+__global__ void __launch_bounds__(kMxThreads, 2)
+dot_mx4_few(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
+            const __grid_constant__ CUtensorMap map_sw, const __grid_constant__ CUtensorMap map_sx, void* __restrict__ out,
+            const FewParams p) {
+  using Cfg = FewCfg<BN>;
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t tiles = (raw + 1023u) & ~1023u;
+  unsigned char* gen_tiles = smem_raw + (tiles - raw);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(gen_tiles + Cfg::kStages * Cfg::kStage);
+  const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8 * Cfg::kStages, bar_done = bar_empty + 8 * Cfg::kStages;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * Cfg::kStages + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = p.split > 1 ? static_cast<int>(cluster_ctarank()) : 0;
+  const int tile = static_cast<int>(blockIdx.x) / p.split;
+  // K blocks of this rank, as even as they go
+  const int kb0 = static_cast<int>(static_cast<int64_t>(p.kblocks) * rank / p.split);
+  const int kb1 = static_cast<int>(static_cast<int64_t>(p.kblocks) * (rank + 1) / p.split);
+
+  if (warp == 0 && elect_one())
+    for (int kb = kb0; kb < kb1; ++kb) tma_prefetch_2d(&map_w, kb * kKBytes, tile * kTile);
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < Cfg::kStages; ++s) { mbar_init(bar_full + 8 * s, 2); mbar_init(bar_empty + 8 * s, 1); }
+    mbar_init(bar_done, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
+                 "r"(static_cast<uint32_t>(Cfg::kTmemCols)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  pdl_wait();
+  pdl_launch_dependents();
+
+  if (warp == 0 || warp == 6) {
+    const bool load_w = warp == 0;
+    const bool leader = elect_one();
+    uint32_t s = 0, ph = 0;
+    for (int kb = kb0; kb < kb1; ++kb) {
+      if (!mbar_wait(bar_empty + 8 * s, ph ^ 1u, abort_flag)) break;
+      const uint32_t full = bar_full + 8 * s, stage = tiles + s * Cfg::kStage, sc = stage + Cfg::kStageA + Cfg::kStageB;
+      if (leader) {
+        mbar_expect_tx(full, (load_w ? Cfg::kStageA : Cfg::kStageB) + 1024);
+        if (load_w) {
+          tma_load_2d(stage, &map_w, kb * kKBytes, tile * kTile, full);
+          tma_load_3d(sc, &map_sw, 0, kb * 2, tile, full);
+        } else {
+          tma_load_2d(stage + Cfg::kStageA, &map_x, kb * kKBytes, 0, full);
+          tma_load_3d(sc + 1024, &map_sx, 0, kb * 2, 0, full);
+        }
+      }
+      if (++s == Cfg::kStages) { s = 0; ph ^= 1u; }
+    }
+  } else if (warp == 1) {
+    const bool leader = elect_one();
+    const uint64_t desc_w0 = make_desc(tiles, 16, 1024, 2), desc_x0 = make_desc(tiles + Cfg::kStageA, 16, 1024, 2);
+    const uint64_t desc_s0 = make_desc(tiles + Cfg::kStageA + Cfg::kStageB, 16, 128, 0);
+    const uint32_t sfw = tmem_base + Cfg::kSfBase, sfx = sfw + 8;
+    uint32_t s = 0, ph = 0;
+    bool ok = true;
+    for (int kb = kb0; kb < kb1; ++kb) {
+      if (!mbar_wait(bar_full + 8 * s, ph, abort_flag)) { ok = false; break; }
+      tc_fence_after();
+      const uint64_t off = (s * Cfg::kStage) >> 4;
+      const int steps = kb + 1 == p.kblocks ? p.last_steps : 4;
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+        if (2 * g < steps) {
+          if (leader) {
+            tc_copy_scales<1>(sfw + 4 * g, desc_s0 + off + ((g * 512) >> 4));
+            tc_copy_scales<1>(sfx + 4 * g, desc_s0 + off + ((1024 + g * 512) >> 4));
+          }
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int k = 2 * g + j;
+            if (k < steps && leader)
+              tc_mma_mx4<1>(tmem_base, desc_w0 + off + 2 * k, desc_x0 + off + 2 * k, make_idesc_mx4(kTile, BN, j), sfw + 4 * g,
+                            sfx + 4 * g, kb != kb0 || k != 0 ? 1u : 0u);
+          }
+        }
+      if (leader) tc_commit(bar_empty + 8 * s);
+      if (++s == Cfg::kStages) { s = 0; ph ^= 1u; }
+    }
+    if (ok && leader) tc_commit(bar_done);
+  }
+  float* part = reinterpret_cast<float*>(gen_tiles);   // [BN][128]: every MMA has read the ring when bar_done flips
+  const int q = warp & 3;
+  const int64_t o = static_cast<int64_t>(tile) * kTile + q * 32 + lane;
+  const bool epilogue = warp >= 2 && warp < 6;
+  if (epilogue) {
+    const bool ok = mbar_wait(bar_done, 0, abort_flag);
+    tc_fence_after();
+    if (ok) {
+#pragma unroll 1
+      for (int c = 0; c < BN; c += 16) {
+        if (c >= p.M) break;
+        uint32_t r[16];
+        tc_load_16cols(tmem_base + (static_cast<uint32_t>(q * 32) << 16) + c, r);
+        if (p.split > 1) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) part[(c + j) * 128 + q * 32 + lane] = __uint_as_float(r[j]);
+        } else if (o < p.O) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            if (c + j < p.M) {
+              const float v = p.relu ? relu_keep_nan(__uint_as_float(r[j])) : __uint_as_float(r[j]);
+              if (p.out_bf16) static_cast<uint16_t*>(out)[(c + j) * p.O + o] = f32_to_bf16(v);
+              else static_cast<float*>(out)[(c + j) * p.O + o] = v;
+            }
+        }
+      }
+    }
+    tc_fence_before();
+  }
+  if (p.split > 1) {
+    __syncwarp();
+    cluster_sync_all();
+    if (epilogue && o < p.O) {
+      const uint32_t mine = smem_u32(part) + (q * 32 + lane) * 4;
+      switch (p.split) {
+        case 2: join_ranks<2>(mine, rank, o, out, p); break;
+        case 4: join_ranks<4>(mine, rank, o, out, p); break;
+        default: join_ranks<8>(mine, rank, o, out, p); break;
+      }
+    }
+  }
+  __syncwarp();
+  if (*abort_flag) {   // copies in flight land before the block leaves
+    const uint64_t t0 = global_timer();
+    while (global_timer() - t0 < 20000000ull) { }
+  }
+  if (p.split > 1) cluster_sync_all();   // the other ranks have read this block's sums
+  else __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base),
+                 "r"(static_cast<uint32_t>(Cfg::kTmemCols)) : "memory");
+  }
+}
+
 // ---- host side ----
+
+// Tensor maps are encoded on every call: 0.05 us each, no more than looking one up.
+bool encode(CUtensorMap* m, CUtensorMapDataType dt, cuuint32_t rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides,
+            const cuuint32_t* box, CUtensorMapSwizzle swz, CUtensorMapL2promotion l2) {
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return driver_api().tiled(m, dt, rank, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swz, l2,
+                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 
 struct Mx4Operand { const void* codes; const void* scale; Mx4View v; };
 
@@ -572,9 +793,8 @@ bool encode_codes(CUtensorMap* m, const Mx4Operand& a, int box_rows) {
   const cuuint64_t dims[2] = {static_cast<cuuint64_t>(a.v.pitch), static_cast<cuuint64_t>(a.v.rows)};
   const cuuint64_t strides[1] = {static_cast<cuuint64_t>(a.v.pitch)};
   const cuuint32_t box[2] = {kKBytes, static_cast<cuuint32_t>(box_rows)};
-  const cuuint32_t estr[2] = {1, 1};
-  return encode_tiled_cached(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, a.codes, dims, strides, box, estr, CU_TENSOR_MAP_SWIZZLE_128B,
-                             CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
+  return encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, a.codes, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
 }
 
 // Scale tiles as (128 words, tiles along K, tiles along the rows); a box is the two tiles of one K block.  Tiles past
@@ -583,9 +803,8 @@ bool encode_scales(CUtensorMap* m, const Mx4Operand& a) {
   const cuuint64_t dims[3] = {128, static_cast<cuuint64_t>(a.v.kt), static_cast<cuuint64_t>(a.v.rt)};
   const cuuint64_t strides[2] = {512, static_cast<cuuint64_t>(a.v.kt) * 512};
   const cuuint32_t box[3] = {128, 2, 1};
-  const cuuint32_t estr[3] = {1, 1, 1};
-  return encode_tiled_cached(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, a.scale, dims, strides, box, estr, CU_TENSOR_MAP_SWIZZLE_NONE,
-                             CU_TENSOR_MAP_L2_PROMOTION_L2_128B);
+  return encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, a.scale, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_NONE,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_128B);
 }
 
 bool encode_out(CUtensorMap* m, void* base, int64_t M, int64_t O, bool bf16) {
@@ -593,9 +812,8 @@ bool encode_out(CUtensorMap* m, void* base, int64_t M, int64_t O, bool bf16) {
   const cuuint64_t dims[2] = {static_cast<cuuint64_t>(O), static_cast<cuuint64_t>(M)};
   const cuuint64_t strides[1] = {static_cast<cuuint64_t>(O) * es};
   const cuuint32_t box[2] = {bf16 ? 64u : 32u, 32};
-  const cuuint32_t estr[2] = {1, 1};
-  return encode_tiled_cached(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, base, dims, strides,
-                             box, estr, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE);
+  return encode(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, base, dims, strides, box,
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE);
 }
 
 struct TilePlanMx4 {
@@ -664,6 +882,58 @@ int run_tiles(const TilePlanMx4& t, cudaStream_t st) {
                     t.ma, t.mb, t.msa, t.msb, t.mc, t.out, t.p) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
 }
 
+struct FewPlan {
+  CUtensorMap mw, mx, msw, msx;
+  FewParams p;
+  void* out;
+  int grid;
+};
+
+template <int BN>
+int plan_few(const Mx4Operand& a, const Mx4Operand& b, void* out, uint32_t flags, FewPlan* t) {
+  static bool attr_set[64] = {false};   // per device; benign race: the call is idempotent
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return GL_ERR_CUDA;
+  if (!attr_set[dev]) {
+    if (cudaFuncSetAttribute(dot_mx4_few<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<BN>::kSmemBytes) != cudaSuccess)
+      return GL_ERR_CUDA;
+    attr_set[dev] = true;
+  }
+  FewParams& p = t->p;
+  p.M = static_cast<int>(a.v.rows);
+  p.O = b.v.rows;
+  const int64_t steps = (a.v.K + 63) / 64;
+  p.kblocks = static_cast<int>((steps + 3) / 4);
+  p.last_steps = static_cast<int>(steps - 4 * static_cast<int64_t>(p.kblocks - 1));
+  p.relu = (flags & GL_EPILOGUE_RELU) ? 1 : 0;
+  p.out_bf16 = (flags & GL_OUT_BF16) ? 1 : 0;
+  if (b.v.rt > (1 << 27)) return GL_ERR_UNSUPPORTED;
+  const int tiles = static_cast<int>(b.v.rt);
+  // as many ranks as still leave every one a K block and all blocks resident at once (two per SM)
+  p.split = 1;
+  while (p.split < 8 && p.split * 2 <= p.kblocks && tiles * p.split * 2 <= 2 * num_sms()) p.split *= 2;
+  t->out = out;
+  t->grid = tiles * p.split;
+  return encode_codes(&t->mw, b, kTile) && encode_codes(&t->mx, a, BN) && encode_scales(&t->msw, b) && encode_scales(&t->msx, a)
+             ? GL_OK : GL_ERR_CUDA;
+}
+
+template <int BN>
+int run_few(const FewPlan& t, cudaStream_t st) {
+  return launch_pdl(dot_mx4_few<BN>, dim3(static_cast<unsigned>(t.grid)), dim3(kMxThreads), FewCfg<BN>::kSmemBytes, st, t.p.split,
+                    t.mw, t.mx, t.msw, t.msx, t.out, t.p) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
+}
+
+template <int BN, typename Pre>
+int product_few(const Mx4Operand& a, const Mx4Operand& b, gl_ap* out, uint32_t flags, cudaStream_t st, Pre&& pre) {
+  FewPlan t;
+  int rc = plan_few<BN>(a, b, out->data, flags, &t);
+  if (rc) return rc;
+  rc = pre();
+  if (rc) return rc;
+  return run_few<BN>(t, st);
+}
+
 // Checks shared by the two products: shapes, result, aliasing rules are the caller's.
 int check_product(const gl_ap* out, int a_access, const int64_t* a_shape, int a_compute, const gl_mx4* a1, uint32_t flags) {
   if (flags & ~(GL_EPILOGUE_RELU | GL_OUT_BF16)) return GL_ERR_UNSUPPORTED;
@@ -686,12 +956,24 @@ int check_product(const gl_ap* out, int a_access, const int64_t* a_shape, int a_
 template <typename Pre>
 int product(const Mx4Operand& a, const Mx4Operand& b, gl_ap* out, uint32_t flags, cudaStream_t st, Pre&& pre) {
   if (!driver_api().ok) return GL_ERR_CUDA;
+  // Up to 128 rows: the weights as the 128-row side, K cut over clusters (64 x 8192 x 8192: 12.8 us against 20.3 us on
+  // the tiles below).
+  if (a.v.rows <= 16) return product_few<16>(a, b, out, flags, st, pre);
+  if (a.v.rows <= 32) return product_few<32>(a, b, out, flags, st, pre);
+  if (a.v.rows <= 64) return product_few<64>(a, b, out, flags, st, pre);
+  if (a.v.rows <= 128) return product_few<128>(a, b, out, flags, st, pre);
+  // 256 x 256 tiles on pairs of SMs move half the bytes per flop of 128 x 128 tiles, but there are a quarter as many.  A
+  // round of them takes one and a half times as long: 768 x 4096 x 4096 (2 rounds or 1) 14.2 us single, 11.4 us in pairs;
+  // 384 x 4096 x 4096 (1 or 1) 9.1 us single, 10.8 us in pairs; 16384 x 8192 x 8192 532 and 360 us.
   TilePlanMx4 t;
-  int rc = plan_tiles<128, 1>(a, b, out->data, flags, &t);
+  const auto tiles = [&](int64_t side) { return ((a.v.rows + side - 1) / side) * ((b.v.rows + side - 1) / side); };
+  const auto rounds = [](int64_t n, int64_t at_once) { return (n + at_once - 1) / at_once; };
+  const bool pairs = 3 * rounds(tiles(256), num_sms() / 2) <= 2 * rounds(tiles(128), num_sms());
+  int rc = pairs ? plan_tiles<256, 2>(a, b, out->data, flags, &t) : plan_tiles<128, 1>(a, b, out->data, flags, &t);
   if (rc) return rc;
   rc = pre();
   if (rc) return rc;
-  return run_tiles<128, 1>(t, st);
+  return pairs ? run_tiles<256, 2>(t, st) : run_tiles<128, 1>(t, st);
 }
 
 size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
