@@ -180,31 +180,36 @@ struct AttendParams {
   int64_t q_pitch;
   int T, heads, group;   // group = heads / kv_heads
   int rows, row_blocks;  // rows = T * group
+  int R, tile;           // rows per row block, tokens per tile
   int grid;
+  int min_share;         // tiles that a block takes at least
   float scale_log2;      // softmax scale * log2(e)
   int out_bf16;
 };
 
-// Tokens that the rows of row block rb can see at most.
-__device__ __forceinline__ int seen_by(int len, int T, int group, int rows, int rb, int R) {
-  const int last = min(rows, (rb + 1) * R) - 1;
-  return min(max(len - T + last / group + 1, 0), len);
+// Tokens that the rows of row block rb can see at most, and the tiles that hold them.
+__device__ __forceinline__ int seen_by(const AttendParams& p, int len, int rb) {
+  const int last = min(p.rows, (rb + 1) * p.R) - 1;
+  return min(max(len - p.T + last / p.group + 1, 0), len);
+}
+__device__ __forceinline__ int seen_tiles(const AttendParams& p, int len, int rb) {
+  return (seen_by(p, len, rb) + p.tile - 1) / p.tile;
 }
 
 // Tiles of one kv head of sequence b over all row blocks.
-__device__ __forceinline__ int64_t head_tiles(const AttendParams& p, int b, int R) {
+__device__ __forceinline__ int64_t head_tiles(const AttendParams& p, int b) {
   const int len = clamped_length(p.c, b);
   int64_t n = 0;
-  for (int rb = 0; rb < p.row_blocks; ++rb) n += (seen_by(len, p.T, p.group, p.rows, rb, R) + kTileTok - 1) / kTileTok;
+  for (int rb = 0; rb < p.row_blocks; ++rb) n += seen_tiles(p, len, rb);
   return n;
 }
 
 // Sum of head_tiles over the sequences before `upto` and over all of them, by the whole block.
 template <int THREADS>
-__device__ __forceinline__ void sum_tiles(const AttendParams& p, int R, int upto, int64_t* before, int64_t* all, int64_t* scratch) {
+__device__ __forceinline__ void sum_tiles(const AttendParams& p, int upto, int64_t* before, int64_t* all, int64_t* scratch) {
   int64_t a = 0, b = 0;
   for (int i = threadIdx.x; i < p.c.batch; i += THREADS) {
-    const int64_t n = head_tiles(p, i, R);
+    const int64_t n = head_tiles(p, i);
     a += n;
     if (i < upto) b += n;
   }
@@ -225,10 +230,60 @@ __device__ __forceinline__ void sum_tiles(const AttendParams& p, int R, int upto
   *before = b * p.c.kv_heads;
 }
 
-// Tiles per block: an even share, but no less than one tile for every warp.
-__device__ __forceinline__ int64_t block_share(int64_t all, int grid) {
-  const int64_t n = (all + grid - 1) / grid;
-  return n < kWarps ? kWarps : n;
+// Tiles per block: an even share, but no less than min_share.
+__device__ __forceinline__ int64_t block_share(const AttendParams& p, int64_t all) {
+  const int64_t n = (all + p.grid - 1) / p.grid;
+  return n < p.min_share ? p.min_share : n;
+}
+
+// A block's way through its part of the list: one (sequence, kv head, row block) after the other, tiles t0 .. t1 of the
+// n_seg that it has.
+struct Walk {
+  int64_t at, end, seg0, per_head;
+  int b, h, rb, t0, t1, n_seg, len, seen;
+
+  __device__ __forceinline__ void start(const AttendParams& p, int64_t all, int block) {
+    const int64_t share = block_share(p, all);
+    at = block * share;
+    end = min(all, at + share);
+    b = 0;
+    seg0 = 0;
+    per_head = at < end ? head_tiles(p, 0) : 0;
+  }
+  __device__ __forceinline__ bool next(const AttendParams& p) {
+    if (at >= end) return false;
+    while (seg0 + per_head * p.c.kv_heads <= at) {
+      if (b + 1 >= p.c.batch) return false;   // (only if lengths changed under the kernel)
+      seg0 += per_head * p.c.kv_heads;
+      per_head = head_tiles(p, ++b);
+    }
+    len = clamped_length(p.c, b);
+    h = static_cast<int>((at - seg0) / per_head);
+    int64_t s0 = seg0 + h * per_head;
+    for (rb = 0;; ++rb) {
+      n_seg = seen_tiles(p, len, rb);
+      if (s0 + n_seg > at || rb + 1 == p.row_blocks) break;
+      s0 += n_seg;
+    }
+    t0 = static_cast<int>(at - s0);
+    t1 = static_cast<int>(min(end - s0, static_cast<int64_t>(n_seg)));
+    seen = seen_by(p, len, rb);
+    at = s0 + t1;
+    return t1 > t0;
+  }
+  __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == n_seg; }
+  // where this block's part of a segment that it does not have to itself goes: it is the block's last or its first
+  __device__ __forceinline__ float* slot(const AttendParams& p, int D) const {
+    return p.part + (static_cast<int64_t>(blockIdx.x) * 2 + (t0 == 0 ? 1 : 0)) * p.R * (D + 2);
+  }
+};
+
+// Element 0 of the result row of query row `row` of (b, h).
+__device__ __forceinline__ int64_t out_row(const AttendParams& p, int b, int h, int row, int D) {
+  return ((static_cast<int64_t>(b) * p.T + row / p.group) * p.heads + static_cast<int64_t>(h) * p.group + row % p.group) * D;
+}
+__device__ __forceinline__ const uint16_t* q_row(const AttendParams& p, int b, int h, int row, int D) {
+  return p.q + (static_cast<int64_t>(b) * p.T + row / p.group) * p.q_pitch + (static_cast<int64_t>(h) * p.group + row % p.group) * D;
 }
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -294,9 +349,9 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
   pdl_wait();
   pdl_launch_dependents();
   int64_t all, before;
-  sum_tiles<kWarps * 32>(p, R, 0, &before, &all, scratch);   // (its barrier also publishes the ones set up above)
-  const int64_t share = block_share(all, p.grid);
-  const int64_t begin = blockIdx.x * share, end = min(all, begin + share);
+  sum_tiles<kWarps * 32>(p, 0, &before, &all, scratch);   // (its barrier also publishes the ones set up above)
+  Walk w;
+  w.start(p, all, blockIdx.x);
 
   const uint32_t my_ring = smem_u32(ring) + warp * kStagesAt * Cfg::kStage;
   const unsigned char* my_gen = ring + warp * kStagesAt * Cfg::kStage;
@@ -304,36 +359,8 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
   uint32_t slot_in = 0, slot_out = 0, phase_out = 0;
   bool ok = true;
 
-  // position in the list: sequence b, kv head h, row block rb, first tile of the segment `seg0`
-  int b = 0;
-  int64_t seg0 = 0, per_head = 0;
-  if (begin < end) {
-    for (;; ++b) {   // (block-uniform; batch is small next to the tiles)
-      per_head = head_tiles(p, b, R);
-      if (seg0 + per_head * p.c.kv_heads > begin) break;
-      seg0 += per_head * p.c.kv_heads;
-    }
-  }
-  int64_t at = begin;
-  while (at < end) {
-    // segment that holds tile `at`
-    while (seg0 + per_head * p.c.kv_heads <= at) {
-      seg0 += per_head * p.c.kv_heads;
-      per_head = head_tiles(p, ++b, R);
-    }
-    const int len = clamped_length(p.c, b);
-    const int h = static_cast<int>((at - seg0) / per_head);
-    int64_t s0 = seg0 + h * per_head;
-    int rb = 0, n_seg;
-    for (;; ++rb) {
-      n_seg = (seen_by(len, p.T, p.group, p.rows, rb, R) + kTileTok - 1) / kTileTok;
-      if (s0 + n_seg > at) break;
-      s0 += n_seg;
-    }
-    const int t0 = static_cast<int>(at - s0);
-    const int t1 = static_cast<int>(min(end - s0, static_cast<int64_t>(n_seg)));
-    const int seen = seen_by(len, p.T, p.group, p.rows, rb, R);
-    at = s0 + t1;
+  while (w.next(p)) {
+    const int b = w.b, h = w.h, rb = w.rb, t0 = w.t0, t1 = w.t1, len = w.len, seen = w.seen;
 
     // ---- ring of this warp: tiles t0 + warp, + kWarps, ...
     uint32_t there = 0;   // two bits per tile in flight: its groups that have a page (oldest tile lowest)
@@ -379,7 +406,7 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
       const int row = rb * R + r;
       const bool live = row < p.rows;
       const uint16_t* src = nullptr;
-      if (live) src = p.q + (static_cast<int64_t>(b) * p.T + row / p.group) * p.q_pitch + (static_cast<int64_t>(h) * p.group + row % p.group) * D;
+      if (live) src = q_row(p, b, h, row, D);
       float x[NB];
       uint32_t top = 0;
 #pragma unroll
@@ -573,19 +600,19 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
             float c0[4] = {0.f, 0.f, 0.f, 0.f}, c1[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int mt = 0; mt < 2; ++mt) {
-              uint32_t w[2], wl[2];
+              uint32_t wh[2], wl[2];
 #pragma unroll
               for (int hf = 0; hf < 2; ++hf) {
                 const float x = s[mt][n][2 * hf] * fac[mt][hf], y = s[mt][n][2 * hf + 1] * fac[mt][hf];
                 const uint32_t packed = pack_f16x2(x, y);
-                w[hf] = transpose8x8(packed);
+                wh[hf] = transpose8x8(packed);
                 if (HILO) {
                   const __half2 r = *reinterpret_cast<const __half2*>(&packed);
                   wl[hf] = transpose8x8(pack_f16x2(x - __low2float(r), y - __high2float(r)));
                 }
               }
-              mma_f16(c0, va[mt][0], w[0], w[1]);
-              mma_f16(c1, va[mt][1], w[0], w[1]);
+              mma_f16(c0, va[mt][0], wh[0], wh[1]);
+              mma_f16(c1, va[mt][1], wh[0], wh[1]);
               if (HILO) {
                 mma_f16(c0, va[mt][0], wl[0], wl[1]);
                 mma_f16(c1, va[mt][1], wl[0], wl[1]);
@@ -653,8 +680,8 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
             *reinterpret_cast<float2*>(row + i * 32 + 4 * g + 2 * k) = make_float2(acc[n][i][k][c], acc[n][i][k][2 + c]);
       }
     __syncthreads();
-    const bool whole = t0 == 0 && t1 == n_seg;
-    float* slot = p.part + (static_cast<int64_t>(blockIdx.x) * 2 + (t0 == 0 ? 1 : 0)) * R * (D + 2);
+    const bool whole = w.whole();
+    float* slot = w.slot(p, D);
     for (int e = threadIdx.x; e < R * (D / 4); e += kWarps * 32) {
       const int r = e / (D / 4), d = e % (D / 4) * 4;
       const int row = rb * R + r;
@@ -677,7 +704,7 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
         if (d == 0) *reinterpret_cast<float2*>(slot + r * (D + 2)) = make_float2(top, sum);
       } else if (row < p.rows) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        const int64_t to = ((static_cast<int64_t>(b) * p.T + row / p.group) * p.heads + static_cast<int64_t>(h) * p.group + row % p.group) * D + d;
+        const int64_t to = out_row(p, b, h, row, D) + d;
         if (p.out_bf16)
           *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + to) =
               make_uint2(pack_bf16x2(__float_as_uint(o.x * inv), __float_as_uint(o.y * inv)),
@@ -693,23 +720,26 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
   }
 }
 
-// Segments that several blocks share, in block order; zeros for segments without a tile.  One block per segment.
-__global__ void __launch_bounds__(128) attend_join(const AttendParams p, int D, int R) {
+// Segments that several blocks share, in block order; zeros for segments without a tile.  A block per segment and 32 rows.
+constexpr int kJoinRows = 32;
+
+__global__ void __launch_bounds__(128) attend_join(const AttendParams p, int D) {
   __shared__ int64_t scratch[8];
   pdl_wait();
   pdl_launch_dependents();
   const int rb = static_cast<int>(blockIdx.x) % p.row_blocks, bh = static_cast<int>(blockIdx.x) / p.row_blocks;
   const int b = bh / p.c.kv_heads, h = bh % p.c.kv_heads;
   int64_t all, first;
-  sum_tiles<128>(p, R, b, &first, &all, scratch);
-  const int64_t share = block_share(all, p.grid);
+  sum_tiles<128>(p, b, &first, &all, scratch);
+  const int64_t share = block_share(p, all);
   const int len = clamped_length(p.c, b);
-  first += h * head_tiles(p, b, R);
-  for (int i = 0; i < rb; ++i) first += (seen_by(len, p.T, p.group, p.rows, i, R) + kTileTok - 1) / kTileTok;
-  const int n = (seen_by(len, p.T, p.group, p.rows, rb, R) + kTileTok - 1) / kTileTok;
+  first += h * head_tiles(p, b);
+  for (int i = 0; i < rb; ++i) first += seen_tiles(p, len, i);
+  const int n = seen_tiles(p, len, rb);
   const int64_t c0 = first / share, c1 = n ? (first + n - 1) / share : c0;
   if (n && c0 == c1) return;   // written by the block that had all of it
-  for (int e = threadIdx.x; e < R * (D / 4); e += 128) {
+  const int R = p.R, r_end = min(R, (static_cast<int>(blockIdx.y) + 1) * kJoinRows);
+  for (int e = threadIdx.x + static_cast<int>(blockIdx.y) * kJoinRows * (D / 4); e < r_end * (D / 4); e += 128) {
     const int r = e / (D / 4), d = e % (D / 4) * 4;
     const int row = rb * R + r;
     if (row >= p.rows) break;
@@ -727,7 +757,7 @@ __global__ void __launch_bounds__(128) attend_join(const AttendParams p, int D, 
         top = t;
       }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    const int64_t to = ((static_cast<int64_t>(b) * p.T + row / p.group) * p.heads + static_cast<int64_t>(h) * p.group + row % p.group) * D + d;
+    const int64_t to = out_row(p, b, h, row, D) + d;
     if (p.out_bf16)
       *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + to) =
           make_uint2(pack_bf16x2(__float_as_uint(o.x * inv), __float_as_uint(o.y * inv)),
@@ -736,6 +766,12 @@ __global__ void __launch_bounds__(128) attend_join(const AttendParams p, int D, 
       *reinterpret_cast<float4*>(static_cast<float*>(p.out) + to) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
   }
 }
+
+}  // namespace
+
+#include "gl_attend_many.cuh"
+
+namespace {
 
 // ---- host side ----
 
@@ -806,39 +842,46 @@ int tokens_params(const gl_cache4* cache, const gl_ap* k, const gl_ap* v, int64_
   return GL_OK;
 }
 
-// Rows per work item: 8, 16 or 32, as many as there are (fewer registers for 256-wide heads).
-int row_tiles(int64_t rows, int d) {
-  if (rows <= 8) return 1;
-  if (rows <= 16 || d == 256) return 2;
-  return 4;
-}
-
-struct AttKernel { void (*fn)(AttendParams); int smem; };
+// Which kernel runs, and its numbers.
+struct AttKernel {
+  void (*fn)(AttendParams);
+  int smem, threads;
+  int rows, tile, min_share;   // rows per work item, tokens per tile, tiles that a block takes at least
+  int per_sm;                  // most blocks per SM
+};
 
 template <int NB, int NT>
-AttKernel att_kernel(bool hilo) {
-  return {hilo ? attend_cache4<NB, NT, true> : attend_cache4<NB, NT, false>, AttCfg<NB, NT>::kSmem};
+AttKernel few_kernel(bool hilo) {
+  return {hilo ? attend_cache4<NB, NT, true> : attend_cache4<NB, NT, false>, AttCfg<NB, NT>::kSmem, kWarps * 32, 8 * NT, kTileTok,
+          kWarps, 4};
+}
+template <int NB>
+AttKernel many_kernel(bool f32) {
+  if (f32) return {attend_many<NB, 3>, ManyCfg<NB, 3>::kSmem, ManyCfg<NB, 3>::kThreads, ManyCfg<NB, 3>::kRows, ManyCfg<NB, 3>::TT, 1, 1};
+  return {attend_many<NB, 1>, ManyCfg<NB, 1>::kSmem, ManyCfg<NB, 1>::kThreads, ManyCfg<NB, 1>::kRows, ManyCfg<NB, 1>::TT, 1, 1};
 }
 
-AttKernel pick_kernel(int d, int nt, bool hilo) {
-  if (d == 64) return nt == 1 ? att_kernel<2, 1>(hilo) : nt == 2 ? att_kernel<2, 2>(hilo) : att_kernel<2, 4>(hilo);
-  if (d == 128) return nt == 1 ? att_kernel<4, 1>(hilo) : nt == 2 ? att_kernel<4, 2>(hilo) : att_kernel<4, 4>(hilo);
-  return nt == 1 ? att_kernel<8, 1>(hilo) : att_kernel<8, 2>(hilo);
+// Up to 32 rows that share a kv head: 8, 16 or 32 of them per warp tile (256-wide heads: 16, two items for more);
+// more rows: 128 or 256 per block on tcgen05.
+AttKernel pick_kernel(int64_t rows, int d, bool f32) {
+  if (rows > 32) return d == 64 ? many_kernel<2>(f32) : d == 128 ? many_kernel<4>(f32) : many_kernel<8>(f32);
+  const int nt = rows <= 8 ? 1 : rows <= 16 || d == 256 ? 2 : 4;
+  if (d == 64) return nt == 1 ? few_kernel<2, 1>(f32) : nt == 2 ? few_kernel<2, 2>(f32) : few_kernel<2, 4>(f32);
+  if (d == 128) return nt == 1 ? few_kernel<4, 1>(f32) : nt == 2 ? few_kernel<4, 2>(f32) : few_kernel<4, 4>(f32);
+  return nt == 1 ? few_kernel<8, 1>(f32) : few_kernel<8, 2>(f32);
 }
-
-constexpr int kMaxBlocksPerSm = 4;
 
 // Blocks of the persistent grid: what is resident at once.
-int att_grid(const AttKernel& k, int d, int nt, bool hilo, int* grid) {
-  static int cached[64][3][3][2];   // per device; benign race: the calls are idempotent
+int att_grid(const AttKernel& k, int d, bool f32, int* grid) {
+  static int cached[64][3][5][2];   // per device; benign race: the calls are idempotent
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return GL_ERR_CUDA;
-  int& n = cached[dev][d == 64 ? 0 : d == 128 ? 1 : 2][nt == 4 ? 2 : nt - 1][hilo ? 1 : 0];
+  int& n = cached[dev][d == 64 ? 0 : d == 128 ? 1 : 2][k.rows <= 8 ? 0 : k.rows <= 16 ? 1 : k.rows <= 32 ? 2 : k.rows <= 128 ? 3 : 4][f32];
   if (!n) {
     if (cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem) != cudaSuccess) return GL_ERR_CUDA;
     int per = 0;
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, k.fn, kWarps * 32, k.smem) != cudaSuccess || per < 1) return GL_ERR_CUDA;
-    n = std::min(per, kMaxBlocksPerSm) * num_sms();
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, k.fn, k.threads, k.smem) != cudaSuccess || per < 1) return GL_ERR_CUDA;
+    n = std::min(per, k.per_sm) * num_sms();
   }
   *grid = n;
   return GL_OK;
@@ -885,8 +928,12 @@ int gl_cache4_read(const gl_cache4* cache, const gl_pages* at, gl_ap* k, gl_ap* 
 size_t gl_attend_cache4_workspace(const gl_ap* q, const gl_cache4* cache) {
   if (check_meta(q) || check_cache_meta(cache) || q->ndim != 4 || q->shape[2] % cache->kv_heads) return 0;
   const int64_t rows = q->shape[1] * (q->shape[2] / cache->kv_heads);
-  const int R = 8 * row_tiles(rows, cache->head_dim);
-  return static_cast<size_t>(kMaxBlocksPerSm) * num_sms() * 2 * R * (cache->head_dim + 2) * sizeof(float);
+  size_t most = 0;
+  for (const bool f32 : {false, true}) {
+    const AttKernel k = pick_kernel(rows, cache->head_dim, f32);
+    most = std::max(most, static_cast<size_t>(k.per_sm) * num_sms() * 2 * k.rows * (cache->head_dim + 2) * sizeof(float));
+  }
+  return most;
 }
 
 int gl_attend_cache4(const gl_ap* q, int64_t token_pitch, const gl_cache4* cache, const gl_pages* at, float scale, gl_ap* out,
@@ -909,12 +956,11 @@ int gl_attend_cache4(const gl_ap* q, int64_t token_pitch, const gl_cache4* cache
   const size_t need = gl_attend_cache4_workspace(q, cache);
   if (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 1023u)) return GL_ERR_WORKSPACE;
   const int64_t group = q->shape[2] / cache->kv_heads, rows = q->shape[1] * group;
-  const int nt = row_tiles(rows, cache->head_dim), R = 8 * nt;
-  const int64_t row_blocks = (rows + R - 1) / R, segments = q->shape[0] * cache->kv_heads * row_blocks;
-  if (rows > INT32_MAX - 64 || segments > INT32_MAX) return GL_ERR_UNSUPPORTED;
-  const bool hilo = !(flags & GL_OUT_BF16);
-  const AttKernel k = pick_kernel(cache->head_dim, nt, hilo);
-  rc = att_grid(k, cache->head_dim, nt, hilo, &p.grid);
+  const bool f32 = !(flags & GL_OUT_BF16);
+  const AttKernel k = pick_kernel(rows, cache->head_dim, f32);
+  const int64_t row_blocks = (rows + k.rows - 1) / k.rows, segments = q->shape[0] * cache->kv_heads * row_blocks;
+  if (rows > INT32_MAX - 512 || segments > INT32_MAX) return GL_ERR_UNSUPPORTED;
+  rc = att_grid(k, cache->head_dim, f32, &p.grid);
   if (rc) return rc;
   p.q = static_cast<const uint16_t*>(q->data);
   p.out = out->data;
@@ -926,11 +972,15 @@ int gl_attend_cache4(const gl_ap* q, int64_t token_pitch, const gl_cache4* cache
   p.rows = static_cast<int>(rows);
   p.row_blocks = static_cast<int>(row_blocks);
   p.scale_log2 = scale * 1.4426950408889634f;
-  p.out_bf16 = hilo ? 0 : 1;
+  p.out_bf16 = f32 ? 0 : 1;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (launch_pdl(k.fn, dim3(static_cast<unsigned>(p.grid)), dim3(kWarps * 32), static_cast<size_t>(k.smem), st, 1, p) != cudaSuccess)
+  p.R = k.rows;
+  p.tile = k.tile;
+  p.min_share = k.min_share;
+  if (launch_pdl(k.fn, dim3(static_cast<unsigned>(p.grid)), dim3(static_cast<unsigned>(k.threads)), static_cast<size_t>(k.smem), st, 1, p) != cudaSuccess)
     return GL_ERR_CUDA;
-  return launch_pdl(attend_join, dim3(static_cast<unsigned>(segments)), dim3(128), 0, st, 1, p, cache->head_dim, R) == cudaSuccess
+  return launch_pdl(attend_join, dim3(static_cast<unsigned>(segments), static_cast<unsigned>((k.rows + kJoinRows - 1) / kJoinRows)), dim3(128), 0, st, 1, p,
+                    cache->head_dim) == cudaSuccess
              ? GL_OK : GL_ERR_CUDA;
 }
 

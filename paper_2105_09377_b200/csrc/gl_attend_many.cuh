@@ -1,0 +1,478 @@
+// Attention over 4-bit pages for many query rows (prompts read in pieces): the two products on tcgen05.
+// Included by gl_attend.cu, whose cache layout, work list and joining it uses.
+//
+// A block has MT x 128 rows that share a kv head and walks along the tokens in tiles of TT.  Four warps widen the
+// tile's codes to bf16, scales included (two significant bits times a power of two: exact), into the swizzled shared-
+// memory layouts of the MMA operands: K as [token][dim] (K-major B of S = Q K^T), V as [token][dim] too, which is the
+// MN-major B of O = P V.  Scores come back from tensor memory a row per thread, are turned into weights and go back
+// into the columns they came from, as the A operand of the second product.  The maximum that the weights refer to is
+// moved only when a row's scores exceed it by 2^8, so that O is rarely rescaled.  MT = 2: while the softmax warps
+// of one half work, the tensor core works for the other.
+// TERMS = 1 rounds the weights to bf16 (8 bits; the result is bf16 too); TERMS = 3 carries them as three bf16 terms
+// for fp32 results.
+//
+// Dims appear in operand order: the conversion of a 32-bit word yields pairs (i, i + 4) for K, where Q's rows are
+// stored in the same order, and pairs of neighbouring blocks for V, undone when the result is stored.
+#pragma once
+
+namespace {
+
+template <int NB, int TERMS>
+struct ManyCfg {
+  static constexpr int D = 32 * NB;
+  static constexpr int MT = (NB <= 4 && TERMS == 1) ? 2 : 1;
+  static constexpr int TT = NB == 8 ? 64 : 128;                 // tokens per tile
+  static constexpr int kRows = 128 * MT;
+  static constexpr int kQ = 128 * D * 2;                        // bytes of one Q tile
+  static constexpr int kKV = TT * D * 2;                        // bytes of a K or V tile
+  static constexpr int kStages = 2;
+  static constexpr int kWarps = 4 * MT + 5;
+  static constexpr int kThreads = 32 * kWarps;
+  static constexpr int kSmem = MT * kQ + kStages * 2 * kKV + 1024 + 512;
+  // tensor memory: scores (weights take their place), third terms, results
+  static constexpr int kS = 0;
+  static constexpr int kLow = MT * TT;
+  static constexpr int kO = 512 - MT * D;
+  static_assert(kLow + (TERMS == 3 ? TT / 2 : 0) <= kO, "tensor memory");
+  static_assert(kSmem <= 232448, "shared memory");
+};
+
+// D[tmem] (+)= A[tmem] * B[smem]: A is a row per lane, two bf16 values per column
+__device__ __forceinline__ void tc_mma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tc_store_16cols(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tc_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// bf16x2 multiplication that keeps subnormals
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(0x80008000u));
+  return d;
+}
+// bf16 bits of 2^k, -127 <= k <= 127
+__device__ __forceinline__ uint32_t bf16_pow2(int k) { return k > -127 ? static_cast<uint32_t>(k + 127) << 7 : 0x0040u; }
+
+// Eight codes (pairs: code i of the low and of the high half) -> four bf16 pairs, times 2^(elo - 127) and 2^(ehi - 127).
+// Moved into the low exponent bits of a bf16 a code reads as its value times 2^-126, subnormals included.
+__device__ __forceinline__ uint4 mx4_pairs_bf16(uint32_t z, uint32_t elo, uint32_t ehi) {
+  uint32_t h[4];
+  h[0] = ((z << 12) & 0x80008000u) | ((z << 6) & 0x01C001C0u);
+  h[1] = ((z << 8) & 0x80008000u) | ((z << 2) & 0x01C001C0u);
+  h[2] = ((z << 4) & 0x80008000u) | ((z >> 2) & 0x01C001C0u);
+  h[3] = (z & 0x80008000u) | ((z >> 6) & 0x01C001C0u);
+  // 2^(e - 1) is a bf16 up to e = 128; larger scales in two steps
+  const uint32_t f = bf16_pow2(min(static_cast<int>(elo), 128) - 1) | bf16_pow2(min(static_cast<int>(ehi), 128) - 1) << 16;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) h[i] = mul_bf16x2(h[i], f);
+  if (max(elo, ehi) > 128u) {
+    const uint32_t lo = elo == 255u ? 0x7FC0u : bf16_pow2(elo > 128u ? static_cast<int>(elo) - 128 : 0);
+    const uint32_t hi = ehi == 255u ? 0x7FC0u : bf16_pow2(ehi > 128u ? static_cast<int>(ehi) - 128 : 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = mul_bf16x2(h[i], lo | hi << 16);
+  }
+  return make_uint4(h[0], h[1], h[2], h[3]);
+}
+
+// What a widening thread holds of a tile: its codes and scales of one of K and V.
+template <int NB, int ITEMS>
+struct Held {
+  uint32_t word[ITEMS][NB];
+  uint32_t exps[ITEMS][NB <= 4 ? 1 : 2];
+  uint32_t live;   // one bit per item: the token exists and is seen by some row
+};
+
+template <int NB, int TERMS>
+__global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(const AttendParams p) {
+  using Cfg = ManyCfg<NB, TERMS>;
+  constexpr int D = Cfg::D, MT = Cfg::MT, TT = Cfg::TT, kGroups = TT / 16;
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  unsigned char* gen = smem_raw + (base - raw);
+  const uint32_t q_at = base, kv_at = base + MT * Cfg::kQ;       // stage s: K at kv_at + 2 s kKV, V behind it
+  unsigned char* tail = gen + MT * Cfg::kQ + Cfg::kStages * 2 * Cfg::kKV;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(tail);
+  const uint32_t bar = smem_u32(bars);
+  const uint32_t b_kfull = bar, b_kempty = bar + 16, b_vfull = bar + 32, b_vempty = bar + 48, b_q = bar + 64, b_s = bar + 80,
+                 b_p = bar + 96, b_o = bar + 112;                // two each
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 16);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  volatile uint32_t* have = reinterpret_cast<volatile uint32_t*>(tmem_slot + 2);   // [4] groups of a tile that have a page
+  int* nan_from = reinterpret_cast<int*>(tmem_slot + 6);                           // [4][NB] first token whose V block is NaN
+  int64_t* scratch = reinterpret_cast<int64_t*>(tail + 288);                       // [2 * kWarps]
+  static_assert(288 + 16 * Cfg::kWarps <= 512 && 128 + 24 + 16 * 8 <= 288, "tail");
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr int kWiden = 4 * MT, kMma = 4 * MT + 4;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(b_kfull + 8 * i, 4);
+      mbar_init(b_vfull + 8 * i, 4);
+      mbar_init(b_kempty + 8 * i, 1);
+      mbar_init(b_vempty + 8 * i, 1);
+      mbar_init(b_q + 8 * i, 4);
+      mbar_init(b_s + 8 * i, 1);
+      mbar_init(b_p + 8 * i, 4);
+      mbar_init(b_o + 8 * i, 1);
+    }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == kMma) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  pdl_wait();
+  pdl_launch_dependents();
+  int64_t all, before;
+  tc_fence_before();
+  sum_tiles<Cfg::kThreads>(p, 0, &before, &all, scratch);   // (its barrier also publishes the set-up above)
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  Walk w;
+  w.start(p, all, blockIdx.x);
+  uint32_t it = 0;     // tiles so far, the same for every role
+  uint32_t item = 0;
+  bool ok = true;
+
+  if (warp < kWiden) {
+    // ---------------- softmax: thread = row ----------------
+    const int m = warp >> 2, r = (warp & 3) * 32 + lane;
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t s_col = tmem + lanes + Cfg::kS + m * TT, o_col = tmem + lanes + Cfg::kO + m * D;
+    const uint32_t low_col = tmem + lanes + Cfg::kLow;
+    const float cf = p.scale_log2, ninf = __uint_as_float(0xFF800000u);
+    for (; ok && w.next(p); ++item) {
+      const int row = w.rb * Cfg::kRows + m * 128 + r;
+      const bool live = row < p.rows;
+      // Q: dims 8c .. 8c + 7 in the order 0 4 1 5 2 6 3 7, 128-byte swizzle
+      {
+        const uint16_t* src = live ? q_row(p, w.b, w.h, row, D) : nullptr;
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c) {
+          uint4 x = live ? *reinterpret_cast<const uint4*>(src + 8 * c) : make_uint4(0, 0, 0, 0);
+          const uint4 y = make_uint4(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632), __byte_perm(x.y, x.w, 0x5410),
+                                     __byte_perm(x.y, x.w, 0x7632));
+          *reinterpret_cast<uint4*>(gen + m * Cfg::kQ + (c >> 3) * 16384 + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = y;
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_q + 8 * m);
+      }
+      const int limit = live ? min(w.len, w.len - p.T + row / p.group + 1) : 0;
+      float ref = ninf, sum = 0.f;
+      for (int tile = w.t0; tile < w.t1; ++tile, ++it) {
+        if (!mbar_wait(b_s + 8 * m, it & 1u, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        const int open = limit - tile * TT;           // columns that this row sees
+        const uint32_t groups = have[it & 3u];
+        const bool masked = __any_sync(0xFFFFFFFFu, open < TT) || groups != (1u << kGroups) - 1u;
+        float top = ninf;
+#pragma unroll 1
+        for (int j = 0; j < TT / 32; ++j) {
+          uint32_t x[32];
+          tc_load_32cols(s_col + 32 * j, x);
+          if (masked) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (32 * j + i < open && (groups >> (2 * j + (i >> 4)) & 1u)) top = fmaxf(top, __uint_as_float(x[i]));
+          } else {
+            float t1 = ninf, t2 = ninf, t3 = ninf;
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) {
+              top = fmaxf(top, __uint_as_float(x[i]));
+              t1 = fmaxf(t1, __uint_as_float(x[i + 1]));
+              t2 = fmaxf(t2, __uint_as_float(x[i + 2]));
+              t3 = fmaxf(t3, __uint_as_float(x[i + 3]));
+            }
+            top = fmaxf(fmaxf(top, t1), fmaxf(t2, t3));
+          }
+        }
+        top *= cf;
+        const bool move = top > ref + 8.f || ref == ninf;
+        const float new_ref = move ? fmaxf(top, ref) : ref;
+        if (__any_sync(0xFFFFFFFFu, move && new_ref != ref) && tile > w.t0) {
+          // O holds the tiles before this one: bring it to the new reference
+          if (!mbar_wait(b_o + 8 * m, (it - 1) & 1u, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+          const float f = new_ref == ref ? 1.f : ex2(ref - new_ref);
+          sum *= f;
+#pragma unroll 1
+          for (int j = 0; j < D / 16; ++j) {
+            uint32_t x[16];
+            tc_load_16cols(o_col + 16 * j, x);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * f);
+            tc_store_16cols(o_col + 16 * j, x);
+          }
+        }
+        ref = new_ref;
+        const float off = ref == ninf ? 0.f : ref;
+        float part = 0.f, part2 = 0.f;
+#pragma unroll 1
+        for (int j = 0; j < TT / 32; ++j) {
+          uint32_t x[32], hi[16], mid[16], lo[16];
+          tc_load_32cols(s_col + 32 * j, x);
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            float a = ex2(fmaf(__uint_as_float(x[i]), cf, -off)), b = ex2(fmaf(__uint_as_float(x[i + 1]), cf, -off));
+            if (masked) {
+              const bool there = groups >> (2 * j + (i >> 4)) & 1u;
+              a = there && 32 * j + i < open ? a : 0.f;
+              b = there && 32 * j + i + 1 < open ? b : 0.f;
+            }
+            part += a;
+            part2 += b;
+            hi[i / 2] = pack_bf16x2(__float_as_uint(a), __float_as_uint(b));
+            if (TERMS == 3) {
+              a -= __uint_as_float(hi[i / 2] << 16);
+              b -= __uint_as_float(hi[i / 2] & 0xFFFF0000u);
+              mid[i / 2] = pack_bf16x2(__float_as_uint(a), __float_as_uint(b));
+              a -= __uint_as_float(mid[i / 2] << 16);
+              b -= __uint_as_float(mid[i / 2] & 0xFFFF0000u);
+              lo[i / 2] = pack_bf16x2(__float_as_uint(a), __float_as_uint(b));
+            }
+          }
+          tc_store_16cols(s_col + 32 * j, hi);
+          if (TERMS == 3) {
+            tc_store_16cols(s_col + 32 * j + 16, mid);
+            tc_store_16cols(low_col + 16 * j, lo);
+          }
+        }
+        sum += part + part2;
+        tc_wait_store();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_p + 8 * m);
+      }
+      if (!ok) break;
+      // ---- result of the item
+      if (!mbar_wait(b_o + 8 * m, (it - 1) & 1u, abort_flag)) { ok = false; break; }
+      tc_fence_after();
+      const bool whole = w.whole();
+      const float inv = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
+      float* slot = w.slot(p, D) + static_cast<int64_t>(m * 128 + r) * (D + 2);
+      const int64_t to = live ? out_row(p, w.b, w.h, row, D) : 0;
+      if (!whole) *reinterpret_cast<float2*>(slot) = make_float2(ref, sum);
+      const int* nan_at = nan_from + (item & 3u) * NB;
+      // columns (g * NB/2 + w) * 8 + 2 i + half hold dims 32 (2 w + half) + 4 g + i
+#pragma unroll 1
+      for (int c = 0; c < D / 16; ++c) {
+        uint32_t x[16];
+        tc_load_16cols(o_col + 16 * c, x);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int word = 2 * c + k, g = word / (NB / 2), wd = word % (NB / 2);
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const int block = 2 * wd + half, d = 32 * block + 4 * g;
+            float v[4];
+            const bool bad = nan_at[block] < limit;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              v[i] = bad ? __uint_as_float(0x7FC00000u) : __uint_as_float(x[8 * k + 2 * i + half]) * inv;
+            if (!whole) {
+              *reinterpret_cast<float2*>(slot + d + 2) = make_float2(v[0], v[1]);
+              *reinterpret_cast<float2*>(slot + d + 4) = make_float2(v[2], v[3]);
+            } else if (live) {
+              if (p.out_bf16)
+                *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + to + d) =
+                    make_uint2(pack_bf16x2(__float_as_uint(v[0]), __float_as_uint(v[1])),
+                               pack_bf16x2(__float_as_uint(v[2]), __float_as_uint(v[3])));
+              else
+                *reinterpret_cast<float4*>(static_cast<float*>(p.out) + to + d) = make_float4(v[0], v[1], v[2], v[3]);
+            }
+          }
+        }
+      }
+      tc_fence_before();
+    }
+  } else if (warp < kMma) {
+    // ---------------- widening: codes from the pages to bf16 operands ----------------
+    constexpr int kItems = TT / 32;
+    const int dw = warp - kWiden, j = lane >> 3;
+    for (; ok && w.next(p); ++item) {
+      if (dw == 0 && lane < NB) nan_from[(item & 3u) * NB + lane] = INT32_MAX;
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+      Held<NB, kItems> hk, hv;
+      uint32_t tile_have = 0;
+      const uint8_t* group[kItems];
+      // page of group `lane` of the tile, then this thread's tokens
+      auto find = [&](int tile) {
+        int32_t page = -1;
+        const int pos = tile * TT + lane * 16;
+        if (lane < kGroups && pos < w.seen) page = p.c.table[static_cast<int64_t>(w.b) * p.c.width + pos / p.c.page_tokens];
+        const bool there = page >= 0 && page < p.c.pages;
+        tile_have = __ballot_sync(0xFFFFFFFFu, there);
+        hk.live = 0;
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+          const int g = 2 * i + (dw >> 1), tok = 32 * i + dw * 8 + (lane & 7);
+          const int32_t pg = __shfl_sync(0xFFFFFFFFu, page, g);
+          const int at = tile * TT + g * 16;
+          group[i] = p.c.data + static_cast<int64_t>(pg) * p.c.page_stride + w.h * p.c.head_stride +
+                     static_cast<int64_t>(at % p.c.page_tokens / kGroup) * group_bytes(D);
+          if ((tile_have >> g & 1u) && tile * TT + tok < w.seen) hk.live |= 1u << i;
+        }
+        hv.live = hk.live;
+      };
+      auto fetch = [&](Held<NB, kItems>& x, int codes_at, int scales_at, bool is_v) {
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+          const int tok = (dw * 8 + (lane & 7)) & 15;   // place in its group
+          const int part = is_v ? j ^ ((tok & 2) ? 2 : 0) : j;
+          const uint8_t* src = group[i] + codes_at + tok * (D / 2) + part * NB * 4;
+          const uint8_t* sc = group[i] + scales_at + tok * NB;
+#pragma unroll
+          for (int k = 0; k < NB; ++k) x.word[i][k] = 0;
+          x.exps[i][0] = 0;
+          if (NB == 8) x.exps[i][NB == 8 ? 1 : 0] = 0;
+          if (x.live >> i & 1u) {
+            if (NB == 2) {
+              const uint2 a = *reinterpret_cast<const uint2*>(src);
+              x.word[i][0] = a.x; x.word[i][1] = a.y;
+              x.exps[i][0] = *reinterpret_cast<const uint16_t*>(sc);
+            } else {
+#pragma unroll
+              for (int k = 0; k < NB / 4; ++k) {
+                const uint4 a = *reinterpret_cast<const uint4*>(src + 16 * k);
+                x.word[i][4 * k] = a.x; x.word[i][4 * k + 1] = a.y; x.word[i][4 * k + 2] = a.z; x.word[i][4 * k + 3] = a.w;
+              }
+              x.exps[i][0] = *reinterpret_cast<const uint32_t*>(sc);
+              if (NB == 8) x.exps[i][NB == 8 ? 1 : 0] = *reinterpret_cast<const uint32_t*>(sc + 4);
+            }
+          }
+        }
+      };
+      find(w.t0);
+      fetch(hk, 0, k_scales_at(D), false);
+      fetch(hv, v_codes_at(D), v_scales_at(D), true);
+      for (int tile = w.t0; tile < w.t1; ++tile, ++it) {
+        const uint32_t st = it & 1u, ph = (it >> 1) & 1u;
+        const uint32_t now_have = tile_have;
+        if (!mbar_wait(b_kempty + 8 * st, ph ^ 1u, abort_flag)) { ok = false; break; }
+        if (dw == 0 && lane == 0) have[it & 3u] = now_have;
+        unsigned char* kt = gen + MT * Cfg::kQ + 2 * st * Cfg::kKV;
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+          const int tok = 32 * i + dw * 8 + (lane & 7);
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            const uint32_t e = hk.exps[i][b >> 2] >> (8 * (b & 3)) & 255u;
+            const int c = b * 4 + j;
+            *reinterpret_cast<uint4*>(kt + (c >> 3) * (TT * 128) + tok * 128 + (((c & 7) ^ (tok & 7)) << 4)) =
+                mx4_pairs_bf16(hk.word[i][b], e, e);
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_kfull + 8 * st);
+        if (!mbar_wait(b_vempty + 8 * st, ph ^ 1u, abort_flag)) { ok = false; break; }
+        unsigned char* vt = kt + Cfg::kKV;
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+          const int tok = 32 * i + dw * 8 + (lane & 7);
+#pragma unroll
+          for (int k = 0; k < NB; ++k) {
+            const int b = 2 * (k % (NB / 2)), c = j * NB + k;
+            uint32_t elo = hv.exps[i][b >> 2] >> (8 * (b & 3)) & 255u, ehi = hv.exps[i][b >> 2] >> (8 * (b & 3) + 8) & 255u;
+            uint32_t word = hv.word[i][k];
+            if (max(elo, ehi) == 255u) {   // NaN goes to the rows that see this token when the result is stored
+              if (elo == 255u) { atomicMin(nan_from + (item & 3u) * NB + b, tile * TT + tok); word &= 0xFFFF0000u; elo = 0; }
+              if (ehi == 255u) { atomicMin(nan_from + (item & 3u) * NB + b + 1, tile * TT + tok); word &= 0xFFFFu; ehi = 0; }
+            }
+            *reinterpret_cast<uint4*>(vt + (c >> 3) * (TT * 128) + tok * 128 + (((c & 7) ^ (tok & 7)) << 4)) =
+                mx4_pairs_bf16(word, elo, ehi);
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_vfull + 8 * st);
+        if (tile + 1 < w.t1) {
+          find(tile + 1);
+          fetch(hk, 0, k_scales_at(D), false);
+          fetch(hv, v_codes_at(D), v_scales_at(D), true);
+        }
+      }
+      if (!ok) break;
+    }
+  } else {
+    // ---------------- MMA issuer ----------------
+    const bool leader = elect_one();
+    constexpr uint32_t idesc_s = make_idesc(128, TT), idesc_o = make_idesc(128, D) | (1u << 16);   // V is MN-major
+    const uint64_t dq = make_desc(q_at, 16, 1024, 2), dk = make_desc(kv_at, 16, 1024, 2);
+    const uint64_t dv = make_desc(kv_at + Cfg::kKV, TT * 128, 1024, 2);
+    // S_m of tile number n (0-based over the block's life)
+    auto scores = [&](uint32_t n, int m) {
+      const uint32_t st = n & 1u;
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) {
+        const uint64_t a = dq + ((m * Cfg::kQ + (k >> 2) * 16384 + (k & 3) * 32) >> 4);
+        const uint64_t b = dk + ((2 * st * Cfg::kKV) >> 4) + (((k >> 2) * (TT * 128) + (k & 3) * 32) >> 4);
+        if (leader) tc_mma_bf16(tmem + Cfg::kS + m * TT, a, b, idesc_s, k ? 1u : 0u);
+      }
+      if (leader) tc_commit(b_s + 8 * m);
+    };
+    for (; ok && w.next(p); ++item) {
+      const int n = w.t1 - w.t0;
+      for (int m = 0; m < MT && ok; ++m) ok = mbar_wait(b_q + 8 * m, item & 1u, abort_flag);
+      if (ok) ok = mbar_wait(b_kfull + 8 * (it & 1u), (it >> 1) & 1u, abort_flag);
+      if (!ok) break;
+      tc_fence_after();
+      for (int m = 0; m < MT; ++m) scores(it, m);
+      if (leader) tc_commit(b_kempty + 8 * (it & 1u));
+      for (int t = 0; t < n && ok; ++t, ++it) {
+        const uint32_t st = it & 1u;
+        if (!mbar_wait(b_vfull + 8 * st, (it >> 1) & 1u, abort_flag)) { ok = false; break; }
+        if (t + 1 < n && !mbar_wait(b_kfull + 8 * (st ^ 1u), ((it + 1) >> 1) & 1u, abort_flag)) { ok = false; break; }
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          if (ok && !mbar_wait(b_p + 8 * m, it & 1u, abort_flag)) ok = false;
+          if (!ok) break;
+          tc_fence_after();
+#pragma unroll
+          for (int k = 0; k < TT / 16; ++k) {
+            const uint64_t b = dv + ((2 * st * Cfg::kKV) >> 4) + ((k * 2048) >> 4);
+            const uint32_t s = tmem + Cfg::kS + m * TT + 32 * (k >> 1) + 8 * (k & 1), o = tmem + Cfg::kO + m * D;
+            if (leader) {
+              tc_mma_bf16_ta(o, s, b, idesc_o, t > 0 || k > 0 ? 1u : 0u);
+              if (TERMS == 3) {
+                tc_mma_bf16_ta(o, s + 16, b, idesc_o, 1u);
+                tc_mma_bf16_ta(o, tmem + Cfg::kLow + 8 * k, b, idesc_o, 1u);
+              }
+            }
+          }
+          if (leader) tc_commit(b_o + 8 * m);
+          if (t + 1 < n) scores(it + 1, m);
+        }
+        if (ok && leader) {
+          tc_commit(b_vempty + 8 * st);
+          if (t + 1 < n) tc_commit(b_kempty + 8 * (st ^ 1u));
+        }
+      }
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kMma) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
+}  // namespace
