@@ -38,6 +38,7 @@ struct CacheView {
   int64_t head_stride, page_stride;   // bytes
   int kv_heads, page_tokens, batch, width;
   int capacity;                       // tokens a sequence can have: width * page_tokens
+  FastDiv div_page;
 };
 
 __device__ __forceinline__ int clamped_length(const CacheView& c, int b) { return min(max(c.lengths[b], 0), c.capacity); }
@@ -313,6 +314,85 @@ __device__ __forceinline__ int token_of_row(int i) {
   return (i & 8) + ((j & 1) ? 4 + ((j >> 1) ^ 1) : (j >> 1));
 }
 
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+// The codes of a word's bytes as fp16 pairs (low code, high code): one conversion instruction a byte, 1.2 cycles of an SM
+// per word of a warp; moving the bits with shifts and masks takes 3.6.
+__device__ __forceinline__ void mx4_bytes_f16(uint32_t w, uint32_t (&h)[4]) {
+  asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
+      "mov.b32 {b0, b1, b2, b3}, %4;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, b0;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %1, b1;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %2, b2;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
+      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
+}
+// N consecutive words, or half words, or scale bytes of a token
+template <int NB>
+__device__ __forceinline__ void load_words(const unsigned char* at, uint32_t (&w)[NB]) {
+  if (NB == 2) {
+    const uint2 x = *reinterpret_cast<const uint2*>(at);
+    w[0] = x.x; w[1] = x.y;
+  } else {
+#pragma unroll
+    for (int i = 0; i < NB / 4; ++i) {
+      const uint4 x = *reinterpret_cast<const uint4*>(at + 16 * i);
+      w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
+    }
+  }
+}
+template <int NB>
+__device__ __forceinline__ void load_halves(const unsigned char* at, uint32_t (&w)[NB / 2]) {
+  if (NB == 2) {
+    w[0] = *reinterpret_cast<const uint32_t*>(at);
+  } else if (NB == 4) {
+    const uint2 x = *reinterpret_cast<const uint2*>(at);
+    w[0] = x.x; w[1] = x.y;
+  } else {
+    const uint4 x = *reinterpret_cast<const uint4*>(at);
+    w[0] = x.x; w[1] = x.y; w[NB == 8 ? 2 : 0] = x.z; w[NB == 8 ? 3 : 0] = x.w;
+  }
+}
+template <int NB>
+__device__ __forceinline__ void load_scales(const unsigned char* at, uint32_t (&w)[(NB + 3) / 4]) {
+  if (NB == 2) w[0] = *reinterpret_cast<const uint16_t*>(at);
+  else if (NB == 4) w[0] = *reinterpret_cast<const uint32_t*>(at);
+  else {
+    const uint2 x = *reinterpret_cast<const uint2*>(at);
+    w[0] = x.x; w[NB == 8 ? 1 : 0] = x.y;
+  }
+}
+// Byte i of a scale word as 2^(e - 127).  (e = 255 gives Inf: a NaN block's codes are zeros, and zero times Inf is NaN.)
+__device__ __forceinline__ float scale_byte(uint32_t w, int i) {
+  const uint32_t bits = (i == 3 ? w >> 1 : w << (23 - 8 * i)) & 0x7F800000u;
+  return __uint_as_float(max(bits, 0x00400000u));
+}
+// Byte i of two words in the two halves of one
+__device__ __forceinline__ uint32_t byte_pair(uint32_t a, uint32_t b, int i) {
+  return __byte_perm(a, b, 0x0400u + 0x0101u * i) & 0x00FF00FFu;
+}
+// V of two neighbouring blocks as 16-row operands: x0..x3 hold dims 4 g .. + 3 of both blocks (low and high half) of the
+// tokens in columns 2 tq, 2 tq + 1, 2 tq + 8, 2 tq + 9.  Bytes with one token's code in each half become fp16 pairs.
+__device__ __forceinline__ void v_operands(uint32_t x0, uint32_t x1, uint32_t x2, uint32_t x3, uint32_t (&va)[2][2][4]) {
+  uint32_t e0[4], o0[4], e1[4], o1[4];   // even and odd dims of both blocks: (block 0: 0 1, block 1: 2 3)
+  mx4_bytes_f16((x0 & 0x0F0F0F0Fu) | ((x1 << 4) & 0xF0F0F0F0u), e0);
+  mx4_bytes_f16(((x0 >> 4) & 0x0F0F0F0Fu) | (x1 & 0xF0F0F0F0u), o0);
+  mx4_bytes_f16((x2 & 0x0F0F0F0Fu) | ((x3 << 4) & 0xF0F0F0F0u), e1);
+  mx4_bytes_f16(((x2 >> 4) & 0x0F0F0F0Fu) | (x3 & 0xF0F0F0F0u), o1);
+#pragma unroll
+  for (int hb = 0; hb < 2; ++hb)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {   // instruction k: row g = dim 2 k, row g + 8 = dim 2 k + 1
+      va[hb][k][0] = e0[2 * hb + k];
+      va[hb][k][1] = o0[2 * hb + k];
+      va[hb][k][2] = e1[2 * hb + k];
+      va[hb][k][3] = o1[2 * hb + k];
+    }
+}
+
 template <int NB, int NT>
 struct AttCfg {
   static constexpr int D = 32 * NB;
@@ -357,6 +437,8 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
   const unsigned char* my_gen = ring + warp * kStagesAt * Cfg::kStage;
   const uint32_t my_bar = smem_u32(bars + warp * kStagesAt);
   uint32_t slot_in = 0, slot_out = 0, phase_out = 0;
+  constexpr int kScaleWords = (NB + 3) / 4;
+  const float ninf = __uint_as_float(0xFF800000u);
   bool ok = true;
 
   while (w.next(p)) {
@@ -372,8 +454,8 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
       page_lo = page_hi = -1;
       if (tile < t1) {
         const int64_t row = static_cast<int64_t>(b) * p.c.width;
-        page_lo = p.c.table[row + pos / p.c.page_tokens];
-        if (pos + kGroup < seen) page_hi = p.c.table[row + (pos + kGroup) / p.c.page_tokens];
+        page_lo = p.c.table[row + p.c.div_page.div(pos)];
+        if (pos + kGroup < seen) page_hi = p.c.table[row + p.c.div_page.div(pos + kGroup)];
       }
     };
     auto issue = [&]() {   // copies of tile `next`, whose pages are in page_lo and page_hi
@@ -382,13 +464,16 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
       const bool lo = page_lo >= 0 && page_lo < p.c.pages, hi = page_hi >= 0 && page_hi < p.c.pages;
       if (lane == 0) {
         const uint32_t bar = my_bar + 8 * slot_in, dst = my_ring + slot_in * Cfg::kStage;
+        uint32_t slot, in_lo, in_hi;
+        p.c.div_page.divmod(pos, slot, in_lo);
+        p.c.div_page.divmod(pos + kGroup, slot, in_hi);
         mbar_expect_tx(bar, (lo ? group_bytes(D) : 0) + (hi ? group_bytes(D) : 0));
         if (lo)
           bulk_copy_g2s(dst, p.c.data + page_lo * p.c.page_stride + h * p.c.head_stride +
-                                 static_cast<int64_t>(pos % p.c.page_tokens / kGroup) * group_bytes(D), group_bytes(D), bar);
+                                 static_cast<int64_t>(in_lo / kGroup) * group_bytes(D), group_bytes(D), bar);
         if (hi)
           bulk_copy_g2s(dst + group_bytes(D), p.c.data + page_hi * p.c.page_stride + h * p.c.head_stride +
-                                 static_cast<int64_t>((pos + kGroup) % p.c.page_tokens / kGroup) * group_bytes(D), group_bytes(D), bar);
+                                 static_cast<int64_t>(in_hi / kGroup) * group_bytes(D), group_bytes(D), bar);
       }
       there |= ((lo ? 1u : 0u) | (hi ? 2u : 0u)) << (2 * in_flight);
       ++in_flight;
@@ -415,234 +500,309 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
         top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
       }
       top = __reduce_max_sync(0xFFFFFFFFu, top);
-      const int e = max(static_cast<int>(top >> 23), 27) - 127;                 // floor(log2) of the largest
+      const int e = max(static_cast<int>(top >> 23), 27) - 127;                 // floor(log2) of the largest, not below -100
       const float f = __uint_as_float(static_cast<uint32_t>(14 - e + 127 > 0 ? 14 - e + 127 : 0) << 23);
-      // lane = dim % 32: word j = lane / 8, pair lane % 4, half (lane / 4) & 1; pair 2i + s is register s of instruction i
-      const int j = lane >> 3, pr = lane & 3, half = (lane >> 2) & 1;
+      // lane = dim % 32: word j = lane / 8, byte (lane / 2) % 4 of the word; byte 2i + s is register s of instruction i
+      const int j = lane >> 3, byte = (lane >> 1) & 3, half = lane & 1;
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
-        __half* dst = reinterpret_cast<__half*>(qfrag + ((i * 2 + (pr >> 1)) * NT + (r >> 3)) * 32 + (r & 7) * 4 + j);
-        dst[(pr & 1) * 2 + half] = __float2half_rn(x[i] * f);
+        __half* dst = reinterpret_cast<__half*>(qfrag + ((i * 2 + (byte >> 1)) * NT + (r >> 3)) * 32 + (r & 7) * 4 + j);
+        dst[(byte & 1) * 2 + half] = __float2half_rn(x[i] * f);
       }
-      // scores carry 2^-14 (codes) * 2^(14 - e) (Q)
-      if (lane == 0) qfac[r] = __uint_as_float(static_cast<uint32_t>(e + 127) << 23) * p.scale_log2;
+      // scores carry the 2^(14 - e) of Q
+      if (lane == 0) qfac[r] = __uint_as_float(static_cast<uint32_t>(e + 127 - 14) << 23) * p.scale_log2;
     }
     __syncthreads();
 
-    float m[NT][2], l[NT][2], cf[NT][2];
-    int limit[NT][2];
+    // ref: what a row's weights refer to; weights are 2^7 p.  top_e: the scale exponent that a block's result refers to.
+    float ref[NT][2], l[NT][2], cf[NT][2];
+    int limit[NT][2], all_see = INT32_MAX, any_sees = 0;
+    uint32_t top_e[NB];
     float acc[NT][NB][2][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const int row = rb * R + n * 8 + tq * 2 + c;
-        m[n][c] = __uint_as_float(0xFF800000u);
+        ref[n][c] = ninf;
         l[n][c] = 0.f;
         cf[n][c] = qfac[n * 8 + tq * 2 + c];
-        limit[n][c] = row < p.rows ? min(len, len - p.T + row / p.group + 1) : 0;
+        limit[n][c] = row < p.rows ? min(len, len - p.T + row / p.group + 1) : seen;   // (rows past the end: anything)
+        all_see = min(all_see, limit[n][c]);
+        any_sees = max(any_sees, limit[n][c]);
       }
 #pragma unroll
       for (int i = 0; i < NB; ++i)
 #pragma unroll
         for (int c = 0; c < 4; ++c) acc[n][i][0][c] = acc[n][i][1][c] = 0.f;
     }
+    all_see = __reduce_min_sync(0xFFFFFFFFu, all_see);
+    any_sees = __reduce_max_sync(0xFFFFFFFFu, any_sees);
+#pragma unroll
+    for (int i = 0; i < NB; ++i) top_e[i] = 0;
+    bool first_tile = true;
 
     for (int tile = t0 + warp; tile < t1; tile += kWarps) {
       if (!mbar_wait(my_bar + 8 * slot_out, phase_out, abort_flag)) { ok = false; break; }
       const unsigned char* st = my_gen + slot_out * Cfg::kStage;
       const uint32_t have = there & 3u;
       const int pos0 = tile * kTileTok;
+      const bool masked = have != 3u || pos0 + kTileTok > all_see;
 
       // ---- scores: s[mt][n] = 16 tokens x 8 rows; thread: tokens of rows g and g + 8, query rows 2 tq and 2 tq + 1
       float s[2][NT][4];
+      {
+        uint32_t wa[2][NB], wb[2][NB], sa[2][kScaleWords], sb[2][kScaleWords];
 #pragma unroll
-      for (int mt = 0; mt < 2; ++mt)
+        for (int mt = 0; mt < 2; ++mt) {
+          const unsigned char* grp = st + mt * group_bytes(D);
+          const int ta = token_of_row(g), tb = ta + 8;
+          load_words<NB>(grp + ta * (D / 2) + tq * (NB * 4), wa[mt]);
+          load_words<NB>(grp + tb * (D / 2) + tq * (NB * 4), wb[mt]);
+          load_scales<NB>(grp + k_scales_at(D) + ta * NB, sa[mt]);
+          load_scales<NB>(grp + k_scales_at(D) + tb * NB, sb[mt]);
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+          for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int c = 0; c < 4; ++c) s[mt][n][c] = 0.f;
-#pragma unroll
-      for (int mt = 0; mt < 2; ++mt) {
-        const unsigned char* grp = st + mt * group_bytes(D);
-        const int ta = token_of_row(g), tb = ta + 8;
-        uint32_t wa[NB], wb[NB];
-        if (NB == 2) {
-          const uint2 x = *reinterpret_cast<const uint2*>(grp + ta * (D / 2) + tq * 8);
-          const uint2 y = *reinterpret_cast<const uint2*>(grp + tb * (D / 2) + tq * 8);
-          wa[0] = x.x; wa[1] = x.y; wb[0] = y.x; wb[1] = y.y;
-        } else {
-#pragma unroll
-          for (int i = 0; i < NB / 4; ++i) {
-            const uint4 x = *reinterpret_cast<const uint4*>(grp + ta * (D / 2) + tq * (NB * 4) + i * 16);
-            const uint4 y = *reinterpret_cast<const uint4*>(grp + tb * (D / 2) + tq * (NB * 4) + i * 16);
-            wa[4 * i] = x.x; wa[4 * i + 1] = x.y; wa[4 * i + 2] = x.z; wa[4 * i + 3] = x.w;
-            wb[4 * i] = y.x; wb[4 * i + 1] = y.y; wb[4 * i + 2] = y.z; wb[4 * i + 3] = y.w;
-          }
+            for (int c = 0; c < 4; ++c) s[mt][n][c] = 0.f;
         }
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
-          uint32_t ha[4], hb[4];
-          mx4_pairs_f16(wa[i], ha);
-          mx4_pairs_f16(wb[i], hb);
-          const uint32_t a0[4] = {ha[0], hb[0], ha[1], hb[1]}, a1[4] = {ha[2], hb[2], ha[3], hb[3]};
-          const float sa = mx4_scale(grp[k_scales_at(D) + ta * NB + i]), sb = mx4_scale(grp[k_scales_at(D) + tb * NB + i]);
+          uint32_t a[2][2][4];
+          float fa[2], fb[2];
+#pragma unroll
+          for (int mt = 0; mt < 2; ++mt) {
+            uint32_t ha[4], hb[4];
+            mx4_bytes_f16(wa[mt][i], ha);
+            mx4_bytes_f16(wb[mt][i], hb);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              a[mt][k][0] = ha[2 * k]; a[mt][k][1] = hb[2 * k]; a[mt][k][2] = ha[2 * k + 1]; a[mt][k][3] = hb[2 * k + 1];
+            }
+            fa[mt] = scale_byte(sa[mt][i >> 2], i & 3);
+            fb[mt] = scale_byte(sb[mt][i >> 2], i & 3);
+          }
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            float c[4] = {0.f, 0.f, 0.f, 0.f};
             const uint2 b0 = qfrag[((i * 2) * NT + n) * 32 + lane], b1 = qfrag[((i * 2 + 1) * NT + n) * 32 + lane];
-            mma_f16(c, a0, b0.x, b0.y);
-            mma_f16(c, a1, b1.x, b1.y);
-            s[mt][n][0] += c[0] * sa;
-            s[mt][n][1] += c[1] * sa;
-            s[mt][n][2] += c[2] * sb;
-            s[mt][n][3] += c[3] * sb;
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt) {
+              float c[4] = {0.f, 0.f, 0.f, 0.f};
+              mma_f16(c, a[mt][0], b0.x, b0.y);
+              mma_f16(c, a[mt][1], b1.x, b1.y);
+              s[mt][n][0] = fmaf(c[0], fa[mt], s[mt][n][0]);
+              s[mt][n][1] = fmaf(c[1], fa[mt], s[mt][n][1]);
+              s[mt][n][2] = fmaf(c[2], fb[mt], s[mt][n][2]);
+              s[mt][n][3] = fmaf(c[3], fb[mt], s[mt][n][3]);
+            }
           }
         }
       }
-
-      // ---- mask, running maximum, weights
-      float corr[NT][2];
+      if (masked) {   // what lies behind the end or on a missing page is never looked at
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
+        for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          float top = m[n][c];
+          for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-              const int pos = pos0 + mt * kGroup + token_of_row(g) + 8 * hf;
-              float& x = s[mt][n][2 * hf + c];
-              // what lies behind the end or on a missing page is never looked at
-              x = (pos < limit[n][c] && (have >> mt & 1u)) ? x * cf[n][c] : __uint_as_float(0xFF800000u);
-              top = fmaxf(top, x);
+            for (int c = 0; c < 4; ++c) {
+              const int pos = pos0 + mt * kGroup + token_of_row(g) + 8 * (c >> 1);
+              if (!(pos < limit[n][c & 1] && (have >> mt & 1u))) s[mt][n][c] = ninf;
             }
-          top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
-          top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
-          top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
-          const float base = top == __uint_as_float(0xFF800000u) ? 0.f : top;   // nothing seen yet
-          corr[n][c] = ex2(m[n][c] - base);
-          m[n][c] = top;
-          float sum = 0.f;
-#pragma unroll
-          for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-              float& x = s[mt][n][2 * hf + c];
-              x = ex2(x - base);
-              sum += x;
-            }
-          l[n][c] = l[n][c] * corr[n][c] + sum;
-        }
       }
 
-      // ---- result, block by block: acc = acc * corr + V^T w
-      int last_seen = 0;
+      // ---- the reference moves only when a weight would pass 2^8 p: a vote, no shuffles, in most tiles
+      bool high = first_tile;
 #pragma unroll
-      for (int n = 0; n < NT; ++n) last_seen = max(last_seen, max(limit[n][0], limit[n][1]));
-      last_seen = __reduce_max_sync(0xFFFFFFFFu, last_seen);
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        // exponents of this thread's four tokens; 256: not seen
-        uint32_t ex[2][2];
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int mt = 0; mt < 2; ++mt) high |= s[mt][n][c] * cf[n][c & 1] > ref[n][c & 1] + 8.f;
+      if (__any_sync(0xFFFFFFFFu, high)) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            float top = fmaxf(fmaxf(s[0][n][c], s[0][n][2 + c]), fmaxf(s[1][n][c], s[1][n][2 + c]));
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
+            const float now = fmaxf(ref[n][c], top * cf[n][c]);
+            const float f = now == ref[n][c] ? 1.f : ex2(ref[n][c] - now);
+            ref[n][c] = now;
+            l[n][c] *= f;
+#pragma unroll
+            for (int i = 0; i < NB; ++i)
+#pragma unroll
+              for (int k = 0; k < 2; ++k) { acc[n][i][k][c] *= f; acc[n][i][k][2 + c] *= f; }
+          }
+        first_tile = false;
+      }
+      // weights, and as the 8-column operand: register hf holds rows 8 hf + 2 tq and + 1 of the 16 tokens, query row g
+      uint32_t wh[2][NT][2], wl[2][NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const float off = ref[n][c & 1] == ninf ? 0.f : 7.f - ref[n][c & 1];   // (nothing seen yet: all scores are -inf)
+            s[mt][n][c] = ex2(fmaf(s[mt][n][c], cf[n][c & 1], off));
+            l[n][c & 1] += s[mt][n][c];
+          }
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            const float x = s[mt][n][2 * hf], y = s[mt][n][2 * hf + 1];
+            const uint32_t packed = pack_f16x2(x, y);
+            wh[mt][n][hf] = transpose8x8(packed);
+            if (HILO) {
+              const __half2 r = *reinterpret_cast<const __half2*>(&packed);
+              wl[mt][n][hf] = transpose8x8(pack_f16x2(x - __low2float(r), y - __high2float(r)));
+            }
+          }
+        }
+
+      // ---- result: acc += V^T w.  Thread: dims 4 g .. + 3 of every block for the tokens of rows 2 tq, 2 tq + 1 and
+      // those 8 further on, k = 0..3
+      uint32_t vw[2][4][NB / 2], vs[2][4][kScaleWords];
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int tok = token_of_row(2 * tq + (k & 1) + 8 * (k >> 1));
+          const unsigned char* grp = st + mt * group_bytes(D);
+          load_halves<NB>(grp + v_codes_at(D) + tok * (D / 2) + (g ^ ((tok & 2) ? 4 : 0)) * NB * 2, vw[mt][k]);
+          load_scales<NB>(grp + v_scales_at(D) + tok * NB, vs[mt][k]);
+        }
+      // distance of every scale from its block's reference, two tokens to a register: 0..7 all over is the plain case
+      uint32_t far = masked ? 1u << 31 : 0u;
+      uint32_t fs[NB][2][2];
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
           for (int hf = 0; hf < 2; ++hf) {
-            const int tok = token_of_row(g) + 8 * hf;
-            const bool vis = (have >> mt & 1u) && pos0 + mt * kGroup + tok < last_seen;
-            ex[mt][hf] = vis ? st[mt * group_bytes(D) + v_scales_at(D) + tok * NB + i] : 256u;
+            const uint32_t pair = byte_pair(vs[mt][2 * hf][i >> 2], vs[mt][2 * hf + 1][i >> 2], i & 3);
+            const uint32_t d = top_e[i] * 0x10001u - pair;
+            far |= d & 0xFFF8FFF8u;
+            fs[i][mt][hf] = 0x3C003C00u - d * 1024u;   // fp16 2^-d
           }
-        // V as the 16-row operand: rows = dims 4 g .. + 3 of the block, columns = tokens
-        uint32_t va[2][2][4];   // [16 tokens][instruction][register]
+      if (!__any_sync(0xFFFFFFFFu, far != 0)) {
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt) {
-          const unsigned char* vc = st + mt * group_bytes(D) + v_codes_at(D);
-          uint32_t hw[4];
+        for (int w2 = 0; w2 < NB / 2; ++w2) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {   // columns 2 tq, 2 tq + 1, 2 tq + 8, 2 tq + 9
-            const int tok = token_of_row(2 * tq + (k & 1) + 8 * (k >> 1));
-            hw[k] = *reinterpret_cast<const uint16_t*>(vc + tok * (D / 2) + ((g ^ ((tok & 2) ? 4 : 0)) * NB + i) * 2);
-          }
-          uint32_t lo[4], hi[4];
-          mx4_pairs_f16(hw[0] | hw[1] << 16, lo);
-          mx4_pairs_f16(hw[2] | hw[3] << 16, hi);
-          va[mt][0][0] = lo[0]; va[mt][0][1] = lo[1]; va[mt][0][2] = hi[0]; va[mt][0][3] = hi[1];
-          va[mt][1][0] = lo[2]; va[mt][1][1] = lo[3]; va[mt][1][2] = hi[2]; va[mt][1][3] = hi[3];
-        }
-        bool first = true, more;
-        uint32_t nan_here = 0;   // this thread's tokens whose block is NaN
-        do {
-          uint32_t top = 0;
+          for (int mt = 0; mt < 2; ++mt) {
+            uint32_t va[2][2][4];   // [block of the pair][instruction][register]
+            v_operands(vw[mt][0][w2], vw[mt][1][w2], vw[mt][2][w2], vw[mt][3][w2], va);
 #pragma unroll
-          for (int mt = 0; mt < 2; ++mt)
+            for (int hb = 0; hb < 2; ++hb) {
+              const int i = 2 * w2 + hb;
 #pragma unroll
-            for (int hf = 0; hf < 2; ++hf) top = max(top, ex[mt][hf] < 255u ? ex[mt][hf] : 0u);
-          const uint32_t ref = __reduce_max_sync(0xFFFFFFFFu, top);
-          float fac[2][2];
-          bool left = false;
-#pragma unroll
-          for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-              const uint32_t e = ex[mt][hf];
-              const bool now = e <= ref && e + 14u >= ref;
-              fac[mt][hf] = now ? __uint_as_float((e + 142u - ref) << 23) : 0.f;      // 2^(e - ref + 15)
-              if (e == 255u) nan_here |= 1u << (2 * mt + hf);
-              if (now || e >= 255u) ex[mt][hf] = 256u;
-              else if (e > 0u) left = true;    // (blocks of zeros have e = 0 and add nothing)
-            }
-          more = __any_sync(0xFFFFFFFFu, left);
-          const float back = ref >= 2u ? __uint_as_float((ref - 1u) << 23) : __uint_as_float(0x00200000u << ref);   // 2^(ref - 128)
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            float c0[4] = {0.f, 0.f, 0.f, 0.f}, c1[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int mt = 0; mt < 2; ++mt) {
-              uint32_t wh[2], wl[2];
-#pragma unroll
-              for (int hf = 0; hf < 2; ++hf) {
-                const float x = s[mt][n][2 * hf] * fac[mt][hf], y = s[mt][n][2 * hf + 1] * fac[mt][hf];
-                const uint32_t packed = pack_f16x2(x, y);
-                wh[hf] = transpose8x8(packed);
+              for (int n = 0; n < NT; ++n) {
+                const uint32_t b0 = mul_f16x2(wh[mt][n][0], fs[i][mt][0]), b1 = mul_f16x2(wh[mt][n][1], fs[i][mt][1]);
+                mma_f16(acc[n][i][0], va[hb][0], b0, b1);
+                mma_f16(acc[n][i][1], va[hb][1], b0, b1);
                 if (HILO) {
-                  const __half2 r = *reinterpret_cast<const __half2*>(&packed);
-                  wl[hf] = transpose8x8(pack_f16x2(x - __low2float(r), y - __high2float(r)));
+                  const uint32_t c0 = mul_f16x2(wl[mt][n][0], fs[i][mt][0]), c1 = mul_f16x2(wl[mt][n][1], fs[i][mt][1]);
+                  mma_f16(acc[n][i][0], va[hb][0], c0, c1);
+                  mma_f16(acc[n][i][1], va[hb][1], c0, c1);
                 }
               }
-              mma_f16(c0, va[mt][0], wh[0], wh[1]);
-              mma_f16(c1, va[mt][1], wh[0], wh[1]);
-              if (HILO) {
-                mma_f16(c0, va[mt][0], wl[0], wl[1]);
-                mma_f16(c1, va[mt][1], wl[0], wl[1]);
-              }
-            }
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              const float keep = first ? corr[n][c & 1] : 1.f;
-              acc[n][i][0][c] = acc[n][i][0][c] * keep + c0[c] * back;
-              acc[n][i][1][c] = acc[n][i][1][c] * keep + c1[c] * back;
             }
           }
-          first = false;
-        } while (more);
-        if (__any_sync(0xFFFFFFFFu, nan_here != 0)) {   // NaN for the rows that see such a token, and for no others
+        }
+      } else {
+        // The end of a sequence, missing pages, NaN, a new largest scale, or scales far apart: per block, the tokens within
+        // seven binades of the largest scale left, then the next ones.
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
+        for (int i = 0; i < NB; ++i) {
+          uint32_t ex[2][4];   // 256: not seen, or done
+          uint32_t top = 0, nan_here = 0;
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              uint32_t bad = 0;
+          for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const int tok = token_of_row(2 * tq + (k & 1) + 8 * (k >> 1));
+              uint32_t e = vs[mt][k][i >> 2] >> (8 * (i & 3)) & 255u;
+              if (!(have >> mt & 1u) || pos0 + mt * kGroup + tok >= any_sees) e = 256u;
+              if (e == 255u) { nan_here |= 1u << (4 * mt + k); e = 256u; }
+              ex[mt][k] = e;
+              if (e < 255u) top = max(top, e);
+            }
+          top = __reduce_max_sync(0xFFFFFFFFu, top);
+          if (top > top_e[i]) {
+            const float f = top - top_e[i] > 126u ? 0.f : __uint_as_float((127u - (top - top_e[i])) << 23);
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int c = 0; c < 4; ++c) { acc[n][i][0][c] *= f; acc[n][i][1][c] *= f; }
+            top_e[i] = top;
+          }
+          bool more;
+          do {
+            uint32_t f2[2][2];
+            uint32_t rest = 0;
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+              for (int hf = 0; hf < 2; ++hf) {
+                f2[mt][hf] = 0;
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                  uint32_t& e = ex[mt][2 * hf + k];
+                  if (e <= top && e + 7u >= top) {
+                    f2[mt][hf] |= (15u - (top - e)) << (10 + 16 * k);
+                    e = 256u;
+                  }
+                  if (e < 255u) rest = max(rest, e);   // (blocks of zeros have e = 0: they add nothing)
+                }
+              }
+            rest = __reduce_max_sync(0xFFFFFFFFu, rest);
+            more = rest > 0u;
+            const uint32_t below = top_e[i] - top;
+            const float f = below > 126u ? 0.f : __uint_as_float((127u - below) << 23);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              float c0[4] = {0.f, 0.f, 0.f, 0.f}, c1[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int mt = 0; mt < 2; ++mt) {
+                uint32_t va[2][2][4];
+                v_operands(vw[mt][0][i >> 1], vw[mt][1][i >> 1], vw[mt][2][i >> 1], vw[mt][3][i >> 1], va);
+                const uint32_t b0 = mul_f16x2(wh[mt][n][0], f2[mt][0]), b1 = mul_f16x2(wh[mt][n][1], f2[mt][1]);
+                mma_f16(c0, va[i & 1][0], b0, b1);
+                mma_f16(c1, va[i & 1][1], b0, b1);
+                if (HILO) {
+                  const uint32_t d0 = mul_f16x2(wl[mt][n][0], f2[mt][0]), d1 = mul_f16x2(wl[mt][n][1], f2[mt][1]);
+                  mma_f16(c0, va[i & 1][0], d0, d1);
+                  mma_f16(c1, va[i & 1][1], d0, d1);
+                }
+              }
+#pragma unroll
+              for (int c = 0; c < 4; ++c) {
+                acc[n][i][0][c] = fmaf(c0[c], f, acc[n][i][0][c]);
+                acc[n][i][1][c] = fmaf(c1[c], f, acc[n][i][1][c]);
+              }
+            }
+            top = rest;
+          } while (more);
+          if (__any_sync(0xFFFFFFFFu, nan_here != 0)) {   // NaN for the rows that see such a token, and for no others
+            int from = INT32_MAX;
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
               for (int k = 0; k < 4; ++k)
-                if ((nan_here >> k & 1u) && pos0 + (k >> 1) * kGroup + token_of_row(g) + 8 * (k & 1) < limit[n][c]) bad = 1;
-              bad |= __shfl_xor_sync(0xFFFFFFFFu, bad, 4);
-              bad |= __shfl_xor_sync(0xFFFFFFFFu, bad, 8);
-              bad |= __shfl_xor_sync(0xFFFFFFFFu, bad, 16);
-              if (bad)
+                if (nan_here >> (4 * mt + k) & 1u)
+                  from = min(from, pos0 + mt * kGroup + token_of_row(2 * tq + (k & 1) + 8 * (k >> 1)));
+            from = __reduce_min_sync(0xFFFFFFFFu, from);
 #pragma unroll
-                for (int k = 0; k < 2; ++k) acc[n][i][k][c] = acc[n][i][k][2 + c] = __uint_as_float(0x7FC00000u);
-            }
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int c = 0; c < 2; ++c)
+                if (from < limit[n][c])
+#pragma unroll
+                  for (int k = 0; k < 2; ++k) acc[n][i][k][c] = acc[n][i][k][2 + c] = __uint_as_float(0x7FC00000u);
+          }
         }
       }
       __syncwarp();   // every lane has read the stage
@@ -669,15 +829,17 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
       for (int c = 0; c < 2; ++c) {
         const int r = n * 8 + tq * 2 + c;
         if (g == 0) {
-          jm[warp * R + r] = m[n][c];
+          jm[warp * R + r] = ref[n][c];
           jl[warp * R + r] = l[n][c];
         }
         float* row = join + (warp * R + r) * Cfg::kAccPitch;
 #pragma unroll
-        for (int i = 0; i < NB; ++i)
+        for (int i = 0; i < NB; ++i) {
+          const float back = mx4_scale(top_e[i]);
 #pragma unroll
           for (int k = 0; k < 2; ++k)
-            *reinterpret_cast<float2*>(row + i * 32 + 4 * g + 2 * k) = make_float2(acc[n][i][k][c], acc[n][i][k][2 + c]);
+            *reinterpret_cast<float2*>(row + i * 32 + 4 * g + 2 * k) = make_float2(acc[n][i][k][c] * back, acc[n][i][k][2 + c] * back);
+        }
       }
     __syncthreads();
     const bool whole = w.whole();
@@ -803,6 +965,7 @@ int check_cache(const gl_cache4* c, const gl_pages* at, CacheView* v) {
   v->batch = at->batch;
   v->width = at->table_width;
   v->capacity = static_cast<int>(cap);
+  v->div_page.set(c->page_tokens);
   return GL_OK;
 }
 
