@@ -169,9 +169,10 @@ __global__ void __launch_bounds__(256) cache4_read(uint16_t* __restrict__ k, uin
 // ring of bulk copies, running maximum, sum and result; the block joins its warps, and a second kernel joins the
 // blocks where a segment was cut.
 
-constexpr int kTileTok = 32;
+constexpr int kTileTok = 64;      // tokens per tile: what a warp waits for and asks for at a time
+constexpr int kSubTok = 32;       // tokens that a warp computes with at a time
 constexpr int kWarps = 4;
-constexpr int kStagesAt = 3;
+constexpr int kStagesAt = 2;
 
 struct AttendParams {
   CacheView c;
@@ -330,49 +331,52 @@ __device__ __forceinline__ void mx4_bytes_f16(uint32_t w, uint32_t (&h)[4]) {
       "cvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
       : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
 }
-// N consecutive words, or half words, or scale bytes of a token
-template <int NB>
-__device__ __forceinline__ void load_words(const unsigned char* at, uint32_t (&w)[NB]) {
-  if (NB == 2) {
-    const uint2 x = *reinterpret_cast<const uint2*>(at);
-    w[0] = x.x; w[1] = x.y;
+// N consecutive words, or half words, or scale bytes of a token (shared-memory addresses)
+template <int N>
+__device__ __forceinline__ void load_shared(uint32_t at, uint32_t (&w)[N]) {
+  static_assert(N == 1 || N == 2 || N % 4 == 0, "1, 2 or whole 16 bytes");
+  if constexpr (N == 1) {
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[0]) : "r"(at));
+  } else if constexpr (N == 2) {
+    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at));
   } else {
 #pragma unroll
-    for (int i = 0; i < NB / 4; ++i) {
-      const uint4 x = *reinterpret_cast<const uint4*>(at + 16 * i);
-      w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
-    }
+    for (int i = 0; i < N; i += 4)
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]) : "r"(at + 4 * i));
   }
 }
 template <int NB>
-__device__ __forceinline__ void load_halves(const unsigned char* at, uint32_t (&w)[NB / 2]) {
-  if (NB == 2) {
-    w[0] = *reinterpret_cast<const uint32_t*>(at);
-  } else if (NB == 4) {
-    const uint2 x = *reinterpret_cast<const uint2*>(at);
-    w[0] = x.x; w[1] = x.y;
+__device__ __forceinline__ void load_words(uint32_t at, uint32_t (&w)[NB]) { load_shared<NB>(at, w); }
+template <int NB>
+__device__ __forceinline__ void load_halves(uint32_t at, uint32_t (&w)[NB / 2]) { load_shared<NB / 2>(at, w); }
+template <int NB>
+__device__ __forceinline__ void load_scales(uint32_t at, uint32_t (&w)[(NB + 3) / 4]) {
+  if constexpr (NB == 2) {
+    uint16_t x;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(at));
+    w[0] = x;
   } else {
-    const uint4 x = *reinterpret_cast<const uint4*>(at);
-    w[0] = x.x; w[1] = x.y; w[NB == 8 ? 2 : 0] = x.z; w[NB == 8 ? 3 : 0] = x.w;
+    load_shared<NB / 4>(at, w);
   }
 }
+// Scale bytes as 2^(e - 127), NaN for 255: two a conversion, by way of bf16
 template <int NB>
-__device__ __forceinline__ void load_scales(const unsigned char* at, uint32_t (&w)[(NB + 3) / 4]) {
-  if (NB == 2) w[0] = *reinterpret_cast<const uint16_t*>(at);
-  else if (NB == 4) w[0] = *reinterpret_cast<const uint32_t*>(at);
-  else {
-    const uint2 x = *reinterpret_cast<const uint2*>(at);
-    w[0] = x.x; w[NB == 8 ? 1 : 0] = x.y;
+__device__ __forceinline__ void scale_floats(const uint32_t (&w)[(NB + 3) / 4], float (&f)[NB]) {
+#pragma unroll
+  for (int i = 0; i < NB; i += 2) {
+    uint32_t two;
+    const uint16_t bytes = static_cast<uint16_t>(w[i >> 2] >> (8 * (i & 2)));
+    asm("cvt.rn.bf16x2.ue8m0x2 %0, %1;" : "=r"(two) : "h"(bytes));
+    f[i] = __uint_as_float(two << 16);
+    f[i + 1] = __uint_as_float(two & 0xFFFF0000u);
   }
 }
-// Byte i of a scale word as 2^(e - 127).  (e = 255 gives Inf: a NaN block's codes are zeros, and zero times Inf is NaN.)
-__device__ __forceinline__ float scale_byte(uint32_t w, int i) {
-  const uint32_t bits = (i == 3 ? w >> 1 : w << (23 - 8 * i)) & 0x7F800000u;
-  return __uint_as_float(max(bits, 0x00400000u));
-}
-// Byte i of two words in the two halves of one
-__device__ __forceinline__ uint32_t byte_pair(uint32_t a, uint32_t b, int i) {
-  return __byte_perm(a, b, 0x0400u + 0x0101u * i) & 0x00FF00FFu;
+// Byte i of two words as the high bytes of two halves, zeros below (the bytes' top bits are clear: their sign is zeros)
+__device__ __forceinline__ uint32_t high_bytes(uint32_t a, uint32_t b, int i) {
+  uint32_t d;
+  asm("prmt.b32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"((8u | i) | i << 4 | (8u | (4u + i)) << 8 | (4u + i) << 12));
+  return d;
 }
 // V of two neighbouring blocks as 16-row operands: x0..x3 hold dims 4 g .. + 3 of both blocks (low and high half) of the
 // tokens in columns 2 tq, 2 tq + 1, 2 tq + 8, 2 tq + 9.  Bytes with one token's code in each half become fp16 pairs.
@@ -397,12 +401,15 @@ template <int NB, int NT>
 struct AttCfg {
   static constexpr int D = 32 * NB;
   static constexpr int R = 8 * NT;
-  static constexpr int kStage = 2 * group_bytes(D);                  // one tile: two groups
+  static constexpr int kStage = kTileTok / kGroup * group_bytes(D);  // one tile
   static constexpr int kRing = kWarps * kStagesAt * kStage;
   static constexpr int kQ = NB * 2 * NT * 32 * 8;                    // fragments of Q
-  static constexpr int kAccPitch = D + 4;
-  static constexpr int kJoin = kWarps * R * (kAccPitch + 2) * 4;     // results, maxima and sums of the warps
-  static constexpr int kSmem = kRing + kQ + R * 4 + kJoin + 256;
+  // results of a warp, in the place of its ring: rows of D floats, then maxima and sums.  Rows are kept apart by their
+  // order in the banks (a pitch of D + 4 floats) where the ring has the room.
+  static constexpr int kWarpRing = kStagesAt * kStage;
+  static constexpr int kAccPitch = R * (D + 6) * 4 <= kWarpRing ? D + 4 : D;
+  static constexpr int kSmem = kRing + kQ + R * 4 + 2 * kWarps * R * 4 + 256;
+  static_assert(R * kAccPitch * 4 <= kWarpRing, "results fit in the ring");
 };
 
 template <int NB, int NT, bool HILO>
@@ -410,11 +417,11 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
   using Cfg = AttCfg<NB, NT>;
   constexpr int D = Cfg::D, R = Cfg::R;
   extern __shared__ __align__(128) unsigned char smem[];
-  unsigned char* ring = smem;
   uint2* qfrag = reinterpret_cast<uint2*>(smem + Cfg::kRing);
   float* qfac = reinterpret_cast<float*>(smem + Cfg::kRing + Cfg::kQ);
-  float* join = qfac + R;
-  unsigned char* tail = smem + Cfg::kRing + Cfg::kQ + R * 4 + Cfg::kJoin;
+  float* jm = qfac + R;             // [kWarps][R] references and sums of the warps
+  float* jl = jm + kWarps * R;
+  unsigned char* tail = smem + Cfg::kRing + Cfg::kQ + R * 4 + 2 * kWarps * R * 4;
   uint64_t* bars = reinterpret_cast<uint64_t*>(tail);                          // [kWarps][kStagesAt]
   int64_t* scratch = reinterpret_cast<int64_t*>(tail + 8 * kWarps * kStagesAt);   // [2 * kWarps]
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 8 * kWarps * kStagesAt + 16 * kWarps);
@@ -433,8 +440,7 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
   Walk w;
   w.start(p, all, blockIdx.x);
 
-  const uint32_t my_ring = smem_u32(ring) + warp * kStagesAt * Cfg::kStage;
-  const unsigned char* my_gen = ring + warp * kStagesAt * Cfg::kStage;
+  const uint32_t my_ring = smem_u32(smem) + warp * kStagesAt * Cfg::kStage;
   const uint32_t my_bar = smem_u32(bars + warp * kStagesAt);
   uint32_t slot_in = 0, slot_out = 0, phase_out = 0;
   constexpr int kScaleWords = (NB + 3) / 4;
@@ -445,48 +451,45 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
     const int b = w.b, h = w.h, rb = w.rb, t0 = w.t0, t1 = w.t1, len = w.len, seen = w.seen;
 
     // ---- ring of this warp: tiles t0 + warp, + kWarps, ...
-    uint32_t there = 0;   // two bits per tile in flight: its groups that have a page (oldest tile lowest)
+    __syncthreads();   // the previous segment's fragments and joined results (which lie in the rings) are read
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    constexpr int kGroupsAt = kTileTok / kGroup;
+    constexpr uint32_t kAllThere = (1u << kGroupsAt) - 1u;
+    uint32_t there = 0;   // kGroupsAt bits per tile in flight: its groups that have a page (oldest tile lowest)
     int in_flight = 0;
     int next = t0 + warp;
-    int32_t page_lo = -1, page_hi = -1;
-    auto fetch_pages = [&](int tile) {
-      const int pos = tile * kTileTok;
-      page_lo = page_hi = -1;
-      if (tile < t1) {
-        const int64_t row = static_cast<int64_t>(b) * p.c.width;
-        page_lo = p.c.table[row + p.c.div_page.div(pos)];
-        if (pos + kGroup < seen) page_hi = p.c.table[row + p.c.div_page.div(pos + kGroup)];
-      }
+    int32_t page = -1;    // lane g < kGroupsAt: page of group g of tile `next`, -1 where there is none
+    auto fetch_pages = [&]() {
+      const int pos = next * kTileTok + lane * kGroup;
+      page = -1;
+      if (next < t1 && lane < kGroupsAt && pos < seen)
+        page = p.c.table[static_cast<int64_t>(b) * p.c.width + p.c.div_page.div(static_cast<uint32_t>(pos))];
     };
-    auto issue = [&]() {   // copies of tile `next`, whose pages are in page_lo and page_hi
+    auto issue = [&]() {   // copies of tile `next`: lane g asks for group g
       if (next >= t1) return;
-      const int pos = next * kTileTok;
-      const bool lo = page_lo >= 0 && page_lo < p.c.pages, hi = page_hi >= 0 && page_hi < p.c.pages;
-      if (lane == 0) {
-        const uint32_t bar = my_bar + 8 * slot_in, dst = my_ring + slot_in * Cfg::kStage;
-        uint32_t slot, in_lo, in_hi;
-        p.c.div_page.divmod(pos, slot, in_lo);
-        p.c.div_page.divmod(pos + kGroup, slot, in_hi);
-        mbar_expect_tx(bar, (lo ? group_bytes(D) : 0) + (hi ? group_bytes(D) : 0));
-        if (lo)
-          bulk_copy_g2s(dst, p.c.data + page_lo * p.c.page_stride + h * p.c.head_stride +
-                                 static_cast<int64_t>(in_lo / kGroup) * group_bytes(D), group_bytes(D), bar);
-        if (hi)
-          bulk_copy_g2s(dst + group_bytes(D), p.c.data + page_hi * p.c.page_stride + h * p.c.head_stride +
-                                 static_cast<int64_t>(in_hi / kGroup) * group_bytes(D), group_bytes(D), bar);
+      const bool mine = page >= 0 && page < p.c.pages;
+      const uint32_t have = __ballot_sync(0xFFFFFFFFu, mine);
+      const uint32_t bar = my_bar + 8 * slot_in;
+      if (lane == 0) mbar_expect_tx(bar, __popc(have) * group_bytes(D));
+      __syncwarp();
+      if (mine) {
+        uint32_t slot, in_page;
+        p.c.div_page.divmod(static_cast<uint32_t>(next * kTileTok + lane * kGroup), slot, in_page);
+        bulk_copy_g2s(my_ring + slot_in * Cfg::kStage + lane * group_bytes(D),
+                      p.c.data + page * p.c.page_stride + h * p.c.head_stride + static_cast<int64_t>(in_page / kGroup) * group_bytes(D),
+                      group_bytes(D), bar);
       }
-      there |= ((lo ? 1u : 0u) | (hi ? 2u : 0u)) << (2 * in_flight);
+      there |= have << (kGroupsAt * in_flight);
       ++in_flight;
       slot_in = slot_in + 1 == kStagesAt ? 0 : slot_in + 1;
       next += kWarps;
-      fetch_pages(next);
+      fetch_pages();
     };
-    fetch_pages(next);
+    fetch_pages();
 #pragma unroll
     for (int i = 0; i < kStagesAt; ++i) issue();
 
     // ---- Q as fragments in shared memory, row r scaled by a power of two into [2^14, 2^15)
-    __syncthreads();   // the previous segment's fragments and joined results are read
     for (int r = warp; r < R; r += kWarps) {
       const int row = rb * R + r;
       const bool live = row < p.rows;
@@ -514,17 +517,18 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
     }
     __syncthreads();
 
-    // ref: what a row's weights refer to; weights are 2^7 p.  top_e: the scale exponent that a block's result refers to.
-    float ref[NT][2], l[NT][2], cf[NT][2];
+    // ref: what a row's weights refer to; a weight is 2^7 p = 2^(s cf + off), off = 7 - ref (+Inf until there is one).
+    // top_e: the scale exponents that the blocks' results refer to, four to a word, 8 at least.
+    float off[NT][2], l[NT][2], cf[NT][2];
     int limit[NT][2], all_see = INT32_MAX, any_sees = 0;
-    uint32_t top_e[NB];
+    uint32_t top_e[kScaleWords];
     float acc[NT][NB][2][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const int row = rb * R + n * 8 + tq * 2 + c;
-        ref[n][c] = ninf;
+        off[n][c] = -ninf;
         l[n][c] = 0.f;
         cf[n][c] = qfac[n * 8 + tq * 2 + c];
         limit[n][c] = row < p.rows ? min(len, len - p.T + row / p.group + 1) : seen;   // (rows past the end: anything)
@@ -539,28 +543,40 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
     all_see = __reduce_min_sync(0xFFFFFFFFu, all_see);
     any_sees = __reduce_max_sync(0xFFFFFFFFu, any_sees);
 #pragma unroll
-    for (int i = 0; i < NB; ++i) top_e[i] = 0;
-    bool first_tile = true;
+    for (int i = 0; i < kScaleWords; ++i) top_e[i] = NB == 2 ? 0x0808u : 0x08080808u;
+    // where this lane's tokens start in a group: K rows g and (8 tokens on) g + 8; V columns 2 tq, 2 tq + 1 and 8 tokens on
+    const uint32_t tok_k = token_of_row(g), tok_v0 = token_of_row(2 * tq), tok_v1 = token_of_row(2 * tq + 1);
+    const uint32_t at_k = tok_k * (D / 2) + tq * (NB * 4), at_ks = k_scales_at(D) + tok_k * NB;
+    const uint32_t at_v0 = v_codes_at(D) + tok_v0 * (D / 2) + (g ^ ((tok_v0 & 2) ? 4 : 0)) * NB * 2;
+    const uint32_t at_v1 = v_codes_at(D) + tok_v1 * (D / 2) + (g ^ ((tok_v1 & 2) ? 4 : 0)) * NB * 2;
+    const uint32_t at_vs0 = v_scales_at(D) + tok_v0 * NB, at_vs1 = v_scales_at(D) + tok_v1 * NB;
 
     for (int tile = t0 + warp; tile < t1; tile += kWarps) {
       if (!mbar_wait(my_bar + 8 * slot_out, phase_out, abort_flag)) { ok = false; break; }
-      const unsigned char* st = my_gen + slot_out * Cfg::kStage;
-      const uint32_t have = there & 3u;
-      const int pos0 = tile * kTileTok;
-      const bool masked = have != 3u || pos0 + kTileTok > all_see;
+      const uint32_t tile_have = there & kAllThere;
+#pragma unroll 1
+      for (int sub = 0; sub < kTileTok / kSubTok; ++sub) {
+      const uint32_t st = my_ring + slot_out * Cfg::kStage + sub * 2 * group_bytes(D);
+      const uint32_t have = tile_have >> (2 * sub) & 3u;
+      const int pos0 = tile * kTileTok + sub * kSubTok;
+      if (pos0 >= any_sees) break;
+      const bool masked = have != 3u || pos0 + kSubTok > all_see;
 
       // ---- scores: s[mt][n] = 16 tokens x 8 rows; thread: tokens of rows g and g + 8, query rows 2 tq and 2 tq + 1
       float s[2][NT][4];
       {
-        uint32_t wa[2][NB], wb[2][NB], sa[2][kScaleWords], sb[2][kScaleWords];
+        uint32_t wa[2][NB], wb[2][NB];
+        float fa[2][NB], fb[2][NB];
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt) {
-          const unsigned char* grp = st + mt * group_bytes(D);
-          const int ta = token_of_row(g), tb = ta + 8;
-          load_words<NB>(grp + ta * (D / 2) + tq * (NB * 4), wa[mt]);
-          load_words<NB>(grp + tb * (D / 2) + tq * (NB * 4), wb[mt]);
-          load_scales<NB>(grp + k_scales_at(D) + ta * NB, sa[mt]);
-          load_scales<NB>(grp + k_scales_at(D) + tb * NB, sb[mt]);
+          const uint32_t grp = st + mt * group_bytes(D);
+          load_words<NB>(grp + at_k, wa[mt]);
+          load_words<NB>(grp + at_k + 8 * (D / 2), wb[mt]);
+          uint32_t sa[kScaleWords], sb[kScaleWords];
+          load_scales<NB>(grp + at_ks, sa);
+          load_scales<NB>(grp + at_ks + 8 * NB, sb);
+          scale_floats<NB>(sa, fa[mt]);
+          scale_floats<NB>(sb, fb[mt]);
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -569,7 +585,6 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
           uint32_t a[2][2][4];
-          float fa[2], fb[2];
 #pragma unroll
           for (int mt = 0; mt < 2; ++mt) {
             uint32_t ha[4], hb[4];
@@ -579,8 +594,6 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
             for (int k = 0; k < 2; ++k) {
               a[mt][k][0] = ha[2 * k]; a[mt][k][1] = hb[2 * k]; a[mt][k][2] = ha[2 * k + 1]; a[mt][k][3] = hb[2 * k + 1];
             }
-            fa[mt] = scale_byte(sa[mt][i >> 2], i & 3);
-            fb[mt] = scale_byte(sb[mt][i >> 2], i & 3);
           }
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
@@ -590,10 +603,10 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
               float c[4] = {0.f, 0.f, 0.f, 0.f};
               mma_f16(c, a[mt][0], b0.x, b0.y);
               mma_f16(c, a[mt][1], b1.x, b1.y);
-              s[mt][n][0] = fmaf(c[0], fa[mt], s[mt][n][0]);
-              s[mt][n][1] = fmaf(c[1], fa[mt], s[mt][n][1]);
-              s[mt][n][2] = fmaf(c[2], fb[mt], s[mt][n][2]);
-              s[mt][n][3] = fmaf(c[3], fb[mt], s[mt][n][3]);
+              s[mt][n][0] = fmaf(c[0], fa[mt][i], s[mt][n][0]);
+              s[mt][n][1] = fmaf(c[1], fa[mt][i], s[mt][n][1]);
+              s[mt][n][2] = fmaf(c[2], fb[mt][i], s[mt][n][2]);
+              s[mt][n][3] = fmaf(c[3], fb[mt][i], s[mt][n][3]);
             }
           }
         }
@@ -605,20 +618,20 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
           for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-              const int pos = pos0 + mt * kGroup + token_of_row(g) + 8 * (c >> 1);
+              const int pos = pos0 + mt * kGroup + static_cast<int>(tok_k) + 8 * (c >> 1);
               if (!(pos < limit[n][c & 1] && (have >> mt & 1u))) s[mt][n][c] = ninf;
             }
       }
 
       // ---- the reference moves only when a weight would pass 2^8 p: a vote, no shuffles, in most tiles
-      bool high = first_tile;
+      float high = ninf;
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
+        for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-          for (int mt = 0; mt < 2; ++mt) high |= s[mt][n][c] * cf[n][c & 1] > ref[n][c & 1] + 8.f;
-      if (__any_sync(0xFFFFFFFFu, high)) {
+          for (int c = 0; c < 4; ++c) high = fmaxf(high, fmaf(s[mt][n][c], cf[n][c & 1], off[n][c & 1]));
+      if (__any_sync(0xFFFFFFFFu, high > 15.f)) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -627,16 +640,16 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
-            const float now = fmaxf(ref[n][c], top * cf[n][c]);
-            const float f = now == ref[n][c] ? 1.f : ex2(ref[n][c] - now);
-            ref[n][c] = now;
+            const float now = fminf(off[n][c], 7.f - top * cf[n][c]);
+            // (off = +Inf, nothing seen so far: sum and result are zeros)
+            const float f = now == off[n][c] || off[n][c] == -ninf ? 1.f : ex2(now - off[n][c]);
+            off[n][c] = now;
             l[n][c] *= f;
 #pragma unroll
             for (int i = 0; i < NB; ++i)
 #pragma unroll
               for (int k = 0; k < 2; ++k) { acc[n][i][k][c] *= f; acc[n][i][k][2 + c] *= f; }
           }
-        first_tile = false;
       }
       // weights, and as the 8-column operand: register hf holds rows 8 hf + 2 tq and + 1 of the 16 tokens, query row g
       uint32_t wh[2][NT][2], wl[2][NT][2];
@@ -646,8 +659,8 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
         for (int mt = 0; mt < 2; ++mt) {
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
-            const float off = ref[n][c & 1] == ninf ? 0.f : 7.f - ref[n][c & 1];   // (nothing seen yet: all scores are -inf)
-            s[mt][n][c] = ex2(fmaf(s[mt][n][c], cf[n][c & 1], off));
+            const float w8 = ex2(fmaf(s[mt][n][c], cf[n][c & 1], off[n][c & 1]));
+            s[mt][n][c] = masked && s[mt][n][c] == ninf ? 0.f : w8;
             l[n][c & 1] += s[mt][n][c];
           }
 #pragma unroll
@@ -669,24 +682,23 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
       for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const int tok = token_of_row(2 * tq + (k & 1) + 8 * (k >> 1));
-          const unsigned char* grp = st + mt * group_bytes(D);
-          load_halves<NB>(grp + v_codes_at(D) + tok * (D / 2) + (g ^ ((tok & 2) ? 4 : 0)) * NB * 2, vw[mt][k]);
-          load_scales<NB>(grp + v_scales_at(D) + tok * NB, vs[mt][k]);
+          const uint32_t grp = st + mt * group_bytes(D) + (k >> 1) * 8 * (D / 2);
+          load_halves<NB>(grp + (k & 1 ? at_v1 : at_v0), vw[mt][k]);
+          load_scales<NB>(st + mt * group_bytes(D) + (k >> 1) * 8 * NB + (k & 1 ? at_vs1 : at_vs0), vs[mt][k]);
         }
-      // distance of every scale from its block's reference, two tokens to a register: 0..7 all over is the plain case
+      // Distance of every scale from its block's reference, byte by byte: 0..7 all over is the plain case.  (References are 8 at
+      // least: no distance that is none of these looks like one after the borrow.)
       uint32_t far = masked ? 1u << 31 : 0u;
-      uint32_t fs[NB][2][2];
+      uint32_t fs[2][4][kScaleWords];   // high bytes of fp16 2^-d
 #pragma unroll
-      for (int i = 0; i < NB; ++i)
+      for (int k2 = 0; k2 < kScaleWords; ++k2)
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            const uint32_t pair = byte_pair(vs[mt][2 * hf][i >> 2], vs[mt][2 * hf + 1][i >> 2], i & 3);
-            const uint32_t d = top_e[i] * 0x10001u - pair;
-            far |= d & 0xFFF8FFF8u;
-            fs[i][mt][hf] = 0x3C003C00u - d * 1024u;   // fp16 2^-d
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t d = top_e[k2] - vs[mt][k][k2];
+            far |= d & 0xF8F8F8F8u;
+            fs[mt][k][k2] = 0x3C3C3C3Cu - 4u * d;
           }
       if (!__any_sync(0xFFFFFFFFu, far != 0)) {
 #pragma unroll
@@ -698,13 +710,15 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
 #pragma unroll
             for (int hb = 0; hb < 2; ++hb) {
               const int i = 2 * w2 + hb;
+              const uint32_t f0 = high_bytes(fs[mt][0][i >> 2], fs[mt][1][i >> 2], i & 3);
+              const uint32_t f1 = high_bytes(fs[mt][2][i >> 2], fs[mt][3][i >> 2], i & 3);
 #pragma unroll
               for (int n = 0; n < NT; ++n) {
-                const uint32_t b0 = mul_f16x2(wh[mt][n][0], fs[i][mt][0]), b1 = mul_f16x2(wh[mt][n][1], fs[i][mt][1]);
+                const uint32_t b0 = mul_f16x2(wh[mt][n][0], f0), b1 = mul_f16x2(wh[mt][n][1], f1);
                 mma_f16(acc[n][i][0], va[hb][0], b0, b1);
                 mma_f16(acc[n][i][1], va[hb][1], b0, b1);
                 if (HILO) {
-                  const uint32_t c0 = mul_f16x2(wl[mt][n][0], fs[i][mt][0]), c1 = mul_f16x2(wl[mt][n][1], fs[i][mt][1]);
+                  const uint32_t c0 = mul_f16x2(wl[mt][n][0], f0), c1 = mul_f16x2(wl[mt][n][1], f1);
                   mma_f16(acc[n][i][0], va[hb][0], c0, c1);
                   mma_f16(acc[n][i][1], va[hb][1], c0, c1);
                 }
@@ -723,7 +737,7 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
           for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              const int tok = token_of_row(2 * tq + (k & 1) + 8 * (k >> 1));
+              const int tok = static_cast<int>(k & 1 ? tok_v1 : tok_v0) + 8 * (k >> 1);
               uint32_t e = vs[mt][k][i >> 2] >> (8 * (i & 3)) & 255u;
               if (!(have >> mt & 1u) || pos0 + mt * kGroup + tok >= any_sees) e = 256u;
               if (e == 255u) { nan_here |= 1u << (4 * mt + k); e = 256u; }
@@ -731,13 +745,15 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
               if (e < 255u) top = max(top, e);
             }
           top = __reduce_max_sync(0xFFFFFFFFu, top);
-          if (top > top_e[i]) {
-            const float f = top - top_e[i] > 126u ? 0.f : __uint_as_float((127u - (top - top_e[i])) << 23);
+          uint32_t base = top_e[i >> 2] >> (8 * (i & 3)) & 255u;
+          if (top > base) {
+            const float f = top - base > 126u ? 0.f : __uint_as_float((127u - (top - base)) << 23);
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
               for (int c = 0; c < 4; ++c) { acc[n][i][0][c] *= f; acc[n][i][1][c] *= f; }
-            top_e[i] = top;
+            top_e[i >> 2] += (top - base) << (8 * (i & 3));
+            base = top;
           }
           bool more;
           do {
@@ -760,7 +776,7 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
               }
             rest = __reduce_max_sync(0xFFFFFFFFu, rest);
             more = rest > 0u;
-            const uint32_t below = top_e[i] - top;
+            const uint32_t below = base - top;
             const float f = below > 126u ? 0.f : __uint_as_float((127u - below) << 23);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
@@ -793,7 +809,7 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
 #pragma unroll
               for (int k = 0; k < 4; ++k)
                 if (nan_here >> (4 * mt + k) & 1u)
-                  from = min(from, pos0 + mt * kGroup + token_of_row(2 * tq + (k & 1) + 8 * (k >> 1)));
+                  from = min(from, pos0 + mt * kGroup + static_cast<int>(k & 1 ? tok_v1 : tok_v0) + 8 * (k >> 1));
             from = __reduce_min_sync(0xFFFFFFFFu, from);
 #pragma unroll
             for (int n = 0; n < NT; ++n)
@@ -805,8 +821,9 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
           }
         }
       }
+      }   // (sub)
       __syncwarp();   // every lane has read the stage
-      there >>= 2;
+      there >>= kGroupsAt;
       --in_flight;
       if (++slot_out == kStagesAt) { slot_out = 0; phase_out ^= 1u; }
       issue();
@@ -821,21 +838,19 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
         l[n][c] += __shfl_xor_sync(0xFFFFFFFFu, l[n][c], 8);
         l[n][c] += __shfl_xor_sync(0xFFFFFFFFu, l[n][c], 16);
       }
-    float* jm = join + kWarps * R * Cfg::kAccPitch;
-    float* jl = jm + kWarps * R;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const int r = n * 8 + tq * 2 + c;
         if (g == 0) {
-          jm[warp * R + r] = ref[n][c];
+          jm[warp * R + r] = 7.f - off[n][c];
           jl[warp * R + r] = l[n][c];
         }
-        float* row = join + (warp * R + r) * Cfg::kAccPitch;
+        float* row = reinterpret_cast<float*>(smem + warp * Cfg::kWarpRing) + r * Cfg::kAccPitch;
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
-          const float back = mx4_scale(top_e[i]);
+          const float back = mx4_scale(top_e[i >> 2] >> (8 * (i & 3)) & 255u);
 #pragma unroll
           for (int k = 0; k < 2; ++k)
             *reinterpret_cast<float2*>(row + i * 32 + 4 * g + 2 * k) = make_float2(acc[n][i][k][c] * back, acc[n][i][k][2 + c] * back);
@@ -856,7 +871,7 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
         const float f = ex2(jm[w * R + r] - base);
-        const float4 x = *reinterpret_cast<const float4*>(join + (w * R + r) * Cfg::kAccPitch + d);
+        const float4 x = *reinterpret_cast<const float4*>(smem + w * Cfg::kWarpRing + (r * Cfg::kAccPitch + d) * 4);
         sum += jl[w * R + r] * f;
         o.x += x.x * f; o.y += x.y * f; o.z += x.z * f; o.w += x.w * f;
       }
@@ -882,17 +897,28 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
   }
 }
 
-// Segments that several blocks share, in block order; zeros for segments without a tile.  A block per segment and 32 rows.
-constexpr int kJoinRows = 32;
+// Segments that several blocks share, joined in a fixed order; zeros for segments without a tile.  A warp adds up a row
+// over the parts `first`, first + step, ...: lane = D / 32 neighbouring dims, four parts requested before the first is
+// used.  Few rows (decoding): the eight warps of a block share one row and meet in shared memory, since a long sequence has a
+// part from every block of the grid (a block per row block that took the parts one by one: 120 us for 296 of them).
+// Many rows: a row per warp.
+constexpr int kJoinWarps = 8;
 
-__global__ void __launch_bounds__(128) attend_join(const AttendParams p, int D) {
-  __shared__ int64_t scratch[8];
+template <int NB>
+__global__ void __launch_bounds__(32 * kJoinWarps) attend_join(const AttendParams p) {
+  constexpr int D = 32 * NB;
+  __shared__ int64_t scratch[2 * kJoinWarps];
+  __shared__ float meet[kJoinWarps][D + 2];
   pdl_wait();
   pdl_launch_dependents();
   const int rb = static_cast<int>(blockIdx.x) % p.row_blocks, bh = static_cast<int>(blockIdx.x) / p.row_blocks;
   const int b = bh / p.c.kv_heads, h = bh % p.c.kv_heads;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const bool shared_row = p.R <= 32;
+  const int r = static_cast<int>(blockIdx.y) * (shared_row ? 1 : kJoinWarps) + (shared_row ? 0 : warp);
+  const int row = rb * p.R + r;
   int64_t all, first;
-  sum_tiles<128>(p, b, &first, &all, scratch);
+  sum_tiles<32 * kJoinWarps>(p, b, &first, &all, scratch);
   const int64_t share = block_share(p, all);
   const int len = clamped_length(p.c, b);
   first += h * head_tiles(p, b);
@@ -900,32 +926,65 @@ __global__ void __launch_bounds__(128) attend_join(const AttendParams p, int D) 
   const int n = seen_tiles(p, len, rb);
   const int64_t c0 = first / share, c1 = n ? (first + n - 1) / share : c0;
   if (n && c0 == c1) return;   // written by the block that had all of it
-  const int R = p.R, r_end = min(R, (static_cast<int>(blockIdx.y) + 1) * kJoinRows);
-  for (int e = threadIdx.x + static_cast<int>(blockIdx.y) * kJoinRows * (D / 4); e < r_end * (D / 4); e += 128) {
-    const int r = e / (D / 4), d = e % (D / 4) * 4;
-    const int row = rb * R + r;
-    if (row >= p.rows) break;
-    float top = __uint_as_float(0xFF800000u), sum = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (n)
-      for (int64_t c = c0; c <= c1; ++c) {
-        const float* slot = p.part + (c * 2 + (c == c0 ? 1 : 0)) * R * (D + 2) + r * (D + 2);
-        const float2 ml = *reinterpret_cast<const float2*>(slot);
-        const float2 x = *reinterpret_cast<const float2*>(slot + d + 2), y = *reinterpret_cast<const float2*>(slot + d + 4);
-        const float t = fmaxf(top, ml.x), base = t == __uint_as_float(0xFF800000u) ? 0.f : t;
-        const float fo = ex2(top - base), fn = ex2(ml.x - base);
-        sum = sum * fo + ml.y * fn;
-        o.x = o.x * fo + x.x * fn; o.y = o.y * fo + x.y * fn; o.z = o.z * fo + y.x * fn; o.w = o.w * fo + y.y * fn;
-        top = t;
+  const float ninf = __uint_as_float(0xFF800000u);
+  float top = ninf, sum = 0.f, o[NB];
+#pragma unroll
+  for (int i = 0; i < NB; ++i) o[i] = 0.f;
+  const auto add = [&](float ref, float l, const float (&x)[NB]) {
+    const float t = fmaxf(top, ref), base = t == ninf ? 0.f : t;
+    const float fo = ex2(top - base), fn = ex2(ref - base);
+    sum = sum * fo + l * fn;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) o[i] = o[i] * fo + x[i] * fn;
+    top = t;
+  };
+  if (n && row < p.rows) {
+    const int step = shared_row ? kJoinWarps : 1;
+    for (int64_t c = c0 + (shared_row ? warp : 0); c <= c1; c += 4 * step) {
+      float2 ml[4];
+      float x[4][NB];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int64_t part = c + k * step;
+        if (part <= c1) {
+          const float* slot = p.part + ((part * 2 + (part == c0 ? 1 : 0)) * p.R + r) * (D + 2);
+          ml[k] = *reinterpret_cast<const float2*>(slot);
+#pragma unroll
+          for (int i = 0; i < NB; i += 2) {
+            const float2 v = *reinterpret_cast<const float2*>(slot + 2 + lane * NB + i);
+            x[k][i] = v.x;
+            x[k][i + 1] = v.y;
+          }
+        }
       }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    const int64_t to = out_row(p, b, h, row, D) + d;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (c + k * step <= c1) add(ml[k].x, ml[k].y, x[k]);
+    }
+  }
+  if (shared_row) {
+    if (lane == 0) { meet[warp][D] = top; meet[warp][D + 1] = sum; }
+#pragma unroll
+    for (int i = 0; i < NB; ++i) meet[warp][lane * NB + i] = o[i];
+    __syncthreads();
+    if (warp != 0) return;
+    for (int w = 1; w < kJoinWarps; ++w) {
+      float x[NB];
+#pragma unroll
+      for (int i = 0; i < NB; ++i) x[i] = meet[w][lane * NB + i];
+      add(meet[w][D], meet[w][D + 1], x);
+    }
+  }
+  if (row >= p.rows) return;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const int64_t to = out_row(p, b, h, row, D) + lane * NB;
+#pragma unroll
+  for (int i = 0; i < NB; i += 2) {
     if (p.out_bf16)
-      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + to) =
-          make_uint2(pack_bf16x2(__float_as_uint(o.x * inv), __float_as_uint(o.y * inv)),
-                     pack_bf16x2(__float_as_uint(o.z * inv), __float_as_uint(o.w * inv)));
+      *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + to + i) =
+          pack_bf16x2(__float_as_uint(o[i] * inv), __float_as_uint(o[i + 1] * inv));
     else
-      *reinterpret_cast<float4*>(static_cast<float*>(p.out) + to) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+      *reinterpret_cast<float2*>(static_cast<float*>(p.out) + to + i) = make_float2(o[i] * inv, o[i + 1] * inv);
   }
 }
 
@@ -1139,11 +1198,14 @@ int gl_attend_cache4(const gl_ap* q, int64_t token_pitch, const gl_cache4* cache
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   p.R = k.rows;
   p.tile = k.tile;
-  p.min_share = k.min_share;
+  // (no more than a segment can have: a block that takes several short segments takes them one after the other)
+  p.min_share = std::min<int>(k.min_share, (p.c.capacity + k.tile - 1) / k.tile);
   if (launch_pdl(k.fn, dim3(static_cast<unsigned>(p.grid)), dim3(static_cast<unsigned>(k.threads)), static_cast<size_t>(k.smem), st, 1, p) != cudaSuccess)
     return GL_ERR_CUDA;
-  return launch_pdl(attend_join, dim3(static_cast<unsigned>(segments), static_cast<unsigned>((k.rows + kJoinRows - 1) / kJoinRows)), dim3(128), 0, st, 1, p,
-                    cache->head_dim) == cudaSuccess
+  const int per = k.rows <= 32 ? 1 : kJoinWarps;
+  const unsigned row_groups = static_cast<unsigned>((std::min<int64_t>(rows, k.rows) + per - 1) / per);
+  void (*const join)(AttendParams) = cache->head_dim == 64 ? attend_join<2> : cache->head_dim == 128 ? attend_join<4> : attend_join<8>;
+  return launch_pdl(join, dim3(static_cast<unsigned>(segments), row_groups), dim3(32 * kJoinWarps), 0, st, 1, p) == cudaSuccess
              ? GL_OK : GL_ERR_CUDA;
 }
 
