@@ -182,7 +182,8 @@ struct AttendParams {
   int64_t q_pitch;
   int T, heads, group;   // group = heads / kv_heads
   int rows, row_blocks;  // rows = T * group
-  int R, tile;           // rows per row block, tokens per tile
+  int R, tile_log2;      // rows per row block, tokens per tile (a power of two)
+  FastDiv div_group;
   int grid;
   int min_share;         // tiles that a block takes at least
   float scale_log2;      // softmax scale * log2(e)
@@ -192,10 +193,10 @@ struct AttendParams {
 // Tokens that the rows of row block rb can see at most, and the tiles that hold them.
 __device__ __forceinline__ int seen_by(const AttendParams& p, int len, int rb) {
   const int last = min(p.rows, (rb + 1) * p.R) - 1;
-  return min(max(len - p.T + last / p.group + 1, 0), len);
+  return min(max(len - p.T + static_cast<int>(p.div_group.div(static_cast<uint32_t>(last))) + 1, 0), len);
 }
 __device__ __forceinline__ int seen_tiles(const AttendParams& p, int len, int rb) {
-  return (seen_by(p, len, rb) + p.tile - 1) / p.tile;
+  return (seen_by(p, len, rb) + (1 << p.tile_log2) - 1) >> p.tile_log2;
 }
 
 // Tiles of one kv head of sequence b over all row blocks.
@@ -280,12 +281,17 @@ struct Walk {
   }
 };
 
-// Element 0 of the result row of query row `row` of (b, h).
+// Token of a query row, and element 0 of the row's result and of the row itself.
+__device__ __forceinline__ int row_token(const AttendParams& p, int row) {
+  return static_cast<int>(p.div_group.div(static_cast<uint32_t>(row)));
+}
 __device__ __forceinline__ int64_t out_row(const AttendParams& p, int b, int h, int row, int D) {
-  return ((static_cast<int64_t>(b) * p.T + row / p.group) * p.heads + static_cast<int64_t>(h) * p.group + row % p.group) * D;
+  const int t = row_token(p, row);
+  return ((static_cast<int64_t>(b) * p.T + t) * p.heads + static_cast<int64_t>(h) * p.group + row - t * p.group) * D;
 }
 __device__ __forceinline__ const uint16_t* q_row(const AttendParams& p, int b, int h, int row, int D) {
-  return p.q + (static_cast<int64_t>(b) * p.T + row / p.group) * p.q_pitch + (static_cast<int64_t>(h) * p.group + row % p.group) * D;
+  const int t = row_token(p, row);
+  return p.q + (static_cast<int64_t>(b) * p.T + t) * p.q_pitch + (static_cast<int64_t>(h) * p.group + row - t * p.group) * D;
 }
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -531,7 +537,7 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
         off[n][c] = -ninf;
         l[n][c] = 0.f;
         cf[n][c] = qfac[n * 8 + tq * 2 + c];
-        limit[n][c] = row < p.rows ? min(len, len - p.T + row / p.group + 1) : seen;   // (rows past the end: anything)
+        limit[n][c] = row < p.rows ? min(len, len - p.T + row_token(p, row) + 1) : seen;   // (rows past the end: anything)
         all_see = min(all_see, limit[n][c]);
         any_sees = max(any_sees, limit[n][c]);
       }
@@ -688,19 +694,49 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
         }
       // Distance of every scale from its block's reference, byte by byte: 0..7 all over is the plain case.  (References are 8 at
       // least: no distance that is none of these looks like one after the borrow.)
-      uint32_t far = masked ? 1u << 31 : 0u;
       uint32_t fs[2][4][kScaleWords];   // high bytes of fp16 2^-d
+      const auto plain = [&]() {
+        uint32_t far = 0;
 #pragma unroll
-      for (int k2 = 0; k2 < kScaleWords; ++k2)
+        for (int k2 = 0; k2 < kScaleWords; ++k2)
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
+          for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const uint32_t d = top_e[k2] - vs[mt][k][k2];
-            far |= d & 0xF8F8F8F8u;
-            fs[mt][k][k2] = 0x3C3C3C3Cu - 4u * d;
-          }
-      if (!__any_sync(0xFFFFFFFFu, far != 0)) {
+            for (int k = 0; k < 4; ++k) {
+              const uint32_t d = top_e[k2] - vs[mt][k][k2];
+              far |= d & 0xF8F8F8F8u;
+              fs[mt][k][k2] = 0x3C3C3C3Cu - 4u * d;
+            }
+        return !__any_sync(0xFFFFFFFFu, far != 0);
+      };
+      // Brings block i's reference up to `top`, one binade more than needed so that the next larger scale finds room.
+      const auto raise = [&](int i, uint32_t top) {
+        const uint32_t base = top_e[i >> 2] >> (8 * (i & 3)) & 255u;
+        if (top <= base) return base;
+        top = min(top + 1u, 254u);
+        const float f = top - base > 126u ? 0.f : __uint_as_float((127u - (top - base)) << 23);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) { acc[n][i][0][c] *= f; acc[n][i][1][c] *= f; }
+        top_e[i >> 2] += (top - base) << (8 * (i & 3));
+        return top;
+      };
+      bool easy = !masked && plain();
+      if (!easy && !masked) {
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+          uint32_t top = 0;
+#pragma unroll
+          for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) top = max(top, vs[mt][k][i >> 2] >> (8 * (i & 3)) & 255u);
+          top = __reduce_max_sync(0xFFFFFFFFu, top);
+          if (top < 255u) raise(i, top);
+        }
+        easy = plain();
+      }
+      if (easy) {
 #pragma unroll
         for (int w2 = 0; w2 < NB / 2; ++w2) {
 #pragma unroll
@@ -727,8 +763,8 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
           }
         }
       } else {
-        // The end of a sequence, missing pages, NaN, a new largest scale, or scales far apart: per block, the tokens within
-        // seven binades of the largest scale left, then the next ones.
+        // The end of a sequence, missing pages, NaN, or scales far apart: per block, the tokens within seven binades of the
+        // largest scale left, then the next ones.
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
           uint32_t ex[2][4];   // 256: not seen, or done
@@ -745,16 +781,7 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
               if (e < 255u) top = max(top, e);
             }
           top = __reduce_max_sync(0xFFFFFFFFu, top);
-          uint32_t base = top_e[i >> 2] >> (8 * (i & 3)) & 255u;
-          if (top > base) {
-            const float f = top - base > 126u ? 0.f : __uint_as_float((127u - (top - base)) << 23);
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-              for (int c = 0; c < 4; ++c) { acc[n][i][0][c] *= f; acc[n][i][1][c] *= f; }
-            top_e[i >> 2] += (top - base) << (8 * (i & 3));
-            base = top;
-          }
+          const uint32_t base = raise(i, top);
           bool more;
           do {
             uint32_t f2[2][2];
@@ -1197,7 +1224,8 @@ int gl_attend_cache4(const gl_ap* q, int64_t token_pitch, const gl_cache4* cache
   p.out_bf16 = f32 ? 0 : 1;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   p.R = k.rows;
-  p.tile = k.tile;
+  p.tile_log2 = k.tile == 64 ? 6 : 7;
+  p.div_group.set(group);
   // (no more than a segment can have: a block that takes several short segments takes them one after the other)
   p.min_share = std::min<int>(k.min_share, (p.c.capacity + k.tile - 1) / k.tile);
   if (launch_pdl(k.fn, dim3(static_cast<unsigned>(p.grid)), dim3(static_cast<unsigned>(k.threads)), static_cast<size_t>(k.smem), st, 1, p) != cudaSuccess)

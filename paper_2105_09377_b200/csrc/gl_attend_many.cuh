@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
         __syncwarp();
         if (lane == 0) mbar_arrive(b_q + 8 * m);
       }
-      const int limit = live ? min(w.len, w.len - p.T + row / p.group + 1) : 0;
+      const int limit = live ? min(w.len, w.len - p.T + row_token(p, row) + 1) : 0;
       float ref = ninf, sum = 0.f;
       for (int tile = w.t0; tile < w.t1; ++tile, ++it) {
         if (!mbar_wait(b_s + 8 * m, it & 1u, abort_flag)) { ok = false; break; }
@@ -315,7 +315,7 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
       auto find = [&](int tile) {
         int32_t page = -1;
         const int pos = tile * TT + lane * 16;
-        if (lane < kGroups && pos < w.seen) page = p.c.table[static_cast<int64_t>(w.b) * p.c.width + pos / p.c.page_tokens];
+        if (lane < kGroups && pos < w.seen) page = p.c.table[static_cast<int64_t>(w.b) * p.c.width + p.c.div_page.div(static_cast<uint32_t>(pos))];
         const bool there = page >= 0 && page < p.c.pages;
         tile_have = __ballot_sync(0xFFFFFFFFu, there);
         hk.live = 0;
@@ -323,9 +323,10 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
         for (int i = 0; i < kItems; ++i) {
           const int g = 2 * i + (dw >> 1), tok = 32 * i + dw * 8 + (lane & 7);
           const int32_t pg = __shfl_sync(0xFFFFFFFFu, page, g);
-          const int at = tile * TT + g * 16;
+          uint32_t slot, in_page;
+          p.c.div_page.divmod(static_cast<uint32_t>(tile * TT + g * 16), slot, in_page);
           group[i] = p.c.data + static_cast<int64_t>(pg) * p.c.page_stride + w.h * p.c.head_stride +
-                     static_cast<int64_t>(at % p.c.page_tokens / kGroup) * group_bytes(D);
+                     static_cast<int64_t>(in_page / kGroup) * group_bytes(D);
           if ((tile_have >> g & 1u) && tile * TT + tok < w.seen) hk.live |= 1u << i;
         }
         hv.live = hk.live;
