@@ -169,10 +169,8 @@ __global__ void __launch_bounds__(256) cache4_read(uint16_t* __restrict__ k, uin
 // ring of bulk copies, running maximum, sum and result; the block joins its warps, and a second kernel joins the
 // blocks where a segment was cut.
 
-constexpr int kTileTok = 64;      // tokens per tile: what a warp waits for and asks for at a time
 constexpr int kSubTok = 32;       // tokens that a warp computes with at a time
 constexpr int kWarps = 4;
-constexpr int kStagesAt = 2;
 
 struct AttendParams {
   CacheView c;
@@ -245,13 +243,47 @@ struct Walk {
   int64_t at, end, seg0, per_head;
   int b, h, rb, t0, t1, n_seg, len, seen;
 
-  __device__ __forceinline__ void start(const AttendParams& p, int64_t all, int block) {
+  // Finds the block's part, by the whole block (scratch: 2 * THREADS / 32 + 4 words): the sequences' tiles are counted by a
+  // thread each and scanned.  (One thread that walks along 64 sequences takes 3 us.)
+  template <int THREADS>
+  __device__ __forceinline__ void start(const AttendParams& p, int block, int64_t* scratch) {
+    int64_t all, before;
+    sum_tiles<THREADS>(p, 0, &before, &all, scratch);
     const int64_t share = block_share(p, all);
     at = block * share;
     end = min(all, at + share);
     b = 0;
-    seg0 = 0;
-    per_head = at < end ? head_tiles(p, 0) : 0;
+    seg0 = per_head = 0;
+    if (at >= end) return;   // (block-uniform)
+    int64_t* found = scratch + 2 * (THREADS / 32);
+    int64_t done = 0;        // tiles of the sequences before this round
+    for (int first = 0; first < p.c.batch; first += THREADS) {
+      const int i = first + static_cast<int>(threadIdx.x), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+      const int64_t heads = i < p.c.batch ? head_tiles(p, i) : 0, mine = heads * p.c.kv_heads;
+      int64_t upto = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t x = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+        if (lane >= o) upto += x;
+      }
+      __syncthreads();
+      if (lane == 31) scratch[warp] = upto;
+      __syncthreads();
+      int64_t total = 0, off = 0;
+#pragma unroll
+      for (int w = 0; w < THREADS / 32; ++w) {
+        if (w < warp) off += scratch[w];
+        total += scratch[w];
+      }
+      const int64_t from = done + off + upto - mine;
+      if (from <= at && at < from + mine) { found[0] = i; found[1] = from; found[2] = heads; }
+      done += total;
+      if (done > at) break;
+    }
+    __syncthreads();
+    b = static_cast<int>(found[0]);
+    seg0 = found[1];
+    per_head = found[2];
   }
   __device__ __forceinline__ bool next(const AttendParams& p) {
     if (at >= end) return false;
@@ -407,6 +439,10 @@ template <int NB, int NT>
 struct AttCfg {
   static constexpr int D = 32 * NB;
   static constexpr int R = 8 * NT;
+  // Tokens per tile (what a warp waits for and asks for at a time) and tiles in a warp's ring: 64 and 2, but 32 and 3 for
+  // 256-wide heads, whose rings would leave room for one block per SM (32 x 4096 tokens: 98 us, 81 us with two blocks).
+  static constexpr int kTileTok = NB == 8 ? 32 : 64;
+  static constexpr int kStagesAt = NB == 8 ? 3 : 2;
   static constexpr int kStage = kTileTok / kGroup * group_bytes(D);  // one tile
   static constexpr int kRing = kWarps * kStagesAt * kStage;
   static constexpr int kQ = NB * 2 * NT * 32 * 8;                    // fragments of Q
@@ -421,7 +457,7 @@ struct AttCfg {
 template <int NB, int NT, bool HILO>
 __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams p) {
   using Cfg = AttCfg<NB, NT>;
-  constexpr int D = Cfg::D, R = Cfg::R;
+  constexpr int D = Cfg::D, R = Cfg::R, kTileTok = Cfg::kTileTok, kStagesAt = Cfg::kStagesAt;
   extern __shared__ __align__(128) unsigned char smem[];
   uint2* qfrag = reinterpret_cast<uint2*>(smem + Cfg::kRing);
   float* qfac = reinterpret_cast<float*>(smem + Cfg::kRing + Cfg::kQ);
@@ -429,8 +465,8 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
   float* jl = jm + kWarps * R;
   unsigned char* tail = smem + Cfg::kRing + Cfg::kQ + R * 4 + 2 * kWarps * R * 4;
   uint64_t* bars = reinterpret_cast<uint64_t*>(tail);                          // [kWarps][kStagesAt]
-  int64_t* scratch = reinterpret_cast<int64_t*>(tail + 8 * kWarps * kStagesAt);   // [2 * kWarps]
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 8 * kWarps * kStagesAt + 16 * kWarps);
+  int64_t* scratch = reinterpret_cast<int64_t*>(tail + 8 * kWarps * kStagesAt);   // [2 * kWarps + 4]
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 8 * kWarps * kStagesAt + 16 * kWarps + 32);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, tq = lane & 3;
 
   if (threadIdx.x == 0) {
@@ -441,10 +477,8 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
   }
   pdl_wait();
   pdl_launch_dependents();
-  int64_t all, before;
-  sum_tiles<kWarps * 32>(p, 0, &before, &all, scratch);   // (its barrier also publishes the ones set up above)
   Walk w;
-  w.start(p, all, blockIdx.x);
+  w.start<kWarps * 32>(p, blockIdx.x, scratch);   // (its barriers also publish the ones set up above)
 
   const uint32_t my_ring = smem_u32(smem) + warp * kStagesAt * Cfg::kStage;
   const uint32_t my_bar = smem_u32(bars + warp * kStagesAt);
@@ -1101,8 +1135,8 @@ struct AttKernel {
 
 template <int NB, int NT>
 AttKernel few_kernel(bool hilo) {
-  return {hilo ? attend_cache4<NB, NT, true> : attend_cache4<NB, NT, false>, AttCfg<NB, NT>::kSmem, kWarps * 32, 8 * NT, kTileTok,
-          kWarps, 4};
+  return {hilo ? attend_cache4<NB, NT, true> : attend_cache4<NB, NT, false>, AttCfg<NB, NT>::kSmem, kWarps * 32, 8 * NT,
+          AttCfg<NB, NT>::kTileTok,           kWarps, 4};
 }
 template <int NB>
 AttKernel many_kernel(bool f32) {
@@ -1224,7 +1258,7 @@ int gl_attend_cache4(const gl_ap* q, int64_t token_pitch, const gl_cache4* cache
   p.out_bf16 = f32 ? 0 : 1;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   p.R = k.rows;
-  p.tile_log2 = k.tile == 64 ? 6 : 7;
+  p.tile_log2 = k.tile == 32 ? 5 : k.tile == 64 ? 6 : 7;
   p.div_group.set(group);
   // (no more than a segment can have: a block that takes several short segments takes them one after the other)
   p.min_share = std::min<int>(k.min_share, (p.c.capacity + k.tile - 1) / k.tile);

@@ -28,7 +28,7 @@ struct ManyCfg {
   static constexpr int kStages = 2;
   static constexpr int kWarps = 4 * MT + 5;
   static constexpr int kThreads = 32 * kWarps;
-  static constexpr int kSmem = MT * kQ + kStages * 2 * kKV + 1024 + 512;
+  static constexpr int kSmem = MT * kQ + kStages * 2 * kKV + 1024 + 544;
   // tensor memory: scores (weights take their place), third terms, results
   static constexpr int kS = 0;
   static constexpr int kLow = MT * TT;
@@ -112,8 +112,8 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile uint32_t* have = reinterpret_cast<volatile uint32_t*>(tmem_slot + 2);   // [4] groups of a tile that have a page
   int* nan_from = reinterpret_cast<int*>(tmem_slot + 6);                           // [4][NB] first token whose V block is NaN
-  int64_t* scratch = reinterpret_cast<int64_t*>(tail + 288);                       // [2 * kWarps]
-  static_assert(288 + 16 * Cfg::kWarps <= 512 && 128 + 24 + 16 * 8 <= 288, "tail");
+  int64_t* scratch = reinterpret_cast<int64_t*>(tail + 288);                       // [2 * kWarps + 4]
+  static_assert(288 + 16 * Cfg::kWarps + 32 <= 544 && 128 + 24 + 16 * 8 <= 288, "tail");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   constexpr int kWiden = 4 * MT, kMma = 4 * MT + 4;
 
@@ -138,13 +138,11 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
   }
   pdl_wait();
   pdl_launch_dependents();
-  int64_t all, before;
   tc_fence_before();
-  sum_tiles<Cfg::kThreads>(p, 0, &before, &all, scratch);   // (its barrier also publishes the set-up above)
+  Walk w;
+  w.start<Cfg::kThreads>(p, blockIdx.x, scratch);   // (its barriers also publish the set-up above)
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  Walk w;
-  w.start(p, all, blockIdx.x);
   uint32_t it = 0;     // tiles so far, the same for every role
   uint32_t item = 0;
   bool ok = true;
