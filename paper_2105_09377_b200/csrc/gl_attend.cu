@@ -183,7 +183,8 @@ struct AttendParams {
   int R, tile_log2;      // rows per row block, tokens per tile (a power of two)
   FastDiv div_group;
   int grid;
-  int min_share;         // tiles that a block takes at least
+  int min_share;         // list entries that a block takes at least
+  int lead;              // what a segment costs beyond its tiles, in tiles (see Walk)
   float scale_log2;      // softmax scale * log2(e)
   int out_bf16;
 };
@@ -197,20 +198,27 @@ __device__ __forceinline__ int seen_tiles(const AttendParams& p, int len, int rb
   return (seen_by(p, len, rb) + (1 << p.tile_log2) - 1) >> p.tile_log2;
 }
 
-// Tiles of one kv head of sequence b over all row blocks.
-__device__ __forceinline__ int64_t head_tiles(const AttendParams& p, int b) {
+// Entries of the work list for a row block and for one kv head of sequence b: its tiles, with `lead` empty entries before
+// them that stand for what every segment costs (fragments of Q, filling the ring, joining the warps).  Without them a
+// block that meets many short sequences gets as many tiles as the others and ends last (16384 and 32 tokens in turn: 66 us,
+// 46 us for the long ones alone).
+__device__ __forceinline__ int seen_entries(const AttendParams& p, int len, int rb) {
+  const int n = seen_tiles(p, len, rb);
+  return n ? n + p.lead : 0;
+}
+__device__ __forceinline__ int64_t head_entries(const AttendParams& p, int b) {
   const int len = clamped_length(p.c, b);
   int64_t n = 0;
-  for (int rb = 0; rb < p.row_blocks; ++rb) n += seen_tiles(p, len, rb);
+  for (int rb = 0; rb < p.row_blocks; ++rb) n += seen_entries(p, len, rb);
   return n;
 }
 
-// Sum of head_tiles over the sequences before `upto` and over all of them, by the whole block.
+// Sum of head_entries over the sequences before `upto` and over all of them, by the whole block.
 template <int THREADS>
-__device__ __forceinline__ void sum_tiles(const AttendParams& p, int upto, int64_t* before, int64_t* all, int64_t* scratch) {
+__device__ __forceinline__ void sum_entries(const AttendParams& p, int upto, int64_t* before, int64_t* all, int64_t* scratch) {
   int64_t a = 0, b = 0;
   for (int i = threadIdx.x; i < p.c.batch; i += THREADS) {
-    const int64_t n = head_tiles(p, i);
+    const int64_t n = head_entries(p, i);
     a += n;
     if (i < upto) b += n;
   }
@@ -231,7 +239,7 @@ __device__ __forceinline__ void sum_tiles(const AttendParams& p, int upto, int64
   *before = b * p.c.kv_heads;
 }
 
-// Tiles per block: an even share, but no less than min_share.
+// Entries per block: an even share, but no less than min_share.
 __device__ __forceinline__ int64_t block_share(const AttendParams& p, int64_t all) {
   const int64_t n = (all + p.grid - 1) / p.grid;
   return n < p.min_share ? p.min_share : n;
@@ -248,7 +256,7 @@ struct Walk {
   template <int THREADS>
   __device__ __forceinline__ void start(const AttendParams& p, int block, int64_t* scratch) {
     int64_t all, before;
-    sum_tiles<THREADS>(p, 0, &before, &all, scratch);
+    sum_entries<THREADS>(p, 0, &before, &all, scratch);
     const int64_t share = block_share(p, all);
     at = block * share;
     end = min(all, at + share);
@@ -259,7 +267,7 @@ struct Walk {
     int64_t done = 0;        // tiles of the sequences before this round
     for (int first = 0; first < p.c.batch; first += THREADS) {
       const int i = first + static_cast<int>(threadIdx.x), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-      const int64_t heads = i < p.c.batch ? head_tiles(p, i) : 0, mine = heads * p.c.kv_heads;
+      const int64_t heads = i < p.c.batch ? head_entries(p, i) : 0, mine = heads * p.c.kv_heads;
       int64_t upto = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -286,25 +294,31 @@ struct Walk {
     per_head = found[2];
   }
   __device__ __forceinline__ bool next(const AttendParams& p) {
-    if (at >= end) return false;
-    while (seg0 + per_head * p.c.kv_heads <= at) {
-      if (b + 1 >= p.c.batch) return false;   // (only if lengths changed under the kernel)
-      seg0 += per_head * p.c.kv_heads;
-      per_head = head_tiles(p, ++b);
+    while (at < end) {
+      while (seg0 + per_head * p.c.kv_heads <= at) {
+        if (b + 1 >= p.c.batch) return false;   // (only if lengths changed under the kernel)
+        seg0 += per_head * p.c.kv_heads;
+        per_head = head_entries(p, ++b);
+      }
+      len = clamped_length(p.c, b);
+      h = static_cast<int>((at - seg0) / per_head);
+      int64_t s0 = seg0 + h * per_head;
+      int n = 0;
+      for (rb = 0;; ++rb) {
+        n = seen_entries(p, len, rb);
+        if (s0 + n > at || rb + 1 == p.row_blocks) break;
+        s0 += n;
+      }
+      const int64_t stop = min(end, s0 + n);
+      if (stop <= at) return false;             // (the same)
+      n_seg = n - p.lead;
+      t0 = max(static_cast<int>(at - s0) - p.lead, 0);
+      t1 = static_cast<int>(stop - s0) - p.lead;
+      seen = seen_by(p, len, rb);
+      at = stop;
+      if (t1 > t0) return true;
     }
-    len = clamped_length(p.c, b);
-    h = static_cast<int>((at - seg0) / per_head);
-    int64_t s0 = seg0 + h * per_head;
-    for (rb = 0;; ++rb) {
-      n_seg = seen_tiles(p, len, rb);
-      if (s0 + n_seg > at || rb + 1 == p.row_blocks) break;
-      s0 += n_seg;
-    }
-    t0 = static_cast<int>(at - s0);
-    t1 = static_cast<int>(min(end - s0, static_cast<int64_t>(n_seg)));
-    seen = seen_by(p, len, rb);
-    at = s0 + t1;
-    return t1 > t0;
+    return false;
   }
   __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == n_seg; }
   // where this block's part of a segment that it does not have to itself goes: it is the block's last or its first
@@ -958,15 +972,16 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
   }
 }
 
-// Segments that several blocks share, joined in a fixed order; zeros for segments without a tile.  A warp adds up a row
-// over the parts `first`, first + step, ...: lane = D / 32 neighbouring dims, four parts requested before the first is
-// used.  Few rows (decoding): the eight warps of a block share one row and meet in shared memory, since a long sequence has a
-// part from every block of the grid (a block per row block that took the parts one by one: 120 us for 296 of them).
-// Many rows: a row per warp.
+// Segments that several blocks share, joined in a fixed order; zeros for segments without a tile.  `wpr` warps share a row:
+// each adds up every wpr-th part (lane = D / 32 neighbouring dims, four parts requested before the first is used), then
+// they meet in shared memory.  Eight to a row when there are few rows in all (a long sequence has a part from every block
+// of the grid: one warp that takes 296 of them by itself needs 120 us), else as few as fill a block.
 constexpr int kJoinWarps = 8;
 
+struct JoinShape { int wpr, rows_per_block; };
+
 template <int NB>
-__global__ void __launch_bounds__(32 * kJoinWarps) attend_join(const AttendParams p) {
+__global__ void __launch_bounds__(32 * kJoinWarps) attend_join(const AttendParams p, const JoinShape js) {
   constexpr int D = 32 * NB;
   __shared__ int64_t scratch[2 * kJoinWarps];
   __shared__ float meet[kJoinWarps][D + 2];
@@ -975,77 +990,80 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join(const AttendParam
   const int rb = static_cast<int>(blockIdx.x) % p.row_blocks, bh = static_cast<int>(blockIdx.x) / p.row_blocks;
   const int b = bh / p.c.kv_heads, h = bh % p.c.kv_heads;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const bool shared_row = p.R <= 32;
-  const int r = static_cast<int>(blockIdx.y) * (shared_row ? 1 : kJoinWarps) + (shared_row ? 0 : warp);
-  const int row = rb * p.R + r;
   int64_t all, first;
-  sum_tiles<32 * kJoinWarps>(p, b, &first, &all, scratch);
+  sum_entries<32 * kJoinWarps>(p, b, &first, &all, scratch);
   const int64_t share = block_share(p, all);
   const int len = clamped_length(p.c, b);
-  first += h * head_tiles(p, b);
-  for (int i = 0; i < rb; ++i) first += seen_tiles(p, len, i);
+  first += h * head_entries(p, b);
+  for (int i = 0; i < rb; ++i) first += seen_entries(p, len, i);
   const int n = seen_tiles(p, len, rb);
-  const int64_t c0 = first / share, c1 = n ? (first + n - 1) / share : c0;
+  const int64_t c0 = (first + p.lead) / share, c1 = n ? (first + p.lead + n - 1) / share : c0;
   if (n && c0 == c1) return;   // written by the block that had all of it
   const float ninf = __uint_as_float(0xFF800000u);
-  float top = ninf, sum = 0.f, o[NB];
+  const int sub = warp % js.wpr, r0 = static_cast<int>(blockIdx.y) * js.rows_per_block;
+  for (int r1 = 0; r1 < js.rows_per_block; r1 += kJoinWarps / js.wpr) {   // (block-uniform)
+    if (rb * p.R + r0 + r1 >= p.rows) break;
+    const int r = r0 + r1 + warp / js.wpr, row = rb * p.R + r;
+    const bool live = r < r0 + js.rows_per_block && row < p.rows;
+    float top = ninf, sum = 0.f, o[NB];
 #pragma unroll
-  for (int i = 0; i < NB; ++i) o[i] = 0.f;
-  const auto add = [&](float ref, float l, const float (&x)[NB]) {
-    const float t = fmaxf(top, ref), base = t == ninf ? 0.f : t;
-    const float fo = ex2(top - base), fn = ex2(ref - base);
-    sum = sum * fo + l * fn;
+    for (int i = 0; i < NB; ++i) o[i] = 0.f;
+    const auto add = [&](float ref, float l, const float (&x)[NB]) {
+      const float t = fmaxf(top, ref), base = t == ninf ? 0.f : t;
+      const float fo = ex2(top - base), fn = ex2(ref - base);
+      sum = sum * fo + l * fn;
 #pragma unroll
-    for (int i = 0; i < NB; ++i) o[i] = o[i] * fo + x[i] * fn;
-    top = t;
-  };
-  if (n && row < p.rows) {
-    const int step = shared_row ? kJoinWarps : 1;
-    for (int64_t c = c0 + (shared_row ? warp : 0); c <= c1; c += 4 * step) {
-      float2 ml[4];
-      float x[4][NB];
+      for (int i = 0; i < NB; ++i) o[i] = o[i] * fo + x[i] * fn;
+      top = t;
+    };
+    if (n && live) {
+      for (int64_t c = c0 + sub; c <= c1; c += 4 * js.wpr) {
+        float2 ml[4];
+        float x[4][NB];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int64_t part = c + k * step;
-        if (part <= c1) {
-          const float* slot = p.part + ((part * 2 + (part == c0 ? 1 : 0)) * p.R + r) * (D + 2);
-          ml[k] = *reinterpret_cast<const float2*>(slot);
+        for (int k = 0; k < 4; ++k) {
+          const int64_t part = c + k * js.wpr;
+          if (part <= c1) {
+            const float* slot = p.part + ((part * 2 + (part == c0 ? 1 : 0)) * p.R + r) * (D + 2);
+            ml[k] = *reinterpret_cast<const float2*>(slot);
 #pragma unroll
-          for (int i = 0; i < NB; i += 2) {
-            const float2 v = *reinterpret_cast<const float2*>(slot + 2 + lane * NB + i);
-            x[k][i] = v.x;
-            x[k][i + 1] = v.y;
+            for (int i = 0; i < NB; i += 2) {
+              const float2 v = *reinterpret_cast<const float2*>(slot + 2 + lane * NB + i);
+              x[k][i] = v.x;
+              x[k][i + 1] = v.y;
+            }
           }
         }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (c + k * js.wpr <= c1) add(ml[k].x, ml[k].y, x[k]);
       }
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (c + k * step <= c1) add(ml[k].x, ml[k].y, x[k]);
     }
-  }
-  if (shared_row) {
-    if (lane == 0) { meet[warp][D] = top; meet[warp][D + 1] = sum; }
+    if (js.wpr > 1) {
+      __syncthreads();   // the previous row's sums are read
+      if (lane == 0) { meet[warp][D] = top; meet[warp][D + 1] = sum; }
 #pragma unroll
-    for (int i = 0; i < NB; ++i) meet[warp][lane * NB + i] = o[i];
-    __syncthreads();
-    if (warp != 0) return;
-    for (int w = 1; w < kJoinWarps; ++w) {
-      float x[NB];
+      for (int i = 0; i < NB; ++i) meet[warp][lane * NB + i] = o[i];
+      __syncthreads();
+      if (sub != 0) continue;
+      for (int w = warp + 1; w < warp + js.wpr; ++w) {
+        float x[NB];
 #pragma unroll
-      for (int i = 0; i < NB; ++i) x[i] = meet[w][lane * NB + i];
-      add(meet[w][D], meet[w][D + 1], x);
+        for (int i = 0; i < NB; ++i) x[i] = meet[w][lane * NB + i];
+        add(meet[w][D], meet[w][D + 1], x);
+      }
     }
-  }
-  if (row >= p.rows) return;
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  const int64_t to = out_row(p, b, h, row, D) + lane * NB;
+    if (!live) continue;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const int64_t to = out_row(p, b, h, row, D) + lane * NB;
 #pragma unroll
-  for (int i = 0; i < NB; i += 2) {
-    if (p.out_bf16)
-      *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + to + i) =
-          pack_bf16x2(__float_as_uint(o[i] * inv), __float_as_uint(o[i + 1] * inv));
-    else
-      *reinterpret_cast<float2*>(static_cast<float*>(p.out) + to + i) = make_float2(o[i] * inv, o[i + 1] * inv);
+    for (int i = 0; i < NB; i += 2) {
+      if (p.out_bf16)
+        *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + to + i) =
+            pack_bf16x2(__float_as_uint(o[i] * inv), __float_as_uint(o[i + 1] * inv));
+      else
+        *reinterpret_cast<float2*>(static_cast<float*>(p.out) + to + i) = make_float2(o[i] * inv, o[i + 1] * inv);
+    }
   }
 }
 
@@ -1130,18 +1148,19 @@ struct AttKernel {
   void (*fn)(AttendParams);
   int smem, threads;
   int rows, tile, min_share;   // rows per work item, tokens per tile, tiles that a block takes at least
+  int lead;                    // what a segment costs beyond its tiles, in tiles
   int per_sm;                  // most blocks per SM
 };
 
 template <int NB, int NT>
 AttKernel few_kernel(bool hilo) {
   return {hilo ? attend_cache4<NB, NT, true> : attend_cache4<NB, NT, false>, AttCfg<NB, NT>::kSmem, kWarps * 32, 8 * NT,
-          AttCfg<NB, NT>::kTileTok,           kWarps, 4};
+          AttCfg<NB, NT>::kTileTok, kWarps, NB == 8 ? 6 : 3, 4};
 }
 template <int NB>
 AttKernel many_kernel(bool f32) {
-  if (f32) return {attend_many<NB, 3>, ManyCfg<NB, 3>::kSmem, ManyCfg<NB, 3>::kThreads, ManyCfg<NB, 3>::kRows, ManyCfg<NB, 3>::TT, 1, 1};
-  return {attend_many<NB, 1>, ManyCfg<NB, 1>::kSmem, ManyCfg<NB, 1>::kThreads, ManyCfg<NB, 1>::kRows, ManyCfg<NB, 1>::TT, 1, 1};
+  if (f32) return {attend_many<NB, 3>, ManyCfg<NB, 3>::kSmem, ManyCfg<NB, 3>::kThreads, ManyCfg<NB, 3>::kRows, ManyCfg<NB, 3>::TT, 1, 1, 1};
+  return {attend_many<NB, 1>, ManyCfg<NB, 1>::kSmem, ManyCfg<NB, 1>::kThreads, ManyCfg<NB, 1>::kRows, ManyCfg<NB, 1>::TT, 1, 1, 1};
 }
 
 // Up to 32 rows that share a kv head: 8, 16 or 32 of them per warp tile (256-wide heads: 16, two items for more);
@@ -1261,14 +1280,20 @@ int gl_attend_cache4(const gl_ap* q, int64_t token_pitch, const gl_cache4* cache
   p.tile_log2 = k.tile == 32 ? 5 : k.tile == 64 ? 6 : 7;
   p.div_group.set(group);
   // (no more than a segment can have: a block that takes several short segments takes them one after the other)
-  p.min_share = std::min<int>(k.min_share, (p.c.capacity + k.tile - 1) / k.tile);
+  p.lead = k.lead;
+  p.min_share = k.lead + std::min<int>(k.min_share, (p.c.capacity + k.tile - 1) / k.tile);
   if (launch_pdl(k.fn, dim3(static_cast<unsigned>(p.grid)), dim3(static_cast<unsigned>(k.threads)), static_cast<size_t>(k.smem), st, 1, p) != cudaSuccess)
     return GL_ERR_CUDA;
-  const int per = k.rows <= 32 ? 1 : kJoinWarps;
-  const unsigned row_groups = static_cast<unsigned>((std::min<int64_t>(rows, k.rows) + per - 1) / per);
-  void (*const join)(AttendParams) = cache->head_dim == 64 ? attend_join<2> : cache->head_dim == 128 ? attend_join<4> : attend_join<8>;
-  return launch_pdl(join, dim3(static_cast<unsigned>(segments), row_groups), dim3(32 * kJoinWarps), 0, st, 1, p) == cudaSuccess
-             ? GL_OK : GL_ERR_CUDA;
+  JoinShape js = {kJoinWarps, 1};
+  int64_t live = std::min<int64_t>(rows, k.rows), row_groups = live;
+  if (segments * live > 4 * num_sms()) {   // (four blocks per SM at once)
+    js.wpr = live <= 1 ? 8 : live <= 2 ? 4 : live <= 4 ? 2 : 1;
+    js.rows_per_block = static_cast<int>(std::min<int64_t>(live, 64));
+    row_groups = (live + js.rows_per_block - 1) / js.rows_per_block;
+  }
+  void (*const join)(AttendParams, JoinShape) = cache->head_dim == 64 ? attend_join<2> : cache->head_dim == 128 ? attend_join<4> : attend_join<8>;
+  return launch_pdl(join, dim3(static_cast<unsigned>(segments), static_cast<unsigned>(row_groups)), dim3(32 * kJoinWarps), 0, st, 1, p,
+                    js) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
 }
 
 }  // extern "C"
