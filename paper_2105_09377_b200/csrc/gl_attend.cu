@@ -201,7 +201,7 @@ __device__ __forceinline__ int seen_tiles(const AttendParams& p, int len, int rb
 // Entries of the work list for a row block and for one kv head of sequence b: its tiles, with `lead` empty entries before
 // them that stand for what every segment costs (fragments of Q, filling the ring, joining the warps).  Without them a
 // block that meets many short sequences gets as many tiles as the others and ends last (16384 and 32 tokens in turn: 66 us,
-// 46 us for the long ones alone).
+// 45 us with eight of them, as for the long sequences alone).
 __device__ __forceinline__ int seen_entries(const AttendParams& p, int len, int rb) {
   const int n = seen_tiles(p, len, rb);
   return n ? n + p.lead : 0;
@@ -1155,7 +1155,7 @@ struct AttKernel {
 template <int NB, int NT>
 AttKernel few_kernel(bool hilo) {
   return {hilo ? attend_cache4<NB, NT, true> : attend_cache4<NB, NT, false>, AttCfg<NB, NT>::kSmem, kWarps * 32, 8 * NT,
-          AttCfg<NB, NT>::kTileTok, kWarps, NB == 8 ? 6 : 3, 4};
+          AttCfg<NB, NT>::kTileTok, kWarps, NB == 8 ? 16 : 8, 4};
 }
 template <int NB>
 AttKernel many_kernel(bool f32) {
