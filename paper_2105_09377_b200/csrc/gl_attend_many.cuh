@@ -1,7 +1,7 @@
 // Attention over 4-bit pages for many query rows (prompts read in pieces): the two products on tcgen05.
 // Included by gl_attend.cu, whose cache layout, work list and joining it uses.
 //
-// A block has MT x 128 rows that share a kv head and walks along the tokens in tiles of TT.  Four warps widen the
+// A block has MT x 128 rows that share a kv head and walks along the tokens in tiles of TT.  Eight warps widen the
 // tile's codes to bf16, scales included (two significant bits times a power of two: exact), into the swizzled shared-
 // memory layouts of the MMA operands: K as [token][dim] (K-major B of S = Q K^T), V as [token][dim] too, which is the
 // MN-major B of O = P V.  Scores come back from tensor memory a row per thread, are turned into weights and go back
@@ -26,9 +26,10 @@ struct ManyCfg {
   static constexpr int kQ = 128 * D * 2;                        // bytes of one Q tile
   static constexpr int kKV = TT * D * 2;                        // bytes of a K or V tile
   static constexpr int kStages = 2;
-  static constexpr int kWarps = 4 * MT + 5;
+  static constexpr int kWidenWarps = 8;
+  static constexpr int kWarps = 4 * MT + kWidenWarps + 1;
   static constexpr int kThreads = 32 * kWarps;
-  static constexpr int kSmem = MT * kQ + kStages * 2 * kKV + 1024 + 544;
+  static constexpr int kSmem = MT * kQ + kStages * 2 * kKV + 1024 + 640;
   // tensor memory: scores (weights take their place), third terms, results
   static constexpr int kS = 0;
   static constexpr int kLow = MT * TT;
@@ -45,6 +46,25 @@ __device__ __forceinline__ void tc_mma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem,
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
       ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
       : "memory");
+}
+__device__ __forceinline__ void tc_load_64cols(uint32_t taddr, uint32_t (&r)[64]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
+      "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
+      "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]),
+        "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]),
+        "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]),
+        "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]), "=r"(r[56]),
+        "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+      : "r"(taddr)
+      : "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void tc_store_16cols(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile(
@@ -91,8 +111,28 @@ template <int NB, int ITEMS>
 struct Held {
   uint32_t word[ITEMS][NB];
   uint32_t exps[ITEMS][NB <= 4 ? 1 : 2];
-  uint32_t live;   // one bit per item: the token exists and is seen by some row
 };
+// Item i: NB words and NB scale bytes; zeros for a token that does not exist or is not seen by any row.
+template <int NB, int ITEMS>
+__device__ __forceinline__ void get(Held<NB, ITEMS>& x, int i, bool live, const uint8_t* codes, const uint8_t* scales) {
+#pragma unroll
+  for (int k = 0; k < NB; ++k) x.word[i][k] = 0;
+#pragma unroll
+  for (int k = 0; k < (NB <= 4 ? 1 : 2); ++k) x.exps[i][k] = 0;
+  if (!live) return;
+  if constexpr (NB == 2) {
+    const uint2 a = *reinterpret_cast<const uint2*>(codes);
+    x.word[i][0] = a.x; x.word[i][1] = a.y;
+    x.exps[i][0] = *reinterpret_cast<const uint16_t*>(scales);
+  } else {
+#pragma unroll
+    for (int k = 0; k < NB / 4; ++k) {
+      const uint4 a = *reinterpret_cast<const uint4*>(codes + 16 * k);
+      x.word[i][4 * k] = a.x; x.word[i][4 * k + 1] = a.y; x.word[i][4 * k + 2] = a.z; x.word[i][4 * k + 3] = a.w;
+      x.exps[i][k] = *reinterpret_cast<const uint32_t*>(scales + 4 * k);
+    }
+  }
+}
 
 template <int NB, int TERMS>
 __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(const AttendParams p) {
@@ -113,14 +153,14 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
   volatile uint32_t* have = reinterpret_cast<volatile uint32_t*>(tmem_slot + 2);   // [4] groups of a tile that have a page
   int* nan_from = reinterpret_cast<int*>(tmem_slot + 6);                           // [4][NB] first token whose V block is NaN
   int64_t* scratch = reinterpret_cast<int64_t*>(tail + 288);                       // [2 * kWarps + 4]
-  static_assert(288 + 16 * Cfg::kWarps + 32 <= 544 && 128 + 24 + 16 * 8 <= 288, "tail");
+  static_assert(288 + 16 * Cfg::kWarps + 32 <= 640 && 128 + 24 + 16 * 8 <= 288, "tail");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  constexpr int kWiden = 4 * MT, kMma = 4 * MT + 4;
+  constexpr int kWiden = 4 * MT, kMma = kWiden + Cfg::kWidenWarps;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
-      mbar_init(b_kfull + 8 * i, 4);
-      mbar_init(b_vfull + 8 * i, 4);
+      mbar_init(b_kfull + 8 * i, Cfg::kWidenWarps);
+      mbar_init(b_vfull + 8 * i, Cfg::kWidenWarps);
       mbar_init(b_kempty + 8 * i, 1);
       mbar_init(b_vempty + 8 * i, 1);
       mbar_init(b_q + 8 * i, 4);
@@ -181,17 +221,17 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
         const bool masked = __any_sync(0xFFFFFFFFu, open < TT) || groups != (1u << kGroups) - 1u;
         float top = ninf;
 #pragma unroll 1
-        for (int j = 0; j < TT / 32; ++j) {
-          uint32_t x[32];
-          tc_load_32cols(s_col + 32 * j, x);
+        for (int j = 0; j < TT / 64; ++j) {
+          uint32_t x[64];
+          tc_load_64cols(s_col + 64 * j, x);
           if (masked) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (32 * j + i < open && (groups >> (2 * j + (i >> 4)) & 1u)) top = fmaxf(top, __uint_as_float(x[i]));
+            for (int i = 0; i < 64; ++i)
+              if (64 * j + i < open && (groups >> (4 * j + (i >> 4)) & 1u)) top = fmaxf(top, __uint_as_float(x[i]));
           } else {
             float t1 = ninf, t2 = ninf, t3 = ninf;
 #pragma unroll
-            for (int i = 0; i < 32; i += 4) {
+            for (int i = 0; i < 64; i += 4) {
               top = fmaxf(top, __uint_as_float(x[i]));
               t1 = fmaxf(t1, __uint_as_float(x[i + 1]));
               t2 = fmaxf(t2, __uint_as_float(x[i + 2]));
@@ -301,74 +341,47 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
     }
   } else if (warp < kMma) {
     // ---------------- widening: codes from the pages to bf16 operands ----------------
-    constexpr int kItems = TT / 32;
+    // Thread: a fourth of a token's codes, tokens 64 apart.  Codes and scales of the next tile are asked for before those of
+    // the current one are widened, its pages a tile earlier still.
+    constexpr int kItems = TT / 64;
     const int dw = warp - kWiden, j = lane >> 3;
     for (; ok && w.next(p); ++item) {
       if (dw == 0 && lane < NB) nan_from[(item & 3u) * NB + lane] = INT32_MAX;
-      asm volatile("bar.sync 1, 128;" ::: "memory");
-      Held<NB, kItems> hk, hv;
-      uint32_t tile_have = 0;
-      const uint8_t* group[kItems];
-      // page of group `lane` of the tile, then this thread's tokens
+      asm volatile("bar.sync 1, %0;" ::"n"(32 * Cfg::kWidenWarps) : "memory");
+      Held<NB, kItems> hk[2], hv[2];
+      uint32_t tile_have[2];
+      int32_t page = -1;        // of group `lane` of the tile to be asked for next
       auto find = [&](int tile) {
-        int32_t page = -1;
         const int pos = tile * TT + lane * 16;
-        if (lane < kGroups && pos < w.seen) page = p.c.table[static_cast<int64_t>(w.b) * p.c.width + p.c.div_page.div(static_cast<uint32_t>(pos))];
+        page = -1;
+        if (lane < kGroups && tile < w.t1 && pos < w.seen)
+          page = p.c.table[static_cast<int64_t>(w.b) * p.c.width + p.c.div_page.div(static_cast<uint32_t>(pos))];
+      };
+      auto fetch = [&](int tile, Held<NB, kItems>& k, Held<NB, kItems>& v, uint32_t& groups) {
         const bool there = page >= 0 && page < p.c.pages;
-        tile_have = __ballot_sync(0xFFFFFFFFu, there);
-        hk.live = 0;
+        groups = __ballot_sync(0xFFFFFFFFu, there);
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
-          const int g = 2 * i + (dw >> 1), tok = 32 * i + dw * 8 + (lane & 7);
+          const int g = 4 * i + (dw >> 1), tok = 64 * i + dw * 8 + (lane & 7), in_group = tok & 15;
           const int32_t pg = __shfl_sync(0xFFFFFFFFu, page, g);
           uint32_t slot, in_page;
           p.c.div_page.divmod(static_cast<uint32_t>(tile * TT + g * 16), slot, in_page);
-          group[i] = p.c.data + static_cast<int64_t>(pg) * p.c.page_stride + w.h * p.c.head_stride +
-                     static_cast<int64_t>(in_page / kGroup) * group_bytes(D);
-          if ((tile_have >> g & 1u) && tile * TT + tok < w.seen) hk.live |= 1u << i;
-        }
-        hv.live = hk.live;
-      };
-      auto fetch = [&](Held<NB, kItems>& x, int codes_at, int scales_at, bool is_v) {
-#pragma unroll
-        for (int i = 0; i < kItems; ++i) {
-          const int tok = (dw * 8 + (lane & 7)) & 15;   // place in its group
-          const int part = is_v ? j ^ ((tok & 2) ? 2 : 0) : j;
-          const uint8_t* src = group[i] + codes_at + tok * (D / 2) + part * NB * 4;
-          const uint8_t* sc = group[i] + scales_at + tok * NB;
-#pragma unroll
-          for (int k = 0; k < NB; ++k) x.word[i][k] = 0;
-          x.exps[i][0] = 0;
-          if (NB == 8) x.exps[i][NB == 8 ? 1 : 0] = 0;
-          if (x.live >> i & 1u) {
-            if (NB == 2) {
-              const uint2 a = *reinterpret_cast<const uint2*>(src);
-              x.word[i][0] = a.x; x.word[i][1] = a.y;
-              x.exps[i][0] = *reinterpret_cast<const uint16_t*>(sc);
-            } else {
-#pragma unroll
-              for (int k = 0; k < NB / 4; ++k) {
-                const uint4 a = *reinterpret_cast<const uint4*>(src + 16 * k);
-                x.word[i][4 * k] = a.x; x.word[i][4 * k + 1] = a.y; x.word[i][4 * k + 2] = a.z; x.word[i][4 * k + 3] = a.w;
-              }
-              x.exps[i][0] = *reinterpret_cast<const uint32_t*>(sc);
-              if (NB == 8) x.exps[i][NB == 8 ? 1 : 0] = *reinterpret_cast<const uint32_t*>(sc + 4);
-            }
-          }
+          const uint8_t* grp = p.c.data + static_cast<int64_t>(pg) * p.c.page_stride + w.h * p.c.head_stride +
+                               static_cast<int64_t>(in_page / kGroup) * group_bytes(D);
+          const bool live = (groups >> g & 1u) && tile * TT + tok < w.seen;
+          get(k, i, live, grp + in_group * (D / 2) + j * NB * 4, grp + k_scales_at(D) + in_group * NB);
+          get(v, i, live, grp + v_codes_at(D) + in_group * (D / 2) + (j ^ ((tok & 2) ? 2 : 0)) * NB * 4,
+              grp + v_scales_at(D) + in_group * NB);
         }
       };
-      find(w.t0);
-      fetch(hk, 0, k_scales_at(D), false);
-      fetch(hv, v_codes_at(D), v_scales_at(D), true);
-      for (int tile = w.t0; tile < w.t1; ++tile, ++it) {
+      auto widen = [&](int tile, const Held<NB, kItems>& hk, const Held<NB, kItems>& hv, uint32_t groups) {
         const uint32_t st = it & 1u, ph = (it >> 1) & 1u;
-        const uint32_t now_have = tile_have;
-        if (!mbar_wait(b_kempty + 8 * st, ph ^ 1u, abort_flag)) { ok = false; break; }
-        if (dw == 0 && lane == 0) have[it & 3u] = now_have;
+        if (!mbar_wait(b_kempty + 8 * st, ph ^ 1u, abort_flag)) return false;
+        if (dw == 0 && lane == 0) have[it & 3u] = groups;
         unsigned char* kt = gen + MT * Cfg::kQ + 2 * st * Cfg::kKV;
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
-          const int tok = 32 * i + dw * 8 + (lane & 7);
+          const int tok = 64 * i + dw * 8 + (lane & 7);
 #pragma unroll
           for (int b = 0; b < NB; ++b) {
             const uint32_t e = hk.exps[i][b >> 2] >> (8 * (b & 3)) & 255u;
@@ -380,11 +393,11 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(b_kfull + 8 * st);
-        if (!mbar_wait(b_vempty + 8 * st, ph ^ 1u, abort_flag)) { ok = false; break; }
+        if (!mbar_wait(b_vempty + 8 * st, ph ^ 1u, abort_flag)) return false;
         unsigned char* vt = kt + Cfg::kKV;
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
-          const int tok = 32 * i + dw * 8 + (lane & 7);
+          const int tok = 64 * i + dw * 8 + (lane & 7);
 #pragma unroll
           for (int k = 0; k < NB; ++k) {
             const int b = 2 * (k % (NB / 2)), c = j * NB + k;
@@ -401,10 +414,21 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(b_vfull + 8 * st);
-        if (tile + 1 < w.t1) {
-          find(tile + 1);
-          fetch(hk, 0, k_scales_at(D), false);
-          fetch(hv, v_codes_at(D), v_scales_at(D), true);
+        return true;
+      };
+      find(w.t0);
+      fetch(w.t0, hk[0], hv[0], tile_have[0]);
+      find(w.t0 + 1);
+      for (int tile = w.t0; tile < w.t1 && ok; tile += 2) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          if (tile + u >= w.t1 || !ok) break;
+          if (tile + u + 1 < w.t1) {
+            fetch(tile + u + 1, hk[u ^ 1], hv[u ^ 1], tile_have[u ^ 1]);
+            find(tile + u + 2);
+          }
+          ok = widen(tile + u, hk[u], hv[u], tile_have[u]);
+          ++it;
         }
       }
       if (!ok) break;
