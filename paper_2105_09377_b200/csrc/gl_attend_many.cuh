@@ -15,6 +15,8 @@
 // stored in the same order, and pairs of neighbouring blocks for V, undone when the result is stored.
 #pragma once
 
+#include <type_traits>
+
 namespace {
 
 template <int NB, int TERMS>
@@ -47,25 +49,6 @@ __device__ __forceinline__ void tc_mma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem,
       ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-__device__ __forceinline__ void tc_load_64cols(uint32_t taddr, uint32_t (&r)[64]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
-      "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
-      "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]),
-        "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]),
-        "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]),
-        "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]), "=r"(r[56]),
-        "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
-      : "r"(taddr)
-      : "memory");
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-}
 __device__ __forceinline__ void tc_store_16cols(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
@@ -82,26 +65,30 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(0x80008000u));
   return d;
 }
-// bf16 bits of 2^k, -127 <= k <= 127
-__device__ __forceinline__ uint32_t bf16_pow2(int k) { return k > -127 ? static_cast<uint32_t>(k + 127) << 7 : 0x0040u; }
+// Scales of four blocks, a byte each: is one of them above 2^1 (e > 128)?
+__device__ __forceinline__ bool any_above_128(uint32_t e4) { return (((e4 & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) & e4 & 0x80808080u) != 0u; }
 
-// Eight codes (pairs: code i of the low and of the high half) -> four bf16 pairs, times 2^(elo - 127) and 2^(ehi - 127).
-// Moved into the low exponent bits of a bf16 a code reads as its value times 2^-126, subnormals included.
-__device__ __forceinline__ uint4 mx4_pairs_bf16(uint32_t z, uint32_t elo, uint32_t ehi) {
+// Eight codes (pairs: code i of the low and of the high half) -> four bf16 pairs times the scales of bytes lo and hi of e4.
+// Moved into the low exponent bits of a bf16 a code reads as its value times 2^-126, subnormals included; 2^(e - 1), the
+// factor that is left, is a bf16 up to e = 128.  `above`: some scale of the four is larger; the factor comes in two steps.
+__device__ __forceinline__ uint4 mx4_pairs_bf16(uint32_t z, uint32_t e4, int lo, int hi, bool above) {
   uint32_t h[4];
   h[0] = ((z << 12) & 0x80008000u) | ((z << 6) & 0x01C001C0u);
   h[1] = ((z << 8) & 0x80008000u) | ((z << 2) & 0x01C001C0u);
   h[2] = ((z << 4) & 0x80008000u) | ((z >> 2) & 0x01C001C0u);
   h[3] = (z & 0x80008000u) | ((z >> 6) & 0x01C001C0u);
-  // 2^(e - 1) is a bf16 up to e = 128; larger scales in two steps
-  const uint32_t f = bf16_pow2(min(static_cast<int>(elo), 128) - 1) | bf16_pow2(min(static_cast<int>(ehi), 128) - 1) << 16;
+  const uint32_t pair = __byte_perm(e4, 0u, lo | 4 << 4 | hi << 8 | 4 << 12);
+  if (above) {
+    const uint32_t el = pair & 0xFFFFu, eh = pair >> 16;
+    const uint32_t first = (min(el, 128u) + 126u) << 7 | (min(eh, 128u) + 126u) << 23;
+    const uint32_t l2 = el == 255u ? 0x7FC0u : (el > 128u ? el - 1u : 127u) << 7;   // 2^(e - 128), or 1
+    const uint32_t h2 = eh == 255u ? 0x7FC0u : (eh > 128u ? eh - 1u : 127u) << 7;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) h[i] = mul_bf16x2(h[i], f);
-  if (max(elo, ehi) > 128u) {
-    const uint32_t lo = elo == 255u ? 0x7FC0u : bf16_pow2(elo > 128u ? static_cast<int>(elo) - 128 : 0);
-    const uint32_t hi = ehi == 255u ? 0x7FC0u : bf16_pow2(ehi > 128u ? static_cast<int>(ehi) - 128 : 0);
+    for (int i = 0; i < 4; ++i) h[i] = mul_bf16x2(mul_bf16x2(h[i], first), l2 | h2 << 16);
+  } else {
+    const uint32_t f = pair * 128u + 0x3F003F00u;   // bf16 2^(e - 1) in both halves
 #pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = mul_bf16x2(h[i], lo | hi << 16);
+    for (int i = 0; i < 4; ++i) h[i] = mul_bf16x2(h[i], f);
   }
   return make_uint4(h[0], h[1], h[2], h[3]);
 }
@@ -221,17 +208,17 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
         const bool masked = __any_sync(0xFFFFFFFFu, open < TT) || groups != (1u << kGroups) - 1u;
         float top = ninf;
 #pragma unroll 1
-        for (int j = 0; j < TT / 64; ++j) {
-          uint32_t x[64];
-          tc_load_64cols(s_col + 64 * j, x);
+        for (int j = 0; j < TT / 32; ++j) {
+          uint32_t x[32];
+          tc_load_32cols(s_col + 32 * j, x);
           if (masked) {
 #pragma unroll
-            for (int i = 0; i < 64; ++i)
-              if (64 * j + i < open && (groups >> (4 * j + (i >> 4)) & 1u)) top = fmaxf(top, __uint_as_float(x[i]));
+            for (int i = 0; i < 32; ++i)
+              if (32 * j + i < open && (groups >> (2 * j + (i >> 4)) & 1u)) top = fmaxf(top, __uint_as_float(x[i]));
           } else {
             float t1 = ninf, t2 = ninf, t3 = ninf;
 #pragma unroll
-            for (int i = 0; i < 64; i += 4) {
+            for (int i = 0; i < 32; i += 4) {
               top = fmaxf(top, __uint_as_float(x[i]));
               t1 = fmaxf(t1, __uint_as_float(x[i + 1]));
               t2 = fmaxf(t2, __uint_as_float(x[i + 2]));
@@ -260,38 +247,43 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
         }
         ref = new_ref;
         const float off = ref == ninf ? 0.f : ref;
-        float part = 0.f, part2 = 0.f;
+        float part[4] = {0.f, 0.f, 0.f, 0.f};
+        // (two copies of the loop: a test of `masked` per weight would cost as much as the weight)
+        const auto weigh = [&](auto with_mask) {
 #pragma unroll 1
-        for (int j = 0; j < TT / 32; ++j) {
-          uint32_t x[32], hi[16], mid[16], lo[16];
-          tc_load_32cols(s_col + 32 * j, x);
+          for (int j = 0; j < TT / 32; ++j) {
+            uint32_t x[32], hi[16], mid[16], lo[16];
+            tc_load_32cols(s_col + 32 * j, x);
 #pragma unroll
-          for (int i = 0; i < 32; i += 2) {
-            float a = ex2(fmaf(__uint_as_float(x[i]), cf, -off)), b = ex2(fmaf(__uint_as_float(x[i + 1]), cf, -off));
-            if (masked) {
-              const bool there = groups >> (2 * j + (i >> 4)) & 1u;
-              a = there && 32 * j + i < open ? a : 0.f;
-              b = there && 32 * j + i + 1 < open ? b : 0.f;
+            for (int i = 0; i < 32; i += 2) {
+              float a = ex2(fmaf(__uint_as_float(x[i]), cf, -off)), b = ex2(fmaf(__uint_as_float(x[i + 1]), cf, -off));
+              if constexpr (decltype(with_mask)::value) {
+                const bool there = groups >> (2 * j + (i >> 4)) & 1u;
+                a = there && 32 * j + i < open ? a : 0.f;
+                b = there && 32 * j + i + 1 < open ? b : 0.f;
+              }
+              part[i & 2] += a;
+              part[(i & 2) + 1] += b;
+              hi[i / 2] = pack_bf16x2(__float_as_uint(a), __float_as_uint(b));
+              if (TERMS == 3) {
+                a -= __uint_as_float(hi[i / 2] << 16);
+                b -= __uint_as_float(hi[i / 2] & 0xFFFF0000u);
+                mid[i / 2] = pack_bf16x2(__float_as_uint(a), __float_as_uint(b));
+                a -= __uint_as_float(mid[i / 2] << 16);
+                b -= __uint_as_float(mid[i / 2] & 0xFFFF0000u);
+                lo[i / 2] = pack_bf16x2(__float_as_uint(a), __float_as_uint(b));
+              }
             }
-            part += a;
-            part2 += b;
-            hi[i / 2] = pack_bf16x2(__float_as_uint(a), __float_as_uint(b));
+            tc_store_16cols(s_col + 32 * j, hi);
             if (TERMS == 3) {
-              a -= __uint_as_float(hi[i / 2] << 16);
-              b -= __uint_as_float(hi[i / 2] & 0xFFFF0000u);
-              mid[i / 2] = pack_bf16x2(__float_as_uint(a), __float_as_uint(b));
-              a -= __uint_as_float(mid[i / 2] << 16);
-              b -= __uint_as_float(mid[i / 2] & 0xFFFF0000u);
-              lo[i / 2] = pack_bf16x2(__float_as_uint(a), __float_as_uint(b));
+              tc_store_16cols(s_col + 32 * j + 16, mid);
+              tc_store_16cols(low_col + 16 * j, lo);
             }
           }
-          tc_store_16cols(s_col + 32 * j, hi);
-          if (TERMS == 3) {
-            tc_store_16cols(s_col + 32 * j + 16, mid);
-            tc_store_16cols(low_col + 16 * j, lo);
-          }
-        }
-        sum += part + part2;
+        };
+        if (masked) weigh(std::true_type{});
+        else weigh(std::false_type{});
+        sum += (part[0] + part[1]) + (part[2] + part[3]);
         tc_wait_store();
         tc_fence_before();
         __syncwarp();
@@ -360,14 +352,14 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
       auto fetch = [&](int tile, Held<NB, kItems>& k, Held<NB, kItems>& v, uint32_t& groups) {
         const bool there = page >= 0 && page < p.c.pages;
         groups = __ballot_sync(0xFFFFFFFFu, there);
+        uint32_t slot, in_page;   // lane g: where group g lies
+        p.c.div_page.divmod(static_cast<uint32_t>(tile * TT + (lane & 7) * 16), slot, in_page);
+        const uint64_t mine = reinterpret_cast<uint64_t>(p.c.data) + static_cast<int64_t>(page) * p.c.page_stride +
+                              w.h * p.c.head_stride + (in_page / kGroup) * group_bytes(D);
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
           const int g = 4 * i + (dw >> 1), tok = 64 * i + dw * 8 + (lane & 7), in_group = tok & 15;
-          const int32_t pg = __shfl_sync(0xFFFFFFFFu, page, g);
-          uint32_t slot, in_page;
-          p.c.div_page.divmod(static_cast<uint32_t>(tile * TT + g * 16), slot, in_page);
-          const uint8_t* grp = p.c.data + static_cast<int64_t>(pg) * p.c.page_stride + w.h * p.c.head_stride +
-                               static_cast<int64_t>(in_page / kGroup) * group_bytes(D);
+          const uint8_t* grp = reinterpret_cast<const uint8_t*>(__shfl_sync(0xFFFFFFFFu, mine, g));
           const bool live = (groups >> g & 1u) && tile * TT + tok < w.seen;
           get(k, i, live, grp + in_group * (D / 2) + j * NB * 4, grp + k_scales_at(D) + in_group * NB);
           get(v, i, live, grp + v_codes_at(D) + in_group * (D / 2) + (j ^ ((tok & 2) ? 2 : 0)) * NB * 4,
@@ -382,12 +374,13 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
           const int tok = 64 * i + dw * 8 + (lane & 7);
+          bool above = any_above_128(hk.exps[i][0]);
+          if (NB == 8) above |= any_above_128(hk.exps[i][NB == 8 ? 1 : 0]);
 #pragma unroll
           for (int b = 0; b < NB; ++b) {
-            const uint32_t e = hk.exps[i][b >> 2] >> (8 * (b & 3)) & 255u;
             const int c = b * 4 + j;
             *reinterpret_cast<uint4*>(kt + (c >> 3) * (TT * 128) + tok * 128 + (((c & 7) ^ (tok & 7)) << 4)) =
-                mx4_pairs_bf16(hk.word[i][b], e, e);
+                mx4_pairs_bf16(hk.word[i][b], hk.exps[i][b >> 2], b & 3, b & 3, above);
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -398,17 +391,23 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
           const int tok = 64 * i + dw * 8 + (lane & 7);
+          bool above = any_above_128(hv.exps[i][0]);
+          if (NB == 8) above |= any_above_128(hv.exps[i][NB == 8 ? 1 : 0]);
 #pragma unroll
           for (int k = 0; k < NB; ++k) {
             const int b = 2 * (k % (NB / 2)), c = j * NB + k;
-            uint32_t elo = hv.exps[i][b >> 2] >> (8 * (b & 3)) & 255u, ehi = hv.exps[i][b >> 2] >> (8 * (b & 3) + 8) & 255u;
-            uint32_t word = hv.word[i][k];
-            if (max(elo, ehi) == 255u) {   // NaN goes to the rows that see this token when the result is stored
-              if (elo == 255u) { atomicMin(nan_from + (item & 3u) * NB + b, tile * TT + tok); word &= 0xFFFF0000u; elo = 0; }
-              if (ehi == 255u) { atomicMin(nan_from + (item & 3u) * NB + b + 1, tile * TT + tok); word &= 0xFFFFu; ehi = 0; }
+            uint32_t word = hv.word[i][k], e4 = hv.exps[i][b >> 2];
+            if (above) {   // a NaN goes to the rows that see this token when the result is stored; zeros in its place
+#pragma unroll
+              for (int s = 0; s < 2; ++s)
+                if ((e4 >> (8 * ((b & 3) + s)) & 255u) == 255u) {
+                  atomicMin(nan_from + (item & 3u) * NB + b + s, tile * TT + tok);
+                  word &= s ? 0x0000FFFFu : 0xFFFF0000u;
+                  e4 &= ~(255u << (8 * ((b & 3) + s)));
+                }
             }
             *reinterpret_cast<uint4*>(vt + (c >> 3) * (TT * 128) + tok * 128 + (((c & 7) ^ (tok & 7)) << 4)) =
-                mx4_pairs_bf16(word, elo, ehi);
+                mx4_pairs_bf16(word, e4, b & 3, (b & 3) + 1, above);
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
