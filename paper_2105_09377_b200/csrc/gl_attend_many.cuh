@@ -70,15 +70,16 @@ __device__ __forceinline__ bool any_above_128(uint32_t e4) { return (((e4 & 0x7F
 
 // Eight codes (pairs: code i of the low and of the high half) -> four bf16 pairs times the scales of bytes lo and hi of e4.
 // Moved into the low exponent bits of a bf16 a code reads as its value times 2^-126, subnormals included; 2^(e - 1), the
-// factor that is left, is a bf16 up to e = 128.  `above`: some scale of the four is larger; the factor comes in two steps.
-__device__ __forceinline__ uint4 mx4_pairs_bf16(uint32_t z, uint32_t e4, int lo, int hi, bool above) {
+// factor that is left, is a bf16 up to e = 128.  ABOVE: some scale may be larger; the factor comes in two steps.
+template <bool ABOVE>
+__device__ __forceinline__ uint4 mx4_pairs_bf16(uint32_t z, uint32_t e4, int lo, int hi) {
   uint32_t h[4];
   h[0] = ((z << 12) & 0x80008000u) | ((z << 6) & 0x01C001C0u);
   h[1] = ((z << 8) & 0x80008000u) | ((z << 2) & 0x01C001C0u);
   h[2] = ((z << 4) & 0x80008000u) | ((z >> 2) & 0x01C001C0u);
   h[3] = (z & 0x80008000u) | ((z >> 6) & 0x01C001C0u);
   const uint32_t pair = __byte_perm(e4, 0u, lo | 4 << 4 | hi << 8 | 4 << 12);
-  if (above) {
+  if constexpr (ABOVE) {
     const uint32_t el = pair & 0xFFFFu, eh = pair >> 16;
     const uint32_t first = (min(el, 128u) + 126u) << 7 | (min(eh, 128u) + 126u) << 23;
     const uint32_t l2 = el == 255u ? 0x7FC0u : (el > 128u ? el - 1u : 127u) << 7;   // 2^(e - 128), or 1
@@ -99,14 +100,9 @@ struct Held {
   uint32_t word[ITEMS][NB];
   uint32_t exps[ITEMS][NB <= 4 ? 1 : 2];
 };
-// Item i: NB words and NB scale bytes; zeros for a token that does not exist or is not seen by any row.
+// Item i: NB words and NB scale bytes.
 template <int NB, int ITEMS>
-__device__ __forceinline__ void get(Held<NB, ITEMS>& x, int i, bool live, const uint8_t* codes, const uint8_t* scales) {
-#pragma unroll
-  for (int k = 0; k < NB; ++k) x.word[i][k] = 0;
-#pragma unroll
-  for (int k = 0; k < (NB <= 4 ? 1 : 2); ++k) x.exps[i][k] = 0;
-  if (!live) return;
+__device__ __forceinline__ void get(Held<NB, ITEMS>& x, int i, const uint8_t* codes, const uint8_t* scales) {
   if constexpr (NB == 2) {
     const uint2 a = *reinterpret_cast<const uint2*>(codes);
     x.word[i][0] = a.x; x.word[i][1] = a.y;
@@ -116,9 +112,22 @@ __device__ __forceinline__ void get(Held<NB, ITEMS>& x, int i, bool live, const 
     for (int k = 0; k < NB / 4; ++k) {
       const uint4 a = *reinterpret_cast<const uint4*>(codes + 16 * k);
       x.word[i][4 * k] = a.x; x.word[i][4 * k + 1] = a.y; x.word[i][4 * k + 2] = a.z; x.word[i][4 * k + 3] = a.w;
-      x.exps[i][k] = *reinterpret_cast<const uint32_t*>(scales + 4 * k);
+    }
+    if constexpr (NB == 4) {
+      x.exps[i][0] = *reinterpret_cast<const uint32_t*>(scales);
+    } else {
+      const uint2 a = *reinterpret_cast<const uint2*>(scales);
+      x.exps[i][0] = a.x; x.exps[i][NB == 8 ? 1 : 0] = a.y;
     }
   }
+}
+// A token that does not exist or is not seen by any row.
+template <int NB, int ITEMS>
+__device__ __forceinline__ void clear(Held<NB, ITEMS>& x, int i) {
+#pragma unroll
+  for (int k = 0; k < NB; ++k) x.word[i][k] = 0;
+#pragma unroll
+  for (int k = 0; k < (NB <= 4 ? 1 : 2); ++k) x.exps[i][k] = 0;
 }
 
 template <int NB, int TERMS>
@@ -356,48 +365,51 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
         p.c.div_page.divmod(static_cast<uint32_t>(tile * TT + (lane & 7) * 16), slot, in_page);
         const uint64_t mine = reinterpret_cast<uint64_t>(p.c.data) + static_cast<int64_t>(page) * p.c.page_stride +
                               w.h * p.c.head_stride + (in_page / kGroup) * group_bytes(D);
+        // (the plain case is a branch of its own: a condition per load costs more than the load)
+        const bool plain = groups == (1u << kGroups) - 1u && (tile + 1) * TT <= w.seen;
+        const int in_group = (dw * 8 + (lane & 7)) & 15, jv = j ^ ((in_group & 2) ? 2 : 0);
+        const uint8_t* grp[kItems];
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) {
-          const int g = 4 * i + (dw >> 1), tok = 64 * i + dw * 8 + (lane & 7), in_group = tok & 15;
-          const uint8_t* grp = reinterpret_cast<const uint8_t*>(__shfl_sync(0xFFFFFFFFu, mine, g));
-          const bool live = (groups >> g & 1u) && tile * TT + tok < w.seen;
-          get(k, i, live, grp + in_group * (D / 2) + j * NB * 4, grp + k_scales_at(D) + in_group * NB);
-          get(v, i, live, grp + v_codes_at(D) + in_group * (D / 2) + (j ^ ((tok & 2) ? 2 : 0)) * NB * 4,
-              grp + v_scales_at(D) + in_group * NB);
+        for (int i = 0; i < kItems; ++i) grp[i] = reinterpret_cast<const uint8_t*>(__shfl_sync(0xFFFFFFFFu, mine, 4 * i + (dw >> 1)));
+        if (plain) {
+#pragma unroll
+          for (int i = 0; i < kItems; ++i) {
+            get(k, i, grp[i] + in_group * (D / 2) + j * NB * 4, grp[i] + k_scales_at(D) + in_group * NB);
+            get(v, i, grp[i] + v_codes_at(D) + in_group * (D / 2) + jv * NB * 4, grp[i] + v_scales_at(D) + in_group * NB);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < kItems; ++i) {
+            clear(k, i);
+            clear(v, i);
+            if ((groups >> (4 * i + (dw >> 1)) & 1u) && tile * TT + 64 * i + dw * 8 + (lane & 7) < w.seen) {
+              get(k, i, grp[i] + in_group * (D / 2) + j * NB * 4, grp[i] + k_scales_at(D) + in_group * NB);
+              get(v, i, grp[i] + v_codes_at(D) + in_group * (D / 2) + jv * NB * 4, grp[i] + v_scales_at(D) + in_group * NB);
+            }
+          }
         }
       };
-      auto widen = [&](int tile, const Held<NB, kItems>& hk, const Held<NB, kItems>& hv, uint32_t groups) {
-        const uint32_t st = it & 1u, ph = (it >> 1) & 1u;
-        if (!mbar_wait(b_kempty + 8 * st, ph ^ 1u, abort_flag)) return false;
-        if (dw == 0 && lane == 0) have[it & 3u] = groups;
-        unsigned char* kt = gen + MT * Cfg::kQ + 2 * st * Cfg::kKV;
+      const auto widen_k = [&](auto above, unsigned char* kt, const Held<NB, kItems>& x) {
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
           const int tok = 64 * i + dw * 8 + (lane & 7);
-          bool above = any_above_128(hk.exps[i][0]);
-          if (NB == 8) above |= any_above_128(hk.exps[i][NB == 8 ? 1 : 0]);
 #pragma unroll
           for (int b = 0; b < NB; ++b) {
             const int c = b * 4 + j;
             *reinterpret_cast<uint4*>(kt + (c >> 3) * (TT * 128) + tok * 128 + (((c & 7) ^ (tok & 7)) << 4)) =
-                mx4_pairs_bf16(hk.word[i][b], hk.exps[i][b >> 2], b & 3, b & 3, above);
+                mx4_pairs_bf16<decltype(above)::value>(x.word[i][b], x.exps[i][b >> 2], b & 3, b & 3);
           }
         }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(b_kfull + 8 * st);
-        if (!mbar_wait(b_vempty + 8 * st, ph ^ 1u, abort_flag)) return false;
-        unsigned char* vt = kt + Cfg::kKV;
+      };
+      const auto widen_v = [&](auto above, unsigned char* vt, const Held<NB, kItems>& x, int tile) {
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
           const int tok = 64 * i + dw * 8 + (lane & 7);
-          bool above = any_above_128(hv.exps[i][0]);
-          if (NB == 8) above |= any_above_128(hv.exps[i][NB == 8 ? 1 : 0]);
 #pragma unroll
           for (int k = 0; k < NB; ++k) {
             const int b = 2 * (k % (NB / 2)), c = j * NB + k;
-            uint32_t word = hv.word[i][k], e4 = hv.exps[i][b >> 2];
-            if (above) {   // a NaN goes to the rows that see this token when the result is stored; zeros in its place
+            uint32_t word = x.word[i][k], e4 = x.exps[i][b >> 2];
+            if constexpr (decltype(above)::value) {   // a NaN goes to the rows that see this token when the result is stored
 #pragma unroll
               for (int s = 0; s < 2; ++s)
                 if ((e4 >> (8 * ((b & 3) + s)) & 255u) == 255u) {
@@ -407,9 +419,29 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
                 }
             }
             *reinterpret_cast<uint4*>(vt + (c >> 3) * (TT * 128) + tok * 128 + (((c & 7) ^ (tok & 7)) << 4)) =
-                mx4_pairs_bf16(word, e4, b & 3, (b & 3) + 1, above);
+                mx4_pairs_bf16<decltype(above)::value>(word, e4, b & 3, (b & 3) + 1);
           }
         }
+      };
+      auto widen = [&](int tile, const Held<NB, kItems>& hk, const Held<NB, kItems>& hv, uint32_t groups) {
+        const uint32_t st = it & 1u, ph = (it >> 1) & 1u;
+        bool large = false;
+#pragma unroll
+        for (int i = 0; i < kItems; ++i)
+#pragma unroll
+          for (int k = 0; k < (NB <= 4 ? 1 : 2); ++k) large |= any_above_128(hk.exps[i][k]) || any_above_128(hv.exps[i][k]);
+        large = __any_sync(0xFFFFFFFFu, large);
+        if (!mbar_wait(b_kempty + 8 * st, ph ^ 1u, abort_flag)) return false;
+        if (dw == 0 && lane == 0) have[it & 3u] = groups;
+        unsigned char* kt = gen + MT * Cfg::kQ + 2 * st * Cfg::kKV;
+        if (large) widen_k(std::true_type{}, kt, hk);
+        else widen_k(std::false_type{}, kt, hk);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_kfull + 8 * st);
+        if (!mbar_wait(b_vempty + 8 * st, ph ^ 1u, abort_flag)) return false;
+        if (large) widen_v(std::true_type{}, kt + Cfg::kKV, hv, tile);
+        else widen_v(std::false_type{}, kt + Cfg::kKV, hv, tile);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(b_vfull + 8 * st);
