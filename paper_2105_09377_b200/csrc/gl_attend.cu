@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(256) cache4_read(uint16_t* __restrict__ k, uin
   const TokenAt t = token_at(p, item);
   const bool is_v = blockIdx.y != 0;
   const uint8_t* at = t.pos >= 0 ? group_of(p.c, t.b, t.h, t.pos) : nullptr;
-  float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  uint32_t w[4] = {0, 0, 0, 0};
   if (at) {
     const int in_page = t.pos % p.c.page_tokens, tok = in_page % kGroup;
     at += static_cast<int64_t>(in_page / kGroup) * group_bytes(p.D);
@@ -143,11 +143,8 @@ __global__ void __launch_bounds__(256) cache4_read(uint16_t* __restrict__ k, uin
       word = *reinterpret_cast<const uint32_t*>(at + tok * (p.D / 2) + (j * NB + b) * 4);
       e = at[k_scales_at(p.D) + tok * NB + b];
     }
-    mx4_values8(word, e, x);
+    mx4_words_bf16(word, e, w);
   }
-  uint32_t w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(__float_as_uint(x[2 * i]), __float_as_uint(x[2 * i + 1]));
   *reinterpret_cast<uint4*>((is_v ? v : k) + static_cast<int64_t>(item) * 8) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 

@@ -59,25 +59,15 @@ __device__ __forceinline__ void tc_store_16cols(uint32_t taddr, const uint32_t (
 }
 __device__ __forceinline__ void tc_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// bf16x2 multiplication that keeps subnormals
-__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
-  uint32_t d;
-  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(0x80008000u));
-  return d;
-}
 // Scales of four blocks, a byte each: is one of them above 2^1 (e > 128)?
 __device__ __forceinline__ bool any_above_128(uint32_t e4) { return (((e4 & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) & e4 & 0x80808080u) != 0u; }
 
 // Eight codes (pairs: code i of the low and of the high half) -> four bf16 pairs times the scales of bytes lo and hi of e4.
-// Moved into the low exponent bits of a bf16 a code reads as its value times 2^-126, subnormals included; 2^(e - 1), the
-// factor that is left, is a bf16 up to e = 128.  ABOVE: some scale may be larger; the factor comes in two steps.
+// 2^(e - 1), the factor that the moved codes lack, is a bf16 up to e = 128.  ABOVE: some scale may be larger; the factor comes in two steps.
 template <bool ABOVE>
 __device__ __forceinline__ uint4 mx4_pairs_bf16(uint32_t z, uint32_t e4, int lo, int hi) {
   uint32_t h[4];
-  h[0] = ((z << 12) & 0x80008000u) | ((z << 6) & 0x01C001C0u);
-  h[1] = ((z << 8) & 0x80008000u) | ((z << 2) & 0x01C001C0u);
-  h[2] = ((z << 4) & 0x80008000u) | ((z >> 2) & 0x01C001C0u);
-  h[3] = (z & 0x80008000u) | ((z >> 6) & 0x01C001C0u);
+  mx4_pairs_moved(z, h);
   const uint32_t pair = __byte_perm(e4, 0u, lo | 4 << 4 | hi << 8 | 4 << 12);
   if constexpr (ABOVE) {
     const uint32_t el = pair & 0xFFFFu, eh = pair >> 16;

@@ -70,52 +70,77 @@ bool same_shape(const gl_ap* a, const gl_mx4* b) {
 // ------------------------------------------------------------------------
 
 // Eight values per thread, four neighbouring threads per block, sixteen per 4-byte group of scales (one row, 128
-// values: the unit in which the scale tiles are addressed).  Thread i of the grid handles item i; U items per
-// thread, 256 apart, are requested before the first is used.
+// values: the unit in which the scale tiles are addressed).  U items per thread, 256 apart, are requested before the
+// first is used.  Both directions are bound by their instructions per value before they are bound by memory (127 a thread
+// and eight values, 100 us for 16384 x 8192 bf16, when every item divided its own index and unpacked before it
+// compared), so rows and columns advance by additions, magnitudes are compared and scaled two to a register and the
+// addresses are offsets from the row's.
 struct QuantParams {
   int64_t K, pitch, kt;
   uint32_t items;        // rows * kt * 16
-  FastDiv div_row;       // kt * 16 items per row
+  uint32_t per_row;      // kt * 16
+  uint32_t step_rows, step_cols;   // 256 items further on
+  FastDiv div_row;       // by per_row
+};
+
+struct ItemAt {
+  uint32_t row, col;
+  __device__ __forceinline__ void advance(const QuantParams& p) {
+    row += p.step_rows;
+    col += p.step_cols;
+    if (col >= p.per_row) { col -= p.per_row; ++row; }
+  }
 };
 
 // Byte of the scale tiles that holds block group `quad` (4 blocks) of row r.
 __device__ __forceinline__ int64_t scale_quad_at(uint32_t r, uint32_t quad, int64_t kt) {
-  return (static_cast<int64_t>(r >> 7) * kt + quad) * 512 + (r & 31u) * 16 + ((r >> 5) & 3u) * 4;
+  return (static_cast<int64_t>(r >> 7) * kt + quad) * 512 + ((r & 31u) * 16 + ((r >> 5) & 3u) * 4);
 }
 
+// A thread's eight values, as they came: four words of bf16 pairs, or eight floats.
+template <bool F32>
+struct Raw8 { uint32_t w[F32 ? 8 : 4]; };
+
 template <bool F32, bool VEC>
-__device__ __forceinline__ void load8(const void* __restrict__ in, uint32_t r, uint32_t c, int64_t K, float (&v)[8]) {
-  const int64_t at = static_cast<int64_t>(r) * K + static_cast<int64_t>(c) * 8;
-  const int64_t left = K - static_cast<int64_t>(c) * 8;
+__device__ __forceinline__ void load8(const void* __restrict__ in, ItemAt at, int64_t K, Raw8<F32>& v) {
+  constexpr int kWords = F32 ? 8 : 4;
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) v.w[i] = 0;
+  const int left = static_cast<int>(K) - static_cast<int>(at.col) * 8;
+  const int64_t first = static_cast<int64_t>(at.row) * K + at.col * 8u;
   if (VEC) {
     // K is a multiple of 8: a group of eight lies wholly inside the row or wholly behind it
     if (left > 0) {
-      if (F32) {
-        const float4 a = __ldcs(reinterpret_cast<const float4*>(static_cast<const float*>(in) + at));
-        const float4 b = __ldcs(reinterpret_cast<const float4*>(static_cast<const float*>(in) + at) + 1);
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-      } else {
-        const uint4 a = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(in) + at));
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+      const uint4* src = reinterpret_cast<const uint4*>(static_cast<const char*>(in) + first * (F32 ? 4 : 2));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          v[2 * i] = __uint_as_float(w[i] << 16);
-          v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-        }
+      for (int i = 0; i < kWords / 4; ++i) {
+        const uint4 x = __ldcs(src + i);
+        v.w[4 * i] = x.x; v.w[4 * i + 1] = x.y; v.w[4 * i + 2] = x.z; v.w[4 * i + 3] = x.w;
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = 0.f;
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (i < left)
-        v[i] = F32 ? static_cast<const float*>(in)[at + i] : bf16_to_f32(static_cast<const uint16_t*>(in)[at + i]);
-      else
-        v[i] = 0.f;
-    }
+    for (int i = 0; i < 8; ++i)
+      if (i < left) {
+        if (F32) v.w[i] = static_cast<const uint32_t*>(in)[first + i];
+        else v.w[i / 2] |= static_cast<uint32_t>(static_cast<const uint16_t*>(in)[first + i]) << (16 * (i & 1));
+      }
   }
+}
+
+// Largest magnitude of the eight values, as fp32 bits (NaN > Inf > finite).
+template <bool F32>
+__device__ __forceinline__ uint32_t largest(const Raw8<F32>& v) {
+  if (F32) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, v.w[i] & 0x7FFFFFFFu);
+    return top;
+  }
+  uint32_t two = 0;   // both halves at once: bf16 magnitudes order like integers
+#pragma unroll
+  for (int i = 0; i < 4; ++i) two = __vmaxu2(two, v.w[i] & 0x7FFF7FFFu);
+  return max(two << 16, two & 0xFFFF0000u);
 }
 
 template <bool F32, bool VEC, int U>
@@ -124,35 +149,38 @@ __global__ void __launch_bounds__(256) quantize_mx4(const void* __restrict__ in,
   pdl_wait();
   pdl_launch_dependents();
   const uint32_t first = blockIdx.x * (256u * U) + threadIdx.x;
-  float v[U][8];
-  uint32_t row[U], col[U];
+  Raw8<F32> v[U];
+  ItemAt at0;
+  p.div_row.divmod(first, at0.row, at0.col);
+  ItemAt at = at0;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const uint32_t i = first + u * 256u;
-    if (i < p.items) {
-      p.div_row.divmod(i, row[u], col[u]);
-      load8<F32, VEC>(in, row[u], col[u], p.K, v[u]);
-    }
+    if (first + u * 256u < p.items) load8<F32, VEC>(in, at, p.K, v[u]);
+    at.advance(p);
   }
+  at = at0;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const uint32_t i = first + u * 256u;
     // groups of sixteen threads share a row and `items` is a multiple of sixteen: the shuffles stay inside a group
-    if (i >= p.items) continue;
+    if (first + u * 256u >= p.items) break;
     const unsigned group = 0xFFFFu << (threadIdx.x & 16u);
-    uint32_t top = 0;   // largest magnitude as bits: NaN > Inf > finite
-#pragma unroll
-    for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[u][j]) & 0x7FFFFFFFu);
+    uint32_t top = largest<F32>(v[u]);
     top = max(top, __shfl_xor_sync(group, top, 1));
     top = max(top, __shfl_xor_sync(group, top, 2));
     const uint32_t e = mx4_exponent(top);
-    const uint32_t word = mx4_codes8(v[u], e);
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      x[i] = F32 ? __uint_as_float(v[u].w[F32 ? i : 0])
+                 : __uint_as_float(i & 1 ? v[u].w[F32 ? 0 : i / 2] & 0xFFFF0000u : v[u].w[F32 ? 0 : i / 2] << 16);
+    const uint32_t word = mx4_codes8(x, e);
     uint32_t quad = __shfl_down_sync(group, e, 4, 16) << 8 | e;
     quad |= __shfl_down_sync(group, quad, 8, 16) << 16;
-    if (static_cast<int64_t>(col[u]) * 4 < p.pitch)
-      *reinterpret_cast<uint32_t*>(codes + static_cast<int64_t>(row[u]) * p.pitch + col[u] * 4) = word;
+    if (at.col * 4u < static_cast<uint32_t>(p.pitch))
+      *reinterpret_cast<uint32_t*>(codes + static_cast<int64_t>(at.row) * p.pitch + at.col * 4u) = word;
     if ((threadIdx.x & 15u) == 0)
-      *reinterpret_cast<uint32_t*>(scale + scale_quad_at(row[u], col[u] >> 4, p.kt)) = quad;
+      *reinterpret_cast<uint32_t*>(scale + scale_quad_at(at.row, at.col >> 4, p.kt)) = quad;
+    at.advance(p);
   }
 }
 
@@ -162,48 +190,47 @@ __global__ void __launch_bounds__(256) dequantize_mx4(const uint8_t* __restrict_
   pdl_wait();
   pdl_launch_dependents();
   const uint32_t first = blockIdx.x * (256u * U) + threadIdx.x;
-  uint32_t word[U], e[U], row[U], col[U];
+  uint32_t word[U], e[U];
+  ItemAt at0;
+  p.div_row.divmod(first, at0.row, at0.col);
+  ItemAt at = at0;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const uint32_t i = first + u * 256u;
-    word[u] = 0;
-    e[u] = 0;
-    row[u] = col[u] = 0;
-    if (i < p.items) {
-      p.div_row.divmod(i, row[u], col[u]);
-      if (static_cast<int64_t>(col[u]) * 8 < p.K) {
-        word[u] = *reinterpret_cast<const uint32_t*>(codes + static_cast<int64_t>(row[u]) * p.pitch + col[u] * 4);
-        e[u] = scale[scale_quad_at(row[u], col[u] >> 4, p.kt) + ((col[u] >> 2) & 3u)];
-      }
+    word[u] = e[u] = 0;
+    if (first + u * 256u < p.items && static_cast<int>(at.col) * 8 < static_cast<int>(p.K)) {
+      word[u] = *reinterpret_cast<const uint32_t*>(codes + static_cast<int64_t>(at.row) * p.pitch + at.col * 4u);
+      e[u] = scale[scale_quad_at(at.row, at.col >> 4, p.kt) + ((at.col >> 2) & 3u)];
     }
+    at.advance(p);
   }
+  at = at0;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const uint32_t i = first + u * 256u;
-    const int64_t left = p.K - static_cast<int64_t>(col[u]) * 8;
-    if (i >= p.items || left <= 0) continue;
-    float v[8];
-    mx4_values8(word[u], e[u], v);
-    const int64_t at = static_cast<int64_t>(row[u]) * p.K + static_cast<int64_t>(col[u]) * 8;
-    if (VEC) {
-      if (F32) {
-        float4* o = reinterpret_cast<float4*>(static_cast<float*>(out) + at);
-        __stcs(o, make_float4(v[0], v[1], v[2], v[3]));
-        __stcs(o + 1, make_float4(v[4], v[5], v[6], v[7]));
-      } else {
-        uint32_t w[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = pack_bf16x2(__float_as_uint(v[2 * j]), __float_as_uint(v[2 * j + 1]));
-        __stcs(reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + at), make_uint4(w[0], w[1], w[2], w[3]));
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j < left) {
-          if (F32) static_cast<float*>(out)[at + j] = v[j];
-          else static_cast<uint16_t*>(out)[at + j] = f32_to_bf16(v[j]);
+    const int left = static_cast<int>(p.K) - static_cast<int>(at.col) * 8;
+    if (first + u * 256u < p.items && left > 0) {
+      const int64_t to = static_cast<int64_t>(at.row) * p.K + at.col * 8u;
+      // bf16 holds every value exactly; fp32 is the same bits with zeros behind
+      uint32_t w[4];
+      mx4_words_bf16(word[u], e[u], w);
+      if (VEC) {
+        if (F32) {
+          uint4* o = reinterpret_cast<uint4*>(static_cast<float*>(out) + to);
+          __stcs(o, make_uint4(w[0] << 16, w[0] & 0xFFFF0000u, w[1] << 16, w[1] & 0xFFFF0000u));
+          __stcs(o + 1, make_uint4(w[2] << 16, w[2] & 0xFFFF0000u, w[3] << 16, w[3] & 0xFFFF0000u));
+        } else {
+          __stcs(reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + to), make_uint4(w[0], w[1], w[2], w[3]));
         }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (j < left) {
+            const uint32_t half = j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xFFFFu;
+            if (F32) static_cast<uint32_t*>(out)[to + j] = half << 16;
+            else static_cast<uint16_t*>(out)[to + j] = static_cast<uint16_t>(half);
+          }
+      }
     }
+    at.advance(p);
   }
 }
 
@@ -214,7 +241,10 @@ int quant_params(const Mx4View& v, QuantParams* p) {
   p->pitch = v.pitch;
   p->kt = v.kt;
   p->items = static_cast<uint32_t>(items);
-  p->div_row.set(v.kt * 16);
+  p->per_row = static_cast<uint32_t>(v.kt * 16);
+  p->step_rows = 256u / p->per_row;
+  p->step_cols = 256u % p->per_row;
+  p->div_row.set(p->per_row);
   return GL_OK;
 }
 

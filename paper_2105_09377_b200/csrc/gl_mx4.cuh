@@ -36,27 +36,39 @@ __device__ __forceinline__ float mx4_scale(uint32_t e) {
   return e == 255u ? __uint_as_float(0x7FC00000u) : __uint_as_float(max(e << 23, 0x00400000u));
 }
 
-// Four pairs of codes -> four pairs of fp16 values times 2^-14.  `z` holds four codes in each 16-bit half; pair i is
-// code i of the low half and code i of the high half.  The three magnitude bits of E2M1 are the low exponent bits and
-// the top mantissa bit of an fp16 with bias 15 instead of 1, subnormals included, so moving the bits is the conversion.
-__device__ __forceinline__ void mx4_pairs_f16(uint32_t z, uint32_t (&h)[4]) {
-  h[0] = ((z << 12) & 0x80008000u) | ((z << 9) & 0x0E000E00u);
-  h[1] = ((z << 8) & 0x80008000u) | ((z << 5) & 0x0E000E00u);
-  h[2] = ((z << 4) & 0x80008000u) | ((z << 1) & 0x0E000E00u);
-  h[3] = (z & 0x80008000u) | ((z >> 3) & 0x0E000E00u);
+// bf16x2 multiplication that keeps subnormals
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(0x80008000u));
+  return d;
+}
+// Four pairs of codes -> four bf16 pairs times 2^-126.  `z` holds four codes in each 16-bit half; pair i is code i of the
+// low half and code i of the high half.  The three magnitude bits of E2M1 are the low exponent bits and the top mantissa
+// bit of a bf16 with bias 127 instead of 1, subnormals included, so moving the bits is the conversion.
+__device__ __forceinline__ void mx4_pairs_moved(uint32_t z, uint32_t (&h)[4]) {
+  h[0] = ((z << 12) & 0x80008000u) | ((z << 6) & 0x01C001C0u);
+  h[1] = ((z << 8) & 0x80008000u) | ((z << 2) & 0x01C001C0u);
+  h[2] = ((z << 4) & 0x80008000u) | ((z >> 2) & 0x01C001C0u);
+  h[3] = (z & 0x80008000u) | ((z >> 6) & 0x01C001C0u);
 }
 
-// Eight codes and their scale exponent -> eight fp32 values (exact: two significant bits).
-__device__ __forceinline__ void mx4_values8(uint32_t word, uint32_t e, float (&v)[8]) {
-  const float s = mx4_scale(e);
+// Eight codes of one block with scale exponent e -> eight bf16 values in their order (exact: two significant bits).
+__device__ __forceinline__ void mx4_words_bf16(uint32_t z, uint32_t e, uint32_t (&w)[4]) {
   uint32_t h[4];
-  mx4_pairs_f16(word, h);
+  mx4_pairs_moved(z, h);
+  // 2^(e - 1) is a bf16 up to e = 128; larger scales in two steps
+  const uint32_t f = (min(e, 128u) + 126u) * 0x00800080u;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __half2 p = *reinterpret_cast<const __half2*>(&h[i]);
-    v[i] = __low2float(p) * 16384.f * s;
-    v[i + 4] = __high2float(p) * 16384.f * s;
+  for (int i = 0; i < 4; ++i) h[i] = mul_bf16x2(h[i], f);
+  if (e > 128u) {
+    const uint32_t f2 = (e == 255u ? 0x7FC0u : (e - 1u) << 7) * 0x00010001u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = mul_bf16x2(h[i], f2);
   }
+  w[0] = __byte_perm(h[0], h[1], 0x5410);
+  w[1] = __byte_perm(h[2], h[3], 0x5410);
+  w[2] = __byte_perm(h[0], h[1], 0x7632);
+  w[3] = __byte_perm(h[2], h[3], 0x7632);
 }
 
 }  // namespace
