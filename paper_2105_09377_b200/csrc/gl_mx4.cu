@@ -69,16 +69,16 @@ bool same_shape(const gl_ap* a, const gl_mx4* b) {
 // Quantisation and its inverse
 // ------------------------------------------------------------------------
 
-// Eight values per thread, four neighbouring threads per block, sixteen per 4-byte group of scales (one row, 128
-// values: the unit in which the scale tiles are addressed).  U items per thread, 256 apart, are requested before the
-// first is used.  Both directions are bound by their instructions per value before they are bound by memory (127 a thread
+// 32 bytes of input per thread when quantising (8 fp32 or 16 bf16 values: four or two neighbouring threads per block, sixteen
+// or eight per 4-byte group of scales, the unit in which the scale tiles are addressed: one row, 128 values), eight values
+// when going back.  U items per thread, 256 apart, are requested before the first is used.  Both directions are bound by their instructions per value before they are bound by memory (127 a thread
 // and eight values, 100 us for 16384 x 8192 bf16, when every item divided its own index and unpacked before it
 // compared), so rows and columns advance by additions, magnitudes are compared and scaled two to a register and the
 // addresses are offsets from the row's.
 struct QuantParams {
   int64_t K, pitch, kt;
-  uint32_t items;        // rows * kt * 16
-  uint32_t per_row;      // kt * 16
+  uint32_t items;        // rows * per_row
+  uint32_t per_row;      // kt * 128 / values per item
   uint32_t step_rows, step_cols;   // 256 items further on
   FastDiv div_row;       // by per_row
 };
@@ -97,89 +97,99 @@ __device__ __forceinline__ int64_t scale_quad_at(uint32_t r, uint32_t quad, int6
   return (static_cast<int64_t>(r >> 7) * kt + quad) * 512 + ((r & 31u) * 16 + ((r >> 5) & 3u) * 4);
 }
 
-// A thread's eight values, as they came: four words of bf16 pairs, or eight floats.
-template <bool F32>
-struct Raw8 { uint32_t w[F32 ? 8 : 4]; };
+// A thread's values, as they came: eight words of bf16 pairs or of floats.
+struct Raw { uint32_t w[8]; };
 
 template <bool F32, bool VEC>
-__device__ __forceinline__ void load8(const void* __restrict__ in, ItemAt at, int64_t K, Raw8<F32>& v) {
-  constexpr int kWords = F32 ? 8 : 4;
+__device__ __forceinline__ void load_raw(const void* __restrict__ in, ItemAt at, int64_t K, Raw& v) {
+  constexpr int kVals = F32 ? 8 : 16;
 #pragma unroll
-  for (int i = 0; i < kWords; ++i) v.w[i] = 0;
-  const int left = static_cast<int>(K) - static_cast<int>(at.col) * 8;
-  const int64_t first = static_cast<int64_t>(at.row) * K + at.col * 8u;
+  for (int i = 0; i < 8; ++i) v.w[i] = 0;
+  const int left = static_cast<int>(K) - static_cast<int>(at.col) * kVals;
+  const int64_t first = static_cast<int64_t>(at.row) * K + at.col * static_cast<uint32_t>(kVals);
   if (VEC) {
-    // K is a multiple of 8: a group of eight lies wholly inside the row or wholly behind it
-    if (left > 0) {
-      const uint4* src = reinterpret_cast<const uint4*>(static_cast<const char*>(in) + first * (F32 ? 4 : 2));
+    // K is a multiple of 8: 16 bytes lie wholly inside the row or wholly behind it
+    const uint4* src = reinterpret_cast<const uint4*>(static_cast<const char*>(in) + first * (F32 ? 4 : 2));
 #pragma unroll
-      for (int i = 0; i < kWords / 4; ++i) {
+    for (int i = 0; i < 2; ++i)
+      if (left > i * (kVals / 2)) {
         const uint4 x = __ldcs(src + i);
         v.w[4 * i] = x.x; v.w[4 * i + 1] = x.y; v.w[4 * i + 2] = x.z; v.w[4 * i + 3] = x.w;
       }
-    }
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < kVals; ++i)
       if (i < left) {
-        if (F32) v.w[i] = static_cast<const uint32_t*>(in)[first + i];
-        else v.w[i / 2] |= static_cast<uint32_t>(static_cast<const uint16_t*>(in)[first + i]) << (16 * (i & 1));
+        if (F32) v.w[i & 7] = static_cast<const uint32_t*>(in)[first + i];
+        else v.w[i / 2 & 7] |= static_cast<uint32_t>(static_cast<const uint16_t*>(in)[first + i]) << (16 * (i & 1));
       }
   }
 }
 
-// Largest magnitude of the eight values, as fp32 bits (NaN > Inf > finite).
+// Largest magnitude of the values, as fp32 bits (NaN > Inf > finite).
 template <bool F32>
-__device__ __forceinline__ uint32_t largest(const Raw8<F32>& v) {
-  if (F32) {
-    uint32_t top = 0;
+__device__ __forceinline__ uint32_t largest(const Raw& v) {
+  uint32_t top = 0;
+  if constexpr (F32) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = max(top, v.w[i] & 0x7FFFFFFFu);
     return top;
   }
-  uint32_t two = 0;   // both halves at once: bf16 magnitudes order like integers
 #pragma unroll
-  for (int i = 0; i < 4; ++i) two = __vmaxu2(two, v.w[i] & 0x7FFF7FFFu);
-  return max(two << 16, two & 0xFFFF0000u);
+  for (int i = 0; i < 8; ++i) top = __vmaxu2(top, v.w[i] & 0x7FFF7FFFu);   // both halves: bf16 magnitudes order like integers
+  return max(top << 16, top & 0xFFFF0000u);
 }
 
 template <bool F32, bool VEC, int U>
 __global__ void __launch_bounds__(256) quantize_mx4(const void* __restrict__ in, uint8_t* __restrict__ codes,
                                                     uint8_t* __restrict__ scale, const QuantParams p) {
+  constexpr int kBlockThreads = F32 ? 4 : 2, kQuadThreads = 4 * kBlockThreads, kCodeBytes = F32 ? 4 : 8;
   pdl_wait();
   pdl_launch_dependents();
   const uint32_t first = blockIdx.x * (256u * U) + threadIdx.x;
-  Raw8<F32> v[U];
+  Raw v[U];
   ItemAt at0;
   p.div_row.divmod(first, at0.row, at0.col);
   ItemAt at = at0;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    if (first + u * 256u < p.items) load8<F32, VEC>(in, at, p.K, v[u]);
+    if (first + u * 256u < p.items) load_raw<F32, VEC>(in, at, p.K, v[u]);
     at.advance(p);
   }
   at = at0;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    // groups of sixteen threads share a row and `items` is a multiple of sixteen: the shuffles stay inside a group
+    // groups of kQuadThreads share a row and `items` is a multiple of that: the shuffles stay inside a group
     if (first + u * 256u >= p.items) break;
-    const unsigned group = 0xFFFFu << (threadIdx.x & 16u);
+    const unsigned group = ((1u << kQuadThreads) - 1u) << (threadIdx.x & 31u & ~(kQuadThreads - 1u));
     uint32_t top = largest<F32>(v[u]);
     top = max(top, __shfl_xor_sync(group, top, 1));
-    top = max(top, __shfl_xor_sync(group, top, 2));
+    if (F32) top = max(top, __shfl_xor_sync(group, top, 2));
     const uint32_t e = mx4_exponent(top);
+    uint32_t quad = __shfl_down_sync(group, e, kBlockThreads, kQuadThreads) << 8 | e;
+    quad |= __shfl_down_sync(group, quad, 2 * kBlockThreads, kQuadThreads) << 16;
+    uint8_t* to = codes + static_cast<int64_t>(at.row) * p.pitch + at.col * static_cast<uint32_t>(kCodeBytes);
+    const bool inside = at.col * static_cast<uint32_t>(kCodeBytes) < static_cast<uint32_t>(p.pitch);
     float x[8];
+    if (F32) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      x[i] = F32 ? __uint_as_float(v[u].w[F32 ? i : 0])
-                 : __uint_as_float(i & 1 ? v[u].w[F32 ? 0 : i / 2] & 0xFFFF0000u : v[u].w[F32 ? 0 : i / 2] << 16);
-    const uint32_t word = mx4_codes8(x, e);
-    uint32_t quad = __shfl_down_sync(group, e, 4, 16) << 8 | e;
-    quad |= __shfl_down_sync(group, quad, 8, 16) << 16;
-    if (at.col * 4u < static_cast<uint32_t>(p.pitch))
-      *reinterpret_cast<uint32_t*>(codes + static_cast<int64_t>(at.row) * p.pitch + at.col * 4u) = word;
-    if ((threadIdx.x & 15u) == 0)
-      *reinterpret_cast<uint32_t*>(scale + scale_quad_at(at.row, at.col >> 4, p.kt)) = quad;
+      for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(v[u].w[i]);
+      if (inside) *reinterpret_cast<uint32_t*>(to) = mx4_codes8(x, e);
+    } else {
+      uint32_t word[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[2 * i] = __uint_as_float(v[u].w[4 * k + i] << 16);
+          x[2 * i + 1] = __uint_as_float(v[u].w[4 * k + i] & 0xFFFF0000u);
+        }
+        word[k] = mx4_codes8(x, e);
+      }
+      if (inside) *reinterpret_cast<uint2*>(to) = make_uint2(word[0], word[1]);   // (the pitch is a multiple of 16)
+    }
+    if ((threadIdx.x & (kQuadThreads - 1u)) == 0)
+      *reinterpret_cast<uint32_t*>(scale + scale_quad_at(at.row, at.col / kQuadThreads, p.kt)) = quad;
     at.advance(p);
   }
 }
@@ -187,6 +197,7 @@ __global__ void __launch_bounds__(256) quantize_mx4(const void* __restrict__ in,
 template <bool F32, bool VEC, int U>
 __global__ void __launch_bounds__(256) dequantize_mx4(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scale,
                                                       void* __restrict__ out, const QuantParams p) {
+  __shared__ __align__(16) uint16_t staged[VEC ? 8 : 256 * 8];
   pdl_wait();
   pdl_launch_dependents();
   const uint32_t first = blockIdx.x * (256u * U) + threadIdx.x;
@@ -207,61 +218,85 @@ __global__ void __launch_bounds__(256) dequantize_mx4(const uint8_t* __restrict_
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int left = static_cast<int>(p.K) - static_cast<int>(at.col) * 8;
-    if (first + u * 256u < p.items && left > 0) {
-      const int64_t to = static_cast<int64_t>(at.row) * p.K + at.col * 8u;
-      // bf16 holds every value exactly; fp32 is the same bits with zeros behind
-      uint32_t w[4];
-      mx4_words_bf16(word[u], e[u], w);
-      if (VEC) {
-        if (F32) {
-          uint4* o = reinterpret_cast<uint4*>(static_cast<float*>(out) + to);
-          __stcs(o, make_uint4(w[0] << 16, w[0] & 0xFFFF0000u, w[1] << 16, w[1] & 0xFFFF0000u));
-          __stcs(o + 1, make_uint4(w[2] << 16, w[2] & 0xFFFF0000u, w[3] << 16, w[3] & 0xFFFF0000u));
-        } else {
-          __stcs(reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + to), make_uint4(w[0], w[1], w[2], w[3]));
-        }
-      } else {
+    // bf16 holds every value exactly; fp32 is the same bits with zeros behind
+    uint32_t w[4];
+    mx4_words_bf16(word[u], e[u], w);
+    if (F32 && VEC) {
+      // Two neighbours' 64 bytes in two stores that each write whole 32-byte sectors: first both halves of the even
+      // lane's values, then of the odd lane's (4096 x 4096: 24 us when each lane stored its own halves).
+      const bool odd = threadIdx.x & 1u;
+      const uint32_t a = __shfl_xor_sync(0xFFFFFFFFu, odd ? w[0] : w[2], 1), b = __shfl_xor_sync(0xFFFFFFFFu, odd ? w[1] : w[3], 1);
+      const uint32_t near[2] = {odd ? a : w[0], odd ? b : w[1]}, far[2] = {odd ? w[2] : a, odd ? w[3] : b};
+      const uint32_t col = at.col & ~1u;
+      if (first + u * 256u < p.items) {
+        uint4* o = reinterpret_cast<uint4*>(static_cast<float*>(out) + static_cast<int64_t>(at.row) * p.K + col * 8u) + odd;
+        const int room = static_cast<int>(p.K) - static_cast<int>(col) * 8;
+        if (room > 0) __stcs(o, make_uint4(near[0] << 16, near[0] & 0xFFFF0000u, near[1] << 16, near[1] & 0xFFFF0000u));
+        if (room > 8) __stcs(o + 2, make_uint4(far[0] << 16, far[0] & 0xFFFF0000u, far[1] << 16, far[1] & 0xFFFF0000u));
+      }
+    } else if (VEC) {
+      if (first + u * 256u < p.items && left > 0)
+        __stcs(reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + static_cast<int64_t>(at.row) * p.K + at.col * 8u),
+               make_uint4(w[0], w[1], w[2], w[3]));
+    } else {
+      // rows without alignment: sixteen lanes hold 128 neighbouring values of a row and store them sixteen at a time
+      const uint32_t lane16 = threadIdx.x & 15u;
+      __syncwarp();
+      *reinterpret_cast<uint4*>(&staged[threadIdx.x * 8u]) = make_uint4(w[0], w[1], w[2], w[3]);
+      __syncwarp();
+      if (first + u * 256u < p.items) {
+        const int col = static_cast<int>(at.col & ~15u) * 8;
+        const int64_t to = static_cast<int64_t>(at.row) * p.K + col;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (j < left) {
-            const uint32_t half = j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xFFFFu;
-            if (F32) static_cast<uint32_t*>(out)[to + j] = half << 16;
-            else static_cast<uint16_t*>(out)[to + j] = static_cast<uint16_t>(half);
+        for (int j = 0; j < 8; ++j) {
+          const int c = j * 16 + static_cast<int>(lane16);
+          const uint16_t half = staged[(threadIdx.x & ~15u) * 8u + c];
+          if (col + c < static_cast<int>(p.K)) {
+            if (F32) static_cast<uint32_t*>(out)[to + c] = static_cast<uint32_t>(half) << 16;
+            else static_cast<uint16_t*>(out)[to + c] = half;
           }
+        }
       }
     }
     at.advance(p);
   }
 }
 
-int quant_params(const Mx4View& v, QuantParams* p) {
-  const int64_t items = v.rows * v.kt * 16;
-  if (items > INT32_MAX - 4096) return GL_ERR_UNSUPPORTED;
+// Parameters for items of `vals` values.
+int quant_params(const Mx4View& v, int vals, QuantParams* p) {
+  const int64_t items = v.rows * v.kt * (128 / vals);
+  if (v.rows * v.kt * 16 > INT32_MAX - 4096) return GL_ERR_UNSUPPORTED;   // (one limit whatever the type)
   p->K = v.K;
   p->pitch = v.pitch;
   p->kt = v.kt;
   p->items = static_cast<uint32_t>(items);
-  p->per_row = static_cast<uint32_t>(v.kt * 16);
+  p->per_row = static_cast<uint32_t>(v.kt * (128 / vals));
   p->step_rows = 256u / p->per_row;
   p->step_cols = 256u % p->per_row;
   p->div_row.set(p->per_row);
   return GL_OK;
 }
 
+// Several items per thread only when every SM has blocks to hold.
+constexpr int kItemsPerThread = 4;
+bool many_items(const QuantParams& p) { return p.items >= 148u * 4u * 256u * kItemsPerThread; }
+dim3 item_grid(const QuantParams& p) {
+  const uint32_t per_block = 256u * (many_items(p) ? kItemsPerThread : 1);
+  return dim3((p.items + per_block - 1) / per_block);
+}
+
 int launch_quantize(const gl_ap& in, const Mx4View& v, void* codes, void* scale, cudaStream_t st) {
-  QuantParams p;
-  const int rc = quant_params(v, &p);
-  if (rc) return rc;
   const bool f32 = in.dtype == GL_F32, vec = v.K % 8 == 0;
-  constexpr int kU = 4;
-  const bool wide = p.items >= 148u * 4u * 256u * kU;   // several items per thread only when every SM has blocks to hold
-  const dim3 grid((p.items + 256u * (wide ? kU : 1) - 1) / (256u * (wide ? kU : 1)));
+  QuantParams p;
+  const int rc = quant_params(v, f32 ? 8 : 16, &p);
+  if (rc) return rc;
+  constexpr int kU = kItemsPerThread;
   void (*k)(const void*, uint8_t*, uint8_t*, QuantParams) =
-      wide ? (f32 ? (vec ? quantize_mx4<true, true, kU> : quantize_mx4<true, false, kU>)
-                  : (vec ? quantize_mx4<false, true, kU> : quantize_mx4<false, false, kU>))
-           : (f32 ? (vec ? quantize_mx4<true, true, 1> : quantize_mx4<true, false, 1>)
-                  : (vec ? quantize_mx4<false, true, 1> : quantize_mx4<false, false, 1>));
-  return launch_pdl(k, grid, dim3(256), 0, st, 1, static_cast<const void*>(in.data), static_cast<uint8_t*>(codes),
+      many_items(p) ? (f32 ? (vec ? quantize_mx4<true, true, kU> : quantize_mx4<true, false, kU>)
+                           : (vec ? quantize_mx4<false, true, kU> : quantize_mx4<false, false, kU>))
+                    : (f32 ? (vec ? quantize_mx4<true, true, 1> : quantize_mx4<true, false, 1>)
+                           : (vec ? quantize_mx4<false, true, 1> : quantize_mx4<false, false, 1>));
+  return launch_pdl(k, item_grid(p), dim3(256), 0, st, 1, static_cast<const void*>(in.data), static_cast<uint8_t*>(codes),
                     static_cast<uint8_t*>(scale), p) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
 }
 
@@ -1051,18 +1086,16 @@ int gl_mx4_dequantize(const gl_mx4* in, gl_ap* out, void* stream) {
   if (rc) return rc;
   if (!same_shape(out, in)) return GL_ERR_SHAPE;
   QuantParams p;
-  rc = quant_params(v, &p);
+  rc = quant_params(v, 8, &p);
   if (rc) return rc;
   const bool f32 = out->dtype == GL_F32, vec = v.K % 8 == 0;
-  constexpr int kU = 4;
-  const bool wide = p.items >= 148u * 4u * 256u * kU;
-  const dim3 grid((p.items + 256u * (wide ? kU : 1) - 1) / (256u * (wide ? kU : 1)));
+  constexpr int kU = kItemsPerThread;
   void (*k)(const uint8_t*, const uint8_t*, void*, QuantParams) =
-      wide ? (f32 ? (vec ? dequantize_mx4<true, true, kU> : dequantize_mx4<true, false, kU>)
-                  : (vec ? dequantize_mx4<false, true, kU> : dequantize_mx4<false, false, kU>))
-           : (f32 ? (vec ? dequantize_mx4<true, true, 1> : dequantize_mx4<true, false, 1>)
-                  : (vec ? dequantize_mx4<false, true, 1> : dequantize_mx4<false, false, 1>));
-  return launch_pdl(k, grid, dim3(256), 0, static_cast<cudaStream_t>(stream), 1, static_cast<const uint8_t*>(in->data),
+      many_items(p) ? (f32 ? (vec ? dequantize_mx4<true, true, kU> : dequantize_mx4<true, false, kU>)
+                           : (vec ? dequantize_mx4<false, true, kU> : dequantize_mx4<false, false, kU>))
+                    : (f32 ? (vec ? dequantize_mx4<true, true, 1> : dequantize_mx4<true, false, 1>)
+                           : (vec ? dequantize_mx4<false, true, 1> : dequantize_mx4<false, false, 1>));
+  return launch_pdl(k, item_grid(p), dim3(256), 0, static_cast<cudaStream_t>(stream), 1, static_cast<const uint8_t*>(in->data),
                     static_cast<const uint8_t*>(in->scale), out->data, p) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
 }
 
@@ -1113,7 +1146,7 @@ int gl_dense_mx4(const gl_ap* a0, const gl_mx4* a1, gl_ap* out, uint32_t flags, 
   rc = check_mx4_data(&q, &a.v);
   if (rc) return rc;
   QuantParams qp;
-  rc = quant_params(a.v, &qp);
+  rc = quant_params(a.v, 8, &qp);
   if (rc) return rc;
   b.codes = a1->data;
   b.scale = a1->scale;
