@@ -43,19 +43,14 @@ struct CacheView {
 
 __device__ __forceinline__ int clamped_length(const CacheView& c, int b) { return min(max(c.lengths[b], 0), c.capacity); }
 
-// Start of the group that holds token `pos` of sequence b, or null where its page does not exist.
-__device__ __forceinline__ uint8_t* group_of(const CacheView& c, int b, int h, int pos) {
-  const int slot = pos / c.page_tokens;
-  const int page = c.table[static_cast<int64_t>(b) * c.width + slot];
-  if (page < 0 || page >= c.pages) return nullptr;
-  return c.data + page * c.page_stride + h * c.head_stride;
-}
-
 // ------------------------------------------------------------------------
 // Storing and reading back
 // ------------------------------------------------------------------------
 
-// Eight dims of one token and head per thread, K and V in the two halves of the grid's y dimension.
+// Eight dims of K and of V of one token and head per item.  Neighbouring threads have neighbouring items: D / 8 of them
+// (8, 16 or 32, inside a warp) share a token and head.  U items per thread, 256 apart, are requested before the first is
+// used.  What bounds both kernels are the instructions that find an item's place: K and V share them (apart, 14 us each
+// way for 8192 tokens of 8 heads of 128).
 struct TokensParams {
   CacheView c;
   int T, D;
@@ -64,88 +59,135 @@ struct TokensParams {
   FastDiv div_row, div_heads, div_T;
 };
 
-struct TokenAt { int b, i, h, w, pos; };
+struct TokenAt {
+  int w;                 // which eight dims
+  int tok;               // place in its group
+  int64_t dense;         // element of the dense side
+  uint8_t* group;        // null: not in the cache
+};
 
 __device__ __forceinline__ TokenAt token_at(const TokensParams& p, uint32_t item) {
-  uint32_t row, w, tok, h, b, i;
+  uint32_t row, w, token, h, b, i;
   p.div_row.divmod(item, row, w);
-  p.div_heads.divmod(row, tok, h);
-  p.div_T.divmod(tok, b, i);
-  TokenAt t = {static_cast<int>(b), static_cast<int>(i), static_cast<int>(h), static_cast<int>(w), 0};
-  t.pos = clamped_length(p.c, t.b) - p.T + t.i;
+  p.div_heads.divmod(row, token, h);
+  p.div_T.divmod(token, b, i);
+  TokenAt t;
+  t.w = static_cast<int>(w);
+  t.dense = static_cast<int64_t>(token) * p.pitch + static_cast<int64_t>(h) * p.D + w * 8u;
+  t.group = nullptr;
+  t.tok = 0;
+  const int pos = clamped_length(p.c, static_cast<int>(b)) - p.T + static_cast<int>(i);
+  if (item < p.items && pos >= 0) {
+    uint32_t slot, in_page;
+    p.c.div_page.divmod(static_cast<uint32_t>(pos), slot, in_page);
+    const int page = p.c.table[static_cast<int64_t>(b) * p.c.width + slot];
+    t.tok = static_cast<int>(in_page % kGroup);
+    if (page >= 0 && page < p.c.pages)
+      t.group = p.c.data + page * p.c.page_stride + h * p.c.head_stride + static_cast<int64_t>(in_page / kGroup) * group_bytes(p.D);
+  }
   return t;
 }
 
-__global__ void __launch_bounds__(256) cache4_append(const uint16_t* __restrict__ k, const uint16_t* __restrict__ v,
-                                                     const TokensParams p) {
-  pdl_wait();
-  pdl_launch_dependents();
-  const uint32_t item = blockIdx.x * 256u + threadIdx.x;
-  if (item >= p.items) return;   // D / 8 is a multiple of eight: groups of four threads (one block of values) stay whole
-  const TokenAt t = token_at(p, item);
-  const bool is_v = blockIdx.y != 0;
-  uint4 raw = make_uint4(0, 0, 0, 0);
-  if (t.pos >= 0)
-    raw = *reinterpret_cast<const uint4*>((is_v ? v : k) + (static_cast<int64_t>(t.b) * p.T + t.i) * p.pitch +
-                                          static_cast<int64_t>(t.h) * p.D + t.w * 8);
+// The thread of dims 32 b + 8 j .. + 7 stores, of V, the four bytes that hold dims 4 g .. + 3, g = 2 j + (b & 1), of the blocks
+// b & ~1 and b | 1: offset in the token's row of codes.
+__device__ __forceinline__ int v_offset(int NB, int b, int j, int tok) {
+  return (((2 * j + (b & 1)) ^ ((tok & 2) ? 4 : 0)) * NB + (b & ~1)) * 2;
+}
+
+// Scale exponent and codes of a thread's eight values, four neighbouring threads a block.  (Every thread of the warp.)
+__device__ __forceinline__ void quantize8(const uint4& raw, uint32_t& e, uint32_t& word) {
   const uint32_t in[4] = {raw.x, raw.y, raw.z, raw.w};
   float x[8];
-  uint32_t top = 0;
+  uint32_t two = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     x[2 * i] = __uint_as_float(in[i] << 16);
     x[2 * i + 1] = __uint_as_float(in[i] & 0xFFFF0000u);
-    top = max(top, max(__float_as_uint(x[2 * i]) & 0x7FFFFFFFu, __float_as_uint(x[2 * i + 1]) & 0x7FFFFFFFu));
+    two = __vmaxu2(two, in[i] & 0x7FFF7FFFu);
   }
-  const unsigned four = 0xFu << (threadIdx.x & 28u);
-  top = max(top, __shfl_xor_sync(four, top, 1));
-  top = max(top, __shfl_xor_sync(four, top, 2));
-  if (t.pos < 0) return;
-  uint8_t* at = group_of(p.c, t.b, t.h, t.pos);
-  if (!at) return;
-  const int in_page = t.pos % p.c.page_tokens, tok = in_page % kGroup;
-  at += static_cast<int64_t>(in_page / kGroup) * group_bytes(p.D);
-  const uint32_t e = mx4_exponent(top), word = mx4_codes8(x, e);
-  const int NB = p.D / 32, b = t.w >> 2, j = t.w & 3;
-  if (is_v) {
-    uint8_t* row = at + v_codes_at(p.D) + tok * (p.D / 2);
-    const int swz = (tok & 2) ? 4 : 0;
-    *reinterpret_cast<uint16_t*>(row + (((2 * j) ^ swz) * NB + b) * 2) = static_cast<uint16_t>(word);
-    *reinterpret_cast<uint16_t*>(row + (((2 * j + 1) ^ swz) * NB + b) * 2) = static_cast<uint16_t>(word >> 16);
-    if (j == 0) at[v_scales_at(p.D) + tok * NB + b] = static_cast<uint8_t>(e);
-  } else {
-    *reinterpret_cast<uint32_t*>(at + tok * (p.D / 2) + (j * NB + b) * 4) = word;
-    if (j == 0) at[k_scales_at(p.D) + tok * NB + b] = static_cast<uint8_t>(e);
+  uint32_t top = max(two << 16, two & 0xFFFF0000u);
+  top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+  top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+  e = mx4_exponent(top);
+  word = mx4_codes8(x, e);
+}
+// Words of the lanes of blocks b & ~1 and b | 1, same j: their low halves, or their high ones.
+__device__ __forceinline__ uint32_t halves_of_pair(uint32_t word, bool high) {
+  const int even = static_cast<int>(threadIdx.x & 31u) & ~4;
+  const uint32_t w0 = __shfl_sync(0xFFFFFFFFu, word, even), w1 = __shfl_sync(0xFFFFFFFFu, word, even | 4);
+  return __byte_perm(w0, w1, high ? 0x7632 : 0x5410);
+}
+
+template <int U>
+__global__ void __launch_bounds__(256) cache4_append(const uint16_t* __restrict__ k, const uint16_t* __restrict__ v,
+                                                     const TokensParams p) {
+  pdl_wait();
+  pdl_launch_dependents();
+  TokenAt at[U];
+  uint4 raw_k[U], raw_v[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const uint32_t item = (blockIdx.x * U + u) * 256u + threadIdx.x;
+    at[u] = token_at(p, item);
+    // (does not wait for the page: a token that is not stored is read all the same)
+    raw_k[u] = raw_v[u] = make_uint4(0, 0, 0, 0);
+    if (item < p.items) {
+      raw_k[u] = __ldcs(reinterpret_cast<const uint4*>(k + at[u].dense));
+      raw_v[u] = __ldcs(reinterpret_cast<const uint4*>(v + at[u].dense));
+    }
+  }
+  const int NB = p.D / 32;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {   // (every thread goes through the shuffles)
+    uint32_t ek, ev, wk, wv;
+    quantize8(raw_k[u], ek, wk);
+    quantize8(raw_v[u], ev, wv);
+    const int b = at[u].w >> 2, j = at[u].w & 3, tok = at[u].tok;
+    wv = halves_of_pair(wv, b & 1);
+    uint8_t* group = at[u].group;
+    if (group) {
+      const int codes = tok * (p.D / 2), scales = tok * NB + b;
+      *reinterpret_cast<uint32_t*>(group + codes + (j * NB + b) * 4) = wk;
+      *reinterpret_cast<uint32_t*>(group + v_codes_at(p.D) + codes + v_offset(NB, b, j, tok)) = wv;
+      if (j == 0) {
+        group[k_scales_at(p.D) + scales] = static_cast<uint8_t>(ek);
+        group[v_scales_at(p.D) + scales] = static_cast<uint8_t>(ev);
+      }
+    }
   }
 }
 
+template <int U>
 __global__ void __launch_bounds__(256) cache4_read(uint16_t* __restrict__ k, uint16_t* __restrict__ v, const TokensParams p) {
   pdl_wait();
   pdl_launch_dependents();
-  const uint32_t item = blockIdx.x * 256u + threadIdx.x;
-  if (item >= p.items) return;
-  const TokenAt t = token_at(p, item);
-  const bool is_v = blockIdx.y != 0;
-  const uint8_t* at = t.pos >= 0 ? group_of(p.c, t.b, t.h, t.pos) : nullptr;
-  uint32_t w[4] = {0, 0, 0, 0};
-  if (at) {
-    const int in_page = t.pos % p.c.page_tokens, tok = in_page % kGroup;
-    at += static_cast<int64_t>(in_page / kGroup) * group_bytes(p.D);
-    const int NB = p.D / 32, b = t.w >> 2, j = t.w & 3;
-    uint32_t word, e;
-    if (is_v) {
-      const uint8_t* row = at + v_codes_at(p.D) + tok * (p.D / 2);
-      const int swz = (tok & 2) ? 4 : 0;
-      word = *reinterpret_cast<const uint16_t*>(row + (((2 * j) ^ swz) * NB + b) * 2);
-      word |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(row + (((2 * j + 1) ^ swz) * NB + b) * 2)) << 16;
-      e = at[v_scales_at(p.D) + tok * NB + b];
-    } else {
-      word = *reinterpret_cast<const uint32_t*>(at + tok * (p.D / 2) + (j * NB + b) * 4);
-      e = at[k_scales_at(p.D) + tok * NB + b];
+  const int NB = p.D / 32;
+  TokenAt at[U];
+  uint32_t wk[U], wv[U], ek[U], ev[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    at[u] = token_at(p, (blockIdx.x * U + u) * 256u + threadIdx.x);
+    wk[u] = wv[u] = ek[u] = ev[u] = 0;
+    if (at[u].group) {
+      const int b = at[u].w >> 2, j = at[u].w & 3, tok = at[u].tok, codes = tok * (p.D / 2), scales = tok * NB + b;
+      wk[u] = *reinterpret_cast<const uint32_t*>(at[u].group + codes + (j * NB + b) * 4);
+      wv[u] = *reinterpret_cast<const uint32_t*>(at[u].group + v_codes_at(p.D) + codes + v_offset(NB, b, j, tok));
+      ek[u] = at[u].group[k_scales_at(p.D) + scales];
+      ev[u] = at[u].group[v_scales_at(p.D) + scales];
     }
-    mx4_words_bf16(word, e, w);
   }
-  *reinterpret_cast<uint4*>((is_v ? v : k) + static_cast<int64_t>(item) * 8) = make_uint4(w[0], w[1], w[2], w[3]);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    // of V, dims 8 j .. + 3 come from the lane of the even block, + 4 .. + 7 from that of the odd one
+    wv[u] = halves_of_pair(wv[u], at[u].w & 4);
+    if ((blockIdx.x * U + u) * 256u + threadIdx.x < p.items) {
+      uint32_t w[4];
+      mx4_words_bf16(wk[u], ek[u], w);
+      __stcs(reinterpret_cast<uint4*>(k + at[u].dense), make_uint4(w[0], w[1], w[2], w[3]));
+      mx4_words_bf16(wv[u], ev[u], w);
+      __stcs(reinterpret_cast<uint4*>(v + at[u].dense), make_uint4(w[0], w[1], w[2], w[3]));
+    }
+  }
 }
 
 // ------------------------------------------------------------------------
@@ -1140,6 +1182,14 @@ int tokens_params(const gl_cache4* cache, const gl_ap* k, const gl_ap* v, int64_
   return GL_OK;
 }
 
+// Several items per thread only when every SM has blocks to hold.
+constexpr int kTokenItems = 2;
+bool several_items(const TokensParams& p) { return p.items >= 148u * 4u * 256u * kTokenItems; }
+dim3 token_grid(const TokensParams& p, bool many) {
+  const uint32_t per_block = 256u * (many ? kTokenItems : 1);
+  return dim3((p.items + per_block - 1) / per_block);
+}
+
 // Which kernel runs, and its numbers.
 struct AttKernel {
   void (*fn)(AttendParams);
@@ -1210,8 +1260,9 @@ int gl_cache4_append(const gl_cache4* cache, const gl_ap* k, const gl_ap* v, int
   TokensParams p;
   const int rc = tokens_params(cache, k, v, token_pitch, at, &p);
   if (rc) return rc;
-  const dim3 grid((p.items + 255) / 256, 2);
-  return launch_pdl(cache4_append, grid, dim3(256), 0, static_cast<cudaStream_t>(stream), 1, static_cast<const uint16_t*>(k->data),
+  const bool many = several_items(p);
+  return launch_pdl(many ? cache4_append<kTokenItems> : cache4_append<1>, token_grid(p, many), dim3(256), 0,
+                    static_cast<cudaStream_t>(stream), 1, static_cast<const uint16_t*>(k->data),
                     static_cast<const uint16_t*>(v->data), p) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
 }
 
@@ -1219,9 +1270,10 @@ int gl_cache4_read(const gl_cache4* cache, const gl_pages* at, gl_ap* k, gl_ap* 
   TokensParams p;
   const int rc = tokens_params(cache, k, v, 0, at, &p);
   if (rc) return rc;
-  const dim3 grid((p.items + 255) / 256, 2);
-  return launch_pdl(cache4_read, grid, dim3(256), 0, static_cast<cudaStream_t>(stream), 1, static_cast<uint16_t*>(k->data),
-                    static_cast<uint16_t*>(v->data), p) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
+  const bool many = several_items(p);
+  return launch_pdl(many ? cache4_read<kTokenItems> : cache4_read<1>, token_grid(p, many), dim3(256), 0,
+                    static_cast<cudaStream_t>(stream), 1, static_cast<uint16_t*>(k->data), static_cast<uint16_t*>(v->data), p) ==
+                 cudaSuccess ? GL_OK : GL_ERR_CUDA;
 }
 
 size_t gl_attend_cache4_workspace(const gl_ap* q, const gl_cache4* cache) {

@@ -134,10 +134,11 @@ __device__ __forceinline__ uint32_t largest(const Raw& v) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = max(top, v.w[i] & 0x7FFFFFFFu);
     return top;
-  }
+  } else {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) top = __vmaxu2(top, v.w[i] & 0x7FFF7FFFu);   // both halves: bf16 magnitudes order like integers
-  return max(top << 16, top & 0xFFFF0000u);
+    for (int i = 0; i < 8; ++i) top = __vmaxu2(top, v.w[i] & 0x7FFF7FFFu);   // both halves: bf16 magnitudes order like integers
+    return max(top << 16, top & 0xFFFF0000u);
+  }
 }
 
 template <bool F32, bool VEC, int U>
