@@ -62,22 +62,23 @@ __device__ __forceinline__ void tc_wait_store() { asm volatile("tcgen05.wait::st
 // Scales of four blocks, a byte each: is one of them above 2^1 (e > 128)?
 __device__ __forceinline__ bool any_above_128(uint32_t e4) { return (((e4 & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) & e4 & 0x80808080u) != 0u; }
 
+// Is one of them NaN (e = 255)?
+__device__ __forceinline__ bool any_255(uint32_t e4) { return ((((~e4) & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | ~e4 | 0x7F7F7F7Fu) != 0xFFFFFFFFu; }
+
 // Eight codes (pairs: code i of the low and of the high half) -> four bf16 pairs times the scales of bytes lo and hi of e4.
-// 2^(e - 1), the factor that the moved codes lack, is a bf16 up to e = 128.  ABOVE: some scale may be larger; the factor comes in two steps.
+// 2^(e - 1), the factor that the moved codes lack, is a bf16 up to e = 128.  ABOVE: some scale may be larger; 2^126 and
+// 2^(e - 127) one after the other (Inf for e = 255: a NaN block's codes are zeros, and zero times Inf is NaN).
 template <bool ABOVE>
 __device__ __forceinline__ uint4 mx4_pairs_bf16(uint32_t z, uint32_t e4, int lo, int hi) {
   uint32_t h[4];
   mx4_pairs_moved(z, h);
   const uint32_t pair = __byte_perm(e4, 0u, lo | 4 << 4 | hi << 8 | 4 << 12);
   if constexpr (ABOVE) {
-    const uint32_t el = pair & 0xFFFFu, eh = pair >> 16;
-    const uint32_t first = (min(el, 128u) + 126u) << 7 | (min(eh, 128u) + 126u) << 23;
-    const uint32_t l2 = el == 255u ? 0x7FC0u : (el > 128u ? el - 1u : 127u) << 7;   // 2^(e - 128), or 1
-    const uint32_t h2 = eh == 255u ? 0x7FC0u : (eh > 128u ? eh - 1u : 127u) << 7;
+    const uint32_t f = __vmaxu2(pair * 128u, 0x00400040u);   // (e = 0: 2^-127 is subnormal)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = mul_bf16x2(mul_bf16x2(h[i], first), l2 | h2 << 16);
+    for (int i = 0; i < 4; ++i) h[i] = mul_bf16x2(mul_bf16x2(h[i], 0x7E807E80u), f);
   } else {
-    const uint32_t f = pair * 128u + 0x3F003F00u;   // bf16 2^(e - 1) in both halves
+    const uint32_t f = pair * 128u + 0x3F003F00u;            // 2^(e - 1) in both halves
 #pragma unroll
     for (int i = 0; i < 4; ++i) h[i] = mul_bf16x2(h[i], f);
   }
@@ -391,36 +392,44 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
           }
         }
       };
-      const auto widen_v = [&](auto above, unsigned char* vt, const Held<NB, kItems>& x, int tile) {
+      const auto widen_v = [&](auto above, unsigned char* vt, const Held<NB, kItems>& x) {
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
           const int tok = 64 * i + dw * 8 + (lane & 7);
 #pragma unroll
           for (int k = 0; k < NB; ++k) {
             const int b = 2 * (k % (NB / 2)), c = j * NB + k;
-            uint32_t word = x.word[i][k], e4 = x.exps[i][b >> 2];
-            if constexpr (decltype(above)::value) {   // a NaN goes to the rows that see this token when the result is stored
-#pragma unroll
-              for (int s = 0; s < 2; ++s)
-                if ((e4 >> (8 * ((b & 3) + s)) & 255u) == 255u) {
-                  atomicMin(nan_from + (item & 3u) * NB + b + s, tile * TT + tok);
-                  word &= s ? 0x0000FFFFu : 0xFFFF0000u;
-                  e4 &= ~(255u << (8 * ((b & 3) + s)));
-                }
-            }
             *reinterpret_cast<uint4*>(vt + (c >> 3) * (TT * 128) + tok * 128 + (((c & 7) ^ (tok & 7)) << 4)) =
-                mx4_pairs_bf16<decltype(above)::value>(word, e4, b & 3, (b & 3) + 1);
+                mx4_pairs_bf16<decltype(above)::value>(x.word[i][k], x.exps[i][b >> 2], b & 3, (b & 3) + 1);
           }
         }
       };
-      auto widen = [&](int tile, const Held<NB, kItems>& hk, const Held<NB, kItems>& hv, uint32_t groups) {
-        const uint32_t st = it & 1u, ph = (it >> 1) & 1u;
-        bool large = false;
+      // V blocks that are NaN: zeros in their place; the NaN goes to the rows that see the token when the result is stored
+      const auto take_nan = [&](Held<NB, kItems>& x, int tile) {
 #pragma unroll
         for (int i = 0; i < kItems; ++i)
 #pragma unroll
-          for (int k = 0; k < (NB <= 4 ? 1 : 2); ++k) large |= any_above_128(hk.exps[i][k]) || any_above_128(hv.exps[i][k]);
+          for (int b = 0; b < NB; ++b)
+            if ((x.exps[i][b >> 2] >> (8 * (b & 3)) & 255u) == 255u) {
+              atomicMin(nan_from + (item & 3u) * NB + b, tile * TT + 64 * i + dw * 8 + (lane & 7));
+              x.exps[i][b >> 2] &= ~(255u << (8 * (b & 3)));
+#pragma unroll
+              for (int k = 0; k < NB; ++k)   // words of the block pair that b is in: its half
+                if (2 * (k % (NB / 2)) == (b & ~1)) x.word[i][k] &= b & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+            }
+      };
+      auto widen = [&](int tile, Held<NB, kItems>& hk, Held<NB, kItems>& hv, uint32_t groups) {
+        const uint32_t st = it & 1u, ph = (it >> 1) & 1u;
+        bool large = false, nan = false;
+#pragma unroll
+        for (int i = 0; i < kItems; ++i)
+#pragma unroll
+          for (int k = 0; k < (NB <= 4 ? 1 : 2); ++k) {
+            large |= any_above_128(hk.exps[i][k]) || any_above_128(hv.exps[i][k]);
+            nan |= any_255(hv.exps[i][k]);
+          }
         large = __any_sync(0xFFFFFFFFu, large);
+        if (__any_sync(0xFFFFFFFFu, nan)) take_nan(hv, tile);
         if (!mbar_wait(b_kempty + 8 * st, ph ^ 1u, abort_flag)) return false;
         if (dw == 0 && lane == 0) have[it & 3u] = groups;
         unsigned char* kt = gen + MT * Cfg::kQ + 2 * st * Cfg::kKV;
@@ -430,8 +439,8 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
         __syncwarp();
         if (lane == 0) mbar_arrive(b_kfull + 8 * st);
         if (!mbar_wait(b_vempty + 8 * st, ph ^ 1u, abort_flag)) return false;
-        if (large) widen_v(std::true_type{}, kt + Cfg::kKV, hv, tile);
-        else widen_v(std::false_type{}, kt + Cfg::kKV, hv, tile);
+        if (large) widen_v(std::true_type{}, kt + Cfg::kKV, hv);
+        else widen_v(std::false_type{}, kt + Cfg::kKV, hv);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(b_vfull + 8 * st);
