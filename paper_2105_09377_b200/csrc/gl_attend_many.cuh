@@ -25,7 +25,7 @@ struct ManyCfg {
   static constexpr int MT = (NB <= 4 && TERMS == 1) ? 2 : 1;
   static constexpr int TT = NB == 8 ? 64 : 128;                 // tokens per tile
   static constexpr int kRows = 128 * MT;
-  static constexpr int kQ = 128 * D * 2;                        // bytes of one Q tile
+  static constexpr int kQ = D == 64 ? 32768 : 128 * D * 2;      // bytes of one Q tile (results are staged in its rows)
   static constexpr int kKV = TT * D * 2;                        // bytes of a K or V tile
   static constexpr int kStages = 2;
   static constexpr int kWidenWarps = 8;
@@ -56,6 +56,16 @@ __device__ __forceinline__ void tc_store_16cols(uint32_t taddr, const uint32_t (
       ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
         "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
+}
+__device__ __forceinline__ void tc_load_8cols(uint32_t taddr, uint32_t (&r)[8]) {   // (waits for nothing)
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tc_wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// Byte of 16-byte piece `piece` (0..15) of staged row `row`: 128 bytes in each of the Q tile's first two chunks, in that
+// row's own place, so that no warp touches another's rows.
+__device__ __forceinline__ uint32_t stage_piece(int row, int piece) {
+  return (piece >> 3) * 16384 + row * 128 + (((piece & 7) ^ (row & 7)) << 4);
 }
 __device__ __forceinline__ void tc_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -184,15 +194,18 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
     for (; ok && w.next(p); ++item) {
       const int row = w.rb * Cfg::kRows + m * 128 + r;
       const bool live = row < p.rows;
-      // Q: dims 8c .. 8c + 7 in the order 0 4 1 5 2 6 3 7, 128-byte swizzle
+      // Q: the warp's 32 rows, 16 bytes a lane along the rows; dims 8c .. 8c + 7 in the order 0 4 1 5 2 6 3 7, 128-byte swizzle
       {
-        const uint16_t* src = live ? q_row(p, w.b, w.h, row, D) : nullptr;
-#pragma unroll
-        for (int c = 0; c < D / 8; ++c) {
-          uint4 x = live ? *reinterpret_cast<const uint4*>(src + 8 * c) : make_uint4(0, 0, 0, 0);
+        constexpr int kLanes = D / 8, kAtOnce = kLanes < 32 ? 32 / kLanes : 1;   // lanes to a row, rows to an access
+        const int c = lane % kLanes;
+#pragma unroll 8
+        for (int i = 0; i < 32; i += kAtOnce) {
+          const int r1 = (warp & 3) * 32 + i + lane / kLanes, row1 = w.rb * Cfg::kRows + m * 128 + r1;
+          uint4 x = make_uint4(0, 0, 0, 0);
+          if (row1 < p.rows) x = *reinterpret_cast<const uint4*>(q_row(p, w.b, w.h, row1, D) + 8 * c);
           const uint4 y = make_uint4(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632), __byte_perm(x.y, x.w, 0x5410),
                                      __byte_perm(x.y, x.w, 0x7632));
-          *reinterpret_cast<uint4*>(gen + m * Cfg::kQ + (c >> 3) * 16384 + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = y;
+          *reinterpret_cast<uint4*>(gen + m * Cfg::kQ + (c >> 3) * 16384 + r1 * 128 + (((c & 7) ^ (r1 & 7)) << 4)) = y;
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
@@ -295,39 +308,51 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
       tc_fence_after();
       const bool whole = w.whole();
       const float inv = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
-      float* slot = w.slot(p, D) + static_cast<int64_t>(m * 128 + r) * (D + 2);
-      const int64_t to = live ? out_row(p, w.b, w.h, row, D) : 0;
-      if (!whole) *reinterpret_cast<float2*>(slot) = make_float2(ref, sum);
+      float* slot = w.slot(p, D) + static_cast<int64_t>(m * 128) * (D + 2);
+      if (!whole) *reinterpret_cast<float2*>(slot + r * (D + 2)) = make_float2(ref, sum);
       const int* nan_at = nan_from + (item & 3u) * NB;
-      // columns (g * NB/2 + w) * 8 + 2 i + half hold dims 32 (2 w + half) + 4 g + i
+      // 64 dims at a time (a pair of blocks), by way of the warp's rows of its Q tile, which no product reads any more:
+      // written a row per lane, stored along the rows.  Columns (g * NB/2 + pair) * 8 + 2 i + half hold dims
+      // 32 (2 pair + half) + 4 g + i.
+      const uint32_t rows_at = q_at + m * Cfg::kQ;
 #pragma unroll 1
-      for (int c = 0; c < D / 16; ++c) {
-        uint32_t x[16];
-        tc_load_16cols(o_col + 16 * c, x);
+      for (int pair = 0; pair < NB / 2; ++pair) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const int word = 2 * c + k, g = word / (NB / 2), wd = word % (NB / 2);
+        for (int hg = 0; hg < 2; ++hg) {   // four g at a time
+          uint32_t x[4][8];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) tc_load_8cols(o_col + ((4 * hg + k) * (NB / 2) + pair) * 8, x[k]);
+          tc_wait_load();
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
-            const int block = 2 * wd + half, d = 32 * block + 4 * g;
-            float v[4];
-            const bool bad = nan_at[block] < limit;
+            const bool bad = nan_at[2 * pair + half] < limit;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              v[i] = bad ? __uint_as_float(0x7FC00000u) : __uint_as_float(x[8 * k + 2 * i + half]) * inv;
-            if (!whole) {
-              *reinterpret_cast<float2*>(slot + d + 2) = make_float2(v[0], v[1]);
-              *reinterpret_cast<float2*>(slot + d + 4) = make_float2(v[2], v[3]);
-            } else if (live) {
-              if (p.out_bf16)
-                *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + to + d) =
-                    make_uint2(pack_bf16x2(__float_as_uint(v[0]), __float_as_uint(v[1])),
-                               pack_bf16x2(__float_as_uint(v[2]), __float_as_uint(v[3])));
-              else
-                *reinterpret_cast<float4*>(static_cast<float*>(p.out) + to + d) = make_float4(v[0], v[1], v[2], v[3]);
+            for (int k = 0; k < 4; ++k) {
+              uint32_t v[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) v[i] = bad ? 0x7FC00000u : __float_as_uint(__uint_as_float(x[k][2 * i + half]) * inv);
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(rows_at + stage_piece(r, half * 8 + 4 * hg + k)),
+                           "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
             }
           }
         }
+        __syncwarp();
+#pragma unroll 4
+        for (int i = 0; i < 32; ++i) {
+          const int r1 = (warp & 3) * 32 + i, row1 = w.rb * Cfg::kRows + m * 128 + r1, d = 64 * pair + 2 * lane;
+          float2 v;
+          asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(rows_at + stage_piece(r1, lane >> 1) + (lane & 1) * 8));
+          if (!whole) {
+            *reinterpret_cast<float2*>(slot + static_cast<int64_t>(r1) * (D + 2) + 2 + d) = v;
+          } else if (row1 < p.rows) {
+            const int64_t to = out_row(p, w.b, w.h, row1, D) + d;
+            if (p.out_bf16)
+              *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + to) = pack_bf16x2(__float_as_uint(v.x), __float_as_uint(v.y));
+            else
+              *reinterpret_cast<float2*>(static_cast<float*>(p.out) + to) = v;
+          }
+        }
+        __syncwarp();
       }
       tc_fence_before();
     }
