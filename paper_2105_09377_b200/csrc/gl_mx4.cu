@@ -649,9 +649,18 @@ dot_mx4(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUten
 // flight: the blocks' partial sums meet in distributed shared memory, added in rank order.  One tile per block, two
 // blocks per SM.  While the kernel that rounds A is still running the weights are on their way into L2.
 
+// At most kFuseRows rows (FUSED): the blocks round A themselves, each its own stretch of K, straight into operand order, while
+// the first weights are on their way: one launch.  (Through 8192 x 8192: one row 7.8 us against 10.1 us with a launch of
+// its own for the rounding, four rows 9.4 against 9.9; with more rows the repeated rounding costs more than the launch.)
+constexpr int kFuseRows = 4;
+constexpr int kFuseBlocks = 12;   // K blocks of A that a block has room for
+
 struct FewParams {
   int M;
   int64_t O;
+  const void* x;          // FUSED: rows of A as they came
+  int64_t K;
+  int x_f32;
   int kblocks, last_steps;
   int split;              // blocks per cluster
   int relu, out_bf16;
@@ -683,31 +692,66 @@ __device__ __forceinline__ void join_ranks(uint32_t mine, int rank, int64_t o, v
   }
 }
 
-template <int BN>
+template <int BN, bool FUSED>
 struct FewCfg {
   static constexpr int kStageA = kTile * kKBytes;                  // weights
-  static constexpr int kStageB = BN * kKBytes;
-  static constexpr int kStage = kStageA + kStageB + 2048;          // and two scale tiles of each side
-  static constexpr int kStages = (112 * 1024 - 1024 - 256) / kStage;
-  static constexpr int kSmemBytes = kStages * kStage + 1024 + 256;
+  static constexpr int kStageB = FUSED ? 0 : BN * kKBytes;
+  static constexpr int kStage = kStageA + kStageB + (FUSED ? 1024 : 2048);   // and two scale tiles of each side
+  static constexpr int kXBlock = BN * kKBytes + 1024;              // FUSED: a K block of A with its scale tiles
+  static constexpr int kXBytes = FUSED ? kFuseBlocks * kXBlock : 0;
+  static constexpr int kStages = (112 * 1024 - 1024 - 256 - kXBytes) / kStage;
+  static constexpr int kSmemBytes = kStages * kStage + kXBytes + 1024 + 256;
   static constexpr int kTmemCols = BN + 16 <= 32 ? 32 : BN + 16 <= 64 ? 64 : BN + 16 <= 128 ? 128 : 256;
   static constexpr int kSfBase = kTmemCols - 16;
-  static_assert(kStages * kStage >= BN * 128 * 4, "partial sums fit in the ring");
+  static_assert(kStages >= 2 && kStages * kStage >= BN * 128 * 4, "partial sums fit in the ring");
 };
 
+// One warp rounds K block kb of row m: lane = 8 values, into the swizzled operand row and the scale tiles.
 template <int BN>
+__device__ __forceinline__ void round_row_block(const FewParams& p, unsigned char* to, int m, int kb, int lane) {
+  const int64_t k0 = static_cast<int64_t>(kb) * 256 + lane * 8, left = p.K - k0, at = static_cast<int64_t>(m) * p.K + k0;
+  float x[8];
+  if (left >= 8 && (p.K & 7) == 0) {
+    if (p.x_f32) {
+      const float4 a = *reinterpret_cast<const float4*>(static_cast<const float*>(p.x) + at);
+      const float4 b = *(reinterpret_cast<const float4*>(static_cast<const float*>(p.x) + at) + 1);
+      x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    } else {
+      const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.x) + at);
+      const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      x[i] = i < left ? (p.x_f32 ? static_cast<const float*>(p.x)[at + i] : bf16_to_f32(static_cast<const uint16_t*>(p.x)[at + i])) : 0.f;
+  }
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+  top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+  top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+  const uint32_t e = mx4_exponent(top);
+  *reinterpret_cast<uint32_t*>(to + m * 128 + (((lane >> 2) ^ (m & 7)) << 4) + (lane & 3) * 4) = mx4_codes8(x, e);
+  if ((lane & 3) == 0) to[BN * kKBytes + (lane >> 4) * 512 + m * 16 + ((lane >> 2) & 3)] = static_cast<uint8_t>(e);
+}
+
+template <int BN, bool FUSED>
 __global__ void __launch_bounds__(kMxThreads, 2)
 dot_mx4_few(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
             const __grid_constant__ CUtensorMap map_sw, const __grid_constant__ CUtensorMap map_sx, void* __restrict__ out,
             const FewParams p) {
-  using Cfg = FewCfg<BN>;
+  using Cfg = FewCfg<BN, FUSED>;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t tiles = (raw + 1023u) & ~1023u;
   unsigned char* gen_tiles = smem_raw + (tiles - raw);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(gen_tiles + Cfg::kStages * Cfg::kStage);
-  const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8 * Cfg::kStages, bar_done = bar_empty + 8 * Cfg::kStages;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * Cfg::kStages + 1);
+  const uint32_t xs = tiles + Cfg::kStages * Cfg::kStage;            // FUSED: A, block by block
+  uint64_t* bars = reinterpret_cast<uint64_t*>(gen_tiles + Cfg::kStages * Cfg::kStage + Cfg::kXBytes);
+  const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8 * Cfg::kStages, bar_done = bar_empty + 8 * Cfg::kStages,
+                 bar_x = bar_done + 8;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * Cfg::kStages + 2);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = p.split > 1 ? static_cast<int>(cluster_ctarank()) : 0;
@@ -719,8 +763,9 @@ dot_mx4_few(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
   if (warp == 0 && elect_one())
     for (int kb = kb0; kb < kb1; ++kb) tma_prefetch_2d(&map_w, kb * kKBytes, tile * kTile);
   if (threadIdx.x == 0) {
-    for (int s = 0; s < Cfg::kStages; ++s) { mbar_init(bar_full + 8 * s, 2); mbar_init(bar_empty + 8 * s, 1); }
+    for (int s = 0; s < Cfg::kStages; ++s) { mbar_init(bar_full + 8 * s, FUSED ? 1 : 2); mbar_init(bar_empty + 8 * s, 1); }
     mbar_init(bar_done, 1);
+    mbar_init(bar_x, 5);   // warps 2 to 6
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -737,7 +782,15 @@ dot_mx4_few(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
   pdl_wait();
   pdl_launch_dependents();
 
-  if (warp == 0 || warp == 6) {
+  if (FUSED && warp >= 2) {
+    const int blocks = kb1 - kb0;   // rows one after the other, their K blocks side by side
+    for (int i = warp - 2; i < p.M * blocks; i += 5)
+      round_row_block<BN>(p, gen_tiles + Cfg::kStages * Cfg::kStage + (i % blocks) * Cfg::kXBlock, i / blocks, kb0 + i % blocks, lane);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar_x);
+  }
+  if (warp == 0 || (warp == 6 && !FUSED)) {
     const bool load_w = warp == 0;
     const bool leader = elect_one();
     uint32_t s = 0, ph = 0;
@@ -758,28 +811,29 @@ dot_mx4_few(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
     }
   } else if (warp == 1) {
     const bool leader = elect_one();
-    const uint64_t desc_w0 = make_desc(tiles, 16, 1024, 2), desc_x0 = make_desc(tiles + Cfg::kStageA, 16, 1024, 2);
+    const uint64_t desc_w0 = make_desc(tiles, 16, 1024, 2), desc_x0 = make_desc(FUSED ? xs : tiles + Cfg::kStageA, 16, 1024, 2);
     const uint64_t desc_s0 = make_desc(tiles + Cfg::kStageA + Cfg::kStageB, 16, 128, 0);
+    const uint64_t desc_sx0 = make_desc(FUSED ? xs + BN * kKBytes : tiles + Cfg::kStageA + Cfg::kStageB + 1024, 16, 128, 0);
     const uint32_t sfw = tmem_base + Cfg::kSfBase, sfx = sfw + 8;
     uint32_t s = 0, ph = 0;
-    bool ok = true;
-    for (int kb = kb0; kb < kb1; ++kb) {
+    bool ok = !FUSED || mbar_wait(bar_x, 0, abort_flag);
+    for (int kb = kb0; kb < kb1 && ok; ++kb) {
       if (!mbar_wait(bar_full + 8 * s, ph, abort_flag)) { ok = false; break; }
       tc_fence_after();
-      const uint64_t off = (s * Cfg::kStage) >> 4;
+      const uint64_t off = (s * Cfg::kStage) >> 4, xoff = FUSED ? ((kb - kb0) * Cfg::kXBlock) >> 4 : off;
       const int steps = kb + 1 == p.kblocks ? p.last_steps : 4;
 #pragma unroll
       for (int g = 0; g < 2; ++g)
         if (2 * g < steps) {
           if (leader) {
             tc_copy_scales<1>(sfw + 4 * g, desc_s0 + off + ((g * 512) >> 4));
-            tc_copy_scales<1>(sfx + 4 * g, desc_s0 + off + ((1024 + g * 512) >> 4));
+            tc_copy_scales<1>(sfx + 4 * g, desc_sx0 + xoff + ((g * 512) >> 4));
           }
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const int k = 2 * g + j;
             if (k < steps && leader)
-              tc_mma_mx4<1>(tmem_base, desc_w0 + off + 2 * k, desc_x0 + off + 2 * k, make_idesc_mx4(kTile, BN, j), sfw + 4 * g,
+              tc_mma_mx4<1>(tmem_base, desc_w0 + off + 2 * k, desc_x0 + xoff + 2 * k, make_idesc_mx4(kTile, BN, j), sfw + 4 * g,
                             sfx + 4 * g, kb != kb0 || k != 0 ? 1u : 0u);
           }
         }
@@ -955,13 +1009,14 @@ struct FewPlan {
   int grid;
 };
 
-template <int BN>
+// `fused`: A is still to be rounded, by the product's own blocks.
+template <int BN, bool FUSED>
 int plan_few(const Mx4Operand& a, const Mx4Operand& b, void* out, uint32_t flags, FewPlan* t) {
   static bool attr_set[64] = {false};   // per device; benign race: the call is idempotent
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return GL_ERR_CUDA;
   if (!attr_set[dev]) {
-    if (cudaFuncSetAttribute(dot_mx4_few<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<BN>::kSmemBytes) != cudaSuccess)
+    if (cudaFuncSetAttribute(dot_mx4_few<BN, FUSED>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<BN, FUSED>::kSmemBytes) != cudaSuccess)
       return GL_ERR_CUDA;
     attr_set[dev] = true;
   }
@@ -980,24 +1035,26 @@ int plan_few(const Mx4Operand& a, const Mx4Operand& b, void* out, uint32_t flags
   while (p.split < 8 && p.split * 2 <= p.kblocks && tiles * p.split * 2 <= 2 * num_sms()) p.split *= 2;
   t->out = out;
   t->grid = tiles * p.split;
-  return encode_codes(&t->mw, b, kTile) && encode_codes(&t->mx, a, BN) && encode_scales(&t->msw, b) && encode_scales(&t->msx, a)
-             ? GL_OK : GL_ERR_CUDA;
+  if (!encode_codes(&t->mw, b, kTile) || !encode_scales(&t->msw, b)) return GL_ERR_CUDA;
+  t->mx = t->mw;   // unused when FUSED; any valid map
+  t->msx = t->msw;
+  return FUSED || (encode_codes(&t->mx, a, BN) && encode_scales(&t->msx, a)) ? GL_OK : GL_ERR_CUDA;
 }
 
-template <int BN>
+template <int BN, bool FUSED>
 int run_few(const FewPlan& t, cudaStream_t st) {
-  return launch_pdl(dot_mx4_few<BN>, dim3(static_cast<unsigned>(t.grid)), dim3(kMxThreads), FewCfg<BN>::kSmemBytes, st, t.p.split,
+  return launch_pdl(dot_mx4_few<BN, FUSED>, dim3(static_cast<unsigned>(t.grid)), dim3(kMxThreads), FewCfg<BN, FUSED>::kSmemBytes, st, t.p.split,
                     t.mw, t.mx, t.msw, t.msx, t.out, t.p) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
 }
 
 template <int BN, typename Pre>
 int product_few(const Mx4Operand& a, const Mx4Operand& b, gl_ap* out, uint32_t flags, cudaStream_t st, Pre&& pre) {
   FewPlan t;
-  int rc = plan_few<BN>(a, b, out->data, flags, &t);
+  int rc = plan_few<BN, false>(a, b, out->data, flags, &t);
   if (rc) return rc;
   rc = pre();
   if (rc) return rc;
-  return run_few<BN>(t, st);
+  return run_few<BN, false>(t, st);
 }
 
 // Checks shared by the two products: shapes, result, aliasing rules are the caller's.
@@ -1154,6 +1211,18 @@ int gl_dense_mx4(const gl_ap* a0, const gl_mx4* a1, gl_ap* out, uint32_t flags, 
   a.codes = q.data;
   a.scale = q.scale;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (a.v.rows <= kFuseRows) {
+    if (!driver_api().ok) return GL_ERR_CUDA;
+    FewPlan t;
+    rc = plan_few<16, true>(a, b, out->data, flags, &t);
+    if (rc) return rc;
+    if ((t.p.kblocks + t.p.split - 1) / t.p.split <= kFuseBlocks) {
+      t.p.x = a0->data;
+      t.p.K = a.v.K;
+      t.p.x_f32 = a0->dtype == GL_F32;
+      return run_few<16, true>(t, st);
+    }
+  }
   return product(a, b, out, flags, st, [&] { return launch_quantize(*a0, a.v, q.data, q.scale, st); });
 }
 

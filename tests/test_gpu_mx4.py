@@ -88,7 +88,8 @@ def test_quantize_items_of_several_dims(gl):
 
 PRODUCTS = [(1, 32, 1), (1, 4096, 1000), (2, 64, 9), (7, 1, 5), (16, 3136, 1000), (33, 96, 130), (128, 256, 128), (129, 257, 127),
             (17, 8192, 264), (301, 1111, 777), (256, 512, 384), (64, 130, 2049), (300, 640, 512), (513, 2048, 260),
-            (2049, 320, 4200), (2300, 700, 2311), (100, 5000, 650), (9, 20000, 70)]
+            (2049, 320, 4200), (2300, 700, 2311), (100, 5000, 650), (9, 20000, 70),
+            (1, 1000, 9000), (3, 33000, 40), (4, 2049, 129)]
 
 
 @pytest.mark.parametrize("form", ["product", "dense"])
