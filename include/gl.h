@@ -23,7 +23,7 @@
  *     `out->access_ndim` and `out->dtype` must already equal what the matching
  *     gl_shape_* call returns, otherwise GL_ERR_SHAPE / GL_ERR_DTYPE.
  *   - Inputs are read-only and must not overlap outputs (gl_compute_relu may
- *     run in place).  Data pointers must be 16-byte aligned (GL_ERR_ALIGN).
+ *     run in place; a gl_cache4 is what gl_cache4_append writes).  Data pointers must be 16-byte aligned (GL_ERR_ALIGN).
  *   - There is no CPU fallback: a combination the kernels do not cover
  *     returns GL_ERR_UNSUPPORTED.
  *   - Calls are re-entrant from several host threads.
@@ -296,7 +296,8 @@ GL_API int gl_cartesian_dot_mx4(const gl_mx4* a0, const gl_mx4* a1, gl_ap* out, 
 
 /* The same with the left operand given as GL_F32 or GL_BF16 and rounded to MX4 by the call (a dense layer: activations
  * a0, weights a1 laid out once by gl_mx4_quantize).  The result does not depend on how many rows a0 has beyond the
- * order of the sums.  `workspace`: gl_dense_mx4_workspace() bytes, 1024-byte aligned, scratch. */
+ * order of the sums.  `workspace`: gl_dense_mx4_workspace() bytes, 1024-byte aligned, scratch: calls that can overlap on
+ * the GPU need one each. */
 GL_API int gl_dense_mx4(const gl_ap* a0, const gl_mx4* a1, gl_ap* out, uint32_t flags, void* workspace,
                         size_t workspace_bytes, void* stream);
 GL_API size_t gl_dense_mx4_workspace(const gl_ap* a0, const gl_mx4* a1);
@@ -328,8 +329,8 @@ GL_API size_t gl_cache4_bytes(const gl_cache4* cache);
 
 /* Rounds k and v, ((B, T, kv_heads),(head_dim)) GL_BF16, into the cache: token i of sequence b becomes its token
  * lengths[b] - T + i; those before token 0 (left padding of a ragged batch) are skipped.  token_pitch: elements between
- * successive tokens of k and of v, a multiple of 8 (0: dense), so that both may be parts of one projection.  Pages that
- * two sequences share may be read but not appended to. */
+ * successive tokens of k and of v, those of a sequence's end and the next one's start too, a multiple of 8 (0: dense), so
+ * that both may be parts of one projection.  Pages that two sequences share may be read but not appended to. */
 GL_API int gl_cache4_append(const gl_cache4* cache, const gl_ap* k, const gl_ap* v, int64_t token_pitch, const gl_pages* at,
                             void* stream);
 
@@ -341,7 +342,10 @@ GL_API int gl_cache4_read(const gl_cache4* cache, const gl_pages* at, gl_ap* k, 
  * sequence, sees the tokens up to and including itself and reads kv head h / (heads / kv_heads):
  *   out[b,i,h] = sum_t p_t V_t,  p = softmax_t(scale * q . K_t);  zeros for a row that sees nothing.
  * scale > 0 and finite; token_pitch as above; out is dense, GL_F32 or, with GL_OUT_BF16 in flags, GL_BF16.
- * Scores and softmax statistics are fp32.  `workspace`: gl_attend_cache4_workspace() bytes, 1024-byte aligned. */
+ * Scores, softmax statistics and sums are fp32.  The weights p are rounded to fp16 (bf16 where more than 32 rows share a
+ * kv head) when the result is bf16, and carried in two or three such terms when it is fp32.  Results repeat bit for bit.
+ * `workspace`: gl_attend_cache4_workspace() bytes, 1024-byte aligned, scratch: calls that can overlap on the GPU need one
+ * each. */
 GL_API int gl_attend_cache4(const gl_ap* q, int64_t token_pitch, const gl_cache4* cache, const gl_pages* at, float scale,
                             gl_ap* out, uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
 GL_API size_t gl_attend_cache4_workspace(const gl_ap* q, const gl_cache4* cache);

@@ -1,6 +1,7 @@
 """Run one workload of the table in `synth` a few times on cuda:0.
 
     python -m paper_2105_09377_b200.run_workload --workload conv3x3_56x56x64 --layout nhwc --iters 3
+    python -m paper_2105_09377_b200.run_workload --workload decoder4_8x128_1024 --iters 64
 
 Prints the mean time per call (CUDA events).  Meant for profilers and quick
 checks; the benchmark proper is bench.py.
@@ -160,8 +161,52 @@ def build_chain(cfg, layout: str, device, seed=None):
     return run, logits, len(steps)
 
 
+class Decoder4:
+    """`synth.Decoder4Case` on the device: weights rounded to MX4 once, pages and their table owned here, `step` for a
+    prompt or for single tokens.  (No normalisation layers: what it shows is how the 4-bit operators go together.)"""
+
+    def __init__(self, cfg, device, seed=None):
+        self.cfg = cfg
+        x, *weights = cfg.inputs(synth.config_seed(6) if seed is None else seed)
+        self.prompt = _bf16(x, device)
+        self.qkv, self.back, self.up, self.down = (gl.gl_mx4_quantize(gl.AccessPattern(_bf16(w, device), 1)) for w in weights)
+        per = -(-cfg.capacity // cfg.page_tokens)
+        self.cache = gl.cache4_empty(cfg.batch * per, cfg.kv_heads, cfg.page_tokens, cfg.head_dim, device)
+        self.table = torch.arange(cfg.batch * per, dtype=torch.int32, device=device).view(cfg.batch, per)
+        self.lengths = torch.zeros(cfg.batch, dtype=torch.int32, device=device)
+
+    def step(self, x):
+        """x bf16 [batch, tokens, width], the tokens that come next; returns every stage, the last one the result."""
+        cfg, flags = self.cfg, gl.GL_OUT_BF16
+        dense = lambda a, w, f=flags: gl.gl_dense_mx4(gl.AccessPattern(a, 2), w, flags=f).tensor
+        qkv = dense(x, self.qkv).view(x.shape[0], x.shape[1], -1, cfg.head_dim)
+        q, k, v = qkv.split([cfg.heads, cfg.kv_heads, cfg.kv_heads], 2)      # parts of one result, read where they are
+        self.lengths += x.shape[1]
+        gl.gl_cache4_append(self.cache, k, v, self.table, self.lengths)
+        seen = gl.gl_attend_cache4(gl.AccessPattern(q, 3), self.cache, self.table, self.lengths, flags=flags).tensor
+        y = dense(seen.view(x.shape), self.back)
+        hidden = dense(y, self.up, flags | gl.GL_EPILOGUE_RELU)
+        return {"qkv": qkv, "seen": seen, "y": y, "hidden": hidden, "out": dense(hidden, self.down)}
+
+
+def run_decoder4(cfg, device, tokens: int):
+    """The prompt, then `tokens` single tokens, each the layer's last result; returns us per token."""
+    layer = Decoder4(cfg, device)
+    x = layer.step(layer.prompt)["out"][:, -1:].contiguous()
+    e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    x = layer.step(x)["out"]
+    torch.cuda.synchronize()
+    e0.record()
+    for _ in range(tokens):
+        x = layer.step(x)["out"]
+    e1.record()
+    torch.cuda.synchronize()
+    return e0.elapsed_time(e1) * 1e3 / tokens
+
+
 def main():
     table = workloads()
+    table[synth.DECODER4.name] = synth.DECODER4
     ap = argparse.ArgumentParser()
     ap.add_argument("--workload", required=True, choices=sorted(table))
     ap.add_argument("--layout", default="nhwc", choices=["nhwc", "nchw", "rewritten"])
@@ -173,6 +218,14 @@ def main():
     args = ap.parse_args()
     device = torch.device("cuda", 0)
     torch.cuda.set_device(device)
+    if args.workload == synth.DECODER4.name:
+        cfg = synth.DECODER4
+        tokens = min(args.iters, cfg.capacity - cfg.prompt - 1)
+        us = run_decoder4(cfg, device, tokens)
+        status = gl.gl_poll_device_status()
+        print("%s: %.2f us per token of %d sequences (%d tokens after a prompt of %d), status %d"
+              % (cfg.name, us, cfg.batch, tokens, cfg.prompt, status))
+        return 0 if status == 0 else 1
     call, flops, nbytes = build_call(table[args.workload], args.layout, device, args.batch or None,
                                      (gl.GL_DOT_GENERAL_KERNEL if args.general else 0) | (gl.GL_OUT_BF16 if args.bf16_out else 0))
     call()

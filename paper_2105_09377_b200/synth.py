@@ -269,5 +269,35 @@ class ChainCase:
 CHAIN_STEM = ChainCase("chain_stem_32x224x224", 32, 224, 224, 64, 64, 8, 1000)
 
 
+@dataclass(frozen=True)
+class Decoder4Case:
+    """A layer that reads a sequence token by token, everything it keeps held in 4 bits: one dense layer to queries, keys
+    and values, the keys and values stored in pages, attention over them, a dense layer back, a dense layer to `hidden`
+    with relu and one back.  A prompt of `prompt` tokens per sequence first, then single tokens."""
+    name: str
+    batch: int
+    prompt: int
+    heads: int
+    kv_heads: int
+    head_dim: int
+    hidden: int
+    page_tokens: int
+    capacity: int
+
+    @property
+    def width(self):
+        return self.heads * self.head_dim
+
+    def inputs(self, seed: int):
+        """(prompt activations [batch, prompt, width], the weights of the four dense layers [outputs, inputs])."""
+        w, qkv = self.width, (self.heads + 2 * self.kv_heads) * self.head_dim
+        shapes = ((qkv, w), (w, w), (self.hidden, w), (w, self.hidden))
+        return (bf16_round(normal(seed, 1, (self.batch, self.prompt, w), 1.0)),) + tuple(
+            bf16_round(normal(seed, 2 + i, s, 1.0 / math.sqrt(s[1]))) for i, s in enumerate(shapes))
+
+
+DECODER4 = Decoder4Case("decoder4_8x128_1024", 8, 128, 16, 4, 64, 4096, 64, 512)
+
+
 def config_seed(config_index: int) -> int:
     return BASE_SEED + config_index

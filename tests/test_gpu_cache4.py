@@ -227,3 +227,39 @@ def test_long_sequences_on_another_stream(gl):
         got = gl.gl_attend_cache4(gl.AccessPattern(q, 3), cache, table, lengths, flags=gl.GL_OUT_BF16)
     side.synchronize()
     _check(gl, cache, table, lengths, k, v, q, lens, d ** -0.5, True, got=got.tensor)
+
+
+@pytest.mark.parametrize("heads,batch", [(1, 300), (40, 1200)])
+def test_more_sequences_than_threads(gl, heads, batch):
+    """The blocks find their place in rounds; every length from none to a few tiles."""
+    lens = [(7 * i) % 90 for i in range(batch)]
+    cache, table, lengths, k, v = _filled(gl, lens, 1, 64, 16)
+    q = _bf16(4, (batch, 1, heads, 64))
+    got = gl.gl_attend_cache4(gl.AccessPattern(q, 3), cache, table, lengths).tensor
+    some = list(range(0, 20)) + list(range(120, 140)) + list(range(batch - 20, batch))
+    at = torch.tensor(some)
+    _check(gl, cache, table, lengths, k[at], v[at], q[at], [lens[i] for i in some], 0.125, False, got=got[at])
+    assert not got[[i for i, n in enumerate(lens) if n == 0]].any()
+
+
+def test_prepared_calls_in_a_graph(gl):
+    lens, d = [50, 20], 64
+    cache, table, lengths, k, v = _filled(gl, lens, 1, d, 64)
+    q, k1, v1 = (_bf16(s, (2, 1, h, d)) for s, h in ((4, 2), (5, 1), (6, 1)))
+    out = gl.AccessPattern(torch.zeros(2, 1, 2, d, device="cuda"), 3)
+    calls = [gl.prepare_cache4_append(cache, k1, v1, table, lengths),
+             gl.prepare_attend_cache4(gl.AccessPattern(q, 3), cache, table, lengths, out)]
+    lengths += 1                       # both are read on the device: the graph goes on with the lengths it finds
+    for call in calls:
+        call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for call in calls:
+            call()
+    lengths += 1
+    k1.copy_(_bf16(7, (2, 1, 1, d)))
+    graph.replay()
+    first = torch.cat([k, _bf16(5, (2, 1, 1, d)), k1], 1), torch.cat([v, v1, v1], 1)
+    # (left-padded: the padding moves along)
+    _check(gl, cache, table, lengths, first[0], first[1], q, [52, 22], d ** -0.5, False, got=out.tensor)
