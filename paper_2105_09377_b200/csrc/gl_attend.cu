@@ -232,6 +232,7 @@ struct AttendParams {
   int grid;
   int min_share;         // list entries that a block takes at least
   int lead;              // what a segment costs beyond its tiles, in tiles (see Walk)
+  int alone;             // a block per segment, no list, nothing to join: caches of a few tiles
   float scale_log2;      // softmax scale * log2(e)
   int out_bf16;
 };
@@ -302,6 +303,20 @@ struct Walk {
   // thread each and scanned.  (One thread that walks along 64 sequences takes 3 us.)
   template <int THREADS>
   __device__ __forceinline__ void start(const AttendParams& p, int block, int64_t* scratch) {
+    if (p.alone) {
+      rb = block % p.row_blocks;
+      h = block / p.row_blocks;
+      b = h / p.c.kv_heads;
+      h -= b * p.c.kv_heads;
+      len = clamped_length(p.c, b);
+      seen = seen_by(p, len, rb);
+      t0 = 0;
+      t1 = n_seg = seen_tiles(p, len, rb);
+      at = 0;
+      end = n_seg ? 1 : 0;
+      __syncthreads();
+      return;
+    }
     int64_t all, before;
     sum_entries<THREADS>(p, 0, &before, &all, scratch);
     const int64_t share = block_share(p, all);
@@ -341,6 +356,7 @@ struct Walk {
     per_head = found[2];
   }
   __device__ __forceinline__ bool next(const AttendParams& p) {
+    if (p.alone) return at++ < end;
     while (at < end) {
       while (seg0 + per_head * p.c.kv_heads <= at) {
         if (b + 1 >= p.c.batch) return false;   // (only if lengths changed under the kernel)
@@ -385,6 +401,19 @@ __device__ __forceinline__ int64_t out_row(const AttendParams& p, int b, int h, 
 __device__ __forceinline__ const uint16_t* q_row(const AttendParams& p, int b, int h, int row, int D) {
   const int t = row_token(p, row);
   return p.q + (static_cast<int64_t>(b) * p.T + t) * p.q_pitch + (static_cast<int64_t>(h) * p.group + row - t * p.group) * D;
+}
+
+// Zeros for a segment without a tile, by its own block (blocks that share a list leave that to the joining kernel).
+template <int THREADS>
+__device__ __forceinline__ void store_empty(const AttendParams& p, const Walk& w, int D) {
+  if (!p.alone || w.n_seg) return;
+  const int rows = min(p.rows - w.rb * p.R, p.R);
+  for (int e = threadIdx.x; e < rows * (D / 4); e += THREADS) {
+    const int r = e / (D / 4), d = e % (D / 4) * 4;
+    const int64_t to = out_row(p, w.b, w.h, w.rb * p.R + r, D) + d;
+    if (p.out_bf16) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + to) = make_uint2(0, 0);
+    else *reinterpret_cast<float4*>(static_cast<float*>(p.out) + to) = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
 }
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -540,6 +569,7 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
   pdl_launch_dependents();
   Walk w;
   w.start<kWarps * 32>(p, blockIdx.x, scratch);   // (its barriers also publish the ones set up above)
+  store_empty<kWarps * 32>(p, w, D);
 
   const uint32_t my_ring = smem_u32(smem) + warp * kStagesAt * Cfg::kStage;
   const uint32_t my_bar = smem_u32(bars + warp * kStagesAt);
@@ -1218,6 +1248,8 @@ AttKernel many_kernel(bool f32) {
   return {attend_many<NB, 1>, ManyCfg<NB, 1>::kSmem, ManyCfg<NB, 1>::kThreads, ManyCfg<NB, 1>::kRows, ManyCfg<NB, 1>::TT, 1, 1, 1};
 }
 
+constexpr int kAloneTiles = 4;
+
 // Up to 32 rows that share a kv head: 8, 16 or 32 of them per warp tile (256-wide heads: 16, two items for more);
 // more rows: 128 or 256 per block on tcgen05.
 AttKernel pick_kernel(int64_t rows, int d, bool f32) {
@@ -1339,8 +1371,15 @@ int gl_attend_cache4(const gl_ap* q, int64_t token_pitch, const gl_cache4* cache
   // (no more than a segment can have: a block that takes several short segments takes them one after the other)
   p.lead = k.lead;
   p.min_share = k.lead + std::min<int>(k.min_share, (p.c.capacity + k.tile - 1) / k.tile);
-  if (launch_pdl(k.fn, dim3(static_cast<unsigned>(p.grid)), dim3(static_cast<unsigned>(k.threads)), static_cast<size_t>(k.smem), st, 1, p) != cudaSuccess)
+  // A cache of at most four tiles per sequence: a block per segment, one launch (8 sequences of 100 tokens, 8 heads: 12.3 us
+  // with the list and the joining kernel, 7.8 us without).  Longer ones have warps with several tiles, which the list
+  // spreads over the blocks.
+  p.alone = p.c.capacity <= kAloneTiles * k.tile ? 1 : 0;
+  const int64_t blocks = p.alone ? segments : p.grid;
+  if (launch_pdl(k.fn, dim3(static_cast<unsigned>(blocks)), dim3(static_cast<unsigned>(k.threads)), static_cast<size_t>(k.smem), st, 1, p) !=
+      cudaSuccess)
     return GL_ERR_CUDA;
+  if (p.alone) return GL_OK;
   JoinShape js = {kJoinWarps, 1};
   int64_t live = std::min<int64_t>(rows, k.rows), row_groups = live;
   if (segments * live > 4 * num_sms()) {   // (four blocks per SM at once)

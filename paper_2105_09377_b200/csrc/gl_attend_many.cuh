@@ -184,6 +184,7 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
   tc_fence_before();
   Walk w;
   w.start<Cfg::kThreads>(p, blockIdx.x, scratch);   // (its barriers also publish the set-up above)
+  store_empty<Cfg::kThreads>(p, w, D);
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   uint32_t it = 0;     // tiles so far, the same for every role

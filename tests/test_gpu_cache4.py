@@ -108,6 +108,10 @@ ATTEND = [
     ([260, 64, 65], 33, 2, 2, 256, 128),
     ([3000], 70, 8, 1, 128, 16),             # 560 rows of one kv head over many blocks
     ([900, 1100], 300, 3, 3, 128, 64),
+    ([0, 256, 3, 129], 1, 6, 2, 64, 256),    # at most 256 tokens: a block per sequence and head
+    ([128, 0, 77], 2, 3, 3, 256, 128),       # (128 of them for 256-wide heads)
+    ([512, 1, 0, 400], 35, 4, 2, 128, 512),  # (512 for more than 32 rows)
+    ([0, 257], 1, 6, 2, 64, 16),
 ]
 
 
