@@ -581,7 +581,7 @@ dot_mx4(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUten
           tc_fence_before();
           __syncwarp();
           if (lane == 0) {
-            if (CTAS == 2) mbar_arrive_cluster(map_to_cta(bar_tempty + 8 * acc, 0));
+            if (CTAS == 2) mbar_arrive_remote(map_to_cta(bar_tempty + 8 * acc, 0));
             else mbar_arrive(bar_tempty + 8 * acc);
           }
         }
