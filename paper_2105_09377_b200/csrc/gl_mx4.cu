@@ -312,7 +312,7 @@ int launch_quantize(const gl_ap& in, const Mx4View& v, void* codes, void* scale,
 //
 // What bounds it at size is what bounds the bf16 product: operands from L2 to the SMs.  A 256 x 256 tile on a pair of SMs
 // needs 64 bytes per cycle and SM, a 128 x 128 tile on one SM twice that.  16384 x 8192 x 8192 with bf16 results: 532 us
-// on single SMs, 357-370 us on pairs, 6.0 PFLOP/s; 4096^3 30 us (fp32 results 36 us: 67 MB to write).  A 256-wide
+// on single SMs, 360 us on pairs, 6.1 PFLOP/s; 4096^3 28 us (fp32 results 34 us: 67 MB to write).  A 256-wide
 // accumulator takes half the tensor memory, so two of them and the scales overlap in 24 columns, which the epilogue empties
 // first; the next tile's products wait for that only.
 
