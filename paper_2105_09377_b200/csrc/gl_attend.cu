@@ -1,11 +1,5 @@
 // Pages of 4-bit keys and values (gl_cache4) and the attention that reads them.
-//
-// Group of 16 tokens of one kv head (17 * D bytes, one bulk copy): codes of K, scales of K, codes of V, scales of V.
-// Inside a token's row of codes the order is the one the tensor-core fragments want, so that a thread reads all it
-// needs of a token in one access and converts whole 32-bit words:
-//   K: word (j, b) = dims 32 b + 8 j .. + 7 of block b, at word j * NB + b           (NB = D / 32 blocks)
-//   V: half word (g, b) = dims 32 b + 4 g .. + 3, at half word (g ^ s) * NB + b, s = 4 for tokens with bit 1 set
-// (the exclusive or spreads the four tokens that a warp reads together over all banks).
+// The order of a page's bytes and where a token lies: gl_cache4.cuh.
 #include <cuda.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -13,6 +7,7 @@
 #include <algorithm>
 #include <cstring>
 
+#include "gl_cache4.cuh"
 #include "gl_internal.h"
 #include "gl_launch.cuh"
 #include "gl_mx4.cuh"
@@ -23,26 +18,6 @@ using namespace gl;
 
 namespace {
 
-constexpr int kGroup = 16;   // tokens per group
-
-__host__ __device__ constexpr int group_bytes(int d) { return 17 * d; }
-__host__ __device__ constexpr int k_scales_at(int d) { return 8 * d; }
-__host__ __device__ constexpr int v_codes_at(int d) { return 8 * d + d / 2; }
-__host__ __device__ constexpr int v_scales_at(int d) { return 16 * d + d / 2; }
-
-struct CacheView {
-  uint8_t* data;
-  const int32_t* table;
-  const int32_t* lengths;
-  int64_t pages;
-  int64_t head_stride, page_stride;   // bytes
-  int kv_heads, page_tokens, batch, width;
-  int capacity;                       // tokens a sequence can have: width * page_tokens
-  FastDiv div_page;
-};
-
-__device__ __forceinline__ int clamped_length(const CacheView& c, int b) { return min(max(c.lengths[b], 0), c.capacity); }
-
 // ------------------------------------------------------------------------
 // Storing and reading back
 // ------------------------------------------------------------------------
@@ -51,48 +26,6 @@ __device__ __forceinline__ int clamped_length(const CacheView& c, int b) { retur
 // (8, 16 or 32, inside a warp) share a token and head.  U items per thread, 256 apart, are requested before the first is
 // used.  What bounds both kernels are the instructions that find an item's place: K and V share them (apart, 14 us each
 // way for 8192 tokens of 8 heads of 128).
-struct TokensParams {
-  CacheView c;
-  int T, D;
-  int64_t pitch;         // elements between tokens of the dense side
-  uint32_t items;        // batch * T * kv_heads * (D / 8)
-  FastDiv div_row, div_heads, div_T;
-};
-
-struct TokenAt {
-  int w;                 // which eight dims
-  int tok;               // place in its group
-  int64_t dense;         // element of the dense side
-  uint8_t* group;        // null: not in the cache
-};
-
-__device__ __forceinline__ TokenAt token_at(const TokensParams& p, uint32_t item) {
-  uint32_t row, w, token, h, b, i;
-  p.div_row.divmod(item, row, w);
-  p.div_heads.divmod(row, token, h);
-  p.div_T.divmod(token, b, i);
-  TokenAt t;
-  t.w = static_cast<int>(w);
-  t.dense = static_cast<int64_t>(token) * p.pitch + static_cast<int64_t>(h) * p.D + w * 8u;
-  t.group = nullptr;
-  t.tok = 0;
-  const int pos = clamped_length(p.c, static_cast<int>(b)) - p.T + static_cast<int>(i);
-  if (item < p.items && pos >= 0) {
-    uint32_t slot, in_page;
-    p.c.div_page.divmod(static_cast<uint32_t>(pos), slot, in_page);
-    const int page = p.c.table[static_cast<int64_t>(b) * p.c.width + slot];
-    t.tok = static_cast<int>(in_page % kGroup);
-    if (page >= 0 && page < p.c.pages)
-      t.group = p.c.data + page * p.c.page_stride + h * p.c.head_stride + static_cast<int64_t>(in_page / kGroup) * group_bytes(p.D);
-  }
-  return t;
-}
-
-// The thread of dims 32 b + 8 j .. + 7 stores, of V, the four bytes that hold dims 4 g .. + 3, g = 2 j + (b & 1), of the blocks
-// b & ~1 and b | 1: offset in the token's row of codes.
-__device__ __forceinline__ int v_offset(int NB, int b, int j, int tok) {
-  return (((2 * j + (b & 1)) ^ ((tok & 2) ? 4 : 0)) * NB + (b & ~1)) * 2;
-}
 
 // Scale exponent and codes of a thread's eight values, four neighbouring threads a block.  (Every thread of the warp.)
 __device__ __forceinline__ void quantize8(const uint4& raw, uint32_t& e, uint32_t& word) {

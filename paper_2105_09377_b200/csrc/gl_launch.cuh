@@ -27,8 +27,14 @@ struct FastDiv {
     mul = pw2 ? static_cast<uint32_t>(((1ull << (31 + pw2)) + divisor - 1) / divisor) : 0u;
     shift = pw2 ? pw2 - 1 : 0u;
   }
-  __device__ __forceinline__ uint32_t div(uint32_t n) const { return mul ? (__umulhi(n, mul) >> shift) : n; }
-  __device__ __forceinline__ void divmod(uint32_t n, uint32_t& q, uint32_t& r) const { q = div(n); r = n - q * d; }
+  __host__ __device__ __forceinline__ uint32_t div(uint32_t n) const {
+#ifdef __CUDA_ARCH__
+    return mul ? (__umulhi(n, mul) >> shift) : n;
+#else
+    return mul ? static_cast<uint32_t>((static_cast<uint64_t>(n) * mul) >> 32) >> shift : n;
+#endif
+  }
+  __host__ __device__ __forceinline__ void divmod(uint32_t n, uint32_t& q, uint32_t& r) const { q = div(n); r = n - q * d; }
 };
 inline FastDiv make_fastdiv(int64_t d) {
   FastDiv fd;
