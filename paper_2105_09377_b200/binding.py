@@ -630,6 +630,9 @@ def _tokens_struct(t: torch.Tensor):
     dense_heads = (d == 1 or t.stride(3) == 1) and (h == 1 or t.stride(2) == d)
     if not dense_heads or (b > 1 and n > 1 and t.stride(0) != n * pitch):
         raise ValueError("tokens are [batch, tokens, heads, head_dim] with dense heads and one distance between tokens")
+    if b * n > 1 and pitch < h * d:
+        # (a broadcast view has a distance of 0, which the library takes for `dense`)
+        raise ValueError("tokens overlap: a broadcast or overlapping view has to be made contiguous first")
     return _meta(tuple(t.shape), 3, _DTYPES[t.dtype], t.data_ptr()), pitch
 
 
