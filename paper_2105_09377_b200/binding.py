@@ -484,6 +484,15 @@ def gl_compute_relu(a: AccessPattern, out: Optional[AccessPattern] = None, strea
 
 # ---- operands held in 4 bits ----
 
+def _on_gpu(*tensors):
+    """The kernels read these addresses themselves: a tensor on the host (lengths or a page table made there, say) would be
+    a fault of the GPU."""
+    device = tensors[0].device
+    for t in tensors:
+        if t is not None and not (t.is_cuda and t.device == device):
+            raise ValueError("tensors have to be on one GPU: %s and %s" % (device, t.device))
+
+
 @dataclass
 class Mx4:
     """A pattern held in 4 bits: E2M1 codes (two a byte) and one E8M0 scale per 32 values of an item."""
@@ -531,6 +540,7 @@ def gl_mx4_quantize(a: AccessPattern, out: Optional[Mx4] = None, stream=None) ->
     sa = _struct(a)
     if out is None:
         out = mx4_empty(tuple(a.tensor.shape), a.access_ndim, a.tensor.device)
+    _on_gpu(a.tensor, out.data, out.scale)
     _check(LIB.gl_mx4_quantize(ctypes.byref(sa), ctypes.byref(_mx4_struct(out)), _stream(stream)), "gl_mx4_quantize")
     return out
 
@@ -538,6 +548,7 @@ def gl_mx4_quantize(a: AccessPattern, out: Optional[Mx4] = None, stream=None) ->
 def gl_mx4_dequantize(m: Mx4, out: Optional[AccessPattern] = None, stream=None) -> AccessPattern:
     if out is None:
         out = AccessPattern(torch.empty(m.dims, dtype=torch.float32, device=m.data.device), m.access_ndim)
+    _on_gpu(m.data, m.scale, out.tensor)
     so = _struct(out)
     _check(LIB.gl_mx4_dequantize(ctypes.byref(_mx4_struct(m)), ctypes.byref(so), _stream(stream)), "gl_mx4_dequantize")
     return out
@@ -552,6 +563,7 @@ def _product_out(access0, access1, flags, device) -> AccessPattern:
 def gl_cartesian_dot_mx4(a0: Mx4, a1: Mx4, out: Optional[AccessPattern] = None, flags: int = 0, stream=None) -> AccessPattern:
     if out is None:
         out = _product_out(a0.shape[0], a1.shape[0], flags, a0.data.device)
+    _on_gpu(a0.data, a0.scale, a1.data, a1.scale, out.tensor)
     so = _struct(out)
     _check(LIB.gl_cartesian_dot_mx4(ctypes.byref(_mx4_struct(a0)), ctypes.byref(_mx4_struct(a1)), ctypes.byref(so), flags,
                                     _stream(stream)), "gl_cartesian_dot_mx4")
@@ -572,6 +584,7 @@ def gl_dense_mx4(a0: AccessPattern, a1: Mx4, out: Optional[AccessPattern] = None
         out = _product_out(a0.access_shape, a1.shape[0], flags, a0.tensor.device)
     if workspace is None:
         workspace = _scratch(gl_dense_mx4_workspace(a0, a1), a0.tensor.device)
+    _on_gpu(a0.tensor, a1.data, a1.scale, out.tensor, workspace)
     s0, so = _struct(a0), _struct(out)
     _check(LIB.gl_dense_mx4(ctypes.byref(s0), ctypes.byref(_mx4_struct(a1)), ctypes.byref(so), flags, *_ws(workspace),
                             _stream(stream)), "gl_dense_mx4")
@@ -637,6 +650,7 @@ def _tokens_struct(t: torch.Tensor):
 
 
 def _append_args(cache: Cache4, k: torch.Tensor, v: torch.Tensor, page_table, lengths):
+    _on_gpu(k, v, cache.data, page_table, lengths)
     sk, pk = _tokens_struct(k)
     sv, pv = _tokens_struct(v)
     if pk != pv:
@@ -651,6 +665,7 @@ def gl_cache4_append(cache: Cache4, k: torch.Tensor, v: torch.Tensor, page_table
 
 
 def _read_args(cache: Cache4, k: torch.Tensor, v: torch.Tensor, page_table, lengths):
+    _on_gpu(k, v, cache.data, page_table, lengths)
     return (ctypes.byref(_cache4_struct(cache)), ctypes.byref(_pages_struct(page_table, lengths)),
             ctypes.byref(_struct(AccessPattern(k, 3))), ctypes.byref(_struct(AccessPattern(v, 3))))
 
@@ -668,6 +683,7 @@ def gl_attend_cache4_workspace(q: AccessPattern, cache: Cache4) -> int:
 
 
 def _attend_args(q, cache, page_table, lengths, out, scale, flags, workspace):
+    _on_gpu(q.tensor, cache.data, page_table, lengths, out.tensor, workspace)
     sq, pitch = _tokens_struct(q.tensor)
     return (ctypes.byref(sq), pitch, ctypes.byref(_cache4_struct(cache)), ctypes.byref(_pages_struct(page_table, lengths)),
             float(scale), ctypes.byref(_struct(out)), flags, *_ws(workspace))
@@ -762,14 +778,17 @@ def prepare_compute_relu(a: AccessPattern, out: AccessPattern) -> Prepared:
 
 
 def prepare_mx4_quantize(a: AccessPattern, out: Mx4) -> Prepared:
+    _on_gpu(a.tensor, out.data, out.scale)
     return Prepared(LIB.gl_mx4_quantize, (ctypes.byref(_struct(a)), ctypes.byref(_mx4_struct(out))), (a, out))
 
 
 def prepare_mx4_dequantize(m: Mx4, out: AccessPattern) -> Prepared:
+    _on_gpu(m.data, m.scale, out.tensor)
     return Prepared(LIB.gl_mx4_dequantize, (ctypes.byref(_mx4_struct(m)), ctypes.byref(_struct(out))), (m, out))
 
 
 def prepare_cartesian_dot_mx4(a0: Mx4, a1: Mx4, out: AccessPattern, flags: int = 0) -> Prepared:
+    _on_gpu(a0.data, a0.scale, a1.data, a1.scale, out.tensor)
     return Prepared(LIB.gl_cartesian_dot_mx4, (ctypes.byref(_mx4_struct(a0)), ctypes.byref(_mx4_struct(a1)),
                                                ctypes.byref(_struct(out)), flags), (a0, a1, out))
 
@@ -778,6 +797,7 @@ def prepare_dense_mx4(a0: AccessPattern, a1: Mx4, out: AccessPattern, flags: int
                       workspace: Optional[torch.Tensor] = None) -> Prepared:
     if workspace is None:
         workspace = _scratch(gl_dense_mx4_workspace(a0, a1), a0.tensor.device)
+    _on_gpu(a0.tensor, a1.data, a1.scale, out.tensor, workspace)
     return Prepared(LIB.gl_dense_mx4, (ctypes.byref(_struct(a0)), ctypes.byref(_mx4_struct(a1)), ctypes.byref(_struct(out)), flags,
                                        *_ws(workspace)), (a0, a1, out, workspace))
 
