@@ -179,14 +179,15 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  pdl_wait();
-  pdl_launch_dependents();
   tc_fence_before();
-  Walk w;
-  w.start<Cfg::kThreads>(p, blockIdx.x, scratch);   // (its barriers also publish the set-up above)
-  store_empty<Cfg::kThreads>(p, w, D);
+  __syncthreads();   // tensor memory is there before the next kernel, which may want some and wait for this one, can start
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  pdl_wait();
+  pdl_launch_dependents();
+  Walk w;
+  w.start<Cfg::kThreads>(p, blockIdx.x, scratch);
+  store_empty<Cfg::kThreads>(p, w, D);
   uint32_t it = 0;     // tiles so far, the same for every role
   uint32_t item = 0;
   bool ok = true;

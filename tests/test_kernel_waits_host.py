@@ -1,0 +1,35 @@
+"""Reads the kernel sources for an order on which it depends that a kernel cannot wait for ever."""
+import os
+import re
+
+import pytest
+
+from paper_2105_09377_b200 import build
+
+FILES = sorted(f for f in os.listdir(build.CSRC) if f.endswith((".cu", ".cuh")))
+
+
+def _code(name):
+    text = open(os.path.join(build.CSRC, name)).read()
+    return re.sub(r"//[^\n]*", "", text)
+
+
+def _kernels(text):
+    """The text of every kernel, from its __global__ to the next one."""
+    at = [m.start() for m in re.finditer(r"__global__", text)]
+    return [text[a:b] for a, b in zip(at, at[1:] + [len(text)])]
+
+
+@pytest.mark.parametrize("name", FILES)
+def test_tensor_memory_is_allocated_before_the_next_kernel_may_start(name):
+    """A kernel of the same stream that starts early allocates tensor memory too, and gives it back only after this one has
+    ended: a block of this one that still waits for its own would wait for ever.  One thread's launch_dependents speaks
+    for its block, so a barrier of the whole block has to lie between."""
+    for kernel in _kernels(_code(name)):
+        alloc = kernel.find("tcgen05.alloc")
+        if alloc < 0:
+            continue
+        start = kernel.find("pdl_launch_dependents()", alloc)
+        assert start > 0
+        between = kernel[alloc:start]
+        assert "__syncthreads()" in between or "cluster_sync_all()" in between, kernel[:200]
