@@ -151,12 +151,13 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
   const uint32_t bar = smem_u32(bars);
   const uint32_t b_kfull = bar, b_kempty = bar + 16, b_vfull = bar + 32, b_vempty = bar + 48, b_q = bar + 64, b_s = bar + 80,
                  b_p = bar + 96, b_o = bar + 112;                // two each
+  const uint32_t b_item = bar + 280;                             // one
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 16);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile uint32_t* have = reinterpret_cast<volatile uint32_t*>(tmem_slot + 2);   // [4] groups of a tile that have a page
   int* nan_from = reinterpret_cast<int*>(tmem_slot + 6);                           // [4][NB] first token whose V block is NaN
   int64_t* scratch = reinterpret_cast<int64_t*>(tail + 288);                       // [2 * kWarps + 4]
-  static_assert(288 + 16 * Cfg::kWarps + 32 <= 640 && 128 + 24 + 16 * 8 <= 288, "tail");
+  static_assert(288 + 16 * Cfg::kWarps + 32 <= 640 && 128 + 24 + 16 * 8 <= 280, "tail");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   constexpr int kWiden = 4 * MT, kMma = kWiden + Cfg::kWidenWarps;
 
@@ -171,6 +172,7 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
       mbar_init(b_p + 8 * i, 4);
       mbar_init(b_o + 8 * i, 1);
     }
+    mbar_init(b_item, Cfg::kWidenWarps);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -371,8 +373,11 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
     constexpr int kItems = TT / 64;
     const int dw = warp - kWiden, j = lane >> 3;
     for (; ok && w.next(p); ++item) {
+      // the item's NaN positions are cleared before any warp of this role notes one
       if (dw == 0 && lane < NB) nan_from[(item & 3u) * NB + lane] = INT32_MAX;
-      asm volatile("bar.sync 1, %0;" ::"n"(32 * Cfg::kWidenWarps) : "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(b_item);
+      if (!mbar_wait(b_item, item & 1u, abort_flag)) { ok = false; break; }
       Held<NB, kItems> hk[2], hv[2];
       uint32_t tile_have[2];
       int32_t page = -1;        // of group `lane` of the tile to be asked for next

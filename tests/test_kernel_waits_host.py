@@ -1,4 +1,4 @@
-"""Reads the kernel sources for an order on which it depends that a kernel cannot wait for ever."""
+"""Reads the kernel sources for two orders on which it depends that a kernel cannot wait for ever."""
 import os
 import re
 
@@ -33,3 +33,11 @@ def test_tensor_memory_is_allocated_before_the_next_kernel_may_start(name):
         assert start > 0
         between = kernel[alloc:start]
         assert "__syncthreads()" in between or "cluster_sync_all()" in between, kernel[:200]
+
+
+@pytest.mark.parametrize("name", FILES)
+def test_roles_wait_for_one_another_with_a_limit(name):
+    """A role that gives up after a bounded wait leaves for the end of the kernel.  A named barrier has no limit: the others
+    would wait there for a warp that has left."""
+    code = _code(name)
+    assert not re.search(r"\b(bar|barrier)\.(cta\.)?sync\b|__barrier_sync|named_barrier", code)
