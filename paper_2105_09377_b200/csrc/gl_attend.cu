@@ -515,7 +515,9 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
     const int b = w.b, h = w.h, rb = w.rb, t0 = w.t0, t1 = w.t1, len = w.len, seen = w.seen;
 
     // ---- ring of this warp: tiles t0 + warp, + kWarps, ...
-    __syncthreads();   // the previous segment's fragments and joined results (which lie in the rings) are read
+    // The previous segment's fragments and joined results (which lie in the rings) are read.  A block that gave up ends here:
+    // it cannot use a barrier again whose copies are still out.
+    if (__syncthreads_or(!ok)) break;
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     constexpr int kGroupsAt = kTileTok / kGroup;
     constexpr uint32_t kAllThere = (1u << kGroupsAt) - 1u;

@@ -558,6 +558,10 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
     }
   }
   __syncwarp();
+  if (*abort_flag) {   // a block that gave up lets its matrix instructions in flight end before it leaves
+    const uint64_t t0 = global_timer();
+    while (global_timer() - t0 < 20000000ull) { }
+  }
   tc_fence_before();
   __syncthreads();
   if (warp == kMma) {

@@ -41,3 +41,18 @@ def test_roles_wait_for_one_another_with_a_limit(name):
     would wait there for a warp that has left."""
     code = _code(name)
     assert not re.search(r"\b(bar|barrier)\.(cta\.)?sync\b|__barrier_sync|named_barrier", code)
+
+
+@pytest.mark.parametrize("name", FILES)
+def test_a_block_that_gave_up_lets_its_work_land(name):
+    """Copies and matrix instructions in flight still write to the block's memory: it may neither leave nor give its tensor
+    memory back right away.  Nor may it arm a barrier again whose copies never came."""
+    for kernel in _kernels(_code(name)):
+        if not re.search(r"abort_flag\s*=\s*reinterpret_cast", kernel) or "bounded_wait_selftest" in kernel[:200]:
+            continue
+        given_up = re.search(r"if \([^\n]*\*abort_flag\)", kernel)
+        assert given_up and "global_timer()" in kernel[given_up.end():given_up.end() + 200], kernel[:200]
+        dealloc = kernel.find("tcgen05.dealloc")
+        assert dealloc < 0 or given_up.end() < dealloc
+        if "attend_cache4(" in kernel[:120]:      # (the one kernel that fills its rings again after joining its warps)
+            assert "if (__syncthreads_or(!ok)) break;" in kernel
