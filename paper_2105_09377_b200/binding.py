@@ -214,9 +214,30 @@ def _struct(a: AccessPattern) -> GlAp:
     return _meta(tuple(t.shape), a.access_ndim, _DTYPES[t.dtype], t.data_ptr())
 
 
-def _alloc(meta: GlAp, device) -> AccessPattern:
+def _stream_object(stream):
+    """`stream` as torch knows it: a torch stream, or the address of one of another library (0: the default stream)."""
+    if hasattr(stream, "cuda_stream"):
+        return stream
+    return torch.cuda.ExternalStream(int(stream)) if int(stream) else torch.cuda.default_stream()
+
+
+def _empty(shape, dtype, device, stream) -> torch.Tensor:
+    """Storage that the call on `stream` (None: the current one) writes.  torch hands a block out again as soon as its tensor
+    is gone, in the order of the stream that it was taken on: so it is taken on the stream that the call runs on, and scratch
+    may be dropped when the call returns."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(_stream_object(stream)):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _scratch(need: int, device, stream=None) -> Optional[torch.Tensor]:
+    return _empty(need + 1024, torch.uint8, device, stream) if need else None
+
+
+def _alloc(meta: GlAp, device, stream=None) -> AccessPattern:
     shape = tuple(meta.shape[i] for i in range(meta.ndim))
-    return AccessPattern(torch.empty(shape, dtype=_TORCH[meta.dtype], device=device), meta.access_ndim)
+    return AccessPattern(_empty(shape, _TORCH[meta.dtype], device, stream), meta.access_ndim)
 
 
 def _stream(stream) -> int:
@@ -312,7 +333,7 @@ def gl_access_windows(a: AccessPattern, w: GlWindows, out: Optional[AccessPatter
     if out is None:
         m = GlAp()
         _check(LIB.gl_shape_windows(ctypes.byref(sa), ctypes.byref(w), ctypes.byref(m)), "gl_shape_windows")
-        out = _alloc(m, a.tensor.device)
+        out = _alloc(m, a.tensor.device, stream)
     so = _struct(out)
     _check(LIB.gl_access_windows(ctypes.byref(sa), ctypes.byref(w), ctypes.byref(so), _stream(stream)), "gl_access_windows")
     return out
@@ -332,7 +353,7 @@ def gl_access_transpose(a: AccessPattern, perm, out: Optional[AccessPattern] = N
     if out is None:
         m = GlAp()
         _check(LIB.gl_shape_transpose(ctypes.byref(sa), arr, ctypes.byref(m)), "gl_shape_transpose")
-        out = _alloc(m, a.tensor.device)
+        out = _alloc(m, a.tensor.device, stream)
     so = _struct(out)
     _check(LIB.gl_access_transpose(ctypes.byref(sa), arr, ctypes.byref(so), _stream(stream)), "gl_access_transpose")
     return out
@@ -344,7 +365,7 @@ def gl_access_pad(a: AccessPattern, dim: int, lo: int, hi: int, pad_kind=GL_PAD_
     if out is None:
         m = GlAp()
         _check(LIB.gl_shape_pad(ctypes.byref(sa), dim, lo, hi, ctypes.byref(m)), "gl_shape_pad")
-        out = _alloc(m, a.tensor.device)
+        out = _alloc(m, a.tensor.device, stream)
     so = _struct(out)
     _check(LIB.gl_access_pad(ctypes.byref(sa), dim, lo, hi, pad_kind, ctypes.byref(so), _stream(stream)), "gl_access_pad")
     return out
@@ -367,11 +388,11 @@ def gl_cartesian_dot(a0: AccessPattern, w: Optional[GlWindows], a1: AccessPatter
                    "gl_shape_cartesian_dot")
         if flags & GL_OUT_BF16:
             m.dtype = GL_BF16
-        out = _alloc(m, a0.tensor.device)
+        out = _alloc(m, a0.tensor.device, stream)
     if workspace is None:
         need = int(LIB.gl_cartesian_dot_workspace(ctypes.byref(s0), _wptr(w), ctypes.byref(s1), flags))
         if need:
-            workspace = torch.empty(need + 1024, dtype=torch.uint8, device=a0.tensor.device)
+            workspace = _scratch(need, a0.tensor.device, stream)
     ws_ptr, ws_bytes = 0, 0
     if workspace is not None:
         ws_ptr = (workspace.data_ptr() + 1023) // 1024 * 1024
@@ -403,7 +424,7 @@ def gl_compute_reduce_max(a: AccessPattern, w: Optional[GlWindows], out: Optiona
     if out is None:
         m = GlAp()
         _check(LIB.gl_shape_reduce_max(ctypes.byref(sa), _wptr(w), ctypes.byref(m)), "gl_shape_reduce_max")
-        out = _alloc(m, a.tensor.device)
+        out = _alloc(m, a.tensor.device, stream)
     so = _struct(out)
     _check(LIB.gl_compute_reduce_max(ctypes.byref(sa), _wptr(w), ctypes.byref(so), _stream(stream)), "gl_compute_reduce_max")
     return out
@@ -415,7 +436,7 @@ def gl_access_slice(a: AccessPattern, dim: int, lo: int, hi: int, out: Optional[
     if out is None:
         m = GlAp()
         _check(LIB.gl_shape_slice(ctypes.byref(sa), dim, lo, hi, ctypes.byref(m)), "gl_shape_slice")
-        out = _alloc(m, a.tensor.device)
+        out = _alloc(m, a.tensor.device, stream)
     so = _struct(out)
     _check(LIB.gl_access_slice(ctypes.byref(sa), dim, lo, hi, ctypes.byref(so), _stream(stream)), "gl_access_slice")
     return out
@@ -427,7 +448,7 @@ def gl_access_concat(a: AccessPattern, b: AccessPattern, dim: int, out: Optional
     if out is None:
         m = GlAp()
         _check(LIB.gl_shape_concat(ctypes.byref(sa), ctypes.byref(sb), dim, ctypes.byref(m)), "gl_shape_concat")
-        out = _alloc(m, a.tensor.device)
+        out = _alloc(m, a.tensor.device, stream)
     so = _struct(out)
     _check(LIB.gl_access_concat(ctypes.byref(sa), ctypes.byref(sb), dim, ctypes.byref(so), _stream(stream)),
            "gl_access_concat")
@@ -439,7 +460,7 @@ def gl_access_pair(a: AccessPattern, b: AccessPattern, out: Optional[AccessPatte
     if out is None:
         m = GlAp()
         _check(LIB.gl_shape_pair(ctypes.byref(sa), ctypes.byref(sb), ctypes.byref(m)), "gl_shape_pair")
-        out = _alloc(m, a.tensor.device)
+        out = _alloc(m, a.tensor.device, stream)
     so = _struct(out)
     _check(LIB.gl_access_pair(ctypes.byref(sa), ctypes.byref(sb), ctypes.byref(so), _stream(stream)), "gl_access_pair")
     return out
@@ -467,7 +488,7 @@ def gl_compute_reduce_sum(a: AccessPattern, out: Optional[AccessPattern] = None,
     if out is None:
         m = GlAp()
         _check(LIB.gl_shape_reduce_sum(ctypes.byref(sa), ctypes.byref(m)), "gl_shape_reduce_sum")
-        out = _alloc(m, a.tensor.device)
+        out = _alloc(m, a.tensor.device, stream)
     so = _struct(out)
     _check(LIB.gl_compute_reduce_sum(ctypes.byref(sa), ctypes.byref(so), _stream(stream)), "gl_compute_reduce_sum")
     return out
@@ -476,7 +497,7 @@ def gl_compute_reduce_sum(a: AccessPattern, out: Optional[AccessPattern] = None,
 def gl_compute_relu(a: AccessPattern, out: Optional[AccessPattern] = None, stream=None) -> AccessPattern:
     sa = _struct(a)
     if out is None:
-        out = AccessPattern(torch.empty_like(a.tensor), a.access_ndim)
+        out = AccessPattern(_empty(a.tensor.shape, a.tensor.dtype, a.tensor.device, stream), a.access_ndim)
     so = _struct(out)
     _check(LIB.gl_compute_relu(ctypes.byref(sa), ctypes.byref(so), _stream(stream)), "gl_compute_relu")
     return out
@@ -526,20 +547,20 @@ def _mx4_meta(shape, access_ndim) -> GlMx4:
     return s
 
 
-def mx4_empty(shape, access_ndim: int, device) -> Mx4:
-    """Storage for a pattern of this shape, contents undefined."""
+def mx4_empty(shape, access_ndim: int, device, stream=None) -> Mx4:
+    """Storage for a pattern of this shape, contents undefined; `stream`: where it is first used, if not the current one."""
     s = _mx4_meta(shape, access_ndim)
     nd, ns = LIB.gl_mx4_data_bytes(ctypes.byref(s)), LIB.gl_mx4_scale_bytes(ctypes.byref(s))
     if not nd:
         raise GlError(4, "mx4_empty")
-    return Mx4(torch.empty(nd, dtype=torch.uint8, device=device), torch.empty(ns, dtype=torch.uint8, device=device),
+    return Mx4(_empty(nd, torch.uint8, device, stream), _empty(ns, torch.uint8, device, stream),
                tuple(int(n) for n in shape), access_ndim)
 
 
 def gl_mx4_quantize(a: AccessPattern, out: Optional[Mx4] = None, stream=None) -> Mx4:
     sa = _struct(a)
     if out is None:
-        out = mx4_empty(tuple(a.tensor.shape), a.access_ndim, a.tensor.device)
+        out = mx4_empty(tuple(a.tensor.shape), a.access_ndim, a.tensor.device, stream)
     _on_gpu(a.tensor, out.data, out.scale)
     _check(LIB.gl_mx4_quantize(ctypes.byref(sa), ctypes.byref(_mx4_struct(out)), _stream(stream)), "gl_mx4_quantize")
     return out
@@ -547,22 +568,22 @@ def gl_mx4_quantize(a: AccessPattern, out: Optional[Mx4] = None, stream=None) ->
 
 def gl_mx4_dequantize(m: Mx4, out: Optional[AccessPattern] = None, stream=None) -> AccessPattern:
     if out is None:
-        out = AccessPattern(torch.empty(m.dims, dtype=torch.float32, device=m.data.device), m.access_ndim)
+        out = AccessPattern(_empty(m.dims, torch.float32, m.data.device, stream), m.access_ndim)
     _on_gpu(m.data, m.scale, out.tensor)
     so = _struct(out)
     _check(LIB.gl_mx4_dequantize(ctypes.byref(_mx4_struct(m)), ctypes.byref(so), _stream(stream)), "gl_mx4_dequantize")
     return out
 
 
-def _product_out(access0, access1, flags, device) -> AccessPattern:
+def _product_out(access0, access1, flags, device, stream) -> AccessPattern:
     shape = tuple(access0) + tuple(access1)
     dtype = torch.bfloat16 if flags & GL_OUT_BF16 else torch.float32
-    return AccessPattern(torch.empty(shape, dtype=dtype, device=device), len(shape))
+    return AccessPattern(_empty(shape, dtype, device, stream), len(shape))
 
 
 def gl_cartesian_dot_mx4(a0: Mx4, a1: Mx4, out: Optional[AccessPattern] = None, flags: int = 0, stream=None) -> AccessPattern:
     if out is None:
-        out = _product_out(a0.shape[0], a1.shape[0], flags, a0.data.device)
+        out = _product_out(a0.shape[0], a1.shape[0], flags, a0.data.device, stream)
     _on_gpu(a0.data, a0.scale, a1.data, a1.scale, out.tensor)
     so = _struct(out)
     _check(LIB.gl_cartesian_dot_mx4(ctypes.byref(_mx4_struct(a0)), ctypes.byref(_mx4_struct(a1)), ctypes.byref(so), flags,
@@ -574,16 +595,12 @@ def gl_dense_mx4_workspace(a0: AccessPattern, a1: Mx4) -> int:
     return int(LIB.gl_dense_mx4_workspace(ctypes.byref(_struct(a0)), ctypes.byref(_mx4_struct(a1))))
 
 
-def _scratch(need: int, device) -> Optional[torch.Tensor]:
-    return torch.empty(need + 1024, dtype=torch.uint8, device=device) if need else None
-
-
 def gl_dense_mx4(a0: AccessPattern, a1: Mx4, out: Optional[AccessPattern] = None, flags: int = 0,
                  workspace: Optional[torch.Tensor] = None, stream=None) -> AccessPattern:
     if out is None:
-        out = _product_out(a0.access_shape, a1.shape[0], flags, a0.tensor.device)
+        out = _product_out(a0.access_shape, a1.shape[0], flags, a0.tensor.device, stream)
     if workspace is None:
-        workspace = _scratch(gl_dense_mx4_workspace(a0, a1), a0.tensor.device)
+        workspace = _scratch(gl_dense_mx4_workspace(a0, a1), a0.tensor.device, stream)
     _on_gpu(a0.tensor, a1.data, a1.scale, out.tensor, workspace)
     s0, so = _struct(a0), _struct(out)
     _check(LIB.gl_dense_mx4(ctypes.byref(s0), ctypes.byref(_mx4_struct(a1)), ctypes.byref(so), flags, *_ws(workspace),
@@ -673,7 +690,7 @@ def _read_args(cache: Cache4, k: torch.Tensor, v: torch.Tensor, page_table, leng
 def gl_cache4_read(cache: Cache4, tokens: int, page_table: torch.Tensor, lengths: torch.Tensor, stream=None):
     """The values of the last `tokens` tokens of every sequence: (k, v), bf16 [B, tokens, kv_heads, head_dim]."""
     shape = (page_table.shape[0], tokens, cache.kv_heads, cache.head_dim)
-    k, v = (torch.empty(shape, dtype=torch.bfloat16, device=cache.data.device) for _ in range(2))
+    k, v = (_empty(shape, torch.bfloat16, cache.data.device, stream) for _ in range(2))
     _check(LIB.gl_cache4_read(*_read_args(cache, k, v, page_table, lengths), _stream(stream)), "gl_cache4_read")
     return k, v
 
@@ -697,9 +714,9 @@ def gl_attend_cache4(q: AccessPattern, cache: Cache4, page_table: torch.Tensor, 
         scale = cache.head_dim ** -0.5
     if out is None:
         dtype = torch.bfloat16 if flags & GL_OUT_BF16 else torch.float32
-        out = AccessPattern(torch.empty(tuple(q.tensor.shape), dtype=dtype, device=q.tensor.device), 3)
+        out = AccessPattern(_empty(tuple(q.tensor.shape), dtype, q.tensor.device, stream), 3)
     if workspace is None:
-        workspace = _scratch(gl_attend_cache4_workspace(q, cache), q.tensor.device)
+        workspace = _scratch(gl_attend_cache4_workspace(q, cache), q.tensor.device, stream)
     _check(LIB.gl_attend_cache4(*_attend_args(q, cache, page_table, lengths, out, scale, flags, workspace), _stream(stream)),
            "gl_attend_cache4")
     return out
@@ -725,13 +742,20 @@ class Prepared:
     """A device call with its argument structures built once, for launch loops
     where Python marshalling would otherwise outweigh a microsecond-scale kernel.
     The stream is looked up at call time, so a prepared call can be captured
-    into a CUDA graph."""
+    into a CUDA graph.  `scratch`: a workspace that nobody else holds.  It was taken
+    on the stream that was current then, so torch is told of every other stream
+    that uses it: dropping the call then waits for them."""
 
-    def __init__(self, fn, args, keep):
-        self._fn, self._args, self._keep = fn, args, keep
+    def __init__(self, fn, args, keep, scratch=None):
+        self._fn, self._args, self._keep, self._scratch = fn, args, keep, scratch
+        self._streams = None if scratch is None else {_stream(None)}
 
     def __call__(self, stream=None):
-        rc = self._fn(*self._args, _stream(stream))
+        raw = _stream(stream)
+        if self._streams is not None and raw not in self._streams:
+            self._scratch.record_stream(_stream_object(torch.cuda.current_stream() if stream is None else stream))
+            self._streams.add(raw)
+        rc = self._fn(*self._args, raw)
         if rc != GL_OK:
             raise GlError(rc, self._fn.__name__)
 
@@ -795,11 +819,11 @@ def prepare_cartesian_dot_mx4(a0: Mx4, a1: Mx4, out: AccessPattern, flags: int =
 
 def prepare_dense_mx4(a0: AccessPattern, a1: Mx4, out: AccessPattern, flags: int = 0,
                       workspace: Optional[torch.Tensor] = None) -> Prepared:
-    if workspace is None:
-        workspace = _scratch(gl_dense_mx4_workspace(a0, a1), a0.tensor.device)
+    scratch = None if workspace is not None else _scratch(gl_dense_mx4_workspace(a0, a1), a0.tensor.device)
+    workspace = scratch if workspace is None else workspace
     _on_gpu(a0.tensor, a1.data, a1.scale, out.tensor, workspace)
     return Prepared(LIB.gl_dense_mx4, (ctypes.byref(_struct(a0)), ctypes.byref(_mx4_struct(a1)), ctypes.byref(_struct(out)), flags,
-                                       *_ws(workspace)), (a0, a1, out, workspace))
+                                       *_ws(workspace)), (a0, a1, out, workspace), scratch)
 
 
 def prepare_cache4_append(cache: Cache4, k, v, page_table, lengths) -> Prepared:
@@ -812,10 +836,10 @@ def prepare_cache4_read(cache: Cache4, k, v, page_table, lengths) -> Prepared:
 
 def prepare_attend_cache4(q: AccessPattern, cache: Cache4, page_table, lengths, out: AccessPattern,
                           scale: Optional[float] = None, flags: int = 0, workspace: Optional[torch.Tensor] = None) -> Prepared:
-    if workspace is None:
-        workspace = _scratch(gl_attend_cache4_workspace(q, cache), q.tensor.device)
+    scratch = None if workspace is not None else _scratch(gl_attend_cache4_workspace(q, cache), q.tensor.device)
+    workspace = scratch if workspace is None else workspace
     args = _attend_args(q, cache, page_table, lengths, out, cache.head_dim ** -0.5 if scale is None else scale, flags, workspace)
-    return Prepared(LIB.gl_attend_cache4, args, (q, cache, page_table, lengths, out, workspace))
+    return Prepared(LIB.gl_attend_cache4, args, (q, cache, page_table, lengths, out, workspace), scratch)
 
 
 def output_like(shape_fn_result, device) -> AccessPattern:

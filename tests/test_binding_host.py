@@ -91,3 +91,81 @@ def test_tensors_are_on_one_gpu(gl):
     for devices in (("cuda:0", "cpu"), ("cpu", "cuda:0"), ("cuda:0", "cuda:1")):
         with pytest.raises(ValueError):
             gl._on_gpu(*(T(d) for d in devices))
+
+
+class _Stream:
+    cuda_stream = 7
+
+
+def _storing_calls(gl):
+    """Calls that take storage for their result or their scratch, as functions of the stream."""
+    bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    ap = gl.AccessPattern
+    a, win = ap(torch.zeros(2, 6, 6, 6), 1), gl.windows_spec((6, 3, 3), (1, 1, 1))
+    b = ap(torch.zeros(2, 6, 6, 6), 1)
+    x, w = ap(torch.zeros(2, 64, 9, 9, dtype=bf), 1), ap(torch.zeros(5, 64, 3, 3, dtype=bf), 1)
+    conv = gl.windows_spec((64, 3, 3), (1, 1, 1))
+    assert gl.gl_cartesian_dot_workspace(x, conv, w) > 0
+    rows = ap(torch.zeros(4, 64, dtype=bf), 1)
+    m0, m1 = gl.mx4_empty((4, 64), 1, "cpu"), gl.mx4_empty((6, 64), 1, "cpu")
+    cache = gl.cache4_empty(2, 1, 16, 64, "cpu")
+    q = ap(torch.zeros(1, 3, 2, 64, dtype=bf), 3)
+    table, lengths = torch.zeros(1, 2, dtype=i32), torch.zeros(1, dtype=i32)
+    return [lambda s: gl.gl_access_windows(a, win, stream=s), lambda s: gl.gl_access_transpose(a, (1, 0, 2, 3), stream=s),
+            lambda s: gl.gl_access_pad(a, 1, 1, 1, stream=s), lambda s: gl.gl_access_slice(a, 1, 0, 2, stream=s),
+            lambda s: gl.gl_access_concat(a, b, 1, stream=s), lambda s: gl.gl_access_pair(a, b, stream=s),
+            lambda s: gl.gl_compute_reduce_max(a, None, stream=s), lambda s: gl.gl_compute_reduce_sum(a, stream=s),
+            lambda s: gl.gl_compute_relu(a, stream=s), lambda s: gl.gl_cartesian_dot(x, conv, w, stream=s),
+            lambda s: gl.gl_mx4_quantize(rows, stream=s), lambda s: gl.gl_mx4_dequantize(m0, stream=s),
+            lambda s: gl.gl_cartesian_dot_mx4(m0, m1, stream=s), lambda s: gl.gl_dense_mx4(rows, m1, stream=s),
+            lambda s: gl.gl_cache4_read(cache, 3, table, lengths, stream=s),
+            lambda s: gl.gl_attend_cache4(q, cache, table, lengths, stream=s)]
+
+
+def test_storage_is_taken_on_the_stream_of_the_call(gl, monkeypatch):
+    """torch hands a block out again in the order of the stream that it was taken on: scratch that is dropped on return may
+    only have been taken on the stream that still uses it."""
+    import contextlib
+    calls = _storing_calls(gl)
+    now, taken, launched = [], [], []
+
+    @contextlib.contextmanager
+    def stream(s):
+        now.append(s.cuda_stream)
+        yield
+        now.pop()
+
+    class Lib:                              # host functions as they are, device calls recorded
+        def __getattr__(self, name):
+            f = getattr(real, name)
+            if name.endswith(("_workspace", "_bytes")) or name.startswith("gl_shape"):
+                return f
+            return lambda *args: launched.append(args[-1]) or 0
+
+    real, empty = gl.LIB, torch.empty
+    monkeypatch.setattr(gl, "LIB", Lib())
+    monkeypatch.setattr(gl, "_on_gpu", lambda *t: None)
+    monkeypatch.setattr(gl, "_stream", lambda s: 3 if s is None else s if isinstance(s, int) else s.cuda_stream)
+    monkeypatch.setattr(torch.cuda, "stream", stream)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda raw: _Stream() if raw == 7 else None)
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: taken.append(now[-1] if now else 3) or empty(*a, **k))
+    monkeypatch.setattr(torch, "empty_like", lambda t: taken.append(now[-1] if now else 3) or empty(t.shape, dtype=t.dtype))
+    for given, raw in ((None, 3), (_Stream(), 7), (7, 7)):
+        for i, call in enumerate(calls):
+            del taken[:], launched[:]
+            call(given)
+            assert launched == [raw] and taken and set(taken) == {raw}, (i, given, taken)
+
+
+def test_prepared_scratch_tells_torch_of_other_streams(gl, monkeypatch):
+    told = []
+
+    class Scratch:
+        def record_stream(self, s):
+            told.append(s.cuda_stream)
+
+    monkeypatch.setattr(gl, "_stream", lambda s: 3 if s is None else s.cuda_stream)
+    call = gl.Prepared(lambda raw: 0, (), (), Scratch())
+    for s in (None, _Stream(), None, _Stream()):
+        call(s)
+    assert told == [7]
