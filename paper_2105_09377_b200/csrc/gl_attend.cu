@@ -127,18 +127,21 @@ __global__ void __launch_bounds__(256) cache4_read(uint16_t* __restrict__ k, uin
 // Attention
 // ------------------------------------------------------------------------
 //
-// out = sum_t p_t V_t / sum_t p_t, p_t = 2^(s_t - ref), s = scale log2(e) q K_t, in one pass over the tokens with a running
-// reference.
+// out = sum_t p_t V_t / sum_t p_t, p_t = 2^((s_t - roof) cf), s = q K_t, cf = scale log2(e), in one pass over the tokens with a
+// running reference `roof`, 8 / cf above the largest score that it was set by.  The reference is held in units of the scores
+// and subtracted before the product with cf: of scores beyond 2^24 / cf the rounded product roof cf would be off by more than
+// the largest weight can bear (from 2^31 on all weights became 0 or Inf).
 //
 // Rows are the T * group query rows that share a kv head, 8 * NT of them per work item; scores are computed transposed,
 // S^T = K Q^T with tokens as the 16-row side of mma.m16n8k16, so that eight rows (a usual group) fill an instruction.
 // Codes become fp16 by the conversion instruction (exact).  The scale of a block of K multiplies the fp32 result of that
-// block's two instructions, so no scale ever meets fp16's range.  Q is scaled per row by a power of two for the same reason.
-// Of V, a token's scale varies along the result, so it goes into the weights: w = 2^7 p * 2^(e - top), top the largest
+// block's two instructions, so no scale ever meets fp16's range.  Q is scaled per row by a power of two for the same reason;
+// the scales of K get 2^-24 for it, or keys beyond 2^100 would leave fp32's range although the scores do not.
+// Of V, a token's scale varies along the result, so it goes into the weights: w = 2^15 p * 2^(e - top), top the largest
 // exponent that the block has met (and one more); the sums refer to it.  Tokens more than seven binades below it take
 // a turn of their own.  fp16 weights keep 11 bits, which a bf16 result cannot show; for fp32 results (HILO) the rounded-off
-// part of the weights is multiplied in a second instruction.  The reference of the maximum moves only when a weight
-// would pass 2^8.
+// part of the weights is multiplied in a second instruction.  The reference moves only when a weight would pass 2^15: then
+// the largest one becomes 2^7.
 //
 // The work is cut along the tokens of all sequences: tiles of 64 (32) tokens of all (sequence, kv head, row block) in one
 // list, the same number to every block.  A block's four warps take turns in the tiles of a segment, each with its own
@@ -167,6 +170,7 @@ struct AttendParams {
   int lead;              // what a segment costs beyond its tiles, in tiles (see Walk)
   int alone;             // a block per segment, no list, nothing to join: caches of a few tiles
   float scale_log2;      // softmax scale * log2(e)
+  float step;            // 8 / scale_log2: how far above the largest score a reference is set
   int out_bf16;
 };
 
@@ -369,6 +373,12 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
   return d;
 }
+// What brings sums that refer to r = `roof` times `cf` to its rounded value, which is what the joining goes by.  (Beyond
+// 2^24 r says no more than which part is ahead.)
+__device__ __forceinline__ float rounded_off(float roof, float cf) {
+  const float rest = fmaf(roof, cf, -(roof * cf));
+  return fabsf(rest) < 1.f ? ex2(rest) : 1.f;
+}
 // Token (0..15) of the group that row i of a 16-row fragment stands for: spreads the tokens that a warp reads in one
 // access over the banks.  Rows come in pairs (2i, 2i+1) -> (i, 4 + (i ^ 1)), the upper eight likewise.
 __device__ __forceinline__ int token_of_row(int i) {
@@ -421,14 +431,15 @@ __device__ __forceinline__ void load_scales(uint32_t at, uint32_t (&w)[(NB + 3) 
     load_shared<NB / 4>(at, w);
   }
 }
-// Scale bytes as 2^(e - 127), NaN for 255: two a conversion, by way of bf16
+// Scale bytes as 2^(e - 127) times the power of two in both halves of `by`, NaN for 255: two a conversion, by way of bf16
 template <int NB>
-__device__ __forceinline__ void scale_floats(const uint32_t (&w)[(NB + 3) / 4], float (&f)[NB]) {
+__device__ __forceinline__ void scale_floats(const uint32_t (&w)[(NB + 3) / 4], uint32_t by, float (&f)[NB]) {
 #pragma unroll
   for (int i = 0; i < NB; i += 2) {
     uint32_t two;
     const uint16_t bytes = static_cast<uint16_t>(w[i >> 2] >> (8 * (i & 2)));
     asm("cvt.rn.bf16x2.ue8m0x2 %0, %1;" : "=r"(two) : "h"(bytes));
+    two = mul_bf16x2(two, by);
     f[i] = __uint_as_float(two << 16);
     f[i + 1] = __uint_as_float(two & 0xFFFF0000u);
   }
@@ -578,14 +589,18 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
         __half* dst = reinterpret_cast<__half*>(qfrag + ((i * 2 + (byte >> 1)) * NT + (r >> 3)) * 32 + (r & 7) * 4 + j);
         dst[(byte & 1) * 2 + half] = __float2half_rn(x[i] * f);
       }
-      // scores carry the 2^(14 - e) of Q
-      if (lane == 0) qfac[r] = __uint_as_float(static_cast<uint32_t>(e + 127 - 14) << 23) * p.scale_log2;
+      if (lane == 0) qfac[r] = __int_as_float(e);
     }
     __syncthreads();
+    // Scores carry the 2^(14 - e) of Q, and the 2^-24 of K unless a query is so large (2^64) that it has no need of it: then
+    // scales of K below 2^-109, which 2^-24 would turn into zeros, still count.
+    const int e_max = __reduce_max_sync(0xFFFFFFFFu, lane < R ? __float_as_int(qfac[lane]) : -127);
+    const int k_down = e_max < 64 ? 24 : 0;
+    const uint32_t k_by = k_down ? 0x33803380u : 0x3F803F80u;   // 2^-24 or 1, twice as bf16
 
-    // ref: what a row's weights refer to; a weight is 2^7 p = 2^(s cf + off), off = 7 - ref (+Inf until there is one).
+    // roof: what a row's weights refer to; a weight is 2^15 p = 2^((s - roof) cf + 15), roof -Inf until there is one.
     // top_e: the scale exponents that the blocks' results refer to, four to a word, 8 at least.
-    float off[NT][2], l[NT][2], cf[NT][2];
+    float roof[NT][2], l[NT][2], cf[NT][2];
     int limit[NT][2], all_see = INT32_MAX, any_sees = 0;
     uint32_t top_e[kScaleWords];
     float acc[NT][NB][2][4];
@@ -594,9 +609,9 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const int row = rb * R + n * 8 + tq * 2 + c;
-        off[n][c] = -ninf;
+        roof[n][c] = ninf;
         l[n][c] = 0.f;
-        cf[n][c] = qfac[n * 8 + tq * 2 + c];
+        cf[n][c] = __uint_as_float(static_cast<uint32_t>(__float_as_int(qfac[n * 8 + tq * 2 + c]) + 127 - 14 + k_down) << 23) * p.scale_log2;
         limit[n][c] = row < p.rows ? min(len, len - p.T + row_token(p, row) + 1) : seen;   // (rows past the end: anything)
         all_see = min(all_see, limit[n][c]);
         any_sees = max(any_sees, limit[n][c]);
@@ -641,8 +656,8 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
           uint32_t sa[kScaleWords], sb[kScaleWords];
           load_scales<NB>(grp + at_ks, sa);
           load_scales<NB>(grp + at_ks + 8 * NB, sb);
-          scale_floats<NB>(sa, fa[mt]);
-          scale_floats<NB>(sb, fb[mt]);
+          scale_floats<NB>(sa, k_by, fa[mt]);
+          scale_floats<NB>(sb, k_by, fb[mt]);
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -689,15 +704,15 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
             }
       }
 
-      // ---- the reference moves only when a weight would pass 2^8 p: a vote, no shuffles, in most tiles
-      float high = ninf;
+      // ---- the reference moves only when a weight would pass 2^15: a vote, no shuffles, in most tiles
+      bool above = false;
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-          for (int c = 0; c < 4; ++c) high = fmaxf(high, fmaf(s[mt][n][c], cf[n][c & 1], off[n][c & 1]));
-      if (__any_sync(0xFFFFFFFFu, high > 15.f)) {
+          for (int c = 0; c < 4; ++c) above |= s[mt][n][c] > roof[n][c & 1];
+      if (__any_sync(0xFFFFFFFFu, above)) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -706,10 +721,11 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
-            const float now = fminf(off[n][c], 7.f - top * cf[n][c]);
-            // (off = +Inf, nothing seen so far: sum and result are zeros)
-            const float f = now == off[n][c] || off[n][c] == -ninf ? 1.f : ex2(now - off[n][c]);
-            off[n][c] = now;
+            // (a step of 2^120 stands for more: all scores are the same to such a cf)
+            const float now = fmaxf(roof[n][c], top + fminf(8.f / cf[n][c], 1.329228e36f));
+            // (roof = -Inf, nothing seen so far: sum and result are zeros)
+            const float f = now == roof[n][c] ? 1.f : ex2((roof[n][c] - now) * cf[n][c]);
+            roof[n][c] = now;
             l[n][c] *= f;
 #pragma unroll
             for (int i = 0; i < NB; ++i)
@@ -725,8 +741,8 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
         for (int mt = 0; mt < 2; ++mt) {
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
-            const float w8 = ex2(fmaf(s[mt][n][c], cf[n][c & 1], off[n][c & 1]));
-            s[mt][n][c] = masked && s[mt][n][c] == ninf ? 0.f : w8;
+            const float w15 = ex2(fmaf(s[mt][n][c] - roof[n][c & 1], cf[n][c & 1], 15.f));
+            s[mt][n][c] = masked && s[mt][n][c] == ninf ? 0.f : w15;
             l[n][c & 1] += s[mt][n][c];
           }
 #pragma unroll
@@ -930,14 +946,15 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const int r = n * 8 + tq * 2 + c;
+        const float adjust = rounded_off(roof[n][c], cf[n][c]);
         if (g == 0) {
-          jm[warp * R + r] = 7.f - off[n][c];
-          jl[warp * R + r] = l[n][c];
+          jm[warp * R + r] = roof[n][c] * cf[n][c];
+          jl[warp * R + r] = l[n][c] * adjust;
         }
         float* row = reinterpret_cast<float*>(smem + warp * Cfg::kWarpRing) + r * Cfg::kAccPitch;
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
-          const float back = mx4_scale(top_e[i >> 2] >> (8 * (i & 3)) & 255u);
+          const float back = mx4_scale(top_e[i >> 2] >> (8 * (i & 3)) & 255u) * adjust;
 #pragma unroll
           for (int k = 0; k < 2; ++k)
             *reinterpret_cast<float2*>(row + i * 32 + 4 * g + 2 * k) = make_float2(acc[n][i][k][c] * back, acc[n][i][k][2 + c] * back);
@@ -1298,6 +1315,7 @@ int gl_attend_cache4(const gl_ap* q, int64_t token_pitch, const gl_cache4* cache
   p.rows = static_cast<int>(rows);
   p.row_blocks = static_cast<int>(row_blocks);
   p.scale_log2 = scale * 1.4426950408889634f;
+  p.step = std::min(8.f / p.scale_log2, 1.329228e36f);   // (2^120 stands for more: all scores are the same to such a scale)
   p.out_bf16 = f32 ? 0 : 1;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   p.R = k.rows;

@@ -6,7 +6,7 @@
 // memory layouts of the MMA operands: K as [token][dim] (K-major B of S = Q K^T), V as [token][dim] too, which is the
 // MN-major B of O = P V.  Scores come back from tensor memory a row per thread, are turned into weights and go back
 // into the columns they came from, as the A operand of the second product.  The maximum that the weights refer to is
-// moved only when a row's scores exceed it by 2^8, so that O is rarely rescaled.  MT = 2: while the softmax warps
+// moved only when a row's scores exceed it, 2^8 above the last one, so that O is rarely rescaled.  MT = 2: while the softmax warps
 // of one half work, the tensor core works for the other.
 // TERMS = 1 rounds the weights to bf16 (8 bits; the result is bf16 too); TERMS = 3 carries them as three bf16 terms
 // for fp32 results.
@@ -128,6 +128,16 @@ __device__ __forceinline__ void get(Held<NB, ITEMS>& x, int i, const uint8_t* co
     }
   }
 }
+// (a + b) * c of two values at a time
+__device__ __forceinline__ float2 add_mul2(float a0, float a1, float b, float c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c;\n\t"
+      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %4};\n\tmov.b64 c, {%5, %5};\n\t"
+      "add.rn.f32x2 a, a, b;\n\tmul.rn.f32x2 a, a, c;\n\t"
+      "mov.b64 {%0, %1}, a;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a0), "f"(a1), "f"(b), "f"(c));
+  return d;
+}
 // A token that does not exist or is not seen by any row.
 template <int NB, int ITEMS>
 __device__ __forceinline__ void clear(Held<NB, ITEMS>& x, int i) {
@@ -222,7 +232,7 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
         if (lane == 0) mbar_arrive(b_q + 8 * m);
       }
       const int limit = live ? min(w.len, w.len - p.T + row_token(p, row) + 1) : 0;
-      float ref = ninf, sum = 0.f;
+      float roof = ninf, sum = 0.f;   // weights are 2^((s - roof) cf)
       for (int tile = w.t0; tile < w.t1; ++tile, ++it) {
         if (!mbar_wait(b_s + 8 * m, it & 1u, abort_flag)) { ok = false; break; }
         tc_fence_after();
@@ -250,14 +260,13 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
             top = fmaxf(fmaxf(top, t1), fmaxf(t2, t3));
           }
         }
-        top *= cf;
-        const bool move = top > ref + 8.f || ref == ninf;
-        const float new_ref = move ? fmaxf(top, ref) : ref;
-        if (__any_sync(0xFFFFFFFFu, move && new_ref != ref) && tile > w.t0) {
+        const bool move = top > roof;
+        const float new_roof = move ? top + p.step : roof;
+        if (__any_sync(0xFFFFFFFFu, move) && tile > w.t0) {
           // O holds the tiles before this one: bring it to the new reference
           if (!mbar_wait(b_o + 8 * m, (it - 1) & 1u, abort_flag)) { ok = false; break; }
           tc_fence_after();
-          const float f = new_ref == ref ? 1.f : ex2(ref - new_ref);
+          const float f = move ? ex2((roof - new_roof) * cf) : 1.f;
           sum *= f;
 #pragma unroll 1
           for (int j = 0; j < D / 16; ++j) {
@@ -268,8 +277,8 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
             tc_store_16cols(o_col + 16 * j, x);
           }
         }
-        ref = new_ref;
-        const float off = ref == ninf ? 0.f : ref;
+        roof = new_roof;
+        const float down = roof == ninf ? 0.f : -roof;
         float part[4] = {0.f, 0.f, 0.f, 0.f};
         // (two copies of the loop: a test of `masked` per weight would cost as much as the weight)
         const auto weigh = [&](auto with_mask) {
@@ -279,7 +288,8 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
             tc_load_32cols(s_col + 32 * j, x);
 #pragma unroll
             for (int i = 0; i < 32; i += 2) {
-              float a = ex2(fmaf(__uint_as_float(x[i]), cf, -off)), b = ex2(fmaf(__uint_as_float(x[i + 1]), cf, -off));
+              const float2 y = add_mul2(__uint_as_float(x[i]), __uint_as_float(x[i + 1]), down, cf);
+              float a = ex2(y.x), b = ex2(y.y);
               if constexpr (decltype(with_mask)::value) {
                 const bool there = groups >> (2 * j + (i >> 4)) & 1u;
                 a = there && 32 * j + i < open ? a : 0.f;
@@ -317,9 +327,10 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
       if (!mbar_wait(b_o + 8 * m, (it - 1) & 1u, abort_flag)) { ok = false; break; }
       tc_fence_after();
       const bool whole = w.whole();
-      const float inv = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
+      const float adjust = rounded_off(roof, cf);
+      const float inv = whole ? (sum == 0.f ? 0.f : 1.f / sum) : adjust;
       float* slot = w.slot(p, D) + static_cast<int64_t>(m * 128) * (D + 2);
-      if (!whole) *reinterpret_cast<float2*>(slot + r * (D + 2)) = make_float2(ref, sum);
+      if (!whole) *reinterpret_cast<float2*>(slot + r * (D + 2)) = make_float2(roof * cf, sum * adjust);
       const int* nan_at = nan_from + (item & 3u) * NB;
       // 64 dims at a time (a pair of blocks), by way of the warp's rows of its Q tile, which no product reads any more:
       // written a row per lane, stored along the rows.  Columns (g * NB/2 + pair) * 8 + 2 i + half hold dims

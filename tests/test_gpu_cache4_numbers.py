@@ -1,0 +1,83 @@
+"""GPU numerics of the attention over 4-bit pages where they are tight: weights and their sum, keys and values near the ends
+of the range."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import mx4
+from paper_2105_09377_b200 import synth
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def gl():
+    from paper_2105_09377_b200 import binding
+    return binding
+
+
+def _to_bf16(x):
+    """Rounded to eight significant bits, ties to even (float64 in and out)."""
+    m, e = np.frexp(x)
+    return np.ldexp(np.round(m * 256.0), e - 8)
+
+
+def _bf16(seed, shape, std=1.0):
+    return (torch.from_numpy(synth.normal(seed, 1, shape)) * std).to(torch.bfloat16).cuda()
+
+
+def _stored(gl, k, v, page):
+    """A cache that holds k and v, [sequences, tokens, kv heads, D] of one length; pages in shuffled order."""
+    b, n, hkv, d = k.shape
+    width = -(-n // page)
+    table = torch.from_numpy(np.random.default_rng(n).permutation(b * width).astype(np.int32).reshape(b, width)).cuda()
+    lengths = torch.full((b,), n, dtype=torch.int32, device="cuda")
+    cache = gl.cache4_empty(b * width, hkv, page, d, "cuda")
+    cache.data.fill_(0xFF)
+    gl.gl_cache4_append(cache, k, v, table, lengths)
+    return cache, table, lengths
+
+
+def _row(q, k, v, scale):
+    """Weights, result and sum of p |v| of one row over all tokens, in 64 bits."""
+    s = scale * (k @ q)
+    p = np.exp(s - s.max())
+    p /= p.sum()
+    return s, p, p @ v, p @ np.abs(v)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("rows,n", [(4, 60), (12, 60), (28, 60), (40, 60), (4, 9000), (28, 3000), (40, 3000)])
+def test_keys_near_the_end_of_the_range(gl, rows, n, d, bf16):
+    """Keys of about 2^112 under queries of many sizes, in one call: scores that are ordinary numbers (queries of 2^-112),
+    scores of up to 2^120 (one token takes all), and zeros.  All of them finite, none beyond fp32."""
+    v = _bf16(2, (1, n, 1, d))
+    k = _bf16(1, (1, n, 1, d), 2.0 ** 112)
+    if n > 100:
+        k[0, 40:n - 50] = _bf16(5, (1, n - 90, 1, d))[0]      # ordinary keys before and between
+    size = np.resize([2.0 ** -112, 1.0, 0.0, 2.0 ** -118, 2.0 ** -20, 2.0 ** -100], rows)
+    q = (torch.from_numpy(synth.normal(3, 1, (rows, d)) * size[:, None])).to(torch.bfloat16).cuda().view(1, 1, rows, d)
+    cache, table, lengths = _stored(gl, k, v, 16)
+    got = gl.gl_attend_cache4(gl.AccessPattern(q, 3), cache, table, lengths, flags=gl.GL_OUT_BF16 if bf16 else 0)
+    got = got.tensor[0, 0].double().cpu().numpy()
+    kd, vd = (mx4.rounded(x[0, :, 0].double().cpu().numpy()) for x in (k, v))
+    qd = q[0, 0].double().cpu().numpy()
+    assert np.isfinite(got).all()
+    checked = 0
+    for h in range(rows):
+        s, p, ref, mag = _row(qd[h], kd, vd, d ** -0.5)
+        # D products of fp32 partial sums, then two roundings, of terms of q k
+        ds = (d / 16 + 6) * 2.0 ** -23 * d ** -0.5 * (np.abs(kd) @ np.abs(qd[h])).max()
+        if np.abs(s).max() > 20:             # one token takes all, if it is ahead by more than the scores are off
+            top = np.sort(s)[::-1]
+            if top[0] - top[1] < 4 * ds + 100:
+                continue
+            ref, mag, ds = vd[s.argmax()], np.abs(vd[s.argmax()]), 0.0
+        rel = 2 * ds + 2.0 ** -20 + (n / 16 + 16) * 2.0 ** -23 + ((2.0 ** -8 if rows > 32 else 2.0 ** -10) if bf16 else 2.0 ** -20)
+        tol = rel * mag
+        lo, hi = (_to_bf16(ref - tol), _to_bf16(ref + tol)) if bf16 else (ref - tol, ref + tol)
+        assert ((got[h] >= lo) & (got[h] <= hi)).all(), (h, size[h], np.abs(got[h] - ref).max())
+        checked += 1
+    assert checked > rows / 2
+    assert gl.gl_poll_device_status() == 0
