@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <cstring>
+#include <type_traits>
 
 #include "gl_cache4.cuh"
 #include "gl_internal.h"
@@ -136,7 +137,8 @@ __global__ void __launch_bounds__(256) cache4_read(uint16_t* __restrict__ k, uin
 // S^T = K Q^T with tokens as the 16-row side of mma.m16n8k16, so that eight rows (a usual group) fill an instruction.
 // Codes become fp16 by the conversion instruction (exact).  The scale of a block of K multiplies the fp32 result of that
 // block's two instructions, so no scale ever meets fp16's range.  Q is scaled per row by a power of two for the same reason;
-// the scales of K get 2^-24 for it, or keys beyond 2^100 would leave fp32's range although the scores do not.
+// the scales of K get 2^-24 for it, or keys beyond 2^100 would leave fp32's range although the scores do not.  (Scales of K
+// below 2^-109 become zeros by it.)
 // Of V, a token's scale varies along the result, so it goes into the weights: w = 2^15 p * 2^(e - top), top the largest
 // exponent that the block has met (and one more); the sums refer to it.  Tokens more than seven binades below it take
 // a turn of their own.  fp16 weights keep 11 bits, which a bf16 result cannot show; for fp32 results (HILO) the rounded-off
@@ -146,7 +148,8 @@ __global__ void __launch_bounds__(256) cache4_read(uint16_t* __restrict__ k, uin
 // The work is cut along the tokens of all sequences: tiles of 64 (32) tokens of all (sequence, kv head, row block) in one
 // list, the same number to every block.  A block's four warps take turns in the tiles of a segment, each with its own
 // ring of bulk copies, running reference, sum and result; the block joins its warps, and a second kernel joins the
-// blocks where a segment was cut.
+// blocks where a segment was cut.  A part is stored divided by its own sum of weights and joined as an average, so that
+// nothing is larger than the values themselves (weights of up to 2^15 over many tokens took values beyond 2^100 to Inf).
 //
 // 64 sequences of 4096 tokens, 32 heads over 8 of 128: 75 us, 3.8 TB/s of cache (0.58 of the copy rate), bound by issue: about
 // 600 instructions per 32 tokens and warp, of which 128 convert codes and 32 are matrix instructions, at half an
@@ -159,7 +162,7 @@ struct AttendParams {
   CacheView c;
   const uint16_t* q;
   void* out;
-  float* part;           // partial results: per block two slots of rows * (D + 2) floats
+  float* part;           // partial results: per block two slots of rows * (D + 2) floats: reference, sum of weights, averages
   int64_t q_pitch;
   int T, heads, group;   // group = heads / kv_heads
   int rows, row_blocks;  // rows = T * group
@@ -170,7 +173,7 @@ struct AttendParams {
   int lead;              // what a segment costs beyond its tiles, in tiles (see Walk)
   int alone;             // a block per segment, no list, nothing to join: caches of a few tiles
   float scale_log2;      // softmax scale * log2(e)
-  float step;            // 8 / scale_log2: how far above the largest score a reference is set
+  float step;            // 8 / scale_log2
   int out_bf16;
 };
 
@@ -431,15 +434,15 @@ __device__ __forceinline__ void load_scales(uint32_t at, uint32_t (&w)[(NB + 3) 
     load_shared<NB / 4>(at, w);
   }
 }
-// Scale bytes as 2^(e - 127) times the power of two in both halves of `by`, NaN for 255: two a conversion, by way of bf16
+// Scale bytes of K as 2^(e - 127 - 24), NaN for 255: two a conversion, by way of bf16
 template <int NB>
-__device__ __forceinline__ void scale_floats(const uint32_t (&w)[(NB + 3) / 4], uint32_t by, float (&f)[NB]) {
+__device__ __forceinline__ void scale_floats(const uint32_t (&w)[(NB + 3) / 4], float (&f)[NB]) {
 #pragma unroll
   for (int i = 0; i < NB; i += 2) {
     uint32_t two;
     const uint16_t bytes = static_cast<uint16_t>(w[i >> 2] >> (8 * (i & 2)));
     asm("cvt.rn.bf16x2.ue8m0x2 %0, %1;" : "=r"(two) : "h"(bytes));
-    two = mul_bf16x2(two, by);
+    two = mul_bf16x2(two, 0x33803380u);
     f[i] = __uint_as_float(two << 16);
     f[i + 1] = __uint_as_float(two & 0xFFFF0000u);
   }
@@ -589,15 +592,10 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
         __half* dst = reinterpret_cast<__half*>(qfrag + ((i * 2 + (byte >> 1)) * NT + (r >> 3)) * 32 + (r & 7) * 4 + j);
         dst[(byte & 1) * 2 + half] = __float2half_rn(x[i] * f);
       }
-      if (lane == 0) qfac[r] = __int_as_float(e);
+      // scores carry the 2^(14 - e) of Q and the 2^-24 of K (queries beyond 2^117 may need more than fp32 has)
+      if (lane == 0) qfac[r] = fminf(__uint_as_float(static_cast<uint32_t>(min(e + 127 - 14 + 24, 254)) << 23) * p.scale_log2, 1.7014118e38f);
     }
     __syncthreads();
-    // Scores carry the 2^(14 - e) of Q, and the 2^-24 of K unless a query is so large (2^64) that it has no need of it: then
-    // scales of K below 2^-109, which 2^-24 would turn into zeros, still count.
-    const int e_max = __reduce_max_sync(0xFFFFFFFFu, lane < R ? __float_as_int(qfac[lane]) : -127);
-    const int k_down = e_max < 64 ? 24 : 0;
-    const uint32_t k_by = k_down ? 0x33803380u : 0x3F803F80u;   // 2^-24 or 1, twice as bf16
-
     // roof: what a row's weights refer to; a weight is 2^15 p = 2^((s - roof) cf + 15), roof -Inf until there is one.
     // top_e: the scale exponents that the blocks' results refer to, four to a word, 8 at least.
     float roof[NT][2], l[NT][2], cf[NT][2];
@@ -611,7 +609,7 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
         const int row = rb * R + n * 8 + tq * 2 + c;
         roof[n][c] = ninf;
         l[n][c] = 0.f;
-        cf[n][c] = __uint_as_float(static_cast<uint32_t>(__float_as_int(qfac[n * 8 + tq * 2 + c]) + 127 - 14 + k_down) << 23) * p.scale_log2;
+        cf[n][c] = qfac[n * 8 + tq * 2 + c];
         limit[n][c] = row < p.rows ? min(len, len - p.T + row_token(p, row) + 1) : seen;   // (rows past the end: anything)
         all_see = min(all_see, limit[n][c]);
         any_sees = max(any_sees, limit[n][c]);
@@ -656,8 +654,8 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
           uint32_t sa[kScaleWords], sb[kScaleWords];
           load_scales<NB>(grp + at_ks, sa);
           load_scales<NB>(grp + at_ks + 8 * NB, sb);
-          scale_floats<NB>(sa, k_by, fa[mt]);
-          scale_floats<NB>(sb, k_by, fb[mt]);
+          scale_floats<NB>(sa, fa[mt]);
+          scale_floats<NB>(sb, fb[mt]);
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -722,7 +720,7 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
             // (a step of 2^120 stands for more: all scores are the same to such a cf)
-            const float now = fmaxf(roof[n][c], top + fminf(8.f / cf[n][c], 1.329228e36f));
+            const float now = fmaxf(roof[n][c], top + fminf(__fdividef(8.f, cf[n][c]), 1.329228e36f));
             // (roof = -Inf, nothing seen so far: sum and result are zeros)
             const float f = now == roof[n][c] ? 1.f : ex2((roof[n][c] - now) * cf[n][c]);
             roof[n][c] = now;
@@ -946,18 +944,19 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const int r = n * 8 + tq * 2 + c;
-        const float adjust = rounded_off(roof[n][c], cf[n][c]);
         if (g == 0) {
           jm[warp * R + r] = roof[n][c] * cf[n][c];
-          jl[warp * R + r] = l[n][c] * adjust;
+          jl[warp * R + r] = l[n][c] * rounded_off(roof[n][c], cf[n][c]);
         }
+        const float inv = l[n][c] == 0.f ? 0.f : __fdividef(1.f, l[n][c]);
         float* row = reinterpret_cast<float*>(smem + warp * Cfg::kWarpRing) + r * Cfg::kAccPitch;
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
-          const float back = mx4_scale(top_e[i >> 2] >> (8 * (i & 3)) & 255u) * adjust;
+          const float back = mx4_scale(top_e[i >> 2] >> (8 * (i & 3)) & 255u);
 #pragma unroll
           for (int k = 0; k < 2; ++k)
-            *reinterpret_cast<float2*>(row + i * 32 + 4 * g + 2 * k) = make_float2(acc[n][i][k][c] * back, acc[n][i][k][2 + c] * back);
+            *reinterpret_cast<float2*>(row + i * 32 + 4 * g + 2 * k) =
+                make_float2(acc[n][i][k][c] * inv * back, acc[n][i][k][2 + c] * inv * back);
         }
       }
     __syncthreads();
@@ -970,28 +969,28 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
 #pragma unroll
       for (int w = 1; w < kWarps; ++w) top = fmaxf(top, jm[w * R + r]);
       const float base = top == __uint_as_float(0xFF800000u) ? 0.f : top;
-      float sum = 0.f;
+      float sum = 0.f, f[kWarps];
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) sum += f[w] = jl[w * R + r] * ex2(jm[w * R + r] - base);
+      const float inv = sum == 0.f ? 0.f : __fdividef(1.f, sum);
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
-        const float f = ex2(jm[w * R + r] - base);
         const float4 x = *reinterpret_cast<const float4*>(smem + w * Cfg::kWarpRing + (r * Cfg::kAccPitch + d) * 4);
-        sum += jl[w * R + r] * f;
-        o.x += x.x * f; o.y += x.y * f; o.z += x.z * f; o.w += x.w * f;
+        f[w] *= inv;
+        o.x += x.x * f[w]; o.y += x.y * f[w]; o.z += x.z * f[w]; o.w += x.w * f[w];
       }
       if (!whole) {
         *reinterpret_cast<float2*>(slot + r * (D + 2) + d + 2) = make_float2(o.x, o.y);
         *reinterpret_cast<float2*>(slot + r * (D + 2) + d + 4) = make_float2(o.z, o.w);
         if (d == 0) *reinterpret_cast<float2*>(slot + r * (D + 2)) = make_float2(top, sum);
       } else if (row < p.rows) {
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
         const int64_t to = out_row(p, b, h, row, D) + d;
         if (p.out_bf16)
           *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + to) =
-              make_uint2(pack_bf16x2(__float_as_uint(o.x * inv), __float_as_uint(o.y * inv)),
-                         pack_bf16x2(__float_as_uint(o.z * inv), __float_as_uint(o.w * inv)));
+              make_uint2(pack_bf16x2(__float_as_uint(o.x), __float_as_uint(o.y)), pack_bf16x2(__float_as_uint(o.z), __float_as_uint(o.w)));
         else
-          *reinterpret_cast<float4*>(static_cast<float*>(p.out) + to) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+          *reinterpret_cast<float4*>(static_cast<float*>(p.out) + to) = o;
       }
     }
   }
@@ -1037,12 +1036,27 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join(const AttendParam
     float top = ninf, sum = 0.f, o[NB];
 #pragma unroll
     for (int i = 0; i < NB; ++i) o[i] = 0.f;
-    const auto add = [&](float ref, float l, const float (&x)[NB]) {
-      const float t = fmaxf(top, ref), base = t == ninf ? 0.f : t;
-      const float fo = ex2(top - base), fn = ex2(ref - base);
-      sum = sum * fo + l * fn;
+    // the average so far and K parts, each with its weight in the sum of all
+    const auto add = [&](auto parts, const float2* ml, const float (*x)[NB]) {
+      constexpr int K = decltype(parts)::value;
+      float t = top, f[K];
 #pragma unroll
-      for (int i = 0; i < NB; ++i) o[i] = o[i] * fo + x[i] * fn;
+      for (int k = 0; k < K; ++k) t = fmaxf(t, ml[k].x);
+      const float base = t == ninf ? 0.f : t;
+      float fo = sum * ex2(top - base);
+      sum = fo;
+#pragma unroll
+      for (int k = 0; k < K; ++k) sum += f[k] = ml[k].y * ex2(ml[k].x - base);
+      const float inv = sum == 0.f ? 0.f : __fdividef(1.f, sum);   // (to 1 ulp; the sums are ordinary numbers)
+      fo *= inv;
+#pragma unroll
+      for (int k = 0; k < K; ++k) f[k] *= inv;
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        o[i] *= fo;
+#pragma unroll
+        for (int k = 0; k < K; ++k) o[i] = fmaf(x[k][i], f[k], o[i]);
+      }
       top = t;
     };
     if (n && live) {
@@ -1052,6 +1066,9 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join(const AttendParam
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const int64_t part = c + k * js.wpr;
+          ml[k] = make_float2(ninf, 0.f);
+#pragma unroll
+          for (int i = 0; i < NB; ++i) x[k][i] = 0.f;
           if (part <= c1) {
             const float* slot = p.part + ((part * 2 + (part == c0 ? 1 : 0)) * p.R + r) * (D + 2);
             ml[k] = *reinterpret_cast<const float2*>(slot);
@@ -1063,9 +1080,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join(const AttendParam
             }
           }
         }
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (c + k * js.wpr <= c1) add(ml[k].x, ml[k].y, x[k]);
+        add(std::integral_constant<int, 4>{}, ml, x);
       }
     }
     if (js.wpr > 1) {
@@ -1076,22 +1091,22 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join(const AttendParam
       __syncthreads();
       if (sub != 0) continue;
       for (int w = warp + 1; w < warp + js.wpr; ++w) {
-        float x[NB];
+        float x[1][NB];
 #pragma unroll
-        for (int i = 0; i < NB; ++i) x[i] = meet[w][lane * NB + i];
-        add(meet[w][D], meet[w][D + 1], x);
+        for (int i = 0; i < NB; ++i) x[0][i] = meet[w][lane * NB + i];
+        const float2 ml = make_float2(meet[w][D], meet[w][D + 1]);
+        add(std::integral_constant<int, 1>{}, &ml, x);
       }
     }
     if (!live) continue;
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
     const int64_t to = out_row(p, b, h, row, D) + lane * NB;
 #pragma unroll
     for (int i = 0; i < NB; i += 2) {
       if (p.out_bf16)
         *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + to + i) =
-            pack_bf16x2(__float_as_uint(o[i] * inv), __float_as_uint(o[i + 1] * inv));
+            pack_bf16x2(__float_as_uint(o[i]), __float_as_uint(o[i + 1]));
       else
-        *reinterpret_cast<float2*>(static_cast<float*>(p.out) + to + i) = make_float2(o[i] * inv, o[i + 1] * inv);
+        *reinterpret_cast<float2*>(static_cast<float*>(p.out) + to + i) = make_float2(o[i], o[i + 1]);
     }
   }
 }

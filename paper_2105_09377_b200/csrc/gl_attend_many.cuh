@@ -6,7 +6,8 @@
 // memory layouts of the MMA operands: K as [token][dim] (K-major B of S = Q K^T), V as [token][dim] too, which is the
 // MN-major B of O = P V.  Scores come back from tensor memory a row per thread, are turned into weights and go back
 // into the columns they came from, as the A operand of the second product.  The maximum that the weights refer to is
-// moved only when a row's scores exceed it, 2^8 above the last one, so that O is rarely rescaled.  MT = 2: while the softmax warps
+// moved only when a weight would pass 2^-8: then the largest one becomes 2^-16, so that O is rarely rescaled, and their
+// sum over all tokens is about 1 at most, so that O is not much larger than the values.  MT = 2: while the softmax warps
 // of one half work, the tensor core works for the other.
 // TERMS = 1 rounds the weights to bf16 (8 bits; the result is bf16 too); TERMS = 3 carries them as three bf16 terms
 // for fp32 results.
@@ -260,8 +261,8 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
             top = fmaxf(fmaxf(top, t1), fmaxf(t2, t3));
           }
         }
-        const bool move = top > roof;
-        const float new_roof = move ? top + p.step : roof;
+        const bool move = top > roof - p.step;        // (roof = -Inf: whenever the row sees something)
+        const float new_roof = move ? top + 2.f * p.step : roof;
         if (__any_sync(0xFFFFFFFFu, move) && tile > w.t0) {
           // O holds the tiles before this one: bring it to the new reference
           if (!mbar_wait(b_o + 8 * m, (it - 1) & 1u, abort_flag)) { ok = false; break; }
@@ -279,7 +280,7 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
         }
         roof = new_roof;
         const float down = roof == ninf ? 0.f : -roof;
-        float part[4] = {0.f, 0.f, 0.f, 0.f};
+        float part[2] = {0.f, 0.f};
         // (two copies of the loop: a test of `masked` per weight would cost as much as the weight)
         const auto weigh = [&](auto with_mask) {
 #pragma unroll 1
@@ -295,9 +296,9 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
                 a = there && 32 * j + i < open ? a : 0.f;
                 b = there && 32 * j + i + 1 < open ? b : 0.f;
               }
-              part[i & 2] += a;
-              part[(i & 2) + 1] += b;
               hi[i / 2] = pack_bf16x2(__float_as_uint(a), __float_as_uint(b));
+              part[0] += a;
+              part[1] += b;
               if (TERMS == 3) {
                 a -= __uint_as_float(hi[i / 2] << 16);
                 b -= __uint_as_float(hi[i / 2] & 0xFFFF0000u);
@@ -316,7 +317,7 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
         };
         if (masked) weigh(std::true_type{});
         else weigh(std::false_type{});
-        sum += (part[0] + part[1]) + (part[2] + part[3]);
+        sum += part[0] + part[1];
         tc_wait_store();
         tc_fence_before();
         __syncwarp();
@@ -327,10 +328,9 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
       if (!mbar_wait(b_o + 8 * m, (it - 1) & 1u, abort_flag)) { ok = false; break; }
       tc_fence_after();
       const bool whole = w.whole();
-      const float adjust = rounded_off(roof, cf);
-      const float inv = whole ? (sum == 0.f ? 0.f : 1.f / sum) : adjust;
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
       float* slot = w.slot(p, D) + static_cast<int64_t>(m * 128) * (D + 2);
-      if (!whole) *reinterpret_cast<float2*>(slot + r * (D + 2)) = make_float2(roof * cf, sum * adjust);
+      if (!whole) *reinterpret_cast<float2*>(slot + r * (D + 2)) = make_float2(roof * cf, sum * rounded_off(roof, cf));
       const int* nan_at = nan_from + (item & 3u) * NB;
       // 64 dims at a time (a pair of blocks), by way of the warp's rows of its Q tile, which no product reads any more:
       // written a row per lane, stored along the rows.  Columns (g * NB/2 + pair) * 8 + 2 i + half hold dims

@@ -81,3 +81,54 @@ def test_keys_near_the_end_of_the_range(gl, rows, n, d, bf16):
         checked += 1
     assert checked > rows / 2
     assert gl.gl_poll_device_status() == 0
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("power", [123, -100])
+@pytest.mark.parametrize("rows,n", [(4, 60), (12, 130), (28, 60), (40, 200), (4, 20000), (28, 3000), (40, 3000)])
+def test_values_near_the_ends_of_the_range(gl, rows, n, power, d, bf16):
+    """Values of 2^123 (up to 2^126) and of 2^-100: an average of them is as large as they are, so nothing may overflow or
+    get lost on the way."""
+    k, q = _bf16(1, (1, n, 1, d)), _bf16(3, (1, 1, rows, d), 1.5)
+    v = _bf16(2, (1, n, 1, d), 2.0 ** power)
+    cache, table, lengths = _stored(gl, k, v, 16)
+    got = gl.gl_attend_cache4(gl.AccessPattern(q, 3), cache, table, lengths, flags=gl.GL_OUT_BF16 if bf16 else 0)
+    got = got.tensor[0, 0].double().cpu().numpy()
+    kd, vd = (mx4.rounded(x[0, :, 0].double().cpu().numpy()) for x in (k, v))
+    qd = q[0, 0].double().cpu().numpy()
+    for h in range(rows):
+        s, p, ref, mag = _row(qd[h], kd, vd, d ** -0.5)
+        ds = (d / 16 + 6) * 2.0 ** -23 * d ** -0.5 * (np.abs(kd) @ np.abs(qd[h])).max()
+        rel = 2 * ds + 2.0 ** -20 + (n / 16 + 16) * 2.0 ** -23 + ((2.0 ** -8 if rows > 32 else 2.0 ** -10) if bf16 else 2.0 ** -20)
+        tol = rel * mag
+        lo, hi = (_to_bf16(ref - tol), _to_bf16(ref + tol)) if bf16 else (ref - tol, ref + tol)
+        assert ((got[h] >= lo) & (got[h] <= hi)).all(), (h, np.abs(got[h] - ref).max() / mag.min())
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("rows", [4, 12, 28, 40])
+def test_queries_near_the_ends_of_the_range(gl, rows, d, bf16):
+    """Queries of 2^120 (scores of up to 2^125, one token takes all) next to those of 2^-120 (scores that are all the same)."""
+    n = 200
+    k, v = _bf16(1, (1, n, 1, d)), _bf16(2, (1, n, 1, d))
+    size = np.resize([2.0 ** 120, 2.0 ** -120, 1.0], rows)
+    q = (torch.from_numpy(synth.normal(3, 1, (rows, d)) * size[:, None])).to(torch.bfloat16).cuda().view(1, 1, rows, d)
+    cache, table, lengths = _stored(gl, k, v, 16)
+    got = gl.gl_attend_cache4(gl.AccessPattern(q, 3), cache, table, lengths, flags=gl.GL_OUT_BF16 if bf16 else 0)
+    got = got.tensor[0, 0].double().cpu().numpy()
+    kd, vd = (mx4.rounded(x[0, :, 0].double().cpu().numpy()) for x in (k, v))
+    qd = q[0, 0].double().cpu().numpy()
+    for h in range(rows):
+        s, p, ref, mag = _row(qd[h], kd, vd, d ** -0.5)
+        ds = (d / 16 + 6) * 2.0 ** -23 * d ** -0.5 * (np.abs(kd) @ np.abs(qd[h])).max()
+        if size[h] > 1:
+            top = np.sort(s)[::-1]
+            if top[0] - top[1] < 4 * ds:
+                continue
+            ref, mag, ds = vd[s.argmax()], np.abs(vd[s.argmax()]), 0.0
+        rel = 2 * ds + 2.0 ** -20 + (n / 16 + 16) * 2.0 ** -23 + ((2.0 ** -8 if rows > 32 else 2.0 ** -10) if bf16 else 2.0 ** -20)
+        tol = rel * mag
+        lo, hi = (_to_bf16(ref - tol), _to_bf16(ref + tol)) if bf16 else (ref - tol, ref + tol)
+        assert ((got[h] >= lo) & (got[h] <= hi)).all(), (h, size[h], np.abs(got[h] - ref).max())
