@@ -382,6 +382,11 @@ __device__ __forceinline__ float rounded_off(float roof, float cf) {
   const float rest = fmaf(roof, cf, -(roof * cf));
   return fabsf(rest) < 1.f ? ex2(rest) : 1.f;
 }
+// lo += low half, hi += high half
+__device__ __forceinline__ void add_halves_f16(uint32_t two, float& lo, float& hi) {
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tadd.f32.f16 %0, l, %0;\n\tadd.f32.f16 %1, h, %1;\n\t}"
+      : "+f"(lo), "+f"(hi) : "r"(two));
+}
 // Token (0..15) of the group that row i of a 16-row fragment stands for: spreads the tokens that a warp reads in one
 // access over the banks.  Rows come in pairs (2i, 2i+1) -> (i, 4 + (i ^ 1)), the upper eight likewise.
 __device__ __forceinline__ int token_of_row(int i) {
@@ -741,13 +746,14 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
           for (int c = 0; c < 4; ++c) {
             const float w15 = ex2(fmaf(s[mt][n][c] - roof[n][c & 1], cf[n][c & 1], 15.f));
             s[mt][n][c] = masked && s[mt][n][c] == ninf ? 0.f : w15;
-            l[n][c & 1] += s[mt][n][c];
+            if (HILO) l[n][c & 1] += s[mt][n][c];
           }
 #pragma unroll
           for (int hf = 0; hf < 2; ++hf) {
             const float x = s[mt][n][2 * hf], y = s[mt][n][2 * hf + 1];
             const uint32_t packed = pack_f16x2(x, y);
             wh[mt][n][hf] = transpose8x8(packed);
+            if (!HILO) add_halves_f16(packed, l[n][0], l[n][1]);   // (the sum is that of the weights as they are used)
             if (HILO) {
               const __half2 r = *reinterpret_cast<const __half2*>(&packed);
               wl[mt][n][hf] = transpose8x8(pack_f16x2(x - __low2float(r), y - __high2float(r)));

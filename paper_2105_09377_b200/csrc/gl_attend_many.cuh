@@ -129,6 +129,11 @@ __device__ __forceinline__ void get(Held<NB, ITEMS>& x, int i, const uint8_t* co
     }
   }
 }
+// lo += low half, hi += high half
+__device__ __forceinline__ void add_halves_bf16(uint32_t two, float& lo, float& hi) {
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tadd.f32.bf16 %0, l, %0;\n\tadd.f32.bf16 %1, h, %1;\n\t}"
+      : "+f"(lo), "+f"(hi) : "r"(two));
+}
 // (a + b) * c of two values at a time
 __device__ __forceinline__ float2 add_mul2(float a0, float a1, float b, float c) {
   float2 d;
@@ -297,9 +302,11 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
                 b = there && 32 * j + i + 1 < open ? b : 0.f;
               }
               hi[i / 2] = pack_bf16x2(__float_as_uint(a), __float_as_uint(b));
-              part[0] += a;
-              part[1] += b;
-              if (TERMS == 3) {
+              if (TERMS == 1) {
+                add_halves_bf16(hi[i / 2], part[0], part[1]);   // (the sum is that of the weights as they are used)
+              } else {
+                part[0] += a;
+                part[1] += b;
                 a -= __uint_as_float(hi[i / 2] << 16);
                 b -= __uint_as_float(hi[i / 2] & 0xFFFF0000u);
                 mid[i / 2] = pack_bf16x2(__float_as_uint(a), __float_as_uint(b));

@@ -132,3 +132,36 @@ def test_queries_near_the_ends_of_the_range(gl, rows, d, bf16):
         tol = rel * mag
         lo, hi = (_to_bf16(ref - tol), _to_bf16(ref + tol)) if bf16 else (ref - tol, ref + tol)
         assert ((got[h] >= lo) & (got[h] <= hi)).all(), (h, size[h], np.abs(got[h] - ref).max())
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("t,heads", [(1, 8), (2, 8), (4, 8), (8, 8)])
+def test_rounded_weights_are_summed_as_they_are_used(gl, t, heads, d):
+    """One late token gets most of the weight, up to 2^7.9 times that of the first ones, so that its weight is no power of
+    two when it is rounded.  With weights w (1 + r), |r| <= r0, in both sums the result is off by
+    sum p r (V - out) / sum p (1 + r): nothing where the values agree.  r0: 2^-11 (fp16), 2^-8 (bf16, more than 32 rows)."""
+    rows = t * heads
+    n, loud = (230, 200) if rows > 32 else (64, 40)
+    sign = np.sign(synth.normal(3, 1, (d,)))
+    k = (synth.normal(4, 1, (n, d)) * 0.02).astype(np.float32)
+    k[loud] = sign
+    grid = np.array([1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+    v = np.tile(grid[np.random.default_rng(d).integers(0, 6, d)], (n, 1))
+    v[loud] = grid[np.random.default_rng(d + 1).integers(0, 6, d)]
+    v[:, ::32] = 6.0                         # (scales of 1: the values are stored as they are)
+    size = np.linspace(2.0, 7.9, rows) / (np.sqrt(d) * np.log2(np.e))
+    q = torch.from_numpy(size[:, None] * sign).to(torch.bfloat16).cuda().view(1, t, heads, d)
+    kt, vt = (torch.from_numpy(x).to(torch.bfloat16).cuda().view(1, n, 1, d) for x in (k, v))
+    cache, table, lengths = _stored(gl, kt, vt, 16)
+    # every row sees the loud token: the last `t` positions lie behind it
+    got = gl.gl_attend_cache4(gl.AccessPattern(q, 3), cache, table, lengths, flags=gl.GL_OUT_BF16).tensor[0].double().cpu().numpy()
+    kd, vd, qd = mx4.rounded(kt[0, :, 0].double().cpu().numpy()), mx4.rounded(vt[0, :, 0].double().cpu().numpy()), q[0].double().cpu().numpy()
+    r0 = 2.0 ** -8 if rows > 32 else 2.0 ** -11
+    for i in range(t):
+        for h in range(heads):
+            keep = n - t + i + 1
+            s, p, ref, mag = _row(qd[i, h], kd[:keep], vd[:keep], d ** -0.5)
+            # scores: D products in fp32, two roundings, an error e in a score moves p by e; ex2 to 2 ulp; sums of n / 16 terms
+            fp32 = 2 * (d / 16 + 6) * 2.0 ** -23 * np.abs(s).max() + 2.0 ** -20 + (n / 16 + 16) * 2.0 ** -23
+            tol = r0 / (1 - r0) * (p[:, None] * np.abs(vd[:keep] - ref)).sum(0) + fp32 * mag
+            assert ((got[i, h] >= _to_bf16(ref - tol)) & (got[i, h] <= _to_bf16(ref + tol))).all(), (i, h)
