@@ -341,7 +341,7 @@ GL_API int gl_cache4_read(const gl_cache4* cache, const gl_pages* at, gl_ap* k, 
 /* Attention of q, ((B, T, heads),(head_dim)) GL_BF16, over the cache: row (b, i, h) is token lengths[b] - T + i of its
  * sequence, sees the tokens up to and including itself and reads kv head h / (heads / kv_heads):
  *   out[b,i,h] = sum_t p_t V_t,  p = softmax_t(scale * q . K_t);  zeros for a row that sees nothing.
- * scale > 0 and finite; token_pitch as above; out is dense, GL_F32 or, with GL_OUT_BF16 in flags, GL_BF16.
+ * scale > 0, 2^127 at most; token_pitch as above; out is dense, GL_F32 or, with GL_OUT_BF16 in flags, GL_BF16.
  * Scores, softmax statistics and sums are fp32.  The weights p are rounded to fp16 (bf16 where more than 32 rows share a
  * kv head) when the result is bf16, and carried in two or three such terms when it is fp32.  Results repeat bit for bit.
  * `workspace`: gl_attend_cache4_workspace() bytes, 1024-byte aligned, scratch: calls that can overlap on the GPU need one

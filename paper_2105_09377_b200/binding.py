@@ -702,6 +702,7 @@ def gl_attend_cache4_workspace(q: AccessPattern, cache: Cache4) -> int:
 def _attend_args(q, cache, page_table, lengths, out, scale, flags, workspace):
     _on_gpu(q.tensor, cache.data, page_table, lengths, out.tensor, workspace)
     sq, pitch = _tokens_struct(q.tensor)
+    sq.access_ndim = q.access_ndim
     return (ctypes.byref(sq), pitch, ctypes.byref(_cache4_struct(cache)), ctypes.byref(_pages_struct(page_table, lengths)),
             float(scale), ctypes.byref(_struct(out)), flags, *_ws(workspace))
 

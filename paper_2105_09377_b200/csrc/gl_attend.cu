@@ -1310,7 +1310,7 @@ int gl_attend_cache4(const gl_ap* q, int64_t token_pitch, const gl_cache4* cache
   rc = check_tokens(q, cache, at, &pitch);
   if (rc) return rc;
   if (q->shape[2] % cache->kv_heads) return GL_ERR_SHAPE;
-  if (!(scale > 0.f) || !(scale <= 3.0e38f)) return GL_ERR_SHAPE;
+  if (!(scale > 0.f) || !(scale <= 1.7014118e38f)) return GL_ERR_SHAPE;   // (2^127: times log2(e) it is still finite)
   gl_ap want = *q;
   want.dtype = (flags & GL_OUT_BF16) ? GL_BF16 : GL_F32;
   rc = check_same_meta(want, out);

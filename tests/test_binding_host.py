@@ -169,3 +169,19 @@ def test_prepared_scratch_tells_torch_of_other_streams(gl, monkeypatch):
     for s in (None, _Stream(), None, _Stream()):
         call(s)
     assert told == [7]
+
+
+def test_attention_checks_the_split_and_the_scale(gl, monkeypatch):
+    monkeypatch.setattr(gl, "_on_gpu", lambda *t: None)
+    cache = gl.cache4_empty(2, 1, 16, 64, "cpu")
+    table, lengths = torch.zeros(1, 2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    out = gl.AccessPattern(torch.zeros(1, 3, 2, 64), 3)
+
+    def call(access, scale):
+        q = gl.AccessPattern(torch.zeros(1, 3, 2, 64, dtype=torch.bfloat16), access)
+        ws = torch.zeros(gl.gl_attend_cache4_workspace(q, cache) + 1024, dtype=torch.uint8)
+        return gl.LIB.gl_attend_cache4(*gl._attend_args(q, cache, table, lengths, out, scale, 0, ws), None)
+
+    assert call(2, 0.125) == 3 and call(4, 0.125) == 3              # ((B, T, heads),(head_dim)) and nothing else
+    for scale in (1.8e38, 2.5e38, 3.3e38):                          # times log2(e) these may leave fp32's range
+        assert call(3, scale) == 4
