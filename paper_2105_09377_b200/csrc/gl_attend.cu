@@ -5,6 +5,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cstring>
 #include <type_traits>
 
@@ -1235,15 +1236,17 @@ AttKernel pick_kernel(int64_t rows, int d, bool f32) {
 
 // Blocks of the persistent grid: what is resident at once.
 int att_grid(const AttKernel& k, int d, bool f32, int* grid) {
-  static int cached[64][3][5][2];   // per device; benign race: the calls are idempotent
+  static std::atomic<int> cached[64][3][5][2];   // per device, 0: not asked yet (threads may ask at once: the calls are idempotent)
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return GL_ERR_CUDA;
-  int& n = cached[dev][d == 64 ? 0 : d == 128 ? 1 : 2][k.rows <= 8 ? 0 : k.rows <= 16 ? 1 : k.rows <= 32 ? 2 : k.rows <= 128 ? 3 : 4][f32];
+  std::atomic<int>& known = cached[dev][d == 64 ? 0 : d == 128 ? 1 : 2][k.rows <= 8 ? 0 : k.rows <= 16 ? 1 : k.rows <= 32 ? 2 : k.rows <= 128 ? 3 : 4][f32];
+  int n = known.load(std::memory_order_acquire);
   if (!n) {
     if (cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem) != cudaSuccess) return GL_ERR_CUDA;
     int per = 0;
     if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, k.fn, k.threads, k.smem) != cudaSuccess || per < 1) return GL_ERR_CUDA;
     n = std::min(per, k.per_sm) * num_sms();
+    known.store(n, std::memory_order_release);
   }
   *grid = n;
   return GL_OK;

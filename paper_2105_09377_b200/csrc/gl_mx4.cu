@@ -14,6 +14,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cstring>
 
 #include "gl_internal.h"
@@ -959,14 +960,14 @@ struct TilePlanMx4 {
 template <int BN, int CTAS>
 int plan_tiles(const Mx4Operand& a, const Mx4Operand& b, void* out, uint32_t flags, TilePlanMx4* t) {
   using Cfg = MxCfg<BN, CTAS>;
-  static bool attr_set[64] = {false};   // per device; benign race: the calls are idempotent
-  static int resident[64] = {0};
+  static std::atomic<int> resident[64];   // per device, 0: not asked yet (threads may ask at once: the calls are idempotent)
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return GL_ERR_CUDA;
-  if (!attr_set[dev]) {
+  int at_once = resident[dev].load(std::memory_order_acquire);
+  if (!at_once) {
     if (cudaFuncSetAttribute(dot_mx4<BN, CTAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes) != cudaSuccess)
       return GL_ERR_CUDA;
-    int units = num_sms();
+    at_once = num_sms();
     if (CTAS == 2) {   // SMs pair up within a GPC: a persistent grid must not exceed what is resident at once
       cudaLaunchConfig_t cfg;
       std::memset(&cfg, 0, sizeof(cfg));
@@ -980,11 +981,10 @@ int plan_tiles(const Mx4Operand& a, const Mx4Operand& b, void* out, uint32_t fla
       cfg.dynamicSmemBytes = Cfg::kSmemBytes;
       cfg.attrs = &at;
       cfg.numAttrs = 1;
-      if (cudaOccupancyMaxActiveClusters(&units, dot_mx4<BN, CTAS>, &cfg) != cudaSuccess || units < 1) return GL_ERR_CUDA;
-      units = std::min(units, num_sms() / 2);
+      if (cudaOccupancyMaxActiveClusters(&at_once, dot_mx4<BN, CTAS>, &cfg) != cudaSuccess || at_once < 1) return GL_ERR_CUDA;
+      at_once = std::min(at_once, num_sms() / 2);
     }
-    resident[dev] = units;
-    attr_set[dev] = true;
+    resident[dev].store(at_once, std::memory_order_release);
   }
   Mx4Params& p = t->p;
   p.M = a.v.rows;
@@ -1000,7 +1000,7 @@ int plan_tiles(const Mx4Operand& a, const Mx4Operand& b, void* out, uint32_t fla
   p.tma_store = p.O % (p.out_bf16 ? 8 : 4) == 0 ? 1 : 0;
   p.div_tiles_n.set(p.tiles_n);
   t->out = out;
-  t->grid = CTAS * std::min(resident[dev], p.tiles_m * p.tiles_n);
+  t->grid = CTAS * std::min(at_once, p.tiles_m * p.tiles_n);
   if (!encode_codes(&t->ma, a, kTile) || !encode_codes(&t->mb, b, BN / CTAS) || !encode_scales(&t->msa, a) ||
       !encode_scales(&t->msb, b))
     return GL_ERR_CUDA;
@@ -1025,13 +1025,13 @@ struct FewPlan {
 // `fused`: A is still to be rounded, by the product's own blocks.
 template <int BN, bool FUSED>
 int plan_few(const Mx4Operand& a, const Mx4Operand& b, void* out, uint32_t flags, FewPlan* t) {
-  static bool attr_set[64] = {false};   // per device; benign race: the call is idempotent
+  static std::atomic<bool> attr_set[64];   // per device (threads may set it at once: the call is idempotent)
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return GL_ERR_CUDA;
-  if (!attr_set[dev]) {
+  if (!attr_set[dev].load(std::memory_order_acquire)) {
     if (cudaFuncSetAttribute(dot_mx4_few<BN, FUSED>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<BN, FUSED>::kSmemBytes) != cudaSuccess)
       return GL_ERR_CUDA;
-    attr_set[dev] = true;
+    attr_set[dev].store(true, std::memory_order_release);
   }
   FewParams& p = t->p;
   p.M = static_cast<int>(a.v.rows);
