@@ -1196,7 +1196,7 @@ int tokens_params(const gl_cache4* cache, const gl_ap* k, const gl_ap* v, int64_
 
 // Several items per thread only when every SM has blocks to hold.
 constexpr int kTokenItems = 2;
-bool several_items(const TokensParams& p) { return p.items >= 148u * 4u * 256u * kTokenItems; }
+bool several_items(const TokensParams& p) { return p.items >= static_cast<uint32_t>(num_sms()) * 4u * 256u * kTokenItems; }
 dim3 token_grid(const TokensParams& p, bool many) {
   const uint32_t per_block = 256u * (many ? kTokenItems : 1);
   return dim3((p.items + per_block - 1) / per_block);

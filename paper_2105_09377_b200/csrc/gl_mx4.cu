@@ -283,7 +283,7 @@ int quant_params(const Mx4View& v, int vals, QuantParams* p) {
 
 // Several items per thread only when every SM has blocks to hold.
 constexpr int kItemsPerThread = 4;
-bool many_items(const QuantParams& p) { return p.items >= 148u * 4u * 256u * kItemsPerThread; }
+bool many_items(const QuantParams& p) { return p.items >= static_cast<uint32_t>(num_sms()) * 4u * 256u * kItemsPerThread; }
 dim3 item_grid(const QuantParams& p) {
   const uint32_t per_block = 256u * (many_items(p) ? kItemsPerThread : 1);
   return dim3((p.items + per_block - 1) / per_block);
