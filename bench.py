@@ -375,6 +375,25 @@ def compact_rows(detail):
     return rows
 
 
+def kernel_source_key(path):
+    """A hash of a kernel file and of the headers beside it that it includes, directly or through one another."""
+    import hashlib
+    import re
+    folder, todo, seen = os.path.dirname(path), [os.path.basename(path)], set()
+    while todo:
+        name = todo.pop()
+        if name in seen or not os.path.exists(os.path.join(folder, name)):
+            continue
+        seen.add(name)
+        with open(os.path.join(folder, name), "rb") as f:
+            todo += re.findall(r'^#include "([^"]+)"', f.read().decode(), re.M)
+    h = hashlib.sha256()
+    for name in sorted(seen):
+        with open(os.path.join(folder, name), "rb") as f:
+            h.update(name.encode() + b"\0" + f.read() + b"\0")
+    return h.hexdigest()[:16]
+
+
 def run_gpu(args):
     import numpy as np
     import torch
@@ -506,15 +525,13 @@ def run_gpu(args):
     kernel_s = seconds / args.steps
     achieved = case.flops / kernel_s / 1e12
     # DRAM bytes per launch from the committed ncu capture of this kernel; the file names the kernel source it was
-    # taken on (a hash of csrc/gl_dot.cu), and the figure is dropped once the kernel has changed since
+    # taken on (see kernel_source_key), and the figure is dropped once the kernel has changed since
     traffic, traffic_source = None, None
     tpath = os.path.join(ROOT, "profiles", "dense_4096_dram_bytes_per_launch.txt")
     if os.path.exists(tpath):
         try:
             fields = open(tpath).read().split()
-            import hashlib
-            src = os.path.join(ROOT, "paper_2105_09377_b200", "csrc", "gl_dot.cu")
-            now = hashlib.sha256(open(src, "rb").read()).hexdigest()[:16]
+            now = kernel_source_key(os.path.join(ROOT, "paper_2105_09377_b200", "csrc", "gl_dot.cu"))
             if len(fields) >= 2 and fields[1] == now:
                 traffic = float(fields[0])
                 traffic_source = "profiles/dense_4096_dram_bytes_per_launch.txt (ncu, kernel source %s)" % now
