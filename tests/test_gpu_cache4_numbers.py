@@ -6,6 +6,7 @@ import torch
 
 from oracle import mx4
 from paper_2105_09377_b200 import synth
+from tests.test_gpu_cache4 import _to_bf16
 
 pytestmark = pytest.mark.gpu
 
@@ -14,12 +15,6 @@ pytestmark = pytest.mark.gpu
 def gl():
     from paper_2105_09377_b200 import binding
     return binding
-
-
-def _to_bf16(x):
-    """Rounded to eight significant bits, ties to even (float64 in and out)."""
-    m, e = np.frexp(x)
-    return np.ldexp(np.round(m * 256.0), e - 8)
 
 
 def _bf16(seed, shape, std=1.0):
@@ -165,3 +160,26 @@ def test_rounded_weights_are_summed_as_they_are_used(gl, t, heads, d):
             fp32 = 2 * (d / 16 + 6) * 2.0 ** -23 * np.abs(s).max() + 2.0 ** -20 + (n / 16 + 16) * 2.0 ** -23
             tol = r0 / (1 - r0) * (p[:, None] * np.abs(vd[:keep] - ref)).sum(0) + fp32 * mag
             assert ((got[i, h] >= _to_bf16(ref - tol)) & (got[i, h] <= _to_bf16(ref + tol))).all(), (i, h)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("page,d", [(48, 64), (48, 128), (80, 256), (112, 128)])
+@pytest.mark.parametrize("rows", [4, 40])
+def test_pages_of_other_sizes(gl, rows, page, d, bf16):
+    """Pages of a multiple of 16 tokens that is no power of two: they end inside a tile, at another place in every one."""
+    n = 613
+    k, v, q = _bf16(1, (2, n, 2, d)), _bf16(2, (2, n, 2, d)), _bf16(3, (2, 1, 2 * rows, d), 1.5)
+    cache, table, lengths = _stored(gl, k, v, page)
+    rk, rv = gl.gl_cache4_read(cache, n, table, lengths)
+    kd, vd = (mx4.rounded(x.double().cpu().numpy()) for x in (k, v))
+    assert np.array_equal(rk.double().cpu().numpy(), kd) and np.array_equal(rv.double().cpu().numpy(), vd)
+    got = gl.gl_attend_cache4(gl.AccessPattern(q, 3), cache, table, lengths, flags=gl.GL_OUT_BF16 if bf16 else 0).tensor
+    got, qd = got.double().cpu().numpy(), q.double().cpu().numpy()
+    for b in range(2):
+        for h in range(2 * rows):
+            s, p, ref, mag = _row(qd[b, 0, h], kd[b, :, h // rows], vd[b, :, h // rows], d ** -0.5)
+            ds = (d / 16 + 6) * 2.0 ** -23 * d ** -0.5 * (np.abs(kd[b, :, h // rows]) @ np.abs(qd[b, 0, h])).max()
+            rel = 2 * ds + 2.0 ** -20 + (n / 16 + 16) * 2.0 ** -23 + ((2.0 ** -8 if rows > 32 else 2.0 ** -10) if bf16 else 2.0 ** -20)
+            tol = rel * mag
+            lo, hi = (_to_bf16(ref - tol), _to_bf16(ref + tol)) if bf16 else (ref - tol, ref + tol)
+            assert ((got[b, 0, h] >= lo) & (got[b, 0, h] <= hi)).all(), (b, h)
