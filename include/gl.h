@@ -267,8 +267,8 @@ GL_API int gl_compute_relu(const gl_ap* in, gl_ap* out, void* stream);
  *          low half; codes past K are zero.
  *   scale: gl_mx4_scale_bytes() bytes; tiles of 128 rows x 4 blocks, 512 bytes each, row tiles outermost; row r and
  *          block b of a tile at byte (r % 32) * 16 + (r / 32) * 4 + b.
- * Both device pointers are 16-byte aligned.  Size limits of all calls: rows * ceil(K/128)*16 < 2^31 (else
- * GL_ERR_UNSUPPORTED); nothing else is assumed of K or of the rows. */
+ * Both device pointers are 16-byte aligned.  Size limits (else GL_ERR_UNSUPPORTED): fewer than 2^31 - 256 rows, K <= 2^30, and
+ * for what a call rounds or widens rows * ceil(K/128)*16 < 2^31; nothing else is assumed of K or of the rows. */
 typedef struct {
   void* data;
   void* scale;
@@ -317,7 +317,8 @@ typedef struct {
 /* Where the tokens of a batch lie.  Token t of sequence b is token t % page_tokens of page
  * page_table[b * table_width + t / page_tokens].  lengths[b] counts the tokens of sequence b, those of this call
  * included.  Both arrays are in DEVICE memory and cannot be checked by the host: lengths are taken as
- * 0..table_width * page_tokens, a token on a page that does not exist is not stored, reads as zeros and is not seen. */
+ * 0..table_width * page_tokens, a token on a page that does not exist is not stored, reads as zeros and is not seen.
+ * The calls read them while they run: like every input they must not change until the call has ended on the GPU. */
 typedef struct {
   const int32_t* page_table;
   const int32_t* lengths;
@@ -342,8 +343,12 @@ GL_API int gl_cache4_read(const gl_cache4* cache, const gl_pages* at, gl_ap* k, 
  * sequence, sees the tokens up to and including itself and reads kv head h / (heads / kv_heads):
  *   out[b,i,h] = sum_t p_t V_t,  p = softmax_t(scale * q . K_t);  zeros for a row that sees nothing.
  * scale > 0, 2^127 at most; token_pitch as above; out is dense, GL_F32 or, with GL_OUT_BF16 in flags, GL_BF16.
- * Scores, softmax statistics and sums are fp32.  The weights p are rounded to fp16 (bf16 where more than 32 rows share a
- * kv head) when the result is bf16, and carried in two or three such terms when it is fp32.  Results repeat bit for bit.
+ * Scores, softmax statistics and sums are fp32.  The weights p are rounded when the result is bf16, to fp16 or, where more
+ * than 32 rows share a kv head, to bf16, and their sum is that of the rounded ones; for fp32 results they are carried in two
+ * such terms (three of bf16).  fp16 ends at 2^-24: with up to 32 rows per kv head every weight may besides be off by 2^-32 of
+ * the row's largest (below 2^-31 of it a weight is nothing), which shows where values of next to no weight are very large.
+ * Keys, values and queries may lie anywhere in bf16's range as long as the scores, before and after `scale`, and sum |p V|
+ * stay in fp32's; with up to 32 rows, blocks of keys with a scale below 2^-109 count as zeros.  Results repeat bit for bit.
  * `workspace`: gl_attend_cache4_workspace() bytes, 1024-byte aligned, scratch: calls that can overlap on the GPU need one
  * each. */
 GL_API int gl_attend_cache4(const gl_ap* q, int64_t token_pitch, const gl_cache4* cache, const gl_pages* at, float scale,

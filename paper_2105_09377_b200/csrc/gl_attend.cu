@@ -153,8 +153,11 @@ __global__ void __launch_bounds__(256) cache4_read(uint16_t* __restrict__ k, uin
 // nothing is larger than the values themselves (weights of up to 2^15 over many tokens took values beyond 2^100 to Inf).
 //
 // 64 sequences of 4096 tokens, 32 heads over 8 of 128: 75 us, 3.8 TB/s of cache (0.58 of the copy rate), bound by issue: about
-// 600 instructions per 32 tokens and warp, of which 128 convert codes and 32 are matrix instructions, at half an
-// instruction per cycle and scheduler.  Four blocks per SM (128 registers) instead of three: 93 us against 88 us.
+// 610 instructions per 32 tokens and warp, of which 128 convert codes and 32 are matrix instructions, at 0.55 instructions
+// per cycle and scheduler.  Four blocks per SM (128 registers) instead of three: 95 us.  fp32 results 82 us.
+// 32 rows per kv head (NT = 4, 255 registers, some spilled): 32 sequences of 4096 tokens, 64 heads over 8, 4 tokens each:
+// 106 us, fp32 results 134 us.  256-wide heads, 16 rows (NT = 2, some spilled), 32 sequences: 114 us and 161 us; 8 rows 76 and
+// 80 us.
 
 constexpr int kSubTok = 32;       // tokens that a warp computes with at a time
 constexpr int kWarps = 4;
@@ -189,8 +192,13 @@ __device__ __forceinline__ int seen_tiles(const AttendParams& p, int len, int rb
 
 // Entries of the work list for a row block and for one kv head of sequence b: its tiles, with `lead` empty entries before
 // them that stand for what every segment costs (fragments of Q, filling the ring, joining the warps).  Without them a
-// block that meets many short sequences gets as many tiles as the others and ends last (16384 and 32 tokens in turn: 66 us,
-// 45 us with eight of them, as for the long sequences alone).
+// block that meets many short sequences gets as many tiles as the others and ends last.  One token per sequence, us with none,
+// 4, 8, 16 and 32 empty entries:
+//   16 sequences of 17 .. 16384 tokens, 128 wide: 79, 54, 46, 47, 50;  64 wide: 53, 38, 32, 33, 35;  256 wide: 142, 91, 86, 79, 81
+//   64 sequences of 100 .. 2000 tokens:           57, 39, 35, 36, 37;           41, 29, 27, 27, 28;            126, 95, 81, 71, 71
+//   32 sequences of 4096 tokens:                  47, 45, 46, 49, 54;           33, 32, 33, 35, 38;            77, 77, 76, 77, 78
+// (so 8, and 16 for 256-wide heads).  attend_many has one; none would cost 3 to 25 % (two prompts of 512 tokens behind 5001 and
+// 8192: 181 us against 174), two or four would gain on ragged prompts (168 and 164 us).
 __device__ __forceinline__ int seen_entries(const AttendParams& p, int len, int rb) {
   const int n = seen_tiles(p, len, rb);
   return n ? n + p.lead : 0;
@@ -483,7 +491,7 @@ struct AttCfg {
   static constexpr int D = 32 * NB;
   static constexpr int R = 8 * NT;
   // Tokens per tile (what a warp waits for and asks for at a time) and tiles in a warp's ring: 64 and 2, but 32 and 3 for
-  // 256-wide heads, whose rings would leave room for one block per SM (32 x 4096 tokens: 98 us, 81 us with two blocks).
+  // 256-wide heads, whose rings would leave room for one block per SM (32 x 4096 tokens: 96 us, 77 us with two blocks).
   static constexpr int kTileTok = NB == 8 ? 32 : 64;
   static constexpr int kStagesAt = NB == 8 ? 3 : 2;
   static constexpr int kStage = kTileTok / kGroup * group_bytes(D);  // one tile
@@ -599,7 +607,8 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
         dst[(byte & 1) * 2 + half] = __float2half_rn(x[i] * f);
       }
       // scores carry the 2^(14 - e) of Q and the 2^-24 of K (queries beyond 2^117 may need more than fp32 has)
-      if (lane == 0) qfac[r] = fminf(__uint_as_float(static_cast<uint32_t>(min(e + 127 - 14 + 24, 254)) << 23) * p.scale_log2, 1.7014118e38f);
+      if (lane == 0)
+        qfac[r] = fminf(__uint_as_float(static_cast<uint32_t>(min(e + 127 - 14 + 24, 254)) << 23) * p.scale_log2, 1.7014118e38f);
     }
     __syncthreads();
     // roof: what a row's weights refer to; a weight is 2^15 p = 2^((s - roof) cf + 15), roof -Inf until there is one.
@@ -879,7 +888,8 @@ __global__ void __launch_bounds__(kWarps * 32) attend_cache4(const AttendParams 
                     f2[mt][hf] |= (15u - (top - e)) << (10 + 16 * k);
                     e = 256u;
                   }
-                  if (e < 255u) rest = max(rest, e);   // (blocks of zeros have e = 0: they add nothing)
+                  // (e = 0 next to a larger scale: zeros, or values below 2^-124, which are left out here)
+                  if (e < 255u) rest = max(rest, e);
                 }
               }
             rest = __reduce_max_sync(0xFFFFFFFFu, rest);
@@ -1348,9 +1358,9 @@ int gl_attend_cache4(const gl_ap* q, int64_t token_pitch, const gl_cache4* cache
   // (no more than a segment can have: a block that takes several short segments takes them one after the other)
   p.lead = k.lead;
   p.min_share = k.lead + std::min<int>(k.min_share, (p.c.capacity + k.tile - 1) / k.tile);
-  // A cache of at most four tiles per sequence: a block per segment, one launch (8 sequences of 100 tokens, 8 heads: 12.3 us
-  // with the list and the joining kernel, 7.8 us without).  Longer ones have warps with several tiles, which the list
-  // spreads over the blocks.
+  // A cache of at most four tiles per sequence: a block per segment, one launch (8 sequences of 100 tokens, 8 heads: 11.2 us
+  // with the list and the joining kernel, 7.0 us without; 64 of 256, 32 heads: 19.3 and 12.1).  Longer ones have warps with
+  // several tiles, which the list spreads over the blocks.
   p.alone = p.c.capacity <= kAloneTiles * k.tile ? 1 : 0;
   const int64_t blocks = p.alone ? segments : p.grid;
   if (launch_pdl(k.fn, dim3(static_cast<unsigned>(blocks)), dim3(static_cast<unsigned>(k.threads)), static_cast<size_t>(k.smem), st, 1, p) !=

@@ -12,8 +12,8 @@
 // TERMS = 1 rounds the weights to bf16 (8 bits; the result is bf16 too); TERMS = 3 carries them as three bf16 terms
 // for fp32 results.
 //
-// 512 tokens behind 5001 and 8192 cached ones, 32 heads over 8 of 128, channels of unequal size: 178 us, 600 TFLOP/s, 0.36
-// of the measured bf16 rate.  Per pair of 128-row tiles and 128 tokens (5.5 k cycles): 2 k of matrix instructions; the
+// 512 tokens behind 5001 and 8192 cached ones, 32 heads over 8 of 128, channels of unequal size: 175 us, 610 TFLOP/s, 0.37
+// of the measured bf16 rate; fp32 results 369 us.  Heads 64 wide 146 us, 256 wide 500 us, fp32 results 674 us.  Per pair of 128-row tiles and 128 tokens (5.5 k cycles): 2 k of matrix instructions; the
 // exponentials of 256 rows take 2 k cycles of their unit; a widening warp is busy 4.2 k (1.3 k each for K and V, 1.6 k to ask
 // for the next tile).  What is left is waiting for one another: the scores of a half are only there after its turn
 // on the tensor core.  Before: widening by four warps with a condition per word 259 us.

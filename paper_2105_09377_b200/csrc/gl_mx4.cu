@@ -660,12 +660,19 @@ dot_mx4(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUten
 // A as the N side (BN = 16 to 128 of them), and K cut over the S blocks of a cluster so that the loads of all SMs are in
 // flight: the blocks' partial sums meet in distributed shared memory, added in rank order.  One tile per block, two
 // blocks per SM.  While the kernel that rounds A is still running the weights are on their way into L2.
-// 8192 x 8192 weights (36 MB): 7.8 us for one row, 8.7 us for 32, 13 us for 64; a launch that does nothing is 2 us of it
-// and filling the machine 2 more.
+// 8192 x 8192 weights (36 MB) in L2, in a graph: 6.9 us for one row, 8.8 us for 16, 10.3 us for 64; weights that are not in L2,
+// one row: 9.2 us, 3.9 TB/s of HBM.  A launch that does nothing is 2 us of it and filling the machine 2 more.
 
 // At most kFuseRows rows (FUSED): the blocks round A themselves, each its own stretch of K, straight into operand order, while
-// the first weights are on their way: one launch.  (Through 8192 x 8192: one row 7.8 us against 10.1 us with a launch of
-// its own for the rounding, four rows 9.4 against 9.9; with more rows the repeated rounding costs more than the launch.)
+// the first weights are on their way: one launch.  Fused against a launch of its own for the rounding, us:
+//   K x O            1 row          4 rows         8 rows         16 rows
+//   1024 x 1024      2.9 / 4.1      3.0 / 4.3      3.4 / 4.3      4.4 / 4.5
+//   3136 x 1000      3.9 / 4.6      3.9 / 4.7      4.7 / 4.8      6.0 / 5.0
+//   4096 x 4096      5.1 / 6.5      5.6 / 6.5      6.7 / 6.8      8.1 / 7.0
+//   2048 x 8192      4.6 / 5.7      5.2 / 5.7      6.0 / 5.8      7.5 / 6.0
+//   8192 x 8192      6.9 / 8.9      9.1 / 8.7      11.6 / 8.6     16.9 / 8.8
+// What every block repeats is rows x K blocks of a rank; up to four rows it is no more than the launch, but for the last line's
+// four rows, which lose 5 %.
 constexpr int kFuseRows = 4;
 constexpr int kFuseBlocks = 12;   // K blocks of A that a block has room for
 
@@ -1099,8 +1106,10 @@ int product(const Mx4Operand& a, const Mx4Operand& b, gl_ap* out, uint32_t flags
   if (a.v.rows <= 64) return product_few<64>(a, b, out, flags, st, pre);
   if (a.v.rows <= 128) return product_few<128>(a, b, out, flags, st, pre);
   // 256 x 256 tiles on pairs of SMs move half the bytes per flop of 128 x 128 tiles, but there are a quarter as many.  A
-  // round of them takes one and a half times as long: 768 x 4096 x 4096 (2 rounds or 1) 14.2 us single, 11.4 us in pairs;
-  // 384 x 4096 x 4096 (1 or 1) 9.1 us single, 10.8 us in pairs; 16384 x 8192 x 8192 532 and 360 us.
+  // round of them takes one and a half times as long.  bf16 results, single / pairs, us: 1024 x 1024 x 1024 4.5 / 5.9;
+  // 256, 512, 768 and 1024 rows through 4096 x 4096 8.1 / 9.4, 8.3 / 9.5, 13.1 / 10.2, 13.3 / 10.4; 129, 256, 384 and 1024 rows
+  // through 8192 x 8192 12.9 / 14.1, 13.0 / 14.1, 22.5 / 15.1, 41.8 / 25.2; 8192 x 2048 x 2048 22.2 / 17.2; 4096^3 38.2 / 26.4;
+  // fp32 results alike.  The rule takes the shorter one in all of them.
   TilePlanMx4 t;
   const auto tiles = [&](int64_t side) { return ((a.v.rows + side - 1) / side) * ((b.v.rows + side - 1) / side); };
   const auto rounds = [](int64_t n, int64_t at_once) { return (n + at_once - 1) / at_once; };
