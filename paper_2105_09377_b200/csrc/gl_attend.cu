@@ -385,10 +385,10 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
   return d;
 }
-// What brings sums that refer to r = `roof` times `cf` to its rounded value, which is what the joining goes by.  (Beyond
-// 2^24 r says no more than which part is ahead.)
-__device__ __forceinline__ float rounded_off(float roof, float cf) {
-  const float rest = fmaf(roof, cf, -(roof * cf));
+// What brings sums that refer to the exact ref cf to its rounded value, which is what the joining goes by.  (Beyond 2^24 that
+// says no more than which part is ahead.)
+__device__ __forceinline__ float rounded_off(float ref, float cf) {
+  const float rest = fmaf(ref, cf, -(ref * cf));
   return fabsf(rest) < 1.f ? ex2(rest) : 1.f;
 }
 // lo += low half, hi += high half

@@ -7,8 +7,9 @@
 // MN-major B of O = P V.  Scores come back from tensor memory a row per thread, are turned into weights and go back
 // into the columns they came from, as the A operand of the second product.  The maximum that the weights refer to is
 // moved only when a weight would pass 2^-8: then the largest one becomes 2^-16, so that O is rarely rescaled, and their
-// sum over all tokens is about 1 at most, so that O is not much larger than the values.  MT = 2: while the softmax warps
-// of one half work, the tensor core works for the other.
+// sum over all tokens is about 1 at most, so that O is not much larger than the values.  It is one of the scores, subtracted
+// before the product with the softmax scale, two values to an instruction: scores of any size keep their differences.
+// MT = 2: while the softmax warps of one half work, the tensor core works for the other.
 // TERMS = 1 rounds the weights to bf16 (8 bits; the result is bf16 too); TERMS = 3 carries them as three bf16 terms
 // for fp32 results.
 //
@@ -134,15 +135,15 @@ __device__ __forceinline__ void add_halves_bf16(uint32_t two, float& lo, float& 
   asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tadd.f32.bf16 %0, l, %0;\n\tadd.f32.bf16 %1, h, %1;\n\t}"
       : "+f"(lo), "+f"(hi) : "r"(two));
 }
-// (a + b) * c of two values at a time
-__device__ __forceinline__ float2 add_mul2(float a0, float a1, float b, float c) {
-  float2 d;
-  asm("{\n\t.reg .b64 a, b, c;\n\t"
-      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %4};\n\tmov.b64 c, {%5, %5};\n\t"
-      "add.rn.f32x2 a, a, b;\n\tmul.rn.f32x2 a, a, c;\n\t"
+// (a + b) * c + d of two values at a time
+__device__ __forceinline__ float2 add_mul_add2(float a0, float a1, float b, float c, float d) {
+  float2 y;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\t"
+      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %4};\n\tmov.b64 c, {%5, %5};\n\tmov.b64 d, {%6, %6};\n\t"
+      "add.rn.f32x2 a, a, b;\n\tfma.rn.f32x2 a, a, c, d;\n\t"
       "mov.b64 {%0, %1}, a;\n\t}"
-      : "=f"(d.x), "=f"(d.y) : "f"(a0), "f"(a1), "f"(b), "f"(c));
-  return d;
+      : "=f"(y.x), "=f"(y.y) : "f"(a0), "f"(a1), "f"(b), "f"(c), "f"(d));
+  return y;
 }
 // A token that does not exist or is not seen by any row.
 template <int NB, int ITEMS>
@@ -238,7 +239,7 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
         if (lane == 0) mbar_arrive(b_q + 8 * m);
       }
       const int limit = live ? min(w.len, w.len - p.T + row_token(p, row) + 1) : 0;
-      float roof = ninf, sum = 0.f;   // weights are 2^((s - roof) cf)
+      float ref = ninf, sum = 0.f;   // weights are 2^((s - ref) cf - 16)
       for (int tile = w.t0; tile < w.t1; ++tile, ++it) {
         if (!mbar_wait(b_s + 8 * m, it & 1u, abort_flag)) { ok = false; break; }
         tc_fence_after();
@@ -266,13 +267,12 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
             top = fmaxf(fmaxf(top, t1), fmaxf(t2, t3));
           }
         }
-        const bool move = top > roof - p.step;        // (roof = -Inf: whenever the row sees something)
-        const float new_roof = move ? top + 2.f * p.step : roof;
+        const bool move = top > ref + p.step;         // (ref = -Inf: whenever the row sees something)
         if (__any_sync(0xFFFFFFFFu, move) && tile > w.t0) {
           // O holds the tiles before this one: bring it to the new reference
           if (!mbar_wait(b_o + 8 * m, (it - 1) & 1u, abort_flag)) { ok = false; break; }
           tc_fence_after();
-          const float f = move ? ex2((roof - new_roof) * cf) : 1.f;
+          const float f = move ? ex2((ref - top) * cf) : 1.f;
           sum *= f;
 #pragma unroll 1
           for (int j = 0; j < D / 16; ++j) {
@@ -283,8 +283,8 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
             tc_store_16cols(o_col + 16 * j, x);
           }
         }
-        roof = new_roof;
-        const float down = roof == ninf ? 0.f : -roof;
+        if (move) ref = top;
+        const float down = ref == ninf ? 0.f : -ref;
         float part[2] = {0.f, 0.f};
         // (two copies of the loop: a test of `masked` per weight would cost as much as the weight)
         const auto weigh = [&](auto with_mask) {
@@ -294,7 +294,7 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
             tc_load_32cols(s_col + 32 * j, x);
 #pragma unroll
             for (int i = 0; i < 32; i += 2) {
-              const float2 y = add_mul2(__uint_as_float(x[i]), __uint_as_float(x[i + 1]), down, cf);
+              const float2 y = add_mul_add2(__uint_as_float(x[i]), __uint_as_float(x[i + 1]), down, cf, -16.f);
               float a = ex2(y.x), b = ex2(y.y);
               if constexpr (decltype(with_mask)::value) {
                 const bool there = groups >> (2 * j + (i >> 4)) & 1u;
@@ -337,7 +337,7 @@ __global__ void __launch_bounds__(ManyCfg<NB, TERMS>::kThreads, 1) attend_many(c
       const bool whole = w.whole();
       const float inv = sum == 0.f ? 0.f : 1.f / sum;
       float* slot = w.slot(p, D) + static_cast<int64_t>(m * 128) * (D + 2);
-      if (!whole) *reinterpret_cast<float2*>(slot + r * (D + 2)) = make_float2(roof * cf, sum * rounded_off(roof, cf));
+      if (!whole) *reinterpret_cast<float2*>(slot + r * (D + 2)) = make_float2(ref * cf, sum * rounded_off(ref, cf));
       const int* nan_at = nan_from + (item & 3u) * NB;
       // 64 dims at a time (a pair of blocks), by way of the warp's rows of its Q tile, which no product reads any more:
       // written a row per lane, stored along the rows.  Columns (g * NB/2 + pair) * 8 + 2 i + half hold dims
