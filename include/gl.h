@@ -95,6 +95,7 @@ typedef struct {
                                       * must then be GL_BF16.  Sums are still carried in fp32; the rounding is
                                       * the last step, after relu.  Lets the next layer read its operand as is
                                       * and halves the bytes written. */
+#define GL_ROTATE_BACK 0x10u         /* gl_compute_rotate only: turn by the negative angles */
 #define GL_DOT_GENERAL_KERNEL 0x100u /* skip the tensor-core path: run the general kernel, which
                                         takes any shape and sums each window in index order      */
 
@@ -354,6 +355,97 @@ GL_API int gl_cache4_read(const gl_cache4* cache, const gl_pages* at, gl_ap* k, 
 GL_API int gl_attend_cache4(const gl_ap* q, int64_t token_pitch, const gl_cache4* cache, const gl_pages* at, float scale,
                             gl_ap* out, uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
 GL_API size_t gl_attend_cache4_workspace(const gl_ap* q, const gl_cache4* cache);
+
+/* ----------------------------------------------------------------------- */
+/* Operands held in 8 bits (F8; not in the paper)                            */
+/* ----------------------------------------------------------------------- */
+
+/* A pattern of shape S_A ++ S_C whose items (the prod(S_C) = K values of one access index) are cut into blocks of 128
+ * consecutive values.  A block is 128 E4M3 codes (sign, 4 bits of exponent, 3 of mantissa, magnitudes up to 448) and one E8M0
+ * scale: value = code * 2^(scale - 127), scale 255 = NaN for the whole block.
+ *   data:  gl_f8_data_bytes() bytes; one row per item of ceil(K/16)*16 bytes, codes past K are zero.
+ *   scale: gl_f8_scale_bytes() bytes; tiles of 128 rows x 4 blocks, 512 bytes each, row tiles outermost; row r and
+ *          block b of a tile at byte (r % 32) * 16 + (r / 32) * 4 + b.
+ * Both device pointers are 16-byte aligned.  Size limits (else GL_ERR_UNSUPPORTED): fewer than 2^31 - 256 rows, K <= 2^30,
+ * rows * (ceil(K/128) + 1) < 2^31. */
+typedef struct {
+  void* data;
+  void* scale;
+  int32_t ndim;
+  int32_t access_ndim;
+  int64_t shape[GL_MAX_DIMS];
+} gl_f8;
+
+/* Bytes of the two arrays (0 on an invalid shape). */
+GL_API size_t gl_f8_data_bytes(const gl_f8* a);
+GL_API size_t gl_f8_scale_bytes(const gl_f8* a);
+
+/* Rounds `in` (GL_F32 or GL_BF16) to `out`, which carries the same shape.  The scale of a block is the smallest power of two,
+ * 2^-127 at least, that its largest magnitude divided by it does not exceed 448; the quotients are rounded to the nearest code,
+ * ties to the even mantissa.  A block that holds an Inf or a NaN becomes NaN as a whole. */
+GL_API int gl_f8_quantize(const gl_ap* in, gl_f8* out, void* stream);
+
+/* The values of `in` as `out`.  GL_F32 holds every one exactly, GL_BF16 those of scales from 2^-124 on (smaller ones are rounded);
+ * a value that its rounding took to 2^128 is Inf. */
+GL_API int gl_f8_dequantize(const gl_f8* in, gl_ap* out, void* stream);
+
+/* compute dotProd (cartProd a0 a1) of two F8 patterns of the same compute shape: ((m..),(k..)), ((o..),(k..)) ->
+ * ((m.., o..),()), sums in fp32, on the tensor cores' block-scaled 8-bit products.  flags: GL_EPILOGUE_RELU (NaN stays
+ * NaN), GL_OUT_BF16; `out` is GL_F32 or, with GL_OUT_BF16, GL_BF16. */
+GL_API int gl_cartesian_dot_f8(const gl_f8* a0, const gl_f8* a1, gl_ap* out, uint32_t flags, void* stream);
+
+/* The same with the left operand given as GL_F32 or GL_BF16 and rounded to F8 by the call (a dense layer: activations
+ * a0, weights a1 laid out once by gl_f8_quantize).  The result does not depend on how many rows a0 has beyond the
+ * order of the sums.  `workspace`: gl_dense_f8_workspace() bytes, 1024-byte aligned, scratch: calls that can overlap on
+ * the GPU need one each. */
+GL_API int gl_dense_f8(const gl_ap* a0, const gl_f8* a1, gl_ap* out, uint32_t flags, void* workspace,
+                       size_t workspace_bytes, void* stream);
+GL_API size_t gl_dense_f8_workspace(const gl_ap* a0, const gl_f8* a1);
+
+/* ----------------------------------------------------------------------- */
+/* Norm and positions (not in the paper)                                     */
+/* ----------------------------------------------------------------------- */
+
+/* compute norm_rms: every item h = x + residual divided by its root mean square,
+ *   out = h / sqrt(mean(h^2) + eps) * weight,   sum = h rounded to its type.
+ * x ((a..),(c..)) with c not empty, GL_F32 or GL_BF16; `residual` (NULL: none) and `sum` (NULL: not wanted; only with a
+ * residual) of the same shape and of one type, GL_F32 or GL_BF16, which may differ from x's; `weight` (NULL: ones)
+ * ((),(c..)), GL_F32 or GL_BF16; eps >= 0 and finite.  out: the shape of x, GL_F32, GL_BF16 or F8.  The norm is that of the
+ * unrounded h, in fp32 throughout; squares have to stay in fp32's range.  `sum` may be `residual` itself, or x where the
+ * types agree, and `out` may be x (or `residual`, if that is not `sum`) where the types agree; other overlaps are not allowed.
+ * Size limits as for F8.  Results repeat bit for bit. */
+GL_API int gl_compute_norm_rms(const gl_ap* x, const gl_ap* residual, const gl_ap* weight, float eps, gl_ap* sum, gl_ap* out,
+                               void* stream);
+GL_API int gl_compute_norm_rms_f8(const gl_ap* x, const gl_ap* residual, const gl_ap* weight, float eps, gl_ap* sum, gl_f8* out,
+                                  void* stream);
+
+/* Rotary positions.  The first 2 * pairs values of a head form pairs, (i, pairs + i) or, `adjacent`, (2i, 2i + 1); pair i belongs
+ * to axis axis[i] and is turned by step[i] * position / 2^64 turns.  gl_rotary_plan fills the struct, which a caller may
+ * change afterwards (other splits of the pairs between the axes, other frequencies). */
+#define GL_MAX_PAIRS 128
+typedef struct {
+  int32_t pairs;                  /* 1..GL_MAX_PAIRS                                       */
+  int32_t axes;                   /* position axes (time, height, width, ..), 1..pairs     */
+  int32_t adjacent;               /* 0 or 1                                                */
+  int32_t reserved_;
+  uint64_t step[GL_MAX_PAIRS];    /* 2^64 * turns per position, modulo 2^64                */
+  uint8_t axis[GL_MAX_PAIRS];
+} gl_rotary;
+
+/* Host only.  Pair i turns by freq[i] radians per position, base^(-i / pairs) where freq is NULL (1 <= base <= 1e30); sections[a]
+ * consecutive pairs belong to axis a (they add up to `pairs`; NULL with one axis). */
+GL_API int gl_rotary_plan(int32_t pairs, double base, const double* freq, const int32_t* sections, int32_t axes,
+                          int32_t adjacent, gl_rotary* out);
+
+/* compute rotate of x ((B, T, heads),(head_dim)), GL_F32 or GL_BF16: in every head the pair (u, v) of pair i of token (b, t) becomes
+ * (u cos - v sin, u sin + v cos) of its angle at positions[axis[i]][b][t]; values behind the pairs are copied.  `positions`:
+ * int32 in DEVICE memory, [axes][B][T], any value.  out: shape and type of x; it may be x itself (same data and
+ * pitch), otherwise the two do not overlap.  token_pitch, out_pitch: elements between successive tokens (0: dense), at least
+ * heads * head_dim.  GL_ROTATE_BACK in flags turns by the negative angles: the inverse, and the gradient.
+ * Angles are exact to position * 2^-65 turns and 2^-24 relative, cosines and products fp32.  Limits (else GL_ERR_UNSUPPORTED):
+ * B * T <= 2^31, heads * head_dim <= 2^24. */
+GL_API int gl_compute_rotate(const gl_ap* x, int64_t token_pitch, const gl_rotary* plan, const int32_t* positions, gl_ap* out,
+                             int64_t out_pitch, uint32_t flags, void* stream);
 
 /* Synchronises `stream`, then reports and clears the device status word:
  * GL_ERR_TIMEOUT if a bounded wait inside a kernel gave up since the last poll

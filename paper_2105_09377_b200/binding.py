@@ -20,6 +20,7 @@ GL_EPILOGUE_RELU = 0x2
 GL_DOT_GENERAL_KERNEL = 0x100
 GL_OUT_NCHW = 0x4
 GL_OUT_BF16 = 0x8
+GL_ROTATE_BACK = 0x10
 GL_OK = 0
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -78,6 +79,24 @@ class GlPages(ctypes.Structure):
     ]
 
 
+class GlF8(ctypes.Structure):
+    _fields_ = list(GlMx4._fields_)
+
+
+GL_MAX_PAIRS = 128
+
+
+class GlRotary(ctypes.Structure):
+    _fields_ = [
+        ("pairs", ctypes.c_int32),
+        ("axes", ctypes.c_int32),
+        ("adjacent", ctypes.c_int32),
+        ("reserved_", ctypes.c_int32),
+        ("step", ctypes.c_uint64 * GL_MAX_PAIRS),
+        ("axis", ctypes.c_uint8 * GL_MAX_PAIRS),
+    ]
+
+
 EXPORTS = [
     "gl_shape_access", "gl_shape_windows", "gl_shape_flatten", "gl_shape_transpose", "gl_shape_pad",
     "gl_shape_cartesian_dot", "gl_shape_reduce_max", "gl_access_windows", "gl_access_flatten",
@@ -90,6 +109,8 @@ EXPORTS = [
     "gl_mx4_data_bytes", "gl_mx4_scale_bytes", "gl_mx4_quantize", "gl_mx4_dequantize", "gl_cartesian_dot_mx4",
     "gl_dense_mx4", "gl_dense_mx4_workspace", "gl_cache4_bytes", "gl_cache4_append", "gl_cache4_read",
     "gl_attend_cache4", "gl_attend_cache4_workspace",
+    "gl_f8_data_bytes", "gl_f8_scale_bytes", "gl_f8_quantize", "gl_f8_dequantize", "gl_cartesian_dot_f8", "gl_dense_f8",
+    "gl_dense_f8_workspace", "gl_compute_norm_rms", "gl_compute_norm_rms_f8", "gl_rotary_plan", "gl_compute_rotate",
 ]
 
 
@@ -102,6 +123,7 @@ def _load() -> ctypes.CDLL:
     ap, win, vp = ctypes.POINTER(GlAp), ctypes.POINTER(GlWindows), ctypes.c_void_p
     i32p = ctypes.POINTER(ctypes.c_int32)
     mx, ca, pg = ctypes.POINTER(GlMx4), ctypes.POINTER(GlCache4), ctypes.POINTER(GlPages)
+    f8, rot, f64p = ctypes.POINTER(GlF8), ctypes.POINTER(GlRotary), ctypes.POINTER(ctypes.c_double)
     sig = {
         "gl_shape_access": [ap, ctypes.c_int32, ap],
         "gl_shape_windows": [ap, win, ap],
@@ -138,6 +160,14 @@ def _load() -> ctypes.CDLL:
         "gl_cache4_append": [ca, ap, ap, ctypes.c_int64, pg, vp],
         "gl_cache4_read": [ca, pg, ap, ap, vp],
         "gl_attend_cache4": [ap, ctypes.c_int64, ca, pg, ctypes.c_float, ap, ctypes.c_uint32, vp, ctypes.c_size_t, vp],
+        "gl_f8_quantize": [ap, f8, vp],
+        "gl_f8_dequantize": [f8, ap, vp],
+        "gl_cartesian_dot_f8": [f8, f8, ap, ctypes.c_uint32, vp],
+        "gl_dense_f8": [ap, f8, ap, ctypes.c_uint32, vp, ctypes.c_size_t, vp],
+        "gl_compute_norm_rms": [ap, ap, ap, ctypes.c_float, ap, ap, vp],
+        "gl_compute_norm_rms_f8": [ap, ap, ap, ctypes.c_float, ap, f8, vp],
+        "gl_rotary_plan": [ctypes.c_int32, ctypes.c_double, f64p, i32p, ctypes.c_int32, ctypes.c_int32, rot],
+        "gl_compute_rotate": [ap, ctypes.c_int64, rot, vp, ap, ctypes.c_int64, ctypes.c_uint32, vp],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -146,7 +176,8 @@ def _load() -> ctypes.CDLL:
     lib.gl_cartesian_dot_workspace.argtypes = [ap, win, ap, ctypes.c_uint32]
     lib.gl_cartesian_dot_workspace.restype = ctypes.c_size_t
     for name, args in {"gl_mx4_data_bytes": [mx], "gl_mx4_scale_bytes": [mx], "gl_dense_mx4_workspace": [ap, mx],
-                       "gl_cache4_bytes": [ca], "gl_attend_cache4_workspace": [ap, ca]}.items():
+                       "gl_cache4_bytes": [ca], "gl_attend_cache4_workspace": [ap, ca],
+                       "gl_f8_data_bytes": [f8], "gl_f8_scale_bytes": [f8], "gl_dense_f8_workspace": [ap, f8]}.items():
         fn = getattr(lib, name)
         fn.argtypes = args
         fn.restype = ctypes.c_size_t
@@ -608,6 +639,168 @@ def gl_dense_mx4(a0: AccessPattern, a1: Mx4, out: Optional[AccessPattern] = None
     return out
 
 
+# ---- operands held in 8 bits, the norm in front of them ----
+
+@dataclass
+class F8:
+    """A pattern held in 8 bits: E4M3 codes and one E8M0 scale per 128 values of an item."""
+
+    data: torch.Tensor    # uint8, gl_f8_data_bytes
+    scale: torch.Tensor   # uint8, gl_f8_scale_bytes
+    dims: tuple           # S_A ++ S_C
+    access_ndim: int
+
+    @property
+    def shape(self):
+        return (self.dims[: self.access_ndim], self.dims[self.access_ndim:])
+
+
+def _f8_meta(shape, access_ndim) -> GlF8:
+    if len(shape) > GL_MAX_DIMS:
+        raise GlError(3, "too many dimensions")
+    s = GlF8()
+    s.ndim, s.access_ndim = len(shape), access_ndim
+    for i, n in enumerate(shape):
+        s.shape[i] = int(n)
+    return s
+
+
+def _f8_struct(m: F8) -> GlF8:
+    s = _f8_meta(m.dims, m.access_ndim)
+    for t, need in ((m.data, LIB.gl_f8_data_bytes(ctypes.byref(s))), (m.scale, LIB.gl_f8_scale_bytes(ctypes.byref(s)))):
+        if t.dtype != torch.uint8 or not t.is_contiguous() or t.numel() < need:
+            raise ValueError("an F8 operand of this shape wants %d contiguous bytes" % need)
+    s.data, s.scale = m.data.data_ptr(), m.scale.data_ptr()
+    return s
+
+
+def f8_empty(shape, access_ndim: int, device, stream=None) -> F8:
+    """Storage for a pattern of this shape, contents undefined; `stream`: where it is first used, if not the current one."""
+    s = _f8_meta(shape, access_ndim)
+    nd, ns = LIB.gl_f8_data_bytes(ctypes.byref(s)), LIB.gl_f8_scale_bytes(ctypes.byref(s))
+    if not nd:
+        raise GlError(4, "f8_empty")
+    return F8(_empty(nd, torch.uint8, device, stream), _empty(ns, torch.uint8, device, stream),
+              tuple(int(n) for n in shape), access_ndim)
+
+
+def gl_f8_quantize(a: AccessPattern, out: Optional[F8] = None, stream=None) -> F8:
+    sa = _struct(a)
+    if out is None:
+        out = f8_empty(tuple(a.tensor.shape), a.access_ndim, a.tensor.device, stream)
+    _on_gpu(a.tensor, out.data, out.scale)
+    _check(LIB.gl_f8_quantize(ctypes.byref(sa), ctypes.byref(_f8_struct(out)), _stream(stream)), "gl_f8_quantize")
+    return out
+
+
+def gl_f8_dequantize(m: F8, out: Optional[AccessPattern] = None, stream=None) -> AccessPattern:
+    if out is None:
+        out = AccessPattern(_empty(m.dims, torch.float32, m.data.device, stream), m.access_ndim)
+    _on_gpu(m.data, m.scale, out.tensor)
+    so = _struct(out)
+    _check(LIB.gl_f8_dequantize(ctypes.byref(_f8_struct(m)), ctypes.byref(so), _stream(stream)), "gl_f8_dequantize")
+    return out
+
+
+def gl_cartesian_dot_f8(a0: F8, a1: F8, out: Optional[AccessPattern] = None, flags: int = 0, stream=None) -> AccessPattern:
+    if out is None:
+        out = _product_out(a0.shape[0], a1.shape[0], flags, a0.data.device, stream)
+    _on_gpu(a0.data, a0.scale, a1.data, a1.scale, out.tensor)
+    so = _struct(out)
+    _check(LIB.gl_cartesian_dot_f8(ctypes.byref(_f8_struct(a0)), ctypes.byref(_f8_struct(a1)), ctypes.byref(so), flags,
+                                   _stream(stream)), "gl_cartesian_dot_f8")
+    return out
+
+
+def gl_dense_f8_workspace(a0: AccessPattern, a1: F8) -> int:
+    return int(LIB.gl_dense_f8_workspace(ctypes.byref(_struct(a0)), ctypes.byref(_f8_struct(a1))))
+
+
+def gl_dense_f8(a0: AccessPattern, a1: F8, out: Optional[AccessPattern] = None, flags: int = 0,
+                workspace: Optional[torch.Tensor] = None, stream=None) -> AccessPattern:
+    if out is None:
+        out = _product_out(a0.access_shape, a1.shape[0], flags, a0.tensor.device, stream)
+    if workspace is None:
+        workspace = _scratch(gl_dense_f8_workspace(a0, a1), a0.tensor.device, stream)
+    _on_gpu(a0.tensor, a1.data, a1.scale, out.tensor, workspace)
+    s0, so = _struct(a0), _struct(out)
+    _check(LIB.gl_dense_f8(ctypes.byref(s0), ctypes.byref(_f8_struct(a1)), ctypes.byref(so), flags, *_ws(workspace),
+                           _stream(stream)), "gl_dense_f8")
+    return out
+
+
+def _ap_ptr(a: Optional[AccessPattern]):
+    return ctypes.byref(_struct(a)) if a is not None else None
+
+
+def _tensor(a: Optional[AccessPattern]):
+    return a.tensor if a is not None else None
+
+
+def _norm_call(x, weight, out, eps, residual, total):
+    """(entry point, arguments) of a norm whose result is an F8 operand or an access pattern."""
+    eight = isinstance(out, F8)
+    _on_gpu(x.tensor, _tensor(weight), _tensor(residual), _tensor(total), *((out.data, out.scale) if eight else (out.tensor,)))
+    args = (_ap_ptr(x), _ap_ptr(residual), _ap_ptr(weight), float(eps), _ap_ptr(total),
+            ctypes.byref(_f8_struct(out)) if eight else _ap_ptr(out))
+    return (LIB.gl_compute_norm_rms_f8 if eight else LIB.gl_compute_norm_rms), args
+
+
+def gl_compute_norm_rms(x: AccessPattern, weight: Optional[AccessPattern] = None, eps: float = 1e-6,
+                        residual: Optional[AccessPattern] = None, total: Optional[AccessPattern] = None, out=None, stream=None):
+    """`out`: an access pattern of x's shape (default: of x's type) or an F8 operand, whose storage says where the result goes.
+    `total` takes x + residual in the residual's type (the header's `sum`); it may be `residual`."""
+    if out is None:
+        out = AccessPattern(_empty(tuple(x.tensor.shape), x.tensor.dtype, x.tensor.device, stream), x.access_ndim)
+    call, args = _norm_call(x, weight, out, eps, residual, total)
+    _check(call(*args, _stream(stream)), call.__name__)
+    return out
+
+
+def gl_compute_norm_rms_f8(x: AccessPattern, weight: Optional[AccessPattern] = None, eps: float = 1e-6,
+                           residual: Optional[AccessPattern] = None, total: Optional[AccessPattern] = None,
+                           out: Optional[F8] = None, stream=None) -> F8:
+    if out is None:
+        out = f8_empty(tuple(x.tensor.shape), x.access_ndim, x.tensor.device, stream)
+    return gl_compute_norm_rms(x, weight, eps, residual, total, out, stream)
+
+
+# ---- rotary positions ----
+
+def rotary_plan(pairs: int, base: float = 10000.0, sections: Optional[Sequence[int]] = None, adjacent: bool = False,
+                freq: Optional[Sequence[float]] = None) -> GlRotary:
+    """Frequencies base^(-i / pairs), or `freq` (radians per position), `sections`: consecutive pairs of each axis."""
+    if freq is not None and len(freq) != pairs:
+        raise ValueError("one frequency per pair")
+    sections = [pairs] if sections is None else list(sections)
+    plan = GlRotary()
+    _check(LIB.gl_rotary_plan(pairs, float(base), (ctypes.c_double * pairs)(*freq) if freq is not None else None,
+                              (ctypes.c_int32 * max(1, len(sections)))(*sections), len(sections), int(adjacent),
+                              ctypes.byref(plan)), "gl_rotary_plan")
+    return plan
+
+
+def _rotate_args(x: AccessPattern, plan: GlRotary, positions: torch.Tensor, out: AccessPattern, flags: int):
+    _on_gpu(x.tensor, positions, out.tensor)
+    sx, pitch = _tokens_struct(x.tensor)
+    so, out_pitch = _tokens_struct(out.tensor)
+    sx.access_ndim, so.access_ndim = x.access_ndim, out.access_ndim
+    if positions.dtype != torch.int32 or not positions.is_contiguous() or \
+            tuple(positions.shape) not in ((plan.axes,) + tuple(x.tensor.shape[:2]), tuple(x.tensor.shape[:2]) if plan.axes == 1 else ()):
+        raise ValueError("positions are contiguous int32 [axes, batch, tokens]")
+    return (ctypes.byref(sx), pitch, ctypes.byref(plan), positions.data_ptr(), ctypes.byref(so), out_pitch, flags)
+
+
+def gl_compute_rotate(x: AccessPattern, plan: GlRotary, positions: torch.Tensor, out: Optional[AccessPattern] = None, flags: int = 0,
+                      stream=None) -> AccessPattern:
+    """x ((B, T, heads),(head_dim)), whose tokens may lie further apart than they are long; positions int32 [axes, B, T], or
+    [B, T] with one axis; out may be x."""
+    if out is None:
+        out = AccessPattern(_empty(tuple(x.tensor.shape), x.tensor.dtype, x.tensor.device, stream), 3)
+    _check(LIB.gl_compute_rotate(*_rotate_args(x, plan, positions, out, flags), _stream(stream)), "gl_compute_rotate")
+    return out
+
+
 # ---- pages of 4-bit keys and values ----
 
 @dataclass
@@ -825,6 +1018,42 @@ def prepare_dense_mx4(a0: AccessPattern, a1: Mx4, out: AccessPattern, flags: int
     _on_gpu(a0.tensor, a1.data, a1.scale, out.tensor, workspace)
     return Prepared(LIB.gl_dense_mx4, (ctypes.byref(_struct(a0)), ctypes.byref(_mx4_struct(a1)), ctypes.byref(_struct(out)), flags,
                                        *_ws(workspace)), (a0, a1, out, workspace), scratch)
+
+
+def prepare_f8_quantize(a: AccessPattern, out: F8) -> Prepared:
+    _on_gpu(a.tensor, out.data, out.scale)
+    return Prepared(LIB.gl_f8_quantize, (ctypes.byref(_struct(a)), ctypes.byref(_f8_struct(out))), (a, out))
+
+
+def prepare_f8_dequantize(m: F8, out: AccessPattern) -> Prepared:
+    _on_gpu(m.data, m.scale, out.tensor)
+    return Prepared(LIB.gl_f8_dequantize, (ctypes.byref(_f8_struct(m)), ctypes.byref(_struct(out))), (m, out))
+
+
+def prepare_cartesian_dot_f8(a0: F8, a1: F8, out: AccessPattern, flags: int = 0) -> Prepared:
+    _on_gpu(a0.data, a0.scale, a1.data, a1.scale, out.tensor)
+    return Prepared(LIB.gl_cartesian_dot_f8, (ctypes.byref(_f8_struct(a0)), ctypes.byref(_f8_struct(a1)),
+                                              ctypes.byref(_struct(out)), flags), (a0, a1, out))
+
+
+def prepare_dense_f8(a0: AccessPattern, a1: F8, out: AccessPattern, flags: int = 0,
+                     workspace: Optional[torch.Tensor] = None) -> Prepared:
+    scratch = None if workspace is not None else _scratch(gl_dense_f8_workspace(a0, a1), a0.tensor.device)
+    workspace = scratch if workspace is None else workspace
+    _on_gpu(a0.tensor, a1.data, a1.scale, out.tensor, workspace)
+    return Prepared(LIB.gl_dense_f8, (ctypes.byref(_struct(a0)), ctypes.byref(_f8_struct(a1)), ctypes.byref(_struct(out)), flags,
+                                      *_ws(workspace)), (a0, a1, out, workspace), scratch)
+
+
+def prepare_compute_norm_rms(x: AccessPattern, weight: Optional[AccessPattern], out, eps: float = 1e-6,
+                             residual: Optional[AccessPattern] = None, total: Optional[AccessPattern] = None) -> Prepared:
+    """out: an access pattern or an F8 operand."""
+    call, args = _norm_call(x, weight, out, eps, residual, total)
+    return Prepared(call, args, (x, weight, out, residual, total))
+
+
+def prepare_compute_rotate(x: AccessPattern, plan: GlRotary, positions: torch.Tensor, out: AccessPattern, flags: int = 0) -> Prepared:
+    return Prepared(LIB.gl_compute_rotate, _rotate_args(x, plan, positions, out, flags), (x, plan, positions, out))
 
 
 def prepare_cache4_append(cache: Cache4, k, v, page_table, lengths) -> Prepared:

@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libglenside.so")
-SOURCES = ["gl_host.cpp", "gl_memops.cu", "gl_dot.cu", "gl_mx4.cu", "gl_attend.cu"]
+SOURCES = ["gl_host.cpp", "gl_memops.cu", "gl_dot.cu", "gl_mx4.cu", "gl_attend.cu", "gl_f8.cu", "gl_norm.cu", "gl_rotate.cu"]
 
 
 def _stale() -> bool:
@@ -27,7 +27,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     tmp = LIB_PATH + ".%d.tmp" % os.getpid()
     cmd = [
         nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-        "-shared", "-Xcompiler", "-fPIC,-fvisibility=hidden", "--cudart", "shared",
+        "--threads", "0", "-shared", "-Xcompiler", "-fPIC,-fvisibility=hidden", "--cudart", "shared",
         "-I", os.path.join(ROOT, "include"), "-I", CSRC,
     ]
     if verbose:

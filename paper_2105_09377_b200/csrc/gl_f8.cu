@@ -1,0 +1,1106 @@
+// Operands held in 8 bits (F8): blocks of 128 consecutive values of an item, E4M3 codes and one E8M0 scale per block.
+//   * gl_f8_quantize / gl_f8_dequantize: between GL_BF16 / GL_F32 patterns and F8 operands;
+//   * gl_cartesian_dot_f8: compute dotProd (cartProd A B) of two F8 operands on the block-scaled tensor-core
+//     instructions (tcgen05.mma kind::mxf8f6f4), the scales applied by the hardware;
+//   * gl_dense_f8: the same with the left operand quantised by the call.
+#include <cuda.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <atomic>
+#include <cstring>
+
+#include "gl_f8.cuh"
+#include "gl_f8.h"
+#include "gl_internal.h"
+#include "gl_launch.cuh"
+#include "gl_tc.cuh"
+#include "gl_tmap.h"
+
+using namespace gl;
+
+namespace {
+
+// ------------------------------------------------------------------------
+// Quantisation and its inverse
+// ------------------------------------------------------------------------
+
+// A warp takes U units of 256 values (two blocks), consecutive ones, all requested before the first is used.  The unit's row and
+// place are the same for the whole warp: one division per warp and unit.  Bound by HBM.
+struct F8QuantParams {
+  int32_t K, pitch;
+  uint32_t kt;
+  uint32_t units;       // rows * per_row
+  FastDiv per_row;      // units per row
+};
+
+template <bool F32, bool VEC, int U>
+__global__ void __launch_bounds__(256) quantize_f8(const void* __restrict__ in, uint8_t* __restrict__ codes,
+                                                   uint8_t* __restrict__ scale, const F8QuantParams p) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31;
+  const uint32_t first = (blockIdx.x * 8u + (threadIdx.x >> 5)) * U;
+  uint32_t raw[U][8];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (first + u >= p.units) break;
+    uint32_t row, at;
+    p.per_row.divmod(first + u, row, at);
+    unit_load<F32, VEC>(static_cast<const char*>(in) + static_cast<int64_t>(row) * p.K * (F32 ? 4 : 2), static_cast<int>(at) * kF8Unit,
+                        p.K, lane, raw[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (first + u >= p.units) break;
+    uint32_t row, at;
+    p.per_row.divmod(first + u, row, at);
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = unit_value<F32, VEC>(raw[u], j);
+    unit_store_f8<VEC>(v, codes + static_cast<int64_t>(row) * p.pitch, static_cast<int>(at) * kF8Unit, p.pitch, lane,
+                       scale + f8_scale_at(row, at * 2, p.kt));
+  }
+}
+
+// Two codes to two values (exact in fp16).
+__device__ __forceinline__ float2 f8_values2(uint32_t two) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(two)));
+  return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
+
+// Going back, the lanes' values follow the stores: eight bf16 values or two times four floats, 16 bytes each.
+template <bool F32, bool VEC, int U>
+__global__ void __launch_bounds__(256) dequantize_f8(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scale,
+                                                     void* __restrict__ out, const F8QuantParams p) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31;
+  const uint32_t first = (blockIdx.x * 8u + (threadIdx.x >> 5)) * U;
+  uint32_t word[U][2], e[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    word[u][0] = word[u][1] = e[u] = 0;
+    if (first + u >= p.units) break;
+    uint32_t row, at;
+    p.per_row.divmod(first + u, row, at);
+    const uint8_t* src = codes + static_cast<int64_t>(row) * p.pitch;
+    const int k0 = static_cast<int>(at) * kF8Unit;
+    e[u] = *reinterpret_cast<const uint16_t*>(scale + f8_scale_at(row, at * 2, p.kt));
+    if (VEC && !F32) {
+      if (k0 + lane * 8 < p.K) {
+        const uint2 w = __ldcs(reinterpret_cast<const uint2*>(src + k0 + lane * 8));
+        word[u][0] = w.x;
+        word[u][1] = w.y;
+      }
+    } else if (VEC) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (k0 + h * 128 + lane * 4 < p.K) word[u][h] = __ldcs(reinterpret_cast<const uint32_t*>(src + k0 + h * 128 + lane * 4));
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (k0 + j * 32 + lane < p.K) word[u][j >> 2] |= static_cast<uint32_t>(src[k0 + j * 32 + lane]) << (8 * (j & 3));
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (first + u >= p.units) break;
+    uint32_t row, at;
+    p.per_row.divmod(first + u, row, at);
+    const int k0 = static_cast<int>(at) * kF8Unit;
+    const float s0 = f8_scale(e[u] & 255u), s1 = f8_scale(e[u] >> 8);
+    const float sa = VEC && !F32 && lane >= 16 ? s1 : s0, sb = VEC && !F32 && lane < 16 ? s0 : s1;
+    float v[8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float s = h ? sb : sa;
+      const float2 a = f8_values2(word[u][h] & 0xFFFFu), b = f8_values2(word[u][h] >> 16);
+      v[4 * h] = a.x * s; v[4 * h + 1] = a.y * s; v[4 * h + 2] = b.x * s; v[4 * h + 3] = b.y * s;
+    }
+    const int64_t base = static_cast<int64_t>(row) * p.K + k0;
+    if (VEC && !F32) {
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(__float_as_uint(v[2 * i]), __float_as_uint(v[2 * i + 1]));
+      if (k0 + lane * 8 < p.K) __stcs(reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + base + lane * 8), make_uint4(w[0], w[1], w[2], w[3]));
+    } else if (VEC) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (k0 + h * 128 + lane * 4 < p.K)
+          __stcs(reinterpret_cast<float4*>(static_cast<float*>(out) + base + h * 128 + lane * 4),
+                 make_float4(v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]));
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (k0 + j * 32 + lane < p.K) {
+          if (F32) static_cast<float*>(out)[base + j * 32 + lane] = v[j];
+          else static_cast<uint16_t*>(out)[base + j * 32 + lane] = f32_to_bf16(v[j]);
+        }
+    }
+  }
+}
+
+F8QuantParams f8_quant_params(const F8View& v) {
+  F8QuantParams p;
+  p.K = static_cast<int32_t>(v.K);
+  p.pitch = static_cast<int32_t>(v.pitch);
+  p.kt = static_cast<uint32_t>(v.kt);
+  const int64_t per_row = (v.nb + 1) / 2;
+  p.units = static_cast<uint32_t>(v.rows * per_row);
+  p.per_row.set(per_row);
+  return p;
+}
+
+// Several units per warp only when every SM has blocks to hold.
+constexpr int kUnitsPerWarp = 4;
+bool many_units(const F8QuantParams& p) { return p.units >= static_cast<uint32_t>(num_sms()) * 4u * 8u * kUnitsPerWarp; }
+dim3 unit_grid(const F8QuantParams& p) {
+  const uint32_t per_block = 8u * (many_units(p) ? kUnitsPerWarp : 1);
+  return dim3((p.units + per_block - 1) / per_block);
+}
+
+int launch_quantize(const gl_ap& in, const F8View& v, void* codes, void* scale, cudaStream_t st) {
+  const bool f32 = in.dtype == GL_F32, vec = v.K % 8 == 0;
+  const F8QuantParams p = f8_quant_params(v);
+  constexpr int kU = kUnitsPerWarp;
+  void (*k)(const void*, uint8_t*, uint8_t*, F8QuantParams) =
+      many_units(p) ? (f32 ? (vec ? quantize_f8<true, true, kU> : quantize_f8<true, false, kU>)
+                           : (vec ? quantize_f8<false, true, kU> : quantize_f8<false, false, kU>))
+                    : (f32 ? (vec ? quantize_f8<true, true, 1> : quantize_f8<true, false, 1>)
+                           : (vec ? quantize_f8<false, true, 1> : quantize_f8<false, false, 1>));
+  return launch_pdl(k, unit_grid(p), dim3(256), 0, st, 1, static_cast<const void*>(in.data), static_cast<uint8_t*>(codes),
+                    static_cast<uint8_t*>(scale), p) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
+}
+
+// ------------------------------------------------------------------------
+// Block-scaled product
+// ------------------------------------------------------------------------
+
+// out[m,o] = sum over blocks b of 2^(ea[m,b] + eb[o,b] - 254) sum_k a[m,k] b[o,k]: the inner products of E4M3 codes, their
+// scaling and the fp32 sum are one instruction, tcgen05.mma kind::mxf8f6f4, which wants a scale for every 32 values; the four
+// instructions of a block read the same scale byte.
+
+// D[tmem] (+)= (A * sfa)[smem] * (B * sfb)[smem]^T, K = 32, one scale per row and instruction.
+template <int CTAS>
+__device__ __forceinline__ void tc_mma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                          uint32_t accumulate) {
+  if (CTAS == 2)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+}
+
+// One scale tile (32 rows x 16 bytes of shared memory) into four columns of tensor memory, repeated in the four lane
+// quarters.  Copies and MMAs of one thread run in the order of their issue.
+template <int CTAS>
+__device__ __forceinline__ void tc_copy_scales(uint32_t taddr, uint64_t desc) {
+  if (CTAS == 2) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+  else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+
+// Instruction descriptor, kind::mxf8f6f4: A and B E4M3 (bits 7-9 and 10-12 = 0), both K-major, N >> 3 at bit 17, scales E8M0
+// (bit 23), M >> 4 at bit 24; which of the four scale bytes of a row the instruction reads: bits 4-5 (B), 29-30 (A).
+__device__ __forceinline__ uint32_t make_idesc_f8(int m, int n, uint32_t byte) {
+  return (byte << 4) | (static_cast<uint32_t>(n >> 3) << 17) | (1u << 23) | (static_cast<uint32_t>(m >> 4) << 24) | (byte << 29);
+}
+
+// relu that lets a NaN through (fmaxf would turn it into 0)
+__device__ __forceinline__ float relu_keep_nan(float v) { return v < 0.f ? 0.f : v; }
+
+constexpr int kTile = 128;           // rows of A per block
+constexpr int kKBytes = 128;         // bytes of a row per K block: one block of 128 values, one 128-byte swizzle row
+constexpr int kF8Threads = 224;      // warp 0 TMA (A), warp 1 MMA, warps 2-5 epilogue, warp 6 TMA (B)
+
+struct F8Params {
+  int64_t M, O;
+  int tiles_m, tiles_n;   // tiles_m counts 128 * CTAS rows
+  int kblocks;            // K blocks of 128 values
+  int last_steps;         // instructions (32 values) in the last K block
+  int relu, out_bf16, tma_store;
+  FastDiv div_tiles_n;
+};
+
+template <int BN, int CTAS>
+struct F8Cfg {
+  static constexpr int kStageA = kTile * kKBytes;
+  static constexpr int kStageB = (BN / CTAS) * kKBytes;
+  static constexpr int kStage = kStageA + kStageB;
+  // A scale tile holds four K blocks: every fourth stage brings one per 128 rows of A and of B.
+  static constexpr int kScaleA = 512, kScaleB = (BN / 128) * 512, kScales = kScaleA + kScaleB;
+  static constexpr int kEpiBytes = 4 * 2 * 4096;
+  static constexpr int kStages = (232448 - kEpiBytes - 1024 - 256) / (kStage + kScales);
+  static constexpr int kSmemBytes = kStages * (kStage + kScales) + kEpiBytes + 1024 + 256;
+  // Tensor memory (512 columns): two sets of scales in the last kSfCols, two accumulators of BN columns before them.
+  // 256-wide accumulators do not fit twice: they share kSfCols columns, which the epilogue empties first.
+  static constexpr int kSfCols = 8 + BN / 16;
+  static constexpr int kSfBase = 512 - kSfCols;
+  static constexpr int kAcc1 = 2 * BN <= kSfBase ? BN : kSfBase - BN;
+  static constexpr bool kOverlap = kAcc1 < BN;
+};
+
+template <int BN, int CTAS>
+__global__ void __launch_bounds__(kF8Threads, 1)
+dot_f8(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+       const __grid_constant__ CUtensorMap map_sa, const __grid_constant__ CUtensorMap map_sb,
+       const __grid_constant__ CUtensorMap map_c, void* __restrict__ out, const F8Params p) {
+  using Cfg = F8Cfg<BN, CTAS>;
+  static_assert(Cfg::kStages >= 2, "ring too shallow");
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t tiles = (raw + 1023u) & ~1023u;   // the 128-byte swizzle wants 1024-byte aligned tiles
+  unsigned char* gen_tiles = smem_raw + (tiles - raw);
+  const uint32_t epi_base = tiles + Cfg::kStages * Cfg::kStage;
+  const uint32_t scales = epi_base + Cfg::kEpiBytes;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(gen_tiles + Cfg::kStages * (Cfg::kStage + Cfg::kScales) + Cfg::kEpiBytes);
+  const uint32_t bar_full = smem_u32(bars);
+  const uint32_t bar_empty = bar_full + 8 * Cfg::kStages;
+  const uint32_t bar_tfull = bar_empty + 8 * Cfg::kStages;
+  const uint32_t bar_tempty = bar_tfull + 16;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * Cfg::kStages + 4);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = CTAS == 2 ? cluster_ctarank() : 0u;
+
+  if (threadIdx.x == 32) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_a)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_b)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_sa)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_sb)) : "memory");
+    if (p.tma_store) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_c)) : "memory");
+  }
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < Cfg::kStages; ++s) { mbar_init(bar_full + 8 * s, 2); mbar_init(bar_empty + 8 * s, 1); }
+    for (int a = 0; a < 2; ++a) { mbar_init(bar_tfull + 8 * a, 1); mbar_init(bar_tempty + 8 * a, 4 * CTAS); }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    if (CTAS == 2) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot)) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot)) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+  }
+  tc_fence_before();
+  if (CTAS == 2) cluster_sync_all();
+  else __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const int num_tiles = p.tiles_m * p.tiles_n;
+  const int unit0 = static_cast<int>(blockIdx.x) / CTAS, unit_step = static_cast<int>(gridDim.x) / CTAS;
+  pdl_wait();
+  pdl_launch_dependents();
+
+  if (warp == 0 || warp == 6) {
+    // ---------------- TMA producers: warp 0 stages A and its scales, warp 6 stages B and its scales ----------------
+    const bool load_a = warp == 0;
+    const bool leader = elect_one();
+    uint32_t s = 0, ph = 0;
+    bool ok = true;
+    for (int u = unit0; u < num_tiles && ok; u += unit_step) {
+      uint32_t tm, tn;
+      p.div_tiles_n.divmod(static_cast<uint32_t>(u), tm, tn);
+      const int m0 = (static_cast<int>(tm) * CTAS + static_cast<int>(rank)) * kTile;
+      const int n0 = static_cast<int>(tn) * BN + static_cast<int>(rank) * (BN / CTAS);
+      for (int kb = 0; kb < p.kblocks; ++kb) {
+        if (!mbar_wait(bar_empty + 8 * s, ph ^ 1u, abort_flag)) { ok = false; break; }
+        const uint32_t full = CTAS == 2 ? map_to_cta(bar_full + 8 * s, 0) : bar_full + 8 * s;
+        const uint32_t stage = tiles + s * Cfg::kStage;
+        const uint32_t sc = scales + s * Cfg::kScales;
+        const bool with_scales = (kb & 3) == 0;
+        if (rank == 0 && leader)
+          mbar_expect_tx(bar_full + 8 * s, CTAS * (load_a ? Cfg::kStageA + (with_scales ? Cfg::kScaleA : 0)
+                                                          : Cfg::kStageB + (with_scales ? Cfg::kScaleB : 0)));
+        if (leader) {
+          if (load_a) {
+            if (CTAS == 2) tma_load_2d_pair(stage, &map_a, kb * kKBytes, m0, full);
+            else tma_load_2d(stage, &map_a, kb * kKBytes, m0, full);
+            if (with_scales) {
+              if (CTAS == 2) tma_load_3d_pair(sc, &map_sa, 0, kb >> 2, m0 / 128, full);
+              else tma_load_3d(sc, &map_sa, 0, kb >> 2, m0 / 128, full);
+            }
+          } else {
+            if (CTAS == 2) tma_load_2d_pair(stage + Cfg::kStageA, &map_b, kb * kKBytes, n0, full);
+            else tma_load_2d(stage + Cfg::kStageA, &map_b, kb * kKBytes, n0, full);
+            if (with_scales) {   // every block of a pair holds the scales of all BN columns
+#pragma unroll
+              for (int h = 0; h < BN / 128; ++h) {
+                const uint32_t dst = sc + Cfg::kScaleA + h * 512;
+                const int rt = static_cast<int>(tn) * (BN / 128) + h;
+                if (CTAS == 2) tma_load_3d_pair(dst, &map_sb, 0, kb >> 2, rt, full);
+                else tma_load_3d(dst, &map_sb, 0, kb >> 2, rt, full);
+              }
+            }
+          }
+        }
+        if (++s == Cfg::kStages) { s = 0; ph ^= 1u; }
+      }
+    }
+  } else if (warp == 1) {
+    // ---------------- MMA issuer ----------------
+    if (rank == 0) {
+      const bool leader = elect_one();
+      const uint64_t desc_a0 = make_desc(tiles, 16, 1024, 2);
+      const uint64_t desc_b0 = make_desc(tiles + Cfg::kStageA, 16, 1024, 2);
+      const uint64_t desc_s0 = make_desc(scales, 16, 128, 0);
+      uint32_t s = 0, ph = 0, tile_it = 0, sets = 0;
+      bool ok = true;
+      for (int u = unit0; u < num_tiles && ok; u += unit_step, ++tile_it) {
+        const uint32_t acc = tile_it & 1u;
+        // separate accumulators: the one two tiles back has been read; overlapping ones: the shared columns of the
+        // previous tile have been read (its epilogue had then finished with the tile before)
+        const uint32_t wait_on = Cfg::kOverlap ? acc ^ 1u : acc;
+        const uint32_t round = Cfg::kOverlap ? (tile_it + 1) >> 1 : tile_it >> 1;
+        if (!mbar_wait(bar_tempty + 8 * wait_on, (round & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t d_tmem = tmem_base + (acc ? Cfg::kAcc1 : 0);
+        uint32_t sfa = 0, sfb = 0;
+        for (int kb = 0; kb < p.kblocks; ++kb) {
+          if (!mbar_wait(bar_full + 8 * s, ph, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+          const uint64_t da0 = desc_a0 + ((s * Cfg::kStage) >> 4);
+          const uint64_t db0 = desc_b0 + ((s * Cfg::kStage) >> 4);
+          if ((kb & 3) == 0) {   // the scales of four K blocks, into the set that the four before do not use
+            sfa = tmem_base + Cfg::kSfBase + (sets & 1u) * 4;
+            sfb = tmem_base + Cfg::kSfBase + 8 + (sets & 1u) * (BN / 32);
+            ++sets;
+            if (leader) {
+              const uint64_t ds0 = desc_s0 + ((s * Cfg::kScales) >> 4);
+              tc_copy_scales<CTAS>(sfa, ds0);
+#pragma unroll
+              for (int h = 0; h < BN / 128; ++h) tc_copy_scales<CTAS>(sfb + 4 * h, ds0 + ((Cfg::kScaleA + h * 512) >> 4));
+            }
+          }
+          const uint32_t idesc = make_idesc_f8(kTile * CTAS, BN, kb & 3);
+          const int steps = kb + 1 == p.kblocks ? p.last_steps : 4;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (k < steps && leader) tc_mma_f8<CTAS>(d_tmem, da0 + 2 * k, db0 + 2 * k, idesc, sfa, sfb, (kb | k) != 0 ? 1u : 0u);
+          if (leader) {
+            if (CTAS == 2) tc_commit_pair(bar_empty + 8 * s);
+            else tc_commit(bar_empty + 8 * s);
+          }
+          if (++s == Cfg::kStages) { s = 0; ph ^= 1u; }
+        }
+        if (ok && leader) {
+          if (CTAS == 2) tc_commit_pair(bar_tfull + 8 * acc);
+          else tc_commit(bar_tfull + 8 * acc);
+        }
+      }
+    }
+  } else {
+    // ---------------- epilogue: TMEM -> registers -> (shared memory -> TMA store | global) ----------------
+    const int q = warp & 3;
+    const bool leader = elect_one();
+    uint32_t tile_it = 0, chunk_it = 0;
+    bool ok = true;
+    const uint32_t stage_buf = epi_base + q * 8192;
+    const int cstep = p.out_bf16 ? 64 : 32;
+    const int nchunks = BN / cstep;
+    for (int u = unit0; u < num_tiles && ok; u += unit_step, ++tile_it) {
+      const uint32_t acc = tile_it & 1u, aph = (tile_it >> 1) & 1u;
+      uint32_t tmu, tn;
+      p.div_tiles_n.divmod(static_cast<uint32_t>(u), tmu, tn);
+      const int tm = static_cast<int>(tmu) * CTAS + static_cast<int>(rank);
+      if (!mbar_wait(bar_tfull + 8 * acc, aph, abort_flag)) { ok = false; break; }
+      tc_fence_after();
+      const uint32_t taddr = tmem_base + (acc ? Cfg::kAcc1 : 0) + (static_cast<uint32_t>(q * 32) << 16);
+      const int64_t m0 = static_cast<int64_t>(tm) * kTile + q * 32;
+#pragma unroll 1
+      for (int i = 0; i < nchunks; ++i) {
+        // the columns that two overlapping accumulators share go first: the last ones of the first, the first ones
+        // of the second
+        const int c = (Cfg::kOverlap && acc == 0 ? nchunks - 1 - i : i) * cstep;
+        const int64_t n0 = static_cast<int64_t>(tn) * BN + c;
+        uint32_t r[32];
+        tc_load_32cols(taddr + c, r);
+        if (p.relu) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(relu_keep_nan(__uint_as_float(r[j])));
+        }
+        if (p.out_bf16) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) r[j] = pack_bf16x2(r[2 * j], r[2 * j + 1]);
+          uint32_t r2[32];
+          tc_load_32cols(taddr + c + 32, r2);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            float a = __uint_as_float(r2[2 * j]), b = __uint_as_float(r2[2 * j + 1]);
+            if (p.relu) { a = relu_keep_nan(a); b = relu_keep_nan(b); }
+            r[16 + j] = pack_bf16x2(__float_as_uint(a), __float_as_uint(b));
+          }
+        }
+        if (i == (Cfg::kOverlap ? 0 : nchunks - 1)) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) {
+            if (CTAS == 2) mbar_arrive_remote(map_to_cta(bar_tempty + 8 * acc, 0));
+            else mbar_arrive(bar_tempty + 8 * acc);
+          }
+        }
+        if (n0 >= p.O) continue;   // uniform across the warp
+        const uint32_t buf = stage_buf + (chunk_it & 1u) * 4096;
+        ++chunk_it;
+        if (p.tma_store && leader) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buf + lane * 128 + ((j ^ (lane & 7)) << 4)),
+                       "r"(r[4 * j]), "r"(r[4 * j + 1]), "r"(r[4 * j + 2]), "r"(r[4 * j + 3])
+                       : "memory");
+        if (p.tma_store) {
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (leader) {
+            if (m0 < p.M)
+              asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
+                               reinterpret_cast<uint64_t>(&map_c)),
+                           "r"(static_cast<int>(n0)), "r"(static_cast<int>(m0)), "r"(buf)
+                           : "memory");
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+          }
+        } else {
+          // rows that are no multiples of 16 bytes: row by row, neighbouring lanes on neighbouring columns
+          __syncwarp();
+          const int rows = static_cast<int>(min(static_cast<int64_t>(32), p.M - m0));
+          const int cols = static_cast<int>(min(static_cast<int64_t>(cstep), p.O - n0));
+          const int64_t base = m0 * p.O + n0;
+#pragma unroll 8
+          for (int row = 0; row < rows; ++row) {
+            uint32_t v;
+            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(buf + row * 128 + (((lane >> 2) ^ (row & 7)) << 4) + (lane & 3) * 4));
+            if (p.out_bf16) {
+              uint16_t* to = static_cast<uint16_t*>(out) + base + row * p.O + 2 * lane;
+              if ((p.O & 1) == 0) {
+                if (2 * lane < cols) *reinterpret_cast<uint32_t*>(to) = v;   // (O even: whole pairs)
+              } else {
+                if (2 * lane < cols) to[0] = static_cast<uint16_t>(v);
+                if (2 * lane + 1 < cols) to[1] = static_cast<uint16_t>(v >> 16);
+              }
+            } else if (lane < cols) {
+              static_cast<float*>(out)[base + row * p.O + lane] = __uint_as_float(v);
+            }
+          }
+        }
+      }
+    }
+    if (p.tma_store && leader) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+  }
+
+  // teardown: a block that gave up lets its copies in flight land before it leaves
+  __syncwarp();
+  if (*abort_flag) {
+    const uint64_t t0 = global_timer();
+    while (global_timer() - t0 < 20000000ull) { }
+  }
+  tc_fence_before();
+  if (CTAS == 2) cluster_sync_all();
+  else __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    if (CTAS == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem_base) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem_base) : "memory");
+  }
+}
+
+// ------------------------------------------------------------------------
+// Few rows of A: the weights take the 128-row side
+// ------------------------------------------------------------------------
+//
+// With at most 128 rows of A the product is bound by reading B (the weights) once.  Tiles of 128 rows of B, all rows of
+// A as the N side (BN = 16 to 128 of them), and K cut over the S blocks of a cluster so that the loads of all SMs are in
+// flight: the blocks' partial sums meet in distributed shared memory, added in rank order.  One tile per block, two
+// blocks per SM.  While the kernel that rounds A is still running the weights are on their way into L2.
+//
+// At most kFuseRows rows (FUSED): the blocks round A themselves, each its own stretch of K, straight into operand order, while
+// the first weights are on their way: one launch.
+constexpr int kFuseRows = 4;
+constexpr int kFuseBlocks = 16;   // K blocks of A that a block has room for
+
+struct F8FewParams {
+  int M;
+  int64_t O;
+  const void* x;          // FUSED: rows of A as they came
+  int64_t K;
+  int x_f32;
+  int kblocks, last_steps;
+  int split;              // blocks per cluster
+  int relu, out_bf16;
+};
+
+// Rank r adds up the columns r, r + S, ...: the S partial sums of a value in rank order, those of four columns requested
+// before the first is added.
+template <int S>
+__device__ __forceinline__ void join_ranks(uint32_t mine, int rank, int64_t o, void* __restrict__ out, const F8FewParams& p) {
+  for (int c0 = rank; c0 < p.M; c0 += 4 * S) {
+    float x[4][S];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int from = 0; from < S; ++from)   // (columns past M are inside the partial sums' space only up to BN)
+        if (c0 + j * S < p.M)
+          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x[j][from]) : "r"(map_to_cta(mine + (c0 + j * S) * 512, from)));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int c = c0 + j * S;
+      if (c >= p.M) break;
+      float v = x[j][0];
+#pragma unroll
+      for (int from = 1; from < S; ++from) v += x[j][from];
+      if (p.relu) v = relu_keep_nan(v);
+      if (p.out_bf16) static_cast<uint16_t*>(out)[c * p.O + o] = f32_to_bf16(v);
+      else static_cast<float*>(out)[c * p.O + o] = v;
+    }
+  }
+}
+
+template <int BN, bool FUSED>
+struct F8FewCfg {
+  static constexpr int kStageA = kTile * kKBytes;                  // weights
+  static constexpr int kStageB = FUSED ? 0 : BN * kKBytes;
+  static constexpr int kStage = kStageA + kStageB;
+  static constexpr int kScales = FUSED ? 512 : 1024;               // a scale tile (four K blocks) of each side
+  static constexpr int kXTiles = kFuseBlocks / 4 + 1;              // FUSED: scale tiles that a stretch of K blocks touches
+  static constexpr int kXBytes = FUSED ? kFuseBlocks * BN * kKBytes + kXTiles * 512 : 0;
+  static constexpr int kStages = (112 * 1024 - 1024 - 256 - kXBytes) / (kStage + kScales);
+  static constexpr int kSmemBytes = kStages * (kStage + kScales) + kXBytes + 1024 + 256;
+  static constexpr int kTmemCols = BN + 16 <= 32 ? 32 : BN + 16 <= 64 ? 64 : BN + 16 <= 128 ? 128 : 256;
+  static constexpr int kSfBase = kTmemCols - 16;                   // two sets of four columns of each side
+  static_assert(kStages >= 2 && kStages * kStage >= BN * 128 * 4, "partial sums fit in the ring");
+  static_assert(FUSED ? BN == 16 : true, "the blocks that round A keep it as 16 rows");
+};
+
+// One warp rounds K block kb of row m: lane = 4 values, into the swizzled operand row and the scale tiles.
+__device__ __forceinline__ void round_row_block(const F8FewParams& p, unsigned char* rows, unsigned char* scale, int m, int kb, int lane) {
+  const int64_t k0 = static_cast<int64_t>(kb) * kF8Block + lane * 4, left = p.K - k0, at = static_cast<int64_t>(m) * p.K + k0;
+  float x[4];
+  if (left >= 4 && (p.K & 3) == 0) {
+    if (p.x_f32) {
+      const float4 a = *reinterpret_cast<const float4*>(static_cast<const float*>(p.x) + at);
+      x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+    } else {
+      const uint2 a = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p.x) + at);
+      x[0] = __uint_as_float(a.x << 16); x[1] = __uint_as_float(a.x & 0xFFFF0000u);
+      x[2] = __uint_as_float(a.y << 16); x[3] = __uint_as_float(a.y & 0xFFFF0000u);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      x[i] = i < left ? (p.x_f32 ? static_cast<const float*>(p.x)[at + i] : bf16_to_f32(static_cast<const uint16_t*>(p.x)[at + i])) : 0.f;
+  }
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+  const uint32_t e = f8_exponent(top);
+  const float f = f8_inverse(e);
+  const uint32_t word = e == 255u ? 0u : f8_codes4(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
+  *reinterpret_cast<uint32_t*>(rows + m * 128 + (((lane >> 2) ^ (m & 7)) << 4) + (lane & 3) * 4) = word;
+  if (lane == 0) scale[m * 16 + (kb & 3)] = static_cast<uint8_t>(e);
+}
+
+template <int BN, bool FUSED>
+__global__ void __launch_bounds__(kF8Threads, 2)
+dot_f8_few(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
+           const __grid_constant__ CUtensorMap map_sw, const __grid_constant__ CUtensorMap map_sx, void* __restrict__ out,
+           const F8FewParams p) {
+  using Cfg = F8FewCfg<BN, FUSED>;
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t tiles = (raw + 1023u) & ~1023u;
+  unsigned char* gen_tiles = smem_raw + (tiles - raw);
+  const uint32_t xs = tiles + Cfg::kStages * Cfg::kStage;            // FUSED: A, block by block, then its scale tiles
+  unsigned char* gen_x = gen_tiles + Cfg::kStages * Cfg::kStage;
+  const uint32_t scales = xs + Cfg::kXBytes;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(gen_x + Cfg::kXBytes + Cfg::kStages * Cfg::kScales);
+  const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8 * Cfg::kStages, bar_done = bar_empty + 8 * Cfg::kStages,
+                 bar_x = bar_done + 8;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * Cfg::kStages + 2);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = p.split > 1 ? static_cast<int>(cluster_ctarank()) : 0;
+  const int tile = static_cast<int>(blockIdx.x) / p.split;
+  // K blocks of this rank, as even as they go
+  const int kb0 = static_cast<int>(static_cast<int64_t>(p.kblocks) * rank / p.split);
+  const int kb1 = static_cast<int>(static_cast<int64_t>(p.kblocks) * (rank + 1) / p.split);
+
+  if (warp == 0 && elect_one())
+    for (int kb = kb0; kb < kb1; ++kb) tma_prefetch_2d(&map_w, kb * kKBytes, tile * kTile);
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < Cfg::kStages; ++s) { mbar_init(bar_full + 8 * s, FUSED ? 1 : 2); mbar_init(bar_empty + 8 * s, 1); }
+    mbar_init(bar_done, 1);
+    mbar_init(bar_x, 5);   // warps 2 to 6
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
+                 "r"(static_cast<uint32_t>(Cfg::kTmemCols)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  pdl_wait();
+  pdl_launch_dependents();
+
+  if (FUSED && warp >= 2) {
+    const int blocks = kb1 - kb0;   // rows one after the other, their K blocks side by side
+    unsigned char* xscale = gen_x + kFuseBlocks * BN * kKBytes;
+    for (int i = warp - 2; i < p.M * blocks; i += 5) {
+      const int b = i % blocks, kb = kb0 + b;
+      round_row_block(p, gen_x + b * (BN * kKBytes), xscale + ((kb >> 2) - (kb0 >> 2)) * 512, i / blocks, kb, lane);
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar_x);
+  }
+  if (warp == 0 || (warp == 6 && !FUSED)) {
+    const bool load_w = warp == 0;
+    const bool leader = elect_one();
+    uint32_t s = 0, ph = 0;
+    for (int kb = kb0; kb < kb1; ++kb) {
+      if (!mbar_wait(bar_empty + 8 * s, ph ^ 1u, abort_flag)) break;
+      const uint32_t full = bar_full + 8 * s, stage = tiles + s * Cfg::kStage, sc = scales + s * Cfg::kScales;
+      const bool with_scales = kb == kb0 || (kb & 3) == 0;
+      if (leader) {
+        mbar_expect_tx(full, (load_w ? Cfg::kStageA : Cfg::kStageB) + (with_scales ? 512 : 0));
+        if (load_w) {
+          tma_load_2d(stage, &map_w, kb * kKBytes, tile * kTile, full);
+          if (with_scales) tma_load_3d(sc, &map_sw, 0, kb >> 2, tile, full);
+        } else {
+          tma_load_2d(stage + Cfg::kStageA, &map_x, kb * kKBytes, 0, full);
+          if (with_scales) tma_load_3d(sc + 512, &map_sx, 0, kb >> 2, 0, full);
+        }
+      }
+      if (++s == Cfg::kStages) { s = 0; ph ^= 1u; }
+    }
+  } else if (warp == 1) {
+    const bool leader = elect_one();
+    const uint64_t desc_w0 = make_desc(tiles, 16, 1024, 2), desc_x0 = make_desc(FUSED ? xs : tiles + Cfg::kStageA, 16, 1024, 2);
+    const uint64_t desc_s0 = make_desc(scales, 16, 128, 0);
+    const uint64_t desc_sx0 = make_desc(FUSED ? xs + kFuseBlocks * BN * kKBytes : scales + 512, 16, 128, 0);
+    uint32_t s = 0, ph = 0, sets = 0, sfw = 0;
+    bool ok = !FUSED || mbar_wait(bar_x, 0, abort_flag);
+    for (int kb = kb0; kb < kb1 && ok; ++kb) {
+      if (!mbar_wait(bar_full + 8 * s, ph, abort_flag)) { ok = false; break; }
+      tc_fence_after();
+      const uint64_t off = (s * Cfg::kStage) >> 4, xoff = FUSED ? ((kb - kb0) * (BN * kKBytes)) >> 4 : off;
+      if (kb == kb0 || (kb & 3) == 0) {
+        sfw = tmem_base + Cfg::kSfBase + (sets & 1u) * 4;
+        ++sets;
+        if (leader) {
+          tc_copy_scales<1>(sfw, desc_s0 + ((s * Cfg::kScales) >> 4));
+          tc_copy_scales<1>(sfw + 8, desc_sx0 + ((FUSED ? ((kb >> 2) - (kb0 >> 2)) * 512 : s * Cfg::kScales) >> 4));
+        }
+      }
+      const uint32_t idesc = make_idesc_f8(kTile, BN, kb & 3);
+      const int steps = kb + 1 == p.kblocks ? p.last_steps : 4;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k < steps && leader)
+          tc_mma_f8<1>(tmem_base, desc_w0 + off + 2 * k, desc_x0 + xoff + 2 * k, idesc, sfw, sfw + 8, kb != kb0 || k != 0 ? 1u : 0u);
+      if (leader) tc_commit(bar_empty + 8 * s);
+      if (++s == Cfg::kStages) { s = 0; ph ^= 1u; }
+    }
+    if (ok && leader) tc_commit(bar_done);
+  }
+  float* part = reinterpret_cast<float*>(gen_tiles);   // [BN][128]: every MMA has read the ring when bar_done flips
+  const int q = warp & 3;
+  const int64_t o = static_cast<int64_t>(tile) * kTile + q * 32 + lane;
+  const bool epilogue = warp >= 2 && warp < 6;
+  if (epilogue) {
+    const bool ok = mbar_wait(bar_done, 0, abort_flag);
+    tc_fence_after();
+    if (ok) {
+#pragma unroll 1
+      for (int c = 0; c < BN; c += 16) {
+        if (c >= p.M) break;
+        uint32_t r[16];
+        tc_load_16cols(tmem_base + (static_cast<uint32_t>(q * 32) << 16) + c, r);
+        if (p.split > 1) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) part[(c + j) * 128 + q * 32 + lane] = __uint_as_float(r[j]);
+        } else if (o < p.O) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            if (c + j < p.M) {
+              const float v = p.relu ? relu_keep_nan(__uint_as_float(r[j])) : __uint_as_float(r[j]);
+              if (p.out_bf16) static_cast<uint16_t*>(out)[(c + j) * p.O + o] = f32_to_bf16(v);
+              else static_cast<float*>(out)[(c + j) * p.O + o] = v;
+            }
+        }
+      }
+    }
+    tc_fence_before();
+  }
+  if (p.split > 1) {
+    __syncwarp();
+    cluster_sync_all();
+    if (epilogue && o < p.O) {
+      const uint32_t mine = smem_u32(part) + (q * 32 + lane) * 4;
+      switch (p.split) {
+        case 2: join_ranks<2>(mine, rank, o, out, p); break;
+        case 4: join_ranks<4>(mine, rank, o, out, p); break;
+        default: join_ranks<8>(mine, rank, o, out, p); break;
+      }
+    }
+  }
+  __syncwarp();
+  if (*abort_flag) {   // copies in flight land before the block leaves
+    const uint64_t t0 = global_timer();
+    while (global_timer() - t0 < 20000000ull) { }
+  }
+  if (p.split > 1) cluster_sync_all();   // the other ranks have read this block's sums
+  else __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base),
+                 "r"(static_cast<uint32_t>(Cfg::kTmemCols)) : "memory");
+  }
+}
+
+// ---- host side ----
+
+// Tensor maps are encoded on every call: 0.05 us each, no more than looking one up.
+bool encode(CUtensorMap* m, CUtensorMapDataType dt, cuuint32_t rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides,
+            const cuuint32_t* box, CUtensorMapSwizzle swz, CUtensorMapL2promotion l2) {
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return driver_api().tiled(m, dt, rank, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swz, l2,
+                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct F8Operand { const void* codes; const void* scale; F8View v; };
+
+bool encode_codes(CUtensorMap* m, const F8Operand& a, int box_rows) {
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(a.v.pitch), static_cast<cuuint64_t>(a.v.rows)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(a.v.pitch)};
+  const cuuint32_t box[2] = {kKBytes, static_cast<cuuint32_t>(box_rows)};
+  return encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, a.codes, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
+}
+
+// Scale tiles as (128 words, tiles along K, tiles along the rows), one tile a box.  Tiles past the end read as zeros.
+bool encode_scales(CUtensorMap* m, const F8Operand& a) {
+  const cuuint64_t dims[3] = {128, static_cast<cuuint64_t>(a.v.kt), static_cast<cuuint64_t>(a.v.rt)};
+  const cuuint64_t strides[2] = {512, static_cast<cuuint64_t>(a.v.kt) * 512};
+  const cuuint32_t box[3] = {128, 1, 1};
+  return encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, a.scale, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_NONE,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_128B);
+}
+
+bool encode_out(CUtensorMap* m, void* base, int64_t M, int64_t O, bool bf16) {
+  const cuuint64_t es = bf16 ? 2 : 4;
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(O), static_cast<cuuint64_t>(M)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(O) * es};
+  const cuuint32_t box[2] = {bf16 ? 64u : 32u, 32};
+  return encode(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, base, dims, strides, box,
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE);
+}
+
+// Instructions of 32 values along K: in K blocks of four, the last one as far as it goes.
+void k_steps(int64_t K, int* kblocks, int* last_steps) {
+  const int64_t steps = (K + 31) / 32;
+  *kblocks = static_cast<int>((steps + 3) / 4);
+  *last_steps = static_cast<int>(steps - 4 * static_cast<int64_t>(*kblocks - 1));
+}
+
+struct TilePlanF8 {
+  CUtensorMap ma, mb, msa, msb, mc;
+  F8Params p;
+  void* out;
+  int grid;
+};
+
+template <int BN, int CTAS>
+int plan_tiles(const F8Operand& a, const F8Operand& b, void* out, uint32_t flags, TilePlanF8* t) {
+  using Cfg = F8Cfg<BN, CTAS>;
+  static std::atomic<int> resident[64];   // per device, 0: not asked yet (threads may ask at once: the calls are idempotent)
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return GL_ERR_CUDA;
+  int at_once = resident[dev].load(std::memory_order_acquire);
+  if (!at_once) {
+    if (cudaFuncSetAttribute(dot_f8<BN, CTAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes) != cudaSuccess)
+      return GL_ERR_CUDA;
+    at_once = num_sms();
+    if (CTAS == 2) {   // SMs pair up within a GPC: a persistent grid must not exceed what is resident at once
+      cudaLaunchConfig_t cfg;
+      std::memset(&cfg, 0, sizeof(cfg));
+      cudaLaunchAttribute at;
+      std::memset(&at, 0, sizeof(at));
+      at.id = cudaLaunchAttributeClusterDimension;
+      at.val.clusterDim.x = CTAS;
+      at.val.clusterDim.y = at.val.clusterDim.z = 1;
+      cfg.gridDim = dim3(static_cast<unsigned>(num_sms() / 2 * 2));
+      cfg.blockDim = dim3(kF8Threads);
+      cfg.dynamicSmemBytes = Cfg::kSmemBytes;
+      cfg.attrs = &at;
+      cfg.numAttrs = 1;
+      if (cudaOccupancyMaxActiveClusters(&at_once, dot_f8<BN, CTAS>, &cfg) != cudaSuccess || at_once < 1) return GL_ERR_CUDA;
+      at_once = std::min(at_once, num_sms() / 2);
+    }
+    resident[dev].store(at_once, std::memory_order_release);
+  }
+  F8Params& p = t->p;
+  p.M = a.v.rows;
+  p.O = b.v.rows;
+  p.tiles_m = static_cast<int>((p.M + kTile * CTAS - 1) / (kTile * CTAS));
+  p.tiles_n = static_cast<int>((p.O + BN - 1) / BN);
+  if (static_cast<int64_t>(p.tiles_m) * p.tiles_n > (1 << 30)) return GL_ERR_UNSUPPORTED;
+  k_steps(a.v.K, &p.kblocks, &p.last_steps);
+  p.relu = (flags & GL_EPILOGUE_RELU) ? 1 : 0;
+  p.out_bf16 = (flags & GL_OUT_BF16) ? 1 : 0;
+  p.tma_store = p.O % (p.out_bf16 ? 8 : 4) == 0 ? 1 : 0;
+  p.div_tiles_n.set(p.tiles_n);
+  t->out = out;
+  t->grid = CTAS * std::min(at_once, p.tiles_m * p.tiles_n);
+  if (!encode_codes(&t->ma, a, kTile) || !encode_codes(&t->mb, b, BN / CTAS) || !encode_scales(&t->msa, a) ||
+      !encode_scales(&t->msb, b))
+    return GL_ERR_CUDA;
+  t->mc = t->ma;   // unused without TMA stores; any valid map
+  if (p.tma_store && !encode_out(&t->mc, out, p.M, p.O, p.out_bf16 != 0)) return GL_ERR_CUDA;
+  return GL_OK;
+}
+
+template <int BN, int CTAS>
+int run_tiles(const TilePlanF8& t, cudaStream_t st) {
+  return launch_pdl(dot_f8<BN, CTAS>, dim3(static_cast<unsigned>(t.grid)), dim3(kF8Threads), F8Cfg<BN, CTAS>::kSmemBytes, st, CTAS,
+                    t.ma, t.mb, t.msa, t.msb, t.mc, t.out, t.p) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
+}
+
+struct FewPlanF8 {
+  CUtensorMap mw, mx, msw, msx;
+  F8FewParams p;
+  void* out;
+  int grid;
+};
+
+// `FUSED`: A is still to be rounded, by the product's own blocks.
+template <int BN, bool FUSED>
+int plan_few(const F8Operand& a, const F8Operand& b, void* out, uint32_t flags, FewPlanF8* t) {
+  static std::atomic<bool> attr_set[64];   // per device (threads may set it at once: the call is idempotent)
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return GL_ERR_CUDA;
+  if (!attr_set[dev].load(std::memory_order_acquire)) {
+    if (cudaFuncSetAttribute(dot_f8_few<BN, FUSED>, cudaFuncAttributeMaxDynamicSharedMemorySize, F8FewCfg<BN, FUSED>::kSmemBytes) !=
+        cudaSuccess)
+      return GL_ERR_CUDA;
+    attr_set[dev].store(true, std::memory_order_release);
+  }
+  F8FewParams& p = t->p;
+  p.M = static_cast<int>(a.v.rows);
+  p.O = b.v.rows;
+  p.x = nullptr;
+  p.K = a.v.K;
+  p.x_f32 = 0;
+  k_steps(a.v.K, &p.kblocks, &p.last_steps);
+  p.relu = (flags & GL_EPILOGUE_RELU) ? 1 : 0;
+  p.out_bf16 = (flags & GL_OUT_BF16) ? 1 : 0;
+  if (b.v.rt > (1 << 27)) return GL_ERR_UNSUPPORTED;
+  const int tiles = static_cast<int>(b.v.rt);
+  // as many ranks as still leave every one a K block and all blocks resident at once (two per SM)
+  p.split = 1;
+  while (p.split < 8 && p.split * 2 <= p.kblocks && tiles * p.split * 2 <= 2 * num_sms()) p.split *= 2;
+  t->out = out;
+  t->grid = tiles * p.split;
+  if (!encode_codes(&t->mw, b, kTile) || !encode_scales(&t->msw, b)) return GL_ERR_CUDA;
+  t->mx = t->mw;   // unused when FUSED; any valid map
+  t->msx = t->msw;
+  return FUSED || (encode_codes(&t->mx, a, BN) && encode_scales(&t->msx, a)) ? GL_OK : GL_ERR_CUDA;
+}
+
+template <int BN, bool FUSED>
+int run_few(const FewPlanF8& t, cudaStream_t st) {
+  return launch_pdl(dot_f8_few<BN, FUSED>, dim3(static_cast<unsigned>(t.grid)), dim3(kF8Threads), F8FewCfg<BN, FUSED>::kSmemBytes, st,
+                    t.p.split, t.mw, t.mx, t.msw, t.msx, t.out, t.p) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
+}
+
+template <int BN, typename Pre>
+int product_few(const F8Operand& a, const F8Operand& b, gl_ap* out, uint32_t flags, cudaStream_t st, Pre&& pre) {
+  FewPlanF8 t;
+  int rc = plan_few<BN, false>(a, b, out->data, flags, &t);
+  if (rc) return rc;
+  rc = pre();
+  if (rc) return rc;
+  return run_few<BN, false>(t, st);
+}
+
+// Checks shared by the two products: shapes, result, aliasing rules are the caller's.
+int check_product(const gl_ap* out, int a_access, const int64_t* a_shape, int a_compute, const gl_f8* a1, uint32_t flags) {
+  if (flags & ~(GL_EPILOGUE_RELU | GL_OUT_BF16)) return GL_ERR_UNSUPPORTED;
+  if (a_compute != a1->ndim - a1->access_ndim) return GL_ERR_SHAPE;
+  for (int i = 0; i < a_compute; ++i)
+    if (a_shape[a_access + i] != a1->shape[a1->access_ndim + i]) return GL_ERR_SHAPE;
+  if (a_access + a1->access_ndim > GL_MAX_DIMS) return GL_ERR_NDIM;
+  gl_ap want;
+  std::memset(&want, 0, sizeof(want));
+  want.dtype = (flags & GL_OUT_BF16) ? GL_BF16 : GL_F32;
+  for (int i = 0; i < a_access; ++i) want.shape[want.ndim++] = a_shape[i];
+  for (int i = 0; i < a1->access_ndim; ++i) want.shape[want.ndim++] = a1->shape[i];
+  want.access_ndim = want.ndim;
+  const int rc = check_same_meta(want, out);
+  if (rc) return rc;
+  return check_data(out);
+}
+
+// Product of two operands that have been checked; everything that can fail does so before `pre` enqueues anything.
+template <typename Pre>
+int product(const F8Operand& a, const F8Operand& b, gl_ap* out, uint32_t flags, cudaStream_t st, Pre&& pre) {
+  if (!driver_api().ok) return GL_ERR_CUDA;
+  // Up to 128 rows: the weights as the 128-row side, K cut over clusters.
+  if (a.v.rows <= 16) return product_few<16>(a, b, out, flags, st, pre);
+  if (a.v.rows <= 32) return product_few<32>(a, b, out, flags, st, pre);
+  if (a.v.rows <= 64) return product_few<64>(a, b, out, flags, st, pre);
+  if (a.v.rows <= 128) return product_few<128>(a, b, out, flags, st, pre);
+  // 256 x 256 tiles on pairs of SMs move half the bytes per flop of 128 x 128 tiles, but there are a quarter as many.
+  TilePlanF8 t;
+  const auto tiles = [&](int64_t side) { return ((a.v.rows + side - 1) / side) * ((b.v.rows + side - 1) / side); };
+  const auto rounds = [](int64_t n, int64_t at_once) { return (n + at_once - 1) / at_once; };
+  const bool pairs = 3 * rounds(tiles(256), num_sms() / 2) <= 2 * rounds(tiles(128), num_sms());
+  int rc = pairs ? plan_tiles<256, 2>(a, b, out->data, flags, &t) : plan_tiles<128, 1>(a, b, out->data, flags, &t);
+  if (rc) return rc;
+  rc = pre();
+  if (rc) return rc;
+  return pairs ? run_tiles<256, 2>(t, st) : run_tiles<128, 1>(t, st);
+}
+
+size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+
+// The left operand of a dense layer, as the call holds it in its workspace.
+gl_f8 rounded_left(const gl_ap* a0) {
+  gl_f8 q;
+  std::memset(&q, 0, sizeof(q));
+  q.ndim = a0->ndim;
+  q.access_ndim = a0->access_ndim;
+  for (int i = 0; i < a0->ndim; ++i) q.shape[i] = a0->shape[i];
+  return q;
+}
+
+}  // namespace
+
+namespace gl {
+int take_status_f8() {
+  unsigned int v = 0;
+  if (cudaMemcpyFromSymbol(&v, g_status, sizeof(v)) != cudaSuccess) return GL_ERR_CUDA;
+  if (!v) return GL_OK;
+  const unsigned int zero = 0;
+  if (cudaMemcpyToSymbol(g_status, &zero, sizeof(zero)) != cudaSuccess) return GL_ERR_CUDA;
+  return GL_ERR_TIMEOUT;
+}
+}  // namespace gl
+
+extern "C" {
+
+size_t gl_f8_data_bytes(const gl_f8* a) {
+  F8View v;
+  return check_f8_meta(a, &v) ? 0 : static_cast<size_t>(v.rows) * v.pitch;
+}
+
+size_t gl_f8_scale_bytes(const gl_f8* a) {
+  F8View v;
+  return check_f8_meta(a, &v) ? 0 : static_cast<size_t>(v.rt) * v.kt * 512;
+}
+
+int gl_f8_quantize(const gl_ap* in, gl_f8* out, void* stream) {
+  int rc = check_data(in);
+  if (rc) return rc;
+  F8View v;
+  rc = check_f8_data(out, &v);
+  if (rc) return rc;
+  if (!f8_same_shape(in, out)) return GL_ERR_SHAPE;
+  return launch_quantize(*in, v, out->data, out->scale, static_cast<cudaStream_t>(stream));
+}
+
+int gl_f8_dequantize(const gl_f8* in, gl_ap* out, void* stream) {
+  F8View v;
+  int rc = check_f8_data(in, &v);
+  if (rc) return rc;
+  rc = check_data(out);
+  if (rc) return rc;
+  if (!f8_same_shape(out, in)) return GL_ERR_SHAPE;
+  const F8QuantParams p = f8_quant_params(v);
+  const bool f32 = out->dtype == GL_F32, vec = v.K % 8 == 0;
+  constexpr int kU = kUnitsPerWarp;
+  void (*k)(const uint8_t*, const uint8_t*, void*, F8QuantParams) =
+      many_units(p) ? (f32 ? (vec ? dequantize_f8<true, true, kU> : dequantize_f8<true, false, kU>)
+                           : (vec ? dequantize_f8<false, true, kU> : dequantize_f8<false, false, kU>))
+                    : (f32 ? (vec ? dequantize_f8<true, true, 1> : dequantize_f8<true, false, 1>)
+                           : (vec ? dequantize_f8<false, true, 1> : dequantize_f8<false, false, 1>));
+  return launch_pdl(k, unit_grid(p), dim3(256), 0, static_cast<cudaStream_t>(stream), 1, static_cast<const uint8_t*>(in->data),
+                    static_cast<const uint8_t*>(in->scale), out->data, p) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
+}
+
+int gl_cartesian_dot_f8(const gl_f8* a0, const gl_f8* a1, gl_ap* out, uint32_t flags, void* stream) {
+  F8Operand a, b;
+  int rc = check_f8_data(a0, &a.v);
+  if (rc) return rc;
+  rc = check_f8_data(a1, &b.v);
+  if (rc) return rc;
+  rc = check_product(out, a0->access_ndim, a0->shape, a0->ndim - a0->access_ndim, a1, flags);
+  if (rc) return rc;
+  a.codes = a0->data;
+  a.scale = a0->scale;
+  b.codes = a1->data;
+  b.scale = a1->scale;
+  return product(a, b, out, flags, static_cast<cudaStream_t>(stream), [] { return GL_OK; });
+}
+
+size_t gl_dense_f8_workspace(const gl_ap* a0, const gl_f8* a1) {
+  F8View v;
+  if (check_meta(a0) || check_f8_meta(a1, &v)) return 0;
+  const gl_f8 q = rounded_left(a0);
+  return round_up(gl_f8_data_bytes(&q), 1024) + gl_f8_scale_bytes(&q);
+}
+
+int gl_dense_f8(const gl_ap* a0, const gl_f8* a1, gl_ap* out, uint32_t flags, void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = check_data(a0);
+  if (rc) return rc;
+  F8Operand a, b;
+  rc = check_f8_data(a1, &b.v);
+  if (rc) return rc;
+  rc = check_product(out, a0->access_ndim, a0->shape, a0->ndim - a0->access_ndim, a1, flags);
+  if (rc) return rc;
+  gl_f8 q = rounded_left(a0);
+  rc = check_f8_meta(&q, &a.v);
+  if (rc) return rc;
+  const size_t need = gl_dense_f8_workspace(a0, a1);
+  if (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 1023u)) return GL_ERR_WORKSPACE;
+  q.data = workspace;
+  q.scale = static_cast<char*>(workspace) + round_up(gl_f8_data_bytes(&q), 1024);
+  b.codes = a1->data;
+  b.scale = a1->scale;
+  a.codes = q.data;
+  a.scale = q.scale;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (a.v.rows <= kFuseRows) {
+    if (!driver_api().ok) return GL_ERR_CUDA;
+    FewPlanF8 t;
+    rc = plan_few<16, true>(a, b, out->data, flags, &t);
+    if (rc) return rc;
+    if ((t.p.kblocks + t.p.split - 1) / t.p.split <= kFuseBlocks) {
+      t.p.x = a0->data;
+      t.p.x_f32 = a0->dtype == GL_F32;
+      return run_few<16, true>(t, st);
+    }
+  }
+  return product(a, b, out, flags, st, [&] { return launch_quantize(*a0, a.v, q.data, q.scale, st); });
+}
+
+}  // extern "C"

@@ -17,6 +17,7 @@
 #include <atomic>
 #include <cstring>
 
+#include "gl_f8.h"
 #include "gl_internal.h"
 #include "gl_launch.cuh"
 #include "gl_mx4.cuh"
@@ -1126,13 +1127,15 @@ size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 }  // namespace
 
 namespace gl {
+// The status words of the operators on narrow operands: this file's and gl_f8.cu's.
 int take_status_mx4() {
   unsigned int v = 0;
   if (cudaMemcpyFromSymbol(&v, g_status, sizeof(v)) != cudaSuccess) return GL_ERR_CUDA;
-  if (!v) return GL_OK;
+  const int eight = take_status_f8();
+  if (!v) return eight;
   const unsigned int zero = 0;
   if (cudaMemcpyToSymbol(g_status, &zero, sizeof(zero)) != cudaSuccess) return GL_ERR_CUDA;
-  return GL_ERR_TIMEOUT;
+  return eight ? eight : GL_ERR_TIMEOUT;
 }
 }  // namespace gl
 

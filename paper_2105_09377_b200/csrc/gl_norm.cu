@@ -1,0 +1,351 @@
+// compute norm_rms: items divided by their root mean square, optionally with a residual added first, results as GL_BF16,
+// GL_F32 or as an F8 operand.
+//   h = x + residual;  sum = h in the residual's type;  y = h / sqrt(mean(h^2) + eps) * weight
+#include <cuda_runtime.h>
+
+#include <cmath>
+#include <cstring>
+
+#include "gl_f8.cuh"
+#include "gl_internal.h"
+#include "gl_launch.cuh"
+#include "gl_tc.cuh"
+#include "gl_tmap.h"
+
+using namespace gl;
+
+namespace {
+
+enum { kNone = 0, kBf16 = 1, kF32 = 2 };              // types of the residual and of the weights
+enum { kOutBf16 = 0, kOutF32 = 1, kOutF8 = 2 };
+
+struct NormParams {
+  const void* x;
+  const void* res;
+  const void* weight;
+  void* sum;
+  void* out;             // values, or codes
+  uint8_t* scale;        // F8 only
+  uint32_t rows;
+  int32_t K, pitch;
+  uint32_t kt;
+  int32_t units;         // units of 256 values per row
+  int32_t weight_type;
+  int32_t row_warps;     // warps per row, a power of two
+  float eps, inv_k;
+};
+
+template <bool VEC>
+__device__ __forceinline__ void load_weights(const NormParams& p, int k0, int lane, float (&w)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) w[j] = 1.f;
+  if (p.weight_type == kNone) return;
+  if (VEC) {
+    const int at = k0 + lane * 8;
+    if (at >= p.K) return;
+    if (p.weight_type == kF32) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float4 v = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(p.weight) + at) + i);
+        w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+      }
+    } else {
+      const uint4 v = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.weight) + at));
+      const uint32_t raw[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { w[2 * i] = __uint_as_float(raw[i] << 16); w[2 * i + 1] = __uint_as_float(raw[i] & 0xFFFF0000u); }
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int at = k0 + j * 32 + lane;
+      if (at < p.K)
+        w[j] = p.weight_type == kF32 ? __ldg(static_cast<const float*>(p.weight) + at)
+                                     : bf16_to_f32(__ldg(static_cast<const uint16_t*>(p.weight) + at));
+    }
+  }
+}
+
+// Eight values per lane of the unit at k0 to the row at `row`.  Every lane of the warp takes part.
+template <bool F32, bool VEC>
+__device__ __forceinline__ void unit_store(const float (&v)[8], void* row, int k0, int K, int lane) {
+  if (VEC && F32) {
+    // two lanes' 64 bytes in two stores that each write whole 32-byte sectors: first the even lane's values, then the odd's
+    const bool odd = lane & 1;
+    float got[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) got[i] = __shfl_xor_sync(0xFFFFFFFFu, odd ? v[i] : v[4 + i], 1);
+    const int at = k0 + (lane & ~1) * 8;
+    float4* o = reinterpret_cast<float4*>(static_cast<float*>(row) + at) + odd;
+    if (at < K) *o = odd ? make_float4(got[0], got[1], got[2], got[3]) : make_float4(v[0], v[1], v[2], v[3]);
+    if (at + 8 < K) o[2] = odd ? make_float4(v[4], v[5], v[6], v[7]) : make_float4(got[0], got[1], got[2], got[3]);
+  } else if (VEC) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(__float_as_uint(v[2 * i]), __float_as_uint(v[2 * i + 1]));
+    const int at = k0 + lane * 8;
+    if (at < K) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(row) + at) = make_uint4(w[0], w[1], w[2], w[3]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int at = k0 + j * 32 + lane;
+      if (at < K) {
+        if (F32) static_cast<float*>(row)[at] = v[j];
+        else static_cast<uint16_t*>(row)[at] = f32_to_bf16(v[j]);
+      }
+    }
+  }
+}
+
+template <int OUT, bool VEC>
+__device__ __forceinline__ void store_result(const float (&y)[8], const NormParams& p, uint32_t row, int unit, int lane) {
+  const int k0 = unit * kF8Unit;
+  if (OUT == kOutF8)
+    unit_store_f8<VEC>(y, static_cast<uint8_t*>(p.out) + static_cast<int64_t>(row) * p.pitch, k0, p.pitch, lane,
+                       p.scale + f8_scale_at(row, unit * 2, p.kt));
+  else
+    unit_store<OUT == kOutF32, VEC>(y, static_cast<char*>(p.out) + static_cast<int64_t>(row) * p.K * (OUT == kOutF32 ? 4 : 2), k0, p.K, lane);
+}
+
+// h of a unit from what was loaded.
+template <bool XF32, int RES, bool VEC>
+__device__ __forceinline__ void add_residual(const uint32_t (&x)[8], const uint32_t (&r)[8], float (&h)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    h[j] = unit_value<XF32, VEC>(x, j);
+    if (RES != kNone) h[j] += unit_value<RES == kF32, VEC>(r, j);
+  }
+}
+
+// Sum over the warps of a row; `slots` holds one float per warp of the block.  All threads of the block call it.
+__device__ __forceinline__ float row_sum(float s, float* slots, int row_warps) {
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+  if (row_warps == 1) return s;
+  const int warp = threadIdx.x >> 5, first = warp & ~(row_warps - 1);
+  if ((threadIdx.x & 31) == 0) slots[warp] = s;
+  __syncthreads();
+  s = 0.f;
+  for (int w = 0; w < row_warps; ++w) s += slots[first + w];
+  return s;
+}
+
+// A row stays in registers between the sum of its squares and its results: C units a warp, `row_warps` warps a row, as many rows a
+// block as fit.  Everything is read once; bound by HBM.
+template <bool XF32, int RES, int OUT, bool VEC, int C>
+__global__ void __launch_bounds__(C == 4 ? 512 : 1024) norm_rms(const NormParams p) {
+  __shared__ float slots[32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t row = blockIdx.x * ((blockDim.x >> 5) / p.row_warps) + warp / p.row_warps;
+  const int unit0 = warp & (p.row_warps - 1);
+  const bool live = row < p.rows;
+  const char* x = static_cast<const char*>(p.x) + static_cast<int64_t>(row) * p.K * (XF32 ? 4 : 2);
+  const char* r = static_cast<const char*>(p.res) + static_cast<int64_t>(row) * p.K * (RES == kF32 ? 4 : 2);
+  pdl_wait();
+  pdl_launch_dependents();
+  uint32_t raw_x[C][8], raw_r[RES == kNone ? 1 : C][8];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int unit = unit0 + c * p.row_warps;
+    if (live && unit < p.units) {
+      unit_load<XF32, VEC>(x, unit * kF8Unit, p.K, lane, raw_x[c]);
+      if (RES != kNone) unit_load<RES == kF32, VEC>(r, unit * kF8Unit, p.K, lane, raw_r[c]);
+    }
+  }
+  float h[C][8], s = 0.f;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int unit = unit0 + c * p.row_warps;
+    if (live && unit < p.units) {
+      add_residual<XF32, RES, VEC>(raw_x[c], raw_r[RES == kNone ? 0 : c], h[c]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s = fmaf(h[c][j], h[c][j], s);
+      if (RES != kNone && p.sum)
+        unit_store<RES == kF32, VEC>(h[c], static_cast<char*>(p.sum) + static_cast<int64_t>(row) * p.K * (RES == kF32 ? 4 : 2),
+                                     unit * kF8Unit, p.K, lane);
+    }
+  }
+  const float rs = 1.f / sqrtf(row_sum(s, slots, p.row_warps) * p.inv_k + p.eps);
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int unit = unit0 + c * p.row_warps;
+    if (live && unit < p.units) {
+      float w[8];
+      load_weights<VEC>(p, unit * kF8Unit, lane, w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] *= h[c][j] * rs;
+      store_result<OUT, VEC>(w, p, row, unit, lane);
+    }
+  }
+}
+
+// Rows that do not fit in a block's registers: a block per row, read twice (the second time mostly from L2).  Nothing is written
+// before a value's second reading, so results may take the operands' place here too.
+template <bool XF32, int RES, int OUT, bool VEC>
+__global__ void __launch_bounds__(1024) norm_rms_long(const NormParams p) {
+  __shared__ float slots[32];
+  const int lane = threadIdx.x & 31;
+  const uint32_t row = blockIdx.x;
+  const char* x = static_cast<const char*>(p.x) + static_cast<int64_t>(row) * p.K * (XF32 ? 4 : 2);
+  const char* r = static_cast<const char*>(p.res) + static_cast<int64_t>(row) * p.K * (RES == kF32 ? 4 : 2);
+  pdl_wait();
+  pdl_launch_dependents();
+  float s = 0.f;
+  uint32_t raw_x[8], raw_r[8];
+  float h[8];
+  for (int unit = threadIdx.x >> 5; unit < p.units; unit += 32) {
+    unit_load<XF32, VEC>(x, unit * kF8Unit, p.K, lane, raw_x);
+    if (RES != kNone) unit_load<RES == kF32, VEC>(r, unit * kF8Unit, p.K, lane, raw_r);
+    add_residual<XF32, RES, VEC>(raw_x, raw_r, h);
+    float part = 0.f;   // (a lane adds up to 2^15 values for the longest rows: by units of eight first)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) part = fmaf(h[j], h[j], part);
+    s += part;
+  }
+  const float rs = 1.f / sqrtf(row_sum(s, slots, 32) * p.inv_k + p.eps);
+  for (int unit = threadIdx.x >> 5; unit < p.units; unit += 32) {
+    unit_load<XF32, VEC>(x, unit * kF8Unit, p.K, lane, raw_x);
+    if (RES != kNone) unit_load<RES == kF32, VEC>(r, unit * kF8Unit, p.K, lane, raw_r);
+    add_residual<XF32, RES, VEC>(raw_x, raw_r, h);
+    if (RES != kNone && p.sum)
+      unit_store<RES == kF32, VEC>(h, static_cast<char*>(p.sum) + static_cast<int64_t>(row) * p.K * (RES == kF32 ? 4 : 2),
+                                   unit * kF8Unit, p.K, lane);
+    float w[8];
+    load_weights<VEC>(p, unit * kF8Unit, lane, w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] *= h[j] * rs;
+    store_result<OUT, VEC>(w, p, row, unit, lane);
+  }
+}
+
+template <bool XF32, int RES, int OUT, bool VEC>
+int launch_norm(NormParams p, cudaStream_t st) {
+  // Four units a warp when there are rows enough to fill the machine; a row alone is spread over as many warps as it has units.
+  const bool spread = p.rows <= static_cast<uint32_t>(num_sms());
+  const int want = spread ? p.units : (p.units + 3) / 4;
+  p.row_warps = 1;
+  while (p.row_warps < want && p.row_warps < 32) p.row_warps *= 2;
+  const int per_warp = (p.units + p.row_warps - 1) / p.row_warps;
+  const int warps = p.row_warps > 8 ? p.row_warps : 8;
+  const uint32_t per_block = static_cast<uint32_t>(warps / p.row_warps);
+  const dim3 grid((p.rows + per_block - 1) / per_block), block(static_cast<unsigned>(warps * 32));
+  void (*k)(NormParams) = per_warp == 1   ? norm_rms<XF32, RES, OUT, VEC, 1>
+                          : per_warp == 2 ? norm_rms<XF32, RES, OUT, VEC, 2>
+                          : p.row_warps <= 16 ? norm_rms<XF32, RES, OUT, VEC, 4>   // (then four units a warp suffice)
+                                              : norm_rms_long<XF32, RES, OUT, VEC>;
+  return launch_pdl(k, grid, block, 0, st, 1, p) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
+}
+
+template <bool XF32, int RES, int OUT>
+int launch_vec(const NormParams& p, cudaStream_t st) {
+  return p.K % 8 == 0 ? launch_norm<XF32, RES, OUT, true>(p, st) : launch_norm<XF32, RES, OUT, false>(p, st);
+}
+template <bool XF32, int RES>
+int launch_out(const NormParams& p, int out, cudaStream_t st) {
+  switch (out) {
+    case kOutBf16: return launch_vec<XF32, RES, kOutBf16>(p, st);
+    case kOutF32: return launch_vec<XF32, RES, kOutF32>(p, st);
+    default: return launch_vec<XF32, RES, kOutF8>(p, st);
+  }
+}
+template <bool XF32>
+int launch_res(const NormParams& p, int res, int out, cudaStream_t st) {
+  switch (res) {
+    case kNone: return launch_out<XF32, kNone>(p, out, st);
+    case kBf16: return launch_out<XF32, kBf16>(p, out, st);
+    default: return launch_out<XF32, kF32>(p, out, st);
+  }
+}
+
+int type_of(const gl_ap* a) { return !a ? kNone : a->dtype == GL_F32 ? kF32 : kBf16; }
+
+bool same_shape(const gl_ap* a, const gl_ap* b) {
+  if (a->ndim != b->ndim || a->access_ndim != b->access_ndim) return false;
+  for (int i = 0; i < a->ndim; ++i)
+    if (a->shape[i] != b->shape[i]) return false;
+  return true;
+}
+
+// Everything but the result, which the two entry points check themselves.
+int norm_params(const gl_ap* x, const gl_ap* residual, const gl_ap* weight, float eps, const gl_ap* sum, NormParams* p) {
+  int rc = check_data(x);
+  if (rc) return rc;
+  if (x->ndim == x->access_ndim) return GL_ERR_SHAPE;   // no compute dimensions to take the mean of
+  if (residual) {
+    rc = check_data(residual);
+    if (rc) return rc;
+    if (!same_shape(x, residual)) return GL_ERR_SHAPE;
+  }
+  if (sum) {
+    if (!residual) return GL_ERR_NULL;
+    rc = check_same_meta(*residual, sum);
+    if (rc) return rc;
+    rc = check_data(sum);
+    if (rc) return rc;
+  }
+  if (weight) {
+    rc = check_data(weight);
+    if (rc) return rc;
+    if (weight->access_ndim != 0 || weight->ndim != x->ndim - x->access_ndim) return GL_ERR_SHAPE;
+    for (int i = 0; i < weight->ndim; ++i)
+      if (weight->shape[i] != x->shape[x->access_ndim + i]) return GL_ERR_SHAPE;
+  }
+  if (!(eps >= 0.f) || std::isinf(eps)) return GL_ERR_SHAPE;
+  gl_f8 as_items;   // (the limits are those of the F8 format, whatever the result's type)
+  std::memset(&as_items, 0, sizeof(as_items));
+  as_items.ndim = x->ndim;
+  as_items.access_ndim = x->access_ndim;
+  for (int i = 0; i < x->ndim; ++i) as_items.shape[i] = x->shape[i];
+  F8View v;
+  rc = check_f8_meta(&as_items, &v);
+  if (rc) return rc;
+  std::memset(p, 0, sizeof(*p));
+  p->x = x->data;
+  p->res = residual ? residual->data : nullptr;
+  p->weight = weight ? weight->data : nullptr;
+  p->sum = sum ? sum->data : nullptr;
+  p->rows = static_cast<uint32_t>(v.rows);
+  p->K = static_cast<int32_t>(v.K);
+  p->pitch = static_cast<int32_t>(v.pitch);
+  p->kt = static_cast<uint32_t>(v.kt);
+  p->units = static_cast<int32_t>((v.nb + 1) / 2);
+  p->weight_type = type_of(weight);
+  p->eps = eps;
+  p->inv_k = static_cast<float>(1.0 / static_cast<double>(v.K));
+  return GL_OK;
+}
+
+int run_norm(const gl_ap* x, const gl_ap* residual, const NormParams& p, int out, void* stream) {
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return x->dtype == GL_F32 ? launch_res<true>(p, type_of(residual), out, st) : launch_res<false>(p, type_of(residual), out, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+int gl_compute_norm_rms(const gl_ap* x, const gl_ap* residual, const gl_ap* weight, float eps, gl_ap* sum, gl_ap* out, void* stream) {
+  NormParams p;
+  int rc = norm_params(x, residual, weight, eps, sum, &p);
+  if (rc) return rc;
+  rc = check_data(out);
+  if (rc) return rc;
+  if (!same_shape(x, out)) return GL_ERR_SHAPE;
+  p.out = out->data;
+  return run_norm(x, residual, p, out->dtype == GL_F32 ? kOutF32 : kOutBf16, stream);
+}
+
+int gl_compute_norm_rms_f8(const gl_ap* x, const gl_ap* residual, const gl_ap* weight, float eps, gl_ap* sum, gl_f8* out, void* stream) {
+  NormParams p;
+  int rc = norm_params(x, residual, weight, eps, sum, &p);
+  if (rc) return rc;
+  F8View v;
+  rc = check_f8_data(out, &v);
+  if (rc) return rc;
+  if (!f8_same_shape(x, out)) return GL_ERR_SHAPE;
+  p.out = out->data;
+  p.scale = static_cast<uint8_t*>(out->scale);
+  return run_norm(x, residual, p, kOutF8, stream);
+}
+
+}  // extern "C"
