@@ -26,41 +26,51 @@ namespace {
 // Quantisation and its inverse
 // ------------------------------------------------------------------------
 
-// A warp takes U units of 256 values (two blocks), consecutive ones, all requested before the first is used.  The unit's row and
-// place are the same for the whole warp: one division per warp and unit.  Bound by HBM.
+// A warp takes strips of U consecutive units of a row, R rows one below the other, all requested before the first is used: U * R is
+// eight when there are strips enough to fill the machine, and U no larger than a row has units.  Places inside a strip are fixed
+// distances, so finding them costs next to nothing.  Bound by HBM.
 struct F8QuantParams {
   int32_t K, pitch;
-  uint32_t kt;
-  uint32_t units;       // rows * per_row
-  FastDiv per_row;      // units per row
+  uint32_t kt, rows;
+  uint32_t strips;      // strips of U units: row groups * strips of a row
+  FastDiv per_row;      // strips of a row
 };
 
-template <bool F32, bool VEC, int U>
+template <bool F32, bool VEC, int U, int R>
 __global__ void __launch_bounds__(256) quantize_f8(const void* __restrict__ in, uint8_t* __restrict__ codes,
                                                    uint8_t* __restrict__ scale, const F8QuantParams p) {
   pdl_wait();
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31;
-  const uint32_t first = (blockIdx.x * 8u + (threadIdx.x >> 5)) * U;
-  uint32_t raw[U][8];
+  const uint32_t strip = blockIdx.x * 8u + (threadIdx.x >> 5);
+  if (strip >= p.strips) return;
+  uint32_t group, at;
+  p.per_row.divmod(strip, group, at);
+  const uint32_t row0 = group * R;
+  const int k0 = static_cast<int>(at) * (U * kF8Unit);
+  const int64_t total = static_cast<int64_t>(p.rows) * p.K * (F32 ? 4 : 2);
+  uint32_t raw[R * U][8];
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    if (first + u >= p.units) break;
-    uint32_t row, at;
-    p.per_row.divmod(first + u, row, at);
-    unit_load<F32, VEC>(static_cast<const char*>(in) + static_cast<int64_t>(row) * p.K * (F32 ? 4 : 2), static_cast<int>(at) * kF8Unit,
-                        p.K, lane, raw[u]);
+  for (int r = 0; r < R; ++r) {
+    if (row0 + r >= p.rows) break;
+    const LaneAt l(row0 + r, k0, p.K, lane, F32 ? 4 : 2);
+#pragma unroll
+    for (int u = 0; u < U; ++u) unit_load<F32, VEC>(in, l, u, total, raw[r * U + u]);
   }
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    if (first + u >= p.units) break;
-    uint32_t row, at;
-    p.per_row.divmod(first + u, row, at);
-    float v[8];
+  for (int r = 0; r < R; ++r) {
+    const uint32_t row = row0 + r;
+    if (row >= p.rows) break;
+    uint8_t* to = codes + static_cast<int64_t>(row) * p.pitch + k0 + lane * 8;
+    uint8_t* scale_to = scale + f8_scale_at(row, at * (2 * U), p.kt);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = unit_value<F32, VEC>(raw[u], j);
-    unit_store_f8<VEC>(v, codes + static_cast<int64_t>(row) * p.pitch, static_cast<int>(at) * kF8Unit, p.pitch, lane,
-                       scale + f8_scale_at(row, at * 2, p.kt));
+    for (int u = 0; u < U; ++u) {
+      if (k0 + u * kF8Unit >= p.K) break;
+      float2 v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = unit_values<F32>(raw[r * U + u], i);
+      unit_store_f8(v, to, p.pitch - k0 - lane * 8, scale_to, u, lane);
+    }
   }
 }
 
@@ -71,107 +81,126 @@ __device__ __forceinline__ float2 f8_values2(uint32_t two) {
   return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
-// Going back, the lanes' values follow the stores: eight bf16 values or two times four floats, 16 bytes each.
-template <bool F32, bool VEC, int U>
+// Going back, aligned fp32 rows are held as two times four values a lane instead of eight in a row: 16-byte stores next to each
+// other.
+template <bool F32, bool VEC, int U, int R>
 __global__ void __launch_bounds__(256) dequantize_f8(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scale,
                                                      void* __restrict__ out, const F8QuantParams p) {
+  constexpr bool kHalves = F32 && VEC;
   pdl_wait();
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31;
-  const uint32_t first = (blockIdx.x * 8u + (threadIdx.x >> 5)) * U;
-  uint32_t word[U][2], e[U];
+  const uint32_t strip = blockIdx.x * 8u + (threadIdx.x >> 5);
+  if (strip >= p.strips) return;
+  uint32_t group, at;
+  p.per_row.divmod(strip, group, at);
+  const uint32_t row0 = group * R;
+  const int k0 = static_cast<int>(at) * (U * kF8Unit);
+  uint32_t word[R * U][2], e[R * U];
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    word[u][0] = word[u][1] = e[u] = 0;
-    if (first + u >= p.units) break;
-    uint32_t row, at;
-    p.per_row.divmod(first + u, row, at);
-    const uint8_t* src = codes + static_cast<int64_t>(row) * p.pitch;
-    const int k0 = static_cast<int>(at) * kF8Unit;
-    e[u] = *reinterpret_cast<const uint16_t*>(scale + f8_scale_at(row, at * 2, p.kt));
-    if (VEC && !F32) {
-      if (k0 + lane * 8 < p.K) {
-        const uint2 w = __ldcs(reinterpret_cast<const uint2*>(src + k0 + lane * 8));
-        word[u][0] = w.x;
-        word[u][1] = w.y;
+  for (int r = 0; r < R; ++r) {
+    const uint32_t row = row0 + r;
+    if (row >= p.rows) break;
+    const uint8_t* src = codes + static_cast<int64_t>(row) * p.pitch + k0;
+    const uint8_t* scale_at = scale + f8_scale_at(row, at * (2 * U), p.kt);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      uint32_t(&w)[2] = word[r * U + u];
+      w[0] = w[1] = 0;
+      if (k0 + u * kF8Unit >= p.K) break;
+      e[r * U + u] = *reinterpret_cast<const uint16_t*>(scale_at + (u >> 1) * 512 + (u & 1) * 2);
+      if (kHalves) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          if (k0 + u * kF8Unit + h * 128 + lane * 4 < p.K)
+            w[h] = __ldcs(reinterpret_cast<const uint32_t*>(src + lane * 4 + u * kF8Unit + h * 128));
+      } else if (k0 + u * kF8Unit + lane * 8 < p.pitch) {
+        const uint2 x = __ldcs(reinterpret_cast<const uint2*>(src + lane * 8 + u * kF8Unit));
+        w[0] = x.x;
+        w[1] = x.y;
       }
-    } else if (VEC) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        if (k0 + h * 128 + lane * 4 < p.K) word[u][h] = __ldcs(reinterpret_cast<const uint32_t*>(src + k0 + h * 128 + lane * 4));
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (k0 + j * 32 + lane < p.K) word[u][j >> 2] |= static_cast<uint32_t>(src[k0 + j * 32 + lane]) << (8 * (j & 3));
     }
   }
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    if (first + u >= p.units) break;
-    uint32_t row, at;
-    p.per_row.divmod(first + u, row, at);
-    const int k0 = static_cast<int>(at) * kF8Unit;
-    const float s0 = f8_scale(e[u] & 255u), s1 = f8_scale(e[u] >> 8);
-    const float sa = VEC && !F32 && lane >= 16 ? s1 : s0, sb = VEC && !F32 && lane < 16 ? s0 : s1;
-    float v[8];
+  for (int r = 0; r < R; ++r) {
+    const uint32_t row = row0 + r;
+    if (row >= p.rows) break;
+    const LaneAt l(row, k0, p.K, lane, F32 ? 4 : 2);
+    float* o = static_cast<float*>(out) + static_cast<int64_t>(row) * p.K + k0 + lane * 4;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const float s = h ? sb : sa;
-      const float2 a = f8_values2(word[u][h] & 0xFFFFu), b = f8_values2(word[u][h] >> 16);
-      v[4 * h] = a.x * s; v[4 * h + 1] = a.y * s; v[4 * h + 2] = b.x * s; v[4 * h + 3] = b.y * s;
-    }
-    const int64_t base = static_cast<int64_t>(row) * p.K + k0;
-    if (VEC && !F32) {
-      uint32_t w[4];
+    for (int u = 0; u < U; ++u) {
+      if (k0 + u * kF8Unit >= p.K) break;
+      const float s0 = f8_scale(e[r * U + u] & 255u), s1 = f8_scale(e[r * U + u] >> 8), mine = lane < 16 ? s0 : s1;
+      float2 v[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(__float_as_uint(v[2 * i]), __float_as_uint(v[2 * i + 1]));
-      if (k0 + lane * 8 < p.K) __stcs(reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + base + lane * 8), make_uint4(w[0], w[1], w[2], w[3]));
-    } else if (VEC) {
+      for (int i = 0; i < 4; ++i) {
+        const float s = kHalves ? (i < 2 ? s0 : s1) : mine;
+        v[i] = mul2(f8_values2(i & 1 ? word[r * U + u][i >> 1] >> 16 : word[r * U + u][i >> 1] & 0xFFFFu), make_float2(s, s));
+      }
+      if (kHalves) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-        if (k0 + h * 128 + lane * 4 < p.K)
-          __stcs(reinterpret_cast<float4*>(static_cast<float*>(out) + base + h * 128 + lane * 4),
-                 make_float4(v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]));
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (k0 + j * 32 + lane < p.K) {
-          if (F32) static_cast<float*>(out)[base + j * 32 + lane] = v[j];
-          else static_cast<uint16_t*>(out)[base + j * 32 + lane] = f32_to_bf16(v[j]);
-        }
+        for (int h = 0; h < 2; ++h)
+          if (k0 + u * kF8Unit + h * 128 + lane * 4 < p.K)
+            __stcs(reinterpret_cast<float4*>(o + u * kF8Unit + h * 128), make_float4(v[2 * h].x, v[2 * h].y, v[2 * h + 1].x, v[2 * h + 1].y));
+      } else {
+        unit_store<F32, VEC>(v, out, l, u, lane);
+      }
     }
   }
 }
 
-F8QuantParams f8_quant_params(const F8View& v) {
+// Units of a strip and rows of a warp.
+struct StripPlan { int units, rows; };
+
+F8QuantParams f8_quant_params(const F8View& v, StripPlan* plan) {
+  const int64_t units = (v.nb + 1) / 2;
+  // several units a warp only when every SM has blocks to hold
+  const bool many = v.rows * units >= static_cast<int64_t>(num_sms()) * 4 * 8 * 8;
+  plan->units = 1;
+  while (many && plan->units < 8 && plan->units < units) plan->units *= 2;
+  plan->rows = many ? 8 / plan->units : 1;
   F8QuantParams p;
   p.K = static_cast<int32_t>(v.K);
   p.pitch = static_cast<int32_t>(v.pitch);
   p.kt = static_cast<uint32_t>(v.kt);
-  const int64_t per_row = (v.nb + 1) / 2;
-  p.units = static_cast<uint32_t>(v.rows * per_row);
+  p.rows = static_cast<uint32_t>(v.rows);
+  const int64_t per_row = (units + plan->units - 1) / plan->units;
+  p.strips = static_cast<uint32_t>((v.rows + plan->rows - 1) / plan->rows * per_row);
   p.per_row.set(per_row);
   return p;
 }
 
-// Several units per warp only when every SM has blocks to hold.
-constexpr int kUnitsPerWarp = 4;
-bool many_units(const F8QuantParams& p) { return p.units >= static_cast<uint32_t>(num_sms()) * 4u * 8u * kUnitsPerWarp; }
-dim3 unit_grid(const F8QuantParams& p) {
-  const uint32_t per_block = 8u * (many_units(p) ? kUnitsPerWarp : 1);
-  return dim3((p.units + per_block - 1) / per_block);
+typedef void (*QuantizeFn)(const void*, uint8_t*, uint8_t*, F8QuantParams);
+typedef void (*DequantizeFn)(const uint8_t*, const uint8_t*, void*, F8QuantParams);
+
+template <bool F32, bool VEC>
+QuantizeFn quantize_fn(const StripPlan& s) {
+  if (s.rows == 1 && s.units == 1) return quantize_f8<F32, VEC, 1, 1>;
+  switch (s.units) {
+    case 1: return quantize_f8<F32, VEC, 1, 8>;
+    case 2: return quantize_f8<F32, VEC, 2, 4>;
+    case 4: return quantize_f8<F32, VEC, 4, 2>;
+    default: return quantize_f8<F32, VEC, 8, 1>;
+  }
+}
+template <bool F32, bool VEC>
+DequantizeFn dequantize_fn(const StripPlan& s) {
+  if (s.rows == 1 && s.units == 1) return dequantize_f8<F32, VEC, 1, 1>;
+  switch (s.units) {
+    case 1: return dequantize_f8<F32, VEC, 1, 8>;
+    case 2: return dequantize_f8<F32, VEC, 2, 4>;
+    case 4: return dequantize_f8<F32, VEC, 4, 2>;
+    default: return dequantize_f8<F32, VEC, 8, 1>;
+  }
 }
 
 int launch_quantize(const gl_ap& in, const F8View& v, void* codes, void* scale, cudaStream_t st) {
   const bool f32 = in.dtype == GL_F32, vec = v.K % 8 == 0;
-  const F8QuantParams p = f8_quant_params(v);
-  constexpr int kU = kUnitsPerWarp;
-  void (*k)(const void*, uint8_t*, uint8_t*, F8QuantParams) =
-      many_units(p) ? (f32 ? (vec ? quantize_f8<true, true, kU> : quantize_f8<true, false, kU>)
-                           : (vec ? quantize_f8<false, true, kU> : quantize_f8<false, false, kU>))
-                    : (f32 ? (vec ? quantize_f8<true, true, 1> : quantize_f8<true, false, 1>)
-                           : (vec ? quantize_f8<false, true, 1> : quantize_f8<false, false, 1>));
-  return launch_pdl(k, unit_grid(p), dim3(256), 0, st, 1, static_cast<const void*>(in.data), static_cast<uint8_t*>(codes),
+  StripPlan s;
+  const F8QuantParams p = f8_quant_params(v, &s);
+  const QuantizeFn k = f32 ? (vec ? quantize_fn<true, true>(s) : quantize_fn<true, false>(s))
+                           : (vec ? quantize_fn<false, true>(s) : quantize_fn<false, false>(s));
+  return launch_pdl(k, dim3((p.strips + 7) / 8), dim3(256), 0, st, 1, static_cast<const void*>(in.data), static_cast<uint8_t*>(codes),
                     static_cast<uint8_t*>(scale), p) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
 }
 
@@ -222,13 +251,28 @@ constexpr int kTile = 128;           // rows of A per block
 constexpr int kKBytes = 128;         // bytes of a row per K block: one block of 128 values, one 128-byte swizzle row
 constexpr int kF8Threads = 224;      // warp 0 TMA (A), warp 1 MMA, warps 2-5 epilogue, warp 6 TMA (B)
 
+// Tile rows of a band, in 256s.  What a band of pairs reads at a time is its rows of A and a few columns of B: 16 rows by 4 or 5
+// columns for 74 pairs.  Walked row by row, the whole of B passes for every two rows of tiles, and what does not come from near
+// L2 costs power, which is what bounds a long run: 16384 x 8192 x 8192 sustained 930 us with one row, 870 with four, 855 with
+// eight, 840 with sixteen, 865 with 24, 930 with 32, 1030 with 64; 8192^3 468, 436, 425, 412, 433 (24), 466 (32).
+constexpr int kBandRows = 16;
+
 struct F8Params {
   int64_t M, O;
   int tiles_m, tiles_n;   // tiles_m counts 128 * CTAS rows
   int kblocks;            // K blocks of 128 values
   int last_steps;         // instructions (32 values) in the last K block
   int relu, out_bf16, tma_store;
-  FastDiv div_tiles_n;
+  int group;              // tiles are walked in bands of `group` tile rows, column by column inside a band
+  FastDiv div_band, div_group, div_last;   // tiles of a band; tile rows of a band, of the last band
+  // Place of tile u.
+  __device__ __forceinline__ void tile_at(int u, uint32_t& tm, uint32_t& tn) const {
+    uint32_t band, in_band, row;
+    div_band.divmod(static_cast<uint32_t>(u), band, in_band);
+    const bool last = static_cast<int>(band + 1) * group > tiles_m;
+    (last ? div_last : div_group).divmod(in_band, tn, row);
+    tm = band * group + row;
+  }
 };
 
 template <int BN, int CTAS>
@@ -313,7 +357,7 @@ dot_f8(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtens
     bool ok = true;
     for (int u = unit0; u < num_tiles && ok; u += unit_step) {
       uint32_t tm, tn;
-      p.div_tiles_n.divmod(static_cast<uint32_t>(u), tm, tn);
+      p.tile_at(u, tm, tn);
       const int m0 = (static_cast<int>(tm) * CTAS + static_cast<int>(rank)) * kTile;
       const int n0 = static_cast<int>(tn) * BN + static_cast<int>(rank) * (BN / CTAS);
       for (int kb = 0; kb < p.kblocks; ++kb) {
@@ -414,7 +458,7 @@ dot_f8(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtens
     for (int u = unit0; u < num_tiles && ok; u += unit_step, ++tile_it) {
       const uint32_t acc = tile_it & 1u, aph = (tile_it >> 1) & 1u;
       uint32_t tmu, tn;
-      p.div_tiles_n.divmod(static_cast<uint32_t>(u), tmu, tn);
+      p.tile_at(u, tmu, tn);
       const int tm = static_cast<int>(tmu) * CTAS + static_cast<int>(rank);
       if (!mbar_wait(bar_tfull + 8 * acc, aph, abort_flag)) { ok = false; break; }
       tc_fence_after();
@@ -474,25 +518,36 @@ dot_f8(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtens
             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
           }
         } else {
-          // rows that are no multiples of 16 bytes: row by row, neighbouring lanes on neighbouring columns
+          // rows that are no multiples of 16 bytes: row by row, neighbouring lanes on neighbouring columns, eight rows read
+          // from shared memory before the first is stored
           __syncwarp();
           const int rows = static_cast<int>(min(static_cast<int64_t>(32), p.M - m0));
-          const int cols = static_cast<int>(min(static_cast<int64_t>(cstep), p.O - n0));
-          const int64_t base = m0 * p.O + n0;
-#pragma unroll 8
-          for (int row = 0; row < rows; ++row) {
-            uint32_t v;
-            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(buf + row * 128 + (((lane >> 2) ^ (row & 7)) << 4) + (lane & 3) * 4));
+          const int cols = static_cast<int>(min(static_cast<int64_t>(cstep), p.O - n0)), col = p.out_bf16 ? 2 * lane : lane;
+          const bool one = col < cols, two = col + 1 < cols;
+          const int64_t first = m0 * p.O + n0 + col;
+          for (int row0 = 0; row0 < rows; row0 += 8) {
+            uint32_t v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v[i]) : "r"(buf + (row0 + i) * 128 + (((lane >> 2) ^ i) << 4) + (lane & 3) * 4));
             if (p.out_bf16) {
-              uint16_t* to = static_cast<uint16_t*>(out) + base + row * p.O + 2 * lane;
+              uint16_t* to = static_cast<uint16_t*>(out) + first + row0 * p.O;
               if ((p.O & 1) == 0) {
-                if (2 * lane < cols) *reinterpret_cast<uint32_t*>(to) = v;   // (O even: whole pairs)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                  if (one && row0 + i < rows) *reinterpret_cast<uint32_t*>(to + i * p.O) = v[i];   // (O even: whole pairs)
               } else {
-                if (2 * lane < cols) to[0] = static_cast<uint16_t>(v);
-                if (2 * lane + 1 < cols) to[1] = static_cast<uint16_t>(v >> 16);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                  if (one && row0 + i < rows) to[i * p.O] = static_cast<uint16_t>(v[i]);
+                  if (two && row0 + i < rows) to[i * p.O + 1] = static_cast<uint16_t>(v[i] >> 16);
+                }
               }
-            } else if (lane < cols) {
-              static_cast<float*>(out)[base + row * p.O + lane] = __uint_as_float(v);
+            } else {
+              float* to = static_cast<float*>(out) + first + row0 * p.O;
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+                if (one && row0 + i < rows) to[i * p.O] = __uint_as_float(v[i]);
             }
           }
         }
@@ -529,6 +584,11 @@ dot_f8(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtens
 // At most kFuseRows rows (FUSED): the blocks round A themselves, each its own stretch of K, straight into operand order, while
 // the first weights are on their way: one launch.
 constexpr int kFuseRows = 4;
+// K blocks that a block asks for before the kernel in front has ended.  More stand in the way of the rows of A behind them, and of
+// weights that are wanted sooner: one row, weights not in L2, 8192 x 8192: none 14.2 us, two 13.6, four 13.5, all sixteen 14.1;
+// 8192 x 28672: none to eight 37.5, all 53.8; 128 rows through 8192 x 8192: none 19.6, four 19.0, all 20.3.
+constexpr int kPrefetch = 4;
+constexpr int kJoinWarps = kF8Threads / 32;
 constexpr int kFuseBlocks = 16;   // K blocks of A that a block has room for
 
 struct F8FewParams {
@@ -542,28 +602,56 @@ struct F8FewParams {
   int relu, out_bf16;
 };
 
-// Rank r adds up the columns r, r + S, ...: the S partial sums of a value in rank order, those of four columns requested
-// before the first is added.
+// The S partial sums of a value in rank order.  A warp takes a column of 128 outputs, four a lane; rank r has the columns r, r + S, ..,
+// several of a warp's requested before the first is summed.
 template <int S>
-__device__ __forceinline__ void join_ranks(uint32_t mine, int rank, int64_t o, void* __restrict__ out, const F8FewParams& p) {
-  for (int c0 = rank; c0 < p.M; c0 += 4 * S) {
-    float x[4][S];
+__device__ __forceinline__ void join_ranks(uint32_t part, int rank, int warp, int lane, int64_t o0, void* __restrict__ out, const F8FewParams& p) {
+  constexpr int kCols = 8 / S < 1 ? 1 : 8 / S;   // columns of a warp in flight
+  const int64_t o = o0 + lane * 4;
+  for (int c0 = rank + warp * S; c0 < p.M; c0 += kCols * kJoinWarps * S) {
+    float4 x[kCols][S];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < kCols; ++j)
 #pragma unroll
-      for (int from = 0; from < S; ++from)   // (columns past M are inside the partial sums' space only up to BN)
-        if (c0 + j * S < p.M)
-          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x[j][from]) : "r"(map_to_cta(mine + (c0 + j * S) * 512, from)));
+      for (int from = 0; from < S; ++from) {
+        const int c = c0 + j * kJoinWarps * S;
+        if (c < p.M)
+          asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                       : "=f"(x[j][from].x), "=f"(x[j][from].y), "=f"(x[j][from].z), "=f"(x[j][from].w)
+                       : "r"(map_to_cta(part + c * 512 + lane * 16, from)));
+      }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int c = c0 + j * S;
+    for (int j = 0; j < kCols; ++j) {
+      const int64_t c = c0 + j * kJoinWarps * S;
       if (c >= p.M) break;
-      float v = x[j][0];
+      float v[4] = {x[j][0].x, x[j][0].y, x[j][0].z, x[j][0].w};
 #pragma unroll
-      for (int from = 1; from < S; ++from) v += x[j][from];
-      if (p.relu) v = relu_keep_nan(v);
-      if (p.out_bf16) static_cast<uint16_t*>(out)[c * p.O + o] = f32_to_bf16(v);
-      else static_cast<float*>(out)[c * p.O + o] = v;
+      for (int from = 1; from < S; ++from) { v[0] += x[j][from].x; v[1] += x[j][from].y; v[2] += x[j][from].z; v[3] += x[j][from].w; }
+      if (p.relu) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = relu_keep_nan(v[i]);
+      }
+      if (p.out_bf16) {
+        uint16_t* to = static_cast<uint16_t*>(out) + c * p.O + o;
+        const uint32_t lo = pack_bf16x2(__float_as_uint(v[0]), __float_as_uint(v[1])), hi = pack_bf16x2(__float_as_uint(v[2]), __float_as_uint(v[3]));
+        if ((p.O & 3) == 0) {
+          if (o < p.O) *reinterpret_cast<uint2*>(to) = make_uint2(lo, hi);
+        } else {
+          if (o < p.O) to[0] = static_cast<uint16_t>(lo);
+          if (o + 1 < p.O) to[1] = static_cast<uint16_t>(lo >> 16);
+          if (o + 2 < p.O) to[2] = static_cast<uint16_t>(hi);
+          if (o + 3 < p.O) to[3] = static_cast<uint16_t>(hi >> 16);
+        }
+      } else {
+        float* to = static_cast<float*>(out) + c * p.O + o;
+        if ((p.O & 3) == 0) {
+          if (o < p.O) *reinterpret_cast<float4*>(to) = make_float4(v[0], v[1], v[2], v[3]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (o + i < p.O) to[i] = v[i];
+        }
+      }
     }
   }
 }
@@ -584,34 +672,50 @@ struct F8FewCfg {
   static_assert(FUSED ? BN == 16 : true, "the blocks that round A keep it as 16 rows");
 };
 
-// One warp rounds K block kb of row m: lane = 4 values, into the swizzled operand row and the scale tiles.
-__device__ __forceinline__ void round_row_block(const F8FewParams& p, unsigned char* rows, unsigned char* scale, int m, int kb, int lane) {
-  const int64_t k0 = static_cast<int64_t>(kb) * kF8Block + lane * 4, left = p.K - k0, at = static_cast<int64_t>(m) * p.K + k0;
-  float x[4];
-  if (left >= 4 && (p.K & 3) == 0) {
+// Sixteen values of a row of A from element k on, zeros behind its end.
+__device__ __forceinline__ void load_row_values(const F8FewParams& p, int m, int64_t k, float (&x)[16]) {
+  const int64_t at = static_cast<int64_t>(m) * p.K + k, left = p.K - k;
+  if (left >= 16 && (p.K & 7) == 0) {
     if (p.x_f32) {
-      const float4 a = *reinterpret_cast<const float4*>(static_cast<const float*>(p.x) + at);
-      x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float4 a = *(reinterpret_cast<const float4*>(static_cast<const float*>(p.x) + at) + i);
+        x[4 * i] = a.x; x[4 * i + 1] = a.y; x[4 * i + 2] = a.z; x[4 * i + 3] = a.w;
+      }
     } else {
-      const uint2 a = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p.x) + at);
-      x[0] = __uint_as_float(a.x << 16); x[1] = __uint_as_float(a.x & 0xFFFF0000u);
-      x[2] = __uint_as_float(a.y << 16); x[3] = __uint_as_float(a.y & 0xFFFF0000u);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint4 a = *(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.x) + at) + i);
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          x[8 * i + 2 * j] = __uint_as_float(w[j] << 16);
+          x[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+        }
+      }
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 16; ++i)
       x[i] = i < left ? (p.x_f32 ? static_cast<const float*>(p.x)[at + i] : bf16_to_f32(static_cast<const uint16_t*>(p.x)[at + i])) : 0.f;
   }
-  uint32_t top = 0;
+}
+
+// Eight lanes round a K block of row m, sixteen values each, into the swizzled operand row and the scale tiles.
+__device__ __forceinline__ void round_row_block(const float (&x)[16], unsigned char* rows, unsigned char* scale, int m, int lane8, bool live) {
+  float top = 0.f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+  for (int i = 0; i < 16; ++i) top = top_of(top, x[i]);
 #pragma unroll
-  for (int d = 1; d < 32; d *= 2) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-  const uint32_t e = f8_exponent(top);
+  for (int d = 1; d < 8; d *= 2) top = top_of(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+  if (!live) return;
+  const uint32_t e = f8_exponent(__float_as_uint(top) & 0x7FFFFFFFu);
   const float f = f8_inverse(e);
-  const uint32_t word = e == 255u ? 0u : f8_codes4(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
-  *reinterpret_cast<uint32_t*>(rows + m * 128 + (((lane >> 2) ^ (m & 7)) << 4) + (lane & 3) * 4) = word;
-  if (lane == 0) scale[m * 16 + (kb & 3)] = static_cast<uint8_t>(e);
+  uint32_t word[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) word[i] = e == 255u ? 0u : f8_codes4(x[4 * i] * f, x[4 * i + 1] * f, x[4 * i + 2] * f, x[4 * i + 3] * f);
+  *reinterpret_cast<uint4*>(rows + m * 128 + ((lane8 ^ (m & 7)) << 4)) = make_uint4(word[0], word[1], word[2], word[3]);
+  if (lane8 == 0) *scale = static_cast<uint8_t>(e);
 }
 
 template <int BN, bool FUSED>
@@ -640,7 +744,7 @@ dot_f8_few(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
   const int kb1 = static_cast<int>(static_cast<int64_t>(p.kblocks) * (rank + 1) / p.split);
 
   if (warp == 0 && elect_one())
-    for (int kb = kb0; kb < kb1; ++kb) tma_prefetch_2d(&map_w, kb * kKBytes, tile * kTile);
+    for (int kb = kb0; kb < min(kb1, kb0 + kPrefetch); ++kb) tma_prefetch_2d(&map_w, kb * kKBytes, tile * kTile);
   if (threadIdx.x == 0) {
     for (int s = 0; s < Cfg::kStages; ++s) { mbar_init(bar_full + 8 * s, FUSED ? 1 : 2); mbar_init(bar_empty + 8 * s, 1); }
     mbar_init(bar_done, 1);
@@ -662,11 +766,18 @@ dot_f8_few(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
   pdl_launch_dependents();
 
   if (FUSED && warp >= 2) {
-    const int blocks = kb1 - kb0;   // rows one after the other, their K blocks side by side
+    // a warp takes four K blocks of a row at a time, eight lanes each
+    const int quads = (kb1 - kb0 + 3) / 4;
     unsigned char* xscale = gen_x + kFuseBlocks * BN * kKBytes;
-    for (int i = warp - 2; i < p.M * blocks; i += 5) {
-      const int b = i % blocks, kb = kb0 + b;
-      round_row_block(p, gen_x + b * (BN * kKBytes), xscale + ((kb >> 2) - (kb0 >> 2)) * 512, i / blocks, kb, lane);
+    int m = 0, g = warp - 2;
+    while (true) {
+      while (g >= quads) { g -= quads; ++m; }
+      if (m >= p.M) break;
+      const int b = g * 4 + (lane >> 3), kb = kb0 + b;
+      float x[16];
+      load_row_values(p, m, static_cast<int64_t>(kb) * kF8Block + (lane & 7) * 16, x);
+      round_row_block(x, gen_x + b * (BN * kKBytes), xscale + ((kb >> 2) - (kb0 >> 2)) * 512 + m * 16 + (kb & 3), m, lane & 7, kb < kb1);
+      g += 5;
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
@@ -754,13 +865,11 @@ dot_f8_few(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
   if (p.split > 1) {
     __syncwarp();
     cluster_sync_all();
-    if (epilogue && o < p.O) {
-      const uint32_t mine = smem_u32(part) + (q * 32 + lane) * 4;
-      switch (p.split) {
-        case 2: join_ranks<2>(mine, rank, o, out, p); break;
-        case 4: join_ranks<4>(mine, rank, o, out, p); break;
-        default: join_ranks<8>(mine, rank, o, out, p); break;
-      }
+    const int64_t o0 = static_cast<int64_t>(tile) * kTile;
+    switch (p.split) {
+      case 2: join_ranks<2>(smem_u32(part), rank, warp, lane, o0, out, p); break;
+      case 4: join_ranks<4>(smem_u32(part), rank, warp, lane, o0, out, p); break;
+      default: join_ranks<8>(smem_u32(part), rank, warp, lane, o0, out, p); break;
     }
   }
   __syncwarp();
@@ -868,7 +977,11 @@ int plan_tiles(const F8Operand& a, const F8Operand& b, void* out, uint32_t flags
   p.relu = (flags & GL_EPILOGUE_RELU) ? 1 : 0;
   p.out_bf16 = (flags & GL_OUT_BF16) ? 1 : 0;
   p.tma_store = p.O % (p.out_bf16 ? 8 : 4) == 0 ? 1 : 0;
-  p.div_tiles_n.set(p.tiles_n);
+  p.group = kBandRows;
+  if (p.group > p.tiles_m) p.group = p.tiles_m;
+  p.div_band.set(static_cast<int64_t>(p.group) * p.tiles_n);
+  p.div_group.set(p.group);
+  p.div_last.set(p.tiles_m % p.group ? p.tiles_m % p.group : p.group);
   t->out = out;
   t->grid = CTAS * std::min(at_once, p.tiles_m * p.tiles_n);
   if (!encode_codes(&t->ma, a, kTile) || !encode_codes(&t->mb, b, BN / CTAS) || !encode_scales(&t->msa, a) ||
@@ -1035,16 +1148,14 @@ int gl_f8_dequantize(const gl_f8* in, gl_ap* out, void* stream) {
   rc = check_data(out);
   if (rc) return rc;
   if (!f8_same_shape(out, in)) return GL_ERR_SHAPE;
-  const F8QuantParams p = f8_quant_params(v);
+  StripPlan s;
+  const F8QuantParams p = f8_quant_params(v, &s);
   const bool f32 = out->dtype == GL_F32, vec = v.K % 8 == 0;
-  constexpr int kU = kUnitsPerWarp;
-  void (*k)(const uint8_t*, const uint8_t*, void*, F8QuantParams) =
-      many_units(p) ? (f32 ? (vec ? dequantize_f8<true, true, kU> : dequantize_f8<true, false, kU>)
-                           : (vec ? dequantize_f8<false, true, kU> : dequantize_f8<false, false, kU>))
-                    : (f32 ? (vec ? dequantize_f8<true, true, 1> : dequantize_f8<true, false, 1>)
-                           : (vec ? dequantize_f8<false, true, 1> : dequantize_f8<false, false, 1>));
-  return launch_pdl(k, unit_grid(p), dim3(256), 0, static_cast<cudaStream_t>(stream), 1, static_cast<const uint8_t*>(in->data),
-                    static_cast<const uint8_t*>(in->scale), out->data, p) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
+  const DequantizeFn k = f32 ? (vec ? dequantize_fn<true, true>(s) : dequantize_fn<true, false>(s))
+                             : (vec ? dequantize_fn<false, true>(s) : dequantize_fn<false, false>(s));
+  return launch_pdl(k, dim3((p.strips + 7) / 8), dim3(256), 0, static_cast<cudaStream_t>(stream), 1,
+                    static_cast<const uint8_t*>(in->data), static_cast<const uint8_t*>(in->scale), out->data, p) == cudaSuccess
+             ? GL_OK : GL_ERR_CUDA;
 }
 
 int gl_cartesian_dot_f8(const gl_f8* a0, const gl_f8* a1, gl_ap* out, uint32_t flags, void* stream) {

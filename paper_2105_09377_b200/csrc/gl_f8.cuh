@@ -1,10 +1,10 @@
 // The 8-bit number format, shared by the kernel files: blocks of 128 consecutive values of an item, E4M3 codes (magnitudes up to
 // 448) and an E8M0 scale 2^(e - 127) per block; e = 255 stands for NaN.
 //
-// A warp works on units of 256 values, two blocks, eight values a lane:
-//   aligned rows (VEC): lane l holds values 8l .. 8l+7, one or two 16-byte loads, lanes 0-15 the first block;
-//   other rows:         lane l holds values 32j + l, j = 0..7, j < 4 the first block, so that loads and stores of neighbouring
-//                       lanes still fall next to each other.
+// A warp works on units of 256 values, two blocks: lane l holds values 8l .. 8l+7, lanes 0-15 the first block.  Where the rows of a
+// pattern are multiples of 16 bytes (VEC) these are 16-byte accesses as they stand.  Other rows start anywhere: the same 16-byte
+// accesses are made at the boundaries before, and the values shifted into place, by the same distance in all lanes.  Codes
+// always start at a boundary.
 // Scales are stored in tiles of 128 rows x 4 blocks (512 bytes), row r and block b of a tile at byte
 // (r % 32) * 16 + (r / 32) * 4 + b: what one tcgen05.cp (32x128b, replicated to the four lane quarters) has to find.
 #pragma once
@@ -14,6 +14,7 @@
 #include <cstring>
 
 #include "gl_internal.h"
+#include "gl_tc.cuh"
 
 namespace {
 
@@ -84,87 +85,217 @@ __device__ __forceinline__ uint32_t f8_codes2(float lo, float hi) {
 }
 __device__ __forceinline__ uint32_t f8_codes4(float a, float b, float c, float d) { return f8_codes2(a, b) | f8_codes2(c, d) << 16; }
 
+// Two fp32 operations an instruction.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t&>(d)) : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
+  return d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(reinterpret_cast<uint64_t&>(d))
+      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)), "l"(reinterpret_cast<uint64_t&>(c)));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t&>(d)) : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
+  return d;
+}
+__device__ __forceinline__ float2 sub2(float2 a, float2 b) {
+  float2 d;
+  asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t&>(d)) : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
+  return d;
+}
+// The larger magnitude; a NaN wins.
+__device__ __forceinline__ float top_of(float a, float b) {
+  float d;
+  asm("{\n\t.reg .f32 x, y;\n\tabs.f32 x, %1;\n\tabs.f32 y, %2;\n\tmax.NaN.f32 %0, x, y;\n\t}" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+
 // Byte of the scale tiles that holds block b of row r.
 __device__ __forceinline__ int64_t f8_scale_at(uint32_t r, uint32_t b, uint32_t kt) {
   return (static_cast<int64_t>(r >> 7) * kt + (b >> 2)) * 512 + ((r & 31u) * 16 + ((r >> 5) & 3u) * 4 + (b & 3u));
 }
 
-// Place of a lane's value j inside a unit.
-template <bool VEC>
-__device__ __forceinline__ int unit_at(int lane, int j) { return VEC ? lane * 8 + j : j * 32 + lane; }
+// ---- units of patterns whose items are `K` values, in memory at `base` (16-byte aligned) ----
 
-// Eight values of the row that starts at `row` (element `k0` is the unit's first), zeros behind K.
+// Words i .. of `w` from byte `t` on (t < 16, even; a multiple of 4 for fp32).
+template <int N, int OUT>
+__device__ __forceinline__ void shift_words(uint32_t (&w)[N], int t, uint32_t (&out)[OUT]) {
+#pragma unroll
+  for (int i = 0; i + 2 < N; ++i) w[i] = (t & 8) ? w[i + 2] : w[i];
+#pragma unroll
+  for (int i = 0; i + 3 < N; ++i) w[i] = (t & 4) ? w[i + 1] : w[i];
+#pragma unroll
+  for (int i = 0; i < OUT; ++i) out[i] = i + 1 < N ? __funnelshift_r(w[i], w[i + 1], (t & 2) * 8) : w[i];
+}
+
+// 16 bytes at a boundary of a pattern of `total` bytes; what lies behind its end is not read.
+__device__ __forceinline__ uint4 load_chunk(const char* base, int64_t at, int64_t total) {
+  if (at + 16 <= total) return *reinterpret_cast<const uint4*>(base + at);
+  uint64_t lo = 0, hi = 0;   // (one lane of the whole grid: small rather than fast)
+#pragma unroll 1
+  for (int left = static_cast<int>(total - at) - 2; left >= 0; left -= 2) {
+    hi = hi << 16 | lo >> 48;
+    lo = lo << 16 | *reinterpret_cast<const uint16_t*>(base + at + left);
+  }
+  return make_uint4(static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32), static_cast<uint32_t>(hi), static_cast<uint32_t>(hi >> 32));
+}
+
+// A lane's place in a pattern whose items are `K` values: its values of unit c are the eight from byte at + c * 256 values on.
+struct LaneAt {
+  int64_t at;     // of the lane's first value in the strip's first unit
+  int left;       // values of the row from there on
+  int strip;      // values of the row from the strip's beginning on (the same for all lanes)
+  __device__ __forceinline__ LaneAt(uint32_t row, int k0, int K, int lane, int value_bytes)
+      : at((static_cast<int64_t>(row) * K + k0 + lane * 8) * value_bytes), left(K - k0 - lane * 8), strip(K - k0) {}
+};
+
+// A lane's eight values of unit c, zeros behind the row's end: four words of bf16 pairs, or eight of floats.  `total`: bytes of
+// the pattern.
 template <bool F32, bool VEC>
-__device__ __forceinline__ void unit_load(const void* __restrict__ row, int k0, int K, int lane, uint32_t (&raw)[8]) {
+__device__ __forceinline__ void unit_load(const void* base, const LaneAt& l, int c, int64_t total, uint32_t (&raw)[8]) {
+  constexpr int kEs = F32 ? 4 : 2, kWords = F32 ? 8 : 4;
 #pragma unroll
   for (int j = 0; j < 8; ++j) raw[j] = 0;
-  if (VEC) {   // K is a multiple of 8: a lane's values lie wholly inside the row or wholly behind it
-    const int at = k0 + lane * 8;
-    if (at < K) {
-      const uint4* src = reinterpret_cast<const uint4*>(static_cast<const char*>(row) + static_cast<int64_t>(at) * (F32 ? 4 : 2));
+  const int left = l.left - c * kF8Unit;
+  if (left <= 0) return;
+  const char* p = static_cast<const char*>(base);
+  if (VEC) {   // rows are multiples of eight values: a lane's lie wholly inside or wholly behind
 #pragma unroll
-      for (int i = 0; i < (F32 ? 2 : 1); ++i) {
-        const uint4 x = __ldcs(src + i);
-        raw[4 * i] = x.x; raw[4 * i + 1] = x.y; raw[4 * i + 2] = x.z; raw[4 * i + 3] = x.w;
-      }
+    for (int i = 0; i < kWords / 4; ++i) {
+      const uint4 x = __ldcs(reinterpret_cast<const uint4*>(p + l.at + c * kF8Unit * kEs) + i);
+      raw[4 * i] = x.x; raw[4 * i + 1] = x.y; raw[4 * i + 2] = x.z; raw[4 * i + 3] = x.w;
     }
   } else {
+    // (the last chunk is the next lane's first: it comes from L1)
+    const int t = static_cast<int>(l.at & 15), n = min(8, left), bytes = t + n * kEs;
+    const int64_t first = l.at - t + c * kF8Unit * kEs;
+    uint32_t w[kWords + 4], x[kWords];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int at = k0 + j * 32 + lane;
-      if (at < K) raw[j] = F32 ? static_cast<const uint32_t*>(row)[at] : static_cast<const uint16_t*>(row)[at];
+    for (int i = 0; i < kWords / 4 + 1; ++i) {
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (16 * i < bytes) v = load_chunk(p, first + 16 * i, total);
+      w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+    }
+    shift_words(w, t, x);
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      if (F32) raw[i] = i < n ? x[i] : 0u;
+      else raw[i] = 2 * i + 1 < n ? x[i] : 2 * i < n ? x[i] & 0xFFFFu : 0u;
     }
   }
 }
-// What unit_load brought, as fp32.
-template <bool F32, bool VEC>
-__device__ __forceinline__ float unit_value(const uint32_t (&raw)[8], int j) {
-  if (F32) return __uint_as_float(raw[j]);
-  if (VEC) return __uint_as_float(j & 1 ? raw[j >> 1] & 0xFFFF0000u : raw[j >> 1] << 16);
-  return __uint_as_float(raw[j] << 16);
+// Values 2i and 2i + 1 of what unit_load brought, as fp32.
+template <bool F32>
+__device__ __forceinline__ float2 unit_values(const uint32_t (&raw)[8], int i) {
+  return F32 ? make_float2(__uint_as_float(raw[2 * i & 7]), __uint_as_float(raw[2 * i + 1 & 7]))
+             : make_float2(__uint_as_float(raw[i] << 16), __uint_as_float(raw[i] & 0xFFFF0000u));
 }
 
-// A unit's eight values per lane to codes and scales.  `codes`: the row of codes, `scale`: the scale byte of the unit's first
-// block (even, so that both bytes are one aligned store; a second block behind the row's end has room in the tile).
-// Every lane of the warp takes part.
-template <bool VEC>
-__device__ __forceinline__ void unit_store_f8(const float (&v)[8], uint8_t* __restrict__ codes, int k0, int pitch, int lane,
-                                              uint8_t* __restrict__ scale) {
-  uint32_t top[2] = {0, 0};
+// Eight values per lane to unit c.  Every lane of the warp takes part, whether or not it has values.
+template <bool F32, bool VEC>
+__device__ __forceinline__ void unit_store(const float2 (&v)[4], void* base, const LaneAt& l, int c, int lane) {
+  constexpr int kEs = F32 ? 4 : 2;
+  char* p = static_cast<char*>(base) + l.at + c * kF8Unit * kEs;
+  const int left = l.left - c * kF8Unit;
+  uint32_t w[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    uint32_t& t = top[!VEC && j >= 4];
-    t = max(t, __float_as_uint(v[j]) & 0x7FFFFFFFu);
+  for (int i = 0; i < 4; ++i) {
+    if (F32) { w[2 * i] = __float_as_uint(v[i].x); w[2 * i + 1] = __float_as_uint(v[i].y); }
+    else { w[i] = pack_bf16x2(__float_as_uint(v[i].x), __float_as_uint(v[i].y)); w[4 + i] = 0; }
   }
+  if (VEC && F32) {
+    // two lanes' 64 bytes in two stores that each write whole 32-byte sectors: first the even lane's values, then the odd's
+    const bool odd = lane & 1;
+    uint32_t got[4];
 #pragma unroll
-  for (int d = 1; d < (VEC ? 16 : 32); d *= 2) {
-    top[0] = max(top[0], __shfl_xor_sync(0xFFFFFFFFu, top[0], d));
-    if (!VEC) top[1] = max(top[1], __shfl_xor_sync(0xFFFFFFFFu, top[1], d));
-  }
-  const uint32_t e0 = f8_exponent(top[0]);
-  if (VEC) {
-    const float f = f8_inverse(e0);
-    const int at = k0 + lane * 8;
-    if (at < pitch)   // (the pitch is a multiple of 16; values behind K are zeros)
-      *reinterpret_cast<uint2*>(codes + at) =
-          make_uint2(e0 == 255u ? 0u : f8_codes4(v[0] * f, v[1] * f, v[2] * f, v[3] * f),
-                     e0 == 255u ? 0u : f8_codes4(v[4] * f, v[5] * f, v[6] * f, v[7] * f));
-    const uint32_t e1 = __shfl_sync(0xFFFFFFFFu, e0, 16);
-    if (lane == 0) *reinterpret_cast<uint16_t*>(scale) = static_cast<uint16_t>(e0 | e1 << 8);
-  } else {
-    const uint32_t e1 = f8_exponent(top[1]);
-    const float f0 = f8_inverse(e0), f1 = f8_inverse(e1);
+    for (int i = 0; i < 4; ++i) got[i] = __shfl_xor_sync(0xFFFFFFFFu, odd ? w[i] : w[4 + i], 1);
+    const int pair = left + (odd ? 8 : 0);   // values from the even lane's first on
+    uint4* o = reinterpret_cast<uint4*>(p - (odd ? 16 : 0));
+    if (pair > 0) *o = odd ? make_uint4(got[0], got[1], got[2], got[3]) : make_uint4(w[0], w[1], w[2], w[3]);
+    if (pair > 8) o[2] = odd ? make_uint4(w[4], w[5], w[6], w[7]) : make_uint4(got[0], got[1], got[2], got[3]);
+  } else if (VEC) {
+    if (left > 0) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  } else if (l.strip - c * kF8Unit < kF8Unit) {
+    // the row's last, partial unit
 #pragma unroll
-    for (int j = 0; j < 8; j += 2) {
-      const bool nan = (j < 4 ? e0 : e1) == 255u;
-      const float f = j < 4 ? f0 : f1;
-      const uint32_t two = nan ? 0u : f8_codes2(v[j] * f, v[j + 1] * f);
-      const int at = k0 + j * 32 + lane;
-      if (at < pitch) codes[at] = static_cast<uint8_t>(two);
-      if (at + 32 < pitch) codes[at + 32] = static_cast<uint8_t>(two >> 8);
+    for (int j = 0; j < 8; ++j)
+      if (j < left) {
+        if (F32) *reinterpret_cast<uint32_t*>(p + 4 * j) = w[j];
+        else *reinterpret_cast<uint16_t*>(p + 2 * j) = static_cast<uint16_t>(w[j >> 1 & 3] >> (16 * (j & 1)));
+      }
+  } else if (F32) {
+    // Whole 16-byte pieces between the boundaries: the lane before has the first one's beginning.  The unit's own first and last
+    // bytes, whose pieces belong to other units too, go one word at a time.
+    const int t = static_cast<int>(-l.at & 15), s = t >> 2;   // bytes, words to the first boundary
+    uint32_t z[12], q[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) z[i] = __shfl_up_sync(0xFFFFFFFFu, w[4 + i], 1);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z[4 + i] = w[i];
+    if (s == 0) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) reinterpret_cast<uint4*>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+      return;
     }
-    if (lane == 0) *reinterpret_cast<uint16_t*>(scale) = static_cast<uint16_t>(e0 | e1 << 8);
+    shift_words(z, t, q);
+    uint4* o = reinterpret_cast<uint4*>(p + t - 16);
+    if (lane > 0) o[0] = make_uint4(q[0], q[1], q[2], q[3]);
+    o[1] = make_uint4(q[4], q[5], q[6], q[7]);
+    uint32_t* words = reinterpret_cast<uint32_t*>(p);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      if (lane == 0 && i < s) words[i] = w[i];
+      if (lane == 31 && 7 - i >= 4 + s) words[7 - i] = w[7 - i];
+    }
+  } else {
+    const int t = static_cast<int>(-l.at & 15);
+    uint32_t z[8], q[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { z[i] = __shfl_up_sync(0xFFFFFFFFu, w[i], 1); z[4 + i] = w[i]; }
+    if (t == 0) {
+      *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+      return;
+    }
+    shift_words(z, t, q);
+    if (lane > 0) *reinterpret_cast<uint4*>(p + t - 16) = make_uint4(q[0], q[1], q[2], q[3]);
+    // values before the first boundary (lane 0) and from it on (lane 31), two at a time where they share a word
+    const bool mine = lane == 0 || lane == 31;
+    if (t & 2) {
+      if (lane == 0) *reinterpret_cast<uint16_t*>(p) = static_cast<uint16_t>(w[0]);
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+        if (mine && (2 + 4 * i < t) == (lane == 0)) *reinterpret_cast<uint32_t*>(p + 2 + 4 * i) = __funnelshift_r(w[i], w[i + 1], 16);
+      if (lane == 31) *reinterpret_cast<uint16_t*>(p + 14) = static_cast<uint16_t>(w[3] >> 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (mine && (4 * i < t) == (lane == 0)) *reinterpret_cast<uint32_t*>(p + 4 * i) = w[i];
+    }
   }
+}
+
+// Unit c's eight values per lane to codes and scales.  `codes`: the lane's first code in the strip's first unit, `room`: bytes of
+// the row of codes from there on, `scale`: the scale byte of the strip's first block.  A unit's two scales are one aligned store; a
+// second block behind the row's end has room in the tile.  A strip of several units begins with an even one, so that its units
+// lie in the scale tiles at fixed distances.  Every lane of the warp takes part.
+__device__ __forceinline__ void unit_store_f8(const float2 (&v)[4], uint8_t* codes, int room, uint8_t* scale, int c, int lane) {
+  float largest = top_of(top_of(top_of(v[0].x, v[0].y), top_of(v[1].x, v[1].y)), top_of(top_of(v[2].x, v[2].y), top_of(v[3].x, v[3].y)));
+#pragma unroll
+  for (int d = 1; d < 16; d *= 2) largest = top_of(largest, __shfl_xor_sync(0xFFFFFFFFu, largest, d));
+  const uint32_t e = f8_exponent(__float_as_uint(largest) & 0x7FFFFFFFu);
+  const float f = f8_inverse(e);
+  float2 q[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) q[i] = mul2(v[i], make_float2(f, f));
+  if (room > c * kF8Unit)   // (the pitch is a multiple of 16; values behind K are zeros)
+    *reinterpret_cast<uint2*>(codes + c * kF8Unit) = make_uint2(e == 255u ? 0u : f8_codes4(q[0].x, q[0].y, q[1].x, q[1].y),
+                                                                e == 255u ? 0u : f8_codes4(q[2].x, q[2].y, q[3].x, q[3].y));
+  const uint32_t second = __shfl_sync(0xFFFFFFFFu, e, 16);
+  if (lane == 0) *reinterpret_cast<uint16_t*>(scale + (c >> 1) * 512 + (c & 1) * 2) = static_cast<uint16_t>(e | second << 8);
 }
 
 }  // namespace

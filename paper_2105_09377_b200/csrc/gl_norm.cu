@@ -35,86 +35,77 @@ struct NormParams {
   float eps, inv_k;
 };
 
-template <bool VEC>
-__device__ __forceinline__ void load_weights(const NormParams& p, int k0, int lane, float (&w)[8]) {
+// Weights of unit c, eight a lane (one row: always at a boundary, the last ones alone).
+__device__ __forceinline__ void load_weights(const NormParams& p, int k, int c, float2 (&w)[4]) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) w[j] = 1.f;
-  if (p.weight_type == kNone) return;
-  if (VEC) {
-    const int at = k0 + lane * 8;
-    if (at >= p.K) return;
+  for (int i = 0; i < 4; ++i) w[i] = make_float2(1.f, 1.f);
+  const int at = k + c * kF8Unit, left = p.K - at;
+  if (p.weight_type == kNone || left <= 0) return;
+  if (left >= 8) {
     if (p.weight_type == kF32) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const float4 v = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(p.weight) + at) + i);
-        w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+        w[2 * i] = make_float2(v.x, v.y);
+        w[2 * i + 1] = make_float2(v.z, v.w);
       }
     } else {
       const uint4 v = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.weight) + at));
-      const uint32_t raw[4] = {v.x, v.y, v.z, v.w};
+      const uint32_t raw[8] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) { w[2 * i] = __uint_as_float(raw[i] << 16); w[2 * i + 1] = __uint_as_float(raw[i] & 0xFFFF0000u); }
+      for (int i = 0; i < 4; ++i) w[i] = unit_values<false>(raw, i);
     }
   } else {
+    float x[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int at = k0 + j * 32 + lane;
-      if (at < p.K)
-        w[j] = p.weight_type == kF32 ? __ldg(static_cast<const float*>(p.weight) + at)
-                                     : bf16_to_f32(__ldg(static_cast<const uint16_t*>(p.weight) + at));
-    }
+    for (int j = 0; j < 8; ++j)
+      x[j] = j >= left ? 0.f
+             : p.weight_type == kF32 ? __ldg(static_cast<const float*>(p.weight) + at + j)
+                                     : bf16_to_f32(__ldg(static_cast<const uint16_t*>(p.weight) + at + j));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = make_float2(x[2 * i], x[2 * i + 1]);
   }
 }
 
-// Eight values per lane of the unit at k0 to the row at `row`.  Every lane of the warp takes part.
-template <bool F32, bool VEC>
-__device__ __forceinline__ void unit_store(const float (&v)[8], void* row, int k0, int K, int lane) {
-  if (VEC && F32) {
-    // two lanes' 64 bytes in two stores that each write whole 32-byte sectors: first the even lane's values, then the odd's
-    const bool odd = lane & 1;
-    float got[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) got[i] = __shfl_xor_sync(0xFFFFFFFFu, odd ? v[i] : v[4 + i], 1);
-    const int at = k0 + (lane & ~1) * 8;
-    float4* o = reinterpret_cast<float4*>(static_cast<float*>(row) + at) + odd;
-    if (at < K) *o = odd ? make_float4(got[0], got[1], got[2], got[3]) : make_float4(v[0], v[1], v[2], v[3]);
-    if (at + 8 < K) o[2] = odd ? make_float4(v[4], v[5], v[6], v[7]) : make_float4(got[0], got[1], got[2], got[3]);
-  } else if (VEC) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(__float_as_uint(v[2 * i]), __float_as_uint(v[2 * i + 1]));
-    const int at = k0 + lane * 8;
-    if (at < K) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(row) + at) = make_uint4(w[0], w[1], w[2], w[3]);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int at = k0 + j * 32 + lane;
-      if (at < K) {
-        if (F32) static_cast<float*>(row)[at] = v[j];
-        else static_cast<uint16_t*>(row)[at] = f32_to_bf16(v[j]);
-      }
-    }
-  }
-}
+// A warp's strip of a row: where its operands and results lie.
+template <bool XF32, int RES, int OUT>
+struct Strip {
+  LaneAt x, r, o;
+  uint8_t* codes;
+  uint8_t* scale;
+  int k, room;
+  __device__ __forceinline__ Strip(const NormParams& p, uint32_t row, int k0, int lane)
+      : x(row, k0, p.K, lane, XF32 ? 4 : 2), r(row, k0, p.K, lane, RES == kF32 ? 4 : 2), o(row, k0, p.K, lane, OUT == kOutF32 ? 4 : 2),
+        codes(static_cast<uint8_t*>(p.out) + static_cast<int64_t>(row) * p.pitch + k0 + lane * 8),
+        scale(p.scale + f8_scale_at(row, static_cast<uint32_t>(k0) / kF8Block, p.kt)), k(k0 + lane * 8), room(p.pitch - k0 - lane * 8) {}
+};
 
-template <int OUT, bool VEC>
-__device__ __forceinline__ void store_result(const float (&y)[8], const NormParams& p, uint32_t row, int unit, int lane) {
-  const int k0 = unit * kF8Unit;
-  if (OUT == kOutF8)
-    unit_store_f8<VEC>(y, static_cast<uint8_t*>(p.out) + static_cast<int64_t>(row) * p.pitch, k0, p.pitch, lane,
-                       p.scale + f8_scale_at(row, unit * 2, p.kt));
-  else
-    unit_store<OUT == kOutF32, VEC>(y, static_cast<char*>(p.out) + static_cast<int64_t>(row) * p.K * (OUT == kOutF32 ? 4 : 2), k0, p.K, lane);
+template <bool XF32, int RES, bool VEC>
+__device__ __forceinline__ void load_operands(const NormParams& p, const LaneAt& x, const LaneAt& r, int c, uint32_t (&raw_x)[8],
+                                              uint32_t (&raw_r)[8]) {
+  const int64_t values = static_cast<int64_t>(p.rows) * p.K;
+  unit_load<XF32, VEC>(p.x, x, c, values * (XF32 ? 4 : 2), raw_x);
+  if (RES != kNone) unit_load<RES == kF32, VEC>(p.res, r, c, values * (RES == kF32 ? 4 : 2), raw_r);
 }
 
 // h of a unit from what was loaded.
-template <bool XF32, int RES, bool VEC>
-__device__ __forceinline__ void add_residual(const uint32_t (&x)[8], const uint32_t (&r)[8], float (&h)[8]) {
+template <bool XF32, int RES>
+__device__ __forceinline__ void add_residual(const uint32_t (&x)[8], const uint32_t (&r)[8], float2 (&h)[4]) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    h[j] = unit_value<XF32, VEC>(x, j);
-    if (RES != kNone) h[j] += unit_value<RES == kF32, VEC>(r, j);
+  for (int i = 0; i < 4; ++i) {
+    h[i] = unit_values<XF32>(x, i);
+    if (RES != kNone) h[i] = add2(h[i], unit_values<RES == kF32>(r, i));
   }
+}
+
+template <int OUT, bool VEC, typename S>
+__device__ __forceinline__ void store_result(const float2 (&h)[4], float rs, const NormParams& p, const S& at, int c, int lane) {
+  float2 y[4];
+  load_weights(p, at.k, c, y);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = mul2(mul2(h[i], make_float2(rs, rs)), y[i]);
+  if (OUT == kOutF8) unit_store_f8(y, at.codes, at.room, at.scale, c, lane);
+  else unit_store<OUT == kOutF32, VEC>(y, p.out, at.o, c, lane);
 }
 
 // Sum over the warps of a row; `slots` holds one float per warp of the block.  All threads of the block call it.
@@ -130,52 +121,36 @@ __device__ __forceinline__ float row_sum(float s, float* slots, int row_warps) {
   return s;
 }
 
-// A row stays in registers between the sum of its squares and its results: C units a warp, `row_warps` warps a row, as many rows a
-// block as fit.  Everything is read once; bound by HBM.
+// A row stays in registers between the sum of its squares and its results: strips of C units a warp, `row_warps` warps a row, as
+// many rows a block as fit.  Everything is read once; bound by HBM.
 template <bool XF32, int RES, int OUT, bool VEC, int C>
 __global__ void __launch_bounds__(C == 4 ? 512 : 1024) norm_rms(const NormParams p) {
   __shared__ float slots[32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t row = blockIdx.x * ((blockDim.x >> 5) / p.row_warps) + warp / p.row_warps;
-  const int unit0 = warp & (p.row_warps - 1);
+  const int k0 = (warp & (p.row_warps - 1)) * (C * kF8Unit);
   const bool live = row < p.rows;
-  const char* x = static_cast<const char*>(p.x) + static_cast<int64_t>(row) * p.K * (XF32 ? 4 : 2);
-  const char* r = static_cast<const char*>(p.res) + static_cast<int64_t>(row) * p.K * (RES == kF32 ? 4 : 2);
+  const Strip<XF32, RES, OUT> at(p, row, k0, lane);
   pdl_wait();
   pdl_launch_dependents();
-  uint32_t raw_x[C][8], raw_r[RES == kNone ? 1 : C][8];
+  uint32_t raw_x[C][8], raw_r[C][8];
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+    if (live && k0 + c * kF8Unit < p.K) load_operands<XF32, RES, VEC>(p, at.x, at.r, c, raw_x[c], raw_r[c]);
+  float2 h[C][4], s = make_float2(0.f, 0.f);
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    const int unit = unit0 + c * p.row_warps;
-    if (live && unit < p.units) {
-      unit_load<XF32, VEC>(x, unit * kF8Unit, p.K, lane, raw_x[c]);
-      if (RES != kNone) unit_load<RES == kF32, VEC>(r, unit * kF8Unit, p.K, lane, raw_r[c]);
-    }
+    if (!live || k0 + c * kF8Unit >= p.K) break;
+    add_residual<XF32, RES>(raw_x[c], raw_r[c], h[c]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s = fma2(h[c][i], h[c][i], s);
+    if (RES != kNone && p.sum) unit_store<RES == kF32, VEC>(h[c], p.sum, at.r, c, lane);
   }
-  float h[C][8], s = 0.f;
+  const float rs = 1.f / sqrtf(row_sum(s.x + s.y, slots, p.row_warps) * p.inv_k + p.eps);
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    const int unit = unit0 + c * p.row_warps;
-    if (live && unit < p.units) {
-      add_residual<XF32, RES, VEC>(raw_x[c], raw_r[RES == kNone ? 0 : c], h[c]);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) s = fmaf(h[c][j], h[c][j], s);
-      if (RES != kNone && p.sum)
-        unit_store<RES == kF32, VEC>(h[c], static_cast<char*>(p.sum) + static_cast<int64_t>(row) * p.K * (RES == kF32 ? 4 : 2),
-                                     unit * kF8Unit, p.K, lane);
-    }
-  }
-  const float rs = 1.f / sqrtf(row_sum(s, slots, p.row_warps) * p.inv_k + p.eps);
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    const int unit = unit0 + c * p.row_warps;
-    if (live && unit < p.units) {
-      float w[8];
-      load_weights<VEC>(p, unit * kF8Unit, lane, w);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] *= h[c][j] * rs;
-      store_result<OUT, VEC>(w, p, row, unit, lane);
-    }
+    if (!live || k0 + c * kF8Unit >= p.K) break;
+    store_result<OUT, VEC>(h[c], rs, p, at, c, lane);
   }
 }
 
@@ -186,35 +161,27 @@ __global__ void __launch_bounds__(1024) norm_rms_long(const NormParams p) {
   __shared__ float slots[32];
   const int lane = threadIdx.x & 31;
   const uint32_t row = blockIdx.x;
-  const char* x = static_cast<const char*>(p.x) + static_cast<int64_t>(row) * p.K * (XF32 ? 4 : 2);
-  const char* r = static_cast<const char*>(p.res) + static_cast<int64_t>(row) * p.K * (RES == kF32 ? 4 : 2);
   pdl_wait();
   pdl_launch_dependents();
-  float s = 0.f;
+  float total = 0.f;
   uint32_t raw_x[8], raw_r[8];
-  float h[8];
+  float2 h[4];
   for (int unit = threadIdx.x >> 5; unit < p.units; unit += 32) {
-    unit_load<XF32, VEC>(x, unit * kF8Unit, p.K, lane, raw_x);
-    if (RES != kNone) unit_load<RES == kF32, VEC>(r, unit * kF8Unit, p.K, lane, raw_r);
-    add_residual<XF32, RES, VEC>(raw_x, raw_r, h);
-    float part = 0.f;   // (a lane adds up to 2^15 values for the longest rows: by units of eight first)
+    const Strip<XF32, RES, OUT> at(p, row, unit * kF8Unit, lane);
+    load_operands<XF32, RES, VEC>(p, at.x, at.r, 0, raw_x, raw_r);
+    add_residual<XF32, RES>(raw_x, raw_r, h);
+    float2 s = make_float2(0.f, 0.f);   // (a lane adds up to 2^15 values for the longest rows: by units of eight first)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) part = fmaf(h[j], h[j], part);
-    s += part;
+    for (int i = 0; i < 4; ++i) s = fma2(h[i], h[i], s);
+    total += s.x + s.y;
   }
-  const float rs = 1.f / sqrtf(row_sum(s, slots, 32) * p.inv_k + p.eps);
+  const float rs = 1.f / sqrtf(row_sum(total, slots, 32) * p.inv_k + p.eps);
   for (int unit = threadIdx.x >> 5; unit < p.units; unit += 32) {
-    unit_load<XF32, VEC>(x, unit * kF8Unit, p.K, lane, raw_x);
-    if (RES != kNone) unit_load<RES == kF32, VEC>(r, unit * kF8Unit, p.K, lane, raw_r);
-    add_residual<XF32, RES, VEC>(raw_x, raw_r, h);
-    if (RES != kNone && p.sum)
-      unit_store<RES == kF32, VEC>(h, static_cast<char*>(p.sum) + static_cast<int64_t>(row) * p.K * (RES == kF32 ? 4 : 2),
-                                   unit * kF8Unit, p.K, lane);
-    float w[8];
-    load_weights<VEC>(p, unit * kF8Unit, lane, w);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) w[j] *= h[j] * rs;
-    store_result<OUT, VEC>(w, p, row, unit, lane);
+    const Strip<XF32, RES, OUT> at(p, row, unit * kF8Unit, lane);
+    load_operands<XF32, RES, VEC>(p, at.x, at.r, 0, raw_x, raw_r);
+    add_residual<XF32, RES>(raw_x, raw_r, h);
+    if (RES != kNone && p.sum) unit_store<RES == kF32, VEC>(h, p.sum, at.r, 0, lane);
+    store_result<OUT, VEC>(h, rs, p, at, 0, lane);
   }
 }
 

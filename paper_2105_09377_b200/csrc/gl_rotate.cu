@@ -2,9 +2,11 @@
 // position[axis of the pair] * frequency of the pair.
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 
+#include "gl_f8.cuh"
 #include "gl_internal.h"
 #include "gl_launch.cuh"
 #include "gl_tc.cuh"
@@ -18,23 +20,24 @@ namespace {
 // out of the integer product by themselves and the rest is exact to position * 2^-65 turns, where an fp32 product of position and
 // frequency is off by a sixteenth of a radian at a million tokens.
 //
-// A block takes a few tokens: cosines and sines of its tokens once into shared memory, then its threads take tasks of W pairs of
-// a head, 2W values, all of a round requested before the first is used (the first round's before the angles are computed).
+// A block takes a few tokens: cosines and sines of its tokens once into shared memory, then every thread takes one group of W
+// pairs, 2W values, of head after head, kRotRows of them requested before the first is used (the first ones before the angles
+// are computed).
 constexpr int kRotThreads = 256;
-constexpr int kRotTasks = 4;          // tasks of a thread in flight
-constexpr int kRotMaxTokens = 16;     // tokens of a block
+constexpr int kRotRows = 4;           // heads of a thread in flight
+constexpr int kRotAngles = 512;       // angles of a block of several tokens
 
 struct RotateParams {
   const void* x;
   void* out;
   const int32_t* positions;    // [axes][tokens]
   int64_t tokens, pitch, out_pitch;
-  int32_t heads, d, pairs;
-  int32_t per_head;            // tasks of a head: pairs / W, then (d - 2 pairs) / (2W), rounded up, that only copy
+  int32_t d, pairs;
+  int32_t groups;              // of a head: pairs / W, then (d - 2 pairs) / (2W), rounded up, that only copy
+  int32_t lanes, rows;         // threads side by side on a head; heads that the block takes at a time
   int32_t per_block;           // tokens of a block
   int32_t back;
-  FastDiv div_head, div_token; // tasks of a head; tasks of a token
-  FastDiv div_pairs;
+  FastDiv div_heads, div_lanes, div_pairs;
   gl_rotary plan;
 };
 
@@ -51,10 +54,12 @@ __device__ __forceinline__ void to_floats(const typename Raw<W * (F32 ? 4 : 2)>:
     const float* f = reinterpret_cast<const float*>(&raw);
 #pragma unroll
     for (int i = 0; i < W; ++i) v[i] = f[i];
+  } else if constexpr (W == 1) {
+    v[0] = bf16_to_f32(raw);
   } else {
-    const uint16_t* h = reinterpret_cast<const uint16_t*>(&raw);
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(&raw);
 #pragma unroll
-    for (int i = 0; i < W; ++i) v[i] = bf16_to_f32(h[i]);
+    for (int i = 0; i < W / 2; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
   }
 }
 template <bool F32, int W>
@@ -74,107 +79,128 @@ __device__ __forceinline__ typename Raw<W * (F32 ? 4 : 2)>::type from_floats(con
   return raw;
 }
 
-struct TaskAt {
-  int64_t in, out;    // element of the token's start
-  int first, second;  // elements of the two groups of W values inside the token; second < 0: there is none
-  int angle;          // index of the first pair's cosine, < 0: values to copy
-  bool live;
-};
-
-template <int W>
-__device__ __forceinline__ TaskAt task_at(const RotateParams& p, uint32_t task, uint32_t tasks, int64_t token0) {
-  TaskAt t;
-  t.live = task < tasks;
-  uint32_t token, in_token, head, i;
-  p.div_token.divmod(t.live ? task : 0u, token, in_token);
-  p.div_head.divmod(in_token, head, i);
-  t.in = (token0 + token) * p.pitch;
-  t.out = (token0 + token) * p.out_pitch;
-  const int base = static_cast<int>(head) * p.d, turned = p.pairs / W;
-  if (static_cast<int>(i) < turned) {
-    const int pair = static_cast<int>(i) * W;
-    t.first = base + (p.plan.adjacent ? 2 * pair : pair);
-    t.second = t.first + (p.plan.adjacent ? W : p.pairs);
-    t.angle = static_cast<int>(token) * p.pairs + pair;
+// N pairs (u, v) turned by N consecutive angles, two at a time.
+template <int N>
+__device__ __forceinline__ void turn(float (&u)[N], float (&v)[N], const float* c, const float* s) {
+  float cs[N], sn[N];
+  if constexpr (N % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      *reinterpret_cast<float4*>(cs + i) = *reinterpret_cast<const float4*>(c + i);
+      *reinterpret_cast<float4*>(sn + i) = *reinterpret_cast<const float4*>(s + i);
+    }
   } else {
-    const int at = 2 * p.pairs + (static_cast<int>(i) - turned) * 2 * W;
-    t.first = base + at;
-    t.second = at + W < p.d ? t.first + W : -1;
-    t.angle = -1;
+#pragma unroll
+    for (int i = 0; i < N; ++i) { cs[i] = c[i]; sn[i] = s[i]; }
   }
-  return t;
+  if constexpr (N % 2 == 0) {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      const float2 a = make_float2(u[i], u[i + 1]), b = make_float2(v[i], v[i + 1]), cc = make_float2(cs[i], cs[i + 1]), ss = make_float2(sn[i], sn[i + 1]);
+      const float2 x = sub2(mul2(a, cc), mul2(b, ss)), y = fma2(a, ss, mul2(b, cc));
+      u[i] = x.x; u[i + 1] = x.y;
+      v[i] = y.x; v[i + 1] = y.y;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float a = u[i], b = v[i];
+      u[i] = a * cs[i] - b * sn[i];
+      v[i] = a * sn[i] + b * cs[i];
+    }
+  }
 }
 
 template <bool F32, int W>
 __global__ void __launch_bounds__(kRotThreads) rotate_pairs(const __grid_constant__ RotateParams p) {
   typedef typename Raw<W * (F32 ? 4 : 2)>::type Word;
-  extern __shared__ float trig[];   // cosines [tokens][pairs], then sines
+  extern __shared__ __align__(16) float trig[];   // cosines [tokens][pairs], then sines
   constexpr int kEs = F32 ? 4 : 2;
   const int64_t token0 = static_cast<int64_t>(blockIdx.x) * p.per_block;
   const int tokens = static_cast<int>(min(static_cast<int64_t>(p.per_block), p.tokens - token0));
-  const uint32_t tasks = static_cast<uint32_t>(tokens) * p.div_token.d;
-  const char* in = static_cast<const char*>(p.x);
-  char* out = static_cast<char*>(p.out);
+  const uint32_t rows = static_cast<uint32_t>(tokens) * p.div_heads.d;   // heads of all of the block's tokens
+  const char* in = static_cast<const char*>(p.x) + token0 * p.pitch * kEs;
+  char* out = static_cast<char*>(p.out) + token0 * p.out_pitch * kEs;
   float* sines = trig + p.per_block * p.pairs;
+  // Neighbouring lanes ask for different pairs: through the cache of data, not that of constants, which serves one address at a
+  // time (8192 tokens of one head of 64 pairs: 11.5 -> 5.8 us).
+  const gl_rotary* plan = &p.plan;
+  asm volatile("" : "+l"(plan));
+  uint32_t first_row, lane;
+  p.div_lanes.divmod(threadIdx.x, first_row, lane);
+  if (first_row >= static_cast<uint32_t>(p.rows)) first_row = rows;      // a thread too many
   pdl_wait();
   pdl_launch_dependents();
-  for (uint32_t round = 0; round < tasks; round += kRotThreads * kRotTasks) {
-    Word a[kRotTasks], b[kRotTasks];
+  bool angles = false;
+  const int turned = p.pairs / W;
+  for (int g0 = 0; g0 < p.groups; g0 += p.lanes) {
+    const int g = g0 + static_cast<int>(lane);
+    // the group's two times W values inside a head
+    const bool turns = g < turned;
+    const int one = turns ? (p.plan.adjacent ? 2 * W * g : W * g) : 2 * (p.pairs + (g - turned) * W);
+    const int two = one + (turns && !p.plan.adjacent ? p.pairs : W);
+    const bool has_one = g < p.groups, has_two = has_one && two < p.d;
+    for (uint32_t r0 = 0; r0 < rows; r0 += kRotRows * p.rows) {
+      Word a[kRotRows], b[kRotRows];
 #pragma unroll
-    for (int j = 0; j < kRotTasks; ++j) {
-      const TaskAt t = task_at<W>(p, round + j * kRotThreads + threadIdx.x, tasks, token0);
-      if (t.live) {
-        a[j] = *reinterpret_cast<const Word*>(in + (t.in + t.first) * kEs);
-        if (t.second >= 0) b[j] = *reinterpret_cast<const Word*>(in + (t.in + t.second) * kEs);
+      for (int j = 0; j < kRotRows; ++j) {
+        const uint32_t r = first_row + r0 + j * p.rows;
+        if (r >= rows) break;
+        uint32_t token, head;
+        p.div_heads.divmod(r, token, head);
+        const char* src = in + (static_cast<int64_t>(token) * p.pitch + static_cast<int>(head) * p.d) * kEs;
+        if (has_one) a[j] = *reinterpret_cast<const Word*>(src + one * kEs);
+        if (has_two) b[j] = *reinterpret_cast<const Word*>(src + two * kEs);
       }
-    }
-    if (round == 0) {
-      for (int i = threadIdx.x; i < tokens * p.pairs; i += kRotThreads) {
-        uint32_t token, pair;
-        p.div_pairs.divmod(static_cast<uint32_t>(i), token, pair);
-        const int64_t at = p.positions[p.plan.axis[pair] * p.tokens + token0 + token];
-        const int64_t phase = static_cast<int64_t>(p.plan.step[pair] * static_cast<uint64_t>(at));
-        float s, c;
-        sincospif(__ll2float_rn(phase) * 0x1p-63f, &s, &c);   // a signed fraction of half a turn
-        trig[i] = c;
-        sines[i] = p.back ? -s : s;
-      }
-      __syncthreads();
-    }
-#pragma unroll
-    for (int j = 0; j < kRotTasks; ++j) {
-      const TaskAt t = task_at<W>(p, round + j * kRotThreads + threadIdx.x, tasks, token0);
-      if (!t.live) continue;
-      if (t.angle >= 0) {
-        float u[W], v[W];
-        to_floats<F32, W>(a[j], u);
-        to_floats<F32, W>(b[j], v);
-        if (p.plan.adjacent && W > 1) {
-          // pairs (0,1), (2,3), ... of the 2W values in u, v
-#pragma unroll
-          for (int i = 0; i < W; i += 2) {
-            const int pu = t.angle + i / 2, pv = pu + W / 2;
-            const float cu = trig[pu], su = sines[pu], cv = trig[pv], sv = sines[pv];
-            const float u0 = u[i], u1 = u[i + 1 < W ? i + 1 : i], v0 = v[i], v1 = v[i + 1 < W ? i + 1 : i];
-            u[i] = u0 * cu - u1 * su;
-            u[i + 1 < W ? i + 1 : i] = u0 * su + u1 * cu;
-            v[i] = v0 * cv - v1 * sv;
-            v[i + 1 < W ? i + 1 : i] = v0 * sv + v1 * cv;
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < W; ++i) {
-            const float c = trig[t.angle + i], s = sines[t.angle + i];
-            const float x0 = u[i], x1 = v[i];
-            u[i] = x0 * c - x1 * s;
-            v[i] = x0 * s + x1 * c;
-          }
+      if (!angles) {
+        angles = true;
+        for (int i = threadIdx.x; i < tokens * p.pairs; i += kRotThreads) {
+          uint32_t token, pair;
+          p.div_pairs.divmod(static_cast<uint32_t>(i), token, pair);
+          const int64_t at = p.positions[plan->axis[pair] * p.tokens + token0 + token];
+          const int64_t phase = static_cast<int64_t>(plan->step[pair] * static_cast<uint64_t>(at));
+          float s, c;
+          sincospif(__ll2float_rn(phase) * 0x1p-63f, &s, &c);   // a signed fraction of half a turn
+          trig[i] = c;
+          sines[i] = p.back ? -s : s;
         }
-        a[j] = from_floats<F32, W>(u);
-        b[j] = from_floats<F32, W>(v);
+        __syncthreads();
       }
-      *reinterpret_cast<Word*>(out + (t.out + t.first) * kEs) = a[j];
-      if (t.second >= 0) *reinterpret_cast<Word*>(out + (t.out + t.second) * kEs) = b[j];
+#pragma unroll
+      for (int j = 0; j < kRotRows; ++j) {
+        const uint32_t r = first_row + r0 + j * p.rows;
+        if (r >= rows) break;
+        uint32_t token, head;
+        p.div_heads.divmod(r, token, head);
+        if (turns) {
+          float u[W], v[W];
+          to_floats<F32, W>(a[j], u);
+          to_floats<F32, W>(b[j], v);
+          const int at = static_cast<int>(token) * p.pairs + g * W;
+          if (W > 1 && p.plan.adjacent) {
+            // (u, v) are 2W values in a row: pairs (0, 1), (2, 3), ..
+            float x[W], y[W];
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+              x[i] = 2 * i < W ? u[2 * i & (W - 1)] : v[2 * i & (W - 1)];
+              y[i] = 2 * i < W ? u[(2 * i + 1) & (W - 1)] : v[(2 * i + 1) & (W - 1)];
+            }
+            turn<W>(x, y, trig + at, sines + at);
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+              (2 * i < W ? u : v)[2 * i & (W - 1)] = x[i];
+              (2 * i < W ? u : v)[(2 * i + 1) & (W - 1)] = y[i];
+            }
+          } else {
+            turn<W>(u, v, trig + at, sines + at);
+          }
+          a[j] = from_floats<F32, W>(u);
+          b[j] = from_floats<F32, W>(v);
+        }
+        char* dst = out + (static_cast<int64_t>(token) * p.out_pitch + static_cast<int>(head) * p.d) * kEs;
+        if (has_one) *reinterpret_cast<Word*>(dst + one * kEs) = a[j];
+        if (has_two) *reinterpret_cast<Word*>(dst + two * kEs) = b[j];
+      }
     }
   }
 }
@@ -263,7 +289,6 @@ int gl_compute_rotate(const gl_ap* x, int64_t token_pitch, const gl_rotary* plan
   p.tokens = b * t;
   p.pitch = token_pitch;
   p.out_pitch = out_pitch;
-  p.heads = static_cast<int32_t>(heads);
   p.d = static_cast<int32_t>(d);
   p.pairs = plan->pairs;
   p.back = (flags & GL_ROTATE_BACK) ? 1 : 0;
@@ -273,14 +298,16 @@ int gl_compute_rotate(const gl_ap* x, int64_t token_pitch, const gl_rotary* plan
   int w = f32 ? 4 : 8;
   while (w > 1 && (p.pairs % w || d % w || token_pitch % w || out_pitch % w)) w /= 2;
   const int64_t copied = d - 2 * p.pairs;
-  p.per_head = static_cast<int32_t>(p.pairs / w + (out->data == x->data ? 0 : (copied + 2 * w - 1) / (2 * w)));
-  const int64_t per_token = heads * p.per_head;
-  // tokens of a block: a round of tasks for its threads
-  p.per_block = 1;
-  while (p.per_block * 2 <= kRotMaxTokens && p.per_block * 2 * per_token <= kRotThreads * kRotTasks) p.per_block *= 2;
-  while (p.per_block > 1 && (p.tokens + p.per_block - 1) / p.per_block < 2 * num_sms()) p.per_block /= 2;
-  p.div_head.set(p.per_head);
-  p.div_token.set(per_token);
+  p.groups = static_cast<int32_t>(p.pairs / w + (out->data == x->data ? 0 : (copied + 2 * w - 1) / (2 * w)));
+  p.lanes = std::min(p.groups, kRotThreads);
+  p.rows = kRotThreads / p.lanes;
+  // tokens of a block: as many heads as its threads hold in flight, and no more angles than a few a thread; fewer while there
+  // are SMs without a block
+  int64_t per_block = std::min<int64_t>(static_cast<int64_t>(kRotRows) * p.rows / heads, kRotAngles / p.pairs);
+  per_block = std::min(per_block, p.tokens / (2 * num_sms()));
+  p.per_block = static_cast<int32_t>(std::max<int64_t>(per_block, 1));
+  p.div_heads.set(heads);
+  p.div_lanes.set(p.lanes);
   p.div_pairs.set(p.pairs);
   const int64_t blocks = (p.tokens + p.per_block - 1) / p.per_block;
   if (blocks > INT32_MAX) return GL_ERR_UNSUPPORTED;
