@@ -48,27 +48,22 @@ __global__ void __launch_bounds__(256) quantize_f8(const void* __restrict__ in, 
   p.per_row.divmod(strip, group, at);
   const uint32_t row0 = group * R;
   const int k0 = static_cast<int>(at) * (U * kF8Unit);
-  const int64_t total = static_cast<int64_t>(p.rows) * p.K * (F32 ? 4 : 2);
-  uint32_t raw[R * U][8];
+  Unit<F32, VEC> held[R * U];
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    if (row0 + r >= p.rows) break;
-    const LaneAt l(row0 + r, k0, p.K, lane, F32 ? 4 : 2);
-#pragma unroll
-    for (int u = 0; u < U; ++u) unit_load<F32, VEC>(in, l, u, total, raw[r * U + u]);
-  }
+  for (int r = 0; r < R; ++r)
+    if (row0 + r < p.rows) units_read<F32, VEC, U>(in, LaneAt(row0 + r, p.rows, k0, p.K, lane, F32 ? 4 : 2), held + r * U);
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const uint32_t row = row0 + r;
     if (row >= p.rows) break;
+    const LaneAt l(row, p.rows, k0, p.K, lane, F32 ? 4 : 2);
     uint8_t* to = codes + static_cast<int64_t>(row) * p.pitch + k0 + lane * 8;
     uint8_t* scale_to = scale + f8_scale_at(row, at * (2 * U), p.kt);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (k0 + u * kF8Unit >= p.K) break;
       float2 v[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = unit_values<F32>(raw[r * U + u], i);
+      unit_values(held[r * U + u], l, u, v);
       unit_store_f8(v, to, p.pitch - k0 - lane * 8, scale_to, u, lane);
     }
   }
@@ -125,7 +120,7 @@ __global__ void __launch_bounds__(256) dequantize_f8(const uint8_t* __restrict__
   for (int r = 0; r < R; ++r) {
     const uint32_t row = row0 + r;
     if (row >= p.rows) break;
-    const LaneAt l(row, k0, p.K, lane, F32 ? 4 : 2);
+    const LaneAt l(row, p.rows, k0, p.K, lane, F32 ? 4 : 2);
     float* o = static_cast<float*>(out) + static_cast<int64_t>(row) * p.K + k0 + lane * 4;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -149,7 +144,8 @@ __global__ void __launch_bounds__(256) dequantize_f8(const uint8_t* __restrict__
   }
 }
 
-// Units of a strip and rows of a warp.
+// Units of a strip and rows of a warp: eight units in flight, four where rows are unaligned (a unit takes half as many registers
+// again, and more).
 struct StripPlan { int units, rows; };
 
 F8QuantParams f8_quant_params(const F8View& v, StripPlan* plan) {
@@ -157,8 +153,9 @@ F8QuantParams f8_quant_params(const F8View& v, StripPlan* plan) {
   // several units a warp only when every SM has blocks to hold
   const bool many = v.rows * units >= static_cast<int64_t>(num_sms()) * 4 * 8 * 8;
   plan->units = 1;
-  while (many && plan->units < 8 && plan->units < units) plan->units *= 2;
-  plan->rows = many ? 8 / plan->units : 1;
+  const int most = v.K % 8 ? 4 : 8;
+  while (many && plan->units < most && plan->units < units) plan->units *= 2;
+  plan->rows = many ? most / plan->units : 1;
   F8QuantParams p;
   p.K = static_cast<int32_t>(v.K);
   p.pitch = static_cast<int32_t>(v.pitch);
@@ -175,22 +172,24 @@ typedef void (*DequantizeFn)(const uint8_t*, const uint8_t*, void*, F8QuantParam
 
 template <bool F32, bool VEC>
 QuantizeFn quantize_fn(const StripPlan& s) {
+  constexpr int kMost = VEC ? 8 : 4;
   if (s.rows == 1 && s.units == 1) return quantize_f8<F32, VEC, 1, 1>;
   switch (s.units) {
-    case 1: return quantize_f8<F32, VEC, 1, 8>;
-    case 2: return quantize_f8<F32, VEC, 2, 4>;
-    case 4: return quantize_f8<F32, VEC, 4, 2>;
-    default: return quantize_f8<F32, VEC, 8, 1>;
+    case 1: return quantize_f8<F32, VEC, 1, kMost>;
+    case 2: return quantize_f8<F32, VEC, 2, kMost / 2>;
+    case 4: return quantize_f8<F32, VEC, 4, kMost / 4>;
+    default: return quantize_f8<F32, VEC, kMost, 1>;
   }
 }
 template <bool F32, bool VEC>
 DequantizeFn dequantize_fn(const StripPlan& s) {
+  constexpr int kMost = VEC ? 8 : 4;
   if (s.rows == 1 && s.units == 1) return dequantize_f8<F32, VEC, 1, 1>;
   switch (s.units) {
-    case 1: return dequantize_f8<F32, VEC, 1, 8>;
-    case 2: return dequantize_f8<F32, VEC, 2, 4>;
-    case 4: return dequantize_f8<F32, VEC, 4, 2>;
-    default: return dequantize_f8<F32, VEC, 8, 1>;
+    case 1: return dequantize_f8<F32, VEC, 1, kMost>;
+    case 2: return dequantize_f8<F32, VEC, 2, kMost / 2>;
+    case 4: return dequantize_f8<F32, VEC, 4, kMost / 4>;
+    default: return dequantize_f8<F32, VEC, kMost, 1>;
   }
 }
 

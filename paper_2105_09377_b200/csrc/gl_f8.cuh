@@ -132,67 +132,97 @@ __device__ __forceinline__ void shift_words(uint32_t (&w)[N], int t, uint32_t (&
   for (int i = 0; i < OUT; ++i) out[i] = i + 1 < N ? __funnelshift_r(w[i], w[i + 1], (t & 2) * 8) : w[i];
 }
 
-// 16 bytes at a boundary of a pattern of `total` bytes; what lies behind its end is not read.
-__device__ __forceinline__ uint4 load_chunk(const char* base, int64_t at, int64_t total) {
-  if (at + 16 <= total) return *reinterpret_cast<const uint4*>(base + at);
-  uint64_t lo = 0, hi = 0;   // (one lane of the whole grid: small rather than fast)
-#pragma unroll 1
-  for (int left = static_cast<int>(total - at) - 2; left >= 0; left -= 2) {
-    hi = hi << 16 | lo >> 48;
-    lo = lo << 16 | *reinterpret_cast<const uint16_t*>(base + at + left);
-  }
-  return make_uint4(static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32), static_cast<uint32_t>(hi), static_cast<uint32_t>(hi >> 32));
-}
-
 // A lane's place in a pattern whose items are `K` values: its values of unit c are the eight from byte at + c * 256 values on.
 struct LaneAt {
   int64_t at;     // of the lane's first value in the strip's first unit
   int left;       // values of the row from there on
   int strip;      // values of the row from the strip's beginning on (the same for all lanes)
-  __device__ __forceinline__ LaneAt(uint32_t row, int k0, int K, int lane, int value_bytes)
-      : at((static_cast<int64_t>(row) * K + k0 + lane * 8) * value_bytes), left(K - k0 - lane * 8), strip(K - k0) {}
+  bool inside;    // the 16 bytes that hold the row's last value lie wholly inside the pattern (the same for all lanes)
+  __device__ __forceinline__ LaneAt(uint32_t row, uint32_t rows, int k0, int K, int lane, int value_bytes)
+      : at((static_cast<int64_t>(row) * K + k0 + lane * 8) * value_bytes), left(K - k0 - lane * 8), strip(K - k0),
+        inside(((static_cast<int64_t>(row) + 1) * K * value_bytes + 15 & ~int64_t{15}) <= static_cast<int64_t>(rows) * K * value_bytes) {}
 };
 
-// A lane's eight values of unit c, zeros behind the row's end: four words of bf16 pairs, or eight of floats.  `total`: bytes of
-// the pattern.
+// What a lane has read of a unit: its eight values, or the 16-byte pieces that hold them.
 template <bool F32, bool VEC>
-__device__ __forceinline__ void unit_load(const void* base, const LaneAt& l, int c, int64_t total, uint32_t (&raw)[8]) {
-  constexpr int kEs = F32 ? 4 : 2, kWords = F32 ? 8 : 4;
+struct Unit {
+  static constexpr int kWords = F32 ? 8 : 4, kHeld = kWords + (VEC ? 0 : 4);
+  uint32_t w[kHeld];
+};
+
+// Requests unit c; nothing behind the row's end is read but what shares a piece with its last value.
+template <bool F32, bool VEC>
+__device__ __forceinline__ void unit_read(const void* base, const LaneAt& l, int c, Unit<F32, VEC>& u) {
+  constexpr int kEs = F32 ? 4 : 2;
+  const int left = l.left - c * kF8Unit, t = VEC ? 0 : static_cast<int>(l.at & 15), bytes = t + min(8, left) * kEs;
+  const uint4* q = reinterpret_cast<const uint4*>(static_cast<const char*>(base) + l.at - t + c * kF8Unit * kEs);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) raw[j] = 0;
-  const int left = l.left - c * kF8Unit;
-  if (left <= 0) return;
-  const char* p = static_cast<const char*>(base);
-  if (VEC) {   // rows are multiples of eight values: a lane's lie wholly inside or wholly behind
-#pragma unroll
-    for (int i = 0; i < kWords / 4; ++i) {
-      const uint4 x = __ldcs(reinterpret_cast<const uint4*>(p + l.at + c * kF8Unit * kEs) + i);
-      raw[4 * i] = x.x; raw[4 * i + 1] = x.y; raw[4 * i + 2] = x.z; raw[4 * i + 3] = x.w;
-    }
-  } else {
-    // (the last chunk is the next lane's first: it comes from L1)
-    const int t = static_cast<int>(l.at & 15), n = min(8, left), bytes = t + n * kEs;
-    const int64_t first = l.at - t + c * kF8Unit * kEs;
-    uint32_t w[kWords + 4], x[kWords];
-#pragma unroll
-    for (int i = 0; i < kWords / 4 + 1; ++i) {
-      uint4 v = make_uint4(0, 0, 0, 0);
-      if (16 * i < bytes) v = load_chunk(p, first + 16 * i, total);
-      w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
-    }
-    shift_words(w, t, x);
-#pragma unroll
-    for (int i = 0; i < kWords; ++i) {
-      if (F32) raw[i] = i < n ? x[i] : 0u;
-      else raw[i] = 2 * i + 1 < n ? x[i] : 2 * i < n ? x[i] & 0xFFFFu : 0u;
-    }
+  for (int i = 0; i < Unit<F32, VEC>::kHeld / 4; ++i) {
+    uint4 x = make_uint4(0, 0, 0, 0);
+    // (aligned rows are multiples of eight values: a lane's lie wholly inside or wholly behind; of the other rows a lane's last
+    // piece is the next one's first, which comes from L1)
+    if (VEC && left > 0) x = __ldcs(q + i);
+    if (!VEC && left > 0 && 16 * i < bytes) x = q[i];
+    u.w[4 * i] = x.x; u.w[4 * i + 1] = x.y; u.w[4 * i + 2] = x.z; u.w[4 * i + 3] = x.w;
   }
 }
-// Values 2i and 2i + 1 of what unit_load brought, as fp32.
-template <bool F32>
-__device__ __forceinline__ float2 unit_values(const uint32_t (&raw)[8], int i) {
-  return F32 ? make_float2(__uint_as_float(raw[2 * i & 7]), __uint_as_float(raw[2 * i + 1 & 7]))
-             : make_float2(__uint_as_float(raw[i] << 16), __uint_as_float(raw[i] & 0xFFFF0000u));
+
+// The same value by value, for the rows whose last piece is not wholly inside the pattern.
+template <bool F32, bool VEC>
+__device__ __forceinline__ void unit_read_edge(const void* base, const LaneAt& l, int c, Unit<F32, VEC>& u) {
+  constexpr int kEs = F32 ? 4 : 2;
+  const int left = l.left - c * kF8Unit, t = static_cast<int>(l.at & 15), bytes = left > 0 ? t + min(8, left) * kEs : 0;
+  const char* q = static_cast<const char*>(base) + l.at - t + c * kF8Unit * kEs;
+#pragma unroll
+  for (int i = 0; i < Unit<F32, VEC>::kHeld; ++i) u.w[i] = 0;
+#pragma unroll
+  for (int i = 0; i < Unit<F32, VEC>::kHeld * 4 / kEs; ++i)
+    if (i * kEs >= t && i * kEs < bytes) {
+      if (F32) u.w[i] = *reinterpret_cast<const uint32_t*>(q + 4 * i);
+      else u.w[i >> 1] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(q + 2 * i)) << (16 * (i & 1));
+    }
+}
+
+// N units of a strip, all requested before the first is used (no branch lies between the requests).
+template <bool F32, bool VEC, int N>
+__device__ __forceinline__ void units_read(const void* base, const LaneAt& l, Unit<F32, VEC>* u) {
+  if (VEC || l.inside) {
+#pragma unroll
+    for (int c = 0; c < N; ++c) unit_read(base, l, c, u[c]);
+  } else {
+#pragma unroll
+    for (int c = 0; c < N; ++c) unit_read_edge(base, l, c, u[c]);
+  }
+}
+
+// A unit's values as fp32, zeros behind the row's end.
+template <bool F32, bool VEC>
+__device__ __forceinline__ void unit_values(const Unit<F32, VEC>& u, const LaneAt& l, int c, float2 (&v)[4]) {
+  constexpr int kWords = Unit<F32, VEC>::kWords;
+  uint32_t x[8];
+  if constexpr (VEC) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) x[i] = u.w[i];
+  } else {
+    uint32_t w[kWords + 4], y[kWords];
+#pragma unroll
+    for (int i = 0; i < kWords + 4; ++i) w[i] = u.w[i];
+    shift_words(w, static_cast<int>(l.at & 15), y);
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) x[i] = y[i];
+    if (l.strip - c * kF8Unit < kF8Unit) {   // the row's last, partial unit
+      const int left = l.left - c * kF8Unit;
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) {
+        if (F32) x[i] = i < left ? x[i] : 0u;
+        else x[i] = 2 * i + 1 < left ? x[i] : 2 * i < left ? x[i] & 0xFFFFu : 0u;
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    v[i] = F32 ? make_float2(__uint_as_float(x[2 * i & 7]), __uint_as_float(x[2 * i + 1 & 7]))
+               : make_float2(__uint_as_float(x[i] << 16), __uint_as_float(x[i] & 0xFFFF0000u));
 }
 
 // Eight values per lane to unit c.  Every lane of the warp takes part, whether or not it has values.

@@ -3,6 +3,7 @@
 //   h = x + residual;  sum = h in the residual's type;  y = h / sqrt(mean(h^2) + eps) * weight
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 
@@ -31,7 +32,8 @@ struct NormParams {
   uint32_t kt;
   int32_t units;         // units of 256 values per row
   int32_t weight_type;
-  int32_t row_warps;     // warps per row, a power of two
+  FastDiv row_warps;     // warps per row
+  int32_t block_rows;    // rows per block
   float eps, inv_k;
 };
 
@@ -51,9 +53,9 @@ __device__ __forceinline__ void load_weights(const NormParams& p, int k, int c, 
       }
     } else {
       const uint4 v = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.weight) + at));
-      const uint32_t raw[8] = {v.x, v.y, v.z, v.w};
+      const uint32_t raw[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = unit_values<false>(raw, i);
+      for (int i = 0; i < 4; ++i) w[i] = make_float2(__uint_as_float(raw[i] << 16), __uint_as_float(raw[i] & 0xFFFF0000u));
     }
   } else {
     float x[8];
@@ -75,26 +77,21 @@ struct Strip {
   uint8_t* scale;
   int k, room;
   __device__ __forceinline__ Strip(const NormParams& p, uint32_t row, int k0, int lane)
-      : x(row, k0, p.K, lane, XF32 ? 4 : 2), r(row, k0, p.K, lane, RES == kF32 ? 4 : 2), o(row, k0, p.K, lane, OUT == kOutF32 ? 4 : 2),
+      : x(row, p.rows, k0, p.K, lane, XF32 ? 4 : 2), r(row, p.rows, k0, p.K, lane, RES == kF32 ? 4 : 2),
+        o(row, p.rows, k0, p.K, lane, OUT == kOutF32 ? 4 : 2),
         codes(static_cast<uint8_t*>(p.out) + static_cast<int64_t>(row) * p.pitch + k0 + lane * 8),
         scale(p.scale + f8_scale_at(row, static_cast<uint32_t>(k0) / kF8Block, p.kt)), k(k0 + lane * 8), room(p.pitch - k0 - lane * 8) {}
 };
 
-template <bool XF32, int RES, bool VEC>
-__device__ __forceinline__ void load_operands(const NormParams& p, const LaneAt& x, const LaneAt& r, int c, uint32_t (&raw_x)[8],
-                                              uint32_t (&raw_r)[8]) {
-  const int64_t values = static_cast<int64_t>(p.rows) * p.K;
-  unit_load<XF32, VEC>(p.x, x, c, values * (XF32 ? 4 : 2), raw_x);
-  if (RES != kNone) unit_load<RES == kF32, VEC>(p.res, r, c, values * (RES == kF32 ? 4 : 2), raw_r);
-}
-
-// h of a unit from what was loaded.
-template <bool XF32, int RES>
-__device__ __forceinline__ void add_residual(const uint32_t (&x)[8], const uint32_t (&r)[8], float2 (&h)[4]) {
+// h of unit c from what was read.
+template <bool XF32, int RES, bool VEC, typename S>
+__device__ __forceinline__ void add_residual(const Unit<XF32, VEC>& x, const Unit<RES == kF32, VEC>& r, const S& at, int c, float2 (&h)[4]) {
+  unit_values(x, at.x, c, h);
+  if (RES != kNone) {
+    float2 v[4];
+    unit_values(r, at.r, c, v);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    h[i] = unit_values<XF32>(x, i);
-    if (RES != kNone) h[i] = add2(h[i], unit_values<RES == kF32>(r, i));
+    for (int i = 0; i < 4; ++i) h[i] = add2(h[i], v[i]);
   }
 }
 
@@ -108,13 +105,13 @@ __device__ __forceinline__ void store_result(const float2 (&h)[4], float rs, con
   else unit_store<OUT == kOutF32, VEC>(y, p.out, at.o, c, lane);
 }
 
-// Sum over the warps of a row; `slots` holds one float per warp of the block.  All threads of the block call it.
-__device__ __forceinline__ float row_sum(float s, float* slots, int row_warps) {
+// Sum over the warps of a row, the block's warps from `first` on; `slots` holds one float per warp of the block.  All threads of the
+// block call it.
+__device__ __forceinline__ float row_sum(float s, float* slots, int first, int row_warps) {
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
   if (row_warps == 1) return s;
-  const int warp = threadIdx.x >> 5, first = warp & ~(row_warps - 1);
-  if ((threadIdx.x & 31) == 0) slots[warp] = s;
+  if ((threadIdx.x & 31) == 0) slots[threadIdx.x >> 5] = s;
   __syncthreads();
   s = 0.f;
   for (int w = 0; w < row_warps; ++w) s += slots[first + w];
@@ -127,26 +124,30 @@ template <bool XF32, int RES, int OUT, bool VEC, int C>
 __global__ void __launch_bounds__(C == 4 ? 512 : 1024) norm_rms(const NormParams p) {
   __shared__ float slots[32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t row = blockIdx.x * ((blockDim.x >> 5) / p.row_warps) + warp / p.row_warps;
-  const int k0 = (warp & (p.row_warps - 1)) * (C * kF8Unit);
+  uint32_t block_row, row_warp;
+  p.row_warps.divmod(static_cast<uint32_t>(warp), block_row, row_warp);
+  const uint32_t row = blockIdx.x * p.block_rows + block_row;
+  const int k0 = static_cast<int>(row_warp) * (C * kF8Unit);
   const bool live = row < p.rows;
   const Strip<XF32, RES, OUT> at(p, row, k0, lane);
   pdl_wait();
   pdl_launch_dependents();
-  uint32_t raw_x[C][8], raw_r[C][8];
-#pragma unroll
-  for (int c = 0; c < C; ++c)
-    if (live && k0 + c * kF8Unit < p.K) load_operands<XF32, RES, VEC>(p, at.x, at.r, c, raw_x[c], raw_r[c]);
+  Unit<XF32, VEC> x[C];
+  Unit<RES == kF32, VEC> r[C];
+  if (live) {
+    units_read<XF32, VEC, C>(p.x, at.x, x);
+    if (RES != kNone) units_read<RES == kF32, VEC, C>(p.res, at.r, r);
+  }
   float2 h[C][4], s = make_float2(0.f, 0.f);
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     if (!live || k0 + c * kF8Unit >= p.K) break;
-    add_residual<XF32, RES>(raw_x[c], raw_r[c], h[c]);
+    add_residual<XF32, RES, VEC>(x[c], r[c], at, c, h[c]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) s = fma2(h[c][i], h[c][i], s);
     if (RES != kNone && p.sum) unit_store<RES == kF32, VEC>(h[c], p.sum, at.r, c, lane);
   }
-  const float rs = 1.f / sqrtf(row_sum(s.x + s.y, slots, p.row_warps) * p.inv_k + p.eps);
+  const float rs = 1.f / sqrtf(row_sum(s.x + s.y, slots, warp - static_cast<int>(row_warp), static_cast<int>(p.row_warps.d)) * p.inv_k + p.eps);
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     if (!live || k0 + c * kF8Unit >= p.K) break;
@@ -164,22 +165,25 @@ __global__ void __launch_bounds__(1024) norm_rms_long(const NormParams p) {
   pdl_wait();
   pdl_launch_dependents();
   float total = 0.f;
-  uint32_t raw_x[8], raw_r[8];
+  Unit<XF32, VEC> x[1];
+  Unit<RES == kF32, VEC> r[1];
   float2 h[4];
   for (int unit = threadIdx.x >> 5; unit < p.units; unit += 32) {
     const Strip<XF32, RES, OUT> at(p, row, unit * kF8Unit, lane);
-    load_operands<XF32, RES, VEC>(p, at.x, at.r, 0, raw_x, raw_r);
-    add_residual<XF32, RES>(raw_x, raw_r, h);
+    units_read<XF32, VEC, 1>(p.x, at.x, x);
+    if (RES != kNone) units_read<RES == kF32, VEC, 1>(p.res, at.r, r);
+    add_residual<XF32, RES, VEC>(x[0], r[0], at, 0, h);
     float2 s = make_float2(0.f, 0.f);   // (a lane adds up to 2^15 values for the longest rows: by units of eight first)
 #pragma unroll
     for (int i = 0; i < 4; ++i) s = fma2(h[i], h[i], s);
     total += s.x + s.y;
   }
-  const float rs = 1.f / sqrtf(row_sum(total, slots, 32) * p.inv_k + p.eps);
+  const float rs = 1.f / sqrtf(row_sum(total, slots, 0, 32) * p.inv_k + p.eps);
   for (int unit = threadIdx.x >> 5; unit < p.units; unit += 32) {
     const Strip<XF32, RES, OUT> at(p, row, unit * kF8Unit, lane);
-    load_operands<XF32, RES, VEC>(p, at.x, at.r, 0, raw_x, raw_r);
-    add_residual<XF32, RES>(raw_x, raw_r, h);
+    units_read<XF32, VEC, 1>(p.x, at.x, x);
+    if (RES != kNone) units_read<RES == kF32, VEC, 1>(p.res, at.r, r);
+    add_residual<XF32, RES, VEC>(x[0], r[0], at, 0, h);
     if (RES != kNone && p.sum) unit_store<RES == kF32, VEC>(h, p.sum, at.r, 0, lane);
     store_result<OUT, VEC>(h, rs, p, at, 0, lane);
   }
@@ -187,19 +191,19 @@ __global__ void __launch_bounds__(1024) norm_rms_long(const NormParams p) {
 
 template <bool XF32, int RES, int OUT, bool VEC>
 int launch_norm(NormParams p, cudaStream_t st) {
-  // Four units a warp when there are rows enough to fill the machine; a row alone is spread over as many warps as it has units.
+  // Four units a warp (two of unaligned rows, which take more registers) when there are rows enough to fill the machine; a row
+  // alone is spread over as many warps as it has units.
+  constexpr int kMost = VEC ? 4 : 2;
   const bool spread = p.rows <= static_cast<uint32_t>(num_sms());
-  const int want = spread ? p.units : (p.units + 3) / 4;
-  p.row_warps = 1;
-  while (p.row_warps < want && p.row_warps < 32) p.row_warps *= 2;
-  const int per_warp = (p.units + p.row_warps - 1) / p.row_warps;
-  const int warps = p.row_warps > 8 ? p.row_warps : 8;
-  const uint32_t per_block = static_cast<uint32_t>(warps / p.row_warps);
-  const dim3 grid((p.rows + per_block - 1) / per_block), block(static_cast<unsigned>(warps * 32));
-  void (*k)(NormParams) = per_warp == 1   ? norm_rms<XF32, RES, OUT, VEC, 1>
-                          : per_warp == 2 ? norm_rms<XF32, RES, OUT, VEC, 2>
-                          : p.row_warps <= 16 ? norm_rms<XF32, RES, OUT, VEC, 4>   // (then four units a warp suffice)
-                                              : norm_rms_long<XF32, RES, OUT, VEC>;
+  const int row_warps = std::min(spread ? p.units : (p.units + kMost - 1) / kMost, 32);
+  const int per_warp = (p.units + row_warps - 1) / row_warps;
+  p.row_warps.set(row_warps);
+  p.block_rows = std::max(8 / row_warps, 1);
+  const dim3 grid((p.rows + p.block_rows - 1) / p.block_rows), block(static_cast<unsigned>(row_warps * p.block_rows * 32));
+  void (*k)(NormParams) = norm_rms_long<XF32, RES, OUT, VEC>;
+  if (per_warp == 1) k = norm_rms<XF32, RES, OUT, VEC, 1>;
+  else if (per_warp == 2) k = norm_rms<XF32, RES, OUT, VEC, 2>;
+  else if (VEC && row_warps <= 16) k = norm_rms<XF32, RES, OUT, VEC, kMost>;   // (then four units a warp suffice)
   return launch_pdl(k, grid, block, 0, st, 1, p) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
 }
 
