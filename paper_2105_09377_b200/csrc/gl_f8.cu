@@ -575,24 +575,36 @@ dot_f8(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtens
 // Few rows of A: the weights take the 128-row side
 // ------------------------------------------------------------------------
 //
-// With at most 128 rows of A the product is bound by reading B (the weights) once.  Tiles of 128 rows of B, all rows of
-// A as the N side (BN = 16 to 128 of them), and K cut over the S blocks of a cluster so that the loads of all SMs are in
-// flight: the blocks' partial sums meet in distributed shared memory, added in rank order.  One tile per block, two
-// blocks per SM.  While the kernel that rounds A is still running the weights are on their way into L2.
+// With few rows of A the product is bound by reading B (the weights) once.  Tiles of 128 rows of B, BN rows of A (16 to 128) as the N
+// side, and K cut over the S blocks of a cluster so that the loads of all SMs are in flight: the blocks' partial sums meet in
+// distributed shared memory, added in rank order.  One tile per block, two blocks per SM.  While the kernel that makes A is
+// still running the first weights are on their way into L2.
+// Weights that come from HBM: 8192 x 8192 one row 13.3 us (67 MB: 5.1 TB/s, of which filling and emptying the machine takes 3 us),
+// 64 rows 15.8, 128 rows 18.7; 28672 x 8192 one row 36.4 us, 6.5 TB/s, the rate of a copy.
 //
-// At most kFuseRows rows (FUSED): the blocks round A themselves, each its own stretch of K, straight into operand order, while
-// the first weights are on their way: one launch.
-constexpr int kFuseRows = 4;
+// A few rows of a dense layer (FUSED): the blocks round A themselves, each its own stretch of K, straight into operand order, while
+// the first weights are on their way: one launch.  Five warps take four K blocks of a row at a time; up to two rounds of that cost
+// less than a launch of its own.  us fused / not, weights of 8192 x 8192 and 4096 x 14336 not in L2:
+//   K x O            1 row          2 rows         4 rows         5 rows         6 rows         8 rows
+//   1024 x 1024      3.5 / 4.5      3.5 / 4.4      3.6 / 4.6      3.6 / 4.6      4.3 / 4.6      4.3 / 4.6     (1, 1, 1, 1, 2, 2 rounds)
+//   3136 x 1000      4.1 / 5.0      4.1 / 5.0      4.1 / 5.1      4.1 / 5.2      4.8 / 5.2      4.8 / 5.1     (1, 1, 1, 1, 2, 2)
+//   4096 x 4096      6.3 / 6.7      6.3 / 6.8      6.6 / 7.0      6.7 / 7.0      7.4 / 7.1      8.2 / 7.2     (1, 1, 2, 2, 3, 4)
+//   8192 x 8192     13.7 / 15.4    14.4 / 15.6    15.5 / 15.7    15.7 / 15.7    16.5 / 15.9    17.9 / 15.9    (1, 2, 4, 4, 5, 7)
+//   4096 x 14336    13.1 / 14.5    13.7 / 14.5    14.9 / 14.8    15.3 / 14.8    15.9 / 14.8    17.2 / 14.8    (1, 2, 4, 4, 5, 7)
+constexpr int kFuseRows = 8;
+constexpr int kFuseBlocks = 16;   // K blocks of A that a block has room for
+constexpr int kFuseWarps = 5, kFuseRounds = 2;
 // K blocks that a block asks for before the kernel in front has ended.  More stand in the way of the rows of A behind them, and of
 // weights that are wanted sooner: one row, weights not in L2, 8192 x 8192: none 14.2 us, two 13.6, four 13.5, all sixteen 14.1;
 // 8192 x 28672: none to eight 37.5, all 53.8; 128 rows through 8192 x 8192: none 19.6, four 19.0, all 20.3.
 constexpr int kPrefetch = 4;
 constexpr int kJoinWarps = kF8Threads / 32;
-constexpr int kFuseBlocks = 16;   // K blocks of A that a block has room for
+// Eight rows of A a K block, 1024 bytes: the instruction's other eight columns read the block behind and are not used.
+constexpr int kXBlock = 8 * kKBytes;
 
 struct F8FewParams {
-  int M;
-  int64_t O;
+  int64_t M, O;
+  int tiles_o;            // tiles of 128 rows of B; a tile of rows of A goes with every one of them
   const void* x;          // FUSED: rows of A as they came
   int64_t K;
   int x_f32;
@@ -604,25 +616,26 @@ struct F8FewParams {
 // The S partial sums of a value in rank order.  A warp takes a column of 128 outputs, four a lane; rank r has the columns r, r + S, ..,
 // several of a warp's requested before the first is summed.
 template <int S>
-__device__ __forceinline__ void join_ranks(uint32_t part, int rank, int warp, int lane, int64_t o0, void* __restrict__ out, const F8FewParams& p) {
+__device__ __forceinline__ void join_ranks(uint32_t part, int rank, int warp, int lane, int64_t o0, int64_t m0, int rows, void* __restrict__ out,
+                                           const F8FewParams& p) {
   constexpr int kCols = 8 / S < 1 ? 1 : 8 / S;   // columns of a warp in flight
   const int64_t o = o0 + lane * 4;
-  for (int c0 = rank + warp * S; c0 < p.M; c0 += kCols * kJoinWarps * S) {
+  for (int c0 = rank + warp * S; c0 < rows; c0 += kCols * kJoinWarps * S) {
     float4 x[kCols][S];
 #pragma unroll
     for (int j = 0; j < kCols; ++j)
 #pragma unroll
       for (int from = 0; from < S; ++from) {
         const int c = c0 + j * kJoinWarps * S;
-        if (c < p.M)
+        if (c < rows)
           asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
                        : "=f"(x[j][from].x), "=f"(x[j][from].y), "=f"(x[j][from].z), "=f"(x[j][from].w)
                        : "r"(map_to_cta(part + c * 512 + lane * 16, from)));
       }
 #pragma unroll
     for (int j = 0; j < kCols; ++j) {
-      const int64_t c = c0 + j * kJoinWarps * S;
-      if (c >= p.M) break;
+      const int c = c0 + j * kJoinWarps * S;
+      if (c >= rows) break;
       float v[4] = {x[j][0].x, x[j][0].y, x[j][0].z, x[j][0].w};
 #pragma unroll
       for (int from = 1; from < S; ++from) { v[0] += x[j][from].x; v[1] += x[j][from].y; v[2] += x[j][from].z; v[3] += x[j][from].w; }
@@ -631,7 +644,7 @@ __device__ __forceinline__ void join_ranks(uint32_t part, int rank, int warp, in
         for (int i = 0; i < 4; ++i) v[i] = relu_keep_nan(v[i]);
       }
       if (p.out_bf16) {
-        uint16_t* to = static_cast<uint16_t*>(out) + c * p.O + o;
+        uint16_t* to = static_cast<uint16_t*>(out) + (m0 + c) * p.O + o;
         const uint32_t lo = pack_bf16x2(__float_as_uint(v[0]), __float_as_uint(v[1])), hi = pack_bf16x2(__float_as_uint(v[2]), __float_as_uint(v[3]));
         if ((p.O & 3) == 0) {
           if (o < p.O) *reinterpret_cast<uint2*>(to) = make_uint2(lo, hi);
@@ -642,7 +655,7 @@ __device__ __forceinline__ void join_ranks(uint32_t part, int rank, int warp, in
           if (o + 3 < p.O) to[3] = static_cast<uint16_t>(hi >> 16);
         }
       } else {
-        float* to = static_cast<float*>(out) + c * p.O + o;
+        float* to = static_cast<float*>(out) + (m0 + c) * p.O + o;
         if ((p.O & 3) == 0) {
           if (o < p.O) *reinterpret_cast<float4*>(to) = make_float4(v[0], v[1], v[2], v[3]);
         } else {
@@ -662,13 +675,13 @@ struct F8FewCfg {
   static constexpr int kStage = kStageA + kStageB;
   static constexpr int kScales = FUSED ? 512 : 1024;               // a scale tile (four K blocks) of each side
   static constexpr int kXTiles = kFuseBlocks / 4 + 1;              // FUSED: scale tiles that a stretch of K blocks touches
-  static constexpr int kXBytes = FUSED ? kFuseBlocks * BN * kKBytes + kXTiles * 512 : 0;
+  static constexpr int kXBytes = FUSED ? (kFuseBlocks + 1) * kXBlock + kXTiles * 512 : 0;
   static constexpr int kStages = (112 * 1024 - 1024 - 256 - kXBytes) / (kStage + kScales);
   static constexpr int kSmemBytes = kStages * (kStage + kScales) + kXBytes + 1024 + 256;
   static constexpr int kTmemCols = BN + 16 <= 32 ? 32 : BN + 16 <= 64 ? 64 : BN + 16 <= 128 ? 128 : 256;
   static constexpr int kSfBase = kTmemCols - 16;                   // two sets of four columns of each side
   static_assert(kStages >= 2 && kStages * kStage >= BN * 128 * 4, "partial sums fit in the ring");
-  static_assert(FUSED ? BN == 16 : true, "the blocks that round A keep it as 16 rows");
+  static_assert(!FUSED || BN == 16, "the instruction's columns are two groups of eight");
 };
 
 // Sixteen values of a row of A from element k on, zeros behind its end.
@@ -737,7 +750,9 @@ dot_f8_few(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = p.split > 1 ? static_cast<int>(cluster_ctarank()) : 0;
-  const int tile = static_cast<int>(blockIdx.x) / p.split;
+  const int unit = static_cast<int>(blockIdx.x) / p.split, xt = unit / p.tiles_o, tile = unit - xt * p.tiles_o;
+  const int64_t m0 = static_cast<int64_t>(xt) * BN;
+  const int rows = static_cast<int>(min(static_cast<int64_t>(BN), p.M - m0));
   // K blocks of this rank, as even as they go
   const int kb0 = static_cast<int>(static_cast<int64_t>(p.kblocks) * rank / p.split);
   const int kb1 = static_cast<int>(static_cast<int64_t>(p.kblocks) * (rank + 1) / p.split);
@@ -747,7 +762,7 @@ dot_f8_few(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
   if (threadIdx.x == 0) {
     for (int s = 0; s < Cfg::kStages; ++s) { mbar_init(bar_full + 8 * s, FUSED ? 1 : 2); mbar_init(bar_empty + 8 * s, 1); }
     mbar_init(bar_done, 1);
-    mbar_init(bar_x, 5);   // warps 2 to 6
+    mbar_init(bar_x, kFuseWarps);   // warps 2 to 6
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -767,16 +782,16 @@ dot_f8_few(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
   if (FUSED && warp >= 2) {
     // a warp takes four K blocks of a row at a time, eight lanes each
     const int quads = (kb1 - kb0 + 3) / 4;
-    unsigned char* xscale = gen_x + kFuseBlocks * BN * kKBytes;
+    unsigned char* xscale = gen_x + (kFuseBlocks + 1) * kXBlock;
     int m = 0, g = warp - 2;
     while (true) {
       while (g >= quads) { g -= quads; ++m; }
-      if (m >= p.M) break;
+      if (m >= rows) break;
       const int b = g * 4 + (lane >> 3), kb = kb0 + b;
       float x[16];
       load_row_values(p, m, static_cast<int64_t>(kb) * kF8Block + (lane & 7) * 16, x);
-      round_row_block(x, gen_x + b * (BN * kKBytes), xscale + ((kb >> 2) - (kb0 >> 2)) * 512 + m * 16 + (kb & 3), m, lane & 7, kb < kb1);
-      g += 5;
+      round_row_block(x, gen_x + b * kXBlock, xscale + ((kb >> 2) - (kb0 >> 2)) * 512 + m * 16 + (kb & 3), m, lane & 7, kb < kb1);
+      g += kFuseWarps;
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
@@ -796,8 +811,8 @@ dot_f8_few(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
           tma_load_2d(stage, &map_w, kb * kKBytes, tile * kTile, full);
           if (with_scales) tma_load_3d(sc, &map_sw, 0, kb >> 2, tile, full);
         } else {
-          tma_load_2d(stage + Cfg::kStageA, &map_x, kb * kKBytes, 0, full);
-          if (with_scales) tma_load_3d(sc + 512, &map_sx, 0, kb >> 2, 0, full);
+          tma_load_2d(stage + Cfg::kStageA, &map_x, kb * kKBytes, static_cast<int>(m0), full);
+          if (with_scales) tma_load_3d(sc + 512, &map_sx, 0, kb >> 2, static_cast<int>(m0 >> 7), full);
         }
       }
       if (++s == Cfg::kStages) { s = 0; ph ^= 1u; }
@@ -806,13 +821,13 @@ dot_f8_few(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
     const bool leader = elect_one();
     const uint64_t desc_w0 = make_desc(tiles, 16, 1024, 2), desc_x0 = make_desc(FUSED ? xs : tiles + Cfg::kStageA, 16, 1024, 2);
     const uint64_t desc_s0 = make_desc(scales, 16, 128, 0);
-    const uint64_t desc_sx0 = make_desc(FUSED ? xs + kFuseBlocks * BN * kKBytes : scales + 512, 16, 128, 0);
+    const uint64_t desc_sx0 = make_desc(FUSED ? xs + (kFuseBlocks + 1) * kXBlock : scales + 512, 16, 128, 0);
     uint32_t s = 0, ph = 0, sets = 0, sfw = 0;
     bool ok = !FUSED || mbar_wait(bar_x, 0, abort_flag);
     for (int kb = kb0; kb < kb1 && ok; ++kb) {
       if (!mbar_wait(bar_full + 8 * s, ph, abort_flag)) { ok = false; break; }
       tc_fence_after();
-      const uint64_t off = (s * Cfg::kStage) >> 4, xoff = FUSED ? ((kb - kb0) * (BN * kKBytes)) >> 4 : off;
+      const uint64_t off = (s * Cfg::kStage) >> 4, xoff = FUSED ? ((kb - kb0) * kXBlock) >> 4 : off;
       if (kb == kb0 || (kb & 3) == 0) {
         sfw = tmem_base + Cfg::kSfBase + (sets & 1u) * 4;
         ++sets;
@@ -833,43 +848,31 @@ dot_f8_few(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
     if (ok && leader) tc_commit(bar_done);
   }
   float* part = reinterpret_cast<float*>(gen_tiles);   // [BN][128]: every MMA has read the ring when bar_done flips
-  const int q = warp & 3;
-  const int64_t o = static_cast<int64_t>(tile) * kTile + q * 32 + lane;
-  const bool epilogue = warp >= 2 && warp < 6;
-  if (epilogue) {
+  if (warp >= 2 && warp < 6) {
+    const int q = warp & 3;
     const bool ok = mbar_wait(bar_done, 0, abort_flag);
     tc_fence_after();
     if (ok) {
 #pragma unroll 1
       for (int c = 0; c < BN; c += 16) {
-        if (c >= p.M) break;
+        if (c >= rows) break;
         uint32_t r[16];
         tc_load_16cols(tmem_base + (static_cast<uint32_t>(q * 32) << 16) + c, r);
-        if (p.split > 1) {
 #pragma unroll
-          for (int j = 0; j < 16; ++j) part[(c + j) * 128 + q * 32 + lane] = __uint_as_float(r[j]);
-        } else if (o < p.O) {
-#pragma unroll
-          for (int j = 0; j < 16; ++j)
-            if (c + j < p.M) {
-              const float v = p.relu ? relu_keep_nan(__uint_as_float(r[j])) : __uint_as_float(r[j]);
-              if (p.out_bf16) static_cast<uint16_t*>(out)[(c + j) * p.O + o] = f32_to_bf16(v);
-              else static_cast<float*>(out)[(c + j) * p.O + o] = v;
-            }
-        }
+        for (int j = 0; j < 16; ++j) part[(c + j) * 128 + q * 32 + lane] = __uint_as_float(r[j]);
       }
     }
     tc_fence_before();
   }
-  if (p.split > 1) {
-    __syncwarp();
-    cluster_sync_all();
-    const int64_t o0 = static_cast<int64_t>(tile) * kTile;
-    switch (p.split) {
-      case 2: join_ranks<2>(smem_u32(part), rank, warp, lane, o0, out, p); break;
-      case 4: join_ranks<4>(smem_u32(part), rank, warp, lane, o0, out, p); break;
-      default: join_ranks<8>(smem_u32(part), rank, warp, lane, o0, out, p); break;
-    }
+  __syncwarp();
+  if (p.split > 1) cluster_sync_all();
+  else __syncthreads();
+  const int64_t o0 = static_cast<int64_t>(tile) * kTile;
+  switch (p.split) {
+    case 1: join_ranks<1>(smem_u32(part), rank, warp, lane, o0, m0, rows, out, p); break;
+    case 2: join_ranks<2>(smem_u32(part), rank, warp, lane, o0, m0, rows, out, p); break;
+    case 4: join_ranks<4>(smem_u32(part), rank, warp, lane, o0, m0, rows, out, p); break;
+    default: join_ranks<8>(smem_u32(part), rank, warp, lane, o0, m0, rows, out, p); break;
   }
   __syncwarp();
   if (*abort_flag) {   // copies in flight land before the block leaves
@@ -1004,6 +1007,23 @@ struct FewPlanF8 {
   int grid;
 };
 
+// Blocks that share a tile's K.  Half the machine is filled as long as a rank keeps two K blocks, the rest as long as it keeps four
+// (eight for clusters of eight, which the hardware then packs two to an SM beside empty ones), and a second block per SM where it
+// keeps sixteen: joining costs 1 to 3 us.  us at half / at this many / at twice as many ranks: 64 x 1024 x 1024 4.7 / 4.4 / 4.8;
+// 64 x 2048 x 2048 5.4 / 4.9 / 5.7; 128 x 4096 x 4096 - / 9.8 / 11.9; 1 x 8192 x 8192 14.4 / 13.4 / -; 256 x 4096 x 1024 - / 7.1 / 8.9;
+// 512 x 8192 x 2048 16.8 / 15.5 / -.
+int few_split(int64_t tiles, int kblocks) {
+  int split = 1;
+  while (split < 8) {
+    const int64_t blocks = tiles * split * 2;
+    const int left = kblocks / (split * 2);   // K blocks of a rank
+    const int need = 2 * blocks <= num_sms() ? 2 : blocks <= num_sms() ? (split == 4 ? 8 : 4) : blocks <= 2 * num_sms() ? 16 : INT32_MAX;
+    if (left < need) break;
+    split *= 2;
+  }
+  return split;
+}
+
 // `FUSED`: A is still to be rounded, by the product's own blocks.
 template <int BN, bool FUSED>
 int plan_few(const F8Operand& a, const F8Operand& b, void* out, uint32_t flags, FewPlanF8* t) {
@@ -1017,7 +1037,7 @@ int plan_few(const F8Operand& a, const F8Operand& b, void* out, uint32_t flags, 
     attr_set[dev].store(true, std::memory_order_release);
   }
   F8FewParams& p = t->p;
-  p.M = static_cast<int>(a.v.rows);
+  p.M = a.v.rows;
   p.O = b.v.rows;
   p.x = nullptr;
   p.K = a.v.K;
@@ -1025,11 +1045,11 @@ int plan_few(const F8Operand& a, const F8Operand& b, void* out, uint32_t flags, 
   k_steps(a.v.K, &p.kblocks, &p.last_steps);
   p.relu = (flags & GL_EPILOGUE_RELU) ? 1 : 0;
   p.out_bf16 = (flags & GL_OUT_BF16) ? 1 : 0;
-  if (b.v.rt > (1 << 27)) return GL_ERR_UNSUPPORTED;
-  const int tiles = static_cast<int>(b.v.rt);
-  // as many ranks as still leave every one a K block and all blocks resident at once (two per SM)
-  p.split = 1;
-  while (p.split < 8 && p.split * 2 <= p.kblocks && tiles * p.split * 2 <= 2 * num_sms()) p.split *= 2;
+  const int64_t all = b.v.rt * ((a.v.rows + BN - 1) / BN);
+  if (all > (1 << 27)) return GL_ERR_UNSUPPORTED;
+  const int tiles = static_cast<int>(all);
+  p.tiles_o = static_cast<int>(b.v.rt);
+  p.split = few_split(tiles, p.kblocks);
   t->out = out;
   t->grid = tiles * p.split;
   if (!encode_codes(&t->mw, b, kTile) || !encode_scales(&t->msw, b)) return GL_ERR_CUDA;
@@ -1076,11 +1096,17 @@ int check_product(const gl_ap* out, int a_access, const int64_t* a_shape, int a_
 template <typename Pre>
 int product(const F8Operand& a, const F8Operand& b, gl_ap* out, uint32_t flags, cudaStream_t st, Pre&& pre) {
   if (!driver_api().ok) return GL_ERR_CUDA;
-  // Up to 128 rows: the weights as the 128-row side, K cut over clusters.
   if (a.v.rows <= 16) return product_few<16>(a, b, out, flags, st, pre);
   if (a.v.rows <= 32) return product_few<32>(a, b, out, flags, st, pre);
   if (a.v.rows <= 64) return product_few<64>(a, b, out, flags, st, pre);
-  if (a.v.rows <= 128) return product_few<128>(a, b, out, flags, st, pre);
+  // More rows: K is cut over clusters where there are few tiles for its length, and a second block per SM saves a round of up to
+  // 128 rows.  us cut / on the tiles below: 128 x 1024 x 1024 5.4 / 5.0; 128 x 2048 x 512 5.7 / 6.7; 512 x 2048 x 2048 7.1 / 7.2;
+  // 128 x 4096 x 4096 9.7 / 12.0, 256 rows 11.9 / 12.2, 384 rows 13.7 / 12.5; 128 x 4096 x 14336 16.9 / 14.9; 256 x 8192 x 8192
+  // 21.8 / 22.2, 384 rows 33 / 28; 512 x 14336 x 4096 32.2 / 32.9; 128 x 8192 x 28672 45 / 48, 129 rows 75 / 56.
+  const int64_t tiles128 = ((a.v.rows + 127) / 128) * b.v.rt;
+  if ((2 * tiles128 <= num_sms() && a.v.nb >= 16) || (tiles128 <= num_sms() && a.v.nb >= 64) ||
+      (a.v.rows <= 128 && tiles128 > num_sms() && tiles128 <= 2 * num_sms()))
+    return product_few<128>(a, b, out, flags, st, pre);
   // 256 x 256 tiles on pairs of SMs move half the bytes per flop of 128 x 128 tiles, but there are a quarter as many.
   TilePlanF8 t;
   const auto tiles = [&](int64_t side) { return ((a.v.rows + side - 1) / side) * ((b.v.rows + side - 1) / side); };
@@ -1204,7 +1230,9 @@ int gl_dense_f8(const gl_ap* a0, const gl_f8* a1, gl_ap* out, uint32_t flags, vo
     FewPlanF8 t;
     rc = plan_few<16, true>(a, b, out->data, flags, &t);
     if (rc) return rc;
-    if ((t.p.kblocks + t.p.split - 1) / t.p.split <= kFuseBlocks) {
+    const int blocks = (t.p.kblocks + t.p.split - 1) / t.p.split;
+    const int items = static_cast<int>(a.v.rows) * ((blocks + 3) / 4);
+    if (blocks <= kFuseBlocks && items <= kFuseWarps * kFuseRounds) {
       t.p.x = a0->data;
       t.p.x_f32 = a0->dtype == GL_F32;
       return run_few<16, true>(t, st);
