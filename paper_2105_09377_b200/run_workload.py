@@ -2,6 +2,7 @@
 
     python -m paper_2105_09377_b200.run_workload --workload conv3x3_56x56x64 --layout nhwc --iters 3
     python -m paper_2105_09377_b200.run_workload --workload decoder4_8x128_1024 --iters 64
+    python -m paper_2105_09377_b200.run_workload --workload decoder8_8x128_1024 --iters 64
 
 Prints the mean time per call (CUDA events).  Meant for profilers and quick
 checks; the benchmark proper is bench.py.
@@ -189,9 +190,49 @@ class Decoder4:
         return {"qkv": qkv, "seen": seen, "y": y, "hidden": hidden, "out": dense(hidden, self.down)}
 
 
-def run_decoder4(cfg, device, tokens: int):
+class Decoder8:
+    """`synth.Decoder8Case` on the device: weights rounded to F8 once, keys and values in the 4-bit pages.  Every norm hands its
+    result on in 8 bits, so no product rounds its operand but the two whose operand is another's result."""
+
+    def __init__(self, cfg, device, seed=None):
+        self.cfg = cfg
+        values = cfg.inputs(synth.config_seed(7) if seed is None else seed)
+        self.prompt = _bf16(values[0], device)
+        self.qkv, self.back, self.up, self.down = (gl.gl_f8_quantize(gl.AccessPattern(_bf16(w, device), 1)) for w in values[1:5])
+        self.norms = [gl.AccessPattern(_bf16(w, device), 0) for w in values[5:]]
+        per = -(-cfg.capacity // cfg.page_tokens)
+        self.cache = gl.cache4_empty(cfg.batch * per, cfg.kv_heads, cfg.page_tokens, cfg.head_dim, device)
+        self.table = torch.arange(cfg.batch * per, dtype=torch.int32, device=device).view(cfg.batch, per)
+        self.lengths = torch.zeros(cfg.batch, dtype=torch.int32, device=device)
+        self.plan = gl.rotary_plan(cfg.head_dim // 2, cfg.base)
+
+    def step(self, x):
+        """x bf16 [batch, tokens, width], the tokens that come next; returns every stage, the last one the result."""
+        cfg, ap, flags = self.cfg, gl.AccessPattern, gl.GL_OUT_BF16
+        b, t = x.shape[:2]
+        first = gl.gl_compute_norm_rms_f8(ap(x, 2), self.norms[0], cfg.eps)
+        qkv = gl.gl_cartesian_dot_f8(first, self.qkv, flags=flags).tensor.view(b, t, -1, cfg.head_dim)
+        raw = qkv.clone()                                                    # (a stage to look at: qkv is turned where it is)
+        positions = self.lengths[:, None] + torch.arange(t, dtype=torch.int32, device=x.device)
+        self.lengths += t
+        q, k, v = qkv.split([cfg.heads, cfg.kv_heads, cfg.kv_heads], 2)      # parts of one result, read where they are
+        both = ap(qkv[:, :, : cfg.heads + cfg.kv_heads], 3)
+        gl.gl_compute_rotate(both, self.plan, positions, both)
+        gl.gl_cache4_append(self.cache, k, v, self.table, self.lengths)
+        seen = gl.gl_attend_cache4(ap(q, 3), self.cache, self.table, self.lengths, flags=flags).tensor
+        y = gl.gl_dense_f8(ap(seen.view(x.shape), 2), self.back, flags=flags).tensor
+        total = torch.empty_like(x)
+        second = gl.gl_compute_norm_rms_f8(ap(y, 2), self.norms[1], cfg.eps, ap(x, 2), ap(total, 2))
+        hidden = gl.gl_cartesian_dot_f8(second, self.up, flags=flags | gl.GL_EPILOGUE_RELU).tensor
+        down = gl.gl_dense_f8(ap(hidden, 2), self.down, flags=flags).tensor
+        out = gl.gl_compute_norm_rms(ap(down, 2), self.norms[2], cfg.eps, ap(total, 2)).tensor
+        return {"first": first, "raw": raw, "qkv": qkv, "seen": seen, "y": y, "total": total, "second": second, "hidden": hidden,
+                "down": down, "out": out}
+
+
+def run_decoder(cfg, device, tokens: int):
     """The prompt, then `tokens` single tokens, each the layer's last result; returns us per token."""
-    layer = Decoder4(cfg, device)
+    layer = (Decoder8 if isinstance(cfg, synth.Decoder8Case) else Decoder4)(cfg, device)
     x = layer.step(layer.prompt)["out"][:, -1:].contiguous()
     e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
     x = layer.step(x)["out"]
@@ -206,7 +247,8 @@ def run_decoder4(cfg, device, tokens: int):
 
 def main():
     table = workloads()
-    table[synth.DECODER4.name] = synth.DECODER4
+    decoders = {c.name: c for c in (synth.DECODER4, synth.DECODER8)}
+    table.update(decoders)
     ap = argparse.ArgumentParser()
     ap.add_argument("--workload", required=True, choices=sorted(table))
     ap.add_argument("--layout", default="nhwc", choices=["nhwc", "nchw", "rewritten"])
@@ -218,10 +260,10 @@ def main():
     args = ap.parse_args()
     device = torch.device("cuda", 0)
     torch.cuda.set_device(device)
-    if args.workload == synth.DECODER4.name:
-        cfg = synth.DECODER4
+    if args.workload in decoders:
+        cfg = decoders[args.workload]
         tokens = min(args.iters, cfg.capacity - cfg.prompt - 1)
-        us = run_decoder4(cfg, device, tokens)
+        us = run_decoder(cfg, device, tokens)
         status = gl.gl_poll_device_status()
         print("%s: %.2f us per token of %d sequences (%d tokens after a prompt of %d), status %d"
               % (cfg.name, us, cfg.batch, tokens, cfg.prompt, status))

@@ -299,5 +299,21 @@ class Decoder4Case:
 DECODER4 = Decoder4Case("decoder4_8x128_1024", 8, 128, 16, 4, 64, 4096, 64, 512)
 
 
+@dataclass(frozen=True)
+class Decoder8Case(Decoder4Case):
+    """The same layer as it stands in a stack, its products in 8 bits: a norm in front of the first dense layer and one, which
+    adds the residual, in front of `hidden`; queries and keys turned by their positions; a last norm that adds the second
+    residual."""
+    eps: float = 1e-5
+    base: float = 10000.0
+
+    def inputs(self, seed: int):
+        """Decoder4Case's, then the weights of the three norms."""
+        return super().inputs(seed) + tuple(bf16_round(1.0 + normal(seed, 6 + i, (self.width,), 0.1)) for i in range(3))
+
+
+DECODER8 = Decoder8Case("decoder8_8x128_1024", 8, 128, 16, 4, 64, 4096, 64, 512)
+
+
 def config_seed(config_index: int) -> int:
     return BASE_SEED + config_index
