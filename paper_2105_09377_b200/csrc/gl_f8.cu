@@ -248,7 +248,9 @@ __device__ __forceinline__ float relu_keep_nan(float v) { return v < 0.f ? 0.f :
 
 constexpr int kTile = 128;           // rows of A per block
 constexpr int kKBytes = 128;         // bytes of a row per K block: one block of 128 values, one 128-byte swizzle row
-constexpr int kF8Threads = 224;      // warp 0 TMA (A), warp 1 MMA, warps 2-5 epilogue, warp 6 TMA (B)
+constexpr int kF8Threads = 352;      // warp 0 TMA (A), warp 1 MMA, warps 2-9 epilogue, warp 10 TMA (B)
+constexpr int kEpiWarps = 8;         // two per quarter of the rows, taking turns at the columns
+constexpr int kFewThreads = 224;     // warp 0 TMA (weights), warp 1 MMA, warps 2-5 sums (2-6 round A), warp 6 TMA (A)
 
 // Tile rows of a band, in 256s.  What a band of pairs reads at a time is its rows of A and a few columns of B: 16 rows by 4 or 5
 // columns for 74 pairs.  Walked row by row, the whole of B passes for every two rows of tiles, and what does not come from near
@@ -281,7 +283,7 @@ struct F8Cfg {
   static constexpr int kStage = kStageA + kStageB;
   // A scale tile holds four K blocks: every fourth stage brings one per 128 rows of A and of B.
   static constexpr int kScaleA = 512, kScaleB = (BN / 128) * 512, kScales = kScaleA + kScaleB;
-  static constexpr int kEpiBytes = 4 * 2 * 4096;
+  static constexpr int kEpiBytes = kEpiWarps * 4096;
   static constexpr int kStages = (232448 - kEpiBytes - 1024 - 256) / (kStage + kScales);
   static constexpr int kSmemBytes = kStages * (kStage + kScales) + kEpiBytes + 1024 + 256;
   // Tensor memory (512 columns): two sets of scales in the last kSfCols, two accumulators of BN columns before them.
@@ -291,6 +293,47 @@ struct F8Cfg {
   static constexpr int kAcc1 = 2 * BN <= kSfBase ? BN : kSfBase - BN;
   static constexpr bool kOverlap = kAcc1 < BN;
 };
+
+// Up to 32 rows that the epilogue has staged (128 bytes a row, 16-byte pieces exchanged as the 128-byte swizzle does) to rows of O
+// results that are no multiples of 16 bytes: row by row, neighbouring lanes on neighbouring columns, sixteen rows read from shared
+// memory before the first is stored.  KIND 0: fp32, 1: bf16 in whole pairs (O even), 2: bf16 one by one.
+template <int KIND>
+__device__ __forceinline__ void store_rows(uint32_t buf, char* to, int64_t O, int rows, int cols, int lane) {
+  const int col = KIND ? 2 * lane : lane;
+  const bool one = col < cols, two = KIND == 2 && col + 1 < cols;
+  const int64_t pitch = O * (KIND ? 2 : 4);
+  const uint32_t from = buf + (lane & 3) * 4;
+  to += col * (KIND ? 2 : 4);
+#pragma unroll
+  for (int row0 = 0; row0 < 32; row0 += 16) {
+    uint32_t v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v[i]) : "r"(from + (row0 + i) * 128 + (((lane >> 2) ^ (i & 7)) << 4)));
+    if (row0 + 16 <= rows) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i, to += pitch) {
+        if (KIND < 2) {
+          if (one) *reinterpret_cast<uint32_t*>(to) = v[i];
+        } else {
+          if (one) *reinterpret_cast<uint16_t*>(to) = static_cast<uint16_t>(v[i]);
+          if (two) *reinterpret_cast<uint16_t*>(to + 2) = static_cast<uint16_t>(v[i] >> 16);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i, to += pitch) {
+        const bool in = row0 + i < rows;
+        if (KIND < 2) {
+          if (one && in) *reinterpret_cast<uint32_t*>(to) = v[i];
+        } else {
+          if (one && in) *reinterpret_cast<uint16_t*>(to) = static_cast<uint16_t>(v[i]);
+          if (two && in) *reinterpret_cast<uint16_t*>(to + 2) = static_cast<uint16_t>(v[i] >> 16);
+        }
+      }
+    }
+  }
+}
 
 template <int BN, int CTAS>
 __global__ void __launch_bounds__(kF8Threads, 1)
@@ -324,7 +367,7 @@ dot_f8(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtens
   }
   if (threadIdx.x == 0) {
     for (int s = 0; s < Cfg::kStages; ++s) { mbar_init(bar_full + 8 * s, 2); mbar_init(bar_empty + 8 * s, 1); }
-    for (int a = 0; a < 2; ++a) { mbar_init(bar_tfull + 8 * a, 1); mbar_init(bar_tempty + 8 * a, 4 * CTAS); }
+    for (int a = 0; a < 2; ++a) { mbar_init(bar_tfull + 8 * a, 1); mbar_init(bar_tempty + 8 * a, kEpiWarps * CTAS); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -348,8 +391,8 @@ dot_f8(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtens
   pdl_wait();
   pdl_launch_dependents();
 
-  if (warp == 0 || warp == 6) {
-    // ---------------- TMA producers: warp 0 stages A and its scales, warp 6 stages B and its scales ----------------
+  if (warp == 0 || warp == 10) {
+    // ---------------- TMA producers: warp 0 stages A and its scales, warp 10 stages B and its scales ----------------
     const bool load_a = warp == 0;
     const bool leader = elect_one();
     uint32_t s = 0, ph = 0;
@@ -447,11 +490,11 @@ dot_f8(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtens
     }
   } else {
     // ---------------- epilogue: TMEM -> registers -> (shared memory -> TMA store | global) ----------------
-    const int q = warp & 3;
+    const int q = warp & 3, turn = (warp - 2) >> 2;
     const bool leader = elect_one();
-    uint32_t tile_it = 0, chunk_it = 0;
+    uint32_t tile_it = 0;
     bool ok = true;
-    const uint32_t stage_buf = epi_base + q * 8192;
+    const uint32_t buf = epi_base + (warp - 2) * 4096;
     const int cstep = p.out_bf16 ? 64 : 32;
     const int nchunks = BN / cstep;
     for (int u = unit0; u < num_tiles && ok; u += unit_step, ++tile_it) {
@@ -464,9 +507,9 @@ dot_f8(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtens
       const uint32_t taddr = tmem_base + (acc ? Cfg::kAcc1 : 0) + (static_cast<uint32_t>(q * 32) << 16);
       const int64_t m0 = static_cast<int64_t>(tm) * kTile + q * 32;
 #pragma unroll 1
-      for (int i = 0; i < nchunks; ++i) {
+      for (int i = turn; i < nchunks; i += 2) {
         // the columns that two overlapping accumulators share go first: the last ones of the first, the first ones
-        // of the second
+        // of the second (all in the first chunk: the warps of the second turn give theirs back with their first)
         const int c = (Cfg::kOverlap && acc == 0 ? nchunks - 1 - i : i) * cstep;
         const int64_t n0 = static_cast<int64_t>(tn) * BN + c;
         uint32_t r[32];
@@ -487,7 +530,7 @@ dot_f8(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtens
             r[16 + j] = pack_bf16x2(__float_as_uint(a), __float_as_uint(b));
           }
         }
-        if (i == (Cfg::kOverlap ? 0 : nchunks - 1)) {
+        if (Cfg::kOverlap ? i == turn : i + 2 >= nchunks) {
           tc_fence_before();
           __syncwarp();
           if (lane == 0) {
@@ -496,9 +539,7 @@ dot_f8(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtens
           }
         }
         if (n0 >= p.O) continue;   // uniform across the warp
-        const uint32_t buf = stage_buf + (chunk_it & 1u) * 4096;
-        ++chunk_it;
-        if (p.tma_store && leader) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+        if (p.tma_store && leader) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
         __syncwarp();
 #pragma unroll
         for (int j = 0; j < 8; ++j)
@@ -517,38 +558,12 @@ dot_f8(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtens
             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
           }
         } else {
-          // rows that are no multiples of 16 bytes: row by row, neighbouring lanes on neighbouring columns, eight rows read
-          // from shared memory before the first is stored
           __syncwarp();
           const int rows = static_cast<int>(min(static_cast<int64_t>(32), p.M - m0));
-          const int cols = static_cast<int>(min(static_cast<int64_t>(cstep), p.O - n0)), col = p.out_bf16 ? 2 * lane : lane;
-          const bool one = col < cols, two = col + 1 < cols;
-          const int64_t first = m0 * p.O + n0 + col;
-          for (int row0 = 0; row0 < rows; row0 += 8) {
-            uint32_t v[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v[i]) : "r"(buf + (row0 + i) * 128 + (((lane >> 2) ^ i) << 4) + (lane & 3) * 4));
-            if (p.out_bf16) {
-              uint16_t* to = static_cast<uint16_t*>(out) + first + row0 * p.O;
-              if ((p.O & 1) == 0) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                  if (one && row0 + i < rows) *reinterpret_cast<uint32_t*>(to + i * p.O) = v[i];   // (O even: whole pairs)
-              } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                  if (one && row0 + i < rows) to[i * p.O] = static_cast<uint16_t>(v[i]);
-                  if (two && row0 + i < rows) to[i * p.O + 1] = static_cast<uint16_t>(v[i] >> 16);
-                }
-              }
-            } else {
-              float* to = static_cast<float*>(out) + first + row0 * p.O;
-#pragma unroll
-              for (int i = 0; i < 8; ++i)
-                if (one && row0 + i < rows) to[i * p.O] = __uint_as_float(v[i]);
-            }
-          }
+          const int cols = static_cast<int>(min(static_cast<int64_t>(cstep), p.O - n0));
+          if (!p.out_bf16) store_rows<0>(buf, static_cast<char*>(out) + (m0 * p.O + n0) * 4, p.O, rows, cols, lane);
+          else if (p.O & 1) store_rows<2>(buf, static_cast<char*>(out) + (m0 * p.O + n0) * 2, p.O, rows, cols, lane);
+          else store_rows<1>(buf, static_cast<char*>(out) + (m0 * p.O + n0) * 2, p.O, rows, cols, lane);
         }
       }
     }
@@ -598,7 +613,7 @@ constexpr int kFuseWarps = 5, kFuseRounds = 2;
 // weights that are wanted sooner: one row, weights not in L2, 8192 x 8192: none 14.2 us, two 13.6, four 13.5, all sixteen 14.1;
 // 8192 x 28672: none to eight 37.5, all 53.8; 128 rows through 8192 x 8192: none 19.6, four 19.0, all 20.3.
 constexpr int kPrefetch = 4;
-constexpr int kJoinWarps = kF8Threads / 32;
+constexpr int kJoinWarps = kFewThreads / 32;
 // Eight rows of A a K block, 1024 bytes: the instruction's other eight columns read the block behind and are not used.
 constexpr int kXBlock = 8 * kKBytes;
 
@@ -731,7 +746,7 @@ __device__ __forceinline__ void round_row_block(const float (&x)[16], unsigned c
 }
 
 template <int BN, bool FUSED>
-__global__ void __launch_bounds__(kF8Threads, 2)
+__global__ void __launch_bounds__(kFewThreads, 2)
 dot_f8_few(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
            const __grid_constant__ CUtensorMap map_sw, const __grid_constant__ CUtensorMap map_sx, void* __restrict__ out,
            const F8FewParams p) {
@@ -1060,7 +1075,7 @@ int plan_few(const F8Operand& a, const F8Operand& b, void* out, uint32_t flags, 
 
 template <int BN, bool FUSED>
 int run_few(const FewPlanF8& t, cudaStream_t st) {
-  return launch_pdl(dot_f8_few<BN, FUSED>, dim3(static_cast<unsigned>(t.grid)), dim3(kF8Threads), F8FewCfg<BN, FUSED>::kSmemBytes, st,
+  return launch_pdl(dot_f8_few<BN, FUSED>, dim3(static_cast<unsigned>(t.grid)), dim3(kFewThreads), F8FewCfg<BN, FUSED>::kSmemBytes, st,
                     t.p.split, t.mw, t.mx, t.msw, t.msx, t.out, t.p) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
 }
 
