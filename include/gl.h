@@ -22,8 +22,8 @@
  *     also owns outputs and workspaces.  `out->shape`, `out->ndim`,
  *     `out->access_ndim` and `out->dtype` must already equal what the matching
  *     gl_shape_* call returns, otherwise GL_ERR_SHAPE / GL_ERR_DTYPE.
- *   - Inputs are read-only and must not overlap outputs (gl_compute_relu may
- *     run in place; a gl_cache4 is what gl_cache4_append writes).  Data pointers must be 16-byte aligned (GL_ERR_ALIGN).
+ *   - Inputs are read-only and must not overlap outputs (gl_compute_relu, gl_compute_rotate and
+ *     gl_compute_norm_rms may run in place; a gl_cache4 is what gl_cache4_append writes).  Data pointers must be 16-byte aligned (GL_ERR_ALIGN).
  *   - There is no CPU fallback: a combination the kernels do not cover
  *     returns GL_ERR_UNSUPPORTED.
  *   - Calls are re-entrant from several host threads.
@@ -366,7 +366,7 @@ GL_API size_t gl_attend_cache4_workspace(const gl_ap* q, const gl_cache4* cache)
  *   data:  gl_f8_data_bytes() bytes; one row per item of ceil(K/16)*16 bytes, codes past K are zero.
  *   scale: gl_f8_scale_bytes() bytes; tiles of 128 rows x 4 blocks, 512 bytes each, row tiles outermost; row r and
  *          block b of a tile at byte (r % 32) * 16 + (r / 32) * 4 + b.
- * Both device pointers are 16-byte aligned.  Size limits (else GL_ERR_UNSUPPORTED): fewer than 2^31 - 256 rows, K <= 2^30,
+ * Both device pointers are 16-byte aligned.  Size limits (else GL_ERR_UNSUPPORTED): fewer than 2^31 - 256 rows, K <= 2^28,
  * rows * (ceil(K/128) + 1) < 2^31. */
 typedef struct {
   void* data;
@@ -412,7 +412,8 @@ GL_API size_t gl_dense_f8_workspace(const gl_ap* a0, const gl_f8* a1);
  * residual) of the same shape and of one type, GL_F32 or GL_BF16, which may differ from x's; `weight` (NULL: ones)
  * ((),(c..)), GL_F32 or GL_BF16; eps >= 0 and finite.  out: the shape of x, GL_F32, GL_BF16 or F8.  The norm is that of the
  * unrounded h, in fp32 throughout; squares have to stay in fp32's range.  `sum` may be `residual` itself, or x where the
- * types agree, and `out` may be x (or `residual`, if that is not `sum`) where the types agree; other overlaps are not allowed.
+ * types agree, and `out` may be x or `residual`, unless that is `sum`, where the types agree; other overlaps are not allowed
+ * (`out` and `sum` in one place: GL_ERR_UNSUPPORTED).
  * Size limits as for F8.  Results repeat bit for bit. */
 GL_API int gl_compute_norm_rms(const gl_ap* x, const gl_ap* residual, const gl_ap* weight, float eps, gl_ap* sum, gl_ap* out,
                                void* stream);

@@ -641,6 +641,18 @@ def gl_dense_mx4(a0: AccessPattern, a1: Mx4, out: Optional[AccessPattern] = None
 
 # ---- operands held in 8 bits, the norm in front of them ----
 
+def _on_this_gpu(*tensors) -> int:
+    """`_on_gpu`, and that GPU is the current one, whose streams and kernels the library uses; returns its index."""
+    _on_gpu(*tensors)
+    return _current_is(tensors[0].device.index)
+
+
+def _current_is(index: int) -> int:
+    if torch._C._cuda_getDevice() != index:
+        raise ValueError("tensors are on GPU %d, which is not the current one: call under torch.cuda.device" % index)
+    return index
+
+
 @dataclass
 class F8:
     """A pattern held in 8 bits: E4M3 codes and one E8M0 scale per 128 values of an item."""
@@ -688,7 +700,7 @@ def gl_f8_quantize(a: AccessPattern, out: Optional[F8] = None, stream=None) -> F
     sa = _struct(a)
     if out is None:
         out = f8_empty(tuple(a.tensor.shape), a.access_ndim, a.tensor.device, stream)
-    _on_gpu(a.tensor, out.data, out.scale)
+    _on_this_gpu(a.tensor, out.data, out.scale)
     _check(LIB.gl_f8_quantize(ctypes.byref(sa), ctypes.byref(_f8_struct(out)), _stream(stream)), "gl_f8_quantize")
     return out
 
@@ -696,7 +708,7 @@ def gl_f8_quantize(a: AccessPattern, out: Optional[F8] = None, stream=None) -> F
 def gl_f8_dequantize(m: F8, out: Optional[AccessPattern] = None, stream=None) -> AccessPattern:
     if out is None:
         out = AccessPattern(_empty(m.dims, torch.float32, m.data.device, stream), m.access_ndim)
-    _on_gpu(m.data, m.scale, out.tensor)
+    _on_this_gpu(m.data, m.scale, out.tensor)
     so = _struct(out)
     _check(LIB.gl_f8_dequantize(ctypes.byref(_f8_struct(m)), ctypes.byref(so), _stream(stream)), "gl_f8_dequantize")
     return out
@@ -705,7 +717,7 @@ def gl_f8_dequantize(m: F8, out: Optional[AccessPattern] = None, stream=None) ->
 def gl_cartesian_dot_f8(a0: F8, a1: F8, out: Optional[AccessPattern] = None, flags: int = 0, stream=None) -> AccessPattern:
     if out is None:
         out = _product_out(a0.shape[0], a1.shape[0], flags, a0.data.device, stream)
-    _on_gpu(a0.data, a0.scale, a1.data, a1.scale, out.tensor)
+    _on_this_gpu(a0.data, a0.scale, a1.data, a1.scale, out.tensor)
     so = _struct(out)
     _check(LIB.gl_cartesian_dot_f8(ctypes.byref(_f8_struct(a0)), ctypes.byref(_f8_struct(a1)), ctypes.byref(so), flags,
                                    _stream(stream)), "gl_cartesian_dot_f8")
@@ -722,7 +734,7 @@ def gl_dense_f8(a0: AccessPattern, a1: F8, out: Optional[AccessPattern] = None, 
         out = _product_out(a0.access_shape, a1.shape[0], flags, a0.tensor.device, stream)
     if workspace is None:
         workspace = _scratch(gl_dense_f8_workspace(a0, a1), a0.tensor.device, stream)
-    _on_gpu(a0.tensor, a1.data, a1.scale, out.tensor, workspace)
+    _on_this_gpu(a0.tensor, a1.data, a1.scale, out.tensor, workspace)
     s0, so = _struct(a0), _struct(out)
     _check(LIB.gl_dense_f8(ctypes.byref(s0), ctypes.byref(_f8_struct(a1)), ctypes.byref(so), flags, *_ws(workspace),
                            _stream(stream)), "gl_dense_f8")
@@ -740,7 +752,7 @@ def _tensor(a: Optional[AccessPattern]):
 def _norm_call(x, weight, out, eps, residual, total):
     """(entry point, arguments) of a norm whose result is an F8 operand or an access pattern."""
     eight = isinstance(out, F8)
-    _on_gpu(x.tensor, _tensor(weight), _tensor(residual), _tensor(total), *((out.data, out.scale) if eight else (out.tensor,)))
+    _on_this_gpu(x.tensor, _tensor(weight), _tensor(residual), _tensor(total), *((out.data, out.scale) if eight else (out.tensor,)))
     args = (_ap_ptr(x), _ap_ptr(residual), _ap_ptr(weight), float(eps), _ap_ptr(total),
             ctypes.byref(_f8_struct(out)) if eight else _ap_ptr(out))
     return (LIB.gl_compute_norm_rms_f8 if eight else LIB.gl_compute_norm_rms), args
@@ -781,7 +793,7 @@ def rotary_plan(pairs: int, base: float = 10000.0, sections: Optional[Sequence[i
 
 
 def _rotate_args(x: AccessPattern, plan: GlRotary, positions: torch.Tensor, out: AccessPattern, flags: int):
-    _on_gpu(x.tensor, positions, out.tensor)
+    _on_this_gpu(x.tensor, positions, out.tensor)
     sx, pitch = _tokens_struct(x.tensor)
     so, out_pitch = _tokens_struct(out.tensor)
     sx.access_ndim, so.access_ndim = x.access_ndim, out.access_ndim
@@ -938,13 +950,16 @@ class Prepared:
     The stream is looked up at call time, so a prepared call can be captured
     into a CUDA graph.  `scratch`: a workspace that nobody else holds.  It was taken
     on the stream that was current then, so torch is told of every other stream
-    that uses it: dropping the call then waits for them."""
+    that uses it: dropping the call then waits for them.  `gpu`: the index of the
+    GPU that has to be current."""
 
-    def __init__(self, fn, args, keep, scratch=None):
-        self._fn, self._args, self._keep, self._scratch = fn, args, keep, scratch
+    def __init__(self, fn, args, keep, scratch=None, gpu=None):
+        self._fn, self._args, self._keep, self._scratch, self._gpu = fn, args, keep, scratch, gpu
         self._streams = None if scratch is None else {_stream(None)}
 
     def __call__(self, stream=None):
+        if self._gpu is not None:
+            _current_is(self._gpu)
         raw = _stream(stream)
         if self._streams is not None and raw not in self._streams:
             self._scratch.record_stream(_stream_object(torch.cuda.current_stream() if stream is None else stream))
@@ -1021,39 +1036,40 @@ def prepare_dense_mx4(a0: AccessPattern, a1: Mx4, out: AccessPattern, flags: int
 
 
 def prepare_f8_quantize(a: AccessPattern, out: F8) -> Prepared:
-    _on_gpu(a.tensor, out.data, out.scale)
-    return Prepared(LIB.gl_f8_quantize, (ctypes.byref(_struct(a)), ctypes.byref(_f8_struct(out))), (a, out))
+    gpu = _on_this_gpu(a.tensor, out.data, out.scale)
+    return Prepared(LIB.gl_f8_quantize, (ctypes.byref(_struct(a)), ctypes.byref(_f8_struct(out))), (a, out), gpu=gpu)
 
 
 def prepare_f8_dequantize(m: F8, out: AccessPattern) -> Prepared:
-    _on_gpu(m.data, m.scale, out.tensor)
-    return Prepared(LIB.gl_f8_dequantize, (ctypes.byref(_f8_struct(m)), ctypes.byref(_struct(out))), (m, out))
+    gpu = _on_this_gpu(m.data, m.scale, out.tensor)
+    return Prepared(LIB.gl_f8_dequantize, (ctypes.byref(_f8_struct(m)), ctypes.byref(_struct(out))), (m, out), gpu=gpu)
 
 
 def prepare_cartesian_dot_f8(a0: F8, a1: F8, out: AccessPattern, flags: int = 0) -> Prepared:
-    _on_gpu(a0.data, a0.scale, a1.data, a1.scale, out.tensor)
+    gpu = _on_this_gpu(a0.data, a0.scale, a1.data, a1.scale, out.tensor)
     return Prepared(LIB.gl_cartesian_dot_f8, (ctypes.byref(_f8_struct(a0)), ctypes.byref(_f8_struct(a1)),
-                                              ctypes.byref(_struct(out)), flags), (a0, a1, out))
+                                              ctypes.byref(_struct(out)), flags), (a0, a1, out), gpu=gpu)
 
 
 def prepare_dense_f8(a0: AccessPattern, a1: F8, out: AccessPattern, flags: int = 0,
                      workspace: Optional[torch.Tensor] = None) -> Prepared:
+    gpu = _on_this_gpu(a0.tensor, a1.data, a1.scale, out.tensor, workspace)
     scratch = None if workspace is not None else _scratch(gl_dense_f8_workspace(a0, a1), a0.tensor.device)
     workspace = scratch if workspace is None else workspace
-    _on_gpu(a0.tensor, a1.data, a1.scale, out.tensor, workspace)
     return Prepared(LIB.gl_dense_f8, (ctypes.byref(_struct(a0)), ctypes.byref(_f8_struct(a1)), ctypes.byref(_struct(out)), flags,
-                                      *_ws(workspace)), (a0, a1, out, workspace), scratch)
+                                      *_ws(workspace)), (a0, a1, out, workspace), scratch, gpu)
 
 
 def prepare_compute_norm_rms(x: AccessPattern, weight: Optional[AccessPattern], out, eps: float = 1e-6,
                              residual: Optional[AccessPattern] = None, total: Optional[AccessPattern] = None) -> Prepared:
     """out: an access pattern or an F8 operand."""
     call, args = _norm_call(x, weight, out, eps, residual, total)
-    return Prepared(call, args, (x, weight, out, residual, total))
+    return Prepared(call, args, (x, weight, out, residual, total), gpu=x.tensor.device.index)
 
 
 def prepare_compute_rotate(x: AccessPattern, plan: GlRotary, positions: torch.Tensor, out: AccessPattern, flags: int = 0) -> Prepared:
-    return Prepared(LIB.gl_compute_rotate, _rotate_args(x, plan, positions, out, flags), (x, plan, positions, out))
+    args = _rotate_args(x, plan, positions, out, flags)
+    return Prepared(LIB.gl_compute_rotate, args, (x, plan, positions, out), gpu=x.tensor.device.index)
 
 
 def prepare_cache4_append(cache: Cache4, k, v, page_table, lengths) -> Prepared:

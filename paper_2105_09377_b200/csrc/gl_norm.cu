@@ -302,6 +302,7 @@ int gl_compute_norm_rms(const gl_ap* x, const gl_ap* residual, const gl_ap* weig
   rc = check_data(out);
   if (rc) return rc;
   if (!same_shape(x, out)) return GL_ERR_SHAPE;
+  if (sum && sum->data == out->data) return GL_ERR_UNSUPPORTED;
   p.out = out->data;
   return run_norm(x, residual, p, out->dtype == GL_F32 ? kOutF32 : kOutBf16, stream);
 }
@@ -314,6 +315,7 @@ int gl_compute_norm_rms_f8(const gl_ap* x, const gl_ap* residual, const gl_ap* w
   rc = check_f8_data(out, &v);
   if (rc) return rc;
   if (!f8_same_shape(x, out)) return GL_ERR_SHAPE;
+  if (out->data == out->scale || (sum && (sum->data == out->data || sum->data == out->scale))) return GL_ERR_UNSUPPORTED;
   p.out = out->data;
   p.scale = static_cast<uint8_t*>(out->scale);
   return run_norm(x, residual, p, kOutF8, stream);

@@ -61,7 +61,7 @@ def test_bytes(gl, rows, k):
 
 
 def test_operands_beyond_the_limits_have_no_size(gl):
-    for shape in ((2 ** 31, 4), (4, 2 ** 30 + 1), (2 ** 30, 300), (2 ** 35, 2 ** 35, 2 ** 35), (3, 0)):
+    for shape in ((2 ** 31, 4), (4, 2 ** 28 + 1), (2 ** 30, 300), (2 ** 35, 2 ** 35, 2 ** 35), (3, 0)):
         s = gl._f8_meta(shape, 1)
         assert gl.LIB.gl_f8_data_bytes(ctypes.byref(s)) == 0 and gl.LIB.gl_f8_scale_bytes(ctypes.byref(s)) == 0
     with pytest.raises(gl.GlError):
@@ -131,6 +131,7 @@ def test_refusals_of_the_norm(gl):
         assert norm(eps=eps) == 4
     assert norm(out=_ap(gl, (4, 63), 1, gl.GL_F32)) == 4 and norm(out=_ap(gl, (4, 64), 1, 5)) == 2
     assert norm(x=_ap(gl, (4, 64), 1, gl.GL_BF16, 0x1002)) == 6
+    assert norm(res=res, total=_ap(gl, (4, 64), 1, gl.GL_F32, 0x7000), out=_ap(gl, (4, 64), 1, gl.GL_F32, 0x7000)) == 7
     assert norm(x=_ap(gl, (2 ** 31, 64), 1, gl.GL_BF16), out=_ap(gl, (2 ** 31, 64), 1, gl.GL_F32)) == 7
     eight = lambda m: gl.LIB.gl_compute_norm_rms_f8(r(x), None, r(w), 1e-5, None, r(m), None)
     assert eight(_f8(gl, (4, 65), 1)) == 4 and eight(_f8(gl, (4, 64), 1, scale=0)) == 1 and eight(_f8(gl, (4, 64), 1, data=0x1001)) == 6
@@ -231,8 +232,31 @@ def test_host_tensors_are_refused(gl, name):
         _calls(gl)[name]()
 
 
+def test_the_gpu_of_the_tensors_is_the_current_one(gl, monkeypatch):
+    """Another one's streams would run the kernels on addresses that are not theirs; a prepared call asks again."""
+    class T:                                       # (what the check looks at; this machine has no GPU)
+        is_cuda = True
+
+        def __init__(self, device):
+            self.device = torch.device(device)
+    now = [0]
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: now[0], raising=False)
+    monkeypatch.setattr(gl, "_stream", lambda s: 3)
+    assert gl._on_this_gpu(T("cuda:0"), None, T("cuda:0")) == 0
+    for devices in (("cuda:1", "cuda:1"), ("cuda:0", "cuda:1")):
+        with pytest.raises(ValueError):
+            gl._on_this_gpu(*(T(d) for d in devices))
+    ran = []
+    call = gl.Prepared(lambda raw: ran.append(raw) or 0, (), (), gpu=1)
+    with pytest.raises(ValueError):
+        call()
+    now[0] = 1
+    call()
+    assert ran == [3] and gl._on_this_gpu(T("cuda:1")) == 1
+
+
 def test_tensors_that_the_binding_refuses(gl, monkeypatch):
-    monkeypatch.setattr(gl, "_on_gpu", lambda *t: None)
+    monkeypatch.setattr(gl, "_on_this_gpu", lambda *t: 0)
     ap, plan = gl.AccessPattern, gl.rotary_plan(16, sections=(10, 6))
     t = ap(_made((2, 3, 4, 64), BF), 3)
     for pos in (_made((2, 2, 3), torch.int64), _made((2, 3), torch.int32), _made((1, 2, 3), torch.int32), _made((2, 2, 6), torch.int32)[..., ::2]):
@@ -279,7 +303,7 @@ def test_storage_is_taken_on_the_stream_of_the_call(gl, monkeypatch):
 
     real, empty = gl.LIB, torch.empty
     monkeypatch.setattr(gl, "LIB", Lib())
-    monkeypatch.setattr(gl, "_on_gpu", lambda *t: None)
+    monkeypatch.setattr(gl, "_on_this_gpu", lambda *t: 0)
     monkeypatch.setattr(gl, "_stream", lambda s: 3 if s is None else s if isinstance(s, int) else s.cuda_stream)
     monkeypatch.setattr(torch.cuda, "stream", stream)
     monkeypatch.setattr(torch.cuda, "ExternalStream", lambda raw: _Stream() if raw == 7 else None)

@@ -159,6 +159,68 @@ def test_whole_numbers_are_exact(gl, m, k, o):
     assert np.array_equal(gl.gl_dense_f8(gl.AccessPattern(_device(a, torch.bfloat16), 1), qb).tensor.double().cpu().numpy(), a @ b.T)
 
 
+# K cut over clusters with more than 64 and more than 128 rows, a second block per SM, pairs of SMs with rows that start anywhere,
+# several rounds of pairs, bands of tile rows of two heights
+@pytest.mark.parametrize("m,k,o", [(70, 2100, 200), (300, 2100, 200), (129, 2048, 99), (200, 8300, 8200), (70, 100, 19000),
+                                   (2000, 300, 2001), (4096, 300, 4099), (5000, 200, 1500), (900, 700, 3000)])
+@pytest.mark.parametrize("bf16", [False, True])
+def test_every_way_of_cutting_a_product(gl, m, k, o, bf16):
+    g = torch.Generator("cuda").manual_seed(m + k + o)
+    a = torch.randint(-3, 4, (m, k), generator=g, device="cuda").float()
+    b = torch.randint(-3, 4, (o, k), generator=g, device="cuda").float()
+    out = gl.gl_dense_f8(gl.AccessPattern(a, 1), gl.gl_f8_quantize(gl.AccessPattern(b, 1)), flags=gl.GL_OUT_BF16 if bf16 else 0).tensor
+    want = a.double() @ b.double().t()              # whole numbers below 2^24: every sum is exact
+    assert torch.equal(out, want.to(out.dtype)) and gl.gl_poll_device_status() == 0
+
+
+def test_what_lies_behind_rows_and_blocks_does_not_matter(gl):
+    """Scale bytes of rows and blocks that do not exist are never written; as NaN they must not reach a result."""
+    for m, k, o in ((1, 130, 5), (40, 700, 200), (130, 900, 131), (600, 300, 700)):
+        ops = []
+        for rows in (m, o):
+            q = gl.f8_empty((rows, k), 1, "cuda")
+            q.data.fill_(0x7F)
+            q.scale.fill_(0xFF)
+            x = torch.randint(-3, 4, (rows, k), generator=torch.Generator("cuda").manual_seed(rows), device="cuda").float()
+            ops.append((x, gl.gl_f8_quantize(gl.AccessPattern(x, 1), q)))
+        (a, qa), (b, qb) = ops
+        want = (a.double() @ b.double().t()).float()
+        assert torch.equal(gl.gl_cartesian_dot_f8(qa, qb).tensor, want)
+        assert torch.equal(gl.gl_dense_f8(gl.AccessPattern(a, 1), qb).tensor, want)
+
+
+@pytest.mark.parametrize("m", [1, 20, 200])
+def test_scales_far_from_one(gl, m):
+    """Factors of every size whose products stay inside fp32: the scales of both sides meet before anything is rounded."""
+    k, o = 640, 150
+    a = synth.uniform_int(41, m, (m, k), -3, 3).astype(np.float64)
+    b = synth.uniform_int(42, o, (o, k), -3, 3).astype(np.float64)
+    for ea, eb in ((-100, 90), (100, -110), (60, 50), (-60, -50), (-118, 118)):
+        fa, fb = 2.0 ** ea, 2.0 ** eb
+        qb = gl.gl_f8_quantize(gl.AccessPattern(_device(b * fb, torch.float32), 1))
+        out = gl.gl_dense_f8(gl.AccessPattern(_device(a * fa, torch.float32), 1), qb).tensor
+        assert np.array_equal(out.double().cpu().numpy(), (a @ b.T) * fa * fb), (ea, eb)
+
+
+def test_beyond_two_to_the_31_values(gl):
+    """Offsets of operands and of results in 64 bits."""
+    rows, k = 270000, 8192
+    x = torch.empty((rows, k), dtype=torch.bfloat16, device="cuda")
+    x[-3:] = torch.randn((3, k), generator=torch.Generator("cuda").manual_seed(1), device="cuda")
+    x[:-3].fill_(1.0)
+    q = gl.gl_f8_quantize(gl.AccessPattern(x, 1))
+    back = gl.gl_f8_dequantize(q, gl.AccessPattern(x, 1)).tensor           # (x has been read)
+    last = torch.randn((3, k), generator=torch.Generator("cuda").manual_seed(1), device="cuda").to(torch.bfloat16)
+    assert np.array_equal(back[-3:].double().cpu().numpy(), f8.rounded(last.double().cpu().numpy())) and (back[:-3] == 1).all()
+    w = torch.randint(-3, 4, (8200, k), generator=torch.Generator("cuda").manual_seed(2), device="cuda").float()
+    qw = gl.gl_f8_quantize(gl.AccessPattern(w, 1))
+    del x, back
+    out = gl.gl_cartesian_dot_f8(q, qw, flags=gl.GL_OUT_BF16).tensor
+    assert torch.equal(out[:-3].amin(0), w.sum(1).to(torch.bfloat16)) and torch.equal(out[:-3].amax(0), w.sum(1).to(torch.bfloat16))
+    a = f8.rounded(last.double().cpu().numpy())
+    _close(out[-3:], a, w.double().cpu().numpy(), False, True)
+
+
 def test_item_shapes_and_guard_bands(gl):
     """((B, T),(c, d)) x ((h, e),(c, d)) -> ((B, T, h, e),()); rows without 16-byte multiples, guarded."""
     for m, o, bf16 in (((2, 3), (3, 5), True), ((2, 70), (3, 43), False), ((3, 67), (5, 31), True)):

@@ -166,3 +166,16 @@ def test_graph_and_stream(gl):
         mine = gl.gl_compute_norm_rms_f8(ap(x, 1), ap(w, 0), 1e-5, ap(r, 1), stream=side)
         torch.cuda.synchronize()
         assert torch.equal(gl.gl_f8_dequantize(q).tensor, gl.gl_f8_dequantize(mine).tensor)
+
+
+def test_beyond_two_to_the_31_values(gl):
+    ap = gl.AccessPattern
+    rows, k = 270000, 8192
+    x = torch.ones((rows, k), dtype=BF, device="cuda")
+    x[-2:] = torch.randn((2, k), generator=torch.Generator("cuda").manual_seed(1), device="cuda")
+    want = gl.gl_compute_norm_rms(ap(x[-2:].clone(), 1), None, 0.0, ap(x[-2:].clone(), 1), None, ap(torch.empty((2, k), dtype=BF, device="cuda"), 1)).tensor
+    ends = x[-2:] + x[-2:]
+    gl.gl_compute_norm_rms(ap(x, 1), None, 0.0, ap(x, 1), ap(x, 1), q := gl.f8_empty((rows, k), 1, "cuda"))
+    assert (x[:-2] == 2).all() and torch.equal(x[-2:], ends)
+    back = gl.gl_f8_dequantize(q, ap(x, 1)).tensor
+    assert (back[:-2] == 1).all() and ((back[-2:].double() - want.double()).abs() <= (2.0 ** -4 + 2.0 ** -7) * want.double().abs() + 2.0 ** -9).all()   # (want is bf16)

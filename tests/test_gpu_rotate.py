@@ -155,3 +155,15 @@ def test_graph_and_stream(gl):
         torch.cuda.synchronize()
         assert torch.equal(out.tensor, mine)
         _check(mine, x, pos[None], plan)
+
+
+def test_beyond_two_to_the_31_values(gl):
+    plan = gl.rotary_plan(64)
+    x = torch.ones((1, 270000, 64, 128), dtype=BF, device="cuda")
+    pos = torch.zeros((1, 270000), dtype=torch.int32, device="cuda")
+    pos[0, -5:] = 123
+    a = gl.AccessPattern(x, 3)
+    gl.gl_compute_rotate(a, plan, pos, a)
+    assert (x[0, :-5] == 1).all()
+    one = torch.ones((1, 5, 64, 128), dtype=BF, device="cuda")
+    _check(x[:, -5:].contiguous(), one, pos[None, :, -5:].contiguous(), plan)
