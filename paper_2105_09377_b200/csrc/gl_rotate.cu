@@ -149,8 +149,8 @@ __global__ void __launch_bounds__(kRotThreads) rotate_pairs(const __grid_constan
         uint32_t token, head;
         p.div_heads.divmod(r, token, head);
         const char* src = in + (static_cast<int64_t>(token) * p.pitch + static_cast<int>(head) * p.d) * kEs;
-        if (has_one) a[j] = *reinterpret_cast<const Word*>(src + one * kEs);
-        if (has_two) b[j] = *reinterpret_cast<const Word*>(src + two * kEs);
+        if (has_one) a[j] = __ldcs(reinterpret_cast<const Word*>(src + one * kEs));
+        if (has_two) b[j] = __ldcs(reinterpret_cast<const Word*>(src + two * kEs));
       }
       if (!angles) {
         angles = true;
@@ -198,8 +198,8 @@ __global__ void __launch_bounds__(kRotThreads) rotate_pairs(const __grid_constan
           b[j] = from_floats<F32, W>(v);
         }
         char* dst = out + (static_cast<int64_t>(token) * p.out_pitch + static_cast<int>(head) * p.d) * kEs;
-        if (has_one) *reinterpret_cast<Word*>(dst + one * kEs) = a[j];
-        if (has_two) *reinterpret_cast<Word*>(dst + two * kEs) = b[j];
+        if (has_one) __stcs(reinterpret_cast<Word*>(dst + one * kEs), a[j]);
+        if (has_two) __stcs(reinterpret_cast<Word*>(dst + two * kEs), b[j]);
       }
     }
   }
