@@ -390,7 +390,8 @@ GL_API int gl_f8_quantize(const gl_ap* in, gl_f8* out, void* stream);
 GL_API int gl_f8_dequantize(const gl_f8* in, gl_ap* out, void* stream);
 
 /* compute dotProd (cartProd a0 a1) of two F8 patterns of the same compute shape: ((m..),(k..)), ((o..),(k..)) ->
- * ((m.., o..),()), sums in fp32, on the tensor cores' block-scaled 8-bit products.  flags: GL_EPILOGUE_RELU (NaN stays
+ * ((m.., o..),()), sums in fp32 (rounded toward zero at every step: results of one sign lie up to K * 2^-33 of themselves
+ * low), on the tensor cores' block-scaled 8-bit products.  Results repeat bit for bit.  flags: GL_EPILOGUE_RELU (NaN stays
  * NaN), GL_OUT_BF16; `out` is GL_F32 or, with GL_OUT_BF16, GL_BF16. */
 GL_API int gl_cartesian_dot_f8(const gl_f8* a0, const gl_f8* a1, gl_ap* out, uint32_t flags, void* stream);
 

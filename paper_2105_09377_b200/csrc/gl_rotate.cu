@@ -22,7 +22,8 @@ namespace {
 //
 // A block takes a few tokens: cosines and sines of its tokens once into shared memory, then every thread takes one group of W
 // pairs, 2W values, of head after head, kRotRows of them requested before the first is used (the first ones before the angles
-// are computed).
+// are computed).  Bound by HBM where there are heads enough to hide the angles: 8198 tokens x 40 heads x 128 bf16 30.4 us, 5.5 TB/s
+// (two heads in flight 37 us), fp32 51.7 us, 6.5 TB/s; one head of 128 at 8192 tokens 5.7 us, 64 tokens x 40 heads 2.3 us.
 constexpr int kRotThreads = 256;
 constexpr int kRotRows = 4;           // heads of a thread in flight
 constexpr int kRotAngles = 512;       // angles of a block of several tokens
