@@ -152,7 +152,7 @@ __global__ void __launch_bounds__(C == 4 ? 512 : 1024) norm_rms(const NormParams
   // (The next kernel may start now: at the top its prefetches would stand in the way of this one's operands.  The norm and a product
   // behind it, 1 x 8192 x 8192: 16.6 -> 15.9 us, 128 x 4096 x 4096: 14.0 -> 12.3 us.)
   pdl_launch_dependents();
-  const float rs = 1.f / sqrtf(row_sum(s.x + s.y, slots, warp - static_cast<int>(row_warp), static_cast<int>(p.row_warps.d)) * p.inv_k + p.eps);
+  const float rs = rsqrtf(row_sum(s.x + s.y, slots, warp - static_cast<int>(row_warp), static_cast<int>(p.row_warps.d)) * p.inv_k + p.eps);
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     if (!live || k0 + c * kF8Unit >= p.K) break;
@@ -183,7 +183,7 @@ __global__ void __launch_bounds__(1024) norm_rms_long(const NormParams p) {
     for (int i = 0; i < 4; ++i) s = fma2(h[i], h[i], s);
     total += s.x + s.y;
   }
-  const float rs = 1.f / sqrtf(row_sum(total, slots, 0, 32) * p.inv_k + p.eps);
+  const float rs = rsqrtf(row_sum(total, slots, 0, 32) * p.inv_k + p.eps);
   for (int unit = threadIdx.x >> 5; unit < p.units; unit += 32) {
     const Strip<XF32, RES, OUT> at(p, row, unit * kF8Unit, lane);
     units_read<XF32, VEC, 1>(p.x, at.x, x);

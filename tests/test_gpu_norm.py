@@ -45,7 +45,7 @@ def _check(gl, rows, k, dtype, res, wtype, out_type, eps=1e-5):
         # h is one fp32 sum: exact to 2^-24 of itself, then half a unit of its type
         assert (np.abs(_np(total.tensor) - h) <= (EPS[res] + 2.0 ** -24) * np.abs(h) * (1 + 2.0 ** -8)).all()
     # sum of squares: up to 32 products in a lane, 5 steps over lanes, 32 warps: 69 roundings, half of it after the root; the
-    # mean, eps, the root, the quotient and three products: 12 more; h itself 1
+    # mean, eps, the reciprocal root (two units, four roundings) and three products: 12 more at most; h itself 1
     tol = (69 / 2 + 12 + 1) * 2.0 ** -24 * np.abs(y)
     if out_type == "f8":
         plain = gl.gl_compute_norm_rms(ap(x, 1), opt(w, 0), eps, opt(r, 1), None, ap(torch.empty((rows, k), device="cuda"), 1))
