@@ -188,6 +188,7 @@ def _load() -> ctypes.CDLL:
 
 
 LIB = _load()
+_BARE = ctypes.CDLL(LIB_PATH)   # the same library; its functions take C values as they are
 
 
 class GlError(RuntimeError):
@@ -944,6 +945,21 @@ def gl_version() -> int:
     return int(LIB.gl_version())
 
 
+def _converted(fn, args):
+    """`fn` without argument types and `args` as the C values that its types make of them: ctypes otherwise converts every one of
+    them on every call (0.5 us of 0.9)."""
+    types = getattr(fn, "argtypes", None)
+    if types is None:
+        return fn, args
+    bare = _BARE[fn.__name__]
+    values = []
+    for value, kind in zip(args, types):
+        if issubclass(kind, ctypes._Pointer):
+            value, kind = ctypes.addressof(value._obj) if value is not None else None, ctypes.c_void_p
+        values.append(kind(value))
+    return bare, tuple(values)
+
+
 class Prepared:
     """A device call with its argument structures built once, for launch loops
     where Python marshalling would otherwise outweigh a microsecond-scale kernel.
@@ -956,15 +972,28 @@ class Prepared:
     def __init__(self, fn, args, keep, scratch=None, gpu=None):
         self._fn, self._args, self._keep, self._scratch, self._gpu = fn, args, keep, scratch, gpu
         self._streams = None if scratch is None else {_stream(None)}
+        if gpu is not None:
+            self._keep = (keep, args)                      # (the structures behind the addresses)
+            self._fn, self._args = _converted(fn, args)
+            self._raw = None, None
+
+    def _on_gpu_call(self, stream):
+        if torch._C._cuda_getDevice() != self._gpu:
+            _current_is(self._gpu)
+        raw = torch._C._cuda_getCurrentRawStream(self._gpu) if stream is None else _stream(stream)
+        if raw != self._raw[0]:
+            self._raw = raw, ctypes.c_void_p(raw)
+        return self._raw
 
     def __call__(self, stream=None):
         if self._gpu is not None:
-            _current_is(self._gpu)
-        raw = _stream(stream)
+            raw, last = self._on_gpu_call(stream)
+        else:
+            raw = last = _stream(stream)
         if self._streams is not None and raw not in self._streams:
             self._scratch.record_stream(_stream_object(torch.cuda.current_stream() if stream is None else stream))
             self._streams.add(raw)
-        rc = self._fn(*self._args, raw)
+        rc = self._fn(*self._args, last)
         if rc != GL_OK:
             raise GlError(rc, self._fn.__name__)
 

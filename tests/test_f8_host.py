@@ -241,18 +241,37 @@ def test_the_gpu_of_the_tensors_is_the_current_one(gl, monkeypatch):
             self.device = torch.device(device)
     now = [0]
     monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: now[0], raising=False)
-    monkeypatch.setattr(gl, "_stream", lambda s: 3)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda gpu: 3 + gpu, raising=False)
     assert gl._on_this_gpu(T("cuda:0"), None, T("cuda:0")) == 0
     for devices in (("cuda:1", "cuda:1"), ("cuda:0", "cuda:1")):
         with pytest.raises(ValueError):
             gl._on_this_gpu(*(T(d) for d in devices))
     ran = []
-    call = gl.Prepared(lambda raw: ran.append(raw) or 0, (), (), gpu=1)
+    call = gl.Prepared(lambda raw: ran.append(raw.value) or 0, (), (), gpu=1)
     with pytest.raises(ValueError):
         call()
     now[0] = 1
     call()
-    assert ran == [3] and gl._on_this_gpu(T("cuda:1")) == 1
+    call(9)
+    assert ran == [4, 9] and gl._on_this_gpu(T("cuda:1")) == 1
+
+
+def test_prepared_calls_hand_on_the_same_values(gl, monkeypatch):
+    """Converted once instead of on every call: refusals come back as from the call itself, whatever the type of an argument."""
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda gpu: 0, raising=False)
+    r = ctypes.byref
+    x, w, out, q = _ap(gl, (4, 64), 1, gl.GL_BF16), _f8(gl, (6, 64), 1), _ap(gl, (4, 6), 2, gl.GL_F32), _f8(gl, (4, 64), 1)
+    plan, t = gl.rotary_plan(16), _ap(gl, (2, 3, 4, 40), 3, gl.GL_BF16)
+    cases = [(gl.LIB.gl_compute_norm_rms, (r(x), None, None, -1.0, None, r(x)), 4), (gl.LIB.gl_compute_norm_rms, (None, None, None, 1.0, None, r(x)), 1),
+             (gl.LIB.gl_dense_f8, (r(x), r(w), r(out), 0x400, 0x4000, 1 << 20), 7), (gl.LIB.gl_dense_f8, (r(x), r(w), r(out), 0, 0x4000, 8), 8),
+             (gl.LIB.gl_cartesian_dot_f8, (r(q), r(w), r(out), gl.GL_OUT_BF16), 2),
+             (gl.LIB.gl_compute_rotate, (r(t), 159, r(plan), 0x1000, r(t), 0, 0), 4), (gl.LIB.gl_f8_quantize, (r(x), r(w)), 4)]
+    for fn, args, code in cases:
+        with pytest.raises(gl.GlError) as e:
+            gl.Prepared(fn, args, (), gpu=0)()
+        assert e.value.code == code and fn.__name__ in str(e.value)
+        assert fn(*args, None) == code
 
 
 def test_tensors_that_the_binding_refuses(gl, monkeypatch):
