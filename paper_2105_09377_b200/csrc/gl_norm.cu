@@ -105,26 +105,32 @@ __device__ __forceinline__ void store_result(const float2 (&h)[4], float rs, con
   else unit_store<OUT == kOutF32, VEC>(y, p.out, at.o, c, lane);
 }
 
-// Sum over the warps of a row, the block's warps from `first` on; `slots` holds one float per warp of the block.  All threads of the
-// block call it.
-__device__ __forceinline__ float row_sum(float s, float* slots, int first, int row_warps) {
+// Sum over the warps of a row, the block's warps from `first` on, G sums each; `slots` holds all of them, added in their order.  All
+// threads of the block call it.
+template <int G>
+__device__ __forceinline__ float row_sum(float (&s)[G], float* slots, int first, int row_warps) {
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
-  if (row_warps == 1) return s;
-  if ((threadIdx.x & 31) == 0) slots[threadIdx.x >> 5] = s;
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) s[g] += __shfl_xor_sync(0xFFFFFFFFu, s[g], d);
+  if (G == 1 && row_warps == 1) return s[0];
+  if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) slots[(threadIdx.x >> 5) * G + g] = s[g];
+  }
   __syncthreads();
-  s = 0.f;
-  for (int w = 0; w < row_warps; ++w) s += slots[first + w];
-  return s;
+  float sum = 0.f;
+  for (int w = 0; w < row_warps * G; ++w) sum += slots[first * G + w];
+  return sum;
 }
 
 // A row stays in registers between the sum of its squares and its results: strips of C units a warp, `row_warps` warps a row, as
 // many rows a block as fit.  Everything is read once.  Bound by HBM where a residual is added: 16384 x 8192 bf16 into F8 143 us, 6.6
-// TB/s (940 MB), into bf16 159 us, fp32 throughout 160 us for 8192 x 8192.  Without a residual into F8 100 us, 4.0 TB/s: half the
-// bytes, the same instructions and time between the barrier and the stores.  Rows that start anywhere: 8192 x 8191 bf16 122 us (79
+// TB/s (940 MB), into bf16 159 us, fp32 throughout 160 us for 8192 x 8192.  Without a residual into bf16 81 us, 6.7 TB/s, into F8 84
+// us, 4.8 TB/s: instructions, and fewer bytes in flight.  Rows that start anywhere: 8192 x 8191 bf16 122 us (79
 // aligned), fp32 185 us.  A row alone, 8192: 2.7 us, a launch that does next to nothing 2.0.
 template <bool XF32, int RES, int OUT, bool VEC, int C>
-__global__ void __launch_bounds__(C == 4 ? 512 : 1024) norm_rms(const NormParams p) {
+__global__ void __launch_bounds__(C >= 4 ? 512 : 1024) norm_rms(const NormParams p) {
   __shared__ float slots[32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint32_t block_row, row_warp;
@@ -140,23 +146,38 @@ __global__ void __launch_bounds__(C == 4 ? 512 : 1024) norm_rms(const NormParams
     units_read<XF32, VEC, C>(p.x, at.x, x);
     if (RES != kNone) units_read<RES == kF32, VEC, C>(p.res, at.r, r);
   }
-  float2 h[C][4], s = make_float2(0.f, 0.f);
+  // (bf16 rows without a residual are held as they came, in half the registers, and converted twice)
+  constexpr bool kHeldRaw = RES == kNone && !XF32 && VEC;
+  // Eight units are summed as two warps' four each: the order of a row's sum, and so its F8 result, is that of its fp32 result.
+  constexpr int kSums = C == 8 ? 2 : 1;
+  float2 h[kHeldRaw ? 1 : C][4], pair[kSums];
+  float s[kSums];
+#pragma unroll
+  for (int g = 0; g < kSums; ++g) pair[g] = make_float2(0.f, 0.f);
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     if (!live || k0 + c * kF8Unit >= p.K) break;
-    add_residual<XF32, RES, VEC>(x[c], r[c], at, c, h[c]);
+    float2(&v)[4] = h[kHeldRaw ? 0 : c];
+    add_residual<XF32, RES, VEC>(x[c], r[c], at, c, v);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s = fma2(h[c][i], h[c][i], s);
-    if (RES != kNone && p.sum) unit_store<RES == kF32, VEC>(h[c], p.sum, at.r, c, lane);
+    for (int i = 0; i < 4; ++i) pair[kSums == 2 ? c / 4 : 0] = fma2(v[i], v[i], pair[kSums == 2 ? c / 4 : 0]);
+    if (RES != kNone && p.sum) unit_store<RES == kF32, VEC>(v, p.sum, at.r, c, lane);
   }
   // (The next kernel may start now: at the top its prefetches would stand in the way of this one's operands.  The norm and a product
   // behind it, 1 x 8192 x 8192: 16.6 -> 15.9 us, 128 x 4096 x 4096: 14.0 -> 12.3 us.)
   pdl_launch_dependents();
-  const float rs = rsqrtf(row_sum(s.x + s.y, slots, warp - static_cast<int>(row_warp), static_cast<int>(p.row_warps.d)) * p.inv_k + p.eps);
+#pragma unroll
+  for (int g = 0; g < kSums; ++g) s[g] = pair[g].x + pair[g].y;
+  const float rs = rsqrtf(row_sum(s, slots, warp - static_cast<int>(row_warp), static_cast<int>(p.row_warps.d)) * p.inv_k + p.eps);
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     if (!live || k0 + c * kF8Unit >= p.K) break;
-    store_result<OUT, VEC>(h[c], rs, p, at, c, lane);
+    if (kHeldRaw) {
+#pragma unroll
+      for (int i = 0; i < Unit<XF32, VEC>::kHeld; ++i) asm volatile("" : "+r"(x[c].w[i]));   // (not the first conversion's results)
+      unit_values(x[c], at.x, c, h[0]);
+    }
+    store_result<OUT, VEC>(h[kHeldRaw ? 0 : c], rs, p, at, c, lane);
   }
 }
 
@@ -169,7 +190,7 @@ __global__ void __launch_bounds__(1024) norm_rms_long(const NormParams p) {
   const uint32_t row = blockIdx.x;
   pdl_wait();
   pdl_launch_dependents();
-  float total = 0.f;
+  float total[1] = {0.f};
   Unit<XF32, VEC> x[1];
   Unit<RES == kF32, VEC> r[1];
   float2 h[4];
@@ -181,7 +202,7 @@ __global__ void __launch_bounds__(1024) norm_rms_long(const NormParams p) {
     float2 s = make_float2(0.f, 0.f);   // (a lane adds up to 2^15 values for the longest rows: by units of eight first)
 #pragma unroll
     for (int i = 0; i < 4; ++i) s = fma2(h[i], h[i], s);
-    total += s.x + s.y;
+    total[0] += s.x + s.y;
   }
   const float rs = rsqrtf(row_sum(total, slots, 0, 32) * p.inv_k + p.eps);
   for (int unit = threadIdx.x >> 5; unit < p.units; unit += 32) {
@@ -194,22 +215,33 @@ __global__ void __launch_bounds__(1024) norm_rms_long(const NormParams p) {
   }
 }
 
-template <bool XF32, int RES, int OUT, bool VEC>
-int launch_norm(NormParams p, cudaStream_t st) {
-  // Four units a warp (two of unaligned rows, which take more registers) when there are rows enough to fill the machine; a row
-  // alone is spread over as many warps as it has units.
-  constexpr int kMost = VEC ? 4 : 2;
-  const bool spread = p.rows <= static_cast<uint32_t>(num_sms());
-  const int row_warps = std::min(spread ? p.units : (p.units + kMost - 1) / kMost, 32);
-  const int per_warp = (p.units + row_warps - 1) / row_warps;
+// Rows of `row_warps` warps with C units each.
+template <bool XF32, int RES, int OUT, bool VEC, int C>
+int launch_strips(NormParams p, int row_warps, cudaStream_t st) {
   p.row_warps.set(row_warps);
   p.block_rows = std::max(8 / row_warps, 1);
   const dim3 grid((p.rows + p.block_rows - 1) / p.block_rows), block(static_cast<unsigned>(row_warps * p.block_rows * 32));
-  void (*k)(NormParams) = norm_rms_long<XF32, RES, OUT, VEC>;
-  if (per_warp == 1) k = norm_rms<XF32, RES, OUT, VEC, 1>;
-  else if (per_warp == 2) k = norm_rms<XF32, RES, OUT, VEC, 2>;
-  else if (VEC && row_warps <= 16) k = norm_rms<XF32, RES, OUT, VEC, kMost>;   // (then four units a warp suffice)
-  return launch_pdl(k, grid, block, 0, st, 1, p) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
+  return launch_pdl(norm_rms<XF32, RES, OUT, VEC, C>, grid, block, 0, st, 1, p) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
+}
+
+template <bool XF32, int RES, int OUT, bool VEC>
+int launch_norm(const NormParams& p, cudaStream_t st) {
+  // Four units a warp (two of unaligned rows, which take more registers) when there are rows enough to fill the machine; a row
+  // alone is spread over as many warps as it has units.
+  // Eight where a row is held as bf16 and its result is F8, if that leaves no warp with less and every SM its 28 warps (and the row
+  // would fit in registers by fours too): 16384 x 8192 97.6 -> 84.8 us, 16384 x 4096 51.1 -> 46.4, but 300 x 8192 4.9 -> 6.1 and
+  // 2048 x 5120 11.2 -> 14.9; into bf16 16384 x 8192 80.6 -> 82.7.
+  constexpr int kMost = VEC ? 4 : 2;
+  constexpr bool kEight = VEC && !XF32 && RES == kNone && OUT == kOutF8;
+  if (kEight && p.units % 8 == 0 && p.units <= 64 && static_cast<int64_t>(p.rows) * p.units >= static_cast<int64_t>(num_sms()) * 28 * 8)
+    return launch_strips<XF32, RES, OUT, VEC, kEight ? 8 : kMost>(p, p.units / 8, st);
+  const bool spread = p.rows <= static_cast<uint32_t>(num_sms());
+  const int row_warps = std::min(spread ? p.units : (p.units + kMost - 1) / kMost, 32);
+  const int per_warp = (p.units + row_warps - 1) / row_warps;
+  if (per_warp == 1) return launch_strips<XF32, RES, OUT, VEC, 1>(p, row_warps, st);
+  if (per_warp == 2) return launch_strips<XF32, RES, OUT, VEC, 2>(p, row_warps, st);
+  if (VEC && row_warps <= 16) return launch_strips<XF32, RES, OUT, VEC, kMost>(p, row_warps, st);   // (then four units a warp suffice)
+  return launch_pdl(norm_rms_long<XF32, RES, OUT, VEC>, dim3(p.rows), dim3(1024), 0, st, 1, p) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
 }
 
 template <bool XF32, int RES, int OUT>

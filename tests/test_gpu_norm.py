@@ -126,6 +126,13 @@ def test_values_at_the_ends(gl):
     assert torch.isnan(gl.gl_compute_norm_rms(ap(x[:1], 1), None, 0.0).tensor).all()         # 0 / 0
 
 
+@pytest.mark.parametrize("rows,k,wtype", [(1100, 8192, BF), (4300, 2048, F32), (2100, 4096, None), (300, 32768, BF)])
+def test_rows_held_as_they_came(gl, rows, k, wtype):
+    """bf16 rows without a residual into F8, eight units a warp: the same codes as of the fp32 result; rows of 128 units and one more."""
+    _check(gl, rows, k, BF, None, wtype, "f8")
+    _check(gl, 40, k + 256, BF, None, wtype, "f8")
+
+
 def test_items_of_several_dimensions_and_guard_bands(gl):
     ap = gl.AccessPattern
     shape = (3, 5, 7, 11)
