@@ -148,6 +148,70 @@ __global__ void __launch_bounds__(256) dequantize_f8(const uint8_t* __restrict__
   }
 }
 
+// Rows of up to 128 values, several side by side: with a unit per row half of a warp's lanes or more would have nothing to do
+// (327680 x 128 bf16 42 -> 22 us, x 64 41 -> 13, x 96 41 -> 21, x 8 40 -> 4.0, fp32 x 128 62 -> 33; 2560 x 128 1.6 -> 1.4).
+template <bool F32, int U>
+__global__ void __launch_bounds__(256) quantize_f8_short(const void* __restrict__ in, uint8_t* __restrict__ codes,
+                                                         uint8_t* __restrict__ scale, const ShortRows r) {
+  pdl_wait();
+  pdl_launch_dependents();
+  Unit<F32, true> held[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) short_read(in, r, ShortAt(r, U, u), held[u]);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    float2 v[4];
+    short_values(held[u], v);
+    short_store_f8(v, codes, scale, r, ShortAt(r, U, u));
+  }
+}
+
+// Going back, fp32 rows are held as two times four values a lane, half a row apart: 16-byte stores next to each other (327680 x 128
+// 33 us; eight values in a row 46; a unit per row 33, x 64 30 -> 18).  bf16 rows 29 -> 21, x 64 29 -> 12.
+template <bool F32, int U>
+__global__ void __launch_bounds__(256) dequantize_f8_short(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scale,
+                                                           void* __restrict__ out, const ShortRows r) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & (r.lanes - 1);
+  const int k0 = F32 ? lane * 4 : lane * 8, k1 = F32 ? (r.lanes + lane) * 4 : k0 + 4;
+  uint32_t word[U][2], e[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const ShortAt at(r, U, u);
+    word[u][0] = word[u][1] = e[u] = 0;
+    if (at.row >= r.rows) continue;
+    const uint8_t* from = codes + static_cast<int64_t>(at.row) * r.pitch;
+    if (F32) {
+      if (k0 < r.K) word[u][0] = __ldcs(reinterpret_cast<const uint32_t*>(from + k0));
+      if (k1 < r.K) word[u][1] = __ldcs(reinterpret_cast<const uint32_t*>(from + k1));
+    } else if (k0 < r.K) {
+      const uint2 both = __ldcs(reinterpret_cast<const uint2*>(from + k0));
+      word[u][0] = both.x;
+      word[u][1] = both.y;
+    }
+    e[u] = scale[f8_scale_at(at.row, 0, 1)];
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const ShortAt at(r, U, u);
+    const float s = f8_scale(e[u]);
+    float2 v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t w = word[u][i / 2];
+      v[i] = mul2(f8_values2(i & 1 ? w >> 16 : w & 0xFFFFu), make_float2(s, s));
+    }
+    if (!F32) {
+      short_store<false>(v, out, r, at);
+    } else if (at.row < r.rows) {
+      float* to = static_cast<float*>(out) + static_cast<int64_t>(at.row) * r.K;
+      if (k0 < r.K) *reinterpret_cast<float4*>(to + k0) = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
+      if (k1 < r.K) *reinterpret_cast<float4*>(to + k1) = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
+    }
+  }
+}
+
 // Units of a strip and rows of a warp: eight units in flight, four where rows are unaligned (a unit takes half as many registers
 // again, and more).
 struct StripPlan { int units, rows; };
@@ -199,6 +263,14 @@ DequantizeFn dequantize_fn(const StripPlan& s) {
 
 int launch_quantize(const gl_ap& in, const F8View& v, void* codes, void* scale, cudaStream_t st) {
   const bool f32 = in.dtype == GL_F32, vec = v.K % 8 == 0;
+  if (is_short(v)) {
+    const ShortRows r = short_rows(v);
+    const int groups = short_groups(r, num_sms());
+    void (*k)(const void*, uint8_t*, uint8_t*, ShortRows) = groups == 4 ? (f32 ? quantize_f8_short<true, 4> : quantize_f8_short<false, 4>)
+                                                                        : (f32 ? quantize_f8_short<true, 1> : quantize_f8_short<false, 1>);
+    return launch_pdl(k, dim3(short_blocks(r, groups)), dim3(256), 0, st, 1, static_cast<const void*>(in.data), static_cast<uint8_t*>(codes),
+                      static_cast<uint8_t*>(scale), r) == cudaSuccess ? GL_OK : GL_ERR_CUDA;
+  }
   StripPlan s;
   const F8QuantParams p = f8_quant_params(v, &s);
   const QuantizeFn k = f32 ? (vec ? quantize_fn<true, true>(s) : quantize_fn<true, false>(s))
@@ -1198,9 +1270,19 @@ int gl_f8_dequantize(const gl_f8* in, gl_ap* out, void* stream) {
   rc = check_data(out);
   if (rc) return rc;
   if (!f8_same_shape(out, in)) return GL_ERR_SHAPE;
+  const bool f32 = out->dtype == GL_F32, vec = v.K % 8 == 0;
+  if (is_short(v)) {
+    const ShortRows r = short_rows(v);
+    const int groups = short_groups(r, num_sms());
+    void (*k)(const uint8_t*, const uint8_t*, void*, ShortRows) =
+        groups == 4 ? (f32 ? dequantize_f8_short<true, 4> : dequantize_f8_short<false, 4>)
+                    : (f32 ? dequantize_f8_short<true, 1> : dequantize_f8_short<false, 1>);
+    return launch_pdl(k, dim3(short_blocks(r, groups)), dim3(256), 0, static_cast<cudaStream_t>(stream), 1,
+                      static_cast<const uint8_t*>(in->data), static_cast<const uint8_t*>(in->scale), out->data, r) == cudaSuccess
+               ? GL_OK : GL_ERR_CUDA;
+  }
   StripPlan s;
   const F8QuantParams p = f8_quant_params(v, &s);
-  const bool f32 = out->dtype == GL_F32, vec = v.K % 8 == 0;
   const DequantizeFn k = f32 ? (vec ? dequantize_fn<true, true>(s) : dequantize_fn<true, false>(s))
                              : (vec ? dequantize_fn<false, true>(s) : dequantize_fn<false, false>(s));
   return launch_pdl(k, dim3((p.strips + 7) / 8), dim3(256), 0, static_cast<cudaStream_t>(stream), 1,

@@ -329,4 +329,96 @@ __device__ __forceinline__ void unit_store_f8(const float2 (&v)[4], uint8_t* cod
   if (lane == 0) *reinterpret_cast<uint16_t*>(scale + (c >> 1) * 512 + (c & 1) * 2) = static_cast<uint16_t>(e | second << 8);
 }
 
+// ---- rows of up to 128 values, a multiple of eight: several side by side in a warp ----
+
+// A row takes `lanes` lanes, a power of two, of eight values each (those behind the row's end are idle); U groups of 32 / lanes rows a
+// warp, one below the other.
+struct ShortRows {
+  uint32_t rows;
+  int32_t K, pitch;
+  int32_t lanes, log_lanes;
+};
+
+inline ShortRows short_rows(const F8View& v) {
+  ShortRows r;
+  r.rows = static_cast<uint32_t>(v.rows);
+  r.K = static_cast<int32_t>(v.K);
+  r.pitch = static_cast<int32_t>(v.pitch);
+  r.lanes = 1;
+  r.log_lanes = 0;
+  while (r.lanes * 8 < r.K) { r.lanes *= 2; ++r.log_lanes; }
+  return r;
+}
+inline bool is_short(const F8View& v) { return v.K <= 128 && v.K % 8 == 0; }
+// Four groups a warp when that still fills every SM with 64 warps (one group and four, us: rounding 327680 x 128 bf16 27.7 and 22.1,
+// 80000 x 128 8.1 and 7.4, 40000 x 128 4.9 and 5.8, 80000 x 64 4.8 and 5.6, 2560 x 128 1.4 and 1.9).
+inline int short_groups(const ShortRows& r, int sms) {
+  return static_cast<int64_t>(r.rows) * r.lanes >= static_cast<int64_t>(sms) * 64 * 4 * 32 ? 4 : 1;
+}
+inline unsigned short_blocks(const ShortRows& r, int groups) {   // of eight warps
+  const int64_t per_block = static_cast<int64_t>(8) * groups * (32 / r.lanes);
+  return static_cast<unsigned>((r.rows + per_block - 1) / per_block);
+}
+
+// Row of this lane in group u, its place in the row, and whether there is such a value.
+struct ShortAt {
+  uint32_t row;
+  int k;
+  bool live;
+  __device__ __forceinline__ ShortAt(const ShortRows& r, int groups, int u) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t warp = blockIdx.x * 8u + (threadIdx.x >> 5);
+    row = ((warp * groups + u) << (5 - r.log_lanes)) + (lane >> r.log_lanes);
+    k = (lane & (r.lanes - 1)) * 8;
+    live = row < r.rows && k < r.K;
+  }
+};
+
+template <bool F32>
+__device__ __forceinline__ void short_read(const void* base, const ShortRows& r, const ShortAt& at, Unit<F32, true>& u) {
+  const uint4* q = reinterpret_cast<const uint4*>(static_cast<const char*>(base) + (static_cast<int64_t>(at.row) * r.K + at.k) * (F32 ? 4 : 2));
+#pragma unroll
+  for (int i = 0; i < Unit<F32, true>::kHeld / 4; ++i) {
+    uint4 x = make_uint4(0, 0, 0, 0);
+    if (at.live) x = __ldcs(q + i);
+    u.w[4 * i] = x.x; u.w[4 * i + 1] = x.y; u.w[4 * i + 2] = x.z; u.w[4 * i + 3] = x.w;
+  }
+}
+template <bool F32>
+__device__ __forceinline__ void short_values(const Unit<F32, true>& u, float2 (&v)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    v[i] = F32 ? make_float2(__uint_as_float(u.w[(2 * i) % Unit<F32, true>::kHeld]), __uint_as_float(u.w[(2 * i + 1) % Unit<F32, true>::kHeld]))
+               : make_float2(__uint_as_float(u.w[i] << 16), __uint_as_float(u.w[i] & 0xFFFF0000u));
+}
+template <bool F32>
+__device__ __forceinline__ void short_store(const float2 (&v)[4], void* base, const ShortRows& r, const ShortAt& at) {
+  if (!at.live) return;
+  char* p = static_cast<char*>(base) + (static_cast<int64_t>(at.row) * r.K + at.k) * (F32 ? 4 : 2);
+  if (F32) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
+    reinterpret_cast<float4*>(p)[1] = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
+  } else {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(__float_as_uint(v[i].x), __float_as_uint(v[i].y));
+    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+// Codes and scale of rows that are one block (one scale tile along K).  Every lane of the warp takes part.
+__device__ __forceinline__ void short_store_f8(const float2 (&v)[4], uint8_t* codes, uint8_t* scale, const ShortRows& r, const ShortAt& at) {
+  float largest = top_of(top_of(top_of(v[0].x, v[0].y), top_of(v[1].x, v[1].y)), top_of(top_of(v[2].x, v[2].y), top_of(v[3].x, v[3].y)));
+  for (int d = 1; d < r.lanes; d *= 2) largest = top_of(largest, __shfl_xor_sync(0xFFFFFFFFu, largest, d));
+  if (!at.live) return;
+  const uint32_t e = f8_exponent(__float_as_uint(largest) & 0x7FFFFFFFu);
+  const float f = f8_inverse(e);
+  float2 q[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) q[i] = mul2(v[i], make_float2(f, f));
+  uint2* to = reinterpret_cast<uint2*>(codes + static_cast<int64_t>(at.row) * r.pitch + at.k);
+  to[0] = make_uint2(e == 255u ? 0u : f8_codes4(q[0].x, q[0].y, q[1].x, q[1].y), e == 255u ? 0u : f8_codes4(q[2].x, q[2].y, q[3].x, q[3].y));
+  if (at.k + 8 == r.K && r.K < r.pitch) to[1] = make_uint2(0u, 0u);   // (the pitch is the next multiple of 16)
+  if (at.k == 0) scale[f8_scale_at(at.row, 0, 1)] = static_cast<uint8_t>(e);
+}
+
 }  // namespace

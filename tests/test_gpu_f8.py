@@ -67,9 +67,16 @@ def test_quantize_bit_for_bit(gl, rows, k, dtype):
     assert np.array_equal(half.double().cpu().numpy(), ref)
 
 
+@pytest.mark.parametrize("rows,k", [(1, 8), (200, 24), (31, 40), (130, 64), (600, 72), (65, 120)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_quantize_short_rows(gl, rows, k, dtype):
+    test_quantize_bit_for_bit(gl, rows, k, dtype)
+
+
 def test_quantize_many_rows(gl):
     """Several units a warp: more rows than one pass over the SMs, a ragged end."""
-    for rows, k, dtype in ((20001, 264, torch.bfloat16), (9001, 263, torch.float32), (40003, 129, torch.bfloat16)):
+    for rows, k, dtype in ((90001, 128, torch.bfloat16), (80003, 72, torch.float32), (300007, 8, torch.bfloat16), (2000, 120, torch.float32),
+                           (20001, 264, torch.bfloat16), (9001, 263, torch.float32), (40003, 129, torch.bfloat16)):
         g = torch.Generator("cuda").manual_seed(rows)
         x = torch.randn((rows, k), generator=g, device="cuda").to(dtype)
         back = gl.gl_f8_dequantize(gl.gl_f8_quantize(gl.AccessPattern(x, 1)), gl.AccessPattern(torch.empty_like(x), 1)).tensor

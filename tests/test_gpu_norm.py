@@ -91,7 +91,7 @@ def test_long_rows(gl, rows, k):
     assert torch.equal(gl.gl_f8_dequantize(q).tensor, gl.gl_f8_dequantize(gl.gl_f8_quantize(out)).tensor)
 
 
-@pytest.mark.parametrize("rows,k", [(3, 1000), (200, 1111), (2, 8192), (300, 4096), (2, 33001), (1, 40000)])
+@pytest.mark.parametrize("rows,k", [(70, 128), (40000, 24), (76003, 128), (3, 1000), (200, 1111), (2, 8192), (300, 4096), (2, 33001), (1, 40000)])
 def test_in_place(gl, rows, k):
     """The sum takes the residual's place, or x's; the result takes x's."""
     ap = gl.AccessPattern
@@ -124,6 +124,16 @@ def test_values_at_the_ends(gl):
     q = gl.gl_f8_dequantize(gl.gl_compute_norm_rms_f8(ap(x, 1), None, 1e-6)).tensor
     assert (q[0] == 0).all() and torch.isnan(q[3]).all() and torch.isnan(q[4, :128]).all() and (q[4, 128:] == 0).all()
     assert torch.isnan(gl.gl_compute_norm_rms(ap(x[:1], 1), None, 0.0).tensor).all()         # 0 / 0
+
+
+@pytest.mark.parametrize("out_type", [BF, F32, "f8"])
+@pytest.mark.parametrize("rows,k", [(1, 16), (5, 24), (31, 8), (1000, 120), (4097, 64), (80001, 128), (999, 40), (300001, 8), (90000, 72),
+                                    (310003, 32)])
+def test_short_rows(gl, rows, k, out_type):
+    """Several rows side by side in a warp: heads, in every number of lanes, one or four groups a warp."""
+    _check(gl, rows, k, BF, None, BF, out_type)
+    _check(gl, rows, k, F32, BF, None, out_type)
+    _check(gl, rows, k, BF, F32, F32, out_type)
 
 
 @pytest.mark.parametrize("rows,k,wtype", [(1100, 8192, BF), (4300, 2048, F32), (2100, 4096, None), (300, 32768, BF)])
