@@ -798,8 +798,9 @@ def _rotate_args(x: AccessPattern, plan: GlRotary, positions: torch.Tensor, out:
     sx, pitch = _tokens_struct(x.tensor)
     so, out_pitch = _tokens_struct(out.tensor)
     sx.access_ndim, so.access_ndim = x.access_ndim, out.access_ndim
-    if positions.dtype != torch.int32 or not positions.is_contiguous() or \
-            tuple(positions.shape) not in ((plan.axes,) + tuple(x.tensor.shape[:2]), tuple(x.tensor.shape[:2]) if plan.axes == 1 else ()):
+    batch_tokens = tuple(x.tensor.shape[:2])
+    shapes = [(plan.axes,) + batch_tokens] + ([batch_tokens] if plan.axes == 1 else [])
+    if positions.dtype != torch.int32 or not positions.is_contiguous() or tuple(positions.shape) not in shapes:
         raise ValueError("positions are contiguous int32 [axes, batch, tokens]")
     return (ctypes.byref(sx), pitch, ctypes.byref(plan), positions.data_ptr(), ctypes.byref(so), out_pitch, flags)
 

@@ -1,0 +1,35 @@
+"""Calls on 8-bit operands, the norm and the rotation that are refused or hold on to nothing of their caller's, checked on the host."""
+import ctypes
+
+import pytest
+import torch
+
+BF, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def gl():
+    from paper_2105_09377_b200 import build
+    build.build()
+    from paper_2105_09377_b200 import binding
+    return binding
+
+
+def _tokens(gl, shape=(2, 3, 4, 64)):
+    return gl.AccessPattern(torch.zeros(shape, dtype=BF), 3)
+
+
+# ---- positions ----
+
+def test_positions_are_counted_with_every_number_of_axes(gl, monkeypatch):
+    """A single number is not [axes, batch, tokens]: the kernel would read behind it."""
+    monkeypatch.setattr(gl, "_on_this_gpu", lambda *t: 0)
+    t = _tokens(gl)
+    for sections in ((16,), (10, 6), (4, 4, 8)):
+        plan = gl.rotary_plan(16, sections=sections)
+        n = len(sections)
+        for shape in ((), (1,), (n,), (n, 6), (n, 2, 3, 1), (n + 1, 2, 3), (n, 3, 2), (3,)):
+            with pytest.raises(ValueError, match="positions"):
+                gl._rotate_args(t, plan, torch.zeros(shape, dtype=torch.int32), t, 0)
+        gl._rotate_args(t, plan, torch.zeros((n, 2, 3), dtype=torch.int32), t, 0)
+    gl._rotate_args(t, gl.rotary_plan(16), torch.zeros((2, 3), dtype=torch.int32), t, 0)
