@@ -802,7 +802,8 @@ def _rotate_args(x: AccessPattern, plan: GlRotary, positions: torch.Tensor, out:
     shapes = [(plan.axes,) + batch_tokens] + ([batch_tokens] if plan.axes == 1 else [])
     if positions.dtype != torch.int32 or not positions.is_contiguous() or tuple(positions.shape) not in shapes:
         raise ValueError("positions are contiguous int32 [axes, batch, tokens]")
-    return (ctypes.byref(sx), pitch, ctypes.byref(plan), positions.data_ptr(), ctypes.byref(so), out_pitch, flags)
+    # (a copy: what the caller changes in the plan later has not been checked against these positions)
+    return (ctypes.byref(sx), pitch, ctypes.byref(GlRotary.from_buffer_copy(plan)), positions.data_ptr(), ctypes.byref(so), out_pitch, flags)
 
 
 def gl_compute_rotate(x: AccessPattern, plan: GlRotary, positions: torch.Tensor, out: Optional[AccessPattern] = None, flags: int = 0,

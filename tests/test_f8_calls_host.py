@@ -33,3 +33,14 @@ def test_positions_are_counted_with_every_number_of_axes(gl, monkeypatch):
                 gl._rotate_args(t, plan, torch.zeros(shape, dtype=torch.int32), t, 0)
         gl._rotate_args(t, plan, torch.zeros((n, 2, 3), dtype=torch.int32), t, 0)
     gl._rotate_args(t, gl.rotary_plan(16), torch.zeros((2, 3), dtype=torch.int32), t, 0)
+
+
+def test_a_prepared_rotation_keeps_its_own_plan(gl, monkeypatch):
+    """The positions were counted for the plan as it was: axes that its caller adds later would be read behind them."""
+    monkeypatch.setattr(gl, "_on_this_gpu", lambda *t: 0)
+    plan, t = gl.rotary_plan(16), _tokens(gl)
+    args = gl._rotate_args(t, plan, torch.zeros((1, 2, 3), dtype=torch.int32), t, 0)
+    step = plan.step[3]
+    plan.axes, plan.axis[3], plan.step[3] = 2, 1, 5
+    held = args[2]._obj
+    assert (held.axes, held.axis[3], held.step[3], held.pairs) == (1, 0, step, 16)
