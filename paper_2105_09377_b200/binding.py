@@ -983,9 +983,10 @@ class Prepared:
         if torch._C._cuda_getDevice() != self._gpu:
             _current_is(self._gpu)
         raw = torch._C._cuda_getCurrentRawStream(self._gpu) if stream is None else _stream(stream)
-        if raw != self._raw[0]:
-            self._raw = raw, ctypes.c_void_p(raw)
-        return self._raw
+        last = self._raw            # (read once: another thread may put its own stream there at any time)
+        if raw != last[0]:
+            last = self._raw = raw, ctypes.c_void_p(raw)
+        return last
 
     def __call__(self, stream=None):
         if self._gpu is not None:

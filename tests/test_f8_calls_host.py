@@ -1,5 +1,5 @@
 """Calls on 8-bit operands, the norm and the rotation that are refused or hold on to nothing of their caller's, checked on the host."""
-import ctypes
+import sys
 
 import pytest
 import torch
@@ -44,3 +44,33 @@ def test_a_prepared_rotation_keeps_its_own_plan(gl, monkeypatch):
     plan.axes, plan.axis[3], plan.step[3] = 2, 1, 5
     held = args[2]._obj
     assert (held.axes, held.axis[3], held.step[3], held.pairs) == (1, 0, step, 16)
+
+
+# ---- prepared calls that threads share ----
+
+def test_a_prepared_call_keeps_to_its_own_stream(gl, monkeypatch):
+    """Another call of the same object, on another stream, between any two lines of this one (as a thread that takes over there
+    makes it): each goes to the stream that it was given."""
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda gpu: 3, raising=False)
+    ran = []
+    call = gl.Prepared(lambda raw: ran.append(raw.value) or 0, (), (), gpu=0)
+    between = [0]
+
+    def other(frame, event, arg):
+        if event in ("line", "return") and frame.f_code.co_filename == gl.__file__:
+            sys.settrace(None)
+            call(1000 + between[0])
+            between[0] += 1
+            sys.settrace(other)
+        return other
+
+    for given, raw in ((7, 7), (None, 3), (8, 8)):
+        del ran[:]
+        between[0] = 0
+        sys.settrace(other)
+        try:
+            call(given)
+        finally:
+            sys.settrace(None)
+        assert between[0] >= 5 and sorted(ran) == [raw] + [1000 + i for i in range(between[0])], (given, ran)
