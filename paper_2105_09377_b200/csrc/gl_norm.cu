@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 
 #include "gl_f8.cuh"
 #include "gl_internal.h"
@@ -326,6 +327,26 @@ bool same_shape(const gl_ap* a, const gl_ap* b) {
   return true;
 }
 
+// Bytes that an operand or a result takes.
+struct Place {
+  uintptr_t at;
+  size_t bytes;
+};
+Place place_of(const gl_ap* a) {
+  size_t n = a->dtype == GL_F32 ? 4 : 2;
+  for (int i = 0; i < a->ndim; ++i) n *= static_cast<size_t>(a->shape[i]);
+  return {reinterpret_cast<uintptr_t>(a->data), n};
+}
+bool meet(const Place& a, const Place& b) { return a.at < b.at + b.bytes && b.at < a.at + a.bytes; }
+// A result of the shape of operand `in` may take its place value for value; otherwise the two have to lie apart, as a block reads
+// rows while others write theirs.
+bool clash(const gl_ap* in, const gl_ap* out) {
+  return in && out && !(in->data == out->data && in->dtype == out->dtype) && meet(place_of(in), place_of(out));
+}
+bool weight_or_sum_clash(const gl_ap* weight, const gl_ap* sum, const Place& out) {
+  return (weight && meet(place_of(weight), out)) || (sum && meet(place_of(sum), out));
+}
+
 // Everything but the result, which the two entry points check themselves.
 int norm_params(const gl_ap* x, const gl_ap* residual, const gl_ap* weight, float eps, const gl_ap* sum, NormParams* p) {
   int rc = check_data(x);
@@ -359,6 +380,7 @@ int norm_params(const gl_ap* x, const gl_ap* residual, const gl_ap* weight, floa
   F8View v;
   rc = check_f8_meta(&as_items, &v);
   if (rc) return rc;
+  if (clash(x, sum) || clash(residual, sum) || (sum && weight && meet(place_of(weight), place_of(sum)))) return GL_ERR_UNSUPPORTED;
   std::memset(p, 0, sizeof(*p));
   p->x = x->data;
   p->res = residual ? residual->data : nullptr;
@@ -391,7 +413,7 @@ int gl_compute_norm_rms(const gl_ap* x, const gl_ap* residual, const gl_ap* weig
   rc = check_data(out);
   if (rc) return rc;
   if (!same_shape(x, out)) return GL_ERR_SHAPE;
-  if (sum && sum->data == out->data) return GL_ERR_UNSUPPORTED;
+  if (clash(x, out) || clash(residual, out) || weight_or_sum_clash(weight, sum, place_of(out))) return GL_ERR_UNSUPPORTED;
   p.out = out->data;
   return run_norm(x, residual, p, out->dtype == GL_F32 ? kOutF32 : kOutBf16, stream);
 }
@@ -404,7 +426,11 @@ int gl_compute_norm_rms_f8(const gl_ap* x, const gl_ap* residual, const gl_ap* w
   rc = check_f8_data(out, &v);
   if (rc) return rc;
   if (!f8_same_shape(x, out)) return GL_ERR_SHAPE;
-  if (out->data == out->scale || (sum && (sum->data == out->data || sum->data == out->scale))) return GL_ERR_UNSUPPORTED;
+  const Place codes = {reinterpret_cast<uintptr_t>(out->data), gl_f8_data_bytes(out)};
+  const Place scale = {reinterpret_cast<uintptr_t>(out->scale), gl_f8_scale_bytes(out)};
+  if (meet(codes, scale)) return GL_ERR_UNSUPPORTED;
+  for (const Place& to : {codes, scale})
+    if (meet(place_of(x), to) || (residual && meet(place_of(residual), to)) || weight_or_sum_clash(weight, sum, to)) return GL_ERR_UNSUPPORTED;
   p.out = out->data;
   p.scale = static_cast<uint8_t*>(out->scale);
   return run_norm(x, residual, p, kOutF8, stream);

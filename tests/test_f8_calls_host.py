@@ -1,4 +1,5 @@
 """Calls on 8-bit operands, the norm and the rotation that are refused or hold on to nothing of their caller's, checked on the host."""
+import ctypes
 import sys
 
 import pytest
@@ -74,3 +75,57 @@ def test_a_prepared_call_keeps_to_its_own_stream(gl, monkeypatch):
         finally:
             sys.settrace(None)
         assert between[0] >= 5 and sorted(ran) == [raw] + [1000 + i for i in range(between[0])], (given, ran)
+
+
+# ---- places that operands and results share ----
+
+UNSUPPORTED = 7
+
+
+def _norm(gl, x, out, residual=None, total=None, weight=None):
+    """Status of a norm of (4, 64): operands as (type, address), an F8 result as a pair of addresses."""
+    r = ctypes.byref
+    at = lambda a, shape=(4, 64): None if a is None else r(gl._meta(shape, len(shape) - 1, a[0], a[1]))
+    args = (at(x), at(residual), at(weight, (64,)), 1e-5, at(total))
+    if out[0] in (gl.GL_F32, gl.GL_BF16):
+        return gl.LIB.gl_compute_norm_rms(*args, at(out), None)
+    q = gl._f8_meta((4, 64), 1)
+    q.data, q.scale = out
+    return gl.LIB.gl_compute_norm_rms_f8(*args, r(q), None)
+
+
+def test_a_norm_in_place_of_another_type_is_refused(gl):
+    """Rows lie at other distances in the two views, so a block would write over rows that another has not read."""
+    b, f, a = gl.GL_BF16, gl.GL_F32, 0x100000
+    away, far = (f, 0x800000), (f, 0x900000)
+    for x, out, more in (((b, a), (f, a), {}), ((f, a), (b, a), {}),                          # the result in x's place
+                         (away, (b, a), dict(residual=(f, a))), (away, (f, a), dict(residual=(b, a))),
+                         ((b, a), away, dict(residual=far, total=(f, a))),                    # the sum in x's place
+                         ((f, a), away, dict(residual=(b, 0x900000), total=(b, a)))):
+        assert _norm(gl, x, out, **more) == UNSUPPORTED, (x, out, more)
+
+
+def test_a_norm_beside_itself_is_refused(gl):
+    """A row further on, or half of one: neither the same place nor another."""
+    f, a, size, far = gl.GL_F32, 0x100000, 4 * 64 * 4, (gl.GL_F32, 0x900000)
+    for d in (16, 256, size - 16, -16, -256, 16 - size):
+        assert _norm(gl, (f, a), (f, a + d)) == UNSUPPORTED, d
+        assert _norm(gl, far, (f, a + d), residual=(f, a)) == UNSUPPORTED, d
+        assert _norm(gl, far, (f, 0x800000), residual=(f, a), total=(f, a + d)) == UNSUPPORTED, d
+        assert _norm(gl, (f, a), (f, 0x800000), residual=far, total=(f, a + d)) == UNSUPPORTED, d
+        assert _norm(gl, (f, 0x700000), (f, a + d), residual=far, total=(f, a)) == UNSUPPORTED, d
+    weight = (f, a + 128)                                                                     # 256 bytes
+    for out in (a, a + 368, a - size + 144):
+        assert _norm(gl, far, (f, out), weight=weight) == UNSUPPORTED
+        assert _norm(gl, far, (f, 0x800000), residual=(f, out), total=(f, out), weight=weight) == UNSUPPORTED
+
+
+def test_a_norm_into_f8_over_its_operands_is_refused(gl):
+    """(4, 64): 256 bytes of codes, 512 of scales."""
+    f, b, a, far = gl.GL_F32, gl.GL_BF16, 0x100000, (gl.GL_F32, 0x900000)
+    for codes, scales in ((a, 0x800000), (0x800000, a), (a + 512 - 16, 0x800000), (0x800000, a - 512 + 16)):
+        assert _norm(gl, (b, a), (codes, scales)) == UNSUPPORTED
+        assert _norm(gl, far, (codes, scales), residual=(b, a)) == UNSUPPORTED
+        assert _norm(gl, far, (codes, scales), residual=(b, 0xA00000), total=(b, a)) == UNSUPPORTED
+    assert _norm(gl, far, (a, 0x800000), weight=(f, a)) == UNSUPPORTED and _norm(gl, far, (0x800000, a), weight=(f, a)) == UNSUPPORTED
+    assert _norm(gl, far, (a, a + 240)) == UNSUPPORTED and _norm(gl, far, (a + 496, a)) == UNSUPPORTED
