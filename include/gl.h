@@ -442,7 +442,7 @@ GL_API int gl_rotary_plan(int32_t pairs, double base, const double* freq, const 
 /* compute rotate of x ((B, T, heads),(head_dim)), GL_F32 or GL_BF16: in every head the pair (u, v) of pair i of token (b, t) becomes
  * (u cos - v sin, u sin + v cos) of its angle at positions[axis[i]][b][t]; values behind the pairs are copied.  `positions`:
  * int32 in DEVICE memory, [axes][B][T], any value.  out: shape and type of x; it may be x itself (same data and
- * pitch), otherwise the two do not overlap.  token_pitch, out_pitch: elements between successive tokens (0: dense), at least
+ * pitch), otherwise no token of one shares a value with a token of the other (GL_ERR_UNSUPPORTED; either may lie in the other's gaps).  token_pitch, out_pitch: elements between successive tokens (0: dense), at least
  * heads * head_dim.  GL_ROTATE_BACK in flags turns by the negative angles: the inverse, and the gradient.
  * Angles are exact to position * 2^-65 turns and 2^-24 relative, cosines and products fp32.  Limits (else GL_ERR_UNSUPPORTED):
  * B * T <= 2^31, heads * head_dim <= 2^24. */

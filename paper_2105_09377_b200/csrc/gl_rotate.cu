@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <numeric>
 
 #include "gl_f8.cuh"
 #include "gl_internal.h"
@@ -206,6 +207,24 @@ __global__ void __launch_bounds__(kRotThreads) rotate_pairs(const __grid_constan
   }
 }
 
+// Whether a token of the operand, `width` elements at i * pitch, and one of the result, at `from` + j * out_pitch, share an element; n
+// tokens each.  Views of one projection may lie in each other's gaps (queries turned into where keys were).
+bool tokens_meet(int64_t from, int64_t n, int64_t pitch, int64_t out_pitch, int64_t width) {
+  typedef __int128 wide;
+  const wide end = static_cast<wide>(n - 1) * pitch + width;          // of the operand
+  if (from >= end || from + static_cast<wide>(n - 1) * out_pitch + width <= 0) return false;
+  // the result's first token that ends behind the operand's beginning; the element before that end, counted in operand's tokens, is
+  // less than two widths into one if and only if the two tokens meet
+  const int64_t first = from + width > 0 ? 0 : -(from + width) / out_pitch + 1;
+  const int64_t period = pitch / std::gcd(pitch, out_pitch);          // (tokens of the result after which the remainders repeat)
+  for (int64_t j = first; j < n && j < first + period; ++j) {
+    const wide last = from + static_cast<wide>(j) * out_pitch + width - 1;
+    if (last - width + 1 >= end) return false;
+    if (static_cast<int64_t>(last % pitch) < 2 * width - 1) return true;
+  }
+  return false;
+}
+
 template <bool F32>
 void (*rotate_kernel(int w))(RotateParams) {
   switch (w) {
@@ -282,6 +301,8 @@ int gl_compute_rotate(const gl_ap* x, int64_t token_pitch, const gl_rotary* plan
   if (token_pitch < heads * d || out_pitch < heads * d) return GL_ERR_SHAPE;
   if (token_pitch > (int64_t{1} << 40) || out_pitch > (int64_t{1} << 40)) return GL_ERR_UNSUPPORTED;
   if (out->data == x->data && out_pitch != token_pitch) return GL_ERR_SHAPE;   // in place is the same view
+  const int64_t apart = (reinterpret_cast<intptr_t>(out->data) - reinterpret_cast<intptr_t>(x->data)) / (x->dtype == GL_F32 ? 4 : 2);
+  if (out->data != x->data && tokens_meet(apart, b * t, token_pitch, out_pitch, heads * d)) return GL_ERR_UNSUPPORTED;
   RotateParams p;
   std::memset(&p, 0, sizeof(p));
   p.x = x->data;

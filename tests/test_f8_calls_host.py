@@ -1,5 +1,6 @@
 """Calls on 8-bit operands, the norm and the rotation that are refused or hold on to nothing of their caller's, checked on the host."""
 import ctypes
+import random
 import sys
 
 import pytest
@@ -129,3 +130,39 @@ def test_a_norm_into_f8_over_its_operands_is_refused(gl):
         assert _norm(gl, far, (codes, scales), residual=(b, 0xA00000), total=(b, a)) == UNSUPPORTED
     assert _norm(gl, far, (a, 0x800000), weight=(f, a)) == UNSUPPORTED and _norm(gl, far, (0x800000, a), weight=(f, a)) == UNSUPPORTED
     assert _norm(gl, far, (a, a + 240)) == UNSUPPORTED and _norm(gl, far, (a + 496, a)) == UNSUPPORTED
+
+
+def _rotate(gl, n, width, x, px, out, po):
+    """Status of a rotation of n tokens of `width` bf16 values, the operand's from element x on, the result's from `out` on."""
+    r, base = ctypes.byref, 0x10000000
+    at = lambda where: r(gl._meta((1, n, 1, width), 3, gl.GL_BF16, base + 2 * where))
+    return gl.LIB.gl_compute_rotate(at(x), px, r(gl.rotary_plan(4)), 0x1000, at(out), po, 0, None)
+
+
+def test_a_rotation_beside_itself_is_refused(gl):
+    """Views of one projection that share values without being one view: blocks would read what others have turned."""
+    heads = 64
+    for d in (8, heads, 2 * heads, 5 * heads, 8 * heads - 8, 10 * heads + 8, 12 * heads, 9 * 12 * heads, -heads, -12 * heads, 4 * heads - 12 * heads - 8):
+        # eight heads of twelve, turned into a view d elements on: the next head, the next token, ..
+        assert _rotate(gl, 19, 8 * heads, 4096, 12 * heads, 4096 + d, 12 * heads) == UNSUPPORTED, d
+    assert _rotate(gl, 1, 64, 0, 64, 56, 64) == UNSUPPORTED and _rotate(gl, 1, 64, 56, 64, 0, 64) == UNSUPPORTED
+    # other distances: the last token of one, or one in the middle, meets a token of the other
+    assert _rotate(gl, 10, 64, 0, 64, 568, 200) == UNSUPPORTED and _rotate(gl, 10, 64, 1800, 64, 0, 200) == UNSUPPORTED
+    assert _rotate(gl, 12, 64, 0, 200, 64, 208) == UNSUPPORTED and _rotate(gl, 3, 8, 8, 1000, 0, 504) == UNSUPPORTED
+
+
+def test_which_tokens_meet(gl):
+    """The refusal is exact: against every pair of tokens.  (No call that is not refused reaches a GPU here.)"""
+    rng, seen = random.Random(5), {False: 0, True: 0}
+    for _ in range(4000):
+        n, width = rng.choice([1, 2, 3, 7, 20]), rng.choice([8, 16, 24])
+        px, po = (width + rng.choice([0, 8, 16, 24, 40, 64, 200]) for _ in range(2))
+        if rng.random() < 0.5:
+            po = px
+        x, out = 8 * rng.randrange(80), 8 * rng.randrange(80)
+        if x == out:
+            continue
+        meet = any(x + i * px < out + j * po + width and out + j * po < x + i * px + width for i in range(n) for j in range(n))
+        assert (_rotate(gl, n, width, x, px, out, po) == UNSUPPORTED) == meet, (n, width, x, px, out, po)
+        seen[meet] += 1
+    assert min(seen.values()) > 500
