@@ -45,8 +45,8 @@ inline int check_f8_meta(const gl_f8* a, F8View* v) {
   v->nb = (v->K + kF8Block - 1) / kF8Block;
   v->kt = (v->nb + 3) / 4;
   v->rt = (v->rows + 127) / 128;
-  // item indices are 32-bit in the kernels, blocks of the whole operand too; a tile of the product has to be done well before its
-  // bounded waits give up (2^28 values of an item take half a second)
+  // item indices are 32-bit in the kernels, blocks of the whole operand too; 2^28 values of an item are 2^12 stretches of a product,
+  // which fp32 adds up to 2^-12
   if (v->rows > INT32_MAX - 256 || v->K > (int64_t{1} << 28) || v->rows * (v->nb + 1) > INT32_MAX) return GL_ERR_UNSUPPORTED;
   return GL_OK;
 }
