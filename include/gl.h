@@ -437,7 +437,8 @@ typedef struct {
 } gl_rotary;
 
 /* Host only.  Pair i turns by freq[i] radians per position, base^(-i / pairs) where freq is NULL (1 <= base <= 1e30); sections[a]
- * consecutive pairs belong to axis a (they add up to `pairs`; NULL with one axis). */
+ * consecutive pairs belong to axis a (they add up to `pairs`; NULL with one axis).  A step is off by half a unit and |freq[i]| * 2^-62
+ * units at most, by two thirds of a unit where a base gives the frequencies. */
 GL_API int gl_rotary_plan(int32_t pairs, double base, const double* freq, const int32_t* sections, int32_t axes,
                           int32_t adjacent, gl_rotary* out);
 
@@ -446,7 +447,7 @@ GL_API int gl_rotary_plan(int32_t pairs, double base, const double* freq, const 
  * int32 in DEVICE memory, [axes][B][T], any value.  out: shape and type of x; it may be x itself (same data and
  * pitch), otherwise no token of one shares a value with a token of the other (GL_ERR_UNSUPPORTED; either may lie in the other's gaps).  token_pitch, out_pitch: elements between successive tokens (0: dense), at least
  * heads * head_dim.  GL_ROTATE_BACK in flags turns by the negative angles: the inverse, and the gradient.
- * Angles are exact to position * 2^-65 turns and 2^-24 relative, cosines and products fp32.  Limits (else GL_ERR_UNSUPPORTED):
+ * Angles are step[i] * position, exact but for a last rounding of 2^-24 of themselves, cosines and products fp32.  Limits (else GL_ERR_UNSUPPORTED):
  * B * T <= 2^31, heads * head_dim <= 2^24. */
 GL_API int gl_compute_rotate(const gl_ap* x, int64_t token_pitch, const gl_rotary* plan, const int32_t* positions, gl_ap* out,
                              int64_t out_pitch, uint32_t flags, void* stream);

@@ -18,7 +18,7 @@ using namespace gl;
 namespace {
 
 // Angles are 64-bit fractions of a turn: step (2^64 times the turns per position) times position, modulo 2^64.  Whole turns fall
-// out of the integer product by themselves and the rest is exact to position * 2^-65 turns, where an fp32 product of position and
+// out of the integer product by themselves and the rest is as exact as the step, to half a unit or little more, where an fp32 product of position and
 // frequency is off by a sixteenth of a radian at a million tokens.
 //
 // A block takes a few tokens: cosines and sines of its tokens once into shared memory, then every thread takes one group of W
@@ -225,6 +225,24 @@ bool tokens_meet(int64_t from, int64_t n, int64_t pitch, int64_t out_pitch, int6
   return false;
 }
 
+// The whole number v, modulo 2^64.
+uint64_t modulo64(long double v) { return v < 0 ? static_cast<uint64_t>(static_cast<int64_t>(v)) : static_cast<uint64_t>(v); }
+
+// 2^64 f / (2 pi) to the nearest whole number, modulo 2^64.  The quotient is taken to twice a long double's 64 bits, as its whole
+// turns would take the place of the bits that count; 2 pi = turn + rest.
+uint64_t step_of(long double f) {
+  if (f < 0) return 0 - step_of(-f);                            // (a fraction below one keeps its last bits, one above minus one does not)
+  const long double turn = 6.283185307179586476925286766559005768L, rest = -1.00331152253366640471146541606615140276673e-19L;
+  long double first = f / turn;
+  long double second = (std::fma(-first, turn, f) - first * rest) / turn;
+  first -= std::floor(first);                                   // whole turns per position change nothing
+  if (std::abs(second) >= 0.25L) second -= std::floor(second);  // (of frequencies beyond 2^60)
+  first *= 18446744073709551616.0L;
+  second *= 18446744073709551616.0L;
+  const long double a = std::floor(first), b = std::floor(second);
+  return modulo64(a) + modulo64(b) + modulo64(std::floor((first - a) + (second - b) + 0.5L));
+}
+
 template <bool F32>
 void (*rotate_kernel(int w))(RotateParams) {
   switch (w) {
@@ -261,18 +279,13 @@ int gl_rotary_plan(int32_t pairs, double base, const double* freq, const int32_t
   out->pairs = pairs;
   out->axes = axes;
   out->adjacent = adjacent;
-  const long double turn = 6.283185307179586476925286766559005768L;
   int axis = 0, left = sections ? sections[0] : pairs;
   for (int i = 0; i < pairs; ++i) {
     while (left == 0) left = sections[++axis];
     out->axis[i] = static_cast<uint8_t>(axis);
     --left;
-    const long double f = freq ? static_cast<long double>(freq[i])
-                               : std::pow(static_cast<long double>(base), -static_cast<long double>(i) / pairs);
-    long double part = f / turn;
-    part -= std::floor(part);                                  // whole turns per position change nothing
-    const long double scaled = std::floor(part * 18446744073709551616.0L + 0.5L);
-    out->step[i] = scaled >= 18446744073709551616.0L ? 0 : static_cast<uint64_t>(scaled);
+    out->step[i] = step_of(freq ? static_cast<long double>(freq[i])
+                                : std::pow(static_cast<long double>(base), -static_cast<long double>(i) / pairs));
   }
   return GL_OK;
 }

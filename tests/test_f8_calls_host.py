@@ -2,6 +2,8 @@
 import ctypes
 import random
 import sys
+from decimal import Decimal, getcontext
+from fractions import Fraction
 
 import pytest
 import torch
@@ -166,3 +168,48 @@ def test_which_tokens_meet(gl):
         assert (_rotate(gl, n, width, x, px, out, po) == UNSUPPORTED) == meet, (n, width, x, px, out, po)
         seen[meet] += 1
     assert min(seen.values()) > 500
+
+
+# ---- the rotary plan ----
+
+def _two_pi():
+    """2 pi to 400 bits: 16 atan(1/5) - 4 atan(1/239), times two."""
+    one = 1 << 440
+
+    def atan_inverse(n):
+        term, total, k = one // n, 0, 1
+        while term:
+            total += term // k if k % 4 == 1 else -(term // k)
+            term, k = term // (n * n), k + 2
+        return total
+
+    return Fraction(2 * (16 * atan_inverse(5) - 4 * atan_inverse(239)), one)
+
+
+def _off(step, turns):
+    """Distance of a step from 2^64 turns, in units, whole turns aside."""
+    d = (Fraction(step) - turns * 2 ** 64) % 2 ** 64
+    return float(min(d, 2 ** 64 - d))
+
+
+def test_steps_of_own_frequencies(gl):
+    """Off by half a unit of 2^-64 turns and |freq| 2^-62 units, as gl.h has it, whatever whole turns a position makes."""
+    freqs = [20.0, 7.0, 1e6, -1e6, 1e12, 1e15 + 0.1, -3e-5, 1e-12, 0.0, 2.0 ** 40 + 0.37, 6.283185307179586, -6.283185307179587, 1.0, -1.0,
+             2.0 ** -70] + [(-1) ** i * 1.37 ** (i - 30) for i in range(100)]
+    plan, two_pi = gl.rotary_plan(len(freqs), freq=freqs), _two_pi()
+    for i, f in enumerate(freqs):
+        assert _off(plan.step[i], Fraction(f) / two_pi) <= 0.5 + abs(f) * 2.0 ** -62 + 1e-9, f
+    huge = gl.rotary_plan(3, freq=[1e300, -1e300, 2.0 ** 66])     # (finite: some angle, the same every time)
+    assert list(huge.step[:3]) == list(gl.rotary_plan(3, freq=[1e300, -1e300, 2.0 ** 66]).step[:3])
+
+
+def test_steps_of_a_base(gl):
+    """Off by two thirds of a unit at most: half a unit of the step and what the power is off by."""
+    getcontext().prec = 60
+    two_pi = _two_pi()
+    two_pi = Decimal(two_pi.numerator) / Decimal(two_pi.denominator)
+    for pairs, base in ((128, 10000.0), (64, 500000.0), (128, 1e30), (31, 1.5)):
+        plan = gl.rotary_plan(pairs, base)
+        for i in range(pairs):
+            want = Decimal(base) ** (Decimal(-i) / Decimal(pairs)) / two_pi * 2 ** 64
+            assert abs(Decimal(plan.step[i]) - want) <= Decimal(2) / 3, (pairs, base, i)
