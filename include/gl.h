@@ -414,7 +414,8 @@ GL_API size_t gl_dense_f8_workspace(const gl_ap* a0, const gl_f8* a1);
  * x ((a..),(c..)) with c not empty, GL_F32 or GL_BF16; `residual` (NULL: none) and `sum` (NULL: not wanted; only with a
  * residual) of the same shape and of one type, GL_F32 or GL_BF16, which may differ from x's; `weight` (NULL: ones)
  * ((),(c..)), GL_F32 or GL_BF16; eps >= 0 and finite.  out: the shape of x, GL_F32, GL_BF16 or F8.  The norm is that of the
- * unrounded h, in fp32 throughout; squares have to stay in fp32's range.  `sum` may be `residual` itself, or x where the
+ * unrounded h, in fp32 throughout (units of eight squares are added in 64 bits where a row is longer than a block holds); squares
+ * have to stay in fp32's range.  `sum` may be `residual` itself, or x where the
  * types agree, and `out` may be x or `residual`, unless that is `sum`, where the types agree; any other overlap of a result with
  * an operand or the other result is refused (GL_ERR_UNSUPPORTED).
  * Size limits as for F8.  Results repeat bit for bit; the F8 result is the GL_F32 result rounded as gl_f8_quantize rounds. */

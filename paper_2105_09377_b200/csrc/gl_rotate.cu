@@ -18,13 +18,13 @@ using namespace gl;
 namespace {
 
 // Angles are 64-bit fractions of a turn: step (2^64 times the turns per position) times position, modulo 2^64.  Whole turns fall
-// out of the integer product by themselves and the rest is as exact as the step, to half a unit or little more, where an fp32 product of position and
-// frequency is off by a sixteenth of a radian at a million tokens.
+// out of the integer product by themselves and the rest is as exact as the step, which is off by half a unit or little more; an fp32
+// product of position and frequency is off by a sixteenth of a radian at a million tokens.
 //
 // A block takes a few tokens: cosines and sines of its tokens once into shared memory, then every thread takes one group of W
 // pairs, 2W values, of head after head, kRotRows of them requested before the first is used (the first ones before the angles
 // are computed).  Bound by HBM where there are heads enough to hide the angles: 8198 tokens x 40 heads x 128 bf16 30.4 us, 5.5 TB/s
-// (two heads in flight 37 us), fp32 51.7 us, 6.5 TB/s; one head of 128 at 8192 tokens 5.7 us, 64 tokens x 40 heads 2.3 us.
+// (two heads in flight 37 us), fp32 51.7 us, 6.5 TB/s; one head of 128 at 8192 tokens 5.4 us, 64 tokens x 40 heads 2.2 us.
 constexpr int kRotThreads = 256;
 constexpr int kRotRows = 4;           // heads of a thread in flight
 constexpr int kRotAngles = 512;       // angles of a block of several tokens
@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(kRotThreads) rotate_pairs(const __grid_constan
   char* out = static_cast<char*>(p.out) + token0 * p.out_pitch * kEs;
   float* sines = trig + p.per_block * p.pairs;
   // Neighbouring lanes ask for different pairs: through the cache of data, not that of constants, which serves one address at a
-  // time (8192 tokens of one head of 64 pairs: 11.5 -> 5.8 us).
+  // time (8192 tokens of one head of 64 pairs: 11.5 -> 5.4 us).
   const gl_rotary* plan = &p.plan;
   asm volatile("" : "+l"(plan));
   uint32_t first_row, lane;
