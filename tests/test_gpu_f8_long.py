@@ -1,4 +1,4 @@
-"""Long rows: sums of squares of up to 2^28 values, against the 64-bit checker and exact values."""
+"""Long rows: sums of squares and products of up to 2^28 values, against exact values."""
 import numpy as np
 import pytest
 import torch
@@ -23,7 +23,7 @@ NORM = (44 / 2 + 4 + 1 + 2) * U
 
 
 @pytest.mark.parametrize("value", [1.39, 1.0, 0.0123, 7.77, 1.0009765625])
-@pytest.mark.parametrize("k", [1 << 23, (1 << 25) + 4099])
+@pytest.mark.parametrize("k", [1 << 23, (1 << 25) + 4099, 1 << 28])
 def test_norm_of_long_constant_rows(gl, k, value):
     ap = gl.AccessPattern
     x = torch.full((2, k), value, device="cuda")
@@ -93,6 +93,13 @@ def test_long_whole_numbers_are_exact(gl, m, o, k):
     assert torch.equal(out.double(), want)
     relu = gl.gl_cartesian_dot_f8(qa, qb, flags=gl.GL_OUT_BF16 | gl.GL_EPILOGUE_RELU).tensor
     assert torch.equal(relu, want.clamp_min(0).to(BF)) and gl.gl_poll_device_status() == 0
+
+
+@pytest.mark.parametrize("m,o", [(1, 1), (70, 2)])
+def test_the_longest_products(gl, m, o):
+    """2^28 values of an item, 4096 stretches; 2^24 of seventy."""
+    k = 1 << (28 if m == 1 else 24)
+    test_small_products_behind_a_large_one(gl, m, o, k)
 
 
 def test_long_products_repeat(gl):
