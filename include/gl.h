@@ -415,8 +415,8 @@ GL_API size_t gl_dense_f8_workspace(const gl_ap* a0, const gl_f8* a1);
  * residual) of the same shape and of one type, GL_F32 or GL_BF16, which may differ from x's; `weight` (NULL: ones)
  * ((),(c..)), GL_F32 or GL_BF16; eps >= 0 and finite.  out: the shape of x, GL_F32, GL_BF16 or F8.  The norm is that of the
  * unrounded h, in fp32 throughout (units of eight squares are added in 64 bits where a row is longer than a block holds); squares
- * have to stay in fp32's range.  `sum` may be `residual` itself, or x where the
- * types agree, and `out` may be x or `residual`, unless that is `sum`, where the types agree; any other overlap of a result with
+ * have to stay in fp32's range.  `sum` may be `residual` itself, or x where the types agree, and `out` may be x or `residual`,
+ * unless that is `sum`, where the types agree; any other overlap of a result with
  * an operand or the other result is refused (GL_ERR_UNSUPPORTED).
  * Size limits as for F8.  Results repeat bit for bit; the F8 result is the GL_F32 result rounded as gl_f8_quantize rounds. */
 GL_API int gl_compute_norm_rms(const gl_ap* x, const gl_ap* residual, const gl_ap* weight, float eps, gl_ap* sum, gl_ap* out,
@@ -446,10 +446,11 @@ GL_API int gl_rotary_plan(int32_t pairs, double base, const double* freq, const 
 /* compute rotate of x ((B, T, heads),(head_dim)), GL_F32 or GL_BF16: in every head the pair (u, v) of pair i of token (b, t) becomes
  * (u cos - v sin, u sin + v cos) of its angle at positions[axis[i]][b][t]; values behind the pairs are copied.  `positions`:
  * int32 in DEVICE memory, [axes][B][T], any value.  out: shape and type of x; it may be x itself (same data and
- * pitch), otherwise no token of one shares a value with a token of the other (GL_ERR_UNSUPPORTED; either may lie in the other's gaps).  token_pitch, out_pitch: elements between successive tokens (0: dense), at least
- * heads * head_dim.  GL_ROTATE_BACK in flags turns by the negative angles: the inverse, and the gradient.
- * Angles are step[i] * position, exact but for a last rounding of 2^-24 of themselves, cosines and products fp32.  Limits (else GL_ERR_UNSUPPORTED):
- * B * T <= 2^31, heads * head_dim <= 2^24. */
+ * pitch), otherwise no token of one shares a value with a token of the other (GL_ERR_UNSUPPORTED; either may lie in the other's
+ * gaps).  token_pitch, out_pitch: elements between successive tokens (0: dense), at least heads * head_dim.  GL_ROTATE_BACK in
+ * flags turns by the negative angles: the inverse, and the gradient.
+ * Angles are step[i] * position, exact but for a last rounding of 2^-24 of themselves, cosines and products fp32.  Limits (else
+ * GL_ERR_UNSUPPORTED): B * T <= 2^31, heads * head_dim <= 2^24. */
 GL_API int gl_compute_rotate(const gl_ap* x, int64_t token_pitch, const gl_rotary* plan, const int32_t* positions, gl_ap* out,
                              int64_t out_pitch, uint32_t flags, void* stream);
 
